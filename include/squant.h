@@ -62,8 +62,8 @@ typedef enum {
   SQUANT_ERR_NULL = 1,      /* a required pointer is NULL */
   SQUANT_ERR_SHAPE = 2,     /* a dimension is <= 0, or the sizes overflow */
   SQUANT_ERR_BITS = 3,      /* bits outside [2, 8] */
-  SQUANT_ERR_MODE = 4,      /* unknown mode */
-  SQUANT_ERR_WORKSPACE = 5, /* a workspace size without a workspace pointer */
+  SQUANT_ERR_MODE = 4,      /* unknown mode, activation or kept form, or a pair of them that does not go together */
+  SQUANT_ERR_WORKSPACE = 5, /* a workspace size without a workspace pointer, or too small or misaligned a workspace */
   SQUANT_ERR_DEVICE = 6,    /* a HIP call failed */
   SQUANT_ERR_UNSUPPORTED = 7, /* not returned by this version: every channel within the shape limits is taken */
   SQUANT_ERR_FORMAT = 8     /* unknown weight or output type, or a buffer misaligned for its element type */
@@ -202,6 +202,92 @@ int squant_quantize_network(const squant_layer_t* h_layers, int32_t n_layers, in
  * about 160 K elements or off 16-byte alignment beyond 64 K) go through a streaming kernel
  * that walks the weights several times: correct for any shape, a fraction of the speed. */
 int64_t squant_max_channel_elems(int32_t kh, int32_t kw);
+
+/* ---------------------------------------------------------------------------
+ * Operators on quantised layers: products with the solver's codes, their gradients, and the
+ * cross entropy over a vocabulary whose output embedding is codes.  Nothing dequantises to memory.
+ *
+ * Element type: the activations' type, binary32, binary16 or bfloat16 (squant_wtype_t), shared by all
+ * activation buffers of a call (x, bias, residual, y, dy, dx, dbias).  Codes times activations are
+ * multiplied exactly (binary32 activations to 22 bits) and added in binary32; every output is rounded
+ * once.  Rows may be any distance apart (ld*, in elements, at least the row's length); activation
+ * buffers need the alignment of their element type, codes none.
+ *
+ * d_workspace: the *_workspace_bytes call's amount, 256-byte aligned, not shared with a call that may
+ * run at the same time; it holds nothing between calls.  rows = 0 is a no-op, apart from d_dbias, which
+ * becomes 0.  The calls launch kernels only and may be captured into a HIP graph.  Infinities and NaN in
+ * the activations act as IEEE arithmetic has it (an infinity times a code of 0 is NaN, and a row that
+ * holds one may be NaN where exact arithmetic has an infinity). */
+
+/* A quantised layer: codes as squant_quantize_ex writes them for SQUANT_OUT_INT8 or SQUANT_OUT_INT4,
+ * rows of cin codes (cin * kh * kw of a convolution's unfolded input). */
+typedef struct {
+  const void* codes;      /* device */
+  const float* scales;    /* device, cout binary32 */
+  int32_t cout, cin;
+  squant_output_t format; /* SQUANT_OUT_INT8 or SQUANT_OUT_INT4 */
+} squant_codes_t;
+
+typedef enum {
+  SQUANT_ACT_NONE = 0,
+  SQUANT_ACT_RELU = 1,
+  SQUANT_ACT_GELU = 2, /* z * Phi(z), Phi the normal distribution's */
+  SQUANT_ACT_SILU = 3  /* z / (1 + exp(-z)) */
+} squant_activation_t;
+
+/* How the pre-activation z is kept for the backward pass.
+ *   INT8  [rows][cout] int8 and [rows][ceil(cout / 64)] binary32 scales: 64 columns of a row share
+ *         scale = max|z| / 127 (1 where all are 0), code = round-half-even(z * (127 / max|z|)).  A NaN
+ *         or an infinity among them makes the scale one.
+ *   FULL  [rows][cout] of the element type. */
+typedef enum {
+  SQUANT_KEEP_NONE = 0,
+  SQUANT_KEEP_INT8 = 1,
+  SQUANT_KEEP_FULL = 2
+} squant_keep_t;
+
+/* y[m][n] = act(z[m][n]) + residual[m][n],  z[m][n] = scales[n] * sum_k x[m][k] * codes[n][k] + bias[n].
+ * d_bias [cout], d_residual [rows][cout] (ldr) and, with SQUANT_KEEP_NONE, d_kept may be NULL;
+ * d_kept_scales only with SQUANT_KEEP_INT8.  d_y may be d_residual (ldy == ldr). */
+size_t squant_linear_workspace_bytes(squant_wtype_t type, int64_t rows, const squant_codes_t* h_w,
+                                     squant_keep_t keep);
+int squant_linear(const void* d_x, int64_t ldx, squant_wtype_t type, int64_t rows,
+                  const squant_codes_t* h_w, const void* d_bias, squant_activation_t act,
+                  const void* d_residual, int64_t ldr, void* d_y, int64_t ldy, squant_keep_t keep,
+                  void* d_kept, float* d_kept_scales, void* d_workspace, size_t workspace_bytes,
+                  void* stream);
+
+/* Gradients of squant_linear, codes and scales held fixed (the residual's is dy itself):
+ * dz = dy * act'(z), z as kept;  dx[m][k] = sum_n dz[m][n] * scales[n] * codes[n][k];
+ * dbias[n] = sum_m dz[m][n].  d_dbias may be NULL.  With SQUANT_ACT_NONE keep is SQUANT_KEEP_NONE, with
+ * the others it is not (SQUANT_ERR_MODE).  dz * scale is held in binary16 with an exponent for each row
+ * (12 bits; binary32: 22). */
+size_t squant_linear_backward_workspace_bytes(squant_wtype_t type, int64_t rows, const squant_codes_t* h_w);
+int squant_linear_backward(const void* d_dy, int64_t lddy, squant_wtype_t type, int64_t rows,
+                           const squant_codes_t* h_w, squant_activation_t act, squant_keep_t keep,
+                           const void* d_kept, const float* d_kept_scales, void* d_dx, int64_t lddx,
+                           void* d_dbias, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* Softmax cross entropy of hidden states h [rows][cin] against a vocabulary of cout entries, without the
+ * logits in memory:  l[t][v] = scales[v] * sum_d h[t][d] * codes[v][d],  lse[t] = log sum_v exp l[t][v],
+ * loss[t] = lse[t] - l[t][label[t]];  0 where the label is ignore_index, NaN where it is neither that
+ * nor in [0, cout).  loss and lse are binary32. */
+size_t squant_cross_entropy_workspace_bytes(squant_wtype_t type, int64_t rows, const squant_codes_t* h_w);
+int squant_cross_entropy(const void* d_h, int64_t ldh, squant_wtype_t type, int64_t rows,
+                         const squant_codes_t* h_w, const int64_t* d_labels, int64_t ignore_index,
+                         float* d_loss, float* d_lse, void* d_workspace, size_t workspace_bytes,
+                         void* stream);
+
+/* dh[t][d] = dloss[t] * (sum_v p[t][v] * scales[v] * codes[v][d] - scales[y] * codes[y][d]) with
+ * p = exp(l - lse) and y the label (lse of the call above; its own gradient is not taken); 0 where the
+ * label is ignore_index.  The vocabulary is walked in pieces whose probabilities fit the workspace. */
+size_t squant_cross_entropy_backward_workspace_bytes(squant_wtype_t type, int64_t rows,
+                                                     const squant_codes_t* h_w);
+int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t type, int64_t rows,
+                                  const squant_codes_t* h_w, const int64_t* d_labels,
+                                  int64_t ignore_index, const float* d_lse, const float* d_dloss,
+                                  void* d_dh, int64_t lddh, void* d_workspace, size_t workspace_bytes,
+                                  void* stream);
 
 const char* squant_status_string(int status);
 int squant_version(void);

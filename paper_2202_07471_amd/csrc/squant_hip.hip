@@ -626,8 +626,8 @@ const char* squant_status_string(int status) {
     case SQUANT_ERR_NULL: return "null pointer";
     case SQUANT_ERR_SHAPE: return "bad shape";
     case SQUANT_ERR_BITS: return "bits must be in [2, 8]";
-    case SQUANT_ERR_MODE: return "unknown mode";
-    case SQUANT_ERR_WORKSPACE: return "workspace size given without a workspace";
+    case SQUANT_ERR_MODE: return "unknown mode, activation or kept form";
+    case SQUANT_ERR_WORKSPACE: return "workspace missing, too small or misaligned";
     case SQUANT_ERR_DEVICE: return "HIP call failed";
     case SQUANT_ERR_UNSUPPORTED: return "unsupported (not returned by this version)";
     case SQUANT_ERR_FORMAT: return "unknown weight or output type, or misaligned buffer";

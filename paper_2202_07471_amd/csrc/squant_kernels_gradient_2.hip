@@ -1,0 +1,14 @@
+// Gradients through codes, row operands of 2 planes.
+#include "squant_lin_kernels.h"
+#include "squant_product.h"
+
+namespace squant {
+namespace lin {
+
+product_t gradient_2(int format, int mt) {
+  return format == SQUANT_OUT_INT4 ? product_of<Half, 2, SQUANT_OUT_INT4, true>(mt)
+                                   : product_of<Half, 2, SQUANT_OUT_INT8, true>(mt);
+}
+
+}  // namespace lin
+}  // namespace squant

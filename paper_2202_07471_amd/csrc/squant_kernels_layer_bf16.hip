@@ -1,0 +1,14 @@
+// Products of bfloat16 rows with codes.
+#include "squant_lin_kernels.h"
+#include "squant_product.h"
+
+namespace squant {
+namespace lin {
+
+product_t layer_bf16(int format, int mt) {
+  return format == SQUANT_OUT_INT4 ? product_of<Brain, 1, SQUANT_OUT_INT4, false>(mt)
+                                   : product_of<Brain, 1, SQUANT_OUT_INT8, false>(mt);
+}
+
+}  // namespace lin
+}  // namespace squant

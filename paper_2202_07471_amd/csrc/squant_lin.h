@@ -1,0 +1,513 @@
+// Shared definitions of the operators that multiply by codes: arguments, the conversion of codes to
+// matrix-unit operands, activations, and what happens to a finished piece of a product.
+//
+// Every product is rows x codes: out[m, c] = sum_i a[m, i] w[i, c], with w[i, c] = code(c, i) for the layer
+// itself (the contraction runs along a code row) and code(i, c) for its gradient (it runs across them).
+// Codes are integers of at most 8 bits, exact in binary16 and in bfloat16, so the matrix units multiply
+// exactly and add in binary32; the scale of an output channel is applied once, to the finished sum (layer)
+// or to the row operand (gradient).  Row operands:
+//   bfloat16, binary16  as they are;
+//   binary32            two binary16 planes, hi + lo = x * 2^e with one e a row (its largest finite element
+//                       lands in [2^14, 2^15)): 22 bits of an element, or 2^-40 of the row's largest where
+//                       that is more.  bfloat16 would take three planes for the same;
+//   gradients           one plane like this for 16-bit outputs (2^-12 of an element, an eighth of what a
+//                       bfloat16 gradient would be off by), two for binary32.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "squant.h"
+
+namespace squant {
+namespace lin {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef __bf16 brain8 __attribute__((ext_vector_type(8)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
+
+constexpr int kLanes = 64;
+constexpr int kBlock = 64;   // contraction elements a step of the main loops takes
+constexpr int kTile = 64;    // columns of a wave, and the columns that share a scale of the kept pre-activation
+constexpr int kWide = 256;   // columns of a workgroup of `product`
+constexpr int kFewRows = 64; // rows up to which `few_rows` is taken
+
+enum Kind { kLinear = 0, kPartial = 1, kStats = 2, kProb = 3, kGrad = 4, kGradLoss = 5 };
+
+// What a finished piece of a product needs; one structure for every kind, so that a kernel's main loop
+// is compiled once.
+struct Finish {
+  int kind;
+  int act;
+  int keep;
+  int out_type;             // squant_wtype_t of `out` where the kernel does not fix it
+  float unit;               // the product's codes are held as multiples of this: 1, 2^-4, 2^-9
+  int64_t rows;
+  int32_t cols;             // of the output
+  const float* row_factor;  // 2^-e of each row, or null
+  const float* scales;
+  const void* bias;
+  const void* residual;
+  int64_t ldr;
+  void* out;
+  int64_t ldo;
+  void* kept;               // int8 [rows][cols] or out's type
+  float* kept_scales;       // [rows][ceil(cols / 64)]
+  float4v* partial;         // kPartial: [slice][row fragment][column fragment][lane]
+  // cross entropy
+  const int64_t* labels;
+  int64_t ignore;
+  float2* stats;            // [rows][chunks]: largest logit and sum of exponentials, base 2
+  float* label_logit;       // [rows]
+  const float* lse;
+  const float* dloss;
+  const float* prob_unit;   // [1]: 2^E that brings p * scale into binary16's range
+  _Float16* prob;           // [rows][planes][ld_prob]
+  int64_t ld_prob;          // elements between rows
+  int64_t prob_plane;       // elements between planes
+  int32_t first_col;        // vocabulary entry of column 0 of the piece
+  const uint8_t* codes;     // kGradLoss: the label's row
+  int64_t code_row;
+  int32_t format;
+};
+
+struct ProductArgs {
+  const void* a;       // row operand [rows][planes][blocks * 64], zero beyond the contraction's length
+  int64_t lda;         // elements between rows
+  int64_t plane;       // elements between planes
+  const uint8_t* w;    // codes; for a piece of the vocabulary, its first row
+  int64_t w_row;       // bytes of a code row
+  int32_t w_rows;      // code rows
+  int32_t w_cols;      // codes of a row
+  const uint8_t* w_end;
+  int32_t blocks;      // ceil(contraction / 64)
+  int32_t slices;      // the contraction is cut into this many
+  int32_t tiles_m, tiles_n;
+  int32_t slice0;      // first slice's index in `partial`
+  Finish f;
+};
+
+typedef void (*product_t)(ProductArgs);
+
+// ---------------------------------------------------------------------------
+// loads at any alignment
+// ---------------------------------------------------------------------------
+
+template <class V>
+__device__ __forceinline__ V load_any(const void* p) {
+  V v;
+  __builtin_memcpy(&v, p, sizeof(V));
+  return v;
+}
+template <class V>
+__device__ __forceinline__ void store_any(void* p, V v) {
+  __builtin_memcpy(p, &v, sizeof(V));
+}
+
+// ---------------------------------------------------------------------------
+// codes to operands
+// ---------------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t pick(uint32_t hi, uint32_t lo, uint32_t sel) {
+  return __builtin_amdgcn_perm(hi, lo, sel);
+}
+
+__device__ __forceinline__ half2v as_half2(uint32_t u) { return __builtin_bit_cast(half2v, u); }
+
+// u in the low byte of each half is the binary16 subnormal u * 2^-24: one fused multiply-add makes it
+// (u - zero) * 2^-9, exactly.
+__device__ __forceinline__ half2v centred(uint32_t u, float zero) {
+  const half2v up = {(_Float16)32768.0f, (_Float16)32768.0f};
+  const _Float16 z = (_Float16)(-zero / 512.0f);
+  return __builtin_elementwise_fma(as_half2(u), up, half2v{z, z});
+}
+
+struct Half {
+  typedef half8 frag;
+  static __device__ __forceinline__ float4v mma(frag w, frag x, float4v c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(w, x, c, 0, 0, 0);
+  }
+};
+struct Brain {
+  typedef brain8 frag;
+  static __device__ __forceinline__ float4v mma(frag w, frag x, float4v c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, c, 0, 0, 0);
+  }
+};
+
+template <int FMT> struct Codes;
+template <> struct Codes<SQUANT_OUT_INT8> {
+  typedef uint4v row16;                       // 16 codes of a row
+  static constexpr int kRow16 = 16;           // its bytes
+  typedef uint32_t col4;                      // 4 codes of a row, one for each of 4 columns
+  static __device__ __forceinline__ int64_t offset(int64_t i) { return i; }
+  static __device__ __forceinline__ int value(const uint8_t* row, int64_t i) { return (int8_t)row[i]; }
+};
+template <> struct Codes<SQUANT_OUT_INT4> {
+  typedef uint2v row16;
+  static constexpr int kRow16 = 8;
+  typedef uint16_t col4;
+  static __device__ __forceinline__ int64_t offset(int64_t i) { return i >> 1; }
+  static __device__ __forceinline__ int value(const uint8_t* row, int64_t i) {
+    return (int)((uint32_t)row[i >> 1] << ((i & 1) ? 24 : 28)) >> 28;
+  }
+};
+
+// The multiple that a converted code is held as; the finished sum is multiplied by its inverse.
+template <class F, int FMT> struct CodeUnit;
+template <> struct CodeUnit<Half, SQUANT_OUT_INT8> { static constexpr float inverse = 1.0f; };
+template <> struct CodeUnit<Brain, SQUANT_OUT_INT8> { static constexpr float inverse = 1.0f; };
+template <> struct CodeUnit<Half, SQUANT_OUT_INT4> { static constexpr float inverse = 512.0f; };
+template <> struct CodeUnit<Brain, SQUANT_OUT_INT4> { static constexpr float inverse = 16.0f; };
+constexpr float kColumnUnitInverse = 512.0f;  // of convert_columns
+
+// Codes 8h .. 8h+7 of 16 consecutive ones.  About 1 instruction a code for binary16, 1.5 otherwise.
+template <class F, int FMT>
+__device__ __forceinline__ typename F::frag convert(const typename Codes<FMT>::row16& r, int h) {
+  uint32_t o[4];
+  if constexpr (FMT == SQUANT_OUT_INT8 && __is_same(F, Half)) {
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+      const uint32_t u = r[2 * h + d] ^ 0x80808080u;  // code + 128, then 1024 + that by its bits
+      const half2v bias = {(_Float16)1152.0f, (_Float16)1152.0f};
+      o[2 * d] = __builtin_bit_cast(uint32_t, as_half2(pick(0x64646464u, u, 0x04010400u)) - bias);
+      o[2 * d + 1] = __builtin_bit_cast(uint32_t, as_half2(pick(0x64646464u, u, 0x04030402u)) - bias);
+    }
+  } else if constexpr (FMT == SQUANT_OUT_INT8) {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {  // an integer of 8 bits is exact in the upper half of its binary32
+      const uint32_t u = r[2 * h + (d >> 1)];
+      const int s = (d & 1) * 16;
+      const float a = (float)(int8_t)(u >> s), b = (float)(int8_t)(u >> (s + 8));
+      o[d] = pick(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+    }
+  } else if constexpr (__is_same(F, Half)) {
+    const uint32_t u = r[h] ^ 0x88888888u;  // code + 8
+    const uint32_t even = u & 0x0f0f0f0fu, odd = (u >> 4) & 0x0f0f0f0fu;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+      o[d] = __builtin_bit_cast(uint32_t, centred(pick(odd, even, 0x0c040c00u + 0x00010001u * (uint32_t)d), 8.0f));
+  } else {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {  // the instruction makes code / 16 of four bits
+      const float a = __builtin_amdgcn_cvt_off_f32_i4((int)(r[h] >> (8 * d)));
+      const float b = __builtin_amdgcn_cvt_off_f32_i4((int)(r[h] >> (8 * d + 4)));
+      o[d] = pick(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+    }
+  }
+  const uint4v v = {o[0], o[1], o[2], o[3]};
+  return __builtin_bit_cast(typename F::frag, v);
+}
+
+// Column j of 8 code rows of 4 columns each, as multiples of 2^-9.
+template <int FMT>
+__device__ __forceinline__ half8 convert_columns(const typename Codes<FMT>::col4* r, int j) {
+  uint32_t o[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    if constexpr (FMT == SQUANT_OUT_INT8) {
+      const uint32_t a = r[2 * d] ^ 0x80808080u, b = r[2 * d + 1] ^ 0x80808080u;
+      o[d] = __builtin_bit_cast(uint32_t, centred(pick(b, a, 0x0c040c00u + 0x00010001u * (uint32_t)j), 128.0f));
+    } else {
+      const uint32_t u = ((uint32_t)r[2 * d] | (uint32_t)r[2 * d + 1] << 16) ^ 0x88888888u;
+      o[d] = __builtin_bit_cast(uint32_t, centred((u >> (4 * j)) & 0x000f000fu, 8.0f));
+    }
+  }
+  const uint4v v = {o[0], o[1], o[2], o[3]};
+  return __builtin_bit_cast(half8, v);
+}
+
+// sizeof(V) bytes from p on, where `end` ends the buffer.  Past a row's end they are the next row's, which the
+// callers multiply by zero or do not store; past the buffer's end nothing is read, and the value's upper bytes are
+// zeros.  `bytes` is the whole buffer's size: one below sizeof(V) is read byte by byte.
+template <class V> struct Shifted { typedef V type; };
+template <> struct Shifted<uint4v> { typedef __uint128_t type; };
+template <> struct Shifted<uint2v> { typedef uint64_t type; };
+template <class V>
+__device__ __forceinline__ V load_before(const uint8_t* p, const uint8_t* end, int64_t bytes) {
+  typedef typename Shifted<V>::type U;
+  constexpr int n = (int)sizeof(V);
+  if (bytes < n) {
+    U u = 0;
+#pragma unroll 1
+    for (int i = 0; i < n; ++i)
+      if (p + i < end) u |= (U)p[i] << (8 * i);
+    return __builtin_bit_cast(V, u);
+  }
+  const int64_t back = max((p + n) - end, (ptrdiff_t)0);
+  const U u = load_any<U>(back >= n ? end - n : p - back);
+  return __builtin_bit_cast(V, back >= n ? (U)0 : (U)(u >> (8 * (int)back)));
+}
+
+// ---------------------------------------------------------------------------
+// types, activations
+// ---------------------------------------------------------------------------
+
+template <class T> __device__ __forceinline__ float widen(T v) { return (float)v; }
+template <class T> __device__ __forceinline__ T narrow(float v) { return (T)v; }
+
+constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// erfc(x) exp(x^2) for x >= 0: a polynomial in t = 1 / (1 + x / 2), least squares of the relative error
+// (weights moved towards equal ripples) over x in [0, 10], where erfc leaves binary32's range.  3e-8 in
+// exact arithmetic, 2.9e-7 in binary32.
+__device__ __forceinline__ float erfcx_poly(float x) {
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.5f, x, 1.0f));
+  float r = -5.505337939e-02f;
+  r = __builtin_fmaf(r, t, 2.639137506e-01f);
+  r = __builtin_fmaf(r, t, -4.415010214e-01f);
+  r = __builtin_fmaf(r, t, 2.212197632e-01f);
+  r = __builtin_fmaf(r, t, 1.705580018e-02f);
+  r = __builtin_fmaf(r, t, 1.812604517e-01f);
+  r = __builtin_fmaf(r, t, 2.497902513e-01f);
+  r = __builtin_fmaf(r, t, 2.810990512e-01f);
+  r = __builtin_fmaf(r, t, 2.822213173e-01f);
+  return __builtin_fmaf(r, t, -6.008548098e-06f);
+}
+
+// exp(-z^2 / 2); the square's rounding error would be magnified by the exponent, so it is carried along.
+__device__ __forceinline__ float exp_half_square(float z) {
+  const float c = -0.5f * kLog2E;
+  const float a = z * z;
+  const float lost = __builtin_fmaf(z, z, -a);
+  const float e = a * c;
+  const float tail = __builtin_fmaf(a, c, -e) + (lost * c + a * -9.6299e-9f);
+  return e < -160.0f ? 0.0f : exp2_fast(e) * (1.0f + kLn2 * tail);
+}
+
+// The normal distribution's Phi(z), and exp(-z^2 / 2) beside it.
+__device__ __forceinline__ float normal_cdf(float z, float& density) {
+  const float x = fabsf(z);
+  density = exp_half_square(z);
+  const float tail = 0.5f * erfcx_poly(x * 0.70710678118654752f) * density;
+  return z < 0.0f ? tail : 1.0f - tail;
+}
+
+__device__ __forceinline__ float sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.0f + exp2_fast(-kLog2E * z));
+}
+
+__device__ __forceinline__ float activate(float z, int act) {
+  if (act == SQUANT_ACT_RELU) return z < 0.0f ? 0.0f : z;  // a NaN stays
+  if (act == SQUANT_ACT_GELU) {
+    float density;
+    return z * normal_cdf(z, density);
+  }
+  if (act == SQUANT_ACT_SILU) return z * sigmoid(z);
+  return z;
+}
+
+__device__ __forceinline__ float slope(float z, int act) {
+  if (act == SQUANT_ACT_RELU) return z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;
+  if (act == SQUANT_ACT_GELU) {
+    float density;
+    const float cdf = normal_cdf(z, density);
+    const float d = 0.3989422804014327f * density;
+    return d > 0.0f ? __builtin_fmaf(z, d, cdf) : cdf + 0.0f * d;  // z may be infinite where the density is 0
+  }
+  if (act == SQUANT_ACT_SILU) {
+    const float p = sigmoid(z), q = sigmoid(-z);  // q = 1 - p without its cancellation
+    return p > 0.0f && q > 0.0f ? p * __builtin_fmaf(z, q, 1.0f) : p;
+  }
+  return 1.0f;
+}
+
+// Largest magnitude by the bits: a NaN is larger than any number and stays.
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// A value over the 4 lanes (16 apart) that hold the 64 columns of a row.
+__device__ __forceinline__ uint32_t group_max(uint32_t v) {
+  v = max(v, (uint32_t)__shfl_xor((int)v, 16));
+  return max(v, (uint32_t)__shfl_xor((int)v, 32));
+}
+
+// ---------------------------------------------------------------------------
+// finished pieces
+// ---------------------------------------------------------------------------
+
+template <int NC, class T>
+__device__ __forceinline__ void load_cols(float (&o)[NC], const T* p, int valid) {
+  if (valid >= NC) {
+    struct Pack { T v[NC]; };
+    const Pack k = load_any<Pack>(p);
+#pragma unroll
+    for (int i = 0; i < NC; ++i) o[i] = widen(k.v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < NC; ++i) o[i] = i < valid ? widen(p[i]) : 0.0f;
+  }
+}
+
+template <int NC, class T>
+__device__ __forceinline__ void store_cols(T* p, const float (&o)[NC], int valid) {
+  if (valid >= NC) {
+    struct Pack { T v[NC]; };
+    Pack k;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) k.v[i] = narrow<T>(o[i]);
+    store_any(p, k);
+  } else {
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+      if (i < valid) p[i] = narrow<T>(o[i]);
+  }
+}
+
+// A lane's NC consecutive columns of one row, `v` the bare sums.  With NC = 16 the lanes l, l^16, l^32, l^48
+// hold the row's 64 columns of one tile (every lane of the wave calls).  T: the output's type.
+template <int NC, class T>
+__device__ __forceinline__ void finish_layer(const Finish& f, int64_t row, int32_t col, float (&v)[NC], int planes) {
+  const bool live = row < f.rows;
+  const int valid = live ? min(max(f.cols - col, 0), NC) : 0;
+  const float factor = f.unit * (f.row_factor && live ? f.row_factor[row] : 1.0f);
+  float s[NC];
+  load_cols<NC, float>(s, f.scales + col, valid);
+#pragma unroll
+  for (int i = 0; i < NC; ++i) v[i] = v[i] * s[i] * factor;  // the scale first: a large row's factor alone may overflow
+  if (f.kind == kLinear) {
+    if (f.bias) {
+      load_cols<NC, T>(s, (const T*)f.bias + col, valid);
+#pragma unroll
+      for (int i = 0; i < NC; ++i) v[i] += s[i];
+    }
+    if constexpr (NC == 16) {
+      if (f.keep == SQUANT_KEEP_FULL) store_cols<NC, T>((T*)f.kept + row * f.cols + col, v, valid);
+      if (f.keep == SQUANT_KEEP_INT8) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) top = max(top, i < valid ? magnitude(v[i]) : 0u);
+        top = group_max(top);
+        const float t = __uint_as_float(top);
+        const float per = top ? 127.0f / t : 0.0f;
+        if (live && col < f.cols && (col & (kTile - 1)) == 0)
+          f.kept_scales[row * ((f.cols + kTile - 1) / kTile) + col / kTile] = top ? t / 127.0f : 1.0f;
+        uint32_t q[4];
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          q[d] = 0;
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            const float c = fminf(fmaxf(rintf(v[4 * d + b] * per), -127.0f), 127.0f);
+            q[d] |= ((uint32_t)(int)c & 255u) << (8 * b);
+          }
+        }
+        int8_t* k = (int8_t*)f.kept + row * f.cols + col;
+        if (valid >= NC) {
+          store_any(k, uint4v{q[0], q[1], q[2], q[3]});
+        } else {
+#pragma unroll
+          for (int i = 0; i < NC; ++i)
+            if (i < valid) k[i] = (int8_t)(q[i >> 2] >> (8 * (i & 3)));
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NC; ++i) v[i] = activate(v[i], f.act);
+    if (f.residual) {
+      load_cols<NC, T>(s, (const T*)f.residual + row * f.ldr + col, valid);
+#pragma unroll
+      for (int i = 0; i < NC; ++i) v[i] += s[i];
+    }
+    store_cols<NC, T>((T*)f.out + row * f.ldo + col, v, valid);
+    return;
+  }
+  if constexpr (NC == 16) {
+    if (f.kind == kStats) {
+      // the label's logit, and the chunk's largest logit and sum of exponentials
+      if (live) {
+        const int64_t at = f.labels[row] - f.first_col - col;
+        if (at >= 0 && at < valid) {
+#pragma unroll
+          for (int i = 0; i < NC; ++i)
+            if (at == i) f.label_logit[row] = v[i];
+        }
+      }
+      float top = -__builtin_inff();
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        v[i] = i < valid ? v[i] * kLog2E : -__builtin_inff();
+        top = fmaxf(top, v[i]);
+      }
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NC; ++i) sum += i < valid ? exp2_fast(v[i] - top) : 0.0f;
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if (live && col < f.cols && (col & (kTile - 1)) == 0)
+        f.stats[row * ((f.cols + kTile - 1) / kTile) + col / kTile] = make_float2(top, sum);
+      return;
+    }
+    if (f.kind == kProb && live && col < (f.cols + kTile - 1) / kTile * kTile) {
+      // p * scale * 2^E; zero from the piece's end to its next multiple of 64 columns
+      const float l2 = f.lse[row] * kLog2E, unit = *f.prob_unit;
+      _Float16* p = f.prob + row * f.ld_prob + col;
+      float lo[NC];
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        v[i] = i < valid ? exp2_fast(__builtin_fmaf(v[i], kLog2E, -l2)) * (s[i] * unit) : 0.0f;
+        lo[i] = v[i] - (float)(_Float16)v[i];
+      }
+      store_cols<NC, _Float16>(p, v, NC);
+      if (planes == 2) store_cols<NC, _Float16>(p + f.prob_plane, lo, NC);
+    }
+  }
+}
+
+// The same for the gradients: columns are the layer's inputs.
+template <class T>
+__device__ __forceinline__ void finish_grad_as(const Finish& f, int64_t row, int32_t col, float (&v)[16]) {
+  const int valid = row < f.rows ? min(max(f.cols - col, 0), 16) : 0;
+  if (valid == 0) return;
+  if (f.kind == kGrad) {
+    const float factor = f.unit * f.row_factor[row];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] *= factor;
+  } else {
+    const int64_t label = f.labels[row];
+    if (label == f.ignore) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+    } else if (label < 0 || label >= f.first_col) {  // first_col holds the vocabulary's size here
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = __builtin_nanf("");
+    } else {
+      const float factor = f.unit / *f.prob_unit, g = f.dloss[row], s = f.scales[label];
+      const uint8_t* codes = f.codes + label * f.code_row;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float c = 0.0f;
+        if (i < valid)
+          c = (float)(f.format == SQUANT_OUT_INT8 ? Codes<SQUANT_OUT_INT8>::value(codes, col + i)
+                                                  : Codes<SQUANT_OUT_INT4>::value(codes, col + i));
+        v[i] = g * (v[i] * factor - s * c);
+      }
+    }
+  }
+  store_cols<16, T>((T*)f.out + row * f.ldo + col, v, valid);
+}
+
+__device__ __forceinline__ void finish_grad(const Finish& f, int64_t row, int32_t col, float (&v)[16]) {
+  if (f.out_type == SQUANT_W_F32) finish_grad_as<float>(f, row, col, v);
+  else if (f.out_type == SQUANT_W_F16) finish_grad_as<_Float16>(f, row, col, v);
+  else finish_grad_as<__bf16>(f, row, col, v);
+}
+
+// The type of a layer's output by its row operand.
+template <class F, int PL> struct OutOf { typedef float type; };
+template <> struct OutOf<Half, 1> { typedef _Float16 type; };
+template <> struct OutOf<Brain, 1> { typedef __bf16 type; };
+
+// Where the 4 values of column fragment `c` of a lane group of 4 lanes go among its 16 columns: the layer's
+// fragments hold 4 consecutive columns, the gradient's every fourth.
+template <bool GRAD>
+__device__ __forceinline__ constexpr int column_of(int c, int i) { return GRAD ? 4 * i + c : 4 * c + i; }
+
+}  // namespace lin
+}  // namespace squant

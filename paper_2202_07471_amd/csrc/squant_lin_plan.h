@@ -1,0 +1,97 @@
+// How a product with codes is cut into workgroups.  Host code only.
+#pragma once
+
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "squant_few_rows.h"
+#include "squant_product.h"
+
+namespace squant {
+namespace lin {
+
+constexpr int32_t kMaxSide = 1 << 24;    // of a layer
+constexpr int64_t kMaxRows = 1 << 26;
+constexpr int kCus = 256;
+
+struct Split {
+  bool few;
+  int mt;              // rows of a workgroup of `product`
+  int row_frags;       // few_rows: fragments of 16 rows
+  int col_frags_each;  // few_rows: fragments of 16 columns a workgroup
+  int tiles_m, tiles_n;
+  int blocks, slices;
+  int64_t workgroups;  // of a slice
+  int threads;
+  size_t lds;
+  int64_t row_frags_all, col_frags_all;  // of the partial sums
+  int64_t partial_vectors() const { return (int64_t)slices * row_frags_all * col_frags_all * kLanes; }
+};
+
+inline int shape_threads(int mt) {
+  return mt == 256 ? Shape<256>::kThreads : mt == 128 ? Shape<128>::kThreads : Shape<64>::kThreads;
+}
+
+// `product` over rows x cols with a contraction of `depth`: the rows of a workgroup and the slices of the
+// contraction by an estimate of the time.  The coefficients are fitted to measured times.
+inline Split split_product(int64_t rows, int64_t cols, int64_t depth, int planes, bool may_split) {
+  Split best{};
+  double best_time = 1e30;
+  const int blocks = (int)((depth + kBlock - 1) / kBlock);
+  for (int mt = 64; mt <= 256; mt *= 2) {
+    const int64_t tm = (rows + mt - 1) / mt, tn = (cols + kWide - 1) / kWide;
+    const double step = (mt == 256 ? 1.5 : mt == 128 ? 0.9 : 0.6) * planes;  // us of 64 contraction elements
+    for (int s = 1; s <= 64 && s <= blocks; s = s < 4 ? s + 1 : s * 2) {
+      if (s > 1 && !may_split) break;
+      const int64_t rounds = (tm * tn * s + kCus - 1) / kCus;
+      const double join = s > 1 ? 3.0 + (double)tm * mt * tn * kWide * 4.0 * s / 3.0e6 : 0.0;
+      const double time = rounds * (step * ((blocks + s - 1) / s) + 3.0) + join;
+      if (time < best_time) {
+        best_time = time;
+        best.mt = mt; best.tiles_m = (int)tm; best.tiles_n = (int)tn; best.slices = s;
+      }
+    }
+  }
+  best.few = false;
+  best.blocks = blocks;
+  best.workgroups = (int64_t)best.tiles_m * best.tiles_n;
+  best.threads = shape_threads(best.mt);
+  best.lds = (size_t)best.mt * kBlock * 2 * planes * 2;
+  best.row_frags_all = (int64_t)best.tiles_m * (best.mt / 16);
+  best.col_frags_all = (int64_t)best.tiles_n * (kWide / 16);
+  return best;
+}
+
+// A layer's product.  `tiled`: columns have to come in whole tiles of 64 (kept pre-activation, loss).
+inline Split split_layer(int64_t rows, int64_t cols, int64_t depth, int planes, bool tiled, bool may_split) {
+  if (rows > kFewRows) return split_product(rows, cols, depth, planes, may_split);
+  Split p{};
+  p.few = true;
+  p.row_frags = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  p.col_frags_each = tiled ? 4 : 1;
+  p.blocks = (int)((depth + kBlock - 1) / kBlock);
+  p.slices = 1;
+  p.tiles_m = p.row_frags;
+  p.tiles_n = (int)((cols + 16 * p.col_frags_each - 1) / (16 * p.col_frags_each));
+  p.workgroups = p.tiles_n;
+  p.threads = kFewWaves * kLanes;
+  p.lds = (size_t)kFewWaves * p.row_frags * p.col_frags_each * kLanes * 16;
+  p.row_frags_all = p.row_frags;
+  p.col_frags_all = (int64_t)p.tiles_n * p.col_frags_each;
+  return p;
+}
+
+inline Split split_gradient(int64_t rows, int64_t cols, int64_t depth, int planes) {
+  return split_product(rows, cols, depth, planes, true);
+}
+
+// Columns of the vocabulary whose probabilities are held at a time: about 256 MB, at least 4096 entries.
+inline int64_t vocabulary_piece(int64_t rows, int64_t cols, int planes) {
+  const int64_t whole = (cols + kTile - 1) / kTile * kTile;
+  const int64_t fit = (int64_t)(128 << 20) / (rows * planes) / kWide * kWide;
+  return std::min(whole, std::max<int64_t>(4096, fit));
+}
+
+}  // namespace lin
+}  // namespace squant

@@ -1,0 +1,203 @@
+// What goes before and after the products with codes: row operands laid out, gradients of the activation, partial
+// sums joined, the loss from its chunks.
+#pragma once
+
+#include "squant_lin.h"
+
+namespace squant {
+namespace lin {
+
+constexpr int kRowThreads = 256;
+
+struct RowsArgs {
+  const void* x;            // rows, or the output's gradient
+  int64_t ldx;
+  int64_t rows;
+  int32_t cols;
+  void* out;                // [rows][planes][padded]
+  int32_t padded;           // cols up to a multiple of 64
+  float* row_factor;
+  // gradient rows only
+  const float* scales;
+  const void* kept;
+  const float* kept_scales;
+  int act, keep;
+  int rows_per_group;
+  float* column_sums;       // [partials][cols], or null
+};
+
+// The power of two that brings a row's largest finite magnitude into [2^14, 2^15), as an exponent.  It stops
+// at 126 (2^-126 and its inverse are normal numbers).
+__device__ __forceinline__ int row_exponent(uint32_t top) {
+  if (top == 0) return 0;
+  const int e = (int)(top >> 23) - 127;  // a subnormal counts as 2^-127
+  return min(14 - e, 126);
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+__device__ __forceinline__ uint32_t finite_magnitude(float v) {
+  const uint32_t m = magnitude(v);
+  return m < 0x7f800000u ? m : 0u;
+}
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+#pragma unroll
+  for (int o = 1; o < kLanes; o <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o));
+  return v;
+}
+
+// hi + lo of 8 values, written to one or two planes.
+template <int PL>
+__device__ __forceinline__ void store_planes(_Float16* p, int64_t plane, const float (&v)[8]) {
+  half8 hi, lo;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    hi[i] = (_Float16)v[i];
+    // an infinity has no remainder
+    lo[i] = magnitude(v[i]) < 0x7f800000u ? (_Float16)(v[i] - (float)hi[i]) : (_Float16)0.0f;
+  }
+  *(half8*)p = hi;
+  if (PL == 2) *(half8*)(p + plane) = lo;
+}
+
+// 16-bit rows copied to where they are aligned and end with zeros.  Any 16-bit type.
+__global__ void __launch_bounds__(kRowThreads) pad_rows(RowsArgs a);
+// binary32 rows to two planes, a workgroup a row.
+__global__ void __launch_bounds__(kRowThreads) split_rows(RowsArgs a);
+
+// Rows of dz * scale, dz = dy * act'(z), as PL binary16 planes with an exponent a row, and the column sums of dz.
+// The exponent comes from the largest |dy * scale| (the slopes stay below 1.13), so that it costs no second
+// evaluation of the slope: dy is read twice, the second time from the cache.  A workgroup takes a few rows;
+// where they have few columns its threads share out the rows as well.
+template <class T, int PL>
+__global__ void __launch_bounds__(kRowThreads) gradient_rows(RowsArgs a) {
+  __shared__ int exponent[64];
+  const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+  const int64_t row0 = (int64_t)blockIdx.x * a.rows_per_group;
+  const int n_rows = (int)min((int64_t)a.rows_per_group, a.rows - row0);
+  for (int r = wave; r < n_rows; r += kRowThreads / kLanes) {
+    const T* dy = (const T*)a.x + (row0 + r) * a.ldx;
+    uint32_t top = 0;
+    for (int32_t c = lane * 8; c < a.cols; c += kLanes * 8) {
+      float v[8], s[8];
+      load_cols<8, T>(v, dy + c, a.cols - c);
+      load_cols<8, float>(s, a.scales + c, a.cols - c);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, finite_magnitude(v[i] * s[i]));
+    }
+    top = wave_max(top);
+    if (lane == 0) {
+      const int e = row_exponent(top) - 1;  // room for slopes beyond 1
+      exponent[r] = e;
+      a.row_factor[row0 + r] = power_of_two(-e);
+    }
+  }
+  __syncthreads();
+  const int vectors = a.padded / 8;
+  const int shares = max(1, kRowThreads / vectors), share = shares > 1 ? (int)threadIdx.x / vectors : 0;
+  if (share >= shares) return;
+  const int32_t chunks = (a.cols + kTile - 1) / kTile;
+  for (int j = shares > 1 ? (int)threadIdx.x % vectors : (int)threadIdx.x; j < vectors; j += kRowThreads) {
+    const int32_t c = j * 8;
+    const int valid = min(max(a.cols - c, 0), 8);
+    float s[8], sum[8];
+    load_cols<8, float>(s, a.scales + c, valid);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+    for (int r = share; r < n_rows; r += shares) {
+      const int64_t row = row0 + r;
+      const float up = power_of_two(exponent[r]);
+      float v[8];
+      load_cols<8, T>(v, (const T*)a.x + row * a.ldx + c, valid);
+      if (a.keep == SQUANT_KEEP_FULL) {
+        float z[8];
+        load_cols<8, T>(z, (const T*)a.kept + row * a.cols + c, valid);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= slope(z[i], a.act);
+      } else if (a.keep == SQUANT_KEEP_INT8) {
+        float z[8];
+        const float unit = valid ? a.kept_scales[row * chunks + c / kTile] : 0.0f;
+        load_cols<8, int8_t>(z, (const int8_t*)a.kept + row * a.cols + c, valid);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= slope(z[i] * unit, a.act);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[i] = i < valid ? v[i] : 0.0f;
+        sum[i] += v[i];
+        v[i] = v[i] * s[i] * up;
+      }
+      store_planes<PL>((_Float16*)a.out + row * PL * a.padded + c, a.padded, v);
+    }
+    if (a.column_sums) {
+      float* out = a.column_sums + ((int64_t)blockIdx.x * shares + share) * a.cols + c;
+      store_cols<8, float>(out, sum, valid);
+    }
+  }
+}
+
+struct ColumnSumArgs {
+  const float* partial;
+  int64_t partials;
+  int32_t cols;
+  void* out;
+  int out_type;
+};
+__global__ void __launch_bounds__(1024) column_sums(ColumnSumArgs a);
+
+struct JoinArgs {
+  const float4v* partial;
+  int slices;
+  int64_t row_frags, col_frags;
+  Finish f;
+  int planes;
+};
+// Adds the slices of a split product in their order: one wave a fragment of 16 rows and 64 columns.
+template <bool GRAD, class T>
+__global__ void __launch_bounds__(kRowThreads) join(JoinArgs a) {
+  const int lane = threadIdx.x & (kLanes - 1);
+  const int64_t at = (int64_t)blockIdx.x * (kRowThreads / kLanes) + threadIdx.x / kLanes;
+  const int64_t tiles = a.col_frags / 4;
+  if (at >= a.row_frags * tiles) return;
+  const int64_t rf = at / tiles, tile = at % tiles;
+  float4v t[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) t[c] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s = 0; s < a.slices; ++s) {
+    const float4v* p = a.partial + ((s * a.row_frags + rf) * a.col_frags + tile * 4) * kLanes + lane;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) t[c] += p[c * kLanes];
+  }
+  float v[16];
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[column_of<GRAD>(c, i)] = t[c][i];
+  const int64_t row = rf * 16 + (lane & 15);
+  const int32_t col = (int32_t)tile * kTile + (lane >> 4) * 16;
+  if constexpr (GRAD) finish_grad(a.f, row, col, v);
+  else finish_layer<16, T>(a.f, row, col, v, a.planes);
+}
+
+struct LossArgs {
+  const float2* stats;
+  int32_t chunks;
+  const float* label_logit;
+  const int64_t* labels;
+  int64_t ignore;
+  int32_t vocabulary;
+  int64_t rows;
+  float* loss;
+  float* lse;
+};
+// A wave a row: the chunks' sums brought to one largest logit.
+__global__ void __launch_bounds__(kRowThreads) loss_rows(LossArgs a);
+
+// 2^E of the gradient's probabilities: the largest scale of the vocabulary comes into [2^13, 2^14).
+__global__ void __launch_bounds__(1024) probability_unit(const float* scales, int32_t n, float* unit);
+
+typedef void (*rows_kernel_t)(RowsArgs);
+typedef void (*join_kernel_t)(JoinArgs);
+
+}  // namespace lin
+}  // namespace squant

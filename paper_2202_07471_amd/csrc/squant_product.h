@@ -1,0 +1,210 @@
+// The product of many rows with codes, for a layer (GRAD = false: the contraction runs along a code row) and
+// for its gradient (GRAD = true: across the code rows).
+//
+// A workgroup makes MT x 256 outputs with waves of (MT / 2) x 64 (64 x 64 where MT is 64).  The row operand goes to
+// the LDS without passing through registers, 64 contraction elements at a time in two buffers; rows of 128 bytes
+// with their 16-byte chunks exchanged by the row's low three bits, so that 8 lanes that read the same chunk of
+// 8 rows use all banks.  Codes go from memory to the registers of the waves that own their columns and are made
+// operands there: they are half or a quarter of the operand's bytes, each wave reads each of its codes once, and
+// no LDS traffic is spent on them.  Codes are the matrix instruction's first operand, rows its second, so that a
+// lane ends with 16 consecutive columns of one row.
+#pragma once
+
+#include "squant_lin.h"
+
+namespace squant {
+namespace lin {
+
+template <int MT> struct Shape {
+  static constexpr int kWavesM = MT == 64 ? 1 : 2;
+  static constexpr int kWaveRows = MT / kWavesM;
+  static constexpr int kWaves = kWavesM * (kWide / kTile);
+  static constexpr int kThreads = kWaves * kLanes;
+  static constexpr int kFrags = kWaveRows / 16;
+};
+
+// 16 bytes a lane from memory to LDS bytes [lds, lds + 1024), in lane order.
+__device__ __forceinline__ void to_lds(const void* p, void* lds) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                   (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+}
+
+// The codes of one step, as loaded.
+template <int FMT, bool GRAD> struct Raw;
+template <int FMT> struct Raw<FMT, false> { typename Codes<FMT>::row16 v[4]; };
+template <int FMT> struct Raw<FMT, true> { typename Codes<FMT>::col4 v[16]; };
+
+template <class F, int PL, int FMT, int MT, bool GRAD>
+__global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a) {
+  typedef Shape<MT> S;
+  constexpr int kPlaneBytes = MT * kBlock * 2;
+  constexpr int kBufBytes = kPlaneBytes * PL;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+  const int wave_m = wave % S::kWavesM, wave_n = wave / S::kWavesM;
+
+  // Each XCD takes a run of consecutive tiles; within it, bands of 8 tiles of rows run along the columns, so that
+  // what an XCD's cache holds of rows and of codes is used by several workgroups.
+  const int tiles = a.tiles_m * a.tiles_n;
+  int tile = blockIdx.x;
+  {
+    const int per = tiles / 8, rest = tiles % 8, x = tile % 8;
+    tile = x * per + min(x, rest) + tile / 8;
+  }
+  const int band = tile / (8 * a.tiles_n);
+  const int band_rows = min(8, a.tiles_m - band * 8);
+  const int in_band = tile - band * 8 * a.tiles_n;
+  const int tile_m = band * 8 + in_band % band_rows, tile_n = in_band / band_rows;
+  const int slice = blockIdx.y;
+  const int first = (int)((int64_t)a.blocks * slice / a.slices), last = (int)((int64_t)a.blocks * (slice + 1) / a.slices);
+
+  const int64_t row0 = (int64_t)tile_m * MT;
+  const int32_t col0 = tile_n * kWide + wave_n * kTile;
+  const int sub = lane & 15, quad = lane >> 4;
+
+  // row operand: 8 rows an instruction; a row past the end is the last one again
+  constexpr int kLoads = MT / 8 / S::kWaves;
+  const char* src[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int r = (wave * kLoads + i) * 8 + (lane >> 3);
+    const int64_t row = min(row0 + r, a.f.rows - 1);
+    src[i] = (const char*)a.a + row * a.lda * 2 + (((lane & 7) ^ (r & 7)) << 4);
+  }
+  auto load_rows = [&](int b, int buf) {
+#pragma unroll
+    for (int p = 0; p < PL; ++p)
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        to_lds(src[i] + p * a.plane * 2 + (int64_t)b * (kBlock * 2),
+               smem + buf * kBufBytes + p * kPlaneBytes + (wave * kLoads + i) * 1024);
+  };
+
+  // Codes.  For a layer each lane reads 16 codes of 4 rows; for a gradient 4 columns of 16 rows, lanes whose columns
+  // do not exist those of the row's last bytes.  `inside`: blocks whose reads stay in the buffer.
+  const int64_t w_bytes = (int64_t)a.w_rows * a.w_row;
+  uint32_t wsrc[GRAD ? 1 : 4];
+  const uint8_t* w_base = a.w;
+  int inside;
+  if constexpr (GRAD) {
+    const uint32_t at = (uint32_t)min(Codes<FMT>::offset(col0 + 4 * sub), a.w_row - 1);
+    wsrc[0] = (uint32_t)quad * 16 * (uint32_t)a.w_row + at;
+    inside = (int)max((w_bytes - 4) / (kBlock * a.w_row), (int64_t)0);
+  } else {
+    w_base += (int64_t)min(col0, a.w_rows - 1) * a.w_row;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      wsrc[c] = (uint32_t)max(min(col0 + (sub >> 2) * 16 + c * 4 + (sub & 3), a.w_rows - 1) - min(col0, a.w_rows - 1), 0) *
+                (uint32_t)a.w_row + (uint32_t)Codes<FMT>::offset(quad * 16);
+    inside = a.w_cols / kBlock;
+  }
+  auto load_codes = [&](int b, Raw<FMT, GRAD>& o) {
+    if constexpr (GRAD) {
+      typedef typename Codes<FMT>::col4 V;
+      const uint8_t* p = w_base + (int64_t)b * kBlock * a.w_row;
+      if (b < inside) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o.v[i] = load_any<V>(p + i * a.w_row + wsrc[0]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o.v[i] = load_before<V>(p + i * a.w_row + wsrc[0], a.w_end, w_bytes);
+      }
+    } else {
+      typedef typename Codes<FMT>::row16 V;
+      const uint8_t* p = w_base + Codes<FMT>::offset((int64_t)b * kBlock);
+      if (b < inside) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o.v[c] = load_any<V>(p + wsrc[c]);
+      } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o.v[c] = load_before<V>(p + wsrc[c], a.w_end, w_bytes);
+      }
+    }
+  };
+
+  float4v acc[S::kFrags][4];
+#pragma unroll
+  for (int m = 0; m < S::kFrags; ++m)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) acc[m][c] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+
+  auto multiply = [&](int buf, const Raw<FMT, GRAD>& r) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      __builtin_amdgcn_sched_barrier(0);  // one half's operands at a time in registers
+      typename F::frag w[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        if constexpr (GRAD) w[c] = convert_columns<FMT>(r.v + 8 * h, c);
+        else w[c] = convert<F, FMT>(r.v[c], h);
+      }
+#pragma unroll
+      for (int p = 0; p < PL; ++p)
+#pragma unroll
+        for (int m = 0; m < S::kFrags; ++m) {
+          const typename F::frag x = *(const typename F::frag*)(
+              smem + buf * kBufBytes + p * kPlaneBytes + m * 2048 + wave_m * S::kWaveRows * 128 + sub * 128 +
+              (((quad * 2 + h) ^ (sub & 7)) << 4));
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[m][c] = F::mma(w[c], x, acc[m][c]);
+        }
+    }
+  };
+  // Every load of a step was issued a step earlier; the barrier also says that the other buffer is read out.
+  auto arrived = [&]() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  };
+
+  if (first < last) {
+    Raw<FMT, GRAD> now, next;
+    load_rows(first, 0);
+    load_codes(first, now);
+    next = now;
+#pragma unroll 1
+    for (int b = first; b < last; ++b) {
+      const int buf = (b - first) & 1;
+      arrived();
+      if (b + 1 < last) {
+        load_rows(b + 1, buf ^ 1);
+        load_codes(b + 1, next);
+      }
+      multiply(buf, now);
+      now = next;
+    }
+  }
+
+  if (a.f.kind == kPartial) {
+    const int64_t frags_n = (int64_t)a.tiles_n * (kWide / 16);
+#pragma unroll
+    for (int m = 0; m < S::kFrags; ++m) {
+      const int64_t row_frag = ((int64_t)slice + a.slice0) * a.tiles_m * (MT / 16) + tile_m * (MT / 16) + wave_m * S::kFrags + m;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        a.f.partial[(row_frag * frags_n + (col0 / 16 + c)) * kLanes + lane] = acc[m][c];
+    }
+    return;
+  }
+#pragma unroll
+  for (int m = 0; m < S::kFrags; ++m) {
+    __builtin_amdgcn_sched_barrier(0);
+    float v[16];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[column_of<GRAD>(c, i)] = acc[m][c][i];
+    const int64_t row = row0 + wave_m * S::kWaveRows + m * 16 + sub;
+    if constexpr (GRAD) finish_grad(a.f, row, col0 + quad * 16, v);
+    else finish_layer<16, typename OutOf<F, PL>::type>(a.f, row, col0 + quad * 16, v, PL);
+  }
+}
+
+template <class F, int PL, int FMT, bool GRAD>
+product_t product_of(int mt) {
+  if (mt == 256) return product<F, PL, FMT, 256, GRAD>;
+  if (mt == 128) return product<F, PL, FMT, 128, GRAD>;
+  return product<F, PL, FMT, 64, GRAD>;
+}
+
+}  // namespace lin
+}  // namespace squant

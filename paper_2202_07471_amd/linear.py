@@ -1,0 +1,299 @@
+"""Operators on quantised layers: ctypes marshalling of the calls that multiply by the solver's codes, and their
+torch autograd forms.
+
+``codes`` and ``scales`` are what ``squant_quantize`` (int8) or ``squant_quantize_ex`` with ``OUT_INT4`` (uint8, two
+codes a byte) return: a weight [cout, cin], or a convolution's [cout, cin, kh, kw] taken as [cout, cin * kh * kw].
+"""
+from __future__ import annotations
+
+import ctypes
+from functools import lru_cache
+from typing import Optional
+
+import torch
+
+from .binding import OUT_INT4, OUT_INT8, SQuantError, _check, _stream_ptr, _WTYPES, lib  # noqa: F401
+
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
+ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "silu": ACT_SILU}
+KEEP_NONE, KEEP_INT8, KEEP_FULL = 0, 1, 2
+KEEPS = {"none": KEEP_NONE, "int8": KEEP_INT8, "full": KEEP_FULL}
+IGNORE_INDEX = -100
+_KEPT_GROUP = 64  # columns of a row that share a scale of the kept pre-activation
+
+
+class squant_codes_t(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("cout", ctypes.c_int32),
+                ("cin", ctypes.c_int32), ("format", ctypes.c_int)]
+
+
+_ready = None
+
+
+def _lib():
+    global _ready
+    if _ready is None:
+        L = lib()
+        i64, vp, sz, en = ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int
+        cp = ctypes.POINTER(squant_codes_t)
+        L.squant_linear.argtypes = [vp, i64, en, i64, cp, vp, en, vp, i64, vp, i64, en, vp, vp, vp, sz, vp]
+        L.squant_linear_backward.argtypes = [vp, i64, en, i64, cp, en, en, vp, vp, vp, i64, vp, vp, sz, vp]
+        L.squant_cross_entropy.argtypes = [vp, i64, en, i64, cp, vp, i64, vp, vp, vp, sz, vp]
+        L.squant_cross_entropy_backward.argtypes = [vp, i64, en, i64, cp, vp, i64, vp, vp, vp, i64, vp, sz, vp]
+        L.squant_linear_workspace_bytes.argtypes = [en, i64, cp, en]
+        for f in ("linear_backward", "cross_entropy", "cross_entropy_backward"):
+            getattr(L, f"squant_{f}_workspace_bytes").argtypes = [en, i64, cp]
+        for f in ("linear", "linear_backward", "cross_entropy", "cross_entropy_backward"):
+            getattr(L, f"squant_{f}").restype = en
+            getattr(L, f"squant_{f}_workspace_bytes").restype = sz
+        _ready = L
+    return _ready
+
+
+@lru_cache(maxsize=1024)
+def _workspace_bytes(call: str, type_: int, rows: int, cout: int, cin: int, fmt: int, *rest: int) -> int:
+    # the size depends on the shapes alone: the pointers only have to be there
+    w = squant_codes_t(256, 256, cout, cin, fmt)
+    return int(getattr(_lib(), f"squant_{call}_workspace_bytes")(type_, rows, ctypes.byref(w), *rest))
+
+
+def _workspace(x: torch.Tensor, nbytes: int, stream) -> Optional[torch.Tensor]:
+    if nbytes == 0:
+        return None
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+    if stream is not None:
+        ws.record_stream(stream)
+    return ws
+
+
+def _rows(t: torch.Tensor, cols: int, what: str, like: Optional[torch.Tensor] = None):
+    """(rows, elements between rows) of an activation tensor whose last dimension is `cols`."""
+    if not t.is_cuda or t.dtype not in _WTYPES:
+        raise ValueError(f"{what} must be a float32, float16 or bfloat16 tensor in device memory")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what} is not on the current device")
+    if like is not None and (t.dtype != like.dtype or t.shape[:-1] != like.shape[:-1]):
+        raise ValueError(f"{what} must have the type and the leading dimensions of the other activations")
+    if t.dim() == 0 or t.shape[-1] != cols:
+        raise ValueError(f"{what} must have {cols} elements in its last dimension")
+    if cols > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{what} must be contiguous in its last dimension")
+    if t.dim() == 1:
+        return 1, cols
+    if t.dim() > 2:
+        if not t.is_contiguous():
+            raise ValueError(f"{what} of more than two dimensions must be contiguous")
+        return t.numel() // cols, cols
+    rows = t.shape[0]
+    ld = t.stride(0) if rows > 1 else cols
+    if ld < cols:
+        raise ValueError(f"rows of {what} overlap")
+    return rows, ld
+
+
+def _codes(codes: torch.Tensor, scales: torch.Tensor, cin: int, like: torch.Tensor) -> squant_codes_t:
+    if codes.dtype == torch.int8:
+        fmt, row = OUT_INT8, cin
+    elif codes.dtype == torch.uint8:
+        fmt, row = OUT_INT4, (cin + 1) // 2
+    else:
+        raise ValueError("codes must be int8, or uint8 with two 4-bit codes a byte")
+    cout = codes.shape[0] if codes.dim() else 0
+    if cin <= 0 or cout <= 0 or codes.numel() != cout * row or not codes.is_contiguous():
+        raise ValueError(f"codes must be contiguous with {row} bytes for each of their output channels")
+    if scales.dtype != torch.float32 or scales.dim() != 1 or scales.shape[0] != cout or not scales.is_contiguous():
+        raise ValueError("scales must be a contiguous float32 tensor with one scale for each output channel")
+    if codes.device != like.device or scales.device != like.device:
+        raise ValueError("codes and scales must be on the activations' device")
+    return squant_codes_t(codes.data_ptr(), scales.data_ptr(), cout, cin, fmt)
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def squant_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                  act: int = ACT_NONE, residual: Optional[torch.Tensor] = None, keep: Optional[int] = None,
+                  out: Optional[torch.Tensor] = None, stream=None):
+    """act(x @ (codes * scales).T + bias) + residual for x [..., cin]; returns [..., cout] of x's type.
+
+    With `keep` (KEEP_INT8, KEEP_FULL or KEEP_NONE) returns (y, kept): the pre-activation for
+    squant_linear_backward as (int8 codes, scales), as a tensor of x's type, or None.  `out` may be `residual`.
+    Asynchronous on `stream` (default: torch's current stream)."""
+    cin = x.shape[-1] if x.dim() else 0
+    rows, ldx = _rows(x, cin, "x")
+    w = _codes(codes, scales, cin, x)
+    cout = w.cout
+    shape = x.shape[:-1] + (cout,)
+    if bias is not None and (bias.dtype != x.dtype or bias.shape != (cout,) or not bias.is_contiguous()
+                             or bias.device != x.device):
+        raise ValueError("bias must be contiguous, of x's type and device, with one element for each output channel")
+    ldr = ldy = cout
+    if residual is not None:
+        ldr = _rows(residual, cout, "residual", x)[1]
+    if out is None:
+        out = torch.empty(shape, dtype=x.dtype, device=x.device)
+    else:
+        ldy = _rows(out, cout, "out", x)[1]
+    kept = kept_scales = None
+    how = KEEP_NONE if keep is None else keep
+    if how == KEEP_INT8:
+        kept = torch.empty(shape, dtype=torch.int8, device=x.device)
+        kept_scales = torch.empty(x.shape[:-1] + (-(-cout // _KEPT_GROUP),), dtype=torch.float32, device=x.device)
+    elif how == KEEP_FULL:
+        kept = torch.empty(shape, dtype=x.dtype, device=x.device)
+    type_ = _WTYPES[x.dtype]
+    nbytes = _workspace_bytes("linear", type_, rows, cout, cin, w.format, how)
+    ws = _workspace(x, nbytes, stream)
+    _check(_lib().squant_linear(x.data_ptr(), ldx, type_, rows, ctypes.byref(w), _ptr(bias), act, _ptr(residual), ldr,
+                                out.data_ptr(), ldy, how, _ptr(kept), _ptr(kept_scales), _ptr(ws), nbytes,
+                                _stream_ptr(stream)))
+    if keep is None:
+        return out
+    return out, ((kept, kept_scales) if how == KEEP_INT8 else kept)
+
+
+def squant_linear_backward(dy: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, cin: int, act: int = ACT_NONE,
+                           kept=None, bias: bool = True, dx: Optional[torch.Tensor] = None, stream=None):
+    """(dx, dbias) of squant_linear for dy [..., cout], codes and scales held fixed; dbias is None without `bias`.
+
+    `kept` is what squant_linear returned beside y.  The residual's gradient is dy."""
+    cout = codes.shape[0] if codes.dim() else 0
+    rows, lddy = _rows(dy, cout, "dy")
+    w = _codes(codes, scales, cin, dy)
+    how, z, z_scales = KEEP_NONE, None, None
+    if isinstance(kept, (tuple, list)):
+        how, (z, z_scales) = KEEP_INT8, kept
+        groups = dy.shape[:-1] + (-(-cout // _KEPT_GROUP),)
+        if (z.dtype != torch.int8 or z.shape != dy.shape or not z.is_contiguous() or z.device != dy.device
+                or z_scales.dtype != torch.float32 or z_scales.shape != groups or not z_scales.is_contiguous()
+                or z_scales.device != dy.device):
+            raise ValueError("kept must be the pair that squant_linear returned for these rows")
+    elif kept is not None:
+        how, z = KEEP_FULL, kept
+        if z.dtype != dy.dtype or z.shape != dy.shape or not z.is_contiguous() or z.device != dy.device:
+            raise ValueError("kept must be the tensor that squant_linear returned for these rows")
+    shape = dy.shape[:-1] + (cin,)
+    lddx = cin
+    if dx is None:
+        dx = torch.empty(shape, dtype=dy.dtype, device=dy.device)
+    else:
+        lddx = _rows(dx, cin, "dx", dy)[1]
+    dbias = torch.empty(cout, dtype=dy.dtype, device=dy.device) if bias else None
+    type_ = _WTYPES[dy.dtype]
+    nbytes = _workspace_bytes("linear_backward", type_, rows, cout, cin, w.format)
+    ws = _workspace(dy, nbytes, stream)
+    _check(_lib().squant_linear_backward(dy.data_ptr(), lddy, type_, rows, ctypes.byref(w), act, how, _ptr(z),
+                                         _ptr(z_scales), dx.data_ptr(), lddx, _ptr(dbias), _ptr(ws), nbytes,
+                                         _stream_ptr(stream)))
+    return dx, dbias
+
+
+def _check_per_row(t: torch.Tensor, dtype, h: torch.Tensor, what: str):
+    if t.dtype != dtype or t.shape != h.shape[:-1] or not t.is_contiguous() or t.device != h.device:
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor with one element for each row of h")
+
+
+def squant_cross_entropy(h: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, labels: torch.Tensor,
+                         ignore_index: int = IGNORE_INDEX, stream=None):
+    """(loss, lse), float32 for each row of h [..., cin], of the logits h @ (codes * scales).T against int64 labels.
+
+    The logits are never in memory.  loss is 0 where the label is `ignore_index` and NaN where it is no entry of
+    the vocabulary."""
+    cin = h.shape[-1] if h.dim() else 0
+    rows, ldh = _rows(h, cin, "h")
+    w = _codes(codes, scales, cin, h)
+    _check_per_row(labels, torch.int64, h, "labels")
+    loss = torch.empty(h.shape[:-1], dtype=torch.float32, device=h.device)
+    lse = torch.empty_like(loss)
+    type_ = _WTYPES[h.dtype]
+    nbytes = _workspace_bytes("cross_entropy", type_, rows, w.cout, cin, w.format)
+    ws = _workspace(h, nbytes, stream)
+    _check(_lib().squant_cross_entropy(h.data_ptr(), ldh, type_, rows, ctypes.byref(w), labels.data_ptr(),
+                                       ignore_index, loss.data_ptr(), lse.data_ptr(), _ptr(ws), nbytes,
+                                       _stream_ptr(stream)))
+    return loss, lse
+
+
+def squant_cross_entropy_backward(h: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, labels: torch.Tensor,
+                                  lse: torch.Tensor, dloss: torch.Tensor, ignore_index: int = IGNORE_INDEX,
+                                  dh: Optional[torch.Tensor] = None, stream=None):
+    """dh of squant_cross_entropy for the losses' gradients dloss (float32, one for each row)."""
+    cin = h.shape[-1] if h.dim() else 0
+    rows, ldh = _rows(h, cin, "h")
+    w = _codes(codes, scales, cin, h)
+    _check_per_row(labels, torch.int64, h, "labels")
+    _check_per_row(lse, torch.float32, h, "lse")
+    _check_per_row(dloss, torch.float32, h, "dloss")
+    lddh = cin
+    if dh is None:
+        dh = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+    else:
+        lddh = _rows(dh, cin, "dh", h)[1]
+    type_ = _WTYPES[h.dtype]
+    nbytes = _workspace_bytes("cross_entropy_backward", type_, rows, w.cout, cin, w.format)
+    ws = _workspace(h, nbytes, stream)
+    _check(_lib().squant_cross_entropy_backward(h.data_ptr(), ldh, type_, rows, ctypes.byref(w), labels.data_ptr(),
+                                                ignore_index, lse.data_ptr(), dloss.data_ptr(), dh.data_ptr(), lddh,
+                                                _ptr(ws), nbytes, _stream_ptr(stream)))
+    return dh
+
+
+def _rowwise(t: torch.Tensor) -> torch.Tensor:
+    """t itself where the calls take it, else a contiguous copy (expanded gradients, transposed views)."""
+    if t.is_contiguous() or (t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]):
+        return t
+    return t.contiguous()
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, codes, scales, bias, act, residual, keep):
+        ctx.act, ctx.cin, ctx.codes, ctx.scales = act, x.shape[-1], codes, scales
+        needed = ctx.needs_input_grad[0] or ctx.needs_input_grad[3]
+        how = keep if act != ACT_NONE and needed else KEEP_NONE
+        y, kept = squant_linear(_rowwise(x), codes, scales, bias, act,
+                                None if residual is None else _rowwise(residual), keep=how)
+        ctx.pair = isinstance(kept, tuple)
+        ctx.save_for_backward(*(kept if ctx.pair else (kept,)))
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        dx = dbias = None
+        if ctx.needs_input_grad[0] or ctx.needs_input_grad[3]:
+            kept = ctx.saved_tensors
+            dx, dbias = squant_linear_backward(_rowwise(dy), ctx.codes, ctx.scales, ctx.cin, ctx.act,
+                                               kept if ctx.pair else kept[0], bias=ctx.needs_input_grad[3])
+        return (dx if ctx.needs_input_grad[0] else None, None, None, dbias, None,
+                dy if ctx.needs_input_grad[5] else None, None)
+
+
+class _CrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, h, codes, scales, labels, ignore_index):
+        h = _rowwise(h)
+        loss, lse = squant_cross_entropy(h, codes, scales, labels, ignore_index)
+        ctx.codes, ctx.scales, ctx.ignore_index = codes, scales, ignore_index
+        ctx.save_for_backward(h, labels, lse)
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss):
+        h, labels, lse = ctx.saved_tensors
+        return (squant_cross_entropy_backward(h, ctx.codes, ctx.scales, labels, lse, dloss.contiguous(),
+                                              ctx.ignore_index), None, None, None, None)
+
+
+def quantized_linear(x, codes, scales, bias=None, act: int = ACT_NONE, residual=None, keep: int = KEEP_INT8):
+    """squant_linear with gradients for x, bias and residual; the pre-activation is kept as `keep` says."""
+    if act != ACT_NONE and keep not in (KEEP_INT8, KEEP_FULL):
+        raise ValueError("keep must be KEEP_INT8 or KEEP_FULL")
+    return _Linear.apply(x, codes, scales, bias, act, residual, keep)
+
+
+def quantized_cross_entropy(h, codes, scales, labels, ignore_index: int = IGNORE_INDEX):
+    """squant_cross_entropy's loss of each row with its gradient for h."""
+    return _CrossEntropy.apply(h, codes, scales, labels, ignore_index)
