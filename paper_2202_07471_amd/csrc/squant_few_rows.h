@@ -75,9 +75,10 @@ __global__ void __launch_bounds__(kFewWaves * kLanes) few_rows(ProductArgs a) {
   }
   for (; b < last; b += kFewWaves) {
     codes16 r[NF];
+    const uint8_t* at[NF];
 #pragma unroll
-    for (int c = 0; c < NF; ++c) 
-      r[c] = load_before<codes16>(w[c] + Codes<FMT>::offset((int64_t)b * kBlock + quad * 16), a.w_end, w_bytes);
+    for (int c = 0; c < NF; ++c) at[c] = w[c] + Codes<FMT>::offset((int64_t)b * kBlock + quad * 16);
+    load_before(r, at, a.w_end, w_bytes);
     multiply(b, r);
   }
 

@@ -220,26 +220,36 @@ __device__ __forceinline__ half8 convert_columns(const typename Codes<FMT>::col4
   return __builtin_bit_cast(half8, v);
 }
 
-// sizeof(V) bytes from p on, where `end` ends the buffer.  Past a row's end they are the next row's, which the
-// callers multiply by zero or do not store; past the buffer's end nothing is read, and the value's upper bytes are
-// zeros.  `bytes` is the whole buffer's size: one below sizeof(V) is read byte by byte.
+// sizeof(V) bytes from each p[i] on, where `end` ends the buffer.  Past a row's end they are the next row's, which
+// the callers multiply by zero or do not store; past the buffer's end nothing is read, and the value's upper bytes
+// are zeros.  `bytes` is the whole buffer's size: one below sizeof(V) is read byte by byte.
 template <class V> struct Shifted { typedef V type; };
 template <> struct Shifted<uint4v> { typedef __uint128_t type; };
 template <> struct Shifted<uint2v> { typedef uint64_t type; };
-template <class V>
-__device__ __forceinline__ V load_before(const uint8_t* p, const uint8_t* end, int64_t bytes) {
+template <class V, int N>
+__device__ __forceinline__ void load_before(V (&o)[N], const uint8_t* const (&p)[N], const uint8_t* end, int64_t bytes) {
   typedef typename Shifted<V>::type U;
   constexpr int n = (int)sizeof(V);
+  U u[N];
   if (bytes < n) {
-    U u = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      u[i] = 0;
 #pragma unroll 1
-    for (int i = 0; i < n; ++i)
-      if (p + i < end) u |= (U)p[i] << (8 * i);
-    return __builtin_bit_cast(V, u);
+      for (int b = 0; b < n; ++b)
+        if (p[i] + b < end) u[i] |= (U)p[i][b] << (8 * b);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) u[i] = load_any<U>(p[i] + n > end ? end - n : p[i]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int64_t past = p[i] + n - end;
+      u[i] = past >= n ? (U)0 : past > 0 ? (U)(u[i] >> (8 * (int)past)) : u[i];
+    }
   }
-  const int64_t back = max((p + n) - end, (ptrdiff_t)0);
-  const U u = load_any<U>(back >= n ? end - n : p - back);
-  return __builtin_bit_cast(V, back >= n ? (U)0 : (U)(u >> (8 * (int)back)));
+#pragma unroll
+  for (int i = 0; i < N; ++i) o[i] = __builtin_bit_cast(V, u[i]);
 }
 
 // ---------------------------------------------------------------------------

@@ -106,8 +106,10 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o.v[i] = load_any<V>(p + i * a.w_row + wsrc[0]);
       } else {
+        const uint8_t* at[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o.v[i] = load_before<V>(p + i * a.w_row + wsrc[0], a.w_end, w_bytes);
+        for (int i = 0; i < 16; ++i) at[i] = p + i * a.w_row + wsrc[0];
+        load_before(o.v, at, a.w_end, w_bytes);
       }
     } else {
       typedef typename Codes<FMT>::row16 V;
@@ -116,8 +118,10 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
 #pragma unroll
         for (int c = 0; c < 4; ++c) o.v[c] = load_any<V>(p + wsrc[c]);
       } else {
+        const uint8_t* at[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) o.v[c] = load_before<V>(p + wsrc[c], a.w_end, w_bytes);
+        for (int c = 0; c < 4; ++c) at[c] = p + wsrc[c];
+        load_before(o.v, at, a.w_end, w_bytes);
       }
     }
   };
@@ -185,14 +189,22 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
     }
     return;
   }
-#pragma unroll
+  // One copy of the epilogue's code: the fragment is picked by uniform branches, so that every register is
+  // named (unrolled eight times it is larger than the instruction cache, indexed it sends the sums to scratch memory).
+#pragma unroll 1
   for (int m = 0; m < S::kFrags; ++m) {
-    __builtin_amdgcn_sched_barrier(0);
+    float4v t[4];
+#pragma unroll
+    for (int j = 0; j < S::kFrags; ++j)
+      if (m == j) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) t[c] = acc[j][c];
+      }
     float v[16];
 #pragma unroll
     for (int c = 0; c < 4; ++c)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[column_of<GRAD>(c, i)] = acc[m][c][i];
+      for (int i = 0; i < 4; ++i) v[column_of<GRAD>(c, i)] = t[c][i];
     const int64_t row = row0 + wave_m * S::kWaveRows + m * 16 + sub;
     if constexpr (GRAD) finish_grad(a.f, row, col0 + quad * 16, v);
     else finish_layer<16, typename OutOf<F, PL>::type>(a.f, row, col0 + quad * 16, v, PL);
