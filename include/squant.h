@@ -213,8 +213,9 @@ int64_t squant_max_channel_elems(int32_t kh, int32_t kw);
  * once.  Rows may be any distance apart (ld*, in elements, at least the row's length); activation
  * buffers need the alignment of their element type, codes none.
  *
- * d_workspace: the *_workspace_bytes call's amount, 256-byte aligned, not shared with a call that may
- * run at the same time; it holds nothing between calls.  rows = 0 is a no-op, apart from d_dbias, which
+ * d_workspace: the *_workspace_bytes call's amount (which depends on the shapes and, through the rows'
+ * alignment, on the address and distance of x or h; 0 for many calls, NULL then), 256-byte aligned, not shared
+ * with a call that may run at the same time; it holds nothing between calls.  rows = 0 is a no-op, apart from d_dbias, which
  * becomes 0.  The calls launch kernels only and may be captured into a HIP graph.  Infinities and NaN in
  * the activations act as IEEE arithmetic has it (an infinity times a code of 0 is NaN, and a row that
  * holds one may be NaN where exact arithmetic has an infinity). */
@@ -249,8 +250,8 @@ typedef enum {
 /* y[m][n] = act(z[m][n]) + residual[m][n],  z[m][n] = scales[n] * sum_k x[m][k] * codes[n][k] + bias[n].
  * d_bias [cout], d_residual [rows][cout] (ldr) and, with SQUANT_KEEP_NONE, d_kept may be NULL;
  * d_kept_scales only with SQUANT_KEEP_INT8.  d_y may be d_residual (ldy == ldr). */
-size_t squant_linear_workspace_bytes(squant_wtype_t type, int64_t rows, const squant_codes_t* h_w,
-                                     squant_keep_t keep);
+size_t squant_linear_workspace_bytes(const void* d_x, int64_t ldx, squant_wtype_t type, int64_t rows,
+                                     const squant_codes_t* h_w, squant_keep_t keep);
 int squant_linear(const void* d_x, int64_t ldx, squant_wtype_t type, int64_t rows,
                   const squant_codes_t* h_w, const void* d_bias, squant_activation_t act,
                   const void* d_residual, int64_t ldr, void* d_y, int64_t ldy, squant_keep_t keep,
@@ -272,7 +273,8 @@ int squant_linear_backward(const void* d_dy, int64_t lddy, squant_wtype_t type, 
  * logits in memory:  l[t][v] = scales[v] * sum_d h[t][d] * codes[v][d],  lse[t] = log sum_v exp l[t][v],
  * loss[t] = lse[t] - l[t][label[t]];  0 where the label is ignore_index, NaN where it is neither that
  * nor in [0, cout).  loss and lse are binary32. */
-size_t squant_cross_entropy_workspace_bytes(squant_wtype_t type, int64_t rows, const squant_codes_t* h_w);
+size_t squant_cross_entropy_workspace_bytes(const void* d_h, int64_t ldh, squant_wtype_t type,
+        int64_t rows, const squant_codes_t* h_w);
 int squant_cross_entropy(const void* d_h, int64_t ldh, squant_wtype_t type, int64_t rows,
                          const squant_codes_t* h_w, const int64_t* d_labels, int64_t ignore_index,
                          float* d_loss, float* d_lse, void* d_workspace, size_t workspace_bytes,
@@ -281,8 +283,8 @@ int squant_cross_entropy(const void* d_h, int64_t ldh, squant_wtype_t type, int6
 /* dh[t][d] = dloss[t] * (sum_v p[t][v] * scales[v] * codes[v][d] - scales[y] * codes[y][d]) with
  * p = exp(l - lse) and y the label (lse of the call above; its own gradient is not taken); 0 where the
  * label is ignore_index.  The vocabulary is walked in pieces whose probabilities fit the workspace. */
-size_t squant_cross_entropy_backward_workspace_bytes(squant_wtype_t type, int64_t rows,
-                                                     const squant_codes_t* h_w);
+size_t squant_cross_entropy_backward_workspace_bytes(const void* d_h, int64_t ldh, squant_wtype_t type,
+        int64_t rows, const squant_codes_t* h_w);
 int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t type, int64_t rows,
                                   const squant_codes_t* h_w, const int64_t* d_labels,
                                   int64_t ignore_index, const float* d_lse, const float* d_dloss,

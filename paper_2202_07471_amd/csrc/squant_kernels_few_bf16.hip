@@ -5,12 +5,16 @@
 namespace squant {
 namespace lin {
 
+namespace {
+template <int NF>
+product_t by_format(int format, int mf) {
+  return format == SQUANT_OUT_INT4 ? few_rows_of<Brain, 1, SQUANT_OUT_INT4, NF>(mf)
+                                   : few_rows_of<Brain, 1, SQUANT_OUT_INT8, NF>(mf);
+}
+}  // namespace
+
 product_t few_bf16(int format, int mf, int nf) {
-  if (nf == 4)
-    return format == SQUANT_OUT_INT4 ? few_rows_of<Brain, 1, SQUANT_OUT_INT4, 4>(mf)
-                                     : few_rows_of<Brain, 1, SQUANT_OUT_INT8, 4>(mf);
-  return format == SQUANT_OUT_INT4 ? few_rows_of<Brain, 1, SQUANT_OUT_INT4, 1>(mf)
-                                   : few_rows_of<Brain, 1, SQUANT_OUT_INT8, 1>(mf);
+  return nf == 4 ? by_format<4>(format, mf) : nf == 2 ? by_format<2>(format, mf) : by_format<1>(format, mf);
 }
 
 }  // namespace lin

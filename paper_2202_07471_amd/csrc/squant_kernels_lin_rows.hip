@@ -56,8 +56,17 @@ __global__ void __launch_bounds__(1024) column_sums(ColumnSumArgs a) {
   const int lane = threadIdx.x & (kLanes - 1), group = threadIdx.x / kLanes;
   const int32_t c = (int32_t)blockIdx.x * kLanes + lane;
   float s = 0.0f;
-  if (c < a.cols)
-    for (int64_t p = group; p < a.partials; p += 16) s += a.partial[p * a.cols + c];
+  if (c < a.cols) {
+    int64_t p = group;
+    for (; p + 7 * 16 < a.partials; p += 8 * 16) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = a.partial[(p + i * 16) * a.cols + c];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += v[i];
+    }
+    for (; p < a.partials; p += 16) s += a.partial[p * a.cols + c];
+  }
   part[group][lane] = s;
   __syncthreads();
   if (group != 0 || c >= a.cols) return;

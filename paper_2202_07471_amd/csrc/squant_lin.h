@@ -263,38 +263,49 @@ constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// erfc(x) exp(x^2) for x >= 0: a polynomial in t = 1 / (1 + x / 2), least squares of the relative error
-// (weights moved towards equal ripples) over x in [0, 10], where erfc leaves binary32's range.  3e-8 in
-// exact arithmetic, 2.9e-7 in binary32.
+// erfc(x) exp(x^2) for x >= 0: a polynomial in t = 1 / (1 + x / 2), least squares of the relative error (weights
+// moved towards equal ripples).  FINE: x in [0, 10], where erfc leaves binary32's range, to 3e-8 in exact arithmetic
+// and 2.9e-7 in binary32.  Otherwise, for 16-bit results: x in [0, 5], to 6.4e-6, a thirtieth of half a binary16
+// step, with 4 multiply-adds less.
+template <bool FINE>
 __device__ __forceinline__ float erfcx_poly(float x) {
   const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.5f, x, 1.0f));
-  float r = -5.505337939e-02f;
-  r = __builtin_fmaf(r, t, 2.639137506e-01f);
-  r = __builtin_fmaf(r, t, -4.415010214e-01f);
-  r = __builtin_fmaf(r, t, 2.212197632e-01f);
-  r = __builtin_fmaf(r, t, 1.705580018e-02f);
-  r = __builtin_fmaf(r, t, 1.812604517e-01f);
-  r = __builtin_fmaf(r, t, 2.497902513e-01f);
-  r = __builtin_fmaf(r, t, 2.810990512e-01f);
-  r = __builtin_fmaf(r, t, 2.822213173e-01f);
-  return __builtin_fmaf(r, t, -6.008548098e-06f);
+  if constexpr (FINE) {
+    float r = -5.505337939e-02f;
+    r = __builtin_fmaf(r, t, 2.639137506e-01f);
+    r = __builtin_fmaf(r, t, -4.415010214e-01f);
+    r = __builtin_fmaf(r, t, 2.212197632e-01f);
+    r = __builtin_fmaf(r, t, 1.705580018e-02f);
+    r = __builtin_fmaf(r, t, 1.812604517e-01f);
+    r = __builtin_fmaf(r, t, 2.497902513e-01f);
+    r = __builtin_fmaf(r, t, 2.810990512e-01f);
+    r = __builtin_fmaf(r, t, 2.822213173e-01f);
+    return __builtin_fmaf(r, t, -6.008548098e-06f);
+  }
+  float r = -2.049253434e-01f;
+  r = __builtin_fmaf(r, t, 5.639148951e-01f);
+  r = __builtin_fmaf(r, t, 1.532078534e-02f);
+  r = __builtin_fmaf(r, t, 3.542144001e-01f);
+  r = __builtin_fmaf(r, t, 2.707676291e-01f);
+  return __builtin_fmaf(r, t, 7.012577262e-04f);
 }
 
-// exp(-z^2 / 2); the square's rounding error would be magnified by the exponent, so it is carried along.
+// exp(-z^2 / 2).  FINE: the square's rounding error would be magnified by the exponent, so it is carried along.
+template <bool FINE>
 __device__ __forceinline__ float exp_half_square(float z) {
   const float c = -0.5f * kLog2E;
-  const float a = z * z;
+  const float a = z * z, e = a * c;
+  if constexpr (!FINE) return exp2_fast(e);
   const float lost = __builtin_fmaf(z, z, -a);
-  const float e = a * c;
   const float tail = __builtin_fmaf(a, c, -e) + (lost * c + a * -9.6299e-9f);
   return e < -160.0f ? 0.0f : exp2_fast(e) * (1.0f + kLn2 * tail);
 }
 
 // The normal distribution's Phi(z), and exp(-z^2 / 2) beside it.
+template <bool FINE>
 __device__ __forceinline__ float normal_cdf(float z, float& density) {
-  const float x = fabsf(z);
-  density = exp_half_square(z);
-  const float tail = 0.5f * erfcx_poly(x * 0.70710678118654752f) * density;
+  density = exp_half_square<FINE>(z);
+  const float tail = 0.5f * erfcx_poly<FINE>(fabsf(z) * 0.70710678118654752f) * density;
   return z < 0.0f ? tail : 1.0f - tail;
 }
 
@@ -302,29 +313,56 @@ __device__ __forceinline__ float sigmoid(float z) {
   return __builtin_amdgcn_rcpf(1.0f + exp2_fast(-kLog2E * z));
 }
 
-__device__ __forceinline__ float activate(float z, int act) {
-  if (act == SQUANT_ACT_RELU) return z < 0.0f ? 0.0f : z;  // a NaN stays
-  if (act == SQUANT_ACT_GELU) {
-    float density;
-    return z * normal_cdf(z, density);
+// N values at a time, so that the choice of activation is made once for them, and four at a time in registers.
+// T: the type of the result.
+__device__ __forceinline__ void after_four(int i) {
+  if ((i & 3) == 3) __builtin_amdgcn_sched_barrier(0);
+}
+template <class T, int N>
+__device__ __forceinline__ void activate(float (&z)[N], int act) {
+  constexpr bool fine = sizeof(T) == 4;
+  if (act == SQUANT_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) z[i] = z[i] < 0.0f ? 0.0f : z[i];  // a NaN stays
+  } else if (act == SQUANT_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float density;
+      z[i] *= normal_cdf<fine>(z[i], density);
+      after_four(i);
+    }
+  } else if (act == SQUANT_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      z[i] *= sigmoid(z[i]);
+      after_four(i);
+    }
   }
-  if (act == SQUANT_ACT_SILU) return z * sigmoid(z);
-  return z;
 }
 
-__device__ __forceinline__ float slope(float z, int act) {
-  if (act == SQUANT_ACT_RELU) return z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;
-  if (act == SQUANT_ACT_GELU) {
-    float density;
-    const float cdf = normal_cdf(z, density);
-    const float d = 0.3989422804014327f * density;
-    return d > 0.0f ? __builtin_fmaf(z, d, cdf) : cdf + 0.0f * d;  // z may be infinite where the density is 0
+// v *= act'(z)
+template <class T, int N>
+__device__ __forceinline__ void apply_slope(float (&v)[N], const float (&z)[N], int act) {
+  constexpr bool fine = sizeof(T) == 4;
+  if (act == SQUANT_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] *= z[i] > 0.0f ? 1.0f : z[i] <= 0.0f ? 0.0f : z[i];
+  } else if (act == SQUANT_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float density;
+      const float cdf = normal_cdf<fine>(z[i], density);
+      const float d = 0.3989422804014327f * density;
+      v[i] *= d > 0.0f ? __builtin_fmaf(z[i], d, cdf) : cdf + 0.0f * d;  // z may be infinite where the density is 0
+    }
+  } else if (act == SQUANT_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      // q = 1 - p without its cancellation
+      const float p = sigmoid(z[i]), q = sigmoid(-z[i]);
+      v[i] *= p > 0.0f && q > 0.0f ? p * __builtin_fmaf(z[i], q, 1.0f) : p;
+    }
   }
-  if (act == SQUANT_ACT_SILU) {
-    const float p = sigmoid(z), q = sigmoid(-z);  // q = 1 - p without its cancellation
-    return p > 0.0f && q > 0.0f ? p * __builtin_fmaf(z, q, 1.0f) : p;
-  }
-  return 1.0f;
 }
 
 // Largest magnitude by the bits: a NaN is larger than any number and stays.
@@ -368,23 +406,36 @@ __device__ __forceinline__ void store_cols(T* p, const float (&o)[NC], int valid
   }
 }
 
+// What a lane's columns share over the rows: loaded once.
+template <int NC> struct Columns {
+  float scale[NC], bias[NC];
+};
+template <int NC, class T>
+__device__ __forceinline__ void load_columns(Columns<NC>& k, const Finish& f, int32_t col) {
+  const int valid = min(max(f.cols - col, 0), NC);
+  load_cols<NC, float>(k.scale, f.scales + col, valid);
+#pragma unroll
+  for (int i = 0; i < NC; ++i) k.bias[i] = 0.0f;
+  if (f.kind == kLinear && f.bias) load_cols<NC, T>(k.bias, (const T*)f.bias + col, valid);
+}
+
 // A lane's NC consecutive columns of one row, `v` the bare sums.  With NC = 16 the lanes l, l^16, l^32, l^48
 // hold the row's 64 columns of one tile (every lane of the wave calls).  T: the output's type.
 template <int NC, class T>
-__device__ __forceinline__ void finish_layer(const Finish& f, int64_t row, int32_t col, float (&v)[NC], int planes) {
+__device__ __forceinline__ void finish_layer(const Finish& f, const Columns<NC>& k, int64_t row, int32_t col, float (&v)[NC],
+                                             int planes) {
   const bool live = row < f.rows;
   const int valid = live ? min(max(f.cols - col, 0), NC) : 0;
   const float factor = f.unit * (f.row_factor && live ? f.row_factor[row] : 1.0f);
   float s[NC];
-  load_cols<NC, float>(s, f.scales + col, valid);
+  const bool add = f.kind == kLinear && f.residual;
+  if (add) load_cols<NC, T>(s, (const T*)f.residual + row * f.ldr + col, valid);
+  // the scale first: a large row's factor alone may overflow
 #pragma unroll
-  for (int i = 0; i < NC; ++i) v[i] = v[i] * s[i] * factor;  // the scale first: a large row's factor alone may overflow
+  for (int i = 0; i < NC; ++i) v[i] = v[i] * k.scale[i] * factor;
   if (f.kind == kLinear) {
-    if (f.bias) {
-      load_cols<NC, T>(s, (const T*)f.bias + col, valid);
 #pragma unroll
-      for (int i = 0; i < NC; ++i) v[i] += s[i];
-    }
+    for (int i = 0; i < NC; ++i) v[i] += k.bias[i];
     if constexpr (NC == 16) {
       if (f.keep == SQUANT_KEEP_FULL) store_cols<NC, T>((T*)f.kept + row * f.cols + col, v, valid);
       if (f.keep == SQUANT_KEEP_INT8) {
@@ -406,20 +457,18 @@ __device__ __forceinline__ void finish_layer(const Finish& f, int64_t row, int32
             q[d] |= ((uint32_t)(int)c & 255u) << (8 * b);
           }
         }
-        int8_t* k = (int8_t*)f.kept + row * f.cols + col;
+        int8_t* out = (int8_t*)f.kept + row * f.cols + col;
         if (valid >= NC) {
-          store_any(k, uint4v{q[0], q[1], q[2], q[3]});
+          store_any(out, uint4v{q[0], q[1], q[2], q[3]});
         } else {
 #pragma unroll
           for (int i = 0; i < NC; ++i)
-            if (i < valid) k[i] = (int8_t)(q[i >> 2] >> (8 * (i & 3)));
+            if (i < valid) out[i] = (int8_t)(q[i >> 2] >> (8 * (i & 3)));
         }
       }
     }
-#pragma unroll
-    for (int i = 0; i < NC; ++i) v[i] = activate(v[i], f.act);
-    if (f.residual) {
-      load_cols<NC, T>(s, (const T*)f.residual + row * f.ldr + col, valid);
+    activate<T, NC>(v, f.act);
+    if (add) {
 #pragma unroll
       for (int i = 0; i < NC; ++i) v[i] += s[i];
     }
@@ -461,7 +510,7 @@ __device__ __forceinline__ void finish_layer(const Finish& f, int64_t row, int32
       float lo[NC];
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
-        v[i] = i < valid ? exp2_fast(__builtin_fmaf(v[i], kLog2E, -l2)) * (s[i] * unit) : 0.0f;
+        v[i] = i < valid ? exp2_fast(__builtin_fmaf(v[i], kLog2E, -l2)) * (k.scale[i] * unit) : 0.0f;
         lo[i] = v[i] - (float)(_Float16)v[i];
       }
       store_cols<NC, _Float16>(p, v, NC);

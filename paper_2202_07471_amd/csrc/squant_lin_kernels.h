@@ -6,7 +6,7 @@
 namespace squant {
 namespace lin {
 
-// `mt` 64, 128 or 256 rows a workgroup; `mf` fragments of 16 rows, 1, 2 or 4; `nf` of 16 columns, 1 or 4.
+// `mt` 64, 128 or 256 rows a workgroup; `mf` fragments of 16 rows, 1, 2 or 4; `nf` of 16 columns, 1, 2 or 4.
 product_t layer_bf16(int format, int mt);
 product_t layer_f16(int format, int mt);
 product_t layer_f32(int format, int mt);

@@ -33,6 +33,10 @@ inline int shape_threads(int mt) {
   return mt == 256 ? Shape<256>::kThreads : mt == 128 ? Shape<128>::kThreads : Shape<64>::kThreads;
 }
 
+inline int shape_depth(int mt) {
+  return mt == 256 ? Shape<256>::kDepth : mt == 128 ? Shape<128>::kDepth : Shape<64>::kDepth;
+}
+
 // `product` over rows x cols with a contraction of `depth`: the rows of a workgroup and the slices of the
 // contraction by an estimate of the time.  The coefficients are fitted to measured times.
 inline Split split_product(int64_t rows, int64_t cols, int64_t depth, int planes, bool may_split) {
@@ -57,7 +61,7 @@ inline Split split_product(int64_t rows, int64_t cols, int64_t depth, int planes
   best.blocks = blocks;
   best.workgroups = (int64_t)best.tiles_m * best.tiles_n;
   best.threads = shape_threads(best.mt);
-  best.lds = (size_t)best.mt * kBlock * 2 * planes * 2;
+  best.lds = (size_t)best.mt * kBlock * 2 * planes * shape_depth(best.mt);
   best.row_frags_all = (int64_t)best.tiles_m * (best.mt / 16);
   best.col_frags_all = (int64_t)best.tiles_n * (kWide / 16);
   return best;
@@ -69,14 +73,15 @@ inline Split split_layer(int64_t rows, int64_t cols, int64_t depth, int planes, 
   Split p{};
   p.few = true;
   p.row_frags = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  p.col_frags_each = tiled ? 4 : 1;
+  // wide workgroups read their rows fewer times, narrow ones fill the chip
+  p.col_frags_each = tiled || cols >= 32 * 1024 ? 4 : cols >= 8 * 1024 ? 2 : 1;
   p.blocks = (int)((depth + kBlock - 1) / kBlock);
   p.slices = 1;
   p.tiles_m = p.row_frags;
   p.tiles_n = (int)((cols + 16 * p.col_frags_each - 1) / (16 * p.col_frags_each));
   p.workgroups = p.tiles_n;
-  p.threads = kFewWaves * kLanes;
-  p.lds = (size_t)kFewWaves * p.row_frags * p.col_frags_each * kLanes * 16;
+  p.threads = few_waves(p.row_frags, p.col_frags_each) * kLanes;
+  p.lds = few_lds(p.row_frags, p.col_frags_each);
   p.row_frags_all = p.row_frags;
   p.col_frags_all = (int64_t)p.tiles_n * p.col_frags_each;
   return p;

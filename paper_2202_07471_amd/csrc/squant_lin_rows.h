@@ -104,6 +104,7 @@ __global__ void __launch_bounds__(kRowThreads) gradient_rows(RowsArgs a) {
     load_cols<8, float>(s, a.scales + c, valid);
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+#pragma unroll 2
     for (int r = share; r < n_rows; r += shares) {
       const int64_t row = row0 + r;
       const float up = power_of_two(exponent[r]);
@@ -112,14 +113,14 @@ __global__ void __launch_bounds__(kRowThreads) gradient_rows(RowsArgs a) {
       if (a.keep == SQUANT_KEEP_FULL) {
         float z[8];
         load_cols<8, T>(z, (const T*)a.kept + row * a.cols + c, valid);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= slope(z[i], a.act);
+        apply_slope<T, 8>(v, z, a.act);
       } else if (a.keep == SQUANT_KEEP_INT8) {
         float z[8];
         const float unit = valid ? a.kept_scales[row * chunks + c / kTile] : 0.0f;
         load_cols<8, int8_t>(z, (const int8_t*)a.kept + row * a.cols + c, valid);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= slope(z[i] * unit, a.act);
+        for (int i = 0; i < 8; ++i) z[i] *= unit;
+        apply_slope<T, 8>(v, z, a.act);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -176,7 +177,11 @@ __global__ void __launch_bounds__(kRowThreads) join(JoinArgs a) {
   const int64_t row = rf * 16 + (lane & 15);
   const int32_t col = (int32_t)tile * kTile + (lane >> 4) * 16;
   if constexpr (GRAD) finish_grad(a.f, row, col, v);
-  else finish_layer<16, T>(a.f, row, col, v, a.planes);
+  else {
+    Columns<16> columns;
+    load_columns<16, T>(columns, a.f, col);
+    finish_layer<16, T>(a.f, columns, row, col, v, a.planes);
+  }
 }
 
 struct LossArgs {

@@ -89,18 +89,19 @@ struct RowOperand {
   const float* factor;
 };
 
-bool direct_rows(const void* x, int64_t ldx, int type, int32_t cin) {
-  return type != SQUANT_W_F32 && cin % kBlock == 0 && ldx % 8 == 0 && !misaligned(x, 16);
+// few_rows reads 16-bit rows at any alignment and of any length.
+bool direct_rows(const void* x, int64_t ldx, int type, int64_t rows, int32_t cin) {
+  if (type == SQUANT_W_F32) return false;
+  return rows <= kFewRows || (cin % kBlock == 0 && ldx % 8 == 0 && !misaligned(x, 16));
 }
 
-// Takes the workspace of a copy whether or not this call needs one: the size call does not see the pointers.
 RowOperand lay_out_rows(Cutter& c, const void* x, int64_t ldx, int type, int64_t rows, int32_t cin, RowsArgs& r, bool& copy) {
+  copy = !direct_rows(x, ldx, type, rows, cin);
+  if (!copy) return RowOperand{x, ldx, 0, nullptr};
   const int planes = planes_of(type);
   const int64_t padded = ((int64_t)cin + kBlock - 1) / kBlock * kBlock;
   uint16_t* out = c.take<uint16_t>(rows * planes * padded);
   float* factor = type == SQUANT_W_F32 ? c.take<float>(rows) : nullptr;
-  copy = !direct_rows(x, ldx, type, cin);
-  if (!copy) return RowOperand{x, ldx, 0, nullptr};
   r.x = x; r.ldx = ldx; r.rows = rows; r.cols = cin; r.out = out; r.padded = (int32_t)padded; r.row_factor = factor;
   return RowOperand{out, planes * padded, padded, factor};
 }
@@ -137,7 +138,7 @@ size_t lay_out_linear(void* ws, const void* x, int64_t ldx, int type, int64_t ro
   return c.used;
 }
 
-int gradient_rows_per_group(int64_t rows) { return (int)std::min<int64_t>(16, std::max<int64_t>(1, (rows + 511) / 512)); }
+int gradient_rows_per_group(int64_t rows) { return (int)std::min<int64_t>(16, std::max<int64_t>(1, (rows + 1023) / 1024)); }
 
 struct BackwardSpace { _Float16* rows; float* factor; float* sums; int64_t partials; int64_t padded; float4v* partial; Split p; };
 size_t lay_out_backward(void* ws, int type, int64_t rows, const squant_codes_t& w, BackwardSpace& s) {
@@ -185,10 +186,10 @@ size_t lay_out_loss_backward(void* ws, const void* h, int64_t ldh, int type, int
 
 extern "C" {
 
-size_t squant_linear_workspace_bytes(squant_wtype_t type, int64_t rows, const squant_codes_t* h_w, squant_keep_t keep) {
+size_t squant_linear_workspace_bytes(const void* d_x, int64_t ldx, squant_wtype_t type, int64_t rows, const squant_codes_t* h_w, squant_keep_t keep) {
   if (check_rows((int)type, rows) || check_codes(h_w) || rows == 0) return 0;
   LinearSpace s;
-  return lay_out_linear(nullptr, nullptr, 0, (int)type, rows, *h_w, (int)keep, s);
+  return lay_out_linear(nullptr, d_x, ldx, (int)type, rows, *h_w, (int)keep, s);
 }
 
 int squant_linear(const void* d_x, int64_t ldx, squant_wtype_t type, int64_t rows, const squant_codes_t* h_w,
@@ -278,10 +279,10 @@ int squant_linear_backward(const void* d_dy, int64_t lddy, squant_wtype_t type, 
   return s.p.slices > 1 ? launch_join(true, (int)type, s.p, s.p.slices, s.partial, done, st) : SQUANT_OK;
 }
 
-size_t squant_cross_entropy_workspace_bytes(squant_wtype_t type, int64_t rows, const squant_codes_t* h_w) {
+size_t squant_cross_entropy_workspace_bytes(const void* d_h, int64_t ldh, squant_wtype_t type, int64_t rows, const squant_codes_t* h_w) {
   if (check_rows((int)type, rows) || check_codes(h_w) || rows == 0) return 0;
   LossSpace s;
-  return lay_out_loss(nullptr, nullptr, 0, (int)type, rows, *h_w, s);
+  return lay_out_loss(nullptr, d_h, ldh, (int)type, rows, *h_w, s);
 }
 
 int squant_cross_entropy(const void* d_h, int64_t ldh, squant_wtype_t type, int64_t rows, const squant_codes_t* h_w,
@@ -313,10 +314,10 @@ int squant_cross_entropy(const void* d_h, int64_t ldh, squant_wtype_t type, int6
   return launch(loss_rows_kernel(), (rows + per - 1) / per, 1, kRowThreads, 0, st, l);
 }
 
-size_t squant_cross_entropy_backward_workspace_bytes(squant_wtype_t type, int64_t rows, const squant_codes_t* h_w) {
+size_t squant_cross_entropy_backward_workspace_bytes(const void* d_h, int64_t ldh, squant_wtype_t type, int64_t rows, const squant_codes_t* h_w) {
   if (check_rows((int)type, rows) || check_codes(h_w) || rows == 0) return 0;
   LossBackwardSpace s;
-  return lay_out_loss_backward(nullptr, nullptr, 0, (int)type, rows, *h_w, s);
+  return lay_out_loss_backward(nullptr, d_h, ldh, (int)type, rows, *h_w, s);
 }
 
 int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t type, int64_t rows, const squant_codes_t* h_w,

@@ -21,6 +21,8 @@ template <int MT> struct Shape {
   static constexpr int kWaves = kWavesM * (kWide / kTile);
   static constexpr int kThreads = kWaves * kLanes;
   static constexpr int kFrags = kWaveRows / 16;
+  // Steps in flight or at work: a step of 256 rows takes longer than memory's latency, one of 64 rows a quarter.
+  static constexpr int kDepth = MT == 256 ? 2 : MT == 128 ? 3 : 4;
 };
 
 // 16 bytes a lane from memory to LDS bytes [lds, lds + 1024), in lane order.
@@ -154,27 +156,37 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
         }
     }
   };
-  // Every load of a step was issued a step earlier; the barrier also says that the other buffer is read out.
-  auto arrived = [&]() {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  // A step's loads were issued kDepth - 1 steps earlier; the barrier also says that the buffer to be loaded next is
+  // read out.  While later steps' loads are on their way only this one's are waited for.
+  constexpr int kIssued = kLoads * PL + (GRAD ? 16 : 4);
+  auto arrived = [&](bool more) {
+    if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kIssued * (S::kDepth - 2)) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   };
 
-  if (first < last) {
-    Raw<FMT, GRAD> now, next;
-    load_rows(first, 0);
-    load_codes(first, now);
-    next = now;
+  Raw<FMT, GRAD> raw[S::kDepth];
+#pragma unroll
+  for (int i = 0; i < S::kDepth - 1; ++i)
+    if (first + i < last) {
+      load_rows(first + i, i);
+      load_codes(first + i, raw[i]);
+    }
 #pragma unroll 1
-    for (int b = first; b < last; ++b) {
-      const int buf = (b - first) & 1;
-      arrived();
-      if (b + 1 < last) {
-        load_rows(b + 1, buf ^ 1);
-        load_codes(b + 1, next);
+  for (int b0 = first; b0 < last; b0 += S::kDepth) {
+#pragma unroll
+    for (int i = 0; i < S::kDepth; ++i) {
+      const int b = b0 + i, ahead = b + S::kDepth - 1;
+      constexpr int D = S::kDepth;
+      if (b < last) {
+        // at the buffer's end loads are not counted: everything is waited for
+        arrived(ahead < last && ahead - 1 < inside);
+        if (ahead < last) {
+          load_rows(ahead, (i + D - 1) % D);
+          load_codes(ahead, raw[(i + D - 1) % D]);
+        }
+        multiply(i, raw[i]);
       }
-      multiply(buf, now);
-      now = next;
     }
   }
 
@@ -191,6 +203,19 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
   }
   // One copy of the epilogue's code: the fragment is picked by uniform branches, so that every register is
   // named (unrolled eight times it is larger than the instruction cache, indexed it sends the sums to scratch memory).
+  typedef typename OutOf<F, PL>::type T;
+  // The columns' scales and biases wait in the LDS, where they cost no registers beside the sums.
+  float* shared_columns = reinterpret_cast<float*>(smem);  // [2][kWide]
+  if constexpr (!GRAD) {
+    __syncthreads();
+    if (threadIdx.x < kWide) {
+      Columns<1> one;
+      load_columns<1, T>(one, a.f, tile_n * kWide + (int)threadIdx.x);
+      shared_columns[threadIdx.x] = one.scale[0];
+      shared_columns[kWide + threadIdx.x] = one.bias[0];
+    }
+    __syncthreads();
+  }
 #pragma unroll 1
   for (int m = 0; m < S::kFrags; ++m) {
     float4v t[4];
@@ -206,8 +231,17 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[column_of<GRAD>(c, i)] = t[c][i];
     const int64_t row = row0 + wave_m * S::kWaveRows + m * 16 + sub;
-    if constexpr (GRAD) finish_grad(a.f, row, col0 + quad * 16, v);
-    else finish_layer<16, typename OutOf<F, PL>::type>(a.f, row, col0 + quad * 16, v, PL);
+    if constexpr (GRAD) {
+      finish_grad(a.f, row, col0 + quad * 16, v);
+    } else {
+      Columns<16> columns;
+      asm volatile("" ::: "memory");  // read again for each fragment
+#pragma unroll
+      for (int i = 0; i < 16; ++i) columns.scale[i] = shared_columns[wave_n * kTile + quad * 16 + i];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) columns.bias[i] = shared_columns[kWide + wave_n * kTile + quad * 16 + i];
+      finish_layer<16, T>(a.f, columns, row, col0 + quad * 16, v, PL);
+    }
   }
 }
 

@@ -40,9 +40,10 @@ def _lib():
         L.squant_linear_backward.argtypes = [vp, i64, en, i64, cp, en, en, vp, vp, vp, i64, vp, vp, sz, vp]
         L.squant_cross_entropy.argtypes = [vp, i64, en, i64, cp, vp, i64, vp, vp, vp, sz, vp]
         L.squant_cross_entropy_backward.argtypes = [vp, i64, en, i64, cp, vp, i64, vp, vp, vp, i64, vp, sz, vp]
-        L.squant_linear_workspace_bytes.argtypes = [en, i64, cp, en]
-        for f in ("linear_backward", "cross_entropy", "cross_entropy_backward"):
-            getattr(L, f"squant_{f}_workspace_bytes").argtypes = [en, i64, cp]
+        L.squant_linear_workspace_bytes.argtypes = [vp, i64, en, i64, cp, en]
+        L.squant_linear_backward_workspace_bytes.argtypes = [en, i64, cp]
+        L.squant_cross_entropy_workspace_bytes.argtypes = [vp, i64, en, i64, cp]
+        L.squant_cross_entropy_backward_workspace_bytes.argtypes = [vp, i64, en, i64, cp]
         for f in ("linear", "linear_backward", "cross_entropy", "cross_entropy_backward"):
             getattr(L, f"squant_{f}").restype = en
             getattr(L, f"squant_{f}_workspace_bytes").restype = sz
@@ -50,11 +51,12 @@ def _lib():
     return _ready
 
 
-@lru_cache(maxsize=1024)
-def _workspace_bytes(call: str, type_: int, rows: int, cout: int, cin: int, fmt: int, *rest: int) -> int:
-    # the size depends on the shapes alone: the pointers only have to be there
+@lru_cache(maxsize=4096)
+def _workspace_bytes(call: str, aligned, type_: int, rows: int, cout: int, cin: int, fmt: int, *rest: int) -> int:
+    # the size depends on the shapes and on whether the rows are aligned to 16 bytes: addresses that stand for both
     w = squant_codes_t(256, 256, cout, cin, fmt)
-    return int(getattr(_lib(), f"squant_{call}_workspace_bytes")(type_, rows, ctypes.byref(w), *rest))
+    x = () if aligned is None else (256, -(-cin // 8) * 8) if aligned else (256, cin | 1)
+    return int(getattr(_lib(), f"squant_{call}_workspace_bytes")(*x, type_, rows, ctypes.byref(w), *rest))
 
 
 def _workspace(x: torch.Tensor, nbytes: int, stream) -> Optional[torch.Tensor]:
@@ -143,7 +145,7 @@ def squant_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bi
     elif how == KEEP_FULL:
         kept = torch.empty(shape, dtype=x.dtype, device=x.device)
     type_ = _WTYPES[x.dtype]
-    nbytes = _workspace_bytes("linear", type_, rows, cout, cin, w.format, how)
+    nbytes = _workspace_bytes("linear", (ldx | x.data_ptr() >> 1) & 7 == 0, type_, rows, cout, cin, w.format, how)
     ws = _workspace(x, nbytes, stream)
     _check(_lib().squant_linear(x.data_ptr(), ldx, type_, rows, ctypes.byref(w), _ptr(bias), act, _ptr(residual), ldr,
                                 out.data_ptr(), ldy, how, _ptr(kept), _ptr(kept_scales), _ptr(ws), nbytes,
@@ -181,7 +183,7 @@ def squant_linear_backward(dy: torch.Tensor, codes: torch.Tensor, scales: torch.
         lddx = _rows(dx, cin, "dx", dy)[1]
     dbias = torch.empty(cout, dtype=dy.dtype, device=dy.device) if bias else None
     type_ = _WTYPES[dy.dtype]
-    nbytes = _workspace_bytes("linear_backward", type_, rows, cout, cin, w.format)
+    nbytes = _workspace_bytes("linear_backward", None, type_, rows, cout, cin, w.format)
     ws = _workspace(dy, nbytes, stream)
     _check(_lib().squant_linear_backward(dy.data_ptr(), lddy, type_, rows, ctypes.byref(w), act, how, _ptr(z),
                                          _ptr(z_scales), dx.data_ptr(), lddx, _ptr(dbias), _ptr(ws), nbytes,
@@ -207,7 +209,7 @@ def squant_cross_entropy(h: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
     loss = torch.empty(h.shape[:-1], dtype=torch.float32, device=h.device)
     lse = torch.empty_like(loss)
     type_ = _WTYPES[h.dtype]
-    nbytes = _workspace_bytes("cross_entropy", type_, rows, w.cout, cin, w.format)
+    nbytes = _workspace_bytes("cross_entropy", (ldh | h.data_ptr() >> 1) & 7 == 0, type_, rows, w.cout, cin, w.format)
     ws = _workspace(h, nbytes, stream)
     _check(_lib().squant_cross_entropy(h.data_ptr(), ldh, type_, rows, ctypes.byref(w), labels.data_ptr(),
                                        ignore_index, loss.data_ptr(), lse.data_ptr(), _ptr(ws), nbytes,
@@ -231,7 +233,7 @@ def squant_cross_entropy_backward(h: torch.Tensor, codes: torch.Tensor, scales: 
     else:
         lddh = _rows(dh, cin, "dh", h)[1]
     type_ = _WTYPES[h.dtype]
-    nbytes = _workspace_bytes("cross_entropy_backward", type_, rows, w.cout, cin, w.format)
+    nbytes = _workspace_bytes("cross_entropy_backward", (ldh | h.data_ptr() >> 1) & 7 == 0, type_, rows, w.cout, cin, w.format)
     ws = _workspace(h, nbytes, stream)
     _check(_lib().squant_cross_entropy_backward(h.data_ptr(), ldh, type_, rows, ctypes.byref(w), labels.data_ptr(),
                                                 ignore_index, lse.data_ptr(), dloss.data_ptr(), dh.data_ptr(), lddh,

@@ -59,10 +59,10 @@ def test_codes(L):
         assert L.squant_linear_backward(P, 8, 0, 4, w, 0, 0, None, None, P, 64, P, WS, BIG, None) == want
         assert L.squant_cross_entropy(P, 64, 0, 4, w, P, -100, P, P, WS, BIG, None) == want
         assert L.squant_cross_entropy_backward(P, 64, 0, 4, w, P, -100, P, P, P, 64, WS, BIG, None) == want
-        assert L.squant_linear_workspace_bytes(0, 4, w, 0) == 0
+        assert L.squant_linear_workspace_bytes(P, 64, 0, 4, w, 0) == 0
         assert L.squant_linear_backward_workspace_bytes(0, 4, w) == 0
-        assert L.squant_cross_entropy_workspace_bytes(0, 4, w) == 0
-        assert L.squant_cross_entropy_backward_workspace_bytes(0, 4, w) == 0
+        assert L.squant_cross_entropy_workspace_bytes(P, 64, 0, 4, w) == 0
+        assert L.squant_cross_entropy_backward_workspace_bytes(P, 64, 0, 4, w) == 0
     assert linear(L, w=ctypes.POINTER(type(codes()._obj))()) == NULL
 
 
@@ -101,8 +101,8 @@ def test_workspaces_grow_with_the_rows(L):
         assert 0 < sizes[0] < sizes[1] < sizes[2]
         # the pieces of the probabilities bound what a long batch needs beside its rows
         w = codes(65536, 64)
-        assert L.squant_cross_entropy_backward_workspace_bytes(type_, 16384, w) < 1 << 30
-    assert L.squant_linear_workspace_bytes(0, 0, codes(), 0) == 0
+        assert L.squant_cross_entropy_backward_workspace_bytes(P, 64, type_, 16384, w) < 1 << 30
+    assert L.squant_linear_workspace_bytes(P, 64, 0, 0, codes(), 0) == 0
 
 
 def test_the_binding_refuses():
