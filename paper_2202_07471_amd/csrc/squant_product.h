@@ -83,15 +83,18 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
   };
 
   // Codes.  For a layer each lane reads 16 codes of 4 rows; for a gradient 4 columns of 16 rows, lanes whose columns
-  // do not exist those of the row's last bytes.  `inside`: blocks whose reads stay in the buffer.
+  // do not exist those of the row's last bytes.  `inside`: blocks that no read leaves the buffer for.
   const int64_t w_bytes = (int64_t)a.w_rows * a.w_row;
   uint32_t wsrc[GRAD ? 1 : 4];
   const uint8_t* w_base = a.w;
   int inside;
   if constexpr (GRAD) {
-    const uint32_t at = (uint32_t)min(Codes<FMT>::offset(col0 + 4 * sub), a.w_row - 1);
+    constexpr int n = (int)sizeof(typename Codes<FMT>::col4);
+    // a row's last load may pass its end by less than n bytes
+    const bool even = a.w_row % n == 0;
+    const uint32_t at = (uint32_t)min(Codes<FMT>::offset(col0 + 4 * sub), a.w_row - (even ? n : 1));
     wsrc[0] = (uint32_t)quad * 16 * (uint32_t)a.w_row + at;
-    inside = (int)max((w_bytes - 4) / (kBlock * a.w_row), (int64_t)0);
+    inside = (int)max((w_bytes - (even ? 0 : n - 1)) / (kBlock * a.w_row), (int64_t)0);
   } else {
     w_base += (int64_t)min(col0, a.w_rows - 1) * a.w_row;
 #pragma unroll
@@ -102,30 +105,24 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
   }
   auto load_codes = [&](int b, Raw<FMT, GRAD>& o) {
     if constexpr (GRAD) {
-      typedef typename Codes<FMT>::col4 V;
       const uint8_t* p = w_base + (int64_t)b * kBlock * a.w_row;
-      if (b < inside) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o.v[i] = load_any<V>(p + i * a.w_row + wsrc[0]);
-      } else {
-        const uint8_t* at[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) at[i] = p + i * a.w_row + wsrc[0];
-        load_before(o.v, at, a.w_end, w_bytes);
-      }
+      for (int i = 0; i < 16; ++i) o.v[i] = load_any<typename Codes<FMT>::col4>(p + i * a.w_row + wsrc[0]);
     } else {
-      typedef typename Codes<FMT>::row16 V;
       const uint8_t* p = w_base + Codes<FMT>::offset((int64_t)b * kBlock);
-      if (b < inside) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) o.v[c] = load_any<V>(p + wsrc[c]);
-      } else {
-        const uint8_t* at[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) at[c] = p + wsrc[c];
-        load_before(o.v, at, a.w_end, w_bytes);
-      }
+      for (int c = 0; c < 4; ++c) o.v[c] = load_any<typename Codes<FMT>::row16>(p + wsrc[c]);
     }
+  };
+  // the same at the buffer's end
+  auto load_last_codes = [&](int b, Raw<FMT, GRAD>& o) {
+    constexpr int n = GRAD ? 16 : 4;
+    const uint8_t* at[n];
+#pragma unroll
+    for (int i = 0; i < n; ++i)
+      at[i] = GRAD ? w_base + ((int64_t)b * kBlock + i) * a.w_row + wsrc[0]
+                   : w_base + Codes<FMT>::offset((int64_t)b * kBlock) + wsrc[GRAD ? 0 : i];
+    load_before(o.v, at, a.w_end, w_bytes);
   };
 
   float4v acc[S::kFrags][4];
@@ -156,38 +153,48 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
         }
     }
   };
-  // A step's loads were issued kDepth - 1 steps earlier; the barrier also says that the buffer to be loaded next is
-  // read out.  While later steps' loads are on their way only this one's are waited for.
+  // A step's loads are issued kDepth - 1 steps before it, without branches around them, so that what is on its way
+  // can be counted: past the last step the last block is loaded again, and not multiplied.  (With a branch around
+  // them the compiler waits for everything before it touches a step's codes.)  The barrier also says that the buffer
+  // to be loaded next is read out.
+  constexpr int D = S::kDepth;
   constexpr int kIssued = kLoads * PL + (GRAD ? 16 : 4);
-  auto arrived = [&](bool more) {
-    if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kIssued * (S::kDepth - 2)) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-  };
-
-  Raw<FMT, GRAD> raw[S::kDepth];
+  constexpr int kOthers = kIssued * (D - 2);  // may be on their way when a step begins
+  static_assert(kOthers < 64, "the wait counter has six bits");
+  const int steady = min(last, inside);
+  if (first < steady) {
+    Raw<FMT, GRAD> raw[D];
 #pragma unroll
-  for (int i = 0; i < S::kDepth - 1; ++i)
-    if (first + i < last) {
-      load_rows(first + i, i);
-      load_codes(first + i, raw[i]);
+    for (int i = 0; i < D - 1; ++i) {
+      load_rows(min(first + i, steady - 1), i);
+      load_codes(min(first + i, steady - 1), raw[i]);
     }
 #pragma unroll 1
-  for (int b0 = first; b0 < last; b0 += S::kDepth) {
+    for (int b0 = first; b0 < steady; b0 += D) {
 #pragma unroll
-    for (int i = 0; i < S::kDepth; ++i) {
-      const int b = b0 + i, ahead = b + S::kDepth - 1;
-      constexpr int D = S::kDepth;
-      if (b < last) {
-        // at the buffer's end loads are not counted: everything is waited for
-        arrived(ahead < last && ahead - 1 < inside);
-        if (ahead < last) {
-          load_rows(ahead, (i + D - 1) % D);
-          load_codes(ahead, raw[(i + D - 1) % D]);
-        }
-        multiply(i, raw[i]);
+      for (int i = 0; i < D; ++i) {
+        // not __syncthreads(), which would wait for every load
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt((kOthers & 15) | (kOthers >> 4) << 14 | 0x070);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const int ahead = min(b0 + i + D - 1, steady - 1);
+        load_rows(ahead, (i + D - 1) % D);
+        load_codes(ahead, raw[(i + D - 1) % D]);
+        if (b0 + i < steady) multiply(i, raw[i]);
       }
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  }
+  for (int b = max(first, steady); b < last; ++b) {  // what ends within a block
+    Raw<FMT, GRAD> raw;
+    load_rows(b, 0);
+    load_last_codes(b, raw);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    multiply(0, raw);
+    __syncthreads();
   }
 
   if (a.f.kind == kPartial) {
