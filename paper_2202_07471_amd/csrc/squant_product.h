@@ -131,26 +131,35 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
 #pragma unroll
     for (int c = 0; c < 4; ++c) acc[m][c] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
 
+  auto operand = [&](const Raw<FMT, GRAD>& r, int h, int c) {
+    if constexpr (GRAD) return convert_columns<FMT>(r.v + 8 * h, c);
+    else return convert<F, FMT>(r.v[c], h);
+  };
+  auto row_frag = [&](int buf, int p, int h, int m) {
+    return *(const typename F::frag*)(smem + buf * kBufBytes + p * kPlaneBytes + m * 2048 + wave_m * S::kWaveRows * 128 +
+                                      sub * 128 + (((quad * 2 + h) ^ (sub & 7)) << 4));
+  };
+  // A half step is 16 fragments of products a fragment of rows; the next fragment of rows is read, and the next
+  // half's codes are converted, between them.
   auto multiply = [&](int buf, const Raw<FMT, GRAD>& r) {
+    constexpr int kSteps = 2 * PL * S::kFrags;
+    typename F::frag w[2][4], x[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      __builtin_amdgcn_sched_barrier(0);  // one half's operands at a time in registers
-      typename F::frag w[4];
+    for (int c = 0; c < 4; ++c) w[0][c] = operand(r, 0, c);
+    x[0] = row_frag(buf, 0, 0, 0);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        if constexpr (GRAD) w[c] = convert_columns<FMT>(r.v + 8 * h, c);
-        else w[c] = convert<F, FMT>(r.v[c], h);
+    for (int s = 0; s < kSteps; ++s) {
+      const int h = s / (PL * S::kFrags), in = s % (PL * S::kFrags), m = in % S::kFrags;
+      if (s + 1 < kSteps) {
+        const int n = s + 1, nin = n % (PL * S::kFrags);
+        x[n & 1] = row_frag(buf, nin / S::kFrags, n / (PL * S::kFrags), nin % S::kFrags);
       }
+      constexpr int per = PL * S::kFrags / 4;  // fragments of rows for each of the next half's operands
+      if (h == 0 && in % per == 0) w[1][in / per] = operand(r, 1, in / per);
+      __builtin_amdgcn_sched_barrier(0x6);  // what is not arithmetic stays in its fragment
 #pragma unroll
-      for (int p = 0; p < PL; ++p)
-#pragma unroll
-        for (int m = 0; m < S::kFrags; ++m) {
-          const typename F::frag x = *(const typename F::frag*)(
-              smem + buf * kBufBytes + p * kPlaneBytes + m * 2048 + wave_m * S::kWaveRows * 128 + sub * 128 +
-              (((quad * 2 + h) ^ (sub & 7)) << 4));
-#pragma unroll
-          for (int c = 0; c < 4; ++c) acc[m][c] = F::mma(w[c], x, acc[m][c]);
-        }
+      for (int c = 0; c < 4; ++c) acc[m][c] = F::mma(w[h][c], x[s & 1], acc[m][c]);
+      __builtin_amdgcn_sched_barrier(0x6);
     }
   };
   // A step's loads are issued kDepth - 1 steps before it, without branches around them, so that what is on its way
