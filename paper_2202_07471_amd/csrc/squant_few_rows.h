@@ -26,7 +26,7 @@ __device__ __forceinline__ uint4v load_row8(const char* row, int64_t k, int64_t 
   return o;
 }
 
-template <class F, int PL, int FMT, int MF, int NF>
+template <class F, int PL, int FMT, int MF, int NF, bool WORDS>
 __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductArgs a) {
   constexpr int kWaves = few_waves(MF, NF);
   constexpr int kHalves = FMT == SQUANT_OUT_INT4 ? 4 : 2;  // groups of 8 codes in 16 bytes
@@ -44,10 +44,12 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductAr
 
   const int64_t w_bytes = (int64_t)a.w_rows * a.w_row;
   const uint8_t* w[NF];
+  uint32_t shift[NF];  // see RowCodes
 #pragma unroll
   for (int c = 0; c < NF; ++c) {
     const int32_t n = NF == 4 ? col0 + (sub >> 2) * 16 + c * 4 + (sub & 3) : col0 + c * 16 + sub;
     w[c] = a.w + (int64_t)min(n, a.w_rows - 1) * a.w_row + quad * 16;
+    shift[c] = WORDS ? 0 : (uint32_t)(reinterpret_cast<uintptr_t>(w[c]) & 3u);
   }
   const char* x[MF];
 #pragma unroll
@@ -61,6 +63,7 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductAr
 
   struct Operands {
     uint4v codes[NF];
+    uint32_t after[WORDS ? 1 : NF];
     uint4v rows[kRowsAhead ? PL : 1][kRowsAhead ? kHalves : 1][kRowsAhead ? MF : 1];
   };
   auto element = [&](int u, int h) { return (int64_t)u * kUnit + quad * (kUnit / 4) + h * 8; };
@@ -77,7 +80,10 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductAr
       load_before(o.codes, at, a.w_end, w_bytes);
     } else {
 #pragma unroll
-      for (int c = 0; c < NF; ++c) o.codes[c] = load_any<uint4v>(w[c] + (int64_t)u * 64);
+      for (int c = 0; c < NF; ++c) {
+        o.codes[c] = load_any<uint4v>(w[c] - shift[c] + (int64_t)u * 64);
+        if constexpr (!WORDS) o.after[c] = load_any<uint32_t>(w[c] - shift[c] + (int64_t)u * 64 + 16);
+      }
     }
     if constexpr (kRowsAhead) {
 #pragma unroll
@@ -95,9 +101,15 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductAr
       typename F::frag wf[NF];
 #pragma unroll
       for (int c = 0; c < NF; ++c) {
+        uint4v q = o.codes[c];
+        if (!WORDS && !ends) {
+#pragma unroll
+          for (int i = h * 4 / kHalves; i < (h + 1) * 4 / kHalves; ++i)
+            q[i] = __builtin_amdgcn_alignbyte(i < 3 ? o.codes[c][i < 3 ? i + 1 : 3] : o.after[c], o.codes[c][i], shift[c]);
+        }
         codes16 r;
-        if constexpr (FMT == SQUANT_OUT_INT4) r = h < 2 ? codes16{o.codes[c][0], o.codes[c][1]} : codes16{o.codes[c][2], o.codes[c][3]};
-        else r = o.codes[c];
+        if constexpr (FMT == SQUANT_OUT_INT4) r = h < 2 ? codes16{q[0], q[1]} : codes16{q[2], q[3]};
+        else r = q;
         wf[c] = convert<F, FMT>(r, h & 1);
       }
 #pragma unroll
@@ -173,11 +185,17 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductAr
   }
 }
 
-template <class F, int PL, int FMT, int NF>
+template <class F, int PL, int FMT, int NF, bool WORDS>
 product_t few_rows_of(int mf) {
-  if (mf == 1) return few_rows<F, PL, FMT, 1, NF>;
-  if (mf == 2) return few_rows<F, PL, FMT, 2, NF>;
-  return few_rows<F, PL, FMT, 4, NF>;
+  if (mf == 1) return few_rows<F, PL, FMT, 1, NF, WORDS>;
+  if (mf == 2) return few_rows<F, PL, FMT, 2, NF, WORDS>;
+  return few_rows<F, PL, FMT, 4, NF, WORDS>;
+}
+template <class F, int PL, int FMT>
+product_t few_of(int mf, int nf, bool words) {
+  if (nf == 4) return words ? few_rows_of<F, PL, FMT, 4, true>(mf) : few_rows_of<F, PL, FMT, 4, false>(mf);
+  if (nf == 2) return words ? few_rows_of<F, PL, FMT, 2, true>(mf) : few_rows_of<F, PL, FMT, 2, false>(mf);
+  return words ? few_rows_of<F, PL, FMT, 1, true>(mf) : few_rows_of<F, PL, FMT, 1, false>(mf);
 }
 
 }  // namespace lin

@@ -59,8 +59,7 @@ template <class A> int launch(void (*k)(A), int64_t gx, int gy, int threads, siz
 
 // Kernels that ask for more LDS than a workgroup gets by default say so, once for each device: the attribute
 // is the kernel's, not a call's.
-int launch_product(product_t k, const Split& p, int format, hipStream_t st, const ProductArgs& a) {
-  (void)format;
+int launch_product(product_t k, const Split& p, hipStream_t st, const ProductArgs& a) {
   if (p.lds > 64 * 1024 &&
       hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.lds) != hipSuccess) {
     (void)hipGetLastError();
@@ -69,12 +68,16 @@ int launch_product(product_t k, const Split& p, int format, hipStream_t st, cons
   return launch(k, p.workgroups, p.slices, p.threads, p.lds, st, a);
 }
 
-product_t layer_kernel(int type, int format, const Split& p) {
+product_t layer_kernel(int type, const squant_codes_t& w, const Split& p) {
+  const bool words = code_row(w) % 4 == 0 && !misaligned(w.codes, 4);
+  const int format = (int)w.format;
   if (p.few)
-    return type == SQUANT_W_F32   ? few_f32(format, p.row_frags, p.col_frags_each)
-           : type == SQUANT_W_F16 ? few_f16(format, p.row_frags, p.col_frags_each)
-                                  : few_bf16(format, p.row_frags, p.col_frags_each);
-  return type == SQUANT_W_F32 ? layer_f32(format, p.mt) : type == SQUANT_W_F16 ? layer_f16(format, p.mt) : layer_bf16(format, p.mt);
+    return type == SQUANT_W_F32   ? few_f32(format, p.row_frags, p.col_frags_each, words)
+           : type == SQUANT_W_F16 ? few_f16(format, p.row_frags, p.col_frags_each, words)
+                                  : few_bf16(format, p.row_frags, p.col_frags_each, words);
+  return type == SQUANT_W_F32   ? layer_f32(format, p.mt, words)
+         : type == SQUANT_W_F16 ? layer_f16(format, p.mt, words)
+                                : layer_bf16(format, p.mt, words);
 }
 
 float layer_unit(int type, int format) {
@@ -223,7 +226,7 @@ int squant_linear(const void* d_x, int64_t ldx, squant_wtype_t type, int64_t row
   f.bias = d_bias; f.residual = d_residual; f.ldr = ldr; f.out = d_y; f.ldo = ldy; f.kept = d_kept; f.kept_scales = d_kept_scales;
   const Finish done = f;
   if (s.p.slices > 1) { f.kind = kPartial; f.partial = s.partial; }
-  if (int rc = launch_product(layer_kernel((int)type, (int)w.format, s.p), s.p, (int)w.format, st, a)) return rc;
+  if (int rc = launch_product(layer_kernel((int)type, w, s.p), s.p, st, a)) return rc;
   return s.p.slices > 1 ? launch_join(false, (int)type, s.p, s.p.slices, s.partial, done, st) : SQUANT_OK;
 }
 
@@ -275,7 +278,7 @@ int squant_linear_backward(const void* d_dy, int64_t lddy, squant_wtype_t type, 
   const Finish done = f;
   if (s.p.slices > 1) { f.kind = kPartial; f.partial = s.partial; }
   const product_t k = planes == 2 ? gradient_2((int)w.format, s.p.mt) : gradient_1((int)w.format, s.p.mt);
-  if (int rc = launch_product(k, s.p, (int)w.format, st, a)) return rc;
+  if (int rc = launch_product(k, s.p, st, a)) return rc;
   return s.p.slices > 1 ? launch_join(true, (int)type, s.p, s.p.slices, s.partial, done, st) : SQUANT_OK;
 }
 
@@ -308,7 +311,7 @@ int squant_cross_entropy(const void* d_h, int64_t ldh, squant_wtype_t type, int6
   f.kind = kStats; f.out_type = (int)type; f.unit = layer_unit((int)type, (int)w.format);
   f.rows = rows; f.cols = w.cout; f.row_factor = s.x.factor; f.scales = w.scales;
   f.labels = d_labels; f.stats = s.stats; f.label_logit = s.label_logit;
-  if (int rc = launch_product(layer_kernel((int)type, (int)w.format, s.p), s.p, (int)w.format, st, a)) return rc;
+  if (int rc = launch_product(layer_kernel((int)type, w, s.p), s.p, st, a)) return rc;
   const LossArgs l{s.stats, (w.cout + kTile - 1) / kTile, s.label_logit, d_labels, ignore_index, w.cout, rows, d_loss, d_lse};
   constexpr int per = kRowThreads / kLanes;
   return launch(loss_rows_kernel(), (rows + per - 1) / per, 1, kRowThreads, 0, st, l);
@@ -353,7 +356,7 @@ int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t t
     f.kind = kProb; f.out_type = (int)type; f.unit = layer_unit((int)type, (int)w.format);
     f.rows = rows; f.cols = piece.cout; f.row_factor = s.x.factor; f.scales = w.scales + first;
     f.lse = d_lse; f.prob_unit = s.unit; f.prob = s.prob; f.ld_prob = planes * s.piece; f.prob_plane = s.piece;
-    if (int rc = launch_product(layer_kernel((int)type, (int)w.format, p), p, (int)w.format, st, a)) return rc;
+    if (int rc = launch_product(layer_kernel((int)type, piece, p), p, st, a)) return rc;
     ProductArgs g{};
     Split split = s.g;
     split.blocks = (int32_t)((piece.cout + kBlock - 1) / kBlock);
@@ -361,7 +364,7 @@ int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t t
     g.slice0 = i * s.g.slices;
     g.f.kind = kPartial; g.f.rows = rows; g.f.cols = w.cin; g.f.partial = s.partial;
     const product_t k = planes == 2 ? gradient_2((int)w.format, s.g.mt) : gradient_1((int)w.format, s.g.mt);
-    if (int rc = launch_product(k, split, (int)w.format, st, g)) return rc;
+    if (int rc = launch_product(k, split, st, g)) return rc;
   }
   Finish f{};
   f.kind = kGradLoss; f.out_type = (int)type; f.unit = kColumnUnitInverse; f.rows = rows; f.cols = w.cin; f.scales = w.scales;

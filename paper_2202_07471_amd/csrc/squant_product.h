@@ -32,11 +32,12 @@ __device__ __forceinline__ void to_lds(const void* p, void* lds) {
 }
 
 // The codes of one step, as loaded.
-template <int FMT, bool GRAD> struct Raw;
-template <int FMT> struct Raw<FMT, false> { typename Codes<FMT>::row16 v[4]; };
-template <int FMT> struct Raw<FMT, true> { typename Codes<FMT>::col4 v[16]; };
+template <int FMT, bool GRAD, bool WORDS> struct Raw;
+template <int FMT, bool WORDS> struct Raw<FMT, false, WORDS> { RowCodes<FMT, WORDS> v[4]; };
+template <int FMT, bool WORDS> struct Raw<FMT, true, WORDS> { typename Codes<FMT>::col4 v[16]; };
 
-template <class F, int PL, int FMT, int MT, bool GRAD>
+// WORDS: code rows begin at whole 32-bit words (see RowCodes; a gradient takes them as they are).
+template <class F, int PL, int FMT, int MT, bool GRAD, bool WORDS>
 __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a) {
   typedef Shape<MT> S;
   constexpr int kPlaneBytes = MT * kBlock * 2;
@@ -102,8 +103,19 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
       wsrc[c] = (uint32_t)max(min(col0 + (sub >> 2) * 16 + c * 4 + (sub & 3), a.w_rows - 1) - min(col0, a.w_rows - 1), 0) *
                 (uint32_t)a.w_row + (uint32_t)Codes<FMT>::offset(quad * 16);
     inside = a.w_cols / kBlock;
+    if constexpr (!WORDS) {
+      const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(w_base) & 3u);
+      w_base -= off;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) wsrc[c] += off;
+    }
   }
-  auto load_codes = [&](int b, Raw<FMT, GRAD>& o) {
+  uint32_t shift[4] = {0, 0, 0, 0};
+  if constexpr (!GRAD && !WORDS) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) shift[c] = wsrc[c] & 3u;
+  }
+  auto load_codes = [&](int b, Raw<FMT, GRAD, WORDS>& o) {
     if constexpr (GRAD) {
       const uint8_t* p = w_base + (int64_t)b * kBlock * a.w_row;
 #pragma unroll
@@ -111,18 +123,28 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
     } else {
       const uint8_t* p = w_base + Codes<FMT>::offset((int64_t)b * kBlock);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) o.v[c] = load_any<typename Codes<FMT>::row16>(p + wsrc[c]);
+      for (int c = 0; c < 4; ++c) o.v[c].load(p + wsrc[c] - shift[c]);
     }
   };
   // the same at the buffer's end
-  auto load_last_codes = [&](int b, Raw<FMT, GRAD>& o) {
+  auto load_last_codes = [&](int b, Raw<FMT, GRAD, WORDS>& o) {
     constexpr int n = GRAD ? 16 : 4;
     const uint8_t* at[n];
 #pragma unroll
     for (int i = 0; i < n; ++i)
       at[i] = GRAD ? w_base + ((int64_t)b * kBlock + i) * a.w_row + wsrc[0]
                    : w_base + Codes<FMT>::offset((int64_t)b * kBlock) + wsrc[GRAD ? 0 : i];
-    load_before(o.v, at, a.w_end, w_bytes);
+    if constexpr (GRAD) {
+      load_before(o.v, at, a.w_end, w_bytes);
+    } else {
+      typename Codes<FMT>::row16 v[4];
+      load_before(v, at, a.w_end, w_bytes);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        o.v[c].set(v[c]);
+        shift[c] = 0;  // nothing is read as whole words after this
+      }
+    }
   };
 
   float4v acc[S::kFrags][4];
@@ -131,9 +153,9 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
 #pragma unroll
     for (int c = 0; c < 4; ++c) acc[m][c] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
 
-  auto operand = [&](const Raw<FMT, GRAD>& r, int h, int c) {
+  auto operand = [&](const Raw<FMT, GRAD, WORDS>& r, int h, int c) {
     if constexpr (GRAD) return convert_columns<FMT>(r.v + 8 * h, c);
-    else return convert<F, FMT>(r.v[c], h);
+    else return convert<F, FMT>(r.v[c].aligned(h, shift[c]), h);
   };
   auto row_frag = [&](int buf, int p, int h, int m) {
     return *(const typename F::frag*)(smem + buf * kBufBytes + p * kPlaneBytes + m * 2048 + wave_m * S::kWaveRows * 128 +
@@ -141,7 +163,7 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
   };
   // A half step is 16 fragments of products a fragment of rows; the next fragment of rows is read, and the next
   // half's codes are converted, between them.
-  auto multiply = [&](int buf, const Raw<FMT, GRAD>& r) {
+  auto multiply = [&](int buf, const Raw<FMT, GRAD, WORDS>& r) {
     constexpr int kSteps = 2 * PL * S::kFrags;
     typename F::frag w[2][4], x[2];
 #pragma unroll
@@ -167,12 +189,12 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
   // them the compiler waits for everything before it touches a step's codes.)  The barrier also says that the buffer
   // to be loaded next is read out.
   constexpr int D = S::kDepth;
-  constexpr int kIssued = kLoads * PL + (GRAD ? 16 : 4);
+  constexpr int kIssued = kLoads * PL + (GRAD ? 16 : WORDS ? 4 : 8);
   constexpr int kOthers = kIssued * (D - 2);  // may be on their way when a step begins
   static_assert(kOthers < 64, "the wait counter has six bits");
   const int steady = min(last, inside);
   if (first < steady) {
-    Raw<FMT, GRAD> raw[D];
+    Raw<FMT, GRAD, WORDS> raw[D];
 #pragma unroll
     for (int i = 0; i < D - 1; ++i) {
       load_rows(min(first + i, steady - 1), i);
@@ -197,7 +219,7 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
     __syncthreads();
   }
   for (int b = max(first, steady); b < last; ++b) {  // what ends within a block
-    Raw<FMT, GRAD> raw;
+    Raw<FMT, GRAD, WORDS> raw;
     load_rows(b, 0);
     load_last_codes(b, raw);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -261,11 +283,15 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
   }
 }
 
-template <class F, int PL, int FMT, bool GRAD>
+template <class F, int PL, int FMT, bool GRAD, bool WORDS>
 product_t product_of(int mt) {
-  if (mt == 256) return product<F, PL, FMT, 256, GRAD>;
-  if (mt == 128) return product<F, PL, FMT, 128, GRAD>;
-  return product<F, PL, FMT, 64, GRAD>;
+  if (mt == 256) return product<F, PL, FMT, 256, GRAD, WORDS>;
+  if (mt == 128) return product<F, PL, FMT, 128, GRAD, WORDS>;
+  return product<F, PL, FMT, 64, GRAD, WORDS>;
+}
+template <class F, int PL, int FMT>
+product_t layer_of(int mt, bool words) {
+  return words ? product_of<F, PL, FMT, false, true>(mt) : product_of<F, PL, FMT, false, false>(mt);
 }
 
 }  // namespace lin
