@@ -1,4 +1,4 @@
-// The product of at most 64 rows with codes: bound by the codes' bytes, or by a few trips to memory where they are
+// The product of at most 64 rows (binary32: 32) with codes: bound by the codes' bytes, or by a few trips to memory where they are
 // few.
 //
 // A workgroup owns 16 * NF columns and its waves share the contraction, a unit of 16 bytes of each code row at a time
@@ -14,7 +14,24 @@ namespace lin {
 
 // Waves of a workgroup: 16 where its columns are few and the waves' registers and sums fit.
 constexpr int few_waves(int mf, int nf) { return nf == 4 || mf * nf > 4 ? 8 : 16; }
-constexpr size_t few_lds(int mf, int nf) { return (size_t)few_waves(mf, nf) * mf * nf * kLanes * 16; }
+constexpr size_t few_lds(int mf, int nf) { return (size_t)few_waves(mf, nf) * mf * (nf * kLanes * 16 + 16 * 4); }
+
+// Rows up to which `few_rows` is taken.  Every workgroup splits its binary32 rows anew: past 32 of them a pass of
+// its own costs less.
+constexpr int few_rows_limit(int planes) { return planes == 1 ? 64 : 32; }
+
+// 8 binary32 numbers as hi + lo of binary16, times `up`.
+struct Planes { half8 v[2]; };
+__device__ __forceinline__ Planes split8(const uint4v (&x)[2], float up) {
+  Planes o;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float f = __uint_as_float(x[i >> 2][i & 3]) * up;
+    o.v[0][i] = (_Float16)f;
+    o.v[1][i] = magnitude(f) < 0x7f800000u ? (_Float16)(f - (float)o.v[0][i]) : (_Float16)0.0f;  // an infinity has no remainder
+  }
+  return o;
+}
 
 // 8 elements of a row from element k on, zeros from element `cols` on.
 __device__ __forceinline__ uint4v load_row8(const char* row, int64_t k, int64_t cols) {
@@ -26,17 +43,19 @@ __device__ __forceinline__ uint4v load_row8(const char* row, int64_t k, int64_t 
   return o;
 }
 
-template <class F, int PL, int FMT, int MF, int NF, bool WORDS>
+// T: the type of the rows and of the output; binary32 with F = Half.
+template <class F, class T, int FMT, int MF, int NF, bool WORDS>
 __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductArgs a) {
   constexpr int kWaves = few_waves(MF, NF);
   constexpr int kHalves = FMT == SQUANT_OUT_INT4 ? 4 : 2;  // groups of 8 codes in 16 bytes
   constexpr int kUnit = 32 * kHalves;                      // contraction elements of a unit
+  constexpr bool kSplit = sizeof(T) == 4;                  // rows are split into planes
+  constexpr int PL = kSplit ? 2 : 1;                         // 16-byte loads of 8 elements
   constexpr int kRowFrags = PL * kHalves * MF;             // of a unit
   constexpr bool kRowsAhead = kRowFrags <= 8;              // its rows are loaded with its codes
   constexpr int kAheadMost = 16 / (NF + (kRowsAhead ? kRowFrags : 0));  // by 64 registers
-  constexpr int kAhead = kAheadMost >= 4 ? 4 : kAheadMost >= 2 ? 2 : 1;
+  constexpr int kAhead = kAheadMost >= 4 && kRowsAhead ? 4 : kAheadMost >= 2 ? 2 : 1;
   typedef typename Codes<FMT>::row16 codes16;
-  typedef typename OutOf<F, PL>::type T;
   extern __shared__ __align__(16) unsigned char smem[];
   const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
   const int sub = lane & 15, quad = lane >> 4;
@@ -53,7 +72,7 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductAr
   }
   const char* x[MF];
 #pragma unroll
-  for (int m = 0; m < MF; ++m) x[m] = (const char*)a.a + min((int64_t)(m * 16 + sub), a.f.rows - 1) * a.lda * 2;
+  for (int m = 0; m < MF; ++m) x[m] = (const char*)a.a + min((int64_t)(m * 16 + sub), a.f.rows - 1) * a.lda * (int)sizeof(T);
 
   float4v acc[MF][NF];
 #pragma unroll
@@ -69,8 +88,19 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductAr
   auto element = [&](int u, int h) { return (int64_t)u * kUnit + quad * (kUnit / 4) + h * 8; };
   // Row elements of a unit; `ends`: it may reach past the row's end.
   auto row_frag = [&](int u, int p, int h, int m, bool ends) {
-    if (ends) return load_row8(x[m] + 2 * p * a.plane, element(u, h), a.w_cols);
-    return load_any<uint4v>(x[m] + 2 * (p * a.plane + element(u, h)));
+    const int64_t k = element(u, h);
+    if constexpr (kSplit) {
+      const float* f = (const float*)x[m] + k + 4 * p;
+      if (!ends) return load_any<uint4v>(f);
+      uint4v o = {0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (k + 4 * p + i < a.w_cols) o[i] = load_any<uint32_t>(f + i);
+      return o;
+    } else {
+      if (ends) return load_row8(x[m], k, a.w_cols);
+      return load_any<uint4v>(x[m] + 2 * k);
+    }
   };
   auto load_unit = [&](int u, Operands& o, bool ends) {
     if (ends) {
@@ -94,6 +124,25 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductAr
           for (int m = 0; m < MF; ++m) o.rows[p][h][m] = row_frag(u, p, h, m, ends);
     }
   };
+  // binary32: what a lane adds up belongs to one row, so that the row's exponent is a number of the lane's.  It
+  // follows the largest element seen; the sums so far are brought to it.
+  int exponent[kSplit ? MF : 1];
+#pragma unroll
+  for (int m = 0; m < (kSplit ? MF : 1); ++m) exponent[m] = 126;
+  auto raise = [&](const uint4v (&rows)[PL], int m) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int p = 0; p < PL; ++p)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = max(top, rows[p][i] & 0x7fffffffu);
+    top = group_max(min(top, 0x7f7fffffu));  // an infinity or a NaN: as the largest number
+    const int e = min(exponent[m], row_exponent(top));
+    if (!__any(top != 0 && e < exponent[m])) return;
+    const int drop = top != 0 ? max(e - exponent[m], -126) : 0;
+    exponent[m] = top != 0 ? e : exponent[m];
+#pragma unroll
+    for (int c = 0; c < NF; ++c) acc[m][c] *= power_of_two(drop);
+  };
   auto multiply = [&](int u, const Operands& o, bool ends) {
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) {
@@ -113,15 +162,25 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductAr
         wf[c] = convert<F, FMT>(r, h & 1);
       }
 #pragma unroll
-      for (int p = 0; p < PL; ++p)
+      for (int m = 0; m < MF; ++m) {
+        uint4v rows[PL];
 #pragma unroll
-        for (int m = 0; m < MF; ++m) {
-          uint4v rows;
-          if constexpr (kRowsAhead) rows = o.rows[p][h][m];
-          else rows = row_frag(u, p, h, m, ends);
-#pragma unroll
-          for (int c = 0; c < NF; ++c) acc[m][c] = F::mma(wf[c], __builtin_bit_cast(typename F::frag, rows), acc[m][c]);
+        for (int p = 0; p < PL; ++p) {
+          if constexpr (kRowsAhead) rows[p] = o.rows[p][h][m];
+          else rows[p] = row_frag(u, p, h, m, ends);
         }
+        if constexpr (kSplit) {
+          raise(rows, m);
+          const Planes x = split8(rows, power_of_two(exponent[m]));
+#pragma unroll
+          for (int p = 1; p >= 0; --p)
+#pragma unroll
+            for (int c = 0; c < NF; ++c) acc[m][c] = F::mma(wf[c], x.v[p], acc[m][c]);
+        } else {
+#pragma unroll
+          for (int c = 0; c < NF; ++c) acc[m][c] = F::mma(wf[c], __builtin_bit_cast(typename F::frag, rows[0]), acc[m][c]);
+        }
+      }
     }
   };
 
@@ -150,52 +209,68 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductAr
   }
 
   float4v* sums = reinterpret_cast<float4v*>(smem);
+  int* exponents = reinterpret_cast<int*>(smem + (size_t)kWaves * MF * NF * kLanes * 16);  // [wave][m][row], binary32
 #pragma unroll
-  for (int m = 0; m < MF; ++m)
+  for (int m = 0; m < MF; ++m) {
 #pragma unroll
     for (int c = 0; c < NF; ++c) sums[((wave * MF + m) * NF + c) * kLanes + lane] = acc[m][c];
+    if (kSplit && lane < 16) exponents[(wave * MF + m) * 16 + lane] = exponent[kSplit ? m : 0];
+  }
   __syncthreads();
-  auto total = [&](int m, int c) {
-    float4v t = sums[(m * NF + c) * kLanes + lane];
+  auto least = [&](int m) {
+    int e = exponents[m * 16 + sub];
 #pragma unroll 4
-    for (int o = 1; o < kWaves; ++o) t += sums[((o * MF + m) * NF + c) * kLanes + lane];
+    for (int o = 1; o < kWaves; ++o) e = min(e, exponents[(o * MF + m) * 16 + sub]);
+    return e;
+  };
+  auto total = [&](int m, int c, int e) {
+    float4v t = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int o = 0; o < kWaves; ++o) {
+      const float4v s = sums[((o * MF + m) * NF + c) * kLanes + lane];
+      if constexpr (kSplit) t += s * power_of_two(max(e - exponents[(o * MF + m) * 16 + sub], -126));
+      else t += s;
+    }
     return t;
   };
   if constexpr (NF == 4) {
     if (wave >= MF) return;
     Columns<16> columns;
     load_columns<16, T>(columns, a.f, col0 + quad * 16);
+    const int e = kSplit ? least(wave) : 0;
     float v[16];
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      const float4v t = total(wave, c);
+      const float4v t = total(wave, c, e);
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[4 * c + i] = t[i];
     }
-    finish_layer<16, T>(a.f, columns, wave * 16 + sub, col0 + quad * 16, v, PL);
+    finish_layer<16, T>(a.f, columns, wave * 16 + sub, col0 + quad * 16, v, power_of_two(-e), kSplit ? 2 : 1);
   } else {
     if (wave >= MF * NF) return;
     const int m = wave / NF, c = wave % NF;
     const int32_t col = col0 + c * 16 + quad * 4;
     Columns<4> columns;
     load_columns<4, T>(columns, a.f, col);
-    const float4v t = total(m, c);
+    const int e = kSplit ? least(m) : 0;
+    const float4v t = total(m, c, e);
     float v[4] = {t[0], t[1], t[2], t[3]};
-    finish_layer<4, T>(a.f, columns, m * 16 + sub, col, v, PL);
+    finish_layer<4, T>(a.f, columns, m * 16 + sub, col, v, power_of_two(-e), 1);
   }
 }
 
-template <class F, int PL, int FMT, int NF, bool WORDS>
+template <class F, class T, int FMT, int NF, bool WORDS>
 product_t few_rows_of(int mf) {
-  if (mf == 1) return few_rows<F, PL, FMT, 1, NF, WORDS>;
-  if (mf == 2) return few_rows<F, PL, FMT, 2, NF, WORDS>;
-  return few_rows<F, PL, FMT, 4, NF, WORDS>;
+  if (mf == 1) return few_rows<F, T, FMT, 1, NF, WORDS>;
+  if constexpr (sizeof(T) == 2)
+    if (mf == 4) return few_rows<F, T, FMT, 4, NF, WORDS>;
+  return few_rows<F, T, FMT, 2, NF, WORDS>;
 }
-template <class F, int PL, int FMT>
+template <class F, class T, int FMT>
 product_t few_of(int mf, int nf, bool words) {
-  if (nf == 4) return words ? few_rows_of<F, PL, FMT, 4, true>(mf) : few_rows_of<F, PL, FMT, 4, false>(mf);
-  if (nf == 2) return words ? few_rows_of<F, PL, FMT, 2, true>(mf) : few_rows_of<F, PL, FMT, 2, false>(mf);
-  return words ? few_rows_of<F, PL, FMT, 1, true>(mf) : few_rows_of<F, PL, FMT, 1, false>(mf);
+  if (nf == 4) return words ? few_rows_of<F, T, FMT, 4, true>(mf) : few_rows_of<F, T, FMT, 4, false>(mf);
+  if (nf == 2) return words ? few_rows_of<F, T, FMT, 2, true>(mf) : few_rows_of<F, T, FMT, 2, false>(mf);
+  return words ? few_rows_of<F, T, FMT, 1, true>(mf) : few_rows_of<F, T, FMT, 1, false>(mf);
 }
 
 }  // namespace lin

@@ -6,8 +6,8 @@ namespace squant {
 namespace lin {
 
 product_t few_bf16(int format, int mf, int nf, bool words) {
-  return format == SQUANT_OUT_INT4 ? few_of<Brain, 1, SQUANT_OUT_INT4>(mf, nf, words)
-                                   : few_of<Brain, 1, SQUANT_OUT_INT8>(mf, nf, words);
+  return format == SQUANT_OUT_INT4 ? few_of<Brain, __bf16, SQUANT_OUT_INT4>(mf, nf, words)
+                                   : few_of<Brain, __bf16, SQUANT_OUT_INT8>(mf, nf, words);
 }
 
 }  // namespace lin

@@ -23,15 +23,22 @@ __global__ void __launch_bounds__(kRowThreads) pad_rows(RowsArgs a) {
 }
 
 __global__ void __launch_bounds__(kRowThreads) split_rows(RowsArgs a) {
+  constexpr int kHeld = 4;  // vectors of 8 elements a thread keeps: rows up to 8192 are read once
   __shared__ uint32_t tops[kRowThreads / kLanes];
   const int64_t row = blockIdx.x;
   const float* x = (const float*)a.x + row * a.ldx;
+  float v[kHeld][8];
   uint32_t top = 0;
-  for (int32_t c = threadIdx.x * 8; c < a.cols; c += kRowThreads * 8) {
-    float v[8];
-    load_cols<8, float>(v, x + c, a.cols - c);
+  for (int32_t c0 = 0; c0 < a.padded; c0 += kHeld * kRowThreads * 8) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, finite_magnitude(v[i]));
+    for (int j = 0; j < kHeld; ++j) {
+      const int32_t c = c0 + (j * kRowThreads + (int)threadIdx.x) * 8;
+      load_cols<8, float>(v[j], x + c, max(a.cols - c, 0));
+    }
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, finite_magnitude(v[j][i]));
   }
   top = wave_max(top);
   if ((threadIdx.x & (kLanes - 1)) == 0) tops[threadIdx.x / kLanes] = top;
@@ -42,12 +49,17 @@ __global__ void __launch_bounds__(kRowThreads) split_rows(RowsArgs a) {
   const float up = power_of_two(e);
   if (threadIdx.x == 0) a.row_factor[row] = power_of_two(-e);
   _Float16* out = (_Float16*)a.out + row * 2 * a.padded;
-  for (int32_t c = threadIdx.x * 8; c < a.padded; c += kRowThreads * 8) {
-    float v[8];
-    load_cols<8, float>(v, x + c, max(a.cols - c, 0));
+  const bool held = a.padded <= kHeld * kRowThreads * 8;
+  for (int32_t c0 = 0; c0 < a.padded; c0 += kHeld * kRowThreads * 8) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= up;
-    store_planes<2>(out + c, a.padded, v);
+    for (int j = 0; j < kHeld; ++j) {
+      const int32_t c = c0 + (j * kRowThreads + (int)threadIdx.x) * 8;
+      if (c >= a.padded) break;
+      if (!held) load_cols<8, float>(v[j], x + c, max(a.cols - c, 0));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[j][i] *= up;
+      store_planes<2>(out + c, a.padded, v[j]);
+    }
   }
 }
 
@@ -78,22 +90,34 @@ __global__ void __launch_bounds__(1024) column_sums(ColumnSumArgs a) {
 }
 
 __global__ void __launch_bounds__(kRowThreads) loss_rows(LossArgs a) {
-  const int lane = threadIdx.x & (kLanes - 1);
-  const int64_t row = (int64_t)blockIdx.x * (kRowThreads / kLanes) + threadIdx.x / kLanes;
-  if (row >= a.rows) return;
+  constexpr int kWaves = kRowThreads / kLanes;
+  __shared__ float tops[kWaves], sums[kWaves];
+  const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+  const int64_t row = blockIdx.x;
   const float2* s = a.stats + row * a.chunks;
   float top = -__builtin_inff();
-  for (int32_t c = lane; c < a.chunks; c += kLanes) top = fmaxf(top, s[c].x);
+#pragma unroll 4
+  for (int32_t c = threadIdx.x; c < a.chunks; c += kRowThreads) top = fmaxf(top, s[c].x);
 #pragma unroll
   for (int o = 1; o < kLanes; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+  if (lane == 0) tops[wave] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) top = fmaxf(top, tops[i]);
   float sum = 0.0f;
-  for (int32_t c = lane; c < a.chunks; c += kLanes) {
+#pragma unroll 4
+  for (int32_t c = threadIdx.x; c < a.chunks; c += kRowThreads) {
     const float2 t = s[c];
     sum += t.y * exp2_fast(t.x - top);
   }
 #pragma unroll
   for (int o = 1; o < kLanes; o <<= 1) sum += __shfl_xor(sum, o);
-  if (lane != 0) return;
+  if (lane == 0) sums[wave] = sum;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) sum += sums[i];
   const float lse = (top + log2f(sum)) * kLn2;
   a.lse[row] = lse;
   const int64_t label = a.labels[row];
@@ -105,6 +129,7 @@ __global__ void __launch_bounds__(kRowThreads) loss_rows(LossArgs a) {
 __global__ void __launch_bounds__(1024) probability_unit(const float* scales, int32_t n, float* unit) {
   __shared__ uint32_t tops[1024 / kLanes];
   uint32_t top = 0;
+  #pragma unroll 4
   for (int64_t i = (int64_t)threadIdx.x * 4; i < n; i += 4096) {
     float v[4];
     load_cols<4, float>(v, scales + i, (int)min((int64_t)4, n - i));

@@ -9,7 +9,8 @@
 //   bfloat16, binary16  as they are;
 //   binary32            two binary16 planes, hi + lo = x * 2^e with one e a row (its largest finite element
 //                       lands in [2^14, 2^15)): 22 bits of an element, or 2^-40 of the row's largest where
-//                       that is more.  bfloat16 would take three planes for the same;
+//                       that is more.  bfloat16 would take three planes for the same.  A pass of its own lays them
+//                       out; few rows are split in registers, with an exponent of what a wave has seen of a row;
 //   gradients           one plane like this for 16-bit outputs (2^-12 of an element, an eighth of what a
 //                       bfloat16 gradient would be off by), two for binary32.
 #pragma once
@@ -33,7 +34,6 @@ constexpr int kLanes = 64;
 constexpr int kBlock = 64;   // contraction elements a step of the main loops takes
 constexpr int kTile = 64;    // columns of a wave, and the columns that share a scale of the kept pre-activation
 constexpr int kWide = 256;   // columns of a workgroup of `product`
-constexpr int kFewRows = 64; // rows up to which `few_rows` is taken
 
 enum Kind { kLinear = 0, kPartial = 1, kStats = 2, kProb = 3, kGrad = 4, kGradLoss = 5 };
 
@@ -404,6 +404,15 @@ __device__ __forceinline__ uint32_t group_max(uint32_t v) {
   return max(v, (uint32_t)__shfl_xor((int)v, 32));
 }
 
+// The power of two that brings a row's largest finite magnitude into [2^14, 2^15), as an exponent.  It stops
+// at 126 (2^-126 and its inverse are normal numbers).
+__device__ __forceinline__ int row_exponent(uint32_t top) {
+  if (top == 0) return 0;
+  const int e = (int)(top >> 23) - 127;  // a subnormal counts as 2^-127
+  return min(14 - e, 126);
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
 // ---------------------------------------------------------------------------
 // finished pieces
 // ---------------------------------------------------------------------------
@@ -451,12 +460,15 @@ __device__ __forceinline__ void load_columns(Columns<NC>& k, const Finish& f, in
 
 // A lane's NC consecutive columns of one row, `v` the bare sums.  With NC = 16 the lanes l, l^16, l^32, l^48
 // hold the row's 64 columns of one tile (every lane of the wave calls).  T: the output's type.
+__device__ __forceinline__ float row_factor_of(const Finish& f, int64_t row) {
+  return f.row_factor && row < f.rows ? f.row_factor[row] : 1.0f;
+}
 template <int NC, class T>
 __device__ __forceinline__ void finish_layer(const Finish& f, const Columns<NC>& k, int64_t row, int32_t col, float (&v)[NC],
-                                             int planes) {
+                                             float row_factor, int planes) {
   const bool live = row < f.rows;
   const int valid = live ? min(max(f.cols - col, 0), NC) : 0;
-  const float factor = f.unit * (f.row_factor && live ? f.row_factor[row] : 1.0f);
+  const float factor = f.unit * row_factor;
   float s[NC];
   const bool add = f.kind == kLinear && f.residual;
   if (add) load_cols<NC, T>(s, (const T*)f.residual + row * f.ldr + col, valid);

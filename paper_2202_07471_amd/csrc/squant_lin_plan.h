@@ -69,7 +69,7 @@ inline Split split_product(int64_t rows, int64_t cols, int64_t depth, int planes
 
 // A layer's product.  `tiled`: columns have to come in whole tiles of 64 (kept pre-activation, loss).
 inline Split split_layer(int64_t rows, int64_t cols, int64_t depth, int planes, bool tiled, bool may_split) {
-  if (rows > kFewRows) return split_product(rows, cols, depth, planes, may_split);
+  if (rows > few_rows_limit(planes)) return split_product(rows, cols, depth, planes, may_split);
   Split p{};
   p.few = true;
   p.row_frags = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;

@@ -8,6 +8,7 @@ namespace squant {
 namespace lin {
 
 constexpr int kRowThreads = 256;
+constexpr int kRowGroup = 16;  // most rows a workgroup of gradient_rows takes
 
 struct RowsArgs {
   const void* x;            // rows, or the output's gradient
@@ -25,15 +26,6 @@ struct RowsArgs {
   int rows_per_group;
   float* column_sums;       // [partials][cols], or null
 };
-
-// The power of two that brings a row's largest finite magnitude into [2^14, 2^15), as an exponent.  It stops
-// at 126 (2^-126 and its inverse are normal numbers).
-__device__ __forceinline__ int row_exponent(uint32_t top) {
-  if (top == 0) return 0;
-  const int e = (int)(top >> 23) - 127;  // a subnormal counts as 2^-127
-  return min(14 - e, 126);
-}
-__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
 __device__ __forceinline__ uint32_t finite_magnitude(float v) {
   const uint32_t m = magnitude(v);
@@ -67,18 +59,22 @@ __global__ void __launch_bounds__(kRowThreads) split_rows(RowsArgs a);
 
 // Rows of dz * scale, dz = dy * act'(z), as PL binary16 planes with an exponent a row, and the column sums of dz.
 // The exponent comes from the largest |dy * scale| (the slopes stay below 1.13), so that it costs no second
-// evaluation of the slope: dy is read twice, the second time from the cache.  A workgroup takes a few rows;
-// where they have few columns its threads share out the rows as well.
+// evaluation of the slope: dy is read twice, the second time from the cache.  A workgroup takes a few rows; where
+// they have few columns its threads share out the rows as well, and where there are few rows several workgroups
+// share out their columns.
 template <class T, int PL>
 __global__ void __launch_bounds__(kRowThreads) gradient_rows(RowsArgs a) {
-  __shared__ int exponent[64];
-  const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+  __shared__ uint32_t tops[kRowGroup];
+  const int lane = threadIdx.x & (kLanes - 1);
   const int64_t row0 = (int64_t)blockIdx.x * a.rows_per_group;
   const int n_rows = (int)min((int64_t)a.rows_per_group, a.rows - row0);
-  for (int r = wave; r < n_rows; r += kRowThreads / kLanes) {
+  if (threadIdx.x < kRowGroup) tops[threadIdx.x] = 0;
+  __syncthreads();
+  for (int r = 0; r < n_rows; ++r) {
     const T* dy = (const T*)a.x + (row0 + r) * a.ldx;
     uint32_t top = 0;
-    for (int32_t c = lane * 8; c < a.cols; c += kLanes * 8) {
+#pragma unroll 2
+    for (int32_t c = threadIdx.x * 8; c < a.cols; c += kRowThreads * 8) {
       float v[8], s[8];
       load_cols<8, T>(v, dy + c, a.cols - c);
       load_cols<8, float>(s, a.scales + c, a.cols - c);
@@ -86,28 +82,27 @@ __global__ void __launch_bounds__(kRowThreads) gradient_rows(RowsArgs a) {
       for (int i = 0; i < 8; ++i) top = max(top, finite_magnitude(v[i] * s[i]));
     }
     top = wave_max(top);
-    if (lane == 0) {
-      const int e = row_exponent(top) - 1;  // room for slopes beyond 1
-      exponent[r] = e;
-      a.row_factor[row0 + r] = power_of_two(-e);
-    }
+    if (lane == 0) atomicMax(&tops[r], top);  // in the LDS; a maximum does not depend on the order
   }
   __syncthreads();
+  if (blockIdx.y == 0 && (int)threadIdx.x < n_rows) a.row_factor[row0 + threadIdx.x] = power_of_two(1 - row_exponent(tops[threadIdx.x]));
   const int vectors = a.padded / 8;
   const int shares = max(1, kRowThreads / vectors), share = shares > 1 ? (int)threadIdx.x / vectors : 0;
   if (share >= shares) return;
   const int32_t chunks = (a.cols + kTile - 1) / kTile;
-  for (int j = shares > 1 ? (int)threadIdx.x % vectors : (int)threadIdx.x; j < vectors; j += kRowThreads) {
+  // with one share the columns are dealt to the workgroups of these rows as well
+  for (int j = shares > 1 ? (int)threadIdx.x % vectors : (int)(blockIdx.y * kRowThreads + threadIdx.x); j < vectors;
+       j += (int)gridDim.y * kRowThreads) {
     const int32_t c = j * 8;
     const int valid = min(max(a.cols - c, 0), 8);
     float s[8], sum[8];
     load_cols<8, float>(s, a.scales + c, valid);
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
-#pragma unroll 2
+#pragma unroll 4
     for (int r = share; r < n_rows; r += shares) {
       const int64_t row = row0 + r;
-      const float up = power_of_two(exponent[r]);
+      const float up = power_of_two(row_exponent(tops[r]) - 1);  // room for slopes beyond 1
       float v[8];
       load_cols<8, T>(v, (const T*)a.x + row * a.ldx + c, valid);
       if (a.keep == SQUANT_KEEP_FULL) {
@@ -164,6 +159,7 @@ __global__ void __launch_bounds__(kRowThreads) join(JoinArgs a) {
   float4v t[4];
 #pragma unroll
   for (int c = 0; c < 4; ++c) t[c] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
   for (int s = 0; s < a.slices; ++s) {
     const float4v* p = a.partial + ((s * a.row_frags + rf) * a.col_frags + tile * 4) * kLanes + lane;
 #pragma unroll
@@ -180,7 +176,7 @@ __global__ void __launch_bounds__(kRowThreads) join(JoinArgs a) {
   else {
     Columns<16> columns;
     load_columns<16, T>(columns, a.f, col);
-    finish_layer<16, T>(a.f, columns, row, col, v, a.planes);
+    finish_layer<16, T>(a.f, columns, row, col, v, row_factor_of(a.f, row), a.planes);
   }
 }
 
@@ -195,7 +191,7 @@ struct LossArgs {
   float* loss;
   float* lse;
 };
-// A wave a row: the chunks' sums brought to one largest logit.
+// A workgroup a row: the chunks' sums brought to one largest logit.
 __global__ void __launch_bounds__(kRowThreads) loss_rows(LossArgs a);
 
 // 2^E of the gradient's probabilities: the largest scale of the vocabulary comes into [2^13, 2^14).

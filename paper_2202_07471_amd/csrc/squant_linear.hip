@@ -92,10 +92,9 @@ struct RowOperand {
   const float* factor;
 };
 
-// few_rows reads 16-bit rows at any alignment and of any length.
+// few_rows reads rows at any alignment and of any length.
 bool direct_rows(const void* x, int64_t ldx, int type, int64_t rows, int32_t cin) {
-  if (type == SQUANT_W_F32) return false;
-  return rows <= kFewRows || (cin % kBlock == 0 && ldx % 8 == 0 && !misaligned(x, 16));
+  return rows <= few_rows_limit(planes_of(type)) || (type != SQUANT_W_F32 && cin % kBlock == 0 && ldx % 8 == 0 && !misaligned(x, 16));
 }
 
 RowOperand lay_out_rows(Cutter& c, const void* x, int64_t ldx, int type, int64_t rows, int32_t cin, RowsArgs& r, bool& copy) {
@@ -141,7 +140,7 @@ size_t lay_out_linear(void* ws, const void* x, int64_t ldx, int type, int64_t ro
   return c.used;
 }
 
-int gradient_rows_per_group(int64_t rows) { return (int)std::min<int64_t>(16, std::max<int64_t>(1, (rows + 1023) / 1024)); }
+int gradient_rows_per_group(int64_t rows) { return (int)std::min<int64_t>(kRowGroup, std::max<int64_t>(1, (rows + 1023) / 1024)); }
 
 struct BackwardSpace { _Float16* rows; float* factor; float* sums; int64_t partials; int64_t padded; float4v* partial; Split p; };
 size_t lay_out_backward(void* ws, int type, int64_t rows, const squant_codes_t& w, BackwardSpace& s) {
@@ -264,7 +263,10 @@ int squant_linear_backward(const void* d_dy, int64_t lddy, squant_wtype_t type, 
   r.scales = w.scales; r.kept = d_kept; r.kept_scales = d_kept_scales; r.act = (int)act; r.keep = (int)keep;
   r.rows_per_group = gradient_rows_per_group(rows);
   r.column_sums = d_dbias ? s.sums : nullptr;
-  if (int rc = launch(gradient_rows_kernel((int)type), (rows + r.rows_per_group - 1) / r.rows_per_group, 1, kRowThreads, 0, st, r)) return rc;
+  const int64_t groups = (rows + r.rows_per_group - 1) / r.rows_per_group, row_threads = (s.padded / 8 + kRowThreads - 1) / kRowThreads;
+  // about 512 workgroups, each of which looks for its rows' largest elements anew
+  const int shared = (int)std::max<int64_t>(1, std::min(row_threads, 512 / groups));
+  if (int rc = launch(gradient_rows_kernel((int)type), groups, shared, kRowThreads, 0, st, r)) return rc;
   if (d_dbias) {
     sums.partial = s.sums; sums.partials = s.partials;
     if (int rc = launch(column_sums_kernel(), sum_groups, 1, 1024, 0, st, sums)) return rc;
@@ -313,8 +315,7 @@ int squant_cross_entropy(const void* d_h, int64_t ldh, squant_wtype_t type, int6
   f.labels = d_labels; f.stats = s.stats; f.label_logit = s.label_logit;
   if (int rc = launch_product(layer_kernel((int)type, w, s.p), s.p, st, a)) return rc;
   const LossArgs l{s.stats, (w.cout + kTile - 1) / kTile, s.label_logit, d_labels, ignore_index, w.cout, rows, d_loss, d_lse};
-  constexpr int per = kRowThreads / kLanes;
-  return launch(loss_rows_kernel(), (rows + per - 1) / per, 1, kRowThreads, 0, st, l);
+  return launch(loss_rows_kernel(), rows, 1, kRowThreads, 0, st, l);
 }
 
 size_t squant_cross_entropy_backward_workspace_bytes(const void* d_h, int64_t ldh, squant_wtype_t type, int64_t rows, const squant_codes_t* h_w) {

@@ -278,7 +278,7 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
       for (int i = 0; i < 16; ++i) columns.scale[i] = shared_columns[wave_n * kTile + quad * 16 + i];
 #pragma unroll
       for (int i = 0; i < 16; ++i) columns.bias[i] = shared_columns[kWide + wave_n * kTile + quad * 16 + i];
-      finish_layer<16, T>(a.f, columns, row, col0 + quad * 16, v, PL);
+      finish_layer<16, T>(a.f, columns, row, col0 + quad * 16, v, row_factor_of(a.f, row), PL);
     }
   }
 }

@@ -68,44 +68,57 @@ def _workspace(x: torch.Tensor, nbytes: int, stream) -> Optional[torch.Tensor]:
     return ws
 
 
-def _rows(t: torch.Tensor, cols: int, what: str, like: Optional[torch.Tensor] = None):
-    """(rows, elements between rows) of an activation tensor whose last dimension is `cols`."""
-    if not t.is_cuda or t.dtype not in _WTYPES:
+def _device(t: torch.Tensor, what: str) -> int:
+    """The index of t's device, which has to be the current one."""
+    device = t.get_device()  # -1 on the host
+    if device < 0 or t.dtype not in _WTYPES:
         raise ValueError(f"{what} must be a float32, float16 or bfloat16 tensor in device memory")
-    if t.device.index != torch.cuda.current_device():
+    if device != torch.cuda.current_device():
         raise ValueError(f"{what} is not on the current device")
-    if like is not None and (t.dtype != like.dtype or t.shape[:-1] != like.shape[:-1]):
-        raise ValueError(f"{what} must have the type and the leading dimensions of the other activations")
-    if t.dim() == 0 or t.shape[-1] != cols:
+    return device
+
+
+def _rows(t: torch.Tensor, cols: int, what: str):
+    """(rows, elements between rows) of an activation tensor whose last dimension is `cols`."""
+    shape, stride = t.shape, t.stride()
+    n = len(shape)
+    if n == 0 or shape[-1] != cols:
         raise ValueError(f"{what} must have {cols} elements in its last dimension")
-    if cols > 1 and t.stride(-1) != 1:
+    if cols > 1 and stride[-1] != 1:
         raise ValueError(f"{what} must be contiguous in its last dimension")
-    if t.dim() == 1:
+    if n == 2:
+        rows = shape[0]
+        ld = stride[0] if rows > 1 else cols
+        if ld < cols:
+            raise ValueError(f"rows of {what} overlap")
+        return rows, ld
+    if n == 1:
         return 1, cols
-    if t.dim() > 2:
-        if not t.is_contiguous():
-            raise ValueError(f"{what} of more than two dimensions must be contiguous")
-        return t.numel() // cols, cols
-    rows = t.shape[0]
-    ld = t.stride(0) if rows > 1 else cols
-    if ld < cols:
-        raise ValueError(f"rows of {what} overlap")
-    return rows, ld
+    if not t.is_contiguous():
+        raise ValueError(f"{what} of more than two dimensions must be contiguous")
+    return t.numel() // cols, cols
 
 
-def _codes(codes: torch.Tensor, scales: torch.Tensor, cin: int, like: torch.Tensor) -> squant_codes_t:
-    if codes.dtype == torch.int8:
+def _like(t: torch.Tensor, cols: int, what: str, like: torch.Tensor, device: int) -> int:
+    """Elements between the rows of an activation tensor that goes with `like`."""
+    if t.dtype != like.dtype or t.get_device() != device or t.shape[:-1] != like.shape[:-1]:
+        raise ValueError(f"{what} must have the type, the device and the leading dimensions of the other activations")
+    return _rows(t, cols, what)[1]
+
+
+def _codes(codes: torch.Tensor, scales: torch.Tensor, cin: int, device: int) -> squant_codes_t:
+    if codes.dtype is torch.int8:
         fmt, row = OUT_INT8, cin
-    elif codes.dtype == torch.uint8:
+    elif codes.dtype is torch.uint8:
         fmt, row = OUT_INT4, (cin + 1) // 2
     else:
         raise ValueError("codes must be int8, or uint8 with two 4-bit codes a byte")
     cout = codes.shape[0] if codes.dim() else 0
     if cin <= 0 or cout <= 0 or codes.numel() != cout * row or not codes.is_contiguous():
         raise ValueError(f"codes must be contiguous with {row} bytes for each of their output channels")
-    if scales.dtype != torch.float32 or scales.dim() != 1 or scales.shape[0] != cout or not scales.is_contiguous():
+    if scales.dtype is not torch.float32 or scales.shape != (cout,) or not scales.is_contiguous():
         raise ValueError("scales must be a contiguous float32 tensor with one scale for each output channel")
-    if codes.device != like.device or scales.device != like.device:
+    if codes.get_device() != device or scales.get_device() != device:
         raise ValueError("codes and scales must be on the activations' device")
     return squant_codes_t(codes.data_ptr(), scales.data_ptr(), cout, cin, fmt)
 
@@ -123,20 +136,21 @@ def squant_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bi
     squant_linear_backward as (int8 codes, scales), as a tensor of x's type, or None.  `out` may be `residual`.
     Asynchronous on `stream` (default: torch's current stream)."""
     cin = x.shape[-1] if x.dim() else 0
+    device = _device(x, "x")
     rows, ldx = _rows(x, cin, "x")
-    w = _codes(codes, scales, cin, x)
+    w = _codes(codes, scales, cin, device)
     cout = w.cout
     shape = x.shape[:-1] + (cout,)
     if bias is not None and (bias.dtype != x.dtype or bias.shape != (cout,) or not bias.is_contiguous()
-                             or bias.device != x.device):
+                             or bias.get_device() != device):
         raise ValueError("bias must be contiguous, of x's type and device, with one element for each output channel")
     ldr = ldy = cout
     if residual is not None:
-        ldr = _rows(residual, cout, "residual", x)[1]
+        ldr = _like(residual, cout, "residual", x, device)
     if out is None:
-        out = torch.empty(shape, dtype=x.dtype, device=x.device)
+        out = x.new_empty(shape)
     else:
-        ldy = _rows(out, cout, "out", x)[1]
+        ldy = _like(out, cout, "out", x, device)
     kept = kept_scales = None
     how = KEEP_NONE if keep is None else keep
     if how == KEEP_INT8:
@@ -161,27 +175,28 @@ def squant_linear_backward(dy: torch.Tensor, codes: torch.Tensor, scales: torch.
 
     `kept` is what squant_linear returned beside y.  The residual's gradient is dy."""
     cout = codes.shape[0] if codes.dim() else 0
+    device = _device(dy, "dy")
     rows, lddy = _rows(dy, cout, "dy")
-    w = _codes(codes, scales, cin, dy)
+    w = _codes(codes, scales, cin, device)
     how, z, z_scales = KEEP_NONE, None, None
     if isinstance(kept, (tuple, list)):
         how, (z, z_scales) = KEEP_INT8, kept
         groups = dy.shape[:-1] + (-(-cout // _KEPT_GROUP),)
-        if (z.dtype != torch.int8 or z.shape != dy.shape or not z.is_contiguous() or z.device != dy.device
+        if (z.dtype != torch.int8 or z.shape != dy.shape or not z.is_contiguous() or z.get_device() != device
                 or z_scales.dtype != torch.float32 or z_scales.shape != groups or not z_scales.is_contiguous()
-                or z_scales.device != dy.device):
+                or z_scales.get_device() != device):
             raise ValueError("kept must be the pair that squant_linear returned for these rows")
     elif kept is not None:
         how, z = KEEP_FULL, kept
-        if z.dtype != dy.dtype or z.shape != dy.shape or not z.is_contiguous() or z.device != dy.device:
+        if z.dtype != dy.dtype or z.shape != dy.shape or not z.is_contiguous() or z.get_device() != device:
             raise ValueError("kept must be the tensor that squant_linear returned for these rows")
     shape = dy.shape[:-1] + (cin,)
     lddx = cin
     if dx is None:
-        dx = torch.empty(shape, dtype=dy.dtype, device=dy.device)
+        dx = dy.new_empty(shape)
     else:
-        lddx = _rows(dx, cin, "dx", dy)[1]
-    dbias = torch.empty(cout, dtype=dy.dtype, device=dy.device) if bias else None
+        lddx = _like(dx, cin, "dx", dy, device)
+    dbias = dy.new_empty(cout) if bias else None
     type_ = _WTYPES[dy.dtype]
     nbytes = _workspace_bytes("linear_backward", None, type_, rows, cout, cin, w.format)
     ws = _workspace(dy, nbytes, stream)
@@ -192,7 +207,7 @@ def squant_linear_backward(dy: torch.Tensor, codes: torch.Tensor, scales: torch.
 
 
 def _check_per_row(t: torch.Tensor, dtype, h: torch.Tensor, what: str):
-    if t.dtype != dtype or t.shape != h.shape[:-1] or not t.is_contiguous() or t.device != h.device:
+    if t.dtype != dtype or t.shape != h.shape[:-1] or not t.is_contiguous() or t.get_device() != h.get_device():
         raise ValueError(f"{what} must be a contiguous {dtype} tensor with one element for each row of h")
 
 
@@ -203,8 +218,9 @@ def squant_cross_entropy(h: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
     The logits are never in memory.  loss is 0 where the label is `ignore_index` and NaN where it is no entry of
     the vocabulary."""
     cin = h.shape[-1] if h.dim() else 0
+    device = _device(h, "h")
     rows, ldh = _rows(h, cin, "h")
-    w = _codes(codes, scales, cin, h)
+    w = _codes(codes, scales, cin, device)
     _check_per_row(labels, torch.int64, h, "labels")
     loss = torch.empty(h.shape[:-1], dtype=torch.float32, device=h.device)
     lse = torch.empty_like(loss)
@@ -222,8 +238,9 @@ def squant_cross_entropy_backward(h: torch.Tensor, codes: torch.Tensor, scales: 
                                   dh: Optional[torch.Tensor] = None, stream=None):
     """dh of squant_cross_entropy for the losses' gradients dloss (float32, one for each row)."""
     cin = h.shape[-1] if h.dim() else 0
+    device = _device(h, "h")
     rows, ldh = _rows(h, cin, "h")
-    w = _codes(codes, scales, cin, h)
+    w = _codes(codes, scales, cin, device)
     _check_per_row(labels, torch.int64, h, "labels")
     _check_per_row(lse, torch.float32, h, "lse")
     _check_per_row(dloss, torch.float32, h, "dloss")
@@ -231,7 +248,7 @@ def squant_cross_entropy_backward(h: torch.Tensor, codes: torch.Tensor, scales: 
     if dh is None:
         dh = torch.empty(h.shape, dtype=h.dtype, device=h.device)
     else:
-        lddh = _rows(dh, cin, "dh", h)[1]
+        lddh = _like(dh, cin, "dh", h, device)
     type_ = _WTYPES[h.dtype]
     nbytes = _workspace_bytes("cross_entropy_backward", (ldh | h.data_ptr() >> 1) & 7 == 0, type_, rows, w.cout, cin, w.format)
     ws = _workspace(h, nbytes, stream)

@@ -29,7 +29,7 @@ def codes(cout=8, cin=64, fmt=0, c=P, s=P):
     return ctypes.byref(squant_codes_t(c, s, cout, cin, fmt))
 
 
-def linear(L, x=P, ldx=64, type_=0, rows=4, w=None, bias=P, act=0, res=P, ldr=8, y=P, ldy=8, keep=0, kept=None, ks=None,
+def linear(L, x=P, ldx=64, type_=0, rows=100, w=None, bias=P, act=0, res=P, ldr=8, y=P, ldy=8, keep=0, kept=None, ks=None,
            ws=WS, nbytes=BIG):
     return L.squant_linear(x, ldx, type_, rows, codes() if w is None else w, bias, act, res, ldr, y, ldy, keep, kept, ks, ws,
                            nbytes, None)
@@ -79,7 +79,7 @@ def test_backward(L):
 
 
 def test_cross_entropy(L):
-    def f(h=P, ldh=64, type_=0, rows=4, labels=P, loss=P, lse=P, ws=WS, nbytes=BIG):
+    def f(h=P, ldh=64, type_=0, rows=100, labels=P, loss=P, lse=P, ws=WS, nbytes=BIG):
         return L.squant_cross_entropy(h, ldh, type_, rows, codes(), labels, -100, loss, lse, ws, nbytes, None)
 
     def g(h=P, ldh=64, type_=0, rows=4, labels=P, lse=P, dloss=P, dh=P, lddh=64, ws=WS, nbytes=BIG):
