@@ -57,7 +57,8 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductAr
   constexpr int kAhead = kAheadMost >= 4 && kRowsAhead ? 4 : kAheadMost >= 2 ? 2 : 1;
   typedef typename Codes<FMT>::row16 codes16;
   extern __shared__ __align__(16) unsigned char smem[];
-  const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+  const int lane = threadIdx.x & (kLanes - 1);
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kLanes);  // known to be uniform
   const int sub = lane & 15, quad = lane >> 4;
   const int32_t col0 = (int32_t)blockIdx.x * (16 * NF);
 

@@ -11,7 +11,9 @@
 namespace squant {
 namespace lin {
 
-constexpr int32_t kMaxSide = 1 << 24;    // of a layer
+// A side of a layer, and the distance of rows that are read in place: 255 rows of two planes are less than 2^32 bytes
+// apart.
+constexpr int32_t kMaxSide = 1 << 22;
 constexpr int64_t kMaxRows = 1 << 26;
 constexpr int kCus = 256;
 

@@ -94,7 +94,7 @@ struct RowOperand {
 
 // few_rows reads rows at any alignment and of any length.
 bool direct_rows(const void* x, int64_t ldx, int type, int64_t rows, int32_t cin) {
-  return rows <= few_rows_limit(planes_of(type)) || (type != SQUANT_W_F32 && cin % kBlock == 0 && ldx % 8 == 0 && !misaligned(x, 16));
+  return rows <= few_rows_limit(planes_of(type)) || (type != SQUANT_W_F32 && cin % kBlock == 0 && ldx % 8 == 0 && ldx <= kMaxSide && !misaligned(x, 16));
 }
 
 RowOperand lay_out_rows(Cutter& c, const void* x, int64_t ldx, int type, int64_t rows, int32_t cin, RowsArgs& r, bool& copy) {

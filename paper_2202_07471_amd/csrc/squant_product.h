@@ -1,7 +1,8 @@
 // The product of many rows with codes, for a layer (GRAD = false: the contraction runs along a code row) and
 // for its gradient (GRAD = true: across the code rows).
 //
-// A workgroup makes MT x 256 outputs with waves of (MT / 2) x 64 (64 x 64 where MT is 64).  The row operand goes to
+// A workgroup makes MT x 256 outputs with waves of (MT / 2) x 64 (64 x 64 where MT is 64: halves
+// of it that convert the same codes twice took 41 us where it takes 29, 1024 x 4096 x 2048).  The row operand goes to
 // the LDS without passing through registers, 64 contraction elements at a time in two buffers; rows of 128 bytes
 // with their 16-byte chunks exchanged by the row's low three bits, so that 8 lanes that read the same chunk of
 // 8 rows use all banks.  Codes go from memory to the registers of the waves that own their columns and are made
@@ -43,7 +44,8 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
   constexpr int kPlaneBytes = MT * kBlock * 2;
   constexpr int kBufBytes = kPlaneBytes * PL;
   extern __shared__ __align__(1024) unsigned char smem[];
-  const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+  const int lane = threadIdx.x & (kLanes - 1);
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kLanes);  // known to be uniform
   const int wave_m = wave % S::kWavesM, wave_n = wave / S::kWavesM;
 
   // Each XCD takes a run of consecutive tiles; within it, bands of 8 tiles of rows run along the columns, so that
@@ -67,19 +69,20 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
 
   // row operand: 8 rows an instruction; a row past the end is the last one again
   constexpr int kLoads = MT / 8 / S::kWaves;
-  const char* src[kLoads];
+  uint32_t src[kLoads];  // bytes from the tile's first row: kMaxSide keeps them in 32 bits
+  const char* rows = (const char*)a.a + row0 * a.lda * 2;
+  const int last_row = (int)min((int64_t)MT, a.f.rows - row0) - 1;
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
     const int r = (wave * kLoads + i) * 8 + (lane >> 3);
-    const int64_t row = min(row0 + r, a.f.rows - 1);
-    src[i] = (const char*)a.a + row * a.lda * 2 + (((lane & 7) ^ (r & 7)) << 4);
+    src[i] = (uint32_t)min(r, last_row) * (uint32_t)(a.lda * 2) + (((lane & 7) ^ (r & 7)) << 4);
   }
   auto load_rows = [&](int b, int buf) {
 #pragma unroll
     for (int p = 0; p < PL; ++p)
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
-        to_lds(src[i] + p * a.plane * 2 + (int64_t)b * (kBlock * 2),
+        to_lds(rows + (p * a.plane * 2 + (int64_t)b * (kBlock * 2)) + src[i],
                smem + buf * kBufBytes + p * kPlaneBytes + (wave * kLoads + i) * 1024);
   };
 
@@ -123,7 +126,7 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
     } else {
       const uint8_t* p = w_base + Codes<FMT>::offset((int64_t)b * kBlock);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) o.v[c].load(p + wsrc[c] - shift[c]);
+      for (int c = 0; c < 4; ++c) o.v[c].load(p + (wsrc[c] - shift[c]));
     }
   };
   // the same at the buffer's end
@@ -176,8 +179,11 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
         const int n = s + 1, nin = n % (PL * S::kFrags);
         x[n & 1] = row_frag(buf, nin / S::kFrags, n / (PL * S::kFrags), nin % S::kFrags);
       }
-      constexpr int per = PL * S::kFrags / 4;  // fragments of rows for each of the next half's operands
-      if (h == 0 && in % per == 0) w[1][in / per] = operand(r, 1, in / per);
+      if (h == 0) {
+        // the next half's operands, dealt to this half's fragments of rows
+#pragma unroll
+        for (int c = in * 4 / (PL * S::kFrags); c < (in + 1) * 4 / (PL * S::kFrags); ++c) w[1][c] = operand(r, 1, c);
+      }
       __builtin_amdgcn_sched_barrier(0x6);  // what is not arithmetic stays in its fragment
 #pragma unroll
       for (int c = 0; c < 4; ++c) acc[m][c] = F::mma(w[h][c], x[s & 1], acc[m][c]);
@@ -193,22 +199,28 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
   constexpr int kOthers = kIssued * (D - 2);  // may be on their way when a step begins
   static_assert(kOthers < 64, "the wait counter has six bits");
   const int steady = min(last, inside);
+  // No load moves over this: the count of one step's is told from the next one's.
+  auto in_order = []() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
   if (first < steady) {
     Raw<FMT, GRAD, WORDS> raw[D];
 #pragma unroll
     for (int i = 0; i < D - 1; ++i) {
       load_rows(min(first + i, steady - 1), i);
       load_codes(min(first + i, steady - 1), raw[i]);
+      in_order();
     }
 #pragma unroll 1
     for (int b0 = first; b0 < steady; b0 += D) {
 #pragma unroll
       for (int i = 0; i < D; ++i) {
         // not __syncthreads(), which would wait for every load
-        asm volatile("" ::: "memory");
+        in_order();
         __builtin_amdgcn_s_waitcnt((kOthers & 15) | (kOthers >> 4) << 14 | 0x070);
         __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        in_order();
         const int ahead = min(b0 + i + D - 1, steady - 1);
         load_rows(ahead, (i + D - 1) % D);
         load_codes(ahead, raw[(i + D - 1) % D]);
