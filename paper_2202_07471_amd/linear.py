@@ -19,6 +19,7 @@ ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "silu": ACT_SILU}
 KEEP_NONE, KEEP_INT8, KEEP_FULL = 0, 1, 2
 KEEPS = {"none": KEEP_NONE, "int8": KEEP_INT8, "full": KEEP_FULL}
 IGNORE_INDEX = -100
+_MAX_STRIDE = 1 << 22  # elements between rows that are read as they are
 _KEPT_GROUP = 64  # columns of a row that share a scale of the kept pre-activation
 
 
@@ -59,13 +60,13 @@ def _workspace_bytes(call: str, aligned, type_: int, rows: int, cout: int, cin: 
     return int(getattr(_lib(), f"squant_{call}_workspace_bytes")(*x, type_, rows, ctypes.byref(w), *rest))
 
 
-def _workspace(x: torch.Tensor, nbytes: int, stream) -> Optional[torch.Tensor]:
-    if nbytes == 0:
-        return None
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
-    if stream is not None:
-        ws.record_stream(stream)
-    return ws
+def _workspace(x: torch.Tensor, nbytes: int) -> Optional[torch.Tensor]:
+    return torch.empty(nbytes, dtype=torch.uint8, device=x.device) if nbytes else None
+
+
+def _aligned(t: torch.Tensor, ld: int) -> bool:
+    """Whether the products read 16-bit rows as they are, if their length allows it."""
+    return (ld | t.data_ptr() >> 1) & 7 == 0 and ld <= _MAX_STRIDE
 
 
 def _device(t: torch.Tensor, what: str) -> int:
@@ -134,7 +135,10 @@ def squant_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bi
 
     With `keep` (KEEP_INT8, KEEP_FULL or KEEP_NONE) returns (y, kept): the pre-activation for
     squant_linear_backward as (int8 codes, scales), as a tensor of x's type, or None.  `out` may be `residual`.
-    Asynchronous on `stream` (default: torch's current stream)."""
+    Asynchronous on `stream` (default: torch's current stream), which the outputs and the workspace belong to."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return squant_linear(x, codes, scales, bias, act, residual, keep, out)
     cin = x.shape[-1] if x.dim() else 0
     device = _device(x, "x")
     rows, ldx = _rows(x, cin, "x")
@@ -159,11 +163,11 @@ def squant_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bi
     elif how == KEEP_FULL:
         kept = torch.empty(shape, dtype=x.dtype, device=x.device)
     type_ = _WTYPES[x.dtype]
-    nbytes = _workspace_bytes("linear", (ldx | x.data_ptr() >> 1) & 7 == 0, type_, rows, cout, cin, w.format, how)
-    ws = _workspace(x, nbytes, stream)
+    nbytes = _workspace_bytes("linear", _aligned(x, ldx), type_, rows, cout, cin, w.format, how)
+    ws = _workspace(x, nbytes)
     _check(_lib().squant_linear(x.data_ptr(), ldx, type_, rows, ctypes.byref(w), _ptr(bias), act, _ptr(residual), ldr,
                                 out.data_ptr(), ldy, how, _ptr(kept), _ptr(kept_scales), _ptr(ws), nbytes,
-                                _stream_ptr(stream)))
+                                _stream_ptr(None)))
     if keep is None:
         return out
     return out, ((kept, kept_scales) if how == KEEP_INT8 else kept)
@@ -174,6 +178,9 @@ def squant_linear_backward(dy: torch.Tensor, codes: torch.Tensor, scales: torch.
     """(dx, dbias) of squant_linear for dy [..., cout], codes and scales held fixed; dbias is None without `bias`.
 
     `kept` is what squant_linear returned beside y.  The residual's gradient is dy."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return squant_linear_backward(dy, codes, scales, cin, act, kept, bias, dx)
     cout = codes.shape[0] if codes.dim() else 0
     device = _device(dy, "dy")
     rows, lddy = _rows(dy, cout, "dy")
@@ -199,10 +206,10 @@ def squant_linear_backward(dy: torch.Tensor, codes: torch.Tensor, scales: torch.
     dbias = dy.new_empty(cout) if bias else None
     type_ = _WTYPES[dy.dtype]
     nbytes = _workspace_bytes("linear_backward", None, type_, rows, cout, cin, w.format)
-    ws = _workspace(dy, nbytes, stream)
+    ws = _workspace(dy, nbytes)
     _check(_lib().squant_linear_backward(dy.data_ptr(), lddy, type_, rows, ctypes.byref(w), act, how, _ptr(z),
                                          _ptr(z_scales), dx.data_ptr(), lddx, _ptr(dbias), _ptr(ws), nbytes,
-                                         _stream_ptr(stream)))
+                                         _stream_ptr(None)))
     return dx, dbias
 
 
@@ -217,6 +224,9 @@ def squant_cross_entropy(h: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
 
     The logits are never in memory.  loss is 0 where the label is `ignore_index` and NaN where it is no entry of
     the vocabulary."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return squant_cross_entropy(h, codes, scales, labels, ignore_index)
     cin = h.shape[-1] if h.dim() else 0
     device = _device(h, "h")
     rows, ldh = _rows(h, cin, "h")
@@ -225,11 +235,11 @@ def squant_cross_entropy(h: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
     loss = torch.empty(h.shape[:-1], dtype=torch.float32, device=h.device)
     lse = torch.empty_like(loss)
     type_ = _WTYPES[h.dtype]
-    nbytes = _workspace_bytes("cross_entropy", (ldh | h.data_ptr() >> 1) & 7 == 0, type_, rows, w.cout, cin, w.format)
-    ws = _workspace(h, nbytes, stream)
+    nbytes = _workspace_bytes("cross_entropy", _aligned(h, ldh), type_, rows, w.cout, cin, w.format)
+    ws = _workspace(h, nbytes)
     _check(_lib().squant_cross_entropy(h.data_ptr(), ldh, type_, rows, ctypes.byref(w), labels.data_ptr(),
                                        ignore_index, loss.data_ptr(), lse.data_ptr(), _ptr(ws), nbytes,
-                                       _stream_ptr(stream)))
+                                       _stream_ptr(None)))
     return loss, lse
 
 
@@ -237,6 +247,9 @@ def squant_cross_entropy_backward(h: torch.Tensor, codes: torch.Tensor, scales: 
                                   lse: torch.Tensor, dloss: torch.Tensor, ignore_index: int = IGNORE_INDEX,
                                   dh: Optional[torch.Tensor] = None, stream=None):
     """dh of squant_cross_entropy for the losses' gradients dloss (float32, one for each row)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return squant_cross_entropy_backward(h, codes, scales, labels, lse, dloss, ignore_index, dh)
     cin = h.shape[-1] if h.dim() else 0
     device = _device(h, "h")
     rows, ldh = _rows(h, cin, "h")
@@ -250,11 +263,11 @@ def squant_cross_entropy_backward(h: torch.Tensor, codes: torch.Tensor, scales: 
     else:
         lddh = _like(dh, cin, "dh", h, device)
     type_ = _WTYPES[h.dtype]
-    nbytes = _workspace_bytes("cross_entropy_backward", (ldh | h.data_ptr() >> 1) & 7 == 0, type_, rows, w.cout, cin, w.format)
-    ws = _workspace(h, nbytes, stream)
+    nbytes = _workspace_bytes("cross_entropy_backward", _aligned(h, ldh), type_, rows, w.cout, cin, w.format)
+    ws = _workspace(h, nbytes)
     _check(_lib().squant_cross_entropy_backward(h.data_ptr(), ldh, type_, rows, ctypes.byref(w), labels.data_ptr(),
                                                 ignore_index, lse.data_ptr(), dloss.data_ptr(), dh.data_ptr(), lddh,
-                                                _ptr(ws), nbytes, _stream_ptr(stream)))
+                                                _ptr(ws), nbytes, _stream_ptr(None)))
     return dh
 
 
@@ -268,13 +281,13 @@ def _rowwise(t: torch.Tensor) -> torch.Tensor:
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, codes, scales, bias, act, residual, keep):
-        ctx.act, ctx.cin, ctx.codes, ctx.scales = act, x.shape[-1], codes, scales
+        ctx.act, ctx.cin = act, x.shape[-1]
         needed = ctx.needs_input_grad[0] or ctx.needs_input_grad[3]
         how = keep if act != ACT_NONE and needed else KEEP_NONE
         y, kept = squant_linear(_rowwise(x), codes, scales, bias, act,
                                 None if residual is None else _rowwise(residual), keep=how)
         ctx.pair = isinstance(kept, tuple)
-        ctx.save_for_backward(*(kept if ctx.pair else (kept,)))
+        ctx.save_for_backward(codes, scales, *(kept if ctx.pair else (kept,)))
         return y
 
     @staticmethod
@@ -282,8 +295,8 @@ class _Linear(torch.autograd.Function):
     def backward(ctx, dy):
         dx = dbias = None
         if ctx.needs_input_grad[0] or ctx.needs_input_grad[3]:
-            kept = ctx.saved_tensors
-            dx, dbias = squant_linear_backward(_rowwise(dy), ctx.codes, ctx.scales, ctx.cin, ctx.act,
+            codes, scales, *kept = ctx.saved_tensors
+            dx, dbias = squant_linear_backward(_rowwise(dy), codes, scales, ctx.cin, ctx.act,
                                                kept if ctx.pair else kept[0], bias=ctx.needs_input_grad[3])
         return (dx if ctx.needs_input_grad[0] else None, None, None, dbias, None,
                 dy if ctx.needs_input_grad[5] else None, None)
@@ -294,16 +307,16 @@ class _CrossEntropy(torch.autograd.Function):
     def forward(ctx, h, codes, scales, labels, ignore_index):
         h = _rowwise(h)
         loss, lse = squant_cross_entropy(h, codes, scales, labels, ignore_index)
-        ctx.codes, ctx.scales, ctx.ignore_index = codes, scales, ignore_index
-        ctx.save_for_backward(h, labels, lse)
+        ctx.ignore_index = ignore_index
+        ctx.save_for_backward(h, codes, scales, labels, lse)
         return loss
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dloss):
-        h, labels, lse = ctx.saved_tensors
-        return (squant_cross_entropy_backward(h, ctx.codes, ctx.scales, labels, lse, dloss.contiguous(),
-                                              ctx.ignore_index), None, None, None, None)
+        h, codes, scales, labels, lse = ctx.saved_tensors
+        return (squant_cross_entropy_backward(h, codes, scales, labels, lse, dloss.contiguous(), ctx.ignore_index),
+                None, None, None, None)
 
 
 def quantized_linear(x, codes, scales, bias=None, act: int = ACT_NONE, residual=None, keep: int = KEEP_INT8):

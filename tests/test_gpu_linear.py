@@ -325,3 +325,46 @@ def test_offsets_beyond_32_bits(sq):
     dy[:, -1] = 1
     dx, _ = sq.squant_linear_backward(dy, codes, scales, k)
     assert (dx[:, :-1] == 1).all() and (dx[:, -1] == 5).all()
+
+
+def test_memory_belongs_to_the_given_stream(sq):
+    """Outputs of a call on another stream do not take memory that the current stream has just let go of."""
+    rng = np.random.default_rng(31)
+    x, c, scales, _ = real_case(rng, 600, 512, 1024, BF16, "int8")
+    x, c, scales = x.cuda(), c.cuda(), scales.cuda()
+    want = sq.squant_linear(x, c, scales)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    freed = torch.empty(600, 1024, dtype=BF16, device="cuda")
+    at = freed.data_ptr()
+    del freed
+    y = sq.squant_linear(x, c, scales, stream=side)
+    side.synchronize()
+    assert y.data_ptr() != at and torch.equal(y, want)
+    again = torch.empty(600, 1024, dtype=BF16, device="cuda")
+    assert again.data_ptr() == at
+
+
+@pytest.mark.parametrize("m", [3, 70])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_far_apart(sq, m, dtype):
+    """More than 2^22 elements between rows: rows are laid out before the product."""
+    rng = np.random.default_rng(37)
+    x, c, scales, _ = real_case(rng, m, 128, 70, dtype, "int8")
+    wide = torch.empty(m, (1 << 22) + 64, dtype=dtype, device="cuda")
+    wide[:, 8:136] = x.cuda()
+    assert torch.equal(sq.squant_linear(wide[:, 8:136], c.cuda(), scales.cuda()), sq.squant_linear(x.cuda(), c.cuda(), scales.cuda()))
+
+
+def test_codes_changed_before_the_backward_pass_are_noticed(sq):
+    rng = np.random.default_rng(41)
+    x, c, scales, _ = real_case(rng, 9, 64, 48, F32, "int8")
+    x, c, scales = x.cuda().requires_grad_(), c.cuda(), scales.cuda()
+    y = sq.quantized_linear(x, c, scales)
+    c.zero_()
+    with pytest.raises(RuntimeError):
+        y.sum().backward()
+    loss = sq.quantized_cross_entropy(x, c, scales, torch.zeros(9, dtype=torch.int64, device="cuda"))
+    scales.mul_(2)
+    with pytest.raises(RuntimeError):
+        loss.sum().backward()
