@@ -86,7 +86,7 @@ struct ProductArgs {
   int32_t blocks;      // ceil(contraction / 64)
   int32_t slices;      // the contraction is cut into this many
   int32_t tiles_m, tiles_n;
-  int32_t slice0;      // first slice's index in `partial`
+  int accumulate;      // kPartial: the sums are added to those in `partial`
   Finish f;
 };
 
@@ -537,8 +537,9 @@ __device__ __forceinline__ void finish_layer(const Finish& f, const Columns<NC>&
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
       float sum = 0.0f;
+      const float from = top == -__builtin_inff() ? 0.0f : top;  // a chunk without a finite logit adds nothing
 #pragma unroll
-      for (int i = 0; i < NC; ++i) sum += i < valid ? exp2_fast(v[i] - top) : 0.0f;
+      for (int i = 0; i < NC; ++i) sum += i < valid ? exp2_fast(v[i] - from) : 0.0f;
       sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
       if (live && col < f.cols && (col & (kTile - 1)) == 0)

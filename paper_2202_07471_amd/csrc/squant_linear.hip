@@ -52,7 +52,7 @@ struct Cutter {
 int64_t code_row(const squant_codes_t& w) { return w.format == SQUANT_OUT_INT8 ? w.cin : ((int64_t)w.cin + 1) / 2; }
 
 template <class A> int launch(void (*k)(A), int64_t gx, int gy, int threads, size_t lds, hipStream_t st, const A& a) {
-  if (gx > 0x7fffffff) return SQUANT_ERR_SHAPE;
+  if (gx * threads > 0xffffffffLL) return SQUANT_ERR_SHAPE;  // a launch counts its threads in 32 bits
   hipLaunchKernelGGL(k, dim3((unsigned)gx, (unsigned)gy), dim3((unsigned)threads), (unsigned)lds, st, a);
   return hipGetLastError() == hipSuccess ? SQUANT_OK : SQUANT_ERR_DEVICE;
 }
@@ -120,9 +120,9 @@ void set_product(ProductArgs& a, const RowOperand& x, const squant_codes_t& w, c
   a.blocks = p.blocks; a.slices = p.slices; a.tiles_m = p.tiles_m; a.tiles_n = p.tiles_n;
 }
 
-int launch_join(bool grad, int type, const Split& p, int slices, const float4v* partial, const Finish& f, hipStream_t st) {
+int launch_join(bool grad, int type, const Split& p, const float4v* partial, const Finish& f, hipStream_t st) {
   JoinArgs j{};
-  j.partial = partial; j.slices = slices; j.row_frags = p.row_frags_all; j.col_frags = p.col_frags_all; j.f = f;
+  j.partial = partial; j.slices = p.slices; j.row_frags = p.row_frags_all; j.col_frags = p.col_frags_all; j.f = f;
   j.planes = planes_of(type);
   const int64_t waves = p.row_frags_all * (p.col_frags_all / 4);
   constexpr int per = kRowThreads / kLanes;
@@ -180,7 +180,7 @@ size_t lay_out_loss_backward(void* ws, const void* h, int64_t ldh, int type, int
   s.pieces = (int32_t)((w.cout + s.piece - 1) / s.piece);
   s.prob = c.take<_Float16>(rows * planes * s.piece);
   s.g = split_gradient(rows, w.cin, s.piece, planes);
-  s.partial = c.take<float4v>(s.g.partial_vectors() * s.pieces);
+  s.partial = c.take<float4v>(s.g.partial_vectors());
   return c.used;
 }
 
@@ -226,7 +226,7 @@ int squant_linear(const void* d_x, int64_t ldx, squant_wtype_t type, int64_t row
   const Finish done = f;
   if (s.p.slices > 1) { f.kind = kPartial; f.partial = s.partial; }
   if (int rc = launch_product(layer_kernel((int)type, w, s.p), s.p, st, a)) return rc;
-  return s.p.slices > 1 ? launch_join(false, (int)type, s.p, s.p.slices, s.partial, done, st) : SQUANT_OK;
+  return s.p.slices > 1 ? launch_join(false, (int)type, s.p, s.partial, done, st) : SQUANT_OK;
 }
 
 size_t squant_linear_backward_workspace_bytes(squant_wtype_t type, int64_t rows, const squant_codes_t* h_w) {
@@ -281,7 +281,7 @@ int squant_linear_backward(const void* d_dy, int64_t lddy, squant_wtype_t type, 
   if (s.p.slices > 1) { f.kind = kPartial; f.partial = s.partial; }
   const product_t k = planes == 2 ? gradient_2((int)w.format, s.p.mt) : gradient_1((int)w.format, s.p.mt);
   if (int rc = launch_product(k, s.p, st, a)) return rc;
-  return s.p.slices > 1 ? launch_join(true, (int)type, s.p, s.p.slices, s.partial, done, st) : SQUANT_OK;
+  return s.p.slices > 1 ? launch_join(true, (int)type, s.p, s.partial, done, st) : SQUANT_OK;
 }
 
 size_t squant_cross_entropy_workspace_bytes(const void* d_h, int64_t ldh, squant_wtype_t type, int64_t rows, const squant_codes_t* h_w) {
@@ -362,7 +362,7 @@ int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t t
     Split split = s.g;
     split.blocks = (int32_t)((piece.cout + kBlock - 1) / kBlock);
     set_product(g, RowOperand{s.prob, planes * s.piece, s.piece, nullptr}, piece, split);
-    g.slice0 = i * s.g.slices;
+    g.accumulate = i > 0;  // what a long batch needs beside its rows does not grow with the vocabulary
     g.f.kind = kPartial; g.f.rows = rows; g.f.cols = w.cin; g.f.partial = s.partial;
     const product_t k = planes == 2 ? gradient_2((int)w.format, s.g.mt) : gradient_1((int)w.format, s.g.mt);
     if (int rc = launch_product(k, split, st, g)) return rc;
@@ -371,7 +371,7 @@ int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t t
   f.kind = kGradLoss; f.out_type = (int)type; f.unit = kColumnUnitInverse; f.rows = rows; f.cols = w.cin; f.scales = w.scales;
   f.out = d_dh; f.ldo = lddh; f.labels = d_labels; f.ignore = ignore_index; f.dloss = d_dloss; f.prob_unit = s.unit;
   f.first_col = w.cout; f.codes = (const uint8_t*)w.codes; f.code_row = w_row; f.format = (int)w.format;
-  return launch_join(true, (int)type, s.g, s.g.slices * s.pieces, s.partial, f, st);
+  return launch_join(true, (int)type, s.g, s.partial, f, st);
 }
 
 }  // extern "C"

@@ -244,10 +244,13 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
     const int64_t frags_n = (int64_t)a.tiles_n * (kWide / 16);
 #pragma unroll
     for (int m = 0; m < S::kFrags; ++m) {
-      const int64_t row_frag = ((int64_t)slice + a.slice0) * a.tiles_m * (MT / 16) + tile_m * (MT / 16) + wave_m * S::kFrags + m;
+      const int64_t row_frag = (int64_t)slice * a.tiles_m * (MT / 16) + tile_m * (MT / 16) + wave_m * S::kFrags + m;
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        a.f.partial[(row_frag * frags_n + (col0 / 16 + c)) * kLanes + lane] = acc[m][c];
+      for (int c = 0; c < 4; ++c) {
+        float4v* p = a.f.partial + (row_frag * frags_n + (col0 / 16 + c)) * kLanes + lane;
+        if (a.accumulate) acc[m][c] += *p;
+        *p = acc[m][c];
+      }
     }
     return;
   }

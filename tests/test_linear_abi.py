@@ -126,3 +126,14 @@ def test_header_compiles_as_c(tmp_path):
                    'int probe(void) { squant_codes_t w; (void)w; return (int)SQUANT_ACT_SILU + (int)SQUANT_KEEP_FULL; }\n')
     subprocess.check_call(["gcc", "-std=c99", "-pedantic", "-Wall", "-Werror", "-fsyntax-only",
                            "-I", os.path.join(ROOT, "include"), str(src)])
+
+
+def test_the_gradient_of_a_long_batch_needs_no_more_for_a_larger_vocabulary(L):
+    """Several pieces of the vocabulary add to the same sums."""
+    small, large = (L.squant_cross_entropy_backward_workspace_bytes(P, 4096, 2, 32768, codes(v, 4096)) for v in (1 << 15, 1 << 18))
+    assert large <= small * 1.1 and large < 2 << 30
+
+
+def test_more_threads_than_a_launch_has_are_refused(L):
+    """A launch counts its threads in 32 bits: rows of which each takes a workgroup."""
+    assert L.squant_cross_entropy(P, 64, 0, 1 << 25, codes(), P, -100, P, P, WS, BIG, None) == SHAPE
