@@ -211,14 +211,16 @@ int64_t squant_max_channel_elems(int32_t kh, int32_t kw);
  * activation buffers of a call (x, bias, residual, y, dy, dx, dbias).  Codes times activations are
  * multiplied exactly (binary32 activations to 22 bits) and added in binary32; every output is rounded
  * once.  Rows may be any distance apart (ld*, in elements, at least the row's length); activation
- * buffers need the alignment of their element type, codes none.
+ * buffers need the alignment of their element type, codes none.  Where codes or rows do not lie as the
+ * matrix units' kernels read them (cin a multiple of 64, 16-byte aligned; few rows: anything goes) a call
+ * copies them to its workspace first.
  *
- * d_workspace: the *_workspace_bytes call's amount (which depends on the shapes and, through the rows'
- * alignment, on the address and distance of x or h; 0 for many calls, NULL then), 256-byte aligned, not shared
- * with a call that may run at the same time; it holds nothing between calls.  rows = 0 is a no-op, apart from d_dbias, which
- * becomes 0.  The calls launch kernels only and may be captured into a HIP graph.  Infinities and NaN in
- * the activations act as IEEE arithmetic has it (an infinity times a code of 0 is NaN, and a row that
- * holds one may be NaN where exact arithmetic has an infinity). */
+ * d_workspace: the *_workspace_bytes call's amount (which depends on the shapes, on ldx or ldh and on
+ * whether x or h and the codes are 16-byte aligned; 0 for many calls, NULL then), 256-byte aligned, not
+ * shared with a call that may run at the same time; it holds nothing between calls.  rows = 0 is a no-op,
+ * apart from d_dbias, which becomes 0.  The calls launch kernels only and may be captured into a HIP
+ * graph.  Infinities and NaN in the activations act as IEEE arithmetic has it (an infinity times a code of
+ * 0 is NaN, and a row that holds one may be NaN where exact arithmetic has an infinity). */
 
 /* A quantised layer: codes as squant_quantize_ex writes them for SQUANT_OUT_INT8 or SQUANT_OUT_INT4,
  * rows of cin codes (cin * kh * kw of a convolution's unfolded input). */

@@ -5,9 +5,9 @@
 namespace squant {
 namespace lin {
 
-product_t layer_f32(int format, int mt, bool words) {
-  return format == SQUANT_OUT_INT4 ? layer_of<Half, 2, SQUANT_OUT_INT4>(mt, words)
-                                   : layer_of<Half, 2, SQUANT_OUT_INT8>(mt, words);
+product_t layer_f32(int format, int mt) {
+  return format == SQUANT_OUT_INT4 ? product_of<Half, 2, SQUANT_OUT_INT4, false>(mt)
+                                   : product_of<Half, 2, SQUANT_OUT_INT8, false>(mt);
 }
 
 }  // namespace lin

@@ -5,6 +5,7 @@ namespace squant {
 namespace lin {
 
 __global__ void __launch_bounds__(kRowThreads) pad_rows(RowsArgs a) {
+  if (a.w.chunks && blockIdx.x >= a.w.first_block) return lay_codes(a.w, blockIdx.x - a.w.first_block);
   const int64_t vectors = a.padded / 8;
   const int64_t at = (int64_t)blockIdx.x * kRowThreads + threadIdx.x;
   if (at >= a.rows * vectors) return;
@@ -25,6 +26,7 @@ __global__ void __launch_bounds__(kRowThreads) pad_rows(RowsArgs a) {
 __global__ void __launch_bounds__(kRowThreads) split_rows(RowsArgs a) {
   constexpr int kHeld = 4;  // vectors of 8 elements a thread keeps: rows up to 8192 are read once
   __shared__ uint32_t tops[kRowThreads / kLanes];
+  if (a.w.chunks && blockIdx.x >= a.w.first_block) return lay_codes(a.w, blockIdx.x - a.w.first_block);
   const int64_t row = blockIdx.x;
   const float* x = (const float*)a.x + row * a.ldx;
   float v[kHeld][8];

@@ -78,7 +78,8 @@ struct ProductArgs {
   const void* a;       // row operand [rows][planes][blocks * 64], zero beyond the contraction's length
   int64_t lda;         // elements between rows
   int64_t plane;       // elements between planes
-  const uint8_t* w;    // codes; for a piece of the vocabulary, its first row
+  const uint8_t* w;    // codes; for a piece of the vocabulary, its first row.  `product`: rows of whole 16-byte words, for a
+                       // layer of whole steps
   int64_t w_row;       // bytes of a code row
   int32_t w_rows;      // code rows
   int32_t w_cols;      // codes of a row
@@ -201,36 +202,6 @@ __device__ __forceinline__ typename F::frag convert(const typename Codes<FMT>::r
   const uint4v v = {o[0], o[1], o[2], o[3]};
   return __builtin_bit_cast(typename F::frag, v);
 }
-
-// 16 codes of a row, as loaded.  Loads off a 32-bit boundary cost two to three times an aligned one (1024 rows by
-// 4096 x 2049 int8 codes: 79 us, 36 us by 4096 x 2052), so rows that do not begin at whole words (WORDS false) are
-// read as the words that hold them, one more than there are words of codes, and shifted into place by their
-// address's low two bits.  No word is read that holds no byte of the buffer: the row has more codes after these, or
-// the shift is not 0.
-template <int FMT, bool WORDS> struct RowCodes;
-template <int FMT> struct RowCodes<FMT, true> {
-  typename Codes<FMT>::row16 v;
-  __device__ __forceinline__ void load(const uint8_t* p) { v = load_any<typename Codes<FMT>::row16>(p); }
-  __device__ __forceinline__ void set(typename Codes<FMT>::row16 o) { v = o; }
-  __device__ __forceinline__ typename Codes<FMT>::row16 aligned(int, uint32_t) const { return v; }
-};
-template <int FMT> struct RowCodes<FMT, false> {
-  static constexpr int n = Codes<FMT>::kRow16 / 4;
-  typename Codes<FMT>::row16 v;
-  uint32_t after;
-  __device__ __forceinline__ void load(const uint8_t* p) {
-    v = load_any<typename Codes<FMT>::row16>(p);
-    after = load_any<uint32_t>(p + 4 * n);
-  }
-  __device__ __forceinline__ void set(typename Codes<FMT>::row16 o) { v = o; after = 0; }
-  // the words that half h of the codes is in
-  __device__ __forceinline__ typename Codes<FMT>::row16 aligned(int h, uint32_t shift) const {
-    typename Codes<FMT>::row16 o = v;
-#pragma unroll
-    for (int i = h * n / 2; i < (h + 1) * n / 2; ++i) o[i] = __builtin_amdgcn_alignbyte(i + 1 < n ? v[i + 1 < n ? i + 1 : 0] : after, v[i], shift);
-    return o;
-  }
-};
 
 // Column j of 8 code rows of 4 columns each, as multiples of 2^-9.
 template <int FMT>

@@ -8,9 +8,9 @@ namespace lin {
 
 // `mt` 64, 128 or 256 rows a workgroup; `mf` fragments of 16 rows, 1, 2 or 4; `nf` of 16 columns, 1, 2 or 4;
 // `words`: code rows begin at whole 32-bit words.
-product_t layer_bf16(int format, int mt, bool words);
-product_t layer_f16(int format, int mt, bool words);
-product_t layer_f32(int format, int mt, bool words);
+product_t layer_bf16(int format, int mt);
+product_t layer_f16(int format, int mt);
+product_t layer_f32(int format, int mt);
 product_t gradient_1(int format, int mt);  // planes of the row operand
 product_t gradient_2(int format, int mt);
 product_t few_bf16(int format, int mf, int nf, bool words);

@@ -26,17 +26,13 @@ struct Split {
   int blocks, slices;
   int64_t workgroups;  // of a slice
   int threads;
-  size_t lds;
+  size_t lds;          // few_rows
   int64_t row_frags_all, col_frags_all;  // of the partial sums
   int64_t partial_vectors() const { return (int64_t)slices * row_frags_all * col_frags_all * kLanes; }
 };
 
 inline int shape_threads(int mt) {
   return mt == 256 ? Shape<256>::kThreads : mt == 128 ? Shape<128>::kThreads : Shape<64>::kThreads;
-}
-
-inline int shape_depth(int mt) {
-  return mt == 256 ? Shape<256>::kDepth : mt == 128 ? Shape<128>::kDepth : Shape<64>::kDepth;
 }
 
 // `product` over rows x cols with a contraction of `depth`: the rows of a workgroup and the slices of the
@@ -47,7 +43,8 @@ inline Split split_product(int64_t rows, int64_t cols, int64_t depth, int planes
   const int blocks = (int)((depth + kBlock - 1) / kBlock);
   for (int mt = 64; mt <= 256; mt *= 2) {
     const int64_t tm = (rows + mt - 1) / mt, tn = (cols + kWide - 1) / kWide;
-    const double step = (mt == 256 ? 1.5 : mt == 128 ? 0.9 : 0.6) * planes;  // us of 64 contraction elements
+    // us of 64 contraction elements; two planes share the codes' conversion
+    const double step = planes == 1 ? (mt == 256 ? 1.6 : mt == 128 ? 0.87 : 0.55) : (mt == 256 ? 2.9 : mt == 128 ? 1.6 : 0.97);
     for (int s = 1; s <= 64 && s <= blocks; s = s < 4 ? s + 1 : s * 2) {
       if (s > 1 && !may_split) break;
       const int64_t rounds = (tm * tn * s + kCus - 1) / kCus;
@@ -63,7 +60,6 @@ inline Split split_product(int64_t rows, int64_t cols, int64_t depth, int planes
   best.blocks = blocks;
   best.workgroups = (int64_t)best.tiles_m * best.tiles_n;
   best.threads = shape_threads(best.mt);
-  best.lds = (size_t)best.mt * kBlock * 2 * planes * shape_depth(best.mt);
   best.row_frags_all = (int64_t)best.tiles_m * (best.mt / 16);
   best.col_frags_all = (int64_t)best.tiles_n * (kWide / 16);
   return best;

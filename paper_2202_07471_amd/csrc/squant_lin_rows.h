@@ -10,7 +10,19 @@ namespace lin {
 constexpr int kRowThreads = 256;
 constexpr int kRowGroup = 16;  // most rows a workgroup of gradient_rows takes
 
+// Code rows copied to rows of whole steps at multiples of 16 bytes, zeros at their ends: by the workgroups of a launch
+// past `first_block`, so that it costs no launch where there are rows to lay out as well.
+struct CodesArgs {
+  const uint8_t* codes;
+  int64_t row;              // bytes
+  uint8_t* out;
+  int32_t out_row;          // bytes
+  int64_t chunks;           // 16 bytes of `out` each; 0: nothing to lay out
+  int64_t first_block;
+};
+
 struct RowsArgs {
+  CodesArgs w;
   const void* x;            // rows, or the output's gradient
   int64_t ldx;
   int64_t rows;
@@ -52,6 +64,34 @@ __device__ __forceinline__ void store_planes(_Float16* p, int64_t plane, const f
   if (PL == 2) *(half8*)(p + plane) = lo;
 }
 
+__device__ __forceinline__ void lay_codes(const CodesArgs& w, int64_t block) {
+  const int64_t at = block * kRowThreads + threadIdx.x;
+  if (at >= w.chunks) return;
+  const int32_t per = w.out_row / 16;
+  int64_t row;
+  if (w.chunks <= 0xffffffffLL) row = (uint32_t)at / (uint32_t)per;  // a third of the instructions of 64 bits
+  else row = at / per;
+  const int32_t c = (int32_t)(at - row * per) * 16;
+  const uint8_t* p = w.codes + row * w.row + c;
+  uint4v o = {0, 0, 0, 0};
+  if (c + 16 <= w.row) {
+    // the words that hold the bytes: the last one is read only if it holds some
+    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3u);
+    const uint32_t* words = reinterpret_cast<const uint32_t*>(p - off);
+    uint32_t v[5];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = words[i];
+    v[4] = off ? words[4] : 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_alignbyte(v[i + 1], v[i], off);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (c + i < w.row) o[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+  }
+  *(uint4v*)(w.out + at * 16) = o;
+}
+
 // 16-bit rows copied to where they are aligned and end with zeros.  Any 16-bit type.
 __global__ void __launch_bounds__(kRowThreads) pad_rows(RowsArgs a);
 // binary32 rows to two planes, a workgroup a row.
@@ -65,6 +105,7 @@ __global__ void __launch_bounds__(kRowThreads) split_rows(RowsArgs a);
 template <class T, int PL>
 __global__ void __launch_bounds__(kRowThreads) gradient_rows(RowsArgs a) {
   __shared__ uint32_t tops[kRowGroup];
+  if (a.w.chunks && blockIdx.x >= a.w.first_block) return lay_codes(a.w, (blockIdx.x - a.w.first_block) * gridDim.y + blockIdx.y);
   const int lane = threadIdx.x & (kLanes - 1);
   const int64_t row0 = (int64_t)blockIdx.x * a.rows_per_group;
   const int n_rows = (int)min((int64_t)a.rows_per_group, a.rows - row0);

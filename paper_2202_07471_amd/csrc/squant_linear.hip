@@ -57,27 +57,33 @@ template <class A> int launch(void (*k)(A), int64_t gx, int gy, int threads, siz
   return hipGetLastError() == hipSuccess ? SQUANT_OK : SQUANT_ERR_DEVICE;
 }
 
-// Kernels that ask for more LDS than a workgroup gets by default say so, once for each device: the attribute
-// is the kernel's, not a call's.
-int launch_product(product_t k, const Split& p, hipStream_t st, const ProductArgs& a) {
-  if (p.lds > 64 * 1024 &&
-      hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.lds) != hipSuccess) {
+// Kernels that ask for more LDS than a workgroup gets by default say so: the attribute is the kernel's, not a call's.
+int launch_product(product_t k, const Split& p, size_t lds, hipStream_t st, const ProductArgs& a) {
+  if (lds > 64 * 1024 &&
+      hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
     (void)hipGetLastError();
     return SQUANT_ERR_DEVICE;
   }
-  return launch(k, p.workgroups, p.slices, p.threads, p.lds, st, a);
+  return launch(k, p.workgroups, p.slices, p.threads, lds, st, a);
 }
 
-product_t layer_kernel(int type, const squant_codes_t& w, const Split& p) {
-  const bool words = code_row(w) % 4 == 0 && !misaligned(w.codes, 4);
+int launch_layer(int type, const squant_codes_t& w, const Split& p, hipStream_t st, const ProductArgs& a) {
   const int format = (int)w.format;
-  if (p.few)
-    return type == SQUANT_W_F32   ? few_f32(format, p.row_frags, p.col_frags_each, words)
-           : type == SQUANT_W_F16 ? few_f16(format, p.row_frags, p.col_frags_each, words)
-                                  : few_bf16(format, p.row_frags, p.col_frags_each, words);
-  return type == SQUANT_W_F32   ? layer_f32(format, p.mt, words)
-         : type == SQUANT_W_F16 ? layer_f16(format, p.mt, words)
-                                : layer_bf16(format, p.mt, words);
+  if (p.few) {
+    const bool words = a.w_row % 4 == 0 && !misaligned(a.w, 4);
+    const product_t k = type == SQUANT_W_F32   ? few_f32(format, p.row_frags, p.col_frags_each, words)
+                        : type == SQUANT_W_F16 ? few_f16(format, p.row_frags, p.col_frags_each, words)
+                                               : few_bf16(format, p.row_frags, p.col_frags_each, words);
+    return launch_product(k, p, p.lds, st, a);
+  }
+  const product_t k = type == SQUANT_W_F32 ? layer_f32(format, p.mt) : type == SQUANT_W_F16 ? layer_f16(format, p.mt) : layer_bf16(format, p.mt);
+  return launch_product(k, p, product_lds(p.mt, planes_of(type), format), st, a);
+}
+
+int launch_gradient(int type, const squant_codes_t& w, const Split& p, hipStream_t st, const ProductArgs& a) {
+  const int format = (int)w.format, planes = planes_of(type);
+  const product_t k = planes == 2 ? gradient_2(format, p.mt) : gradient_1(format, p.mt);
+  return launch_product(k, p, product_lds(p.mt, planes, format), st, a);
 }
 
 float layer_unit(int type, int format) {
@@ -108,14 +114,35 @@ RowOperand lay_out_rows(Cutter& c, const void* x, int64_t ldx, int type, int64_t
   return RowOperand{out, planes * padded, padded, factor};
 }
 
-int copy_rows(const RowsArgs& r, int type, hipStream_t st) {
-  if (type == SQUANT_W_F32) return launch(split_rows_kernel(), r.rows, 1, kRowThreads, 0, st, r);
-  return launch(pad_rows_kernel(), (r.rows * (r.padded / 8) + kRowThreads - 1) / kRowThreads, 1, kRowThreads, 0, st, r);
+// The codes of a product: the caller's where the kernels can read them as they are, else a copy.
+struct CodeOperand {
+  const uint8_t* p;
+  int64_t row;
+};
+CodeOperand as_they_are(const squant_codes_t& w) { return CodeOperand{(const uint8_t*)w.codes, code_row(w)}; }
+
+// `whole`: rows of whole steps (a layer's product; a gradient reads across rows).
+CodeOperand lay_out_codes(Cutter& c, const squant_codes_t& w, bool whole, CodesArgs& k) {
+  const int64_t row = code_row(w);
+  if (!misaligned(w.codes, 16) && (whole ? w.cin % kBlock == 0 : row % 16 == 0)) return as_they_are(w);
+  const int64_t out_row = ((int64_t)w.cin + kBlock - 1) / kBlock * (w.format == SQUANT_OUT_INT8 ? kBlock : kBlock / 2);
+  k.codes = (const uint8_t*)w.codes; k.row = row; k.out = c.take<uint8_t>(w.cout * out_row); k.out_row = (int32_t)out_row;
+  k.chunks = w.cout * (out_row / 16);
+  return CodeOperand{k.out, out_row};
+}
+int64_t code_blocks(const CodesArgs& k) { return (k.chunks + kRowThreads - 1) / kRowThreads; }
+
+// Rows (`copy`) and codes that are laid out before a product, in one launch.
+int lay_out(RowsArgs& r, bool copy, int type, hipStream_t st) {
+  if (!copy && !r.w.chunks) return SQUANT_OK;
+  const bool split = copy && type == SQUANT_W_F32;
+  r.w.first_block = !copy ? 0 : split ? r.rows : (r.rows * (r.padded / 8) + kRowThreads - 1) / kRowThreads;
+  return launch(split ? split_rows_kernel() : pad_rows_kernel(), r.w.first_block + code_blocks(r.w), 1, kRowThreads, 0, st, r);
 }
 
-void set_product(ProductArgs& a, const RowOperand& x, const squant_codes_t& w, const Split& p) {
+void set_product(ProductArgs& a, const RowOperand& x, const CodeOperand& c, const squant_codes_t& w, const Split& p) {
   a.a = x.p; a.lda = x.ld; a.plane = x.plane;
-  a.w = (const uint8_t*)w.codes; a.w_row = code_row(w); a.w_rows = w.cout; a.w_cols = w.cin;
+  a.w = c.p; a.w_row = c.row; a.w_rows = w.cout; a.w_cols = w.cin;
   a.w_end = a.w + (int64_t)w.cout * a.w_row;
   a.blocks = p.blocks; a.slices = p.slices; a.tiles_m = p.tiles_m; a.tiles_n = p.tiles_n;
 }
@@ -130,22 +157,25 @@ int launch_join(bool grad, int type, const Split& p, const float4v* partial, con
 }
 
 // Workspaces.  Each is laid out by the function that also runs the call, so that the two agree.
-struct LinearSpace { RowOperand x; RowsArgs rows; bool copy; float4v* partial; Split p; };
+struct LinearSpace { RowOperand x; CodeOperand w; RowsArgs rows; bool copy; float4v* partial; Split p; };
 size_t lay_out_linear(void* ws, const void* x, int64_t ldx, int type, int64_t rows, const squant_codes_t& w, int keep, LinearSpace& s) {
   Cutter c{(char*)ws};
   s.rows = RowsArgs{};
   s.x = lay_out_rows(c, x, ldx, type, rows, w.cin, s.rows, s.copy);
   s.p = split_layer(rows, w.cout, w.cin, planes_of(type), keep != SQUANT_KEEP_NONE, true);
+  s.w = s.p.few ? as_they_are(w) : lay_out_codes(c, w, true, s.rows.w);
   s.partial = s.p.slices > 1 ? c.take<float4v>(s.p.partial_vectors()) : nullptr;
   return c.used;
 }
 
 int gradient_rows_per_group(int64_t rows) { return (int)std::min<int64_t>(kRowGroup, std::max<int64_t>(1, (rows + 1023) / 1024)); }
 
-struct BackwardSpace { _Float16* rows; float* factor; float* sums; int64_t partials; int64_t padded; float4v* partial; Split p; };
+struct BackwardSpace { CodeOperand w; CodesArgs codes; _Float16* rows; float* factor; float* sums; int64_t partials; int64_t padded; float4v* partial; Split p; };
 size_t lay_out_backward(void* ws, int type, int64_t rows, const squant_codes_t& w, BackwardSpace& s) {
   Cutter c{(char*)ws};
   const int planes = planes_of(type), group = gradient_rows_per_group(rows);
+  s.codes = CodesArgs{};
+  s.w = lay_out_codes(c, w, false, s.codes);
   s.padded = ((int64_t)w.cout + kBlock - 1) / kBlock * kBlock;
   s.rows = c.take<_Float16>(rows * planes * s.padded);
   s.factor = c.take<float>(rows);
@@ -156,7 +186,7 @@ size_t lay_out_backward(void* ws, int type, int64_t rows, const squant_codes_t& 
   return c.used;
 }
 
-struct LossSpace { RowOperand x; RowsArgs rows; bool copy; float2* stats; float* label_logit; Split p; };
+struct LossSpace { RowOperand x; CodeOperand w; RowsArgs rows; bool copy; float2* stats; float* label_logit; Split p; };
 size_t lay_out_loss(void* ws, const void* h, int64_t ldh, int type, int64_t rows, const squant_codes_t& w, LossSpace& s) {
   Cutter c{(char*)ws};
   s.rows = RowsArgs{};
@@ -164,17 +194,19 @@ size_t lay_out_loss(void* ws, const void* h, int64_t ldh, int type, int64_t rows
   s.stats = c.take<float2>(rows * (((int64_t)w.cout + kTile - 1) / kTile));
   s.label_logit = c.take<float>(rows);
   s.p = split_layer(rows, w.cout, w.cin, planes_of(type), true, false);
+  s.w = s.p.few ? as_they_are(w) : lay_out_codes(c, w, true, s.rows.w);
   return c.used;
 }
 
 struct LossBackwardSpace {
-  RowOperand x; RowsArgs rows; bool copy; float* unit; _Float16* prob; int64_t piece; int32_t pieces; float4v* partial; Split g;
+  RowOperand x; CodeOperand w; RowsArgs rows; bool copy; float* unit; _Float16* prob; int64_t piece; int32_t pieces; float4v* partial; Split g;
 };
 size_t lay_out_loss_backward(void* ws, const void* h, int64_t ldh, int type, int64_t rows, const squant_codes_t& w, LossBackwardSpace& s) {
   Cutter c{(char*)ws};
   const int planes = planes_of(type);
   s.rows = RowsArgs{};
   s.x = lay_out_rows(c, h, ldh, type, rows, w.cin, s.rows, s.copy);
+  s.w = lay_out_codes(c, w, true, s.rows.w);
   s.unit = c.take<float>(1);
   s.piece = vocabulary_piece(rows, w.cout, planes);
   s.pieces = (int32_t)((w.cout + s.piece - 1) / s.piece);
@@ -214,10 +246,9 @@ int squant_linear(const void* d_x, int64_t ldx, squant_wtype_t type, int64_t row
   const size_t need = lay_out_linear(d_workspace, d_x, ldx, (int)type, rows, w, (int)keep, s);
   if (int rc = check_workspace(d_workspace, workspace_bytes, need)) return rc;
   hipStream_t st = (hipStream_t)stream;
-  if (s.copy)
-    if (int rc = copy_rows(s.rows, (int)type, st)) return rc;
+  if (int rc = lay_out(s.rows, s.copy, (int)type, st)) return rc;
   ProductArgs a{};
-  set_product(a, s.x, w, s.p);
+  set_product(a, s.x, s.w, w, s.p);
   Finish& f = a.f;
   f.kind = kLinear; f.act = (int)act; f.keep = (int)keep; f.out_type = (int)type;
   f.unit = layer_unit((int)type, (int)w.format);
@@ -225,7 +256,7 @@ int squant_linear(const void* d_x, int64_t ldx, squant_wtype_t type, int64_t row
   f.bias = d_bias; f.residual = d_residual; f.ldr = ldr; f.out = d_y; f.ldo = ldy; f.kept = d_kept; f.kept_scales = d_kept_scales;
   const Finish done = f;
   if (s.p.slices > 1) { f.kind = kPartial; f.partial = s.partial; }
-  if (int rc = launch_product(layer_kernel((int)type, w, s.p), s.p, st, a)) return rc;
+  if (int rc = launch_layer((int)type, w, s.p, st, a)) return rc;
   return s.p.slices > 1 ? launch_join(false, (int)type, s.p, s.partial, done, st) : SQUANT_OK;
 }
 
@@ -266,21 +297,23 @@ int squant_linear_backward(const void* d_dy, int64_t lddy, squant_wtype_t type, 
   const int64_t groups = (rows + r.rows_per_group - 1) / r.rows_per_group, row_threads = (s.padded / 8 + kRowThreads - 1) / kRowThreads;
   // about 512 workgroups, each of which looks for its rows' largest elements anew
   const int shared = (int)std::max<int64_t>(1, std::min(row_threads, 512 / groups));
-  if (int rc = launch(gradient_rows_kernel((int)type), groups, shared, kRowThreads, 0, st, r)) return rc;
+  r.w = s.codes;
+  r.w.first_block = groups;
+  const int64_t code_groups = (code_blocks(r.w) + shared - 1) / shared;
+  if (int rc = launch(gradient_rows_kernel((int)type), groups + code_groups, shared, kRowThreads, 0, st, r)) return rc;
   if (d_dbias) {
     sums.partial = s.sums; sums.partials = s.partials;
     if (int rc = launch(column_sums_kernel(), sum_groups, 1, 1024, 0, st, sums)) return rc;
   }
   const int planes = planes_of((int)type);
   ProductArgs a{};
-  set_product(a, RowOperand{s.rows, planes * s.padded, s.padded, s.factor}, w, s.p);
+  set_product(a, RowOperand{s.rows, planes * s.padded, s.padded, s.factor}, s.w, w, s.p);
   Finish& f = a.f;
   f.kind = kGrad; f.out_type = (int)type; f.unit = kColumnUnitInverse; f.rows = rows; f.cols = w.cin; f.row_factor = s.factor;
   f.out = d_dx; f.ldo = lddx;
   const Finish done = f;
   if (s.p.slices > 1) { f.kind = kPartial; f.partial = s.partial; }
-  const product_t k = planes == 2 ? gradient_2((int)w.format, s.p.mt) : gradient_1((int)w.format, s.p.mt);
-  if (int rc = launch_product(k, s.p, st, a)) return rc;
+  if (int rc = launch_gradient((int)type, w, s.p, st, a)) return rc;
   return s.p.slices > 1 ? launch_join(true, (int)type, s.p, s.partial, done, st) : SQUANT_OK;
 }
 
@@ -305,15 +338,14 @@ int squant_cross_entropy(const void* d_h, int64_t ldh, squant_wtype_t type, int6
   const size_t need = lay_out_loss(d_workspace, d_h, ldh, (int)type, rows, w, s);
   if (int rc = check_workspace(d_workspace, workspace_bytes, need)) return rc;
   hipStream_t st = (hipStream_t)stream;
-  if (s.copy)
-    if (int rc = copy_rows(s.rows, (int)type, st)) return rc;
+  if (int rc = lay_out(s.rows, s.copy, (int)type, st)) return rc;
   ProductArgs a{};
-  set_product(a, s.x, w, s.p);
+  set_product(a, s.x, s.w, w, s.p);
   Finish& f = a.f;
   f.kind = kStats; f.out_type = (int)type; f.unit = layer_unit((int)type, (int)w.format);
   f.rows = rows; f.cols = w.cout; f.row_factor = s.x.factor; f.scales = w.scales;
   f.labels = d_labels; f.stats = s.stats; f.label_logit = s.label_logit;
-  if (int rc = launch_product(layer_kernel((int)type, w, s.p), s.p, st, a)) return rc;
+  if (int rc = launch_layer((int)type, w, s.p, st, a)) return rc;
   const LossArgs l{s.stats, (w.cout + kTile - 1) / kTile, s.label_logit, d_labels, ignore_index, w.cout, rows, d_loss, d_lse};
   return launch(loss_rows_kernel(), rows, 1, kRowThreads, 0, st, l);
 }
@@ -340,37 +372,34 @@ int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t t
   const size_t need = lay_out_loss_backward(d_workspace, d_h, ldh, (int)type, rows, w, s);
   if (int rc = check_workspace(d_workspace, workspace_bytes, need)) return rc;
   hipStream_t st = (hipStream_t)stream;
-  if (s.copy)
-    if (int rc = copy_rows(s.rows, (int)type, st)) return rc;
+  if (int rc = lay_out(s.rows, s.copy, (int)type, st)) return rc;
   hipLaunchKernelGGL(probability_unit_kernel(), dim3(1), dim3(1024), 0, st, w.scales, w.cout, s.unit);
   if (hipGetLastError() != hipSuccess) return SQUANT_ERR_DEVICE;
-  const int64_t w_row = code_row(w);
   for (int32_t i = 0; i < s.pieces; ++i) {
     const int32_t first = (int32_t)(i * s.piece);
     squant_codes_t piece = w;
-    piece.codes = (const uint8_t*)w.codes + first * w_row;
+    const CodeOperand codes{s.w.p + first * s.w.row, s.w.row};
     piece.cout = (int32_t)std::min<int64_t>(s.piece, w.cout - first);
     const Split p = split_layer(rows, piece.cout, w.cin, planes, true, false);
     ProductArgs a{};
-    set_product(a, s.x, piece, p);
+    set_product(a, s.x, codes, piece, p);
     Finish& f = a.f;
     f.kind = kProb; f.out_type = (int)type; f.unit = layer_unit((int)type, (int)w.format);
     f.rows = rows; f.cols = piece.cout; f.row_factor = s.x.factor; f.scales = w.scales + first;
     f.lse = d_lse; f.prob_unit = s.unit; f.prob = s.prob; f.ld_prob = planes * s.piece; f.prob_plane = s.piece;
-    if (int rc = launch_product(layer_kernel((int)type, piece, p), p, st, a)) return rc;
+    if (int rc = launch_layer((int)type, piece, p, st, a)) return rc;
     ProductArgs g{};
     Split split = s.g;
     split.blocks = (int32_t)((piece.cout + kBlock - 1) / kBlock);
-    set_product(g, RowOperand{s.prob, planes * s.piece, s.piece, nullptr}, piece, split);
+    set_product(g, RowOperand{s.prob, planes * s.piece, s.piece, nullptr}, codes, piece, split);
     g.accumulate = i > 0;  // what a long batch needs beside its rows does not grow with the vocabulary
     g.f.kind = kPartial; g.f.rows = rows; g.f.cols = w.cin; g.f.partial = s.partial;
-    const product_t k = planes == 2 ? gradient_2((int)w.format, s.g.mt) : gradient_1((int)w.format, s.g.mt);
-    if (int rc = launch_product(k, split, st, g)) return rc;
+    if (int rc = launch_gradient((int)type, piece, split, st, g)) return rc;
   }
   Finish f{};
   f.kind = kGradLoss; f.out_type = (int)type; f.unit = kColumnUnitInverse; f.rows = rows; f.cols = w.cin; f.scales = w.scales;
   f.out = d_dh; f.ldo = lddh; f.labels = d_labels; f.ignore = ignore_index; f.dloss = d_dloss; f.prob_unit = s.unit;
-  f.first_col = w.cout; f.codes = (const uint8_t*)w.codes; f.code_row = w_row; f.format = (int)w.format;
+  f.first_col = w.cout; f.codes = (const uint8_t*)w.codes; f.code_row = code_row(w); f.format = (int)w.format;
   return launch_join(true, (int)type, s.g, s.partial, f, st);
 }
 

@@ -1,14 +1,16 @@
 // The product of many rows with codes, for a layer (GRAD = false: the contraction runs along a code row) and
 // for its gradient (GRAD = true: across the code rows).
 //
-// A workgroup makes MT x 256 outputs with waves of (MT / 2) x 64 (64 x 64 where MT is 64: halves
-// of it that convert the same codes twice took 41 us where it takes 29, 1024 x 4096 x 2048).  The row operand goes to
-// the LDS without passing through registers, 64 contraction elements at a time in two buffers; rows of 128 bytes
-// with their 16-byte chunks exchanged by the row's low three bits, so that 8 lanes that read the same chunk of
-// 8 rows use all banks.  Codes go from memory to the registers of the waves that own their columns and are made
-// operands there: they are half or a quarter of the operand's bytes, each wave reads each of its codes once, and
-// no LDS traffic is spent on them.  Codes are the matrix instruction's first operand, rows its second, so that a
-// lane ends with 16 consecutive columns of one row.
+// A workgroup makes MT x 256 outputs with waves of (MT / 2) x 64 (64 x 64 where MT is 64: halves of it that convert
+// the same codes twice took 41 us where it takes 29, 1024 x 4096 x 2048).  Rows and codes go to the LDS without passing
+// through registers, 64 contraction elements at a time; the 16-byte chunks of what lies there in one row are exchanged so
+// that lanes that read at once use all banks.  Waves read the codes of their 64 columns and make them operands in
+// registers.  Codes that do not lie in whole steps at multiples of 16 bytes are laid out so before (lay_codes): read as
+// they were they cost twice the time (777 x 2049 x 2559 45 us, 777 x 2048 x 2560 23 us).  Codes are the matrix
+// instruction's first operand, rows its second, so that a lane ends with 16 consecutive columns of one row.
+//
+// Bound by the matrix units and the power they draw: a step of 64 of a 256 x 256 tile takes 1.66 us on all compute units,
+// 1.3 PFLOP/s, as a library product of the same size does over its whole time; the rest is a launch's start and end.
 #pragma once
 
 #include "squant_lin.h"
@@ -19,12 +21,29 @@ namespace lin {
 template <int MT> struct Shape {
   static constexpr int kWavesM = MT == 64 ? 1 : 2;
   static constexpr int kWaveRows = MT / kWavesM;
-  static constexpr int kWaves = kWavesM * (kWide / kTile);
-  static constexpr int kThreads = kWaves * kLanes;
+  // Groups of waves that take every other step of the contraction, each with row buffers of its own; their sums meet
+  // in the LDS at the end.  A tile of 64 rows has work for 4 waves, one a SIMD, that wait for each other's latencies.
+  static constexpr int kGroups = MT == 64 ? 2 : 1;
+  static constexpr int kWaves = kWavesM * (kWide / kTile);  // of a group
+  static constexpr int kThreads = kGroups * kWaves * kLanes;
   static constexpr int kFrags = kWaveRows / 16;
-  // Steps in flight or at work: a step of 256 rows takes longer than memory's latency, one of 64 rows a quarter.
-  static constexpr int kDepth = MT == 256 ? 2 : MT == 128 ? 3 : 4;
+  static constexpr int kOwn = kFrags / kGroups;  // fragments of rows that a wave finishes
 };
+
+constexpr int kLdsBytes = 160 * 1024;
+// LDS of one step: the rows' planes, then the codes.
+constexpr int step_codes(int format) { return format == SQUANT_OUT_INT4 ? kWide * kBlock / 2 : kWide * kBlock; }
+constexpr int step_bytes(int mt, int planes, int format) { return mt * kBlock * 2 * planes + step_codes(format); }
+constexpr int row_groups(int mt) { return mt == 64 ? Shape<64>::kGroups : 1; }
+// Steps in flight or at work: a step of 256 rows takes longer than memory's latency, one of 64 rows a quarter.
+constexpr int product_depth(int mt, int planes, int format) {
+  const int wanted = mt == 64 ? 4 : mt == 128 ? 3 : 2;
+  const int each = step_bytes(mt, planes, format) * row_groups(mt);
+  return wanted * each <= kLdsBytes ? wanted : kLdsBytes / each;
+}
+constexpr int product_lds(int mt, int planes, int format) {
+  return product_depth(mt, planes, format) * step_bytes(mt, planes, format) * row_groups(mt);
+}
 
 // 16 bytes a lane from memory to LDS bytes [lds, lds + 1024), in lane order.
 __device__ __forceinline__ void to_lds(const void* p, void* lds) {
@@ -32,20 +51,22 @@ __device__ __forceinline__ void to_lds(const void* p, void* lds) {
                                    (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
 }
 
-// The codes of one step, as loaded.
-template <int FMT, bool GRAD, bool WORDS> struct Raw;
-template <int FMT, bool WORDS> struct Raw<FMT, false, WORDS> { RowCodes<FMT, WORDS> v[4]; };
-template <int FMT, bool WORDS> struct Raw<FMT, true, WORDS> { typename Codes<FMT>::col4 v[16]; };
+// A wave's codes of one step: 16 of each of its lanes' 4 columns (layer), or 4 columns of 16 rows (gradient).
+template <int FMT, bool GRAD> struct Raw { typename Codes<FMT>::row16 v[4]; };
+template <int FMT> struct Raw<FMT, true> { typename Codes<FMT>::col4 v[16]; };
 
-// WORDS: code rows begin at whole 32-bit words (see RowCodes; a gradient takes them as they are).
-template <class F, int PL, int FMT, int MT, bool GRAD, bool WORDS>
+template <class F, int PL, int FMT, int MT, bool GRAD>
 __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a) {
   typedef Shape<MT> S;
+  constexpr bool kInt8 = FMT == SQUANT_OUT_INT8;
+  constexpr int D = product_depth(MT, PL, FMT);
   constexpr int kPlaneBytes = MT * kBlock * 2;
-  constexpr int kBufBytes = kPlaneBytes * PL;
+  constexpr int kBufBytes = step_bytes(MT, PL, FMT);
   extern __shared__ __align__(1024) unsigned char smem[];
   const int lane = threadIdx.x & (kLanes - 1);
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kLanes);  // known to be uniform
+  const int wave_of_all = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kLanes);  // known to be uniform
+  const int group = wave_of_all / S::kWaves, wave = wave_of_all % S::kWaves;
+  unsigned char* buffers = smem + group * (kBufBytes * D);
   const int wave_m = wave % S::kWavesM, wave_n = wave / S::kWavesM;
 
   // Each XCD takes a run of consecutive tiles; within it, bands of 8 tiles of rows run along the columns, so that
@@ -75,7 +96,7 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
     const int r = (wave * kLoads + i) * 8 + (lane >> 3);
-    src[i] = (uint32_t)min(r, last_row) * (uint32_t)(a.lda * 2) + (((lane & 7) ^ (r & 7)) << 4);
+    src[i] = (uint32_t)min(r, last_row) * (uint32_t)(a.lda * 2) + (((lane & 7) ^ ((r >> 1) & 7)) << 4);
   }
   auto load_rows = [&](int b, int buf) {
 #pragma unroll
@@ -83,70 +104,52 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
         to_lds(rows + (p * a.plane * 2 + (int64_t)b * (kBlock * 2)) + src[i],
-               smem + buf * kBufBytes + p * kPlaneBytes + (wave * kLoads + i) * 1024);
+               buffers + buf * kBufBytes + p * kPlaneBytes + (wave * kLoads + i) * 1024);
   };
 
-  // Codes.  For a layer each lane reads 16 codes of 4 rows; for a gradient 4 columns of 16 rows, lanes whose columns
-  // do not exist those of the row's last bytes.  `inside`: blocks that no read leaves the buffer for.
-  const int64_t w_bytes = (int64_t)a.w_rows * a.w_row;
-  uint32_t wsrc[GRAD ? 1 : 4];
-  const uint8_t* w_base = a.w;
-  int inside;
-  if constexpr (GRAD) {
-    constexpr int n = (int)sizeof(typename Codes<FMT>::col4);
-    // a row's last load may pass its end by less than n bytes
-    const bool even = a.w_row % n == 0;
-    const uint32_t at = (uint32_t)min(Codes<FMT>::offset(col0 + 4 * sub), a.w_row - (even ? n : 1));
-    wsrc[0] = (uint32_t)quad * 16 * (uint32_t)a.w_row + at;
-    inside = (int)max((w_bytes - (even ? 0 : n - 1)) / (kBlock * a.w_row), (int64_t)0);
-  } else {
-    w_base += (int64_t)min(col0, a.w_rows - 1) * a.w_row;
+  // Codes: 64 of each column in turn (layer), columns in the order in which a lane group reads them as operands, or 256
+  // columns of each row in turn (gradient).  A column or row past the end is the last one again: the columns are not
+  // stored, the rows' operands are zero.
+  constexpr int kCodeLoads = step_codes(FMT) / 1024 / S::kWaves;
+  constexpr int kCodeRow = (GRAD ? kWide : kBlock) / (kInt8 ? 1 : 2);  // bytes of a column or row of a step
+  const int32_t tile_col = tile_n * kWide;
+  const uint8_t* codes = a.w + (GRAD ? 0 : (int64_t)tile_col * a.w_row);
+  uint32_t csrc[kCodeLoads];
+  int crow[GRAD ? kCodeLoads : 1];
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-      wsrc[c] = (uint32_t)max(min(col0 + (sub >> 2) * 16 + c * 4 + (sub & 3), a.w_rows - 1) - min(col0, a.w_rows - 1), 0) *
-                (uint32_t)a.w_row + (uint32_t)Codes<FMT>::offset(quad * 16);
-    inside = a.w_cols / kBlock;
-    if constexpr (!WORDS) {
-      const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(w_base) & 3u);
-      w_base -= off;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) wsrc[c] += off;
+  for (int i = 0; i < kCodeLoads; ++i) {
+    const int place = ((wave * kCodeLoads + i) * 1024 + lane * 16) / kCodeRow, chunk = lane & (kCodeRow / 16 - 1);
+    if constexpr (GRAD) {
+      crow[i] = place;
+      const int32_t at = (int32_t)Codes<FMT>::offset(tile_col) + (chunk ^ (place >> 4) * (kCodeRow / 64)) * 16;
+      csrc[i] = (uint32_t)min(at, (int32_t)a.w_row - 16);
+    } else {
+      const int sub16 = place & 15;
+      const int32_t col = (place >> 6) * 64 + (sub16 >> 2) * 16 + ((place >> 4) & 3) * 4 + (sub16 & 3);
+      csrc[i] = (uint32_t)min(col, a.w_rows - 1 - tile_col) * (uint32_t)a.w_row + (uint32_t)(chunk ^ (sub16 >> (kInt8 ? 2 : 3))) * 16;
     }
   }
-  uint32_t shift[4] = {0, 0, 0, 0};
-  if constexpr (!GRAD && !WORDS) {
+  auto load_codes = [&](int b, int buf) {
+    const uint8_t* p = codes + (GRAD ? (int64_t)b * kBlock * a.w_row : Codes<FMT>::offset((int64_t)b * kBlock));
+    const int last_code_row = a.w_rows - 1 - b * kBlock;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) shift[c] = wsrc[c] & 3u;
-  }
-  auto load_codes = [&](int b, Raw<FMT, GRAD, WORDS>& o) {
-    if constexpr (GRAD) {
-      const uint8_t* p = w_base + (int64_t)b * kBlock * a.w_row;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o.v[i] = load_any<typename Codes<FMT>::col4>(p + i * a.w_row + wsrc[0]);
-    } else {
-      const uint8_t* p = w_base + Codes<FMT>::offset((int64_t)b * kBlock);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) o.v[c].load(p + (wsrc[c] - shift[c]));
+    for (int i = 0; i < kCodeLoads; ++i) {
+      uint32_t at = csrc[i];
+      if constexpr (GRAD) at += (uint32_t)min(crow[i], last_code_row) * (uint32_t)a.w_row;
+      to_lds(p + at, buffers + buf * kBufBytes + PL * kPlaneBytes + (wave * kCodeLoads + i) * 1024);
     }
   };
-  // the same at the buffer's end
-  auto load_last_codes = [&](int b, Raw<FMT, GRAD, WORDS>& o) {
-    constexpr int n = GRAD ? 16 : 4;
-    const uint8_t* at[n];
-#pragma unroll
-    for (int i = 0; i < n; ++i)
-      at[i] = GRAD ? w_base + ((int64_t)b * kBlock + i) * a.w_row + wsrc[0]
-                   : w_base + Codes<FMT>::offset((int64_t)b * kBlock) + wsrc[GRAD ? 0 : i];
+  auto read_codes = [&](int buf, Raw<FMT, GRAD>& o) {
+    const unsigned char* p = buffers + buf * kBufBytes + PL * kPlaneBytes;
     if constexpr (GRAD) {
-      load_before(o.v, at, a.w_end, w_bytes);
-    } else {
-      typename Codes<FMT>::row16 v[4];
-      load_before(v, at, a.w_end, w_bytes);
+      typedef typename Codes<FMT>::col4 col4;
+      p += quad * 16 * kCodeRow + ((wave_n ^ quad) * 16 + sub) * (int)sizeof(col4);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        o.v[c].set(v[c]);
-        shift[c] = 0;  // nothing is read as whole words after this
-      }
+      for (int i = 0; i < 16; ++i) o.v[i] = *(const col4*)(p + i * kCodeRow);
+    } else {
+      p += (wave_n * 64 + sub) * kCodeRow + (kInt8 ? (quad ^ (sub >> 2)) * 16 : ((quad >> 1) ^ (sub >> 3)) * 16 + (quad & 1) * 8);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o.v[c] = *(const typename Codes<FMT>::row16*)(p + c * 16 * kCodeRow);
     }
   };
 
@@ -156,33 +159,35 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
 #pragma unroll
     for (int c = 0; c < 4; ++c) acc[m][c] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
 
-  auto operand = [&](const Raw<FMT, GRAD, WORDS>& r, int h, int c) {
+  auto operand = [&](const Raw<FMT, GRAD>& r, int h, int c) {
     if constexpr (GRAD) return convert_columns<FMT>(r.v + 8 * h, c);
-    else return convert<F, FMT>(r.v[c].aligned(h, shift[c]), h);
+    else return convert<F, FMT>(r.v[c], h);
   };
   auto row_frag = [&](int buf, int p, int h, int m) {
-    return *(const typename F::frag*)(smem + buf * kBufBytes + p * kPlaneBytes + m * 2048 + wave_m * S::kWaveRows * 128 +
-                                      sub * 128 + (((quad * 2 + h) ^ (sub & 7)) << 4));
+    return *(const typename F::frag*)(buffers + buf * kBufBytes + p * kPlaneBytes + m * 2048 + wave_m * S::kWaveRows * 128 +
+                                      sub * 128 + (((quad * 2 + h) ^ (sub >> 1)) << 4));
   };
   // A half step is 16 fragments of products a fragment of rows; the next fragment of rows is read, and the next
   // half's codes are converted, between them.
-  auto multiply = [&](int buf, const Raw<FMT, GRAD, WORDS>& r) {
-    constexpr int kSteps = 2 * PL * S::kFrags;
+  auto multiply = [&](int buf) {
+    constexpr int kHalf = PL * S::kFrags, kSteps = 2 * kHalf;
+    Raw<FMT, GRAD> r;
+    read_codes(buf, r);
     typename F::frag w[2][4], x[2];
 #pragma unroll
     for (int c = 0; c < 4; ++c) w[0][c] = operand(r, 0, c);
     x[0] = row_frag(buf, 0, 0, 0);
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
-      const int h = s / (PL * S::kFrags), in = s % (PL * S::kFrags), m = in % S::kFrags;
+      const int h = s / kHalf, in = s % kHalf, m = in % S::kFrags;
       if (s + 1 < kSteps) {
-        const int n = s + 1, nin = n % (PL * S::kFrags);
-        x[n & 1] = row_frag(buf, nin / S::kFrags, n / (PL * S::kFrags), nin % S::kFrags);
+        const int n = s + 1, nin = n % kHalf;
+        x[n & 1] = row_frag(buf, nin / S::kFrags, n / kHalf, nin % S::kFrags);
       }
       if (h == 0) {
         // the next half's operands, dealt to this half's fragments of rows
 #pragma unroll
-        for (int c = in * 4 / (PL * S::kFrags); c < (in + 1) * 4 / (PL * S::kFrags); ++c) w[1][c] = operand(r, 1, c);
+        for (int c = in * 4 / kHalf; c < (in + 1) * 4 / kHalf; ++c) w[1][c] = operand(r, 1, c);
       }
       __builtin_amdgcn_sched_barrier(0x6);  // what is not arithmetic stays in its fragment
 #pragma unroll
@@ -190,30 +195,26 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
       __builtin_amdgcn_sched_barrier(0x6);
     }
   };
-  // A step's loads are issued kDepth - 1 steps before it, without branches around them, so that what is on its way
-  // can be counted: past the last step the last block is loaded again, and not multiplied.  (With a branch around
-  // them the compiler waits for everything before it touches a step's codes.)  The barrier also says that the buffer
-  // to be loaded next is read out.
-  constexpr int D = S::kDepth;
-  constexpr int kIssued = kLoads * PL + (GRAD ? 16 : WORDS ? 4 : 8);
-  constexpr int kOthers = kIssued * (D - 2);  // may be on their way when a step begins
-  static_assert(kOthers < 64, "the wait counter has six bits");
-  const int steady = min(last, inside);
+  // A step's loads are issued D - 1 steps before it, without branches around them, so that what is on its way can be
+  // counted: past the last step the last block is loaded again, and not multiplied.  The barrier also says that the
+  // buffer to be loaded next is read out.
+  constexpr int kOthers = (kLoads * PL + kCodeLoads) * (D - 2);  // may be on their way when a step begins
+  static_assert(D >= 2 && kOthers < 64, "the wait counter has six bits");
   // No load moves over this: the count of one step's is told from the next one's.
   auto in_order = []() {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   };
-  if (first < steady) {
-    Raw<FMT, GRAD, WORDS> raw[D];
+  if (first < last) {  // a short last piece of the vocabulary may leave a slice without a step
 #pragma unroll
     for (int i = 0; i < D - 1; ++i) {
-      load_rows(min(first + i, steady - 1), i);
-      load_codes(min(first + i, steady - 1), raw[i]);
+      const int b = min(first + i * S::kGroups + group, last - 1);
+      load_rows(b, i);
+      load_codes(b, i);
       in_order();
     }
 #pragma unroll 1
-    for (int b0 = first; b0 < steady; b0 += D) {
+    for (int b0 = first; b0 < last; b0 += D * S::kGroups) {
 #pragma unroll
       for (int i = 0; i < D; ++i) {
         // not __syncthreads(), which would wait for every load
@@ -221,30 +222,36 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
         __builtin_amdgcn_s_waitcnt((kOthers & 15) | (kOthers >> 4) << 14 | 0x070);
         __builtin_amdgcn_s_barrier();
         in_order();
-        const int ahead = min(b0 + i + D - 1, steady - 1);
+        const int b = b0 + i * S::kGroups + group, ahead = min(b + (D - 1) * S::kGroups, last - 1);
         load_rows(ahead, (i + D - 1) % D);
-        load_codes(ahead, raw[(i + D - 1) % D]);
-        if (b0 + i < steady) multiply(i, raw[i]);
+        load_codes(ahead, (i + D - 1) % D);
+        if (b < last) multiply(i);
       }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   }
-  for (int b = max(first, steady); b < last; ++b) {  // what ends within a block
-    Raw<FMT, GRAD, WORDS> raw;
-    load_rows(b, 0);
-    load_last_codes(b, raw);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  if constexpr (S::kGroups == 2) {
+    // each group hands half of its fragments to the other and keeps the sums of the other half
+    float4v* given = reinterpret_cast<float4v*>(smem) + wave * (S::kOwn * 4 * kLanes) + lane;
+    constexpr int kGiven = S::kWaves * S::kOwn * 4 * kLanes;  // of a group
+#pragma unroll
+    for (int m = 0; m < S::kOwn; ++m)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) given[group * kGiven + (m * 4 + c) * kLanes] = acc[group == 0 ? m + S::kOwn : m][c];
     __syncthreads();
-    multiply(0, raw);
-    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < S::kOwn; ++m)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[m][c] = acc[group == 0 ? m : m + S::kOwn][c] + given[(1 - group) * kGiven + (m * 4 + c) * kLanes];
   }
+  const int first_frag = wave_m * S::kFrags + group * S::kOwn;  // of those that this wave finishes, in the tile
 
   if (a.f.kind == kPartial) {
     const int64_t frags_n = (int64_t)a.tiles_n * (kWide / 16);
 #pragma unroll
-    for (int m = 0; m < S::kFrags; ++m) {
-      const int64_t row_frag = (int64_t)slice * a.tiles_m * (MT / 16) + tile_m * (MT / 16) + wave_m * S::kFrags + m;
+    for (int m = 0; m < S::kOwn; ++m) {
+      const int64_t row_frag = (int64_t)slice * a.tiles_m * (MT / 16) + tile_m * (MT / 16) + first_frag + m;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         float4v* p = a.f.partial + (row_frag * frags_n + (col0 / 16 + c)) * kLanes + lane;
@@ -270,10 +277,10 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
     __syncthreads();
   }
 #pragma unroll 1
-  for (int m = 0; m < S::kFrags; ++m) {
+  for (int m = 0; m < S::kOwn; ++m) {
     float4v t[4];
 #pragma unroll
-    for (int j = 0; j < S::kFrags; ++j)
+    for (int j = 0; j < S::kOwn; ++j)
       if (m == j) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) t[c] = acc[j][c];
@@ -283,7 +290,7 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
     for (int c = 0; c < 4; ++c)
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[column_of<GRAD>(c, i)] = t[c][i];
-    const int64_t row = row0 + wave_m * S::kWaveRows + m * 16 + sub;
+    const int64_t row = row0 + (first_frag + m) * 16 + sub;
     if constexpr (GRAD) {
       finish_grad(a.f, row, col0 + quad * 16, v);
     } else {
@@ -298,15 +305,11 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
   }
 }
 
-template <class F, int PL, int FMT, bool GRAD, bool WORDS>
+template <class F, int PL, int FMT, bool GRAD>
 product_t product_of(int mt) {
-  if (mt == 256) return product<F, PL, FMT, 256, GRAD, WORDS>;
-  if (mt == 128) return product<F, PL, FMT, 128, GRAD, WORDS>;
-  return product<F, PL, FMT, 64, GRAD, WORDS>;
-}
-template <class F, int PL, int FMT>
-product_t layer_of(int mt, bool words) {
-  return words ? product_of<F, PL, FMT, false, true>(mt) : product_of<F, PL, FMT, false, false>(mt);
+  if (mt == 256) return product<F, PL, FMT, 256, GRAD>;
+  if (mt == 128) return product<F, PL, FMT, 128, GRAD>;
+  return product<F, PL, FMT, 64, GRAD>;
 }
 
 }  // namespace lin

@@ -53,9 +53,10 @@ def _lib():
 
 
 @lru_cache(maxsize=4096)
-def _workspace_bytes(call: str, aligned, type_: int, rows: int, cout: int, cin: int, fmt: int, *rest: int) -> int:
-    # the size depends on the shapes and on whether the rows are aligned to 16 bytes: addresses that stand for both
-    w = squant_codes_t(256, 256, cout, cin, fmt)
+def _workspace_bytes(call: str, aligned, codes_aligned, type_: int, rows: int, cout: int, cin: int, fmt: int,
+                     *rest: int) -> int:
+    # the size depends on the shapes and on whether rows and codes are aligned to 16 bytes: addresses that stand for both
+    w = squant_codes_t(256 if codes_aligned else 257, 256, cout, cin, fmt)
     x = () if aligned is None else (256, -(-cin // 8) * 8) if aligned else (256, cin | 1)
     return int(getattr(_lib(), f"squant_{call}_workspace_bytes")(*x, type_, rows, ctypes.byref(w), *rest))
 
@@ -163,7 +164,7 @@ def squant_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bi
     elif how == KEEP_FULL:
         kept = torch.empty(shape, dtype=x.dtype, device=x.device)
     type_ = _WTYPES[x.dtype]
-    nbytes = _workspace_bytes("linear", _aligned(x, ldx), type_, rows, cout, cin, w.format, how)
+    nbytes = _workspace_bytes("linear", _aligned(x, ldx), w.codes & 15 == 0, type_, rows, cout, cin, w.format, how)
     ws = _workspace(x, nbytes)
     _check(_lib().squant_linear(x.data_ptr(), ldx, type_, rows, ctypes.byref(w), _ptr(bias), act, _ptr(residual), ldr,
                                 out.data_ptr(), ldy, how, _ptr(kept), _ptr(kept_scales), _ptr(ws), nbytes,
@@ -205,7 +206,7 @@ def squant_linear_backward(dy: torch.Tensor, codes: torch.Tensor, scales: torch.
         lddx = _like(dx, cin, "dx", dy, device)
     dbias = dy.new_empty(cout) if bias else None
     type_ = _WTYPES[dy.dtype]
-    nbytes = _workspace_bytes("linear_backward", None, type_, rows, cout, cin, w.format)
+    nbytes = _workspace_bytes("linear_backward", None, w.codes & 15 == 0, type_, rows, cout, cin, w.format)
     ws = _workspace(dy, nbytes)
     _check(_lib().squant_linear_backward(dy.data_ptr(), lddy, type_, rows, ctypes.byref(w), act, how, _ptr(z),
                                          _ptr(z_scales), dx.data_ptr(), lddx, _ptr(dbias), _ptr(ws), nbytes,
@@ -235,7 +236,7 @@ def squant_cross_entropy(h: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
     loss = torch.empty(h.shape[:-1], dtype=torch.float32, device=h.device)
     lse = torch.empty_like(loss)
     type_ = _WTYPES[h.dtype]
-    nbytes = _workspace_bytes("cross_entropy", _aligned(h, ldh), type_, rows, w.cout, cin, w.format)
+    nbytes = _workspace_bytes("cross_entropy", _aligned(h, ldh), w.codes & 15 == 0, type_, rows, w.cout, cin, w.format)
     ws = _workspace(h, nbytes)
     _check(_lib().squant_cross_entropy(h.data_ptr(), ldh, type_, rows, ctypes.byref(w), labels.data_ptr(),
                                        ignore_index, loss.data_ptr(), lse.data_ptr(), _ptr(ws), nbytes,
@@ -263,7 +264,7 @@ def squant_cross_entropy_backward(h: torch.Tensor, codes: torch.Tensor, scales: 
     else:
         lddh = _like(dh, cin, "dh", h, device)
     type_ = _WTYPES[h.dtype]
-    nbytes = _workspace_bytes("cross_entropy_backward", _aligned(h, ldh), type_, rows, w.cout, cin, w.format)
+    nbytes = _workspace_bytes("cross_entropy_backward", _aligned(h, ldh), w.codes & 15 == 0, type_, rows, w.cout, cin, w.format)
     ws = _workspace(h, nbytes)
     _check(_lib().squant_cross_entropy_backward(h.data_ptr(), ldh, type_, rows, ctypes.byref(w), labels.data_ptr(),
                                                 ignore_index, lse.data_ptr(), dloss.data_ptr(), dh.data_ptr(), lddh,

@@ -368,3 +368,29 @@ def test_codes_changed_before_the_backward_pass_are_noticed(sq):
     scales.mul_(2)
     with pytest.raises(RuntimeError):
         loss.sum().backward()
+
+
+@pytest.mark.parametrize("fmt", ["int8", "int4"])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("k", [512, 516, 545, 2048 + 64, 32, 128])
+@pytest.mark.parametrize("m,n", [(4100, 4128), (1030, 4352), (520, 1008)])
+def test_exact_products_of_every_tile(sq, m, n, k, dtype, fmt):
+    """Long and short contractions, code rows that begin at multiples of 16 bytes, of 4, and anywhere, and codes of which
+    the first begins off them; the layer and its gradient."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(m + k)
+    x = torch.randint(-4, 5, (m, k), device="cuda", generator=gen).float()
+    dy = torch.randint(-4, 5, (m, n), device="cuda", generator=gen).float()
+    c = codes_of(np.random.default_rng([m, k, n]), n, k, fmt)
+    packed = (pack(c) if fmt == "int4" else c).cuda()
+    scales = 2.0 ** torch.randint(-9, -5, (n,), device="cuda", generator=gen).float()
+    c64 = c.double().cuda()
+    want = (x.double() @ c64.t()) * scales.double()
+    want_dx = (dy.double() * scales.double()) @ c64
+    x, dy = x.to(dtype), dy.to(dtype)
+    for off in (0, 4, 1):
+        buf = torch.zeros(packed.numel() + 16, dtype=packed.dtype, device="cuda")
+        w = buf[off:off + packed.numel()].view(packed.shape)
+        w.copy_(packed)
+        assert_rounded(sq.squant_linear(x, w, scales), want.cpu(), dtype, f"codes {off} bytes on")
+        assert_rounded(sq.squant_linear_backward(dy, w, scales, k, bias=False)[0], want_dx.cpu(), dtype, f"dx, codes {off} bytes on")
