@@ -42,9 +42,13 @@ __device__ __forceinline__ Planes split8(const uint4v (&x)[2], float up) {
 __device__ __forceinline__ uint4v load_row8(const char* row, int64_t k, int64_t cols) {
   if (k + 8 <= cols) return load_any<uint4v>(row + 2 * k);
   uint4v o = {0, 0, 0, 0};
+  if (k >= cols) return o;
+  uint32_t v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = load_any<uint16_t>(row + 2 * (k + i < cols ? k + i : k));
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    if (k + i < cols) o[i >> 1] |= (uint32_t)load_any<uint16_t>(row + 2 * (k + i)) << (16 * (i & 1));
+    if (k + i < cols) o[i >> 1] |= v[i] << (16 * (i & 1));
   return o;
 }
 
@@ -99,9 +103,11 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductAr
       const float* f = (const float*)x[m] + k + 4 * p;
       if (!ends) return load_any<uint4v>(f);
       uint4v o = {0, 0, 0, 0};
+      if (k + 4 * p >= a.w_cols) return o;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (k + 4 * p + i < a.w_cols) o[i] = load_any<uint32_t>(f + i);
+      for (int i = 0; i < 4; ++i) o[i] = load_any<uint32_t>(f + (k + 4 * p + i < a.w_cols ? i : 0));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = k + 4 * p + i < a.w_cols ? o[i] : 0;
       return o;
     } else {
       if (ends) return load_row8(x[m], k, a.w_cols);

@@ -15,10 +15,13 @@ __global__ void __launch_bounds__(kRowThreads) pad_rows(RowsArgs a) {
   uint4v o = {0, 0, 0, 0};
   if (c + 8 <= a.cols) {
     o = load_any<uint4v>(x);
-  } else {
+  } else if (c < a.cols) {
+    uint32_t v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = x[c + i < a.cols ? i : 0];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (c + i < a.cols) o[i >> 1] |= (uint32_t)x[i] << (16 * (i & 1));
+      if (c + i < a.cols) o[i >> 1] |= v[i] << (16 * (i & 1));
   }
   *(uint4v*)((uint16_t*)a.out + row * a.padded + c) = o;
 }

@@ -388,27 +388,80 @@ __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((u
 // finished pieces
 // ---------------------------------------------------------------------------
 
+// NC elements in whole.  16-bit ones of rows of odd lengths begin between 32-bit words, where a wide access costs
+// several times an aligned one: they go as the words that hold them, shifted by an element, and by themselves at the
+// ends (777 x 2559 outputs with residual and kept pre-activation 36.4 us, now 32.7 us).
+template <class T, int NC> struct Pack { T v[NC]; };
+template <class T> __device__ __forceinline__ bool between_words(const T* p) {
+  return sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(p) & 2u) != 0;
+}
+template <int NC, class T>
+__device__ __forceinline__ Pack<T, NC> load_pack(const T* p) {
+  if constexpr (sizeof(T) == 2 && NC >= 4) {
+    const bool between = between_words(p);
+    if (__any(between)) {
+      struct Words { uint32_t w[NC / 2]; };
+      const char* from = (const char*)p - (between ? 2 : 0);
+      Words a;
+      __builtin_memcpy(&a, __builtin_assume_aligned(from, 4), sizeof(a));
+      const uint32_t after = between ? *(const uint32_t*)(from + 2 * NC) : 0;
+#pragma unroll
+      for (int i = 0; i < NC / 2; ++i) a.w[i] = __builtin_amdgcn_alignbyte(i + 1 < NC / 2 ? a.w[i + 1 < NC / 2 ? i + 1 : 0] : after, a.w[i], between ? 2 : 0);
+      return __builtin_bit_cast(Pack<T, NC>, a);
+    }
+  }
+  return load_any<Pack<T, NC>>(p);
+}
+template <int NC, class T>
+__device__ __forceinline__ void store_pack(T* p, const Pack<T, NC>& k) {
+  if constexpr (sizeof(T) == 2 && NC >= 4) {
+    const bool between = between_words(p);
+    if (__any(between)) {
+      struct Words { uint32_t w[NC / 2]; };
+      struct Inner { uint32_t w[NC / 2 - 1]; };
+      const Words a = __builtin_bit_cast(Words, k);
+      Inner o;
+#pragma unroll
+      for (int i = 0; i + 1 < NC / 2; ++i) o.w[i] = __builtin_amdgcn_alignbyte(a.w[i + 1], a.w[i], between ? 2 : 0);
+      __builtin_memcpy(__builtin_assume_aligned((char*)p + (between ? 2 : 0), 4), &o, sizeof(o));
+      if (between) {
+        p[0] = k.v[0];
+        p[NC - 1] = k.v[NC - 1];
+      } else {
+        *(uint32_t*)(p + NC - 2) = a.w[NC / 2 - 1];
+      }
+      return;
+    }
+  }
+  store_any(p, k);
+}
+
 template <int NC, class T>
 __device__ __forceinline__ void load_cols(float (&o)[NC], const T* p, int valid) {
   if (valid >= NC) {
-    struct Pack { T v[NC]; };
-    const Pack k = load_any<Pack>(p);
+    const Pack<T, NC> k = load_pack<NC, T>(p);
 #pragma unroll
     for (int i = 0; i < NC; ++i) o[i] = widen(k.v[i]);
   } else {
 #pragma unroll
-    for (int i = 0; i < NC; ++i) o[i] = i < valid ? widen(p[i]) : 0.0f;
+    for (int i = 0; i < NC; ++i) o[i] = 0.0f;
+    if (valid > 0) {
+      T v[NC];  // every load on its way before the first is waited for
+#pragma unroll
+      for (int i = 0; i < NC; ++i) v[i] = p[i < valid ? i : 0];
+#pragma unroll
+      for (int i = 0; i < NC; ++i) o[i] = i < valid ? widen(v[i]) : 0.0f;
+    }
   }
 }
 
 template <int NC, class T>
 __device__ __forceinline__ void store_cols(T* p, const float (&o)[NC], int valid) {
   if (valid >= NC) {
-    struct Pack { T v[NC]; };
-    Pack k;
+    Pack<T, NC> k;
 #pragma unroll
     for (int i = 0; i < NC; ++i) k.v[i] = narrow<T>(o[i]);
-    store_any(p, k);
+    store_pack<NC, T>(p, k);
   } else {
 #pragma unroll
     for (int i = 0; i < NC; ++i)

@@ -85,9 +85,14 @@ __device__ __forceinline__ void lay_codes(const CodesArgs& w, int64_t block) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_alignbyte(v[i + 1], v[i], off);
   } else {
+    if (c < w.row) {
+      uint32_t v[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (c + i < w.row) o[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+      for (int i = 0; i < 16; ++i) v[i] = p[c + i < w.row ? i : 0];
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (c + i < w.row) o[i >> 2] |= v[i] << (8 * (i & 3));
+    }
   }
   *(uint4v*)(w.out + at * 16) = o;
 }
