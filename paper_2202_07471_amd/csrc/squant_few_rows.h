@@ -54,7 +54,7 @@ __device__ __forceinline__ uint4v load_row8(const char* row, int64_t k, int64_t 
 
 // T: the type of the rows and of the output; binary32 with F = Half.
 template <class F, class T, int FMT, int MF, int NF, bool WORDS>
-__global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductArgs a) {
+__global__ void __launch_bounds__(few_waves(MF, NF) * kLanes, sizeof(T) == 2 && MF * NF <= 8 ? 4 : 2) few_rows(ProductArgs a) {
   constexpr int kWaves = few_waves(MF, NF);
   constexpr int kHalves = FMT == SQUANT_OUT_INT4 ? 4 : 2;  // groups of 8 codes in 16 bytes
   constexpr int kUnit = 32 * kHalves;                      // contraction elements of a unit
@@ -70,6 +70,7 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductAr
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kLanes);  // known to be uniform
   const int sub = lane & 15, quad = lane >> 4;
   const int32_t col0 = (int32_t)blockIdx.x * (16 * NF);
+  const int32_t row0 = (int32_t)blockIdx.y * (16 * MF);
 
   const int64_t w_bytes = (int64_t)a.w_rows * a.w_row;
   const uint8_t* w[NF];
@@ -82,7 +83,7 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductAr
   }
   const char* x[MF];
 #pragma unroll
-  for (int m = 0; m < MF; ++m) x[m] = (const char*)a.a + min((int64_t)(m * 16 + sub), a.f.rows - 1) * a.lda * (int)sizeof(T);
+  for (int m = 0; m < MF; ++m) x[m] = (const char*)a.a + min((int64_t)(row0 + m * 16 + sub), a.f.rows - 1) * a.lda * (int)sizeof(T);
 
   float4v acc[MF][NF];
 #pragma unroll
@@ -257,7 +258,7 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductAr
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[4 * c + i] = t[i];
     }
-    finish_layer<16, T>(a.f, columns, wave * 16 + sub, col0 + quad * 16, v, power_of_two(-e), kSplit ? 2 : 1);
+    finish_layer<16, T>(a.f, columns, row0 + wave * 16 + sub, col0 + quad * 16, v, power_of_two(-e), kSplit ? 2 : 1);
   } else {
     if (wave >= MF * NF) return;
     const int m = wave / NF, c = wave % NF;
@@ -267,7 +268,7 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes) few_rows(ProductAr
     const int e = kSplit ? least(m) : 0;
     const float4v t = total(m, c, e);
     float v[4] = {t[0], t[1], t[2], t[3]};
-    finish_layer<4, T>(a.f, columns, m * 16 + sub, col, v, power_of_two(-e), 1);
+    finish_layer<4, T>(a.f, columns, row0 + m * 16 + sub, col, v, power_of_two(-e), 1);
   }
 }
 

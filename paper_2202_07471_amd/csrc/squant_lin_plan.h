@@ -70,18 +70,18 @@ inline Split split_layer(int64_t rows, int64_t cols, int64_t depth, int planes, 
   if (rows > few_rows_limit(planes)) return split_product(rows, cols, depth, planes, may_split);
   Split p{};
   p.few = true;
-  p.row_frags = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  const int frags = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   // wide workgroups read their rows fewer times, narrow ones fill the chip
   p.col_frags_each = tiled || cols >= 32 * 1024 ? 4 : cols >= 8 * 1024 ? 2 : 1;
   p.blocks = (int)((depth + kBlock - 1) / kBlock);
   p.slices = 1;
-  p.tiles_m = p.row_frags;
   p.tiles_n = (int)((cols + 16 * p.col_frags_each - 1) / (16 * p.col_frags_each));
+  // where the columns leave half of the chip without work, rows go to workgroups of their own
+  p.row_frags = p.tiles_n * 2 <= kCus ? 1 : frags;
+  p.tiles_m = (int)((rows + 16 * p.row_frags - 1) / (16 * p.row_frags));
   p.workgroups = p.tiles_n;
   p.threads = few_waves(p.row_frags, p.col_frags_each) * kLanes;
   p.lds = few_lds(p.row_frags, p.col_frags_each);
-  p.row_frags_all = p.row_frags;
-  p.col_frags_all = (int64_t)p.tiles_n * p.col_frags_each;
   return p;
 }
 

@@ -64,7 +64,7 @@ int launch_product(product_t k, const Split& p, size_t lds, hipStream_t st, cons
     (void)hipGetLastError();
     return SQUANT_ERR_DEVICE;
   }
-  return launch(k, p.workgroups, p.slices, p.threads, lds, st, a);
+  return launch(k, p.workgroups, p.few ? p.tiles_m : p.slices, p.threads, lds, st, a);
 }
 
 int launch_layer(int type, const squant_codes_t& w, const Split& p, hipStream_t st, const ProductArgs& a) {

@@ -12,7 +12,7 @@ from typing import Optional
 
 import torch
 
-from .binding import OUT_INT4, OUT_INT8, SQuantError, _check, _stream_ptr, _WTYPES, lib  # noqa: F401
+from .binding import OUT_INT4, OUT_INT8, SQuantError, _check, _raw_stream, _stream_ptr, _WTYPES, lib  # noqa: F401
 
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "silu": ACT_SILU}
@@ -70,12 +70,19 @@ def _aligned(t: torch.Tensor, ld: int) -> bool:
     return (ld | t.data_ptr() >> 1) & 7 == 0 and ld <= _MAX_STRIDE
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _current_stream(device: int) -> int:
+    return int(_raw_stream(device)) if _raw_stream is not None else _stream_ptr(None)
+
+
 def _device(t: torch.Tensor, what: str) -> int:
     """The index of t's device, which has to be the current one."""
     device = t.get_device()  # -1 on the host
     if device < 0 or t.dtype not in _WTYPES:
         raise ValueError(f"{what} must be a float32, float16 or bfloat16 tensor in device memory")
-    if device != torch.cuda.current_device():
+    if device != _current_device():
         raise ValueError(f"{what} is not on the current device")
     return device
 
@@ -103,8 +110,11 @@ def _rows(t: torch.Tensor, cols: int, what: str):
 
 def _like(t: torch.Tensor, cols: int, what: str, like: torch.Tensor, device: int) -> int:
     """Elements between the rows of an activation tensor that goes with `like`."""
-    if t.dtype != like.dtype or t.get_device() != device or t.shape[:-1] != like.shape[:-1]:
+    shape, other = t.shape, like.shape
+    if t.dtype is not like.dtype or t.get_device() != device or shape[:-1] != other[:-1]:
         raise ValueError(f"{what} must have the type, the device and the leading dimensions of the other activations")
+    if shape[-1:] == (cols,) and t.is_contiguous():
+        return cols
     return _rows(t, cols, what)[1]
 
 
@@ -168,7 +178,7 @@ def squant_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bi
     ws = _workspace(x, nbytes)
     _check(_lib().squant_linear(x.data_ptr(), ldx, type_, rows, ctypes.byref(w), _ptr(bias), act, _ptr(residual), ldr,
                                 out.data_ptr(), ldy, how, _ptr(kept), _ptr(kept_scales), _ptr(ws), nbytes,
-                                _stream_ptr(None)))
+                                _current_stream(device)))
     if keep is None:
         return out
     return out, ((kept, kept_scales) if how == KEEP_INT8 else kept)
@@ -210,7 +220,7 @@ def squant_linear_backward(dy: torch.Tensor, codes: torch.Tensor, scales: torch.
     ws = _workspace(dy, nbytes)
     _check(_lib().squant_linear_backward(dy.data_ptr(), lddy, type_, rows, ctypes.byref(w), act, how, _ptr(z),
                                          _ptr(z_scales), dx.data_ptr(), lddx, _ptr(dbias), _ptr(ws), nbytes,
-                                         _stream_ptr(None)))
+                                         _current_stream(device)))
     return dx, dbias
 
 
@@ -240,7 +250,7 @@ def squant_cross_entropy(h: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
     ws = _workspace(h, nbytes)
     _check(_lib().squant_cross_entropy(h.data_ptr(), ldh, type_, rows, ctypes.byref(w), labels.data_ptr(),
                                        ignore_index, loss.data_ptr(), lse.data_ptr(), _ptr(ws), nbytes,
-                                       _stream_ptr(None)))
+                                       _current_stream(device)))
     return loss, lse
 
 
@@ -268,7 +278,7 @@ def squant_cross_entropy_backward(h: torch.Tensor, codes: torch.Tensor, scales: 
     ws = _workspace(h, nbytes)
     _check(_lib().squant_cross_entropy_backward(h.data_ptr(), ldh, type_, rows, ctypes.byref(w), labels.data_ptr(),
                                                 ignore_index, lse.data_ptr(), dloss.data_ptr(), dh.data_ptr(), lddh,
-                                                _ptr(ws), nbytes, _stream_ptr(None)))
+                                                _ptr(ws), nbytes, _current_stream(device)))
     return dh
 
 
