@@ -218,11 +218,12 @@ __global__ void __launch_bounds__(kRowThreads) join(JoinArgs a) {
     for (int i = 0; i < 4; ++i) v[column_of<GRAD>(c, i)] = t[c][i];
   const int64_t row = rf * 16 + (lane & 15);
   const int32_t col = (int32_t)tile * kTile + (lane >> 4) * 16;
-  if constexpr (GRAD) finish_grad(a.f, row, col, v);
+  const RowValues shared = row_values(a.f, row);
+  if constexpr (GRAD) finish_grad(a.f, row, col, v, shared.factor);
   else {
     Columns<16> columns;
     load_columns<16, T>(columns, a.f, col);
-    finish_layer<16, T>(a.f, columns, row, col, v, row_factor_of(a.f, row), a.planes);
+    finish_layer<16, T>(a.f, columns, row, col, v, shared, a.planes);
   }
 }
 

@@ -264,18 +264,23 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
   // One copy of the epilogue's code: the fragment is picked by uniform branches, so that every register is
   // named (unrolled eight times it is larger than the instruction cache, indexed it sends the sums to scratch memory).
   typedef typename OutOf<F, PL>::type T;
-  // The columns' scales and biases wait in the LDS, where they cost no registers beside the sums.
-  float* shared_columns = reinterpret_cast<float*>(smem);  // [2][kWide]
-  if constexpr (!GRAD) {
-    __syncthreads();
-    if (threadIdx.x < kWide) {
+  // What columns and rows share waits in the LDS, where it costs no registers beside the sums and no trip to memory
+  // for each fragment.
+  float* shared_columns = reinterpret_cast<float*>(smem);              // [2][kWide]
+  RowValues* shared_rows = reinterpret_cast<RowValues*>(smem + 2 * kWide * sizeof(float));  // [MT]
+  __syncthreads();
+  if (threadIdx.x < kWide) {
+    if constexpr (!GRAD) {
       Columns<1> one;
       load_columns<1, T>(one, a.f, tile_n * kWide + (int)threadIdx.x);
       shared_columns[threadIdx.x] = one.scale[0];
       shared_columns[kWide + threadIdx.x] = one.bias[0];
     }
-    __syncthreads();
+    if (threadIdx.x < MT) shared_rows[threadIdx.x] = row_values(a.f, row0 + threadIdx.x);
   }
+  const float prob_unit = a.f.kind == kProb ? *a.f.prob_unit : 1.0f;
+  const int32_t out_col = col0 + quad * 16;
+  __syncthreads();
 #pragma unroll 1
   for (int m = 0; m < S::kOwn; ++m) {
     float4v t[4];
@@ -290,9 +295,10 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
     for (int c = 0; c < 4; ++c)
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[column_of<GRAD>(c, i)] = t[c][i];
-    const int64_t row = row0 + (first_frag + m) * 16 + sub;
+    const int in_tile = (first_frag + m) * 16 + sub;
+    const int64_t row = row0 + in_tile;
     if constexpr (GRAD) {
-      finish_grad(a.f, row, col0 + quad * 16, v);
+      finish_grad(a.f, row, out_col, v, shared_rows[in_tile].factor);
     } else {
       Columns<16> columns;
       asm volatile("" ::: "memory");  // read again for each fragment
@@ -300,7 +306,7 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
       for (int i = 0; i < 16; ++i) columns.scale[i] = shared_columns[wave_n * kTile + quad * 16 + i];
 #pragma unroll
       for (int i = 0; i < 16; ++i) columns.bias[i] = shared_columns[kWide + wave_n * kTile + quad * 16 + i];
-      finish_layer<16, T>(a.f, columns, row, col0 + quad * 16, v, row_factor_of(a.f, row), PL);
+      finish_layer<16, T>(a.f, columns, row, out_col, v, shared_rows[in_tile], PL, prob_unit);
     }
   }
 }
