@@ -359,9 +359,9 @@ __device__ __forceinline__ void apply_slope(float (&v)[N], const float (&z)[N], 
   } else if (act == SQUANT_ACT_SILU) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      // q = 1 - p without its cancellation
-      const float p = sigmoid(z[i]), q = sigmoid(-z[i]);
-      v[i] *= p > 0.0f && q > 0.0f ? p * __builtin_fmaf(z[i], q, 1.0f) : p;
+      // 1 - p = e p without its cancellation; where p or e has left the range of numbers the slope is p
+      const float e = exp2_fast(-kLog2E * z[i]), p = __builtin_amdgcn_rcpf(1.0f + e);
+      v[i] *= p > 0.0f && e > 0.0f ? p * __builtin_fmaf(z[i], e * p, 1.0f) : p;
     }
   }
 }

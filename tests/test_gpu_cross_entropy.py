@@ -184,3 +184,21 @@ def test_zero_rows_streams_and_a_graph(sq):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(step(), out)), f"replay {i}"
+
+
+def test_a_last_piece_shorter_than_the_slices(sq):
+    """The gradient's contraction is cut into slices by a whole piece; a last piece of two steps leaves some of them empty."""
+    t, d, v = 2100, 64, 63744 + 70  # a piece holds 2^27 probabilities in whole tiles of 256 entries: 63744 for 2100 rows
+    assert (1 << 27) // t // 256 * 256 == 63744
+    rng = np.random.default_rng(43)
+    h = torch.from_numpy(rng.standard_normal((t, d)).astype(np.float32)).to(BF16)
+    c = codes_of(rng, v, d, "int8", False)
+    scales = torch.from_numpy(rng.uniform(0.001, 0.004, v).astype(np.float32))
+    labels = torch.from_numpy(rng.integers(63700, v, t))
+    hg, cg, sg, lg = h.cuda(), c.cuda(), scales.cuda(), labels.cuda()
+    loss, lse = sq.squant_cross_entropy(hg, cg, sg, lg)
+    dh = sq.squant_cross_entropy_backward(hg, cg, sg, lg, lse, torch.ones(t, device="cuda"))
+    rows = torch.from_numpy(rng.integers(0, t, 40))
+    w, logits, lse64, loss64, p, y, g, want = definition(h[rows], c, scales, labels[rows], torch.ones(40))
+    assert ((loss.cpu().double()[rows] - loss64).abs() <= 2.0 ** -16).all()
+    assert ((dh.cpu().double()[rows] - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -10 * (p ** 2 @ w ** 2).sqrt() + 2.0 ** -20).all()
