@@ -394,3 +394,25 @@ def test_exact_products_of_every_tile(sq, m, n, k, dtype, fmt):
         w.copy_(packed)
         assert_rounded(sq.squant_linear(x, w, scales), want.cpu(), dtype, f"codes {off} bytes on")
         assert_rounded(sq.squant_linear_backward(dy, w, scales, k, bias=False)[0], want_dx.cpu(), dtype, f"dx, codes {off} bytes on")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "int4"])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("m,k", [(2, 40001), (16, 4100), (40, 2050), (64, 1024)])
+def test_few_long_rows_between_words(sq, m, k, dtype, fmt):
+    """16-bit rows that begin off 32-bit words, and enough of them that they are laid out first."""
+    rng = np.random.default_rng([m, k])
+    x = torch.from_numpy(rng.integers(-2, 3, (m, k)).astype(np.float32))
+    c = codes_of(rng, 150, k, fmt)
+    scales = torch.full((150,), 2.0 ** -8)
+    want = (x.double() @ c.double().t()) * 2.0 ** -8
+    labels = torch.from_numpy(rng.integers(0, 150, m)).cuda()
+    lse = None
+    for pad, begin in ((0, 0), (1, 0), (3, 1), (2, 1), (8, 0)):
+        buf = torch.full((m, k + pad), float("nan"), dtype=dtype, device="cuda")
+        view = buf[:, begin:begin + k]
+        view.copy_(x)
+        assert_rounded(sq.squant_linear(view, on_gpu(c, fmt), scales.cuda()), want, dtype, f"pad {pad}, from {begin}")
+        got = sq.squant_cross_entropy(view, on_gpu(c, fmt), scales.cuda() / 64, labels)[1]
+        lse = got if lse is None else lse
+        assert torch.equal(got, lse)
