@@ -264,7 +264,7 @@ int squant_linear(const void* d_x, int64_t ldx, squant_wtype_t type, int64_t row
  * dz = dy * act'(z), z as kept;  dx[m][k] = sum_n dz[m][n] * scales[n] * codes[n][k];
  * dbias[n] = sum_m dz[m][n].  d_dbias may be NULL.  With SQUANT_ACT_NONE keep is SQUANT_KEEP_NONE, with
  * the others it is not (SQUANT_ERR_MODE).  dz * scale is held in binary16 with an exponent for each row
- * (12 bits; binary32: 22). */
+ * (11 bits; binary32: 22). */
 size_t squant_linear_backward_workspace_bytes(squant_wtype_t type, int64_t rows, const squant_codes_t* h_w);
 int squant_linear_backward(const void* d_dy, int64_t lddy, squant_wtype_t type, int64_t rows,
                            const squant_codes_t* h_w, squant_activation_t act, squant_keep_t keep,

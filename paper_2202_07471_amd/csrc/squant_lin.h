@@ -11,8 +11,9 @@
 //                       lands in [2^14, 2^15)): 22 bits of an element, or 2^-40 of the row's largest where
 //                       that is more.  bfloat16 would take three planes for the same.  A pass of its own lays them
 //                       out; few rows are split in registers, with an exponent of what a wave has seen of a row;
-//   gradients           one plane like this for 16-bit outputs (2^-12 of an element, an eighth of what a
-//                       bfloat16 gradient would be off by), two for binary32.
+//   gradients           one plane like this for 16-bit outputs (at most 2^-11 of an element: an eighth of what a
+//                       bfloat16 gradient would be off by, for a binary16 one as much as its output's rounding; two
+//                       planes would take twice the products), two for binary32.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -48,7 +48,7 @@ inline Split split_product(int64_t rows, int64_t cols, int64_t depth, int planes
     for (int s = 1; s <= 64 && s <= blocks; s = s < 4 ? s + 1 : s * 2) {
       if (s > 1 && !may_split) break;
       const int64_t rounds = (tm * tn * s + kCus - 1) / kCus;
-      const double join = s > 1 ? 3.0 + (double)tm * mt * tn * kWide * 4.0 * s / 3.0e6 : 0.0;
+      const double join = s > 1 ? 4.5 + (double)tm * mt * tn * kWide * 4.0 * s / 3.0e6 : 0.0;
       const double time = rounds * (step * ((blocks + s - 1) / s) + 3.0) + join;
       if (time < best_time) {
         best_time = time;
