@@ -282,9 +282,12 @@ int squant_cross_entropy(const void* d_h, int64_t ldh, squant_wtype_t type, int6
                          float* d_loss, float* d_lse, void* d_workspace, size_t workspace_bytes,
                          void* stream);
 
-/* dh[t][d] = dloss[t] * (sum_v p[t][v] * scales[v] * codes[v][d] - scales[y] * codes[y][d]) with
- * p = exp(l - lse) and y the label (lse of the call above; its own gradient is not taken); 0 where the
- * label is ignore_index.  The vocabulary is walked in pieces whose probabilities fit the workspace. */
+/* dh[t][d] = dloss[t] * sum over v != y of p[t][v] * (scales[v] * codes[v][d] - scales[y] * codes[y][d])
+ * with p = exp(l - lse) and y the label (lse of the call above; its own gradient is not taken), which is the
+ * gradient in the form that keeps its precision where the label is likely; 0 where the label is
+ * ignore_index, NaN where it is no entry.  p * scale is held in binary16 (11 bits; binary32: 22), or to 2^-38 of
+ * the vocabulary's largest scale where that is more.  The vocabulary is walked in pieces whose
+ * probabilities are in the workspace: about 256 MB, or 4096 entries of each row where that is more. */
 size_t squant_cross_entropy_backward_workspace_bytes(const void* d_h, int64_t ldh, squant_wtype_t type,
         int64_t rows, const squant_codes_t* h_w);
 int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t type, int64_t rows,

@@ -260,8 +260,13 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes, sizeof(T) == 2 && 
     }
     RowValues shared = row_values(a.f, row0 + wave * 16 + sub);
     shared.factor = power_of_two(-e);
-    finish_layer<16, T>(a.f, columns, row0 + wave * 16 + sub, col0 + quad * 16, v, shared, kSplit ? 2 : 1,
-                        a.f.kind == kProb ? *a.f.prob_unit : 1.0f);
+    const int64_t row = row0 + wave * 16 + sub;
+    if (a.f.kind == kProb) {
+      const float others = finish_prob<PL>(a.f, columns, row, col0 + quad * 16, v, shared, *a.f.prob_unit);
+      if (quad == 0) store_others(a.f, row, blockIdx.x, others, a.accumulate);
+    } else {
+      finish_layer<16, T>(a.f, columns, row, col0 + quad * 16, v, shared);
+    }
   } else {
     if (wave >= MF * NF) return;
     const int m = wave / NF, c = wave % NF;
@@ -271,7 +276,7 @@ __global__ void __launch_bounds__(few_waves(MF, NF) * kLanes, sizeof(T) == 2 && 
     const int e = kSplit ? least(m) : 0;
     const float4v t = total(m, c, e);
     float v[4] = {t[0], t[1], t[2], t[3]};
-    finish_layer<4, T>(a.f, columns, row0 + m * 16 + sub, col, v, RowValues{power_of_two(-e), -1, 0.0f}, 1);
+    finish_layer<4, T>(a.f, columns, row0 + m * 16 + sub, col, v, RowValues{power_of_two(-e), -1, 0.0f});
   }
 }
 

@@ -6,8 +6,8 @@ namespace squant {
 namespace lin {
 
 product_t gradient_2(int format, int mt) {
-  return format == SQUANT_OUT_INT4 ? product_of<Half, 2, SQUANT_OUT_INT4, true>(mt)
-                                   : product_of<Half, 2, SQUANT_OUT_INT8, true>(mt);
+  return format == SQUANT_OUT_INT4 ? product_of<Half, 2, SQUANT_OUT_INT4, kGradient>(mt)
+                                   : product_of<Half, 2, SQUANT_OUT_INT8, kGradient>(mt);
 }
 
 }  // namespace lin

@@ -6,8 +6,8 @@ namespace squant {
 namespace lin {
 
 product_t layer_bf16(int format, int mt) {
-  return format == SQUANT_OUT_INT4 ? product_of<Brain, 1, SQUANT_OUT_INT4, false>(mt)
-                                   : product_of<Brain, 1, SQUANT_OUT_INT8, false>(mt);
+  return format == SQUANT_OUT_INT4 ? product_of<Brain, 1, SQUANT_OUT_INT4, kLayer>(mt)
+                                   : product_of<Brain, 1, SQUANT_OUT_INT8, kLayer>(mt);
 }
 
 }  // namespace lin

@@ -6,8 +6,8 @@ namespace squant {
 namespace lin {
 
 product_t layer_f32(int format, int mt) {
-  return format == SQUANT_OUT_INT4 ? product_of<Half, 2, SQUANT_OUT_INT4, false>(mt)
-                                   : product_of<Half, 2, SQUANT_OUT_INT8, false>(mt);
+  return format == SQUANT_OUT_INT4 ? product_of<Half, 2, SQUANT_OUT_INT4, kLayer>(mt)
+                                   : product_of<Half, 2, SQUANT_OUT_INT8, kLayer>(mt);
 }
 
 }  // namespace lin

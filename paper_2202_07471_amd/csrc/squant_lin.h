@@ -69,7 +69,11 @@ struct Finish {
   _Float16* prob;           // [rows][planes][ld_prob]
   int64_t ld_prob;          // elements between rows
   int64_t prob_plane;       // elements between planes
+  float* label_prob;        // [rows]
+  float* other_sums;        // [tiles of columns][rows]: sums of the probabilities beside the label's
+  int32_t other_tiles;
   int32_t first_col;        // vocabulary entry of column 0 of the piece
+  int32_t vocabulary;
   const uint8_t* codes;     // kGradLoss: the label's row
   int64_t code_row;
   int32_t format;
@@ -88,7 +92,7 @@ struct ProductArgs {
   int32_t blocks;      // ceil(contraction / 64)
   int32_t slices;      // the contraction is cut into this many
   int32_t tiles_m, tiles_n;
-  int accumulate;      // kPartial: the sums are added to those in `partial`
+  int accumulate;      // kPartial, kProb: the sums are added to those in `partial`, `other_sums`
   Finish f;
 };
 
@@ -487,14 +491,14 @@ __device__ __forceinline__ void load_columns(Columns<NC>& k, const Finish& f, in
 // memory in each (loss and gradient of 2048 rows over 32768 entries 799 us with, 785 us without).
 struct RowValues {
   float factor;  // of a row held in planes
-  int32_t label;  // kStats: the label's column, or -1
+  int32_t label;  // kStats, kProb: the label's column, or -1
   float lse;      // kProb: base 2
 };
 __device__ __forceinline__ RowValues row_values(const Finish& f, int64_t row) {
   RowValues r = {1.0f, -1, 0.0f};
   if (row >= f.rows) return r;
   if (f.row_factor) r.factor = f.row_factor[row];
-  if (f.kind == kStats) {
+  if (f.kind == kStats || f.kind == kProb) {
     const int64_t at = f.labels[row] - f.first_col;
     r.label = at >= 0 && at < f.cols ? (int32_t)at : -1;
   }
@@ -506,7 +510,7 @@ __device__ __forceinline__ RowValues row_values(const Finish& f, int64_t row) {
 // hold the row's 64 columns of one tile (every lane of the wave calls).  T: the output's type.
 template <int NC, class T>
 __device__ __forceinline__ void finish_layer(const Finish& f, const Columns<NC>& k, int64_t row, int32_t col, float (&v)[NC],
-                                             const RowValues& shared, int planes, float prob_unit = 1.0f) {
+                                             const RowValues& shared) {
   const bool live = row < f.rows;
   const int valid = live ? min(max(f.cols - col, 0), NC) : 0;
   const float factor = f.unit * shared.factor;
@@ -585,25 +589,64 @@ __device__ __forceinline__ void finish_layer(const Finish& f, const Columns<NC>&
       sum += __shfl_xor(sum, 32);
       if (live && col < f.cols && (col & (kTile - 1)) == 0)
         f.stats[row * ((f.cols + kTile - 1) / kTile) + col / kTile] = make_float2(top, sum);
-      return;
-    }
-    if (f.kind == kProb && live && col < (f.cols + kTile - 1) / kTile * kTile) {
-      // p * scale * 2^E; zero from the piece's end to its next multiple of 64 columns
-      const float l2 = shared.lse;
-      _Float16* p = f.prob + row * f.ld_prob + col;
-      float lo[NC];
-#pragma unroll
-      for (int i = 0; i < NC; ++i) {
-        v[i] = i < valid ? exp2_fast(__builtin_fmaf(v[i], kLog2E, -l2)) * (k.scale[i] * prob_unit) : 0.0f;
-        lo[i] = v[i] - (float)(_Float16)v[i];
-      }
-      store_cols<NC, _Float16>(p, v, NC);
-      if (planes == 2) store_cols<NC, _Float16>(p + f.prob_plane, lo, NC);
     }
   }
 }
 
+// The gradient's row operand from 16 logits of a row, on the same lanes: p * scale * 2^E in PL planes, zero at the label and
+// from the piece's end to its next multiple of 64 columns.  Returns the sum of the tile's probabilities beside the label's.
+template <int PL>
+__device__ __forceinline__ float finish_prob(const Finish& f, const Columns<16>& k, int64_t row, int32_t col, float (&v)[16],
+                                             const RowValues& shared, float prob_unit) {
+  const bool live = row < f.rows;
+  const int valid = live ? min(max(f.cols - col, 0), 16) : 0;
+  const float factor = f.unit * shared.factor;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    v[i] = v[i] * k.scale[i] * factor;
+    v[i] = i < valid ? exp2_fast(__builtin_fmaf(v[i], kLog2E, -shared.lse)) : 0.0f;
+  }
+  const int32_t at = shared.label - col;
+  if (__any(at >= 0 && at < valid)) {
+    if (at >= 0 && at < valid) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (at == i) f.label_prob[row] = v[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = at == i ? 0.0f : v[i];
+  }
+  float others = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    others += v[i];
+    v[i] *= k.scale[i] * prob_unit;
+  }
+  if (live && col < (f.cols + kTile - 1) / kTile * kTile) {
+    _Float16* p = f.prob + row * f.ld_prob + col;
+    store_cols<16, _Float16>(p, v, 16);
+    if (PL == 2) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] -= (float)(_Float16)v[i];
+      store_cols<16, _Float16>(p + f.prob_plane, v, 16);
+    }
+  }
+  others += __shfl_xor(others, 16);
+  return others + __shfl_xor(others, 32);
+}
+
+// kProb: a row's sum of one tile of columns.  Pieces of the vocabulary add to the same sums.
+__device__ __forceinline__ void store_others(const Finish& f, int64_t row, int32_t tile, float sum, bool accumulate) {
+  if (row >= f.rows) return;
+  float* p = f.other_sums + tile * f.rows + row;
+  *p = accumulate ? *p + sum : sum;
+}
+
 // The same for the gradients: columns are the layer's inputs.
+//
+// Of the loss: dh = g * (sum over v != y of p_v w_v - (1 - p_y) w_y).  Where p_y > 1/2, 1 - p_y is the other probabilities' sum: as
+// a difference it would be off by the rounding of p_y, many times the gradient of a row whose label is likely.
+// `row_factor`: 2^-e of the row, or 1 - p_y (kGradLoss).
 template <class T>
 __device__ __forceinline__ void finish_grad_as(const Finish& f, int64_t row, int32_t col, float (&v)[16], float row_factor) {
   const int valid = row < f.rows ? min(max(f.cols - col, 0), 16) : 0;
@@ -617,11 +660,11 @@ __device__ __forceinline__ void finish_grad_as(const Finish& f, int64_t row, int
     if (label == f.ignore) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) v[i] = 0.0f;
-    } else if (label < 0 || label >= f.first_col) {  // first_col holds the vocabulary's size here
+    } else if (label < 0 || label >= f.vocabulary) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) v[i] = __builtin_nanf("");
     } else {
-      const float factor = f.unit / *f.prob_unit, g = f.dloss[row], s = f.scales[label];
+      const float factor = f.unit / *f.prob_unit, g = f.dloss[row], s = row_factor * f.scales[label];
       const uint8_t* codes = f.codes + label * f.code_row;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {

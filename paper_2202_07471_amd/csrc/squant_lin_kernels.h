@@ -11,6 +11,9 @@ namespace lin {
 product_t layer_bf16(int format, int mt);
 product_t layer_f16(int format, int mt);
 product_t layer_f32(int format, int mt);
+product_t prob_bf16(int format, int mt);
+product_t prob_f16(int format, int mt);
+product_t prob_f32(int format, int mt);
 product_t gradient_1(int format, int mt);  // planes of the row operand
 product_t gradient_2(int format, int mt);
 product_t few_bf16(int format, int mf, int nf, bool words);

@@ -192,7 +192,6 @@ struct JoinArgs {
   int slices;
   int64_t row_frags, col_frags;
   Finish f;
-  int planes;
 };
 // Adds the slices of a split product in their order: one wave a fragment of 16 rows and 64 columns.
 template <bool GRAD, class T>
@@ -219,11 +218,26 @@ __global__ void __launch_bounds__(kRowThreads) join(JoinArgs a) {
   const int64_t row = rf * 16 + (lane & 15);
   const int32_t col = (int32_t)tile * kTile + (lane >> 4) * 16;
   const RowValues shared = row_values(a.f, row);
-  if constexpr (GRAD) finish_grad(a.f, row, col, v, shared.factor);
-  else {
+  if constexpr (GRAD) {
+    float factor = shared.factor;
+    if (a.f.kind == kGradLoss) {
+      const int64_t at = min(row, a.f.rows - 1);
+      const float label = a.f.label_prob[at];
+      factor = 1.0f - label;
+      if (__any(label > 0.5f)) {
+        float others = 0.0f;
+#pragma unroll 8
+        for (int32_t i = lane >> 4; i < a.f.other_tiles; i += 4) others += a.f.other_sums[i * a.f.rows + at];
+        others += __shfl_xor(others, 16);
+        others += __shfl_xor(others, 32);
+        factor = label > 0.5f ? others : factor;
+      }
+    }
+    finish_grad(a.f, row, col, v, factor);
+  } else {
     Columns<16> columns;
     load_columns<16, T>(columns, a.f, col);
-    finish_layer<16, T>(a.f, columns, row, col, v, shared, a.planes);
+    finish_layer<16, T>(a.f, columns, row, col, v, shared);
   }
 }
 

@@ -76,7 +76,10 @@ int launch_layer(int type, const squant_codes_t& w, const Split& p, hipStream_t 
                                                : few_bf16(format, p.row_frags, p.col_frags_each, words);
     return launch_product(k, p, p.lds, st, a);
   }
-  const product_t k = type == SQUANT_W_F32 ? layer_f32(format, p.mt) : type == SQUANT_W_F16 ? layer_f16(format, p.mt) : layer_bf16(format, p.mt);
+  const bool prob = a.f.kind == kProb;
+  const product_t k = type == SQUANT_W_F32   ? (prob ? prob_f32 : layer_f32)(format, p.mt)
+                      : type == SQUANT_W_F16 ? (prob ? prob_f16 : layer_f16)(format, p.mt)
+                                             : (prob ? prob_bf16 : layer_bf16)(format, p.mt);
   return launch_product(k, p, product_lds(p.mt, planes_of(type), format), st, a);
 }
 
@@ -156,7 +159,6 @@ void set_product(ProductArgs& a, const RowOperand& x, const CodeOperand& c, cons
 int launch_join(bool grad, int type, const Split& p, const float4v* partial, const Finish& f, hipStream_t st) {
   JoinArgs j{};
   j.partial = partial; j.slices = p.slices; j.row_frags = p.row_frags_all; j.col_frags = p.col_frags_all; j.f = f;
-  j.planes = planes_of(type);
   const int64_t waves = p.row_frags_all * (p.col_frags_all / 4);
   constexpr int per = kRowThreads / kLanes;
   return launch(join_kernel(grad, type), (waves + per - 1) / per, 1, kRowThreads, 0, st, j);
@@ -205,7 +207,8 @@ size_t lay_out_loss(void* ws, const void* h, int64_t ldh, int type, int64_t rows
 }
 
 struct LossBackwardSpace {
-  RowOperand x; CodeOperand w; RowsArgs rows; bool copy; float* unit; _Float16* prob; int64_t piece; int32_t pieces; float4v* partial; Split g;
+  RowOperand x; CodeOperand w; RowsArgs rows; bool copy; float* unit; _Float16* prob; int64_t piece; int32_t pieces;
+  float* label_prob; float* other_sums; int32_t other_tiles; float4v* partial; Split g;
 };
 size_t lay_out_loss_backward(void* ws, const void* h, int64_t ldh, int type, int64_t rows, const squant_codes_t& w, LossBackwardSpace& s) {
   Cutter c{(char*)ws};
@@ -217,6 +220,9 @@ size_t lay_out_loss_backward(void* ws, const void* h, int64_t ldh, int type, int
   s.piece = vocabulary_piece(rows, w.cout, planes);
   s.pieces = (int32_t)((w.cout + s.piece - 1) / s.piece);
   s.prob = c.take<_Float16>(rows * planes * s.piece);
+  s.other_tiles = split_layer(rows, s.piece, w.cin, planes, true, false).tiles_n;  // of the first piece: a last one has fewer
+  s.other_sums = c.take<float>(rows * s.other_tiles);
+  s.label_prob = c.take<float>(rows);
   s.g = split_gradient(rows, w.cin, s.piece, planes);
   s.partial = c.take<float4v>(s.g.partial_vectors());
   return c.used;
@@ -393,6 +399,8 @@ int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t t
     f.kind = kProb; f.out_type = (int)type; f.unit = layer_unit((int)type, (int)w.format);
     f.rows = rows; f.cols = piece.cout; f.row_factor = s.x.factor; f.scales = w.scales + first;
     f.lse = d_lse; f.prob_unit = s.unit; f.prob = s.prob; f.ld_prob = planes * s.piece; f.prob_plane = s.piece;
+    f.labels = d_labels; f.first_col = first; f.label_prob = s.label_prob; f.other_sums = s.other_sums;
+    a.accumulate = i > 0;
     if (int rc = launch_layer((int)type, piece, p, st, a)) return rc;
     ProductArgs g{};
     Split split = s.g;
@@ -405,7 +413,7 @@ int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t t
   Finish f{};
   f.kind = kGradLoss; f.out_type = (int)type; f.unit = kColumnUnitInverse; f.rows = rows; f.cols = w.cin; f.scales = w.scales;
   f.out = d_dh; f.ldo = lddh; f.labels = d_labels; f.ignore = ignore_index; f.dloss = d_dloss; f.prob_unit = s.unit;
-  f.first_col = w.cout; f.codes = (const uint8_t*)w.codes; f.code_row = code_row(w); f.format = (int)w.format;
+  f.vocabulary = w.cout; f.label_prob = s.label_prob; f.other_sums = s.other_sums; f.other_tiles = s.other_tiles; f.codes = (const uint8_t*)w.codes; f.code_row = code_row(w); f.format = (int)w.format;
   return launch_join(true, (int)type, s.g, s.partial, f, st);
 }
 

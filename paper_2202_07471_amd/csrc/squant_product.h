@@ -51,13 +51,19 @@ __device__ __forceinline__ void to_lds(const void* p, void* lds) {
                                    (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
 }
 
+// What a product is for.  The loss gradient's logits have kernels of their own: with their epilogue beside the layer's the
+// latter spills registers (256 rows: 6 registers, 15 with the sums of the probabilities; 4096 x 4096 x 8192 with gelu and
+// residual 258 us, 268 us).
+enum Role { kLayer, kProbabilities, kGradient };
+
 // A wave's codes of one step: 16 of each of its lanes' 4 columns (layer), or 4 columns of 16 rows (gradient).
 template <int FMT, bool GRAD> struct Raw { typename Codes<FMT>::row16 v[4]; };
 template <int FMT> struct Raw<FMT, true> { typename Codes<FMT>::col4 v[16]; };
 
-template <class F, int PL, int FMT, int MT, bool GRAD>
+template <class F, int PL, int FMT, int MT, Role ROLE>
 __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a) {
   typedef Shape<MT> S;
+  constexpr bool GRAD = ROLE == kGradient;
   constexpr bool kInt8 = FMT == SQUANT_OUT_INT8;
   constexpr int D = product_depth(MT, PL, FMT);
   constexpr int kPlaneBytes = MT * kBlock * 2;
@@ -247,7 +253,7 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
   }
   const int first_frag = wave_m * S::kFrags + group * S::kOwn;  // of those that this wave finishes, in the tile
 
-  if (a.f.kind == kPartial) {
+  if (ROLE != kProbabilities && a.f.kind == kPartial) {
     const int64_t frags_n = (int64_t)a.tiles_n * (kWide / 16);
 #pragma unroll
     for (int m = 0; m < S::kOwn; ++m) {
@@ -267,7 +273,8 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
   // What columns and rows share waits in the LDS, where it costs no registers beside the sums and no trip to memory
   // for each fragment.
   float* shared_columns = reinterpret_cast<float*>(smem);              // [2][kWide]
-  RowValues* shared_rows = reinterpret_cast<RowValues*>(smem + 2 * kWide * sizeof(float));  // [MT]
+  float* shared_sums = shared_columns + 2 * kWide;                      // [kWide / kTile][MT], kProb
+  RowValues* shared_rows = reinterpret_cast<RowValues*>(shared_sums + kWide / kTile * MT);  // [MT]
   __syncthreads();
   if (threadIdx.x < kWide) {
     if constexpr (!GRAD) {
@@ -278,7 +285,7 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
     }
     if (threadIdx.x < MT) shared_rows[threadIdx.x] = row_values(a.f, row0 + threadIdx.x);
   }
-  const float prob_unit = a.f.kind == kProb ? *a.f.prob_unit : 1.0f;
+  const float prob_unit = ROLE == kProbabilities ? *a.f.prob_unit : 1.0f;
   const int32_t out_col = col0 + quad * 16;
   __syncthreads();
 #pragma unroll 1
@@ -306,16 +313,29 @@ __global__ void __launch_bounds__(Shape<MT>::kThreads, 2) product(ProductArgs a)
       for (int i = 0; i < 16; ++i) columns.scale[i] = shared_columns[wave_n * kTile + quad * 16 + i];
 #pragma unroll
       for (int i = 0; i < 16; ++i) columns.bias[i] = shared_columns[kWide + wave_n * kTile + quad * 16 + i];
-      finish_layer<16, T>(a.f, columns, row, out_col, v, shared_rows[in_tile], PL, prob_unit);
+      if constexpr (ROLE == kProbabilities) {
+        const float sum = finish_prob<PL>(a.f, columns, row, out_col, v, shared_rows[in_tile], prob_unit);
+        if (quad == 0) shared_sums[wave_n * MT + in_tile] = sum;
+      } else {
+        finish_layer<16, T>(a.f, columns, row, out_col, v, shared_rows[in_tile]);
+      }
     }
+  }
+  if constexpr (ROLE == kProbabilities) {
+    __syncthreads();
+    if (threadIdx.x >= MT) return;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kWide / kTile; ++i) sum += shared_sums[i * MT + threadIdx.x];
+    store_others(a.f, row0 + threadIdx.x, tile_n, sum, a.accumulate);
   }
 }
 
-template <class F, int PL, int FMT, bool GRAD>
+template <class F, int PL, int FMT, Role ROLE>
 product_t product_of(int mt) {
-  if (mt == 256) return product<F, PL, FMT, 256, GRAD>;
-  if (mt == 128) return product<F, PL, FMT, 128, GRAD>;
-  return product<F, PL, FMT, 64, GRAD>;
+  if (mt == 256) return product<F, PL, FMT, 256, ROLE>;
+  if (mt == 128) return product<F, PL, FMT, 128, ROLE>;
+  return product<F, PL, FMT, 64, ROLE>;
 }
 
 }  // namespace lin

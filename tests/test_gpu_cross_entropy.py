@@ -202,3 +202,72 @@ def test_a_last_piece_shorter_than_the_slices(sq):
     w, logits, lse64, loss64, p, y, g, want = definition(h[rows], c, scales, labels[rows], torch.ones(40))
     assert ((loss.cpu().double()[rows] - loss64).abs() <= 2.0 ** -16).all()
     assert ((dh.cpu().double()[rows] - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -10 * (p ** 2 @ w ** 2).sqrt() + 2.0 ** -20).all()
+
+
+def likely_label_case(t, d, v, dtype, first_label=0, seed=0):
+    """Rows whose label is their likeliest entry, with losses from 1 to 1e-5: each is the label's codes made as long as it takes, and noise."""
+    rng = np.random.default_rng([t, d, v, seed])
+    c = codes_of(rng, v, d, "int8", False)
+    scales = torch.from_numpy((rng.uniform(0.5, 2.0, v) / (64.0 * np.sqrt(d))).astype(np.float32))
+    w = c.double() * scales.double()[:, None]
+    labels = torch.from_numpy(rng.integers(first_label, v, t))
+    noise = 0.3 * torch.from_numpy(rng.standard_normal((t, d)))
+    wanted = 10.0 ** -torch.linspace(0, 5, t, dtype=torch.float64)
+    low, high = torch.zeros(t, dtype=torch.float64), torch.full((t,), 400.0, dtype=torch.float64)
+    to = w[labels] / w[labels].norm(dim=1, keepdim=True)
+    for _ in range(40):
+        middle = (low + high) / 2
+        logits = (noise + middle[:, None] * to) @ w.t()
+        loss = torch.logsumexp(logits, 1) - logits.gather(1, labels[:, None])[:, 0]
+        low, high = torch.where(loss > wanted, middle, low), torch.where(loss > wanted, high, middle)
+    h = (noise + high[:, None] * to).to(dtype)
+    dloss = torch.from_numpy(rng.uniform(0.5, 2, t).astype(np.float32))
+    return h, c, scales, labels, dloss
+
+
+def likely_label_bound(h, c, scales, labels, dloss, dtype):
+    """(dh in 64 bits, how far it may be off).  dh = g sum_{v != y} p_v (w_v - w_y): every term is relative to the entries beside the label."""
+    w, logits, lse, loss, p, y, g, _ = definition(h, c, scales, labels, dloss)
+    assert (loss[-1] < 3e-5) and (loss[0] > 0.3)
+    others = p.scatter(1, y[:, None], 0.0)
+    dh = (others @ w - others.sum(1)[:, None] * w[y]) * g[:, None]  # without the cancellation of 1 - p
+    rms = ((h.double() ** 2) @ (w.t() ** 2)).sqrt()
+    e = sum_error(rms, h.shape[1]) + 2.0 ** -22 * logits.abs()  # of a logit
+    e_lse = (p * e).sum(1) + 2.0 ** -20 + 2.0 ** -22 * lse.abs()
+    off = others * (e + e_lse[:, None] + 2.0 ** -20)  # of a probability
+    pw = ((others ** 2) @ (w ** 2)).sqrt()
+    # a product's operand rounds to 2^-11 of itself (two halves: 2^-22) or 2^-38 of the largest one possible: random errors
+    # of at most that, so 4 times their root-sum-square is seven times the sum's deviation
+    operand = 2.0 ** -22 if dtype == F32 else 2.0 ** -11
+    least = 2.0 ** -38 * scales.double().max() * (c.double() ** 2).sum(0).sqrt()
+    tol = off @ w.abs() + off.sum(1)[:, None] * w[y].abs() + 4 * operand * pw + 4 * least + sum_error(pw, c.shape[0])
+    tol = tol + 2.0 ** -20 * others.sum(1)[:, None] * w[y].abs()
+    return dh, g.abs()[:, None] * tol + U[dtype] * dh.abs() + TINY[dtype]
+
+
+@pytest.mark.parametrize("fmt", ["int8", "int4"])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("t,d,v", [(7, 256, 2000), (50, 130, 517), (130, 256, 2049), (300, 512, 5000)])
+def test_gradient_where_the_label_is_likely(sq, t, d, v, dtype, fmt):
+    h, c, scales, labels, dloss = likely_label_case(t, d, v, dtype)
+    if fmt == "int4":  # the same weights to four bits, scaled up
+        c, scales = torch.clamp(torch.round(c.float() / 18), -7, 7).to(torch.int8), scales * 18
+    want, tol = likely_label_bound(h, c, scales, labels, dloss, dtype)
+    codes = (pack(c) if fmt == "int4" else c).cuda()
+    _, lse = sq.squant_cross_entropy(h.cuda(), codes, scales.cuda(), labels.cuda())
+    got = sq.squant_cross_entropy_backward(h.cuda(), codes, scales.cuda(), labels.cuda(), lse, dloss.cuda())
+    bad = (got.cpu().double() - want).abs() > tol
+    assert not bad.any(), f"rows {bad.any(1).nonzero()[:, 0].tolist()}"
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("first_label", [0, 4096])
+def test_gradient_where_the_label_is_likely_in_pieces(sq, dtype, first_label):
+    """So many rows that the vocabulary is taken in pieces of 4096 entries; labels anywhere, and all in the last piece."""
+    h, c, scales, labels, dloss = likely_label_case(60, 64, 4096 * 2 + 77, dtype, 2 * first_label, seed=1)
+    want, tol = likely_label_bound(h, c, scales, labels, dloss, dtype)
+    times = 560
+    hg, lg, gg = h.repeat(times, 1).cuda(), labels.repeat(times).cuda(), dloss.repeat(times).cuda()
+    _, lse = sq.squant_cross_entropy(hg, c.cuda(), scales.cuda(), lg)
+    got = sq.squant_cross_entropy_backward(hg, c.cuda(), scales.cuda(), lg, lse, gg).cpu().double().view(times, 60, 64)
+    assert ((got - want).abs() <= tol).all()
