@@ -334,6 +334,8 @@ def quantized_linear(x, codes, scales, bias=None, act: int = ACT_NONE, residual=
     """squant_linear with gradients for x, bias and residual; the pre-activation is kept as `keep` says."""
     if act != ACT_NONE and keep not in (KEEP_INT8, KEEP_FULL):
         raise ValueError("keep must be KEEP_INT8 or KEEP_FULL")
+    if not torch.is_grad_enabled():  # the function's own needs_input_grad does not tell
+        keep = KEEP_NONE
     return _Linear.apply(x, codes, scales, bias, act, residual, keep)
 
 

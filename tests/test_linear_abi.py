@@ -137,3 +137,26 @@ def test_the_gradient_of_a_long_batch_needs_no_more_for_a_larger_vocabulary(L):
 def test_more_threads_than_a_launch_has_are_refused(L):
     """A launch counts its threads in 32 bits: rows of which each takes a workgroup."""
     assert L.squant_cross_entropy(P, 64, 0, 1 << 25, codes(), P, -100, P, P, WS, BIG, None) == SHAPE
+
+
+@pytest.mark.parametrize("off", [lambda: torch.no_grad(), lambda: torch.inference_mode()])
+def test_nothing_is_kept_for_a_backward_pass_that_cannot_come(monkeypatch, off):
+    """Without gradients a layer whose bias is trained keeps no pre-activation; with them it does."""
+    from paper_2202_07471_amd import linear
+    keeps = []
+
+    def call(x, codes, scales, bias=None, act=0, residual=None, keep=None, out=None, stream=None):
+        keeps.append(keep)
+        y = torch.zeros(x.shape[0], codes.shape[0])
+        return y, {linear.KEEP_NONE: None, linear.KEEP_FULL: y.clone(), linear.KEEP_INT8: (y.to(torch.int8), y[:, :1])}[keep]
+
+    monkeypatch.setattr(linear, "squant_linear", call)
+    x, c, s = torch.zeros(4, 8), torch.zeros(3, 8, dtype=torch.int8), torch.ones(3)
+    bias = torch.nn.Parameter(torch.zeros(3))
+    for keep in (linear.KEEP_INT8, linear.KEEP_FULL):
+        with off():
+            linear.quantized_linear(x, c, s, bias, linear.ACT_GELU, keep=keep)
+        linear.quantized_linear(x, c, s, bias, linear.ACT_GELU, keep=keep)
+        linear.quantized_linear(x, c, s, bias.detach(), linear.ACT_GELU, keep=keep)
+    none = linear.KEEP_NONE
+    assert keeps == [none, linear.KEEP_INT8, none, none, linear.KEEP_FULL, none]
