@@ -218,8 +218,10 @@ int64_t squant_max_channel_elems(int32_t kh, int32_t kw);
  * d_workspace: the *_workspace_bytes call's amount (which depends on the shapes, on ldx or ldh and on
  * whether x or h and the codes are 16-byte aligned; 0 for many calls, NULL then), 256-byte aligned, not
  * shared with a call that may run at the same time; it holds nothing between calls.  rows = 0 is a no-op,
- * apart from d_dbias, which becomes 0.  The calls launch kernels only and may be captured into a HIP
- * graph.  Infinities and NaN in the activations act as IEEE arithmetic has it (an infinity times a code of
+ * apart from d_dbias, which becomes 0.  A call of which a launch would need 2^32 threads (among others the
+ * loss of 2^24 rows, and a layer of as many binary32 rows) is refused with SQUANT_ERR_SHAPE before its
+ * first launch, and its amount of workspace is 0.  The calls launch kernels only and may be captured into
+ * a HIP graph.  Infinities and NaN in the activations act as IEEE arithmetic has it (an infinity times a code of
  * 0 is NaN, and a row that holds one may be NaN where exact arithmetic has an infinity). */
 
 /* A quantised layer: codes as squant_quantize_ex writes them for SQUANT_OUT_INT8 or SQUANT_OUT_INT4,

@@ -51,8 +51,12 @@ struct Cutter {
 
 int64_t code_row(const squant_codes_t& w) { return w.format == SQUANT_OUT_INT8 ? w.cin : ((int64_t)w.cin + 1) / 2; }
 
+// A launch counts its threads in 32 bits.  Every call asks for all of its launches before the first.
+bool fits(int64_t groups, int threads) { return groups * threads <= 0xffffffffLL; }
+bool fits(const Split& p) { return fits(p.workgroups, p.threads); }
+
 template <class A> int launch(void (*k)(A), int64_t gx, int gy, int threads, size_t lds, hipStream_t st, const A& a) {
-  if (gx * threads > 0xffffffffLL) return SQUANT_ERR_SHAPE;  // a launch counts its threads in 32 bits
+  if (!fits(gx, threads)) return SQUANT_ERR_SHAPE;
   hipLaunchKernelGGL(k, dim3((unsigned)gx, (unsigned)gy), dim3((unsigned)threads), (unsigned)lds, st, a);
   return hipGetLastError() == hipSuccess ? SQUANT_OK : SQUANT_ERR_DEVICE;
 }
@@ -141,12 +145,15 @@ CodeOperand lay_out_codes(Cutter& c, const squant_codes_t& w, bool whole, CodesA
 }
 int64_t code_blocks(const CodesArgs& k) { return (k.chunks + kRowThreads - 1) / kRowThreads; }
 
-// Rows (`copy`) and codes that are laid out before a product, in one launch.
+// Rows (`copy`) and codes that are laid out before a product, in one launch of this many workgroups.
+int64_t lay_out_groups(RowsArgs& r, bool copy, int type) {
+  r.w.first_block = !copy ? 0 : type == SQUANT_W_F32 ? r.rows : (r.rows * (r.padded / 8) + kRowThreads - 1) / kRowThreads;
+  return r.w.first_block + code_blocks(r.w);
+}
 int lay_out(RowsArgs& r, bool copy, int type, hipStream_t st) {
-  if (!copy && !r.w.chunks) return SQUANT_OK;
-  const bool split = copy && type == SQUANT_W_F32;
-  r.w.first_block = !copy ? 0 : split ? r.rows : (r.rows * (r.padded / 8) + kRowThreads - 1) / kRowThreads;
-  return launch(split ? split_rows_kernel() : pad_rows_kernel(), r.w.first_block + code_blocks(r.w), 1, kRowThreads, 0, st, r);
+  const int64_t groups = lay_out_groups(r, copy, type);
+  if (!groups) return SQUANT_OK;
+  return launch(copy && type == SQUANT_W_F32 ? split_rows_kernel() : pad_rows_kernel(), groups, 1, kRowThreads, 0, st, r);
 }
 
 void set_product(ProductArgs& a, const RowOperand& x, const CodeOperand& c, const squant_codes_t& w, const Split& p) {
@@ -156,16 +163,18 @@ void set_product(ProductArgs& a, const RowOperand& x, const CodeOperand& c, cons
   a.blocks = p.blocks; a.slices = p.slices; a.tiles_m = p.tiles_m; a.tiles_n = p.tiles_n;
 }
 
+int64_t join_groups(const Split& p) {
+  constexpr int per = kRowThreads / kLanes;
+  return (p.row_frags_all * (p.col_frags_all / 4) + per - 1) / per;
+}
 int launch_join(bool grad, int type, const Split& p, const float4v* partial, const Finish& f, hipStream_t st) {
   JoinArgs j{};
   j.partial = partial; j.slices = p.slices; j.row_frags = p.row_frags_all; j.col_frags = p.col_frags_all; j.f = f;
-  const int64_t waves = p.row_frags_all * (p.col_frags_all / 4);
-  constexpr int per = kRowThreads / kLanes;
-  return launch(join_kernel(grad, type), (waves + per - 1) / per, 1, kRowThreads, 0, st, j);
+  return launch(join_kernel(grad, type), join_groups(p), 1, kRowThreads, 0, st, j);
 }
 
-// Workspaces.  Each is laid out by the function that also runs the call, so that the two agree.
-struct LinearSpace { RowOperand x; CodeOperand w; RowsArgs rows; bool copy; float4v* partial; Split p; };
+// Workspaces.  Each is laid out by the function that also runs the call, so that the two agree.  `fit`: so do its launches.
+struct LinearSpace { RowOperand x; CodeOperand w; RowsArgs rows; bool copy; float4v* partial; Split p; bool fit; };
 size_t lay_out_linear(void* ws, const void* x, int64_t ldx, int type, int64_t rows, const squant_codes_t& w, int keep, LinearSpace& s) {
   Cutter c{(char*)ws};
   s.rows = RowsArgs{};
@@ -173,12 +182,18 @@ size_t lay_out_linear(void* ws, const void* x, int64_t ldx, int type, int64_t ro
   s.p = split_layer(rows, w.cout, w.cin, planes_of(type), keep != SQUANT_KEEP_NONE, true);
   s.w = s.p.few ? as_they_are(w) : lay_out_codes(c, w, true, s.rows.w);
   s.partial = s.p.slices > 1 ? c.take<float4v>(s.p.partial_vectors()) : nullptr;
-  return c.used;
+  s.fit = fits(lay_out_groups(s.rows, s.copy, type), kRowThreads) && fits(s.p) && (s.p.slices == 1 || fits(join_groups(s.p), kRowThreads));
+  return s.fit ? c.used : 0;
 }
 
 int gradient_rows_per_group(int64_t rows) { return (int)std::min<int64_t>(kRowGroup, std::max<int64_t>(1, (rows + 1023) / 1024)); }
 
-struct BackwardSpace { CodeOperand w; CodesArgs codes; _Float16* rows; float* factor; float* sums; int64_t partials; int64_t padded; float4v* partial; Split p; };
+struct BackwardSpace {
+  CodeOperand w; CodesArgs codes; _Float16* rows; float* factor; float* sums; int64_t partials; int64_t padded; float4v* partial; Split p;
+  int64_t groups;  // of gradient_rows, by `shared`; the codes' behind them
+  int shared;
+  bool fit;
+};
 size_t lay_out_backward(void* ws, int type, int64_t rows, const squant_codes_t& w, BackwardSpace& s) {
   Cutter c{(char*)ws};
   const int planes = planes_of(type), group = gradient_rows_per_group(rows);
@@ -191,10 +206,16 @@ size_t lay_out_backward(void* ws, int type, int64_t rows, const squant_codes_t& 
   s.sums = c.take<float>(s.partials * w.cout);
   s.p = split_gradient(rows, w.cin, w.cout, planes);
   s.partial = s.p.slices > 1 ? c.take<float4v>(s.p.partial_vectors()) : nullptr;
-  return c.used;
+  const int64_t row_groups = (rows + group - 1) / group, row_threads = (s.padded / 8 + kRowThreads - 1) / kRowThreads;
+  // about 512 workgroups, each of which looks for its rows' largest elements anew
+  s.shared = (int)std::max<int64_t>(1, std::min(row_threads, 512 / row_groups));
+  s.codes.first_block = row_groups;
+  s.groups = row_groups + (code_blocks(s.codes) + s.shared - 1) / s.shared;
+  s.fit = fits(s.groups, kRowThreads) && fits(s.p) && (s.p.slices == 1 || fits(join_groups(s.p), kRowThreads));
+  return s.fit ? c.used : 0;
 }
 
-struct LossSpace { RowOperand x; CodeOperand w; RowsArgs rows; bool copy; float2* stats; float* label_logit; Split p; };
+struct LossSpace { RowOperand x; CodeOperand w; RowsArgs rows; bool copy; float2* stats; float* label_logit; Split p; bool fit; };
 size_t lay_out_loss(void* ws, const void* h, int64_t ldh, int type, int64_t rows, const squant_codes_t& w, LossSpace& s) {
   Cutter c{(char*)ws};
   s.rows = RowsArgs{};
@@ -203,12 +224,13 @@ size_t lay_out_loss(void* ws, const void* h, int64_t ldh, int type, int64_t rows
   s.label_logit = c.take<float>(rows);
   s.p = split_layer(rows, w.cout, w.cin, planes_of(type), true, false);
   s.w = s.p.few ? as_they_are(w) : lay_out_codes(c, w, true, s.rows.w);
-  return c.used;
+  s.fit = fits(lay_out_groups(s.rows, s.copy, type), kRowThreads) && fits(s.p) && fits(rows, kRowThreads);
+  return s.fit ? c.used : 0;
 }
 
 struct LossBackwardSpace {
   RowOperand x; CodeOperand w; RowsArgs rows; bool copy; float* unit; _Float16* prob; int64_t piece; int32_t pieces;
-  float* label_prob; float* other_sums; int32_t other_tiles; float4v* partial; Split g;
+  float* label_prob; float* other_sums; int32_t other_tiles; float4v* partial; Split g; bool fit;
 };
 size_t lay_out_loss_backward(void* ws, const void* h, int64_t ldh, int type, int64_t rows, const squant_codes_t& w, LossBackwardSpace& s) {
   Cutter c{(char*)ws};
@@ -220,12 +242,15 @@ size_t lay_out_loss_backward(void* ws, const void* h, int64_t ldh, int type, int
   s.piece = vocabulary_piece(rows, w.cout, planes);
   s.pieces = (int32_t)((w.cout + s.piece - 1) / s.piece);
   s.prob = c.take<_Float16>(rows * planes * s.piece);
-  s.other_tiles = split_layer(rows, s.piece, w.cin, planes, true, false).tiles_n;  // of the first piece: a last one has fewer
+  const Split first = split_layer(rows, std::min<int64_t>(s.piece, w.cout), w.cin, planes, true, false);
+  const Split last = split_layer(rows, w.cout - (s.pieces - 1) * s.piece, w.cin, planes, true, false);
+  s.other_tiles = first.tiles_n;  // a last piece has fewer
   s.other_sums = c.take<float>(rows * s.other_tiles);
   s.label_prob = c.take<float>(rows);
   s.g = split_gradient(rows, w.cin, s.piece, planes);
   s.partial = c.take<float4v>(s.g.partial_vectors());
-  return c.used;
+  s.fit = fits(lay_out_groups(s.rows, s.copy, type), kRowThreads) && fits(first) && fits(last) && fits(s.g) && fits(join_groups(s.g), kRowThreads);
+  return s.fit ? c.used : 0;
 }
 
 }  // namespace
@@ -256,6 +281,7 @@ int squant_linear(const void* d_x, int64_t ldx, squant_wtype_t type, int64_t row
     return SQUANT_ERR_FORMAT;
   LinearSpace s;
   const size_t need = lay_out_linear(d_workspace, d_x, ldx, (int)type, rows, w, (int)keep, s);
+  if (!s.fit) return SQUANT_ERR_SHAPE;
   if (int rc = check_workspace(d_workspace, workspace_bytes, need)) return rc;
   hipStream_t st = (hipStream_t)stream;
   if (int rc = lay_out(s.rows, s.copy, (int)type, st)) return rc;
@@ -300,19 +326,15 @@ int squant_linear_backward(const void* d_dy, int64_t lddy, squant_wtype_t type, 
     return SQUANT_ERR_FORMAT;
   BackwardSpace s;
   const size_t need = lay_out_backward(d_workspace, (int)type, rows, w, s);
+  if (!s.fit) return SQUANT_ERR_SHAPE;
   if (int rc = check_workspace(d_workspace, workspace_bytes, need)) return rc;
   RowsArgs r{};
   r.x = d_dy; r.ldx = lddy; r.rows = rows; r.cols = w.cout; r.out = s.rows; r.padded = (int32_t)s.padded; r.row_factor = s.factor;
   r.scales = w.scales; r.kept = d_kept; r.kept_scales = d_kept_scales; r.act = (int)act; r.keep = (int)keep;
   r.rows_per_group = gradient_rows_per_group(rows);
   r.column_sums = d_dbias ? s.sums : nullptr;
-  const int64_t groups = (rows + r.rows_per_group - 1) / r.rows_per_group, row_threads = (s.padded / 8 + kRowThreads - 1) / kRowThreads;
-  // about 512 workgroups, each of which looks for its rows' largest elements anew
-  const int shared = (int)std::max<int64_t>(1, std::min(row_threads, 512 / groups));
   r.w = s.codes;
-  r.w.first_block = groups;
-  const int64_t code_groups = (code_blocks(r.w) + shared - 1) / shared;
-  if (int rc = launch(gradient_rows_kernel((int)type), groups + code_groups, shared, kRowThreads, 0, st, r)) return rc;
+  if (int rc = launch(gradient_rows_kernel((int)type), s.groups, s.shared, kRowThreads, 0, st, r)) return rc;
   if (d_dbias) {
     sums.partial = s.sums; sums.partials = s.partials;
     if (int rc = launch(column_sums_kernel(), sum_groups, 1, 1024, 0, st, sums)) return rc;
@@ -348,6 +370,7 @@ int squant_cross_entropy(const void* d_h, int64_t ldh, squant_wtype_t type, int6
     return SQUANT_ERR_FORMAT;
   LossSpace s;
   const size_t need = lay_out_loss(d_workspace, d_h, ldh, (int)type, rows, w, s);
+  if (!s.fit) return SQUANT_ERR_SHAPE;
   if (int rc = check_workspace(d_workspace, workspace_bytes, need)) return rc;
   hipStream_t st = (hipStream_t)stream;
   if (int rc = lay_out(s.rows, s.copy, (int)type, st)) return rc;
@@ -382,6 +405,7 @@ int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t t
     return SQUANT_ERR_FORMAT;
   LossBackwardSpace s;
   const size_t need = lay_out_loss_backward(d_workspace, d_h, ldh, (int)type, rows, w, s);
+  if (!s.fit) return SQUANT_ERR_SHAPE;
   if (int rc = check_workspace(d_workspace, workspace_bytes, need)) return rc;
   hipStream_t st = (hipStream_t)stream;
   if (int rc = lay_out(s.rows, s.copy, (int)type, st)) return rc;

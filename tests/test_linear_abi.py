@@ -160,3 +160,22 @@ def test_nothing_is_kept_for_a_backward_pass_that_cannot_come(monkeypatch, off):
         linear.quantized_linear(x, c, s, bias.detach(), linear.ACT_GELU, keep=keep)
     none = linear.KEEP_NONE
     assert keeps == [none, linear.KEEP_INT8, none, none, linear.KEEP_FULL, none]
+
+
+@pytest.mark.parametrize("type_", [0, 1, 2])
+def test_a_call_with_a_launch_too_large_is_refused_before_its_first(L, type_):
+    """From 2^24 rows on the loss would need 2^32 threads; without a device a launch would say 6."""
+    fits, over = (1 << 24) - 1, 1 << 24
+    for rows in (over, 1 << 25, 1 << 26):
+        assert L.squant_cross_entropy(P, 64, type_, rows, codes(), P, -100, P, P, WS, 1 << 60, None) == SHAPE
+        assert L.squant_cross_entropy_workspace_bytes(P, 64, type_, rows, codes()) == 0
+    assert L.squant_cross_entropy_workspace_bytes(P, 64, type_, fits, codes()) > 0
+    if type_ == 0:  # binary32 rows are laid out by a workgroup each; 16-bit ones are read as they are
+        assert linear(L, rows=over, nbytes=1 << 60) == SHAPE
+        assert L.squant_linear_workspace_bytes(P, 64, 0, over, codes(), 0) == 0 < L.squant_linear_workspace_bytes(P, 64, 0, fits, codes(), 0)
+    big = codes(1 << 22, 1 << 22)  # 2^26 rows: more tiles than a launch has
+    assert linear(L, type_=type_, rows=1 << 26, w=big, ldx=1 << 22, ldr=1 << 22, ldy=1 << 22, nbytes=1 << 62) == SHAPE
+    assert L.squant_linear_backward(P, 1 << 22, type_, 1 << 26, big, 0, 0, None, None, P, 1 << 22, P, WS, 1 << 62, None) == SHAPE
+    assert L.squant_linear_backward_workspace_bytes(type_, 1 << 26, big) == 0
+    assert L.squant_cross_entropy_backward(P, 1 << 22, type_, 1 << 26, big, P, -100, P, P, P, 1 << 22, WS, 1 << 62, None) == SHAPE
+    assert L.squant_cross_entropy_backward_workspace_bytes(P, 1 << 22, type_, 1 << 26, big) == 0
