@@ -531,7 +531,8 @@ __device__ __forceinline__ void finish_layer(const Finish& f, const Columns<NC>&
         for (int i = 0; i < NC; ++i) top = max(top, i < valid ? magnitude(v[i]) : 0u);
         top = group_max(top);
         const float t = __uint_as_float(top);
-        const float per = top ? 127.0f / t : 0.0f;
+        // next to zero 127 / t leaves binary32's range: the group is taken 2^60 times as large
+        const float up = t < 0x1p-60f ? 0x1p60f : 1.0f, per = top ? 127.0f / (t * up) : 0.0f;
         if (live && col < f.cols && (col & (kTile - 1)) == 0)
           f.kept_scales[row * ((f.cols + kTile - 1) / kTile) + col / kTile] = top ? t / 127.0f : 1.0f;
         uint32_t q[4];
@@ -540,7 +541,7 @@ __device__ __forceinline__ void finish_layer(const Finish& f, const Columns<NC>&
           q[d] = 0;
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
-            const float c = fminf(fmaxf(rintf(v[4 * d + b] * per), -127.0f), 127.0f);
+            const float c = fminf(fmaxf(rintf(v[4 * d + b] * up * per), -127.0f), 127.0f);
             q[d] |= ((uint32_t)(int)c & 255u) << (8 * b);
           }
         }

@@ -416,3 +416,24 @@ def test_few_long_rows_between_words(sq, m, k, dtype, fmt):
         got = sq.squant_cross_entropy(view, on_gpu(c, fmt), scales.cuda() / 64, labels)[1]
         lse = got if lse is None else lse
         assert torch.equal(got, lse)
+
+
+@pytest.mark.parametrize("m", [5, 80])
+@pytest.mark.parametrize("size", [2.0 ** -100, 2.0 ** -122, 2.0 ** -126, 2.0 ** -140])
+def test_kept_codes_of_groups_next_to_zero(sq, m, size):
+    """A group's largest |z| may be so small that 127 / it is no binary32 number: the codes are still rounded quotients, zeros among them."""
+    rng = np.random.default_rng(47)
+    z = torch.from_numpy(rng.integers(-100, 101, (m, 192)))
+    z[:, ::3] = 0
+    z[:, 64:128] = 0  # a group of zeros
+    z[:, 1], z[:, 130] = 101, -102
+    x = torch.zeros(m, 192)
+    x[:] = z.float()
+    c = torch.eye(192, dtype=torch.int8)
+    _, (q, s) = sq.squant_linear(x.cuda(), c.cuda(), torch.full((192,), size, device="cuda"), keep=sq.KEEP_INT8)
+    for g, top in ((0, 101.0), (1, 0.0), (2, 102.0)):
+        want = z[:, 64 * g:64 * g + 64].double() * (127 / top) if top else torch.zeros(m, 64)
+        # 2^-22 of a quotient of at most 127, which no quotient here is nearer to a half than
+        assert ((q.cpu()[:, 64 * g:64 * g + 64] - want).abs() <= 0.5 + 2.0 ** -14).all(), f"group {g}"
+        unit = top * size / 127 if top else 1.0
+        assert ((s[:, g].cpu().double() - unit).abs() <= 2.0 ** -23 * unit + 2.0 ** -150).all()
