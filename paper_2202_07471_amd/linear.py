@@ -91,8 +91,8 @@ def _rows(t: torch.Tensor, cols: int, what: str):
     """(rows, elements between rows) of an activation tensor whose last dimension is `cols`."""
     shape, stride = t.shape, t.stride()
     n = len(shape)
-    if n == 0 or shape[-1] != cols:
-        raise ValueError(f"{what} must have {cols} elements in its last dimension")
+    if n == 0 or shape[-1] != cols or cols == 0:
+        raise ValueError(f"{what} must have {cols or 'some'} elements in its last dimension")
     if cols > 1 and stride[-1] != 1:
         raise ValueError(f"{what} must be contiguous in its last dimension")
     if n == 2:

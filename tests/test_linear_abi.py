@@ -179,3 +179,10 @@ def test_a_call_with_a_launch_too_large_is_refused_before_its_first(L, type_):
     assert L.squant_linear_backward_workspace_bytes(type_, 1 << 26, big) == 0
     assert L.squant_cross_entropy_backward(P, 1 << 22, type_, 1 << 26, big, P, -100, P, P, P, 1 << 22, WS, 1 << 62, None) == SHAPE
     assert L.squant_cross_entropy_backward_workspace_bytes(P, 1 << 22, type_, 1 << 26, big) == 0
+
+
+@pytest.mark.parametrize("shape", [(0,), (4, 0), (2, 3, 0), (0, 3, 0)])
+def test_rows_without_elements_are_refused(shape):
+    from paper_2202_07471_amd import linear
+    with pytest.raises(ValueError):
+        linear._rows(torch.zeros(shape), 0, "x")
