@@ -253,7 +253,7 @@ typedef enum {
 
 /* y[m][n] = act(z[m][n]) + residual[m][n],  z[m][n] = scales[n] * sum_k x[m][k] * codes[n][k] + bias[n].
  * d_bias [cout], d_residual [rows][cout] (ldr) and, with SQUANT_KEEP_NONE, d_kept may be NULL;
- * d_kept_scales only with SQUANT_KEEP_INT8.  d_y may be d_residual (ldy == ldr). */
+ * d_kept_scales only with SQUANT_KEEP_INT8.  d_y may be d_residual (ldy == ldr) and overlaps nothing else. */
 size_t squant_linear_workspace_bytes(const void* d_x, int64_t ldx, squant_wtype_t type, int64_t rows,
                                      const squant_codes_t* h_w, squant_keep_t keep);
 int squant_linear(const void* d_x, int64_t ldx, squant_wtype_t type, int64_t rows,

@@ -145,7 +145,8 @@ def squant_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bi
     """act(x @ (codes * scales).T + bias) + residual for x [..., cin]; returns [..., cout] of x's type.
 
     With `keep` (KEEP_INT8, KEEP_FULL or KEEP_NONE) returns (y, kept): the pre-activation for
-    squant_linear_backward as (int8 codes, scales), as a tensor of x's type, or None.  `out` may be `residual`.
+    squant_linear_backward as (int8 codes, scales), as a tensor of x's type, or None.  `out` may be `residual` and
+    may not overlap anything else that is read.
     Asynchronous on `stream` (default: torch's current stream), which the outputs and the workspace belong to."""
     if stream is not None:
         with torch.cuda.stream(stream):
@@ -166,6 +167,9 @@ def squant_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bi
         out = x.new_empty(shape)
     else:
         ldy = _like(out, cout, "out", x, device)
+        at = out.data_ptr()
+        if rows and (at == x.data_ptr() or (residual is not None and at == residual.data_ptr() and ldy != ldr)):
+            raise ValueError("out may not lie over x, nor over residual with another distance between rows")
     kept = kept_scales = None
     how = KEEP_NONE if keep is None else keep
     if how == KEEP_INT8:

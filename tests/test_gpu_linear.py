@@ -437,3 +437,19 @@ def test_kept_codes_of_groups_next_to_zero(sq, m, size):
         assert ((q.cpu()[:, 64 * g:64 * g + 64] - want).abs() <= 0.5 + 2.0 ** -14).all(), f"group {g}"
         unit = top * size / 127 if top else 1.0
         assert ((s[:, g].cpu().double() - unit).abs() <= 2.0 ** -23 * unit + 2.0 ** -150).all()
+
+
+def test_an_output_over_what_is_read_is_refused(sq):
+    """Workgroups write while others still read: only the residual may be written over, in its own layout."""
+    rng = np.random.default_rng(53)
+    x, c, scales, bias = real_case(rng, 200, 96, 96, BF16, "int8")
+    x, c, scales = x.cuda(), c.cuda(), scales.cuda()
+    kept = x.clone()
+    with pytest.raises(ValueError):
+        sq.squant_linear(x, c, scales, out=x)
+    wide = torch.zeros(200, 128, dtype=BF16, device="cuda")
+    with pytest.raises(ValueError):  # the residual's rows 96 apart, the output's 128, from the same element on
+        sq.squant_linear(x, c, scales, residual=wide.view(-1)[:200 * 96].view(200, 96), out=wide[:, :96])
+    torch.cuda.synchronize()
+    assert torch.equal(x, kept) and not wide.any()
+    assert torch.equal(sq.squant_linear(x, c, scales, residual=wide[:, :96], out=wide[:, :96]), sq.squant_linear(x, c, scales))
