@@ -66,13 +66,23 @@ inline Split split_product(int64_t rows, int64_t cols, int64_t depth, int planes
 }
 
 // A layer's product.  `tiled`: columns have to come in whole tiles of 64 (kept pre-activation, loss).
-inline Split split_layer(int64_t rows, int64_t cols, int64_t depth, int planes, bool tiled, bool may_split) {
+inline Split split_layer(int64_t rows, int64_t cols, int64_t depth, int planes, int format, bool tiled, bool may_split) {
   if (rows > few_rows_limit(planes)) return split_product(rows, cols, depth, planes, may_split);
   Split p{};
   p.few = true;
   const int frags = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  // wide workgroups read their rows fewer times, narrow ones fill the chip
-  p.col_frags_each = tiled || cols >= 32 * 1024 ? 4 : cols >= 8 * 1024 ? 2 : 1;
+  // Wide workgroups read their rows fewer times, narrow ones fill the chip: the narrowest of which one for each 16 rows
+  // has a compute unit to itself.  16-bit rows with 8-bit codes stay at 32 columns while those alone fill between half of
+  // the compute units and all.  us with 16, 32, 64 columns a workgroup, rows of 4096, int8 codes:
+  //   13 bfloat16 rows  4096 columns 7.2 8.8 13.3, 6000 12.5 9.2 13.4, 8192 12.8 9.3 14.3, 16384 23.4 18.4 15.6
+  //   64 bfloat16 rows  2048 13.6 9.8 13.7, 4096 18.8 18.2 13.8, 6000 34.9 20.8 27.2, 8192 35.3 21.0 25.2, 16384 68.6 38.5 27.2
+  //   32 binary32 rows  2048 13.4 14.6 19.5, 4096 22.0 15.1 19.7, 6000 38.7 23.3 20.7, 8192 39.1 23.6 20.3, 16384 75.4 45.1 28.2
+  const int64_t row_groups = (rows + 15) / 16;
+  auto groups = [&](int each) { return (cols + 16 * each - 1) / (16 * each); };
+  const bool rows_together = planes == 1 && format == SQUANT_OUT_INT8 && groups(2) <= kCus && groups(2) * 2 > kCus;
+  if (tiled) p.col_frags_each = 4;
+  else if (groups(1) * row_groups <= kCus) p.col_frags_each = 1;
+  else p.col_frags_each = groups(2) * row_groups <= kCus || rows_together ? 2 : 4;
   p.blocks = (int)((depth + kBlock - 1) / kBlock);
   p.slices = 1;
   p.tiles_n = (int)((cols + 16 * p.col_frags_each - 1) / (16 * p.col_frags_each));

@@ -179,7 +179,7 @@ size_t lay_out_linear(void* ws, const void* x, int64_t ldx, int type, int64_t ro
   Cutter c{(char*)ws};
   s.rows = RowsArgs{};
   s.x = lay_out_rows(c, x, ldx, type, rows, w.cin, s.rows, s.copy);
-  s.p = split_layer(rows, w.cout, w.cin, planes_of(type), keep != SQUANT_KEEP_NONE, true);
+  s.p = split_layer(rows, w.cout, w.cin, planes_of(type), (int)w.format, keep != SQUANT_KEEP_NONE, true);
   s.w = s.p.few ? as_they_are(w) : lay_out_codes(c, w, true, s.rows.w);
   s.partial = s.p.slices > 1 ? c.take<float4v>(s.p.partial_vectors()) : nullptr;
   s.fit = fits(lay_out_groups(s.rows, s.copy, type), kRowThreads) && fits(s.p) && (s.p.slices == 1 || fits(join_groups(s.p), kRowThreads));
@@ -222,7 +222,7 @@ size_t lay_out_loss(void* ws, const void* h, int64_t ldh, int type, int64_t rows
   s.x = lay_out_rows(c, h, ldh, type, rows, w.cin, s.rows, s.copy);
   s.stats = c.take<float2>(rows * (((int64_t)w.cout + kTile - 1) / kTile));
   s.label_logit = c.take<float>(rows);
-  s.p = split_layer(rows, w.cout, w.cin, planes_of(type), true, false);
+  s.p = split_layer(rows, w.cout, w.cin, planes_of(type), (int)w.format, true, false);
   s.w = s.p.few ? as_they_are(w) : lay_out_codes(c, w, true, s.rows.w);
   s.fit = fits(lay_out_groups(s.rows, s.copy, type), kRowThreads) && fits(s.p) && fits(rows, kRowThreads);
   return s.fit ? c.used : 0;
@@ -242,8 +242,8 @@ size_t lay_out_loss_backward(void* ws, const void* h, int64_t ldh, int type, int
   s.piece = vocabulary_piece(rows, w.cout, planes);
   s.pieces = (int32_t)((w.cout + s.piece - 1) / s.piece);
   s.prob = c.take<_Float16>(rows * planes * s.piece);
-  const Split first = split_layer(rows, std::min<int64_t>(s.piece, w.cout), w.cin, planes, true, false);
-  const Split last = split_layer(rows, w.cout - (s.pieces - 1) * s.piece, w.cin, planes, true, false);
+  const Split first = split_layer(rows, std::min<int64_t>(s.piece, w.cout), w.cin, planes, (int)w.format, true, false);
+  const Split last = split_layer(rows, w.cout - (s.pieces - 1) * s.piece, w.cin, planes, (int)w.format, true, false);
   s.other_tiles = first.tiles_n;  // a last piece has fewer
   s.other_sums = c.take<float>(rows * s.other_tiles);
   s.label_prob = c.take<float>(rows);
@@ -416,7 +416,7 @@ int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t t
     squant_codes_t piece = w;
     const CodeOperand codes{s.w.p + first * s.w.row, s.w.row};
     piece.cout = (int32_t)std::min<int64_t>(s.piece, w.cout - first);
-    const Split p = split_layer(rows, piece.cout, w.cin, planes, true, false);
+    const Split p = split_layer(rows, piece.cout, w.cin, planes, (int)w.format, true, false);
     ProductArgs a{};
     set_product(a, s.x, codes, piece, p);
     Finish& f = a.f;

@@ -453,3 +453,17 @@ def test_an_output_over_what_is_read_is_refused(sq):
     torch.cuda.synchronize()
     assert torch.equal(x, kept) and not wide.any()
     assert torch.equal(sq.squant_linear(x, c, scales, residual=wide[:, :96], out=wide[:, :96]), sq.squant_linear(x, c, scales))
+
+
+@pytest.mark.parametrize("fmt", ["int8", "int4"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("m", [1, 17, 32, 64])
+@pytest.mark.parametrize("n", [1030, 2051, 4102, 8197, 12290])
+def test_exact_products_of_few_rows_at_every_width(sq, m, n, dtype, fmt):
+    """Each number of columns a workgroup, next to where the plan goes from one to the next."""
+    rng = np.random.default_rng([m, n])
+    x = torch.from_numpy(rng.integers(-4, 5, (m, 258)).astype(np.float32))
+    c = codes_of(rng, n, 258, fmt)
+    scales = torch.from_numpy(2.0 ** rng.integers(-9, -5, n).astype(np.float32))
+    want = (x.double() @ c.double().t()) * scales.double()
+    assert_rounded(sq.squant_linear(x.to(dtype).cuda(), on_gpu(c, fmt), scales.cuda()), want, dtype, "y")
