@@ -1,8 +1,8 @@
 """Quantise a small language model's weights with the solver, then train what is left of it through the codes.
 
 A block of two layers (4-bit codes, packed) and a vocabulary (8-bit codes); the embedding and the biases stay in
-bfloat16 and learn to predict a synthetic sequence.  No weight is dequantised, no logits are kept, and the
-activations wait for the backward pass in 8 bits.  Run on an MI355X:
+bfloat16 and learn to predict a synthetic sequence.  No weight is dequantised, the loss
+keeps no logits, and the activations wait for the backward pass in 8 bits.  Run on an MI355X:
 
     python examples/finetune_quantized.py --steps 50
 """

@@ -205,12 +205,13 @@ int64_t squant_max_channel_elems(int32_t kh, int32_t kw);
 
 /* ---------------------------------------------------------------------------
  * Operators on quantised layers: products with the solver's codes, their gradients, and the
- * cross entropy over a vocabulary whose output embedding is codes.  Nothing dequantises to memory.
+ * cross entropy over a vocabulary whose output embedding is codes.  No weights are dequantised to memory.
  *
  * Element type: the activations' type, binary32, binary16 or bfloat16 (squant_wtype_t), shared by all
  * activation buffers of a call (x, bias, residual, y, dy, dx, dbias).  Codes times activations are
- * multiplied exactly (binary32 activations to 22 bits) and added in binary32; every output is rounded
- * once.  Rows may be any distance apart (ld*, in elements, at least the row's length); activation
+ * multiplied exactly (binary32 activations to 22 bits) and added in binary32; the outputs of a forward
+ * call are rounded once.  dx and dh are rounded twice: what is multiplied by the codes is held in 11 bits
+ * (binary32: 22), which for binary16 is as much again as the output's own rounding.  Rows may be any distance apart (ld*, in elements, at least the row's length); activation
  * buffers need the alignment of their element type, codes none.  Where codes or rows do not lie as the
  * matrix units' kernels read them (cin a multiple of 64, 16-byte aligned; few rows: anything goes) a call
  * copies them to its workspace first.

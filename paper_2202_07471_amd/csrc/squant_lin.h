@@ -12,8 +12,8 @@
 //                       that is more.  bfloat16 would take three planes for the same.  A pass of its own lays them
 //                       out; few rows are split in registers, with an exponent of what a wave has seen of a row;
 //   gradients           one plane like this for 16-bit outputs (at most 2^-11 of an element: an eighth of what a
-//                       bfloat16 gradient would be off by, for a binary16 one as much as its output's rounding; two
-//                       planes would take twice the products), two for binary32.
+//                       bfloat16 gradient would be off by, for a binary16 one as much as its output's rounding,
+//                       1.4 times that in all; two planes would take twice the products), two for binary32.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -36,7 +36,10 @@ inline int shape_threads(int mt) {
 }
 
 // `product` over rows x cols with a contraction of `depth`: the rows of a workgroup and the slices of the
-// contraction by an estimate of the time.  The coefficients are fitted to measured times.
+// contraction by an estimate of the time.  It is there to rank them: the coefficients come from bare products of 44 shapes, of
+// which its choice was within 8 % of the best tile and slices.  It knows neither the codes' format nor the epilogue nor the laying
+// out of rows: bfloat16 and int8 codes, 1024 x 2048 x 4096 20.6 us for 26.3 measured, 4096 x 4096 x 8192 211 for 235 (with gelu and
+// residual 250), 2048 x 2048 x 32768 217 for 262; binary32 1024 x 2048 x 4096 34 for 48, 7 to 10 of them the rows' split.
 inline Split split_product(int64_t rows, int64_t cols, int64_t depth, int planes, bool may_split) {
   Split best{};
   double best_time = 1e30;

@@ -261,7 +261,10 @@ def squant_cross_entropy(h: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
 def squant_cross_entropy_backward(h: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, labels: torch.Tensor,
                                   lse: torch.Tensor, dloss: torch.Tensor, ignore_index: int = IGNORE_INDEX,
                                   dh: Optional[torch.Tensor] = None, stream=None):
-    """dh of squant_cross_entropy for the losses' gradients dloss (float32, one for each row)."""
+    """dh of squant_cross_entropy for the losses' gradients dloss (float32, one for each row).
+
+    The workspace holds the probabilities of a piece of the vocabulary in 16 bits (float32: 32): about 256 MB, or 4096
+    entries of each row where that is more."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return squant_cross_entropy_backward(h, codes, scales, labels, lse, dloss, ignore_index, dh)
