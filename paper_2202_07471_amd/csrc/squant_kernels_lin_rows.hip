@@ -123,12 +123,12 @@ __global__ void __launch_bounds__(kRowThreads) loss_rows(LossArgs a) {
   sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) sum += sums[i];
-  const float lse = (top + log2f(sum)) * kLn2;
-  a.lse[row] = lse;
+  const float rest = log2f(sum);
+  a.lse[row] = (top + rest) * kLn2;
   const int64_t label = a.labels[row];
   if (label == a.ignore) a.loss[row] = 0.0f;
   else if (label < 0 || label >= a.vocabulary) a.loss[row] = __builtin_nanf("");
-  else a.loss[row] = lse - a.label_logit[row];
+  else a.loss[row] = ((top - a.label_logit[row]) + rest) * kLn2;  // not by the log-sum-exp, whose rounding is that of a logit
 }
 
 __global__ void __launch_bounds__(1024) probability_unit(const float* scales, int32_t n, float* unit) {

@@ -62,7 +62,7 @@ struct Finish {
   const int64_t* labels;
   int64_t ignore;
   float2* stats;            // [rows][chunks]: largest logit and sum of exponentials, base 2
-  float* label_logit;       // [rows]
+  float* label_logit;       // [rows], base 2
   const float* lse;
   const float* dloss;
   const float* prob_unit;   // [1]: 2^E that brings p * scale into binary16's range
@@ -565,7 +565,13 @@ __device__ __forceinline__ void finish_layer(const Finish& f, const Columns<NC>&
   }
   if constexpr (NC == 16) {
     if (f.kind == kStats) {
-      // the label's logit, and the chunk's largest logit and sum of exponentials
+      // base 2: the label's logit, and the chunk's largest logit and sum of exponentials
+      float top = -__builtin_inff();
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        v[i] = i < valid ? v[i] * kLog2E : -__builtin_inff();
+        top = fmaxf(top, v[i]);
+      }
       if (live) {
         const int32_t at = shared.label - col;
         if (at >= 0 && at < valid) {
@@ -573,12 +579,6 @@ __device__ __forceinline__ void finish_layer(const Finish& f, const Columns<NC>&
           for (int i = 0; i < NC; ++i)
             if (at == i) f.label_logit[row] = v[i];
         }
-      }
-      float top = -__builtin_inff();
-#pragma unroll
-      for (int i = 0; i < NC; ++i) {
-        v[i] = i < valid ? v[i] * kLog2E : -__builtin_inff();
-        top = fmaxf(top, v[i]);
       }
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));

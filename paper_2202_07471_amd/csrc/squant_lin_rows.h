@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(kRowThreads) join(JoinArgs a) {
 struct LossArgs {
   const float2* stats;
   int32_t chunks;
-  const float* label_logit;
+  const float* label_logit;  // base 2
   const int64_t* labels;
   int64_t ignore;
   int32_t vocabulary;

@@ -271,3 +271,32 @@ def test_gradient_where_the_label_is_likely_in_pieces(sq, dtype, first_label):
     _, lse = sq.squant_cross_entropy(hg, c.cuda(), scales.cuda(), lg)
     got = sq.squant_cross_entropy_backward(hg, c.cuda(), scales.cuda(), lg, lse, gg).cpu().double().view(times, 60, 64)
     assert ((got - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("t,d,v", [(7, 256, 2000), (50, 130, 517), (130, 256, 2049), (300, 512, 5000)])
+def test_losses_of_likely_labels(sq, t, d, v, dtype):
+    h, c, scales, labels, dloss = likely_label_case(t, d, v, dtype)
+    labels[t // 2:] = ((h.double() @ (c.double() * scales.double()[:, None]).t()).argmax(1))[t // 2:]
+    w, logits, lse, loss, p, y, g, _ = definition(h, c, scales, labels, dloss)
+    others = p.scatter(1, y[:, None], 0.0)
+    loss = -torch.log1p(-others.sum(1))
+    got, _ = sq.squant_cross_entropy(h.cuda(), c.cuda(), scales.cuda(), labels.cuda())
+    got = got.cpu().double()
+    assert (got >= 0).all(), f"{(got < 0).sum().item()} of {t}"
+    # a logit's error counts with 1 - p; a sum of at most 30 terms in a row from 1 on is off by 2^-24 for each
+    e = sum_error(((h.double() ** 2) @ (w.t() ** 2)).sqrt(), d) + 2.0 ** -22 * logits.abs()
+    tol = (others * (e + e.gather(1, y[:, None]))).sum(1) + 30 * 2.0 ** -24 + 2.0 ** -21 * loss
+    assert ((got - loss).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("t", [20, 130])
+def test_losses_of_certain_labels_are_not_below_zero(sq, t, dtype):
+    """Rows so long that the label takes all: the loss is 0 or next to it, and on the right side."""
+    h, c, scales, labels, _ = likely_label_case(t, 256, 2049, dtype)
+    size = torch.linspace(1, 6, t)[:, None]
+    h = (h.float() * size).to(dtype)
+    labels = (h.double() @ (c.double() * scales.double()[:, None]).t()).argmax(1)
+    loss, _ = sq.squant_cross_entropy(h.cuda(), c.cuda(), scales.cuda(), labels.cuda())
+    assert (loss >= 0).all(), f"{(loss < 0).sum().item()} of {t}, least {loss.min().item()}"
