@@ -211,10 +211,11 @@ int64_t squant_max_channel_elems(int32_t kh, int32_t kw);
  * activation buffers of a call (x, bias, residual, y, dy, dx, dbias).  Codes times activations are
  * multiplied exactly (binary32 activations to 22 bits) and added in binary32; the outputs of a forward
  * call are rounded once.  dx and dh are rounded twice: what is multiplied by the codes is held in 11 bits
- * (binary32: 22), which for binary16 is as much again as the output's own rounding.  Rows may be any distance apart (ld*, in elements, at least the row's length); activation
- * buffers need the alignment of their element type, codes none.  Where codes or rows do not lie as the
- * matrix units' kernels read them (cin a multiple of 64, 16-byte aligned; few rows: anything goes) a call
- * copies them to its workspace first.
+ * (binary32: 22), which for binary16 is as much again as the output's own rounding.  Rows may be any
+ * distance apart (ld*, in elements, at least the row's length); activation buffers need the alignment of
+ * their element type, codes none.  Where codes or rows do not lie as the matrix units' kernels read them
+ * (cin a multiple of 64, 16-byte aligned; few rows: anything goes) a call copies them to its workspace
+ * first.
  *
  * d_workspace: the *_workspace_bytes call's amount (which depends on the shapes, on ldx or ldh and on
  * whether x or h and the codes are 16-byte aligned; 0 for many calls, NULL then), 256-byte aligned, not
