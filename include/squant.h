@@ -300,6 +300,107 @@ int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t t
                                   void* d_dh, int64_t lddh, void* d_workspace, size_t workspace_bytes,
                                   void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Attention, and a cache of keys and values in 4 or 8 bits: what a language model of quantised layers has between
+ * its projections.
+ *
+ * Element type (squant_wtype_t): that of queries, keys, values, outputs and gradients of a call.  Products are taken
+ * of the elements as they are (binary32: in binary32) and added in binary32, softmax statistics are binary32.  What is
+ * multiplied by the values (and, in a backward pass, by queries, keys and output gradients) is rounded to the
+ * element type first (binary32: not; attention over a cache: to 11 bits, binary32 to 22, or to 2^-39 of the row's
+ * largest weight where that is more).  Every output is rounded once.
+ *
+ * Rows are tokens.  Sequences lie one after the other: sequence b has the rows starts[b] to starts[b + 1] - 1, starts
+ * holding sequences + 1 numbers that begin with 0 and do not fall; sequences may be empty.  Rows from
+ * starts[sequences] on belong to no sequence (padding): what is computed for them is 0, nothing is written to a cache for
+ * them, and what they hold does not matter.  A row that sees no key gets 0 (and a log-sum-exp of minus infinity); keys and
+ * values that a row does not see do not reach its output, whatever they hold.  starts, lengths and tables are read on the
+ * device; numbers there that break the rules give unspecified values, never an access out of the buffers.
+ *
+ * Query heads share key heads in groups: heads is a multiple of the key heads, query head h goes with key head
+ * h / (heads / key heads).  No atomics: results are the same from run to run.  The calls launch kernels only and may be
+ * captured into a HIP graph.  rows = 0 is a no-op unless said otherwise.  Workspaces as for the calls above. */
+
+/* [rows][heads][head_dim] elements; a head's elements lie beside each other. */
+typedef struct {
+  void* data;      /* device, aligned to its element type */
+  int64_t row;     /* elements between rows, */
+  int64_t head;    /* and between heads: multiples of nothing, at least head_dim */
+} squant_heads_t;
+
+/* A paged cache of keys and values.  Codes [pages][heads][page_size][head_dim], int8 (SQUANT_OUT_INT8) or two 4-bit
+ * codes a byte (SQUANT_OUT_INT4, as squant_output_t has them); each 32 consecutive elements of a head share a scale,
+ * [pages][heads][page_size][head_dim / 32] bfloat16:
+ *   scale = max|x| / qmax in binary32, rounded to bfloat16 (qmax = 7 or 127),
+ *   code  = round-half-even(x / scale), at most qmax in magnitude; 0 where the scale is 0.
+ * A NaN or an infinity among the 32 makes the scale NaN and the codes 0.  The value held is code * scale.
+ * head_dim is 32, 64, 96, 128, 192 or 256; codes are aligned to 16 bytes; pages * heads * page_size < 2^31. */
+typedef struct {
+  void* key_codes;    /* all: device */
+  void* key_scales;
+  void* value_codes;
+  void* value_scales;
+  int32_t pages, page_size, heads, head_dim;
+  squant_output_t format;
+} squant_cache_t;
+
+/* Where sequences lie in a cache, and which of their tokens a call is about.  Token t of sequence b is in slot
+ * t % page_size of page table[b][t / page_size].  lengths[b] tokens of it count, the call's own among them: row r of
+ * sequence b is token lengths[b] - (starts[b + 1] - r), the rows being its last ones.  starts NULL: one row for each
+ * sequence.  A table's entry that is no page, or lengths beyond the table: nothing is written there, and NaN is read. */
+typedef struct {
+  const int32_t* table;   /* device, [sequences][table_width] */
+  const int32_t* lengths; /* device, [sequences] */
+  const int32_t* starts;  /* device, [sequences + 1], or NULL */
+  int32_t sequences, table_width;
+} squant_paged_t;
+
+/* Quantises keys and values of `rows` tokens, [rows][heads][head_dim], into their slots; other slots stay as they are.
+ * A slot that two rows name (a page in two places of the table) holds a mixture of them afterwards. */
+int squant_cache_write(const squant_heads_t* h_k, const squant_heads_t* h_v, squant_wtype_t type, int64_t rows,
+                       const squant_cache_t* h_cache, const squant_paged_t* h_where, void* stream);
+
+/* The values of these tokens' keys and values, code * scale rounded to the element type.  Rows of no sequence, and tokens
+ * before the first, are written as 0. */
+int squant_cache_read(const squant_cache_t* h_cache, const squant_paged_t* h_where, squant_wtype_t type, int64_t rows,
+                      const squant_heads_t* h_k, const squant_heads_t* h_v, void* stream);
+
+/* out[r][h] = sum_t p[t] value[t],  p = softmax over t of scale * q[r][h] . key[t],  t the tokens up to the row's own
+ * (which are in the cache already).  scale is finite and not negative.  For one or a few rows a sequence: 16 or 32 rows
+ * times grouped heads share a pass over the cache. */
+size_t squant_cache_attention_workspace_bytes(int64_t rows, int32_t heads, const squant_cache_t* h_cache,
+                                              const squant_paged_t* h_where);
+int squant_cache_attention(const squant_heads_t* h_q, squant_wtype_t type, int64_t rows, int32_t heads,
+                           const squant_cache_t* h_cache, const squant_paged_t* h_where, float scale,
+                           const squant_heads_t* h_out, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* Whole prompts: queries [q_rows][heads][head_dim] against keys and values [k_rows][kv_heads][head_dim].
+ * causal: the last row of a sequence sees all of its keys, the row before it one less, and so on. */
+typedef struct {
+  const int32_t* q_starts; /* device, [sequences + 1], or NULL: one sequence of all rows */
+  const int32_t* k_starts; /* the same for keys; both or neither */
+  int32_t sequences;
+  int64_t q_rows, k_rows;
+  int32_t heads, kv_heads, head_dim; /* head_dim a multiple of 8 up to 256 */
+  int32_t causal;
+  float scale;             /* finite, not negative */
+} squant_packed_t;
+
+/* out[r][h] = sum_t p[t] v[t],  lse[h][r] = log sum_t exp(scale * q[r][h] . k[t])  (binary32 [heads][q_rows]; may be NULL). */
+int squant_attention(const squant_heads_t* h_q, const squant_heads_t* h_k, const squant_heads_t* h_v, squant_wtype_t type,
+                     const squant_packed_t* h_packed, const squant_heads_t* h_out, float* d_lse, void* stream);
+
+/* Gradients of squant_attention for the output's gradient (lse's own is not taken): with p = exp(scale * q . k - lse),
+ * dv = sum p dout,  ds = p (dout . v - dout . out),  dq = scale * sum ds k,  dk = scale * sum ds q, the latter two sums
+ * over the query heads of a group as well.  Rows of no sequence get 0.  A NaN or an infinity in a position that a row
+ * does not see may make gradients of up to 128 rows beside it NaN.  rows = 0: keys without queries get 0. */
+size_t squant_attention_backward_workspace_bytes(const squant_packed_t* h_packed);
+int squant_attention_backward(const squant_heads_t* h_dout, const squant_heads_t* h_q, const squant_heads_t* h_k,
+                              const squant_heads_t* h_v, const squant_heads_t* h_out, const float* d_lse,
+                              squant_wtype_t type, const squant_packed_t* h_packed, const squant_heads_t* h_dq,
+                              const squant_heads_t* h_dk, const squant_heads_t* h_dv, void* d_workspace,
+                              size_t workspace_bytes, void* stream);
+
 const char* squant_status_string(int status);
 int squant_version(void);
 

@@ -1,0 +1,347 @@
+"""Attention and a cache of keys and values in 4 or 8 bits: ctypes marshalling of the calls, and attention's torch
+autograd form.
+
+Queries, keys, values and outputs are [rows, heads, head_dim] in float32, float16 or bfloat16, a row for each token; sequences lie
+one after the other, and ``starts`` (int32, on the device, one more than sequences, from 0) says where each begins.  Heads
+and rows may be any distance apart (slices of a projection's output), a head's elements are contiguous.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import NamedTuple, Optional, Tuple
+
+import torch
+
+from .binding import OUT_INT4, OUT_INT8, _check, _WTYPES, lib
+from .linear import _current_stream, _device, _workspace
+
+_SCALE_GROUP = 32  # elements of a head that share a scale in the cache
+
+
+class squant_heads_t(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class squant_cache_t(ctypes.Structure):
+    _fields_ = [("key_codes", ctypes.c_void_p), ("key_scales", ctypes.c_void_p), ("value_codes", ctypes.c_void_p),
+                ("value_scales", ctypes.c_void_p), ("pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("format", ctypes.c_int)]
+
+
+class squant_paged_t(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("starts", ctypes.c_void_p),
+                ("sequences", ctypes.c_int32), ("table_width", ctypes.c_int32)]
+
+
+class squant_packed_t(ctypes.Structure):
+    _fields_ = [("q_starts", ctypes.c_void_p), ("k_starts", ctypes.c_void_p), ("sequences", ctypes.c_int32),
+                ("q_rows", ctypes.c_int64), ("k_rows", ctypes.c_int64), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+_ready = None
+
+
+def _lib():
+    global _ready
+    if _ready is None:
+        L = lib()
+        i64, i32, vp, sz, en, fl = ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_float
+        hp, cp = ctypes.POINTER(squant_heads_t), ctypes.POINTER(squant_cache_t)
+        wp, pp = ctypes.POINTER(squant_paged_t), ctypes.POINTER(squant_packed_t)
+        L.squant_cache_write.argtypes = [hp, hp, en, i64, cp, wp, vp]
+        L.squant_cache_read.argtypes = [cp, wp, en, i64, hp, hp, vp]
+        L.squant_cache_attention_workspace_bytes.argtypes = [i64, i32, cp, wp]
+        L.squant_cache_attention.argtypes = [hp, en, i64, i32, cp, wp, fl, hp, vp, sz, vp]
+        L.squant_attention.argtypes = [hp, hp, hp, en, pp, hp, vp, vp]
+        L.squant_attention_backward_workspace_bytes.argtypes = [pp]
+        L.squant_attention_backward.argtypes = [hp, hp, hp, hp, hp, vp, en, pp, hp, hp, hp, vp, sz, vp]
+        for f in ("cache_write", "cache_read", "cache_attention", "attention", "attention_backward"):
+            getattr(L, f"squant_{f}").restype = en
+        L.squant_cache_attention_workspace_bytes.restype = sz
+        L.squant_attention_backward_workspace_bytes.restype = sz
+        _ready = L
+    return _ready
+
+
+class QuantizedCache(NamedTuple):
+    """Keys and values of 4-bit (uint8, two codes a byte) or 8-bit (int8) codes [pages, heads, page_size, head_dim or half of
+    it], with a bfloat16 scale [pages, heads, page_size, head_dim / 32] for each 32 of a head's elements."""
+    key_codes: torch.Tensor
+    key_scales: torch.Tensor
+    value_codes: torch.Tensor
+    value_scales: torch.Tensor
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, page_size: int, head_dim: int, format: int = OUT_INT4, device="cuda") -> "QuantizedCache":
+        """A cache whose slots hold nothing yet."""
+        if format not in (OUT_INT4, OUT_INT8):
+            raise ValueError("format must be OUT_INT4 or OUT_INT8")
+        if head_dim not in (32, 64, 96, 128, 192, 256):
+            raise ValueError("head_dim must be 32, 64, 96, 128, 192 or 256")
+        shape = (pages, heads, page_size)
+
+        def one():
+            if format == OUT_INT4:
+                codes = torch.empty(shape + (head_dim // 2,), dtype=torch.uint8, device=device)
+            else:
+                codes = torch.empty(shape + (head_dim,), dtype=torch.int8, device=device)
+            return codes, torch.empty(shape + (head_dim // _SCALE_GROUP,), dtype=torch.bfloat16, device=device)
+        return cls(*one(), *one())
+
+
+def _cache(cache: QuantizedCache, device: int) -> squant_cache_t:
+    kc, ks, vc, vs = cache
+    shape = kc.shape
+    if kc.dtype is torch.uint8:
+        fmt, dim = OUT_INT4, 2 * shape[-1] if len(shape) == 4 else 0
+    elif kc.dtype is torch.int8:
+        fmt, dim = OUT_INT8, shape[-1] if len(shape) == 4 else 0
+    else:
+        raise ValueError("a cache's codes must be int8, or uint8 with two 4-bit codes a byte")
+    if dim not in (32, 64, 96, 128, 192, 256):
+        raise ValueError("a cache's codes must be [pages, heads, page_size, bytes] of heads of 32, 64, 96, 128, 192 or 256 elements")
+    scales = shape[:3] + (dim // _SCALE_GROUP,)
+    if (vc.dtype is not kc.dtype or vc.shape != shape or ks.shape != scales or vs.shape != scales
+            or ks.dtype is not torch.bfloat16 or vs.dtype is not torch.bfloat16):
+        raise ValueError("a cache's values must be like its keys, its scales bfloat16 with one for each 32 elements")
+    for t in cache:
+        if not t.is_contiguous() or t.get_device() != device:
+            raise ValueError("a cache's tensors must be contiguous and on the activations' device")
+    return squant_cache_t(kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr(), shape[0], shape[2], shape[1], dim, fmt)
+
+
+def _ints(t: torch.Tensor, count: Optional[int], what: str, device: int) -> int:
+    if (t.dtype is not torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.get_device() != device
+            or (t.shape[0] < 1 if count is None else t.shape[0] != count)):
+        raise ValueError(f"{what} must be a contiguous int32 tensor on the activations' device"
+                         + (f" of {count} elements" if count is not None else ""))
+    return t.data_ptr()
+
+
+def _paged(table: torch.Tensor, lengths: torch.Tensor, starts: Optional[torch.Tensor], rows: int, device: int) -> squant_paged_t:
+    if table.dtype is not torch.int32 or table.dim() != 2 or not table.is_contiguous() or table.get_device() != device:
+        raise ValueError("table must be a contiguous int32 tensor [sequences, pages of each] on the activations' device")
+    sequences, width = table.shape
+    _ints(lengths, sequences, "lengths", device)
+    if starts is not None:
+        _ints(starts, sequences + 1, "starts", device)
+    elif rows != sequences:
+        raise ValueError("without starts there must be one row for each sequence")
+    return squant_paged_t(table.data_ptr(), lengths.data_ptr(), None if starts is None else starts.data_ptr(), sequences, width)
+
+
+def _heads(t: torch.Tensor, heads: Optional[int], dim: Optional[int], what: str, device: int, like: Optional[torch.Tensor] = None,
+           rows: Optional[int] = None) -> squant_heads_t:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or (heads is not None and shape[1] != heads) or (dim is not None and shape[2] != dim) or (
+            rows is not None and shape[0] != rows):
+        raise ValueError(f"{what} must be [{'rows' if rows is None else rows}, {'heads' if heads is None else heads}, "
+                         f"{'head_dim' if dim is None else dim}]")
+    if t.get_device() != device or (like is not None and t.dtype is not like.dtype):
+        raise ValueError(f"{what} must have the type and the device of the other activations")
+    if (shape[2] > 1 and stride[2] != 1) or (shape[1] > 1 and stride[1] < shape[2]) or (shape[0] > 1 and stride[0] < shape[2]):
+        raise ValueError(f"{what} must have contiguous heads that do not overlap")
+    return squant_heads_t(t.data_ptr(), stride[0], stride[1])
+
+
+def _result(t: torch.Tensor, like: torch.Tensor, heads: int, dim: int, what: str, device: int, rows: int) -> squant_heads_t:
+    h = _heads(t, heads, dim, what, device, like, rows)
+    if rows > 1 and heads > 1 and abs(t.stride(0)) < (heads - 1) * t.stride(1) + dim and t.stride(1) < (rows - 1) * t.stride(0) + dim:
+        raise ValueError(f"rows and heads of {what} overlap")
+    return h
+
+
+_ref = ctypes.byref
+
+
+def squant_cache_write(k: torch.Tensor, v: torch.Tensor, cache: QuantizedCache, table: torch.Tensor, lengths: torch.Tensor,
+                       starts: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Quantises new tokens' keys and values [rows, heads, head_dim] into their slots of the cache.
+
+    Token t of sequence b is in slot t % page_size of page table[b, t // page_size]; the rows starts[b] to
+    starts[b + 1] - 1 are the last of lengths[b] tokens (the lengths count them).  Without starts, one row for each sequence.
+    Rows behind the last sequence, and tokens whose page is none, are written nowhere."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return squant_cache_write(k, v, cache, table, lengths, starts)
+    device = _device(k, "k")
+    c = _cache(cache, device)
+    rows = k.shape[0] if k.dim() else 0
+    hk = _heads(k, c.heads, c.head_dim, "k", device)
+    hv = _heads(v, c.heads, c.head_dim, "v", device, k, rows)
+    w = _paged(table, lengths, starts, rows, device)
+    _check(_lib().squant_cache_write(_ref(hk), _ref(hv), _WTYPES[k.dtype], rows, _ref(c), _ref(w), _current_stream(device)))
+
+
+def squant_cache_read(cache: QuantizedCache, table: torch.Tensor, lengths: torch.Tensor, starts: Optional[torch.Tensor], rows: int,
+                      dtype: torch.dtype, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
+                      stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(keys, values) [rows, heads, head_dim] that the cache holds for the last tokens of each sequence, placed as in
+    squant_cache_write; rows behind the last sequence are 0, tokens whose page is none NaN."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return squant_cache_read(cache, table, lengths, starts, rows, dtype, k, v)
+    device = _device(cache.key_scales, "cache")
+    if dtype not in _WTYPES:
+        raise ValueError("dtype must be float32, float16 or bfloat16")
+    c = _cache(cache, device)
+    if rows < 0:
+        raise ValueError("rows must not be negative")
+    shape = (rows, c.heads, c.head_dim)
+    if k is None:
+        k = torch.empty(shape, dtype=dtype, device=cache.key_scales.device)
+    if v is None:
+        v = torch.empty(shape, dtype=dtype, device=cache.key_scales.device)
+    if k.dtype is not dtype:
+        raise ValueError("k must have the type asked for")
+    hk = _result(k, k, c.heads, c.head_dim, "k", device, rows)
+    hv = _result(v, k, c.heads, c.head_dim, "v", device, rows)
+    w = _paged(table, lengths, starts, rows, device)
+    _check(_lib().squant_cache_read(_ref(c), _ref(w), _WTYPES[dtype], rows, _ref(hk), _ref(hv), _current_stream(device)))
+    return k, v
+
+
+def squant_cache_attention(q: torch.Tensor, cache: QuantizedCache, table: torch.Tensor, lengths: torch.Tensor,
+                           starts: Optional[torch.Tensor] = None, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                           stream=None) -> torch.Tensor:
+    """Attention of new tokens' queries [rows, heads, head_dim] over the cache, which holds their keys and values already;
+    rows are placed as in squant_cache_write, and each sees the tokens up to its own.
+
+    heads is a multiple of the cache's; scale defaults to head_dim ** -0.5.  For one or a few new tokens of each sequence; a whole
+    prompt is squant_attention's.  Rows that see nothing are 0, rows behind the last sequence too."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return squant_cache_attention(q, cache, table, lengths, starts, scale, out)
+    device = _device(q, "q")
+    c = _cache(cache, device)
+    hq = _heads(q, None, c.head_dim, "q", device)
+    rows, heads = q.shape[0], q.shape[1]
+    if heads % c.heads or heads == 0:
+        raise ValueError("q must have a multiple of the cache's heads")
+    w = _paged(table, lengths, starts, rows, device)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    ho = _result(out, q, heads, c.head_dim, "out", device, rows)
+    nbytes = _lib().squant_cache_attention_workspace_bytes(rows, heads, _ref(c), _ref(w))
+    ws = _workspace(q, nbytes)
+    _check(_lib().squant_cache_attention(_ref(hq), _WTYPES[q.dtype], rows, heads, _ref(c), _ref(w),
+                                         c.head_dim ** -0.5 if scale is None else scale, _ref(ho),
+                                         None if ws is None else ws.data_ptr(), nbytes, _current_stream(device)))
+    return out
+
+
+def _packed(q: torch.Tensor, k: torch.Tensor, starts, k_starts, scale, causal, device: int) -> squant_packed_t:
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q, k and v must be [rows, heads, head_dim]")
+    heads, dim, kv_heads = q.shape[1], q.shape[2], k.shape[1]
+    if dim == 0 or dim % 8 or dim > 256:
+        raise ValueError("head_dim must be a multiple of 8 up to 256")
+    if kv_heads == 0 or heads == 0 or heads % kv_heads:
+        raise ValueError("q must have a multiple of the heads of k")
+    if starts is None:
+        if k_starts is not None:
+            raise ValueError("k_starts without starts")
+        qs = ks = None
+        sequences = 1
+    else:
+        qs = _ints(starts, None, "starts", device)
+        sequences = starts.shape[0] - 1
+        if k_starts is None and k.shape[0] != q.shape[0]:
+            raise ValueError("without k_starts there must be as many keys as queries")
+        ks = qs if k_starts is None else _ints(k_starts, sequences + 1, "k_starts", device)
+    scale = dim ** -0.5 if scale is None else float(scale)
+    if not (0 <= scale < math.inf):
+        raise ValueError("scale must be finite and not negative")
+    return squant_packed_t(qs, ks, sequences, q.shape[0], k.shape[0], heads, kv_heads, dim, bool(causal), scale)
+
+
+def squant_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None,
+                     k_starts: Optional[torch.Tensor] = None, scale: Optional[float] = None, causal: bool = True,
+                     out: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(out, lse) of attention over whole prompts: q [q_rows, heads, head_dim], k and v [k_rows, kv_heads, head_dim].
+
+    Query head h goes with key head h // (heads / kv_heads).  starts are the sequences' first rows of q (and of k, unless
+    k_starts says otherwise), None: one sequence.  causal: a sequence's last row sees all of its keys, the row before it one
+    less, and so on.  lse [heads, q_rows] is the float32 log-sum-exp of each row's scores.  Rows that see no key are 0."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return squant_attention(q, k, v, starts, k_starts, scale, causal, out)
+    device = _device(q, "q")
+    p = _packed(q, k, starts, k_starts, scale, causal, device)
+    hq = _heads(q, None, None, "q", device)
+    hk = _heads(k, p.kv_heads, p.head_dim, "k", device, q)
+    hv = _heads(v, p.kv_heads, p.head_dim, "v", device, q, p.k_rows)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    ho = _result(out, q, p.heads, p.head_dim, "out", device, p.q_rows)
+    lse = torch.empty((p.heads, p.q_rows), dtype=torch.float32, device=q.device)
+    _check(_lib().squant_attention(_ref(hq), _ref(hk), _ref(hv), _WTYPES[q.dtype], _ref(p), _ref(ho), lse.data_ptr(),
+                                   _current_stream(device)))
+    return out, lse
+
+
+def squant_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                              lse: torch.Tensor, starts: Optional[torch.Tensor] = None, k_starts: Optional[torch.Tensor] = None,
+                              scale: Optional[float] = None, causal: bool = True, dq: Optional[torch.Tensor] = None,
+                              dk: Optional[torch.Tensor] = None, dv: Optional[torch.Tensor] = None,
+                              stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """(dq, dk, dv) of squant_attention for the gradient dout of its output; out and lse are what it returned."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return squant_attention_backward(dout, q, k, v, out, lse, starts, k_starts, scale, causal, dq, dk, dv)
+    device = _device(q, "q")
+    p = _packed(q, k, starts, k_starts, scale, causal, device)
+    h, kv, dim = p.heads, p.kv_heads, p.head_dim
+    hq = _heads(q, None, None, "q", device)
+    hk = _heads(k, kv, dim, "k", device, q)
+    hv = _heads(v, kv, dim, "v", device, q, p.k_rows)
+    ho = _heads(out, h, dim, "out", device, q, p.q_rows)
+    hd = _heads(dout, h, dim, "dout", device, q, p.q_rows)
+    if lse.dtype is not torch.float32 or lse.shape != (h, p.q_rows) or not lse.is_contiguous() or lse.get_device() != device:
+        raise ValueError("lse must be what squant_attention returned for these rows")
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
+    dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dk is None else dk
+    dv = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dv is None else dv
+    gq = _result(dq, q, h, dim, "dq", device, p.q_rows)
+    gk = _result(dk, q, kv, dim, "dk", device, p.k_rows)
+    gv = _result(dv, q, kv, dim, "dv", device, p.k_rows)
+    nbytes = _lib().squant_attention_backward_workspace_bytes(_ref(p))
+    ws = _workspace(q, nbytes)
+    _check(_lib().squant_attention_backward(_ref(hd), _ref(hq), _ref(hk), _ref(hv), _ref(ho), lse.data_ptr(), _WTYPES[q.dtype],
+                                            _ref(p), _ref(gq), _ref(gk), _ref(gv), None if ws is None else ws.data_ptr(), nbytes,
+                                            _current_stream(device)))
+    return dq, dk, dv
+
+
+def _headwise(t: torch.Tensor) -> torch.Tensor:
+    """t itself where the calls take it, else a contiguous copy (expanded gradients, transposed views)."""
+    stride, shape = t.stride(), t.shape
+    if len(shape) == 3 and stride[2] == 1 and stride[1] >= shape[2] and stride[0] >= shape[2]:
+        return t
+    return t.contiguous()
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, starts, k_starts, scale, causal):
+        q, k, v = _headwise(q), _headwise(k), _headwise(v)
+        out, lse = squant_attention(q, k, v, starts, k_starts, scale, causal)
+        ctx.scale, ctx.causal = scale, causal
+        ctx.save_for_backward(q, k, v, out, lse, starts, k_starts)
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        q, k, v, out, lse, starts, k_starts = ctx.saved_tensors
+        dq, dk, dv = squant_attention_backward(_headwise(dout), q, k, v, out, lse, starts, k_starts, ctx.scale, ctx.causal)
+        need = ctx.needs_input_grad
+        return dq if need[0] else None, dk if need[1] else None, dv if need[2] else None, None, None, None, None
+
+
+def packed_attention(q, k, v, starts=None, k_starts=None, scale: Optional[float] = None, causal: bool = True) -> torch.Tensor:
+    """squant_attention's output with gradients for q, k and v."""
+    return _Attention.apply(q, k, v, starts, k_starts, scale, causal)

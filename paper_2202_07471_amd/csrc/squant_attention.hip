@@ -1,0 +1,276 @@
+// Host side of attention and of the quantised cache: argument checks, how far a sequence is split, launches.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "squant.h"
+
+#include "squant_cache_attention.h"
+#include "squant_prompt.h"
+
+namespace {
+
+using namespace squant;
+using namespace squant::att;
+
+constexpr int64_t kMost = 0x7fffffffLL;
+
+int element_bytes(int type) { return type == SQUANT_W_F32 ? 4 : 2; }
+bool misaligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
+int check_type(int type) { return type < SQUANT_W_F32 || type > SQUANT_W_BF16 ? SQUANT_ERR_FORMAT : SQUANT_OK; }
+
+// [rows][heads][dim] whose data is there, aligned and without heads or rows of negative or overlapping steps.
+int check_heads(const squant_heads_t* h, int64_t rows, int32_t heads, int32_t dim, int type) {
+  if (!h || !h->data) return SQUANT_ERR_NULL;
+  if (misaligned(h->data, element_bytes(type))) return SQUANT_ERR_FORMAT;
+  constexpr int64_t far = (int64_t)1 << 40;  // rows times this stays within 64 bits with what is allowed for rows
+  if ((heads > 1 && (h->head < dim || h->head > far)) || (rows > 1 && (h->row < dim || h->row > far))) return SQUANT_ERR_SHAPE;
+  if (rows > 1 && rows * (double)h->row > 4e18) return SQUANT_ERR_SHAPE;
+  return SQUANT_OK;
+}
+Strided strided(const squant_heads_t* h) { return Strided{(char*)h->data, h->row, h->head}; }
+
+int check_cache(const squant_cache_t* c) {
+  if (!c || !c->key_codes || !c->key_scales || !c->value_codes || !c->value_scales) return SQUANT_ERR_NULL;
+  if (c->format != SQUANT_OUT_INT8 && c->format != SQUANT_OUT_INT4) return SQUANT_ERR_FORMAT;
+  if (misaligned(c->key_codes, 16) || misaligned(c->value_codes, 16) || misaligned(c->key_scales, 2) || misaligned(c->value_scales, 2))
+    return SQUANT_ERR_FORMAT;
+  if (c->pages <= 0 || c->page_size <= 0 || c->heads <= 0) return SQUANT_ERR_SHAPE;
+  if ((double)c->pages * c->page_size * c->heads > (double)kMost) return SQUANT_ERR_SHAPE;
+  const int32_t d = c->head_dim;
+  return d == 32 || d == 64 || d == 96 || d == 128 || d == 192 || d == 256 ? SQUANT_OK : SQUANT_ERR_SHAPE;
+}
+
+int check_paged(const squant_paged_t* w, int64_t rows) {
+  if (!w) return SQUANT_ERR_NULL;
+  if (rows < 0 || rows > kMost || w->sequences < 0 || w->table_width < 0) return SQUANT_ERR_SHAPE;
+  if (!w->starts && rows != w->sequences) return SQUANT_ERR_SHAPE;
+  if (misaligned(w->table, 4) || misaligned(w->lengths, 4) || misaligned(w->starts, 4)) return SQUANT_ERR_FORMAT;
+  return w->sequences && (!w->lengths || (w->table_width && !w->table)) ? SQUANT_ERR_NULL : SQUANT_OK;
+}
+
+Cache cache_of(const squant_cache_t& c, const squant_paged_t& w) {
+  Cache o{};
+  o.codes[0] = (uint8_t*)c.key_codes, o.codes[1] = (uint8_t*)c.value_codes;
+  o.scales[0] = (uint16_t*)c.key_scales, o.scales[1] = (uint16_t*)c.value_scales;
+  o.pages = c.pages, o.page_size = c.page_size, o.heads = c.heads, o.dim = c.head_dim;
+  int l = 0;
+  while (((int64_t)1 << l) < c.page_size) ++l;
+  o.shift = l - 1;
+  o.magic = l ? (uint32_t)((((uint64_t)1 << (31 + l)) / (uint32_t)c.page_size) + 1) : 0;
+  o.table = w.table, o.table_width = w.table_width, o.lengths = w.lengths;
+  return o;
+}
+Packed packed_of(const squant_paged_t& w, int64_t rows) { return Packed{w.starts, w.sequences, (int32_t)rows, !w.starts}; }
+
+bool fits(int64_t groups, int64_t gy = 1) { return groups > 0 && groups * kThreads <= 0xffffffffLL && gy <= 0xffff; }
+
+template <class A> int launch(void (*k)(A), int64_t gx, int64_t gy, size_t lds, hipStream_t st, const A& a) {
+  if (!fits(gx, gy)) return SQUANT_ERR_SHAPE;
+  // kernels that ask for more LDS than a workgroup gets by default say so: the attribute is the kernel's, not a call's
+  if (lds > 64 * 1024 &&
+      hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
+    (void)hipGetLastError();
+    return SQUANT_ERR_DEVICE;
+  }
+  hipLaunchKernelGGL(k, dim3((unsigned)gx, (unsigned)gy), dim3(kThreads), (unsigned)lds, st, a);
+  return hipGetLastError() == hipSuccess ? SQUANT_OK : SQUANT_ERR_DEVICE;
+}
+
+int cache_rows(bool write, const squant_heads_t* k, const squant_heads_t* v, int type, int64_t rows, const squant_cache_t* c,
+               const squant_paged_t* w, void* stream) {
+  if (int rc = check_type(type)) return rc;
+  if (int rc = check_cache(c)) return rc;
+  if (int rc = check_paged(w, rows)) return rc;
+  if (rows == 0) return SQUANT_OK;
+  if (int rc = check_heads(k, rows, c->heads, c->head_dim, type)) return rc;
+  if (int rc = check_heads(v, rows, c->heads, c->head_dim, type)) return rc;
+  CacheRowsArgs a{};
+  a.cache = cache_of(*c, *w);
+  a.rows = packed_of(*w, rows);
+  a.x[0] = strided(k), a.x[1] = strided(v);
+  const int64_t pieces = (int64_t)2 * c->heads * (c->head_dim / 8);
+  if (pieces > 1 << 20) return SQUANT_ERR_SHAPE;
+  a.pieces = (int32_t)pieces, a.dim_pieces = c->head_dim / 8;
+  a.piece_magic = (uint32_t)((((uint64_t)1 << 32) / (uint64_t)pieces) + 1);
+  a.rows_each = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kMostRows, kThreads / pieces));
+  const int64_t groups = (rows + a.rows_each - 1) / a.rows_each;
+  return launch(write ? cache_write_kernel(type, (int)c->format) : cache_read_kernel(type, (int)c->format), groups, 1, 0, (hipStream_t)stream, a);
+}
+
+// How attention over a cache is cut: 16 or 32 rows (tokens times grouped heads) a workgroup, and stretches of the sequences,
+// whose lengths the host does not know, so that their capacity gives about kGroups workgroups.
+struct CacheSplit {
+  int rt;
+  int64_t tiles;
+  int64_t splits, chunk;
+  size_t stats_bytes, bytes;
+};
+constexpr int64_t kGroups = 2048, kLeastChunk = 256, kMostChunk = 8192;
+
+bool split_cache(int64_t rows, int32_t heads, const squant_cache_t& c, const squant_paged_t& w, CacheSplit& s) {
+  const int group = heads / c.heads;
+  const int64_t each = w.sequences ? (rows + w.sequences - 1) / w.sequences : 0;
+  s.rt = each * group > 16 && c.head_dim <= 128 ? 2 : 1;
+  const int tile = 16 * s.rt;
+  s.tiles = w.starts ? tiles_bound(rows, group, tile, w.sequences) : (int64_t)w.sequences * ((group + tile - 1) / tile);
+  const int64_t capacity = std::min<int64_t>((int64_t)w.table_width * c.page_size, kMost);
+  const int64_t groups = s.tiles * c.heads;
+  int64_t chunk = capacity * groups / kGroups;
+  chunk = std::max(kLeastChunk, std::min(kMostChunk, (chunk + 127) / 128 * 128));
+  s.splits = std::max<int64_t>(1, (capacity + chunk - 1) / chunk);
+  s.chunk = s.splits == 1 ? std::max<int64_t>(128, (capacity + 127) / 128 * 128) : chunk;
+  s.stats_bytes = s.splits > 1 ? (size_t)(s.splits * rows * heads * 8 + 255) / 256 * 256 : 0;
+  s.bytes = s.splits > 1 ? s.stats_bytes + (size_t)s.splits * rows * heads * c.head_dim * 4 : 0;
+  return fits(groups, s.splits) && fits((rows * heads + kWaves - 1) / kWaves) && s.splits * (double)rows * heads < 4e15;
+}
+
+int check_cache_attention(int64_t rows, int32_t heads, const squant_cache_t* c, const squant_paged_t* w) {
+  if (int rc = check_cache(c)) return rc;
+  if (int rc = check_paged(w, rows)) return rc;
+  return heads <= 0 || heads % c->heads || (double)rows * heads > (double)kMost ? SQUANT_ERR_SHAPE : SQUANT_OK;
+}
+
+int check_packed(const squant_packed_t* p) {
+  if (!p) return SQUANT_ERR_NULL;
+  if (p->q_rows < 0 || p->k_rows < 0 || p->q_rows > kMost || p->k_rows > kMost || p->sequences < 0) return SQUANT_ERR_SHAPE;
+  if (p->heads <= 0 || p->kv_heads <= 0 || p->heads % p->kv_heads || p->head_dim <= 0 || p->head_dim > 256 || p->head_dim % 8)
+    return SQUANT_ERR_SHAPE;
+  if ((double)p->q_rows * p->heads > (double)kMost) return SQUANT_ERR_SHAPE;
+  if (!p->q_starts != !p->k_starts) return SQUANT_ERR_NULL;
+  if (!p->q_starts && p->sequences != 1) return SQUANT_ERR_SHAPE;
+  if (misaligned(p->q_starts, 4) || misaligned(p->k_starts, 4)) return SQUANT_ERR_FORMAT;
+  if (!(p->scale >= 0.0f) || !std::isfinite(p->scale) || p->causal < 0 || p->causal > 1) return SQUANT_ERR_MODE;
+  return SQUANT_OK;
+}
+
+PromptArgs prompt_args(const squant_packed_t& p) {
+  PromptArgs a{};
+  a.queries = Packed{p.q_starts, p.sequences, (int32_t)p.q_rows, false};
+  a.keys = Packed{p.k_starts, p.sequences, (int32_t)p.k_rows, false};
+  a.heads = p.heads, a.kv_heads = p.kv_heads, a.group = p.heads / p.kv_heads, a.dim = p.head_dim;
+  a.causal = p.causal, a.scale = p.scale;
+  a.scale2 = std::max(p.scale * kLog2E, 1.4e-45f);
+  return a;
+}
+int64_t prompt_groups(const Packed& p, const PromptKernel& k, int32_t heads) {
+  return tiles_bound(p.rows, 1, k.shape.rows, p.count) * heads;
+}
+
+size_t delta_bytes(const squant_packed_t& p) { return ((size_t)p.q_rows * p.heads * 4 + 255) / 256 * 256; }
+
+}  // namespace
+
+extern "C" {
+
+int squant_cache_write(const squant_heads_t* h_k, const squant_heads_t* h_v, squant_wtype_t type, int64_t rows,
+                       const squant_cache_t* h_cache, const squant_paged_t* h_where, void* stream) {
+  return cache_rows(true, h_k, h_v, (int)type, rows, h_cache, h_where, stream);
+}
+
+int squant_cache_read(const squant_cache_t* h_cache, const squant_paged_t* h_where, squant_wtype_t type, int64_t rows,
+                      const squant_heads_t* h_k, const squant_heads_t* h_v, void* stream) {
+  return cache_rows(false, h_k, h_v, (int)type, rows, h_cache, h_where, stream);
+}
+
+size_t squant_cache_attention_workspace_bytes(int64_t rows, int32_t heads, const squant_cache_t* h_cache, const squant_paged_t* h_where) {
+  CacheSplit s;
+  if (check_cache_attention(rows, heads, h_cache, h_where) || rows == 0 || !split_cache(rows, heads, *h_cache, *h_where, s)) return 0;
+  return s.bytes;
+}
+
+int squant_cache_attention(const squant_heads_t* h_q, squant_wtype_t type, int64_t rows, int32_t heads, const squant_cache_t* h_cache,
+                           const squant_paged_t* h_where, float scale, const squant_heads_t* h_out, void* d_workspace,
+                           size_t workspace_bytes, void* stream) {
+  if (int rc = check_type((int)type)) return rc;
+  if (int rc = check_cache_attention(rows, heads, h_cache, h_where)) return rc;
+  if (!(scale >= 0.0f) || !std::isfinite(scale)) return SQUANT_ERR_MODE;
+  if (rows == 0) return SQUANT_OK;
+  const squant_cache_t& c = *h_cache;
+  if (int rc = check_heads(h_q, rows, heads, c.head_dim, (int)type)) return rc;
+  if (int rc = check_heads(h_out, rows, heads, c.head_dim, (int)type)) return rc;
+  CacheSplit s;
+  if (!split_cache(rows, heads, c, *h_where, s)) return SQUANT_ERR_SHAPE;
+  if (workspace_bytes < s.bytes || (s.bytes && (!d_workspace || misaligned(d_workspace, 256)))) return SQUANT_ERR_WORKSPACE;
+  CacheAttentionArgs a{};
+  a.cache = cache_of(c, *h_where);
+  a.rows = packed_of(*h_where, rows);
+  a.q = strided(h_q), a.out = strided(h_out);
+  a.type = (int)type, a.heads = heads, a.group = heads / c.heads;
+  a.splits = (int32_t)s.splits, a.chunk = (int32_t)s.chunk;
+  a.scale = std::max(scale * kLog2E, 1.4e-45f);
+  if (s.splits > 1) a.stats = (float2*)d_workspace, a.partial = (float*)((char*)d_workspace + s.stats_bytes);
+  const int ng = c.head_dim / kGroup;
+  const bool wide = type == SQUANT_W_F32;
+  const cache_attention_t k = c.format == SQUANT_OUT_INT4 ? (wide ? cache_attention_int4_2 : cache_attention_int4_1)(ng, s.rt)
+                                                          : (wide ? cache_attention_int8_2 : cache_attention_int8_1)(ng, s.rt);
+  hipStream_t st = (hipStream_t)stream;
+  if (int rc = launch(k, s.tiles * c.heads, s.splits, cache_attention_lds(ng, s.rt), st, a)) return rc;
+  return s.splits > 1 ? launch(join_splits_kernel(), (rows * heads + kWaves - 1) / kWaves, 1, 0, st, a) : SQUANT_OK;
+}
+
+int squant_attention(const squant_heads_t* h_q, const squant_heads_t* h_k, const squant_heads_t* h_v, squant_wtype_t type,
+                     const squant_packed_t* h_packed, const squant_heads_t* h_out, float* d_lse, void* stream) {
+  if (int rc = check_type((int)type)) return rc;
+  if (int rc = check_packed(h_packed)) return rc;
+  const squant_packed_t& p = *h_packed;
+  if (p.q_rows == 0) return SQUANT_OK;
+  if (int rc = check_heads(h_q, p.q_rows, p.heads, p.head_dim, (int)type)) return rc;
+  if (int rc = check_heads(h_out, p.q_rows, p.heads, p.head_dim, (int)type)) return rc;
+  if (p.k_rows) {
+    if (int rc = check_heads(h_k, p.k_rows, p.kv_heads, p.head_dim, (int)type)) return rc;
+    if (int rc = check_heads(h_v, p.k_rows, p.kv_heads, p.head_dim, (int)type)) return rc;
+  }
+  if (misaligned(d_lse, 4)) return SQUANT_ERR_FORMAT;
+  PromptArgs a = prompt_args(p);
+  a.q = strided(h_q), a.o = strided(h_out);
+  if (p.k_rows) a.k = strided(h_k), a.v = strided(h_v);
+  a.lse = d_lse;
+  const PromptKernel k = type == SQUANT_W_F32 ? prompt_forward_f32(p.head_dim) : type == SQUANT_W_F16 ? prompt_forward_f16(p.head_dim) : prompt_forward_bf16(p.head_dim);
+  return launch(k.run, prompt_groups(a.queries, k, p.heads), 1, k.shape.lds, (hipStream_t)stream, a);
+}
+
+size_t squant_attention_backward_workspace_bytes(const squant_packed_t* h_packed) {
+  return check_packed(h_packed) || !h_packed->q_rows ? 0 : delta_bytes(*h_packed);
+}
+
+int squant_attention_backward(const squant_heads_t* h_dout, const squant_heads_t* h_q, const squant_heads_t* h_k, const squant_heads_t* h_v,
+                              const squant_heads_t* h_out, const float* d_lse, squant_wtype_t type, const squant_packed_t* h_packed,
+                              const squant_heads_t* h_dq, const squant_heads_t* h_dk, const squant_heads_t* h_dv, void* d_workspace,
+                              size_t workspace_bytes, void* stream) {
+  if (int rc = check_type((int)type)) return rc;
+  if (int rc = check_packed(h_packed)) return rc;
+  const squant_packed_t& p = *h_packed;
+  const int t = (int)type;
+  if (p.q_rows) {
+    for (const squant_heads_t* h : {h_dout, h_q, h_out, h_dq})
+      if (int rc = check_heads(h, p.q_rows, p.heads, p.head_dim, t)) return rc;
+    if (!d_lse) return SQUANT_ERR_NULL;
+    if (misaligned(d_lse, 4)) return SQUANT_ERR_FORMAT;
+  }
+  if (p.k_rows)
+    for (const squant_heads_t* h : {h_k, h_v, h_dk, h_dv})
+      if (int rc = check_heads(h, p.k_rows, p.kv_heads, p.head_dim, t)) return rc;
+  const size_t need = p.q_rows ? delta_bytes(p) : 0;
+  if (workspace_bytes < need || (need && (!d_workspace || misaligned(d_workspace, 256)))) return SQUANT_ERR_WORKSPACE;
+  PromptArgs a = prompt_args(p);
+  if (p.q_rows) a.q = strided(h_q), a.o = strided(h_out), a.d_o = strided(h_dout), a.dq = strided(h_dq);
+  if (p.k_rows) a.k = strided(h_k), a.v = strided(h_v), a.dk = strided(h_dk), a.dv = strided(h_dv);
+  a.lse = const_cast<float*>(d_lse);
+  a.delta = (float*)d_workspace;
+  const PromptKernel kq = t == SQUANT_W_F32 ? prompt_queries_f32(p.head_dim) : t == SQUANT_W_F16 ? prompt_queries_f16(p.head_dim) : prompt_queries_bf16(p.head_dim);
+  const PromptKernel kk = t == SQUANT_W_F32 ? prompt_keys_f32(p.head_dim) : t == SQUANT_W_F16 ? prompt_keys_f16(p.head_dim) : prompt_keys_bf16(p.head_dim);
+  const int64_t delta_groups = (p.q_rows * p.heads * 16 + kThreads - 1) / kThreads;
+  const int64_t q_groups = prompt_groups(a.queries, kq, p.heads), k_groups = prompt_groups(a.keys, kk, p.kv_heads);
+  if ((p.q_rows && (!fits(delta_groups) || !fits(q_groups))) || (p.k_rows && !fits(k_groups))) return SQUANT_ERR_SHAPE;
+  hipStream_t st = (hipStream_t)stream;
+  if (p.q_rows) {
+    if (int rc = launch(prompt_delta_kernel(t), delta_groups, 1, 0, st, a)) return rc;
+    if (int rc = launch(kq.run, q_groups, 1, kq.shape.lds, st, a)) return rc;
+  }
+  return p.k_rows ? launch(kk.run, k_groups, 1, kk.shape.lds, st, a) : SQUANT_OK;
+}
+
+}  // extern "C"

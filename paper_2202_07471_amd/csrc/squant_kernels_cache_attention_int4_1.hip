@@ -1,0 +1,11 @@
+// Attention over a cache of 4-bit codes, 16-bit queries.
+#include "squant_cache_attention.h"
+
+namespace squant {
+namespace att {
+
+cache_attention_t cache_attention_int4_1(int ng, int rt) { return cache_attention_of<SQUANT_OUT_INT4, 1>(ng, rt); }
+cache_attention_t join_splits_kernel() { return join_splits<0>; }
+
+}  // namespace att
+}  // namespace squant

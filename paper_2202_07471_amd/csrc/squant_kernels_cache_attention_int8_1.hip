@@ -1,0 +1,10 @@
+// Attention over a cache of 8-bit codes, 16-bit queries.
+#include "squant_cache_attention.h"
+
+namespace squant {
+namespace att {
+
+cache_attention_t cache_attention_int8_1(int ng, int rt) { return cache_attention_of<SQUANT_OUT_INT8, 1>(ng, rt); }
+
+}  // namespace att
+}  // namespace squant

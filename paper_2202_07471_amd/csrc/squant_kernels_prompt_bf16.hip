@@ -1,0 +1,10 @@
+// Attention over whole prompts, bfloat16.
+#include "squant_prompt.h"
+
+namespace squant {
+namespace att {
+
+PromptKernel prompt_forward_bf16(int dim) { return forward_for<__bf16>(dim); }
+
+}  // namespace att
+}  // namespace squant

@@ -1,0 +1,10 @@
+// Attention over whole prompts, binary16.
+#include "squant_prompt.h"
+
+namespace squant {
+namespace att {
+
+PromptKernel prompt_forward_f16(int dim) { return forward_for<_Float16>(dim); }
+
+}  // namespace att
+}  // namespace squant

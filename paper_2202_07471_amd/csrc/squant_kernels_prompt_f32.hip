@@ -1,0 +1,14 @@
+// Attention over whole prompts, binary32.
+#include "squant_prompt.h"
+
+namespace squant {
+namespace att {
+
+PromptKernel prompt_forward_f32(int dim) { return forward_for<float>(dim); }
+
+prompt_t prompt_delta_kernel(int type) {
+  return type == SQUANT_W_F32 ? prompt_delta<float> : type == SQUANT_W_F16 ? prompt_delta<_Float16> : prompt_delta<__bf16>;
+}
+
+}  // namespace att
+}  // namespace squant

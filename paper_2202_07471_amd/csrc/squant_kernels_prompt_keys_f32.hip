@@ -1,0 +1,10 @@
+// Gradients of attention over whole prompts, binary32: keys and values.
+#include "squant_prompt.h"
+
+namespace squant {
+namespace att {
+
+PromptKernel prompt_keys_f32(int dim) { return backward_for<float, true>(dim); }
+
+}  // namespace att
+}  // namespace squant

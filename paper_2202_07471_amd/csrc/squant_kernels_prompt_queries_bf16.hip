@@ -1,0 +1,10 @@
+// Gradients of attention over whole prompts, bfloat16: queries.
+#include "squant_prompt.h"
+
+namespace squant {
+namespace att {
+
+PromptKernel prompt_queries_bf16(int dim) { return backward_for<__bf16, false>(dim); }
+
+}  // namespace att
+}  // namespace squant

@@ -1,0 +1,273 @@
+"""Attention over whole prompts and its gradients on the GPU, against their definitions in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from attention_reference import BF16, F16, F32, attention64, close, packed64, starts_of
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def sq():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2202_07471_amd as sq
+    sq.binding.lib()
+    return sq
+
+
+def inputs(seed, rows, keys, heads, kv, dim, dtype, peak=2.0):
+    gen = torch.Generator().manual_seed(seed)
+    q = (torch.randn(rows, heads, dim, generator=gen) * peak * torch.rand(rows, 1, 1, generator=gen)).to(dtype)
+    k, v = (torch.randn(keys, kv, dim, generator=gen).to(dtype) for _ in range(2))
+    dout = (torch.randn(rows, heads, dim, generator=gen) * 0.1).to(dtype)
+    return q, k, v, dout
+
+
+def both(sq, q, k, v, dout, qs, ks, scale, causal):
+    q, k, v, dout = (t.cuda() for t in (q, k, v, dout))
+    qs, ks = (None if s is None else s.cuda() for s in (qs, ks))
+    out, lse = sq.squant_attention(q, k, v, qs, ks, scale, causal)
+    return (out, lse) + sq.squant_attention_backward(dout, q, k, v, out, lse, qs, ks, scale, causal)
+
+
+def check(sq, seed, q_counts, k_counts, heads, kv, dim, dtype, causal, q_pad=0, k_pad=0, scale=None):
+    q, k, v, dout = inputs(seed, sum(q_counts) + q_pad, sum(k_counts) + k_pad, heads, kv, dim, dtype)
+    scale = dim ** -0.5 if scale is None else scale
+    got = both(sq, q, k, v, dout, starts_of(q_counts), starts_of(k_counts), scale, causal)
+    r = packed64(q.double(), k.double(), v.double(), q_counts, k_counts, scale, causal, dtype, dout.double())
+    for t, name in zip(got, ("out", "lse", "dq", "dk", "dv")):
+        close(t, r, name, f"{q_counts} {k_counts} {heads}/{kv} x {dim} {dtype} {causal}")
+
+
+LENGTHS = [([1], [1]), ([5], [5]), ([16], [33]), ([64], [64]), ([65], [127]), ([129], [129]), ([200, 1, 0, 77], [200, 1, 0, 77]),
+           ([3, 130, 31], [40, 130, 95]), ([1, 1, 1], [300, 1, 64]), ([0, 0], [0, 0])]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("q_counts,k_counts", LENGTHS)
+def test_lengths(sq, q_counts, k_counts, dtype, causal):
+    check(sq, 1, q_counts, k_counts, 4, 2, 64, dtype, causal)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("dim", [8, 16, 32, 40, 64, 72, 80, 96, 104, 128, 136, 160, 192, 200, 224, 256])
+def test_head_sizes(sq, dim, dtype):
+    check(sq, dim, [70, 21], [70, 50], 2, 1, dim, dtype, True)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("heads,kv", [(1, 1), (3, 3), (7, 1), (6, 2), (12, 4), (8, 8)])
+def test_heads(sq, heads, kv, dtype):
+    check(sq, heads, [90, 45], [90, 45], heads, kv, 32, dtype, True)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_long(sq, dtype):
+    check(sq, 3, [700, 333], [700, 1000], 2, 1, 128, dtype, True)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("causal", [True, False])
+def test_rows_that_see_nothing(sq, dtype, causal):
+    """More queries than keys (causal: the first rows see none), a sequence without keys, one without queries, padding rows."""
+    check(sq, 4, [40, 9, 0, 5], [17, 0, 12, 5], 4, 2, 64, dtype, causal, q_pad=7, k_pad=70)
+
+
+@pytest.mark.parametrize("scale", [0.0, 1e-3, 1.0])
+def test_scales(sq, scale):
+    check(sq, 5, [50], [50], 2, 2, 64, BF16, True, scale=scale)
+
+
+def test_one_sequence_without_starts(sq):
+    q, k, v, dout = inputs(6, 100, 100, 2, 1, 64, BF16)
+    r = packed64(q.double(), k.double(), v.double(), [100], [100], 0.125, True, BF16, dout.double())
+    for t, name in zip(both(sq, q, k, v, dout, None, None, 0.125, True), ("out", "lse", "dq", "dk", "dv")):
+        close(t, r, name)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_hidden_values(sq, dtype):
+    """NaN and infinities in keys and values that a row does not see leave its output alone."""
+    q, k, v, _ = inputs(7, 150, 150, 2, 1, 64, dtype)
+    k2, v2 = k.clone(), v.clone()
+    for at, value in ((60, math.nan), (101, math.inf), (149, -math.inf)):
+        k2[at], v2[at] = value, value
+    starts = starts_of([150]).cuda()
+    one = sq.squant_attention(q.cuda(), k.cuda(), v.cuda(), starts)[0]
+    two = sq.squant_attention(q.cuda(), k2.cuda(), v2.cuda(), starts)[0]
+    r = attention64(q.double(), k.double(), v.double(), 0.125, True, dtype)
+    r = {x: t[:60] for x, t in r.items()}
+    close(one[:60], r, "out")
+    close(two[:60], r, "out")
+    assert two[60:].isnan().any(-1).all()
+    # a padding key's contents, and those of the next sequence
+    starts = starts_of([60, 41]).cuda()
+    three = sq.squant_attention(q.cuda(), k2.cuda(), v2.cuda(), starts)[0]
+    close(three[:60], r, "out")
+    assert (three[101:] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_values_hidden_one_by_one(sq, dtype):
+    """A value that is an infinity, its key ordinary: rows from it on are infinite there, rows before it are not touched."""
+    q, k, v, _ = inputs(8, 70, 70, 1, 1, 64, dtype)
+    v2 = v.clone()
+    v2[33, 0, 5] = math.inf
+    out = sq.squant_attention(q.cuda(), k.cuda(), v2.cuda())[0].cpu()
+    want = sq.squant_attention(q.cuda(), k.cuda(), v.cuda())[0].cpu()
+    assert (out[33:, 0, 5] == math.inf).all()
+    v2[33, 0, 5] = 0
+    r = attention64(q.double(), k.double(), v.double(), 0.125, True, dtype)
+    r = {x: t[:33] for x, t in r.items()}
+    close(out[:33], r, "out")
+    close(want[:33], r, "out")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_strides(sq, dtype):
+    """Slices of one projection, an odd distance between rows, heads outside rows, results in given buffers."""
+    heads, kv, dim, rows = 4, 2, 64, 75
+    gen = torch.Generator().manual_seed(9)
+    fused = torch.randn(rows, (heads + 2 * kv) * dim + 3, generator=gen).to(dtype).cuda()
+    x = fused[:, 1:1 + (heads + 2 * kv) * dim].unflatten(1, (-1, dim))
+    q, k, v = x[:, :heads], x[:, heads:heads + kv], x[:, heads + kv:]
+    dout = torch.randn(heads, rows, dim, generator=gen).to(dtype).cuda().transpose(0, 1)
+    starts = starts_of([70, 5]).cuda()
+    buf = torch.full((rows, heads * dim + 5), math.nan, dtype=dtype, device="cuda")
+    out = buf[:, 2:2 + heads * dim].unflatten(1, (heads, dim))
+    got, lse = sq.squant_attention(q, k, v, starts, out=out)
+    assert got.data_ptr() == out.data_ptr()
+    grads = torch.full((3, heads, rows, dim), math.nan, dtype=dtype, device="cuda")
+    dq, dk, dv = grads[0].transpose(0, 1), grads[1, :kv].transpose(0, 1), grads[2, :kv].transpose(0, 1)
+    sq.squant_attention_backward(dout, q, k, v, out, lse, starts, dq=dq, dk=dk, dv=dv)
+    r = packed64(*(t.double().cpu() for t in (q, k, v)), [70, 5], [70, 5], dim ** -0.5, True, dtype, dout.double().cpu())
+    for t, name in ((out, "out"), (lse, "lse"), (dq, "dq"), (dk, "dk"), (dv, "dv")):
+        close(t, r, name)
+    assert buf[:, :2].isnan().all() and buf[:, 2 + heads * dim:].isnan().all() and grads[1:, kv:].isnan().all()
+
+
+def test_small_gradients_of_binary16(sq):
+    """Gradients far below binary16's least normal number times a weight: still told apart."""
+    q, k, v, dout = inputs(10, 200, 200, 2, 1, 64, F16)
+    dout = (dout.float() * 2.0 ** -8).half()
+    dout[:100] *= 2.0 ** -4
+    r = packed64(q.double(), k.double(), v.double(), [100, 100], [100, 100], 0.125, False, F16, dout.double())
+    got = both(sq, q, k, v, dout, starts_of([100, 100]), starts_of([100, 100]), 0.125, False)
+    for t, name in zip(got, ("out", "lse", "dq", "dk", "dv")):
+        close(t, r, name)
+
+
+def test_autograd_and_differences(sq):
+    """packed_attention's gradients: the definition's, through views and with some inputs that need none, and differences of the
+    output along a direction."""
+    q, k, v, w = (t.cuda() for t in inputs(11, 60, 60, 4, 2, 32, F32, peak=1.0))
+    starts = starts_of([40, 20]).cuda()
+    leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+    out = sq.packed_attention(*leaves, starts)
+    (out * w).sum().backward()
+    r = packed64(*(t.double().cpu() for t in (q, k, v)), [40, 20], [40, 20], 32 ** -0.5, True, F32, w.double().cpu())
+    for t, name in zip(leaves, ("dq", "dk", "dv")):
+        close(t.grad, r, name)
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    for leaf, at in zip(leaves, range(3)):
+        d = torch.randn(leaf.shape, device="cuda", generator=gen)
+        step = 2.0 ** -6
+        ends = []
+        for sign in (1, -1):
+            x = [q, k, v]
+            x[at] = x[at] + sign * step * d
+            ends.append((sq.packed_attention(*x, starts).double() * w.double()).sum())
+        slope = ((ends[0] - ends[1]) / (2 * step)).item()
+        want = (leaf.grad.double() * d.double()).sum().item()
+        # the step's square times a third derivative of order |d|^3 / sqrt(D)^3 per row, and rounding of 7680 terms over the step
+        assert abs(slope - want) <= 0.01 * (leaf.grad.double().norm() * d.double().norm()).item() / 8
+    k2 = k.clone().requires_grad_()
+    sq.packed_attention(q, k2, v, starts).sum().backward()
+    assert k2.grad.shape == k2.shape
+    expanded = leaves[0].detach().clone().requires_grad_()
+    sq.packed_attention(expanded, k, v, starts).sum().backward()  # the output's gradient is an expanded 1
+    assert expanded.grad.isfinite().all()
+
+
+def test_shared_heads_add_up(sq):
+    """The gradient of a key head that query heads share is the sum of its copies' gradients."""
+    q, k, v, dout = inputs(13, 64, 64, 6, 2, 64, F32)
+    shared = both(sq, q, k, v, dout, None, None, 0.125, True)
+    apart = both(sq, q, k.repeat_interleave(3, 1), v.repeat_interleave(3, 1), dout, None, None, 0.125, True)
+    r = packed64(q.double(), k.double(), v.double(), [64], [64], 0.125, True, F32, dout.double())
+    for i, name in ((3, "dk"), (4, "dv")):
+        close(shared[i], r, name)
+        close(apart[i].unflatten(1, (2, 3)).sum(2), {name: r[name], name + "_tol": 2 * r[name + "_tol"]}, name)
+
+
+def test_same_bits(sq):
+    q, k, v, dout = inputs(14, 513, 513, 8, 2, 128, BF16)
+    one, two = (both(sq, q, k, v, dout, None, None, None, True) for _ in range(2))
+    assert all(torch.equal(a, b) for a, b in zip(one, two))
+
+
+def test_empty(sq):
+    q, k, v, dout = inputs(15, 0, 9, 2, 1, 64, BF16)
+    out, lse, dq, dk, dv = both(sq, q, k, v, dout, starts_of([0]), starts_of([9]), None, True)
+    assert out.shape == q.shape and lse.shape == (2, 0) and dq.shape == q.shape and (dk == 0).all() and (dv == 0).all()
+    q, k, v, dout = inputs(15, 9, 0, 2, 1, 64, BF16)
+    out, lse, dq, dk, dv = both(sq, q, k, v, dout, starts_of([9]), starts_of([0]), None, True)
+    assert (out == 0).all() and (lse == -math.inf).all() and (dq == 0).all() and dk.shape == k.shape
+
+
+def test_streams_and_graphs(sq):
+    """On a stream of their own, and captured: a replay gives what a call gives, with other lengths too."""
+    q, k, v, dout = (t.cuda() for t in inputs(16, 200, 200, 4, 2, 64, BF16))
+    starts = starts_of([120, 80]).cuda()
+    want = sq.squant_attention(q, k, v, starts)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = sq.squant_attention(q, k, v, starts, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+    def step():
+        out, lse = sq.squant_attention(q, k, v, starts)
+        return (out, lse) + sq.squant_attention_backward(dout, q, k, v, out, lse, starts)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for counts in ([120, 80], [1, 150], [0, 0], [200, 0]):
+        starts.copy_(starts_of(counts))
+        q.mul_(0.75)
+        torch.cuda.synchronize()
+        graph.replay()
+        for a, b in zip(held, step()):
+            assert torch.equal(a, b)
+
+
+def test_refusals(sq):
+    q, k, v, dout = (t.cuda() for t in inputs(17, 8, 8, 4, 2, 64, BF16))
+    starts = starts_of([8]).cuda()
+    out, lse = sq.squant_attention(q, k, v, starts)
+    bad = [lambda: sq.squant_attention(q, k.half(), v, starts), lambda: sq.squant_attention(q, k, v[:4], starts),
+           lambda: sq.squant_attention(q, k[:4], v[:4], starts), lambda: sq.squant_attention(q, k[:, :, :32], v, starts),
+           lambda: sq.squant_attention(q[:, :3], k, v, starts), lambda: sq.squant_attention(q, k, v, starts.long()),
+           lambda: sq.squant_attention(q, k, v, starts, k_starts=starts[:1]), lambda: sq.squant_attention(q, k, v, k_starts=starts),
+           lambda: sq.squant_attention(q, k, v, starts.cpu()), lambda: sq.squant_attention(q, k.cpu(), v, starts),
+           lambda: sq.squant_attention(q, k, v, starts, scale=-1.0), lambda: sq.squant_attention(q, k, v, starts, scale=math.nan),
+           lambda: sq.squant_attention(q[:, :, :60], k[:, :, :60], v[:, :, :60], starts),
+           lambda: sq.squant_attention(q.transpose(1, 2), k, v, starts), lambda: sq.squant_attention(q.double(), k, v, starts),
+           lambda: sq.squant_attention(q[:, :, ::2], k[:, :, ::2], v[:, :, ::2], starts),
+           lambda: sq.squant_attention(q, k, v, starts, out=out[:, :, :32]),
+           lambda: sq.squant_attention(q, k, v, starts, out=out[:1].expand(8, 4, 64)),
+           lambda: sq.squant_attention_backward(dout[:4], q, k, v, out, lse, starts),
+           lambda: sq.squant_attention_backward(dout, q, k, v, out, lse.half(), starts),
+           lambda: sq.squant_attention_backward(dout, q, k, v, out, lse[:2], starts),
+           lambda: sq.squant_attention_backward(dout, q, k, v, out, lse, starts, dk=k[:4])]
+    for f in bad:
+        with pytest.raises(ValueError):
+            f()
