@@ -324,8 +324,8 @@ int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t t
 /* [rows][heads][head_dim] elements; a head's elements lie beside each other. */
 typedef struct {
   void* data;      /* device, aligned to its element type */
-  int64_t row;     /* elements between rows, */
-  int64_t head;    /* and between heads: multiples of nothing, at least head_dim */
+  int64_t row;     /* elements between rows, from head_dim to 2^22, */
+  int64_t head;    /* and between heads, from head_dim to 2^31; any number where there is one row or one head */
 } squant_heads_t;
 
 /* A paged cache of keys and values.  Codes [pages][heads][page_size][head_dim], int8 (SQUANT_OUT_INT8) or two 4-bit

@@ -16,6 +16,8 @@ using namespace squant;
 using namespace squant::att;
 
 constexpr int64_t kMost = 0x7fffffffLL;
+// Elements between rows and between heads: a tile's rows are within 32 bits of bytes of each other, a buffer's within 64.
+constexpr int64_t kFarRow = (int64_t)1 << 22, kFarHead = (int64_t)1 << 31;
 
 int element_bytes(int type) { return type == SQUANT_W_F32 ? 4 : 2; }
 bool misaligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
@@ -25,12 +27,16 @@ int check_type(int type) { return type < SQUANT_W_F32 || type > SQUANT_W_BF16 ? 
 int check_heads(const squant_heads_t* h, int64_t rows, int32_t heads, int32_t dim, int type) {
   if (!h || !h->data) return SQUANT_ERR_NULL;
   if (misaligned(h->data, element_bytes(type))) return SQUANT_ERR_FORMAT;
-  constexpr int64_t far = (int64_t)1 << 40;  // rows times this stays within 64 bits with what is allowed for rows
-  if ((heads > 1 && (h->head < dim || h->head > far)) || (rows > 1 && (h->row < dim || h->row > far))) return SQUANT_ERR_SHAPE;
-  if (rows > 1 && rows * (double)h->row > 4e18) return SQUANT_ERR_SHAPE;
+  if ((heads > 1 && (h->head < dim || h->head > kFarHead)) || (rows > 1 && (h->row < dim || h->row > kFarRow))) return SQUANT_ERR_SHAPE;
   return SQUANT_OK;
 }
-Strided strided(const squant_heads_t* h) { return Strided{(char*)h->data, h->row, h->head}; }
+// Whether every head of every row begins at a multiple of 16 bytes.
+bool whole_pieces(const squant_heads_t* h, int type) {
+  const int e = element_bytes(type);
+  return !misaligned(h->data, 16) && h->row * e % 16 == 0 && h->head * e % 16 == 0;
+}
+// A step that is never taken counts as none.
+Strided strided(const squant_heads_t* h, int64_t rows) { return Strided{(char*)h->data, rows > 1 ? h->row : 0, h->head}; }
 
 int check_cache(const squant_cache_t* c) {
   if (!c || !c->key_codes || !c->key_scales || !c->value_codes || !c->value_scales) return SQUANT_ERR_NULL;
@@ -65,17 +71,17 @@ Cache cache_of(const squant_cache_t& c, const squant_paged_t& w) {
 }
 Packed packed_of(const squant_paged_t& w, int64_t rows) { return Packed{w.starts, w.sequences, (int32_t)rows, !w.starts}; }
 
-bool fits(int64_t groups, int64_t gy = 1) { return groups > 0 && groups * kThreads <= 0xffffffffLL && gy <= 0xffff; }
+bool fits(int64_t groups, int64_t gy = 1, int threads = kThreads) { return groups > 0 && groups * threads <= 0xffffffffLL && gy <= 0xffff; }
 
-template <class A> int launch(void (*k)(A), int64_t gx, int64_t gy, size_t lds, hipStream_t st, const A& a) {
-  if (!fits(gx, gy)) return SQUANT_ERR_SHAPE;
+template <class A> int launch(void (*k)(A), int64_t gx, int64_t gy, size_t lds, hipStream_t st, const A& a, int threads = kThreads) {
+  if (!fits(gx, gy, threads)) return SQUANT_ERR_SHAPE;
   // kernels that ask for more LDS than a workgroup gets by default say so: the attribute is the kernel's, not a call's
   if (lds > 64 * 1024 &&
       hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess) {
     (void)hipGetLastError();
     return SQUANT_ERR_DEVICE;
   }
-  hipLaunchKernelGGL(k, dim3((unsigned)gx, (unsigned)gy), dim3(kThreads), (unsigned)lds, st, a);
+  hipLaunchKernelGGL(k, dim3((unsigned)gx, (unsigned)gy), dim3((unsigned)threads), (unsigned)lds, st, a);
   return hipGetLastError() == hipSuccess ? SQUANT_OK : SQUANT_ERR_DEVICE;
 }
 
@@ -90,7 +96,7 @@ int cache_rows(bool write, const squant_heads_t* k, const squant_heads_t* v, int
   CacheRowsArgs a{};
   a.cache = cache_of(*c, *w);
   a.rows = packed_of(*w, rows);
-  a.x[0] = strided(k), a.x[1] = strided(v);
+  a.x[0] = strided(k, rows), a.x[1] = strided(v, rows);
   const int64_t pieces = (int64_t)2 * c->heads * (c->head_dim / 8);
   if (pieces > 1 << 20) return SQUANT_ERR_SHAPE;
   a.pieces = (int32_t)pieces, a.dim_pieces = c->head_dim / 8;
@@ -156,7 +162,7 @@ PromptArgs prompt_args(const squant_packed_t& p) {
   return a;
 }
 int64_t prompt_groups(const Packed& p, const PromptKernel& k, int32_t heads) {
-  return tiles_bound(p.rows, 1, k.shape.rows, p.count) * heads;
+  return tiles_bound(p.rows, 1, k.rows, p.count) * heads;
 }
 
 size_t delta_bytes(const squant_packed_t& p) { return ((size_t)p.q_rows * p.heads * 4 + 255) / 256 * 256; }
@@ -197,7 +203,7 @@ int squant_cache_attention(const squant_heads_t* h_q, squant_wtype_t type, int64
   CacheAttentionArgs a{};
   a.cache = cache_of(c, *h_where);
   a.rows = packed_of(*h_where, rows);
-  a.q = strided(h_q), a.out = strided(h_out);
+  a.q = strided(h_q, rows), a.out = strided(h_out, rows);
   a.type = (int)type, a.heads = heads, a.group = heads / c.heads;
   a.splits = (int32_t)s.splits, a.chunk = (int32_t)s.chunk;
   a.scale = std::max(scale * kLog2E, 1.4e-45f);
@@ -225,11 +231,12 @@ int squant_attention(const squant_heads_t* h_q, const squant_heads_t* h_k, const
   }
   if (misaligned(d_lse, 4)) return SQUANT_ERR_FORMAT;
   PromptArgs a = prompt_args(p);
-  a.q = strided(h_q), a.o = strided(h_out);
-  if (p.k_rows) a.k = strided(h_k), a.v = strided(h_v);
+  a.q = strided(h_q, p.q_rows), a.o = strided(h_out, p.q_rows);
+  if (p.k_rows) a.k = strided(h_k, p.k_rows), a.v = strided(h_v, p.k_rows);
   a.lse = d_lse;
-  const PromptKernel k = type == SQUANT_W_F32 ? prompt_forward_f32(p.head_dim) : type == SQUANT_W_F16 ? prompt_forward_f16(p.head_dim) : prompt_forward_bf16(p.head_dim);
-  return launch(k.run, prompt_groups(a.queries, k, p.heads), 1, k.shape.lds, (hipStream_t)stream, a);
+  const bool direct = !p.k_rows || (whole_pieces(h_k, (int)type) && whole_pieces(h_v, (int)type));
+  const PromptKernel k = (type == SQUANT_W_F32 ? prompt_forward_f32 : type == SQUANT_W_F16 ? prompt_forward_f16 : prompt_forward_bf16)(p.head_dim, direct);
+  return launch(k.run, prompt_groups(a.queries, k, p.heads), 1, k.lds, (hipStream_t)stream, a, k.threads);
 }
 
 size_t squant_attention_backward_workspace_bytes(const squant_packed_t* h_packed) {
@@ -256,21 +263,24 @@ int squant_attention_backward(const squant_heads_t* h_dout, const squant_heads_t
   const size_t need = p.q_rows ? delta_bytes(p) : 0;
   if (workspace_bytes < need || (need && (!d_workspace || misaligned(d_workspace, 256)))) return SQUANT_ERR_WORKSPACE;
   PromptArgs a = prompt_args(p);
-  if (p.q_rows) a.q = strided(h_q), a.o = strided(h_out), a.d_o = strided(h_dout), a.dq = strided(h_dq);
-  if (p.k_rows) a.k = strided(h_k), a.v = strided(h_v), a.dk = strided(h_dk), a.dv = strided(h_dv);
+  const int64_t qr = p.q_rows, kr = p.k_rows;
+  if (qr) a.q = strided(h_q, qr), a.o = strided(h_out, qr), a.d_o = strided(h_dout, qr), a.dq = strided(h_dq, qr);
+  if (kr) a.k = strided(h_k, kr), a.v = strided(h_v, kr), a.dk = strided(h_dk, kr), a.dv = strided(h_dv, kr);
   a.lse = const_cast<float*>(d_lse);
   a.delta = (float*)d_workspace;
-  const PromptKernel kq = t == SQUANT_W_F32 ? prompt_queries_f32(p.head_dim) : t == SQUANT_W_F16 ? prompt_queries_f16(p.head_dim) : prompt_queries_bf16(p.head_dim);
-  const PromptKernel kk = t == SQUANT_W_F32 ? prompt_keys_f32(p.head_dim) : t == SQUANT_W_F16 ? prompt_keys_f16(p.head_dim) : prompt_keys_bf16(p.head_dim);
+  const bool keys_direct = !p.k_rows || (whole_pieces(h_k, t) && whole_pieces(h_v, t));
+  const bool queries_direct = !p.q_rows || (whole_pieces(h_q, t) && whole_pieces(h_dout, t));
+  const PromptKernel kq = (t == SQUANT_W_F32 ? prompt_queries_f32 : t == SQUANT_W_F16 ? prompt_queries_f16 : prompt_queries_bf16)(p.head_dim, keys_direct);
+  const PromptKernel kk = (t == SQUANT_W_F32 ? prompt_keys_f32 : t == SQUANT_W_F16 ? prompt_keys_f16 : prompt_keys_bf16)(p.head_dim, queries_direct);
   const int64_t delta_groups = (p.q_rows * p.heads * 16 + kThreads - 1) / kThreads;
   const int64_t q_groups = prompt_groups(a.queries, kq, p.heads), k_groups = prompt_groups(a.keys, kk, p.kv_heads);
-  if ((p.q_rows && (!fits(delta_groups) || !fits(q_groups))) || (p.k_rows && !fits(k_groups))) return SQUANT_ERR_SHAPE;
+  if ((p.q_rows && (!fits(delta_groups) || !fits(q_groups, 1, kq.threads))) || (p.k_rows && !fits(k_groups, 1, kk.threads))) return SQUANT_ERR_SHAPE;
   hipStream_t st = (hipStream_t)stream;
   if (p.q_rows) {
     if (int rc = launch(prompt_delta_kernel(t), delta_groups, 1, 0, st, a)) return rc;
-    if (int rc = launch(kq.run, q_groups, 1, kq.shape.lds, st, a)) return rc;
+    if (int rc = launch(kq.run, q_groups, 1, kq.lds, st, a, kq.threads)) return rc;
   }
-  return p.k_rows ? launch(kk.run, k_groups, 1, kk.shape.lds, st, a) : SQUANT_OK;
+  return p.k_rows ? launch(kk.run, k_groups, 1, kk.lds, st, a, kk.threads) : SQUANT_OK;
 }
 
 }  // extern "C"

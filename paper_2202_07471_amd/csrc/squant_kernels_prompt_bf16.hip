@@ -4,7 +4,7 @@
 namespace squant {
 namespace att {
 
-PromptKernel prompt_forward_bf16(int dim) { return forward_for<__bf16>(dim); }
+PromptKernel prompt_forward_bf16(int dim, bool direct) { return forward_for<__bf16>(dim, direct); }
 
 }  // namespace att
 }  // namespace squant

@@ -4,7 +4,7 @@
 namespace squant {
 namespace att {
 
-PromptKernel prompt_forward_f16(int dim) { return forward_for<_Float16>(dim); }
+PromptKernel prompt_forward_f16(int dim, bool direct) { return forward_for<_Float16>(dim, direct); }
 
 }  // namespace att
 }  // namespace squant

@@ -4,7 +4,7 @@
 namespace squant {
 namespace att {
 
-PromptKernel prompt_forward_f32(int dim) { return forward_for<float>(dim); }
+PromptKernel prompt_forward_f32(int dim, bool direct) { return forward_for<float>(dim, direct); }
 
 prompt_t prompt_delta_kernel(int type) {
   return type == SQUANT_W_F32 ? prompt_delta<float> : type == SQUANT_W_F16 ? prompt_delta<_Float16> : prompt_delta<__bf16>;

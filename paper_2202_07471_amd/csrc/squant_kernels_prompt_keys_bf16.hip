@@ -4,7 +4,7 @@
 namespace squant {
 namespace att {
 
-PromptKernel prompt_keys_bf16(int dim) { return backward_for<__bf16, true>(dim); }
+PromptKernel prompt_keys_bf16(int dim, bool direct) { return backward_for<__bf16, true>(dim, direct); }
 
 }  // namespace att
 }  // namespace squant

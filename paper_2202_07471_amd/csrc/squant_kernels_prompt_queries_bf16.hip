@@ -4,7 +4,7 @@
 namespace squant {
 namespace att {
 
-PromptKernel prompt_queries_bf16(int dim) { return backward_for<__bf16, false>(dim); }
+PromptKernel prompt_queries_bf16(int dim, bool direct) { return backward_for<__bf16, false>(dim, direct); }
 
 }  // namespace att
 }  // namespace squant

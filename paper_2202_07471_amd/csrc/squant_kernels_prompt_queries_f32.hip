@@ -4,7 +4,7 @@
 namespace squant {
 namespace att {
 
-PromptKernel prompt_queries_f32(int dim) { return backward_for<float, false>(dim); }
+PromptKernel prompt_queries_f32(int dim, bool direct) { return backward_for<float, false>(dim, direct); }
 
 }  // namespace att
 }  // namespace squant

@@ -35,88 +35,133 @@ template <class T, int DP> struct TileOf {
   static constexpr int kPiece = 16 / (int)sizeof(T);                     // elements of 16 bytes
   static constexpr int kPieces = DP / kPiece;                            // of a row
   static constexpr int kRowBytes = (DP * (int)sizeof(T) + 127) / 128 * 128;
-  // Byte address of piece c of row r.  Eight rows' same piece lie in eight different 16-byte columns of 128 bytes, four
-  // rows' same pair of pieces in four different 32-byte columns.
-  static __device__ __forceinline__ int place(int r, int c) {
-    return r * kRowBytes + ((c ^ (((r & 3) << 1) | ((r >> 2) & 1))) << 4);
+  // Byte address of piece c of row r.  The LDS serves 256 bytes at once: 16 rows' same piece (operands of rows), or 8 rows' same
+  // pair of pieces (transposing reads), lie in different columns of 256 bytes.
+  static __device__ __forceinline__ int turn(int r) {
+    return kRowBytes % 256 == 0 ? ((r & 7) << 1) ^ (((r >> 3) & 1) * 9) : (r & 6) ^ (((r >> 3) & 1) * 5);
   }
+  static __device__ __forceinline__ int place(int r, int c) { return r * kRowBytes + ((c ^ turn(r)) << 4); }
 };
 
-// A tile of ROWS rows on its way from memory: pieces behind `count` rows or `dim` elements are zeros.
-template <class T, int DP, int ROWS> struct Staged {
+// Tiles of ROWS rows on their way from memory to the LDS.  DIRECT: without passing through registers, which takes rows at
+// multiples of 16 bytes; otherwise by registers.  A row past the last is the last one again, a piece past the head's elements the
+// first one: both meet zeros or are hidden.  Bytes of the tile are dealt to lanes in their order, 16 each.
+template <class T, int DP, int ROWS, int WAVES, bool DIRECT> struct Loader {
   typedef TileOf<T, DP> TL;
-  static constexpr int kEach = ROWS * TL::kPieces / kThreads;
-  static_assert(ROWS * TL::kPieces % kThreads == 0, "");
-  uint4v piece[kEach];
-  __device__ __forceinline__ void load(const Strided& s, int64_t row0, int head, int count, int dim) {
+  static constexpr int kBytes = ROWS * TL::kRowBytes;
+  static constexpr int kEach = kBytes / (WAVES * 1024);
+  static_assert(kBytes % (WAVES * 1024) == 0, "");
+  uint32_t offset[kEach];  // of full tiles, bytes from the tile's first row
+  uint4v piece[DIRECT ? 1 : kEach];
+
+  static __device__ __forceinline__ int first(int i) { return (__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * kEach + i) * 1024; }
+  static __device__ __forceinline__ int position(int i) { return first(i) + ((int)threadIdx.x & 63) * 16; }
+  static __device__ __forceinline__ uint32_t offset_of(int i, uint32_t row_bytes, int last, int dim) {
+    const int at = position(i), r = at / TL::kRowBytes;
+    int c = (at % TL::kRowBytes >> 4) ^ TL::turn(r);
+    if (c * TL::kPiece >= dim) c = 0;
+    return (uint32_t)min(r, last) * row_bytes + (uint32_t)(c << 4);
+  }
+  __device__ __forceinline__ void begin(uint32_t row_bytes, int dim) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) offset[i] = offset_of(i, row_bytes, ROWS, dim);
+  }
+  template <class OFFSET> __device__ __forceinline__ void take(const char* from, char* tile, OFFSET off) {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int at = (int)threadIdx.x + i * kThreads, r = at / TL::kPieces, c = at % TL::kPieces;
-      piece[i] = uint4v{0, 0, 0, 0};
-      if (r < count && c * TL::kPiece < dim) piece[i] = load_any<uint4v>(element<T>(s, row0 + r, head) + c * TL::kPiece);
+      if constexpr (DIRECT)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + off(i)),
+                                         (__attribute__((address_space(3))) void*)(tile + first(i)), 16, 0, 0);
+      else
+        piece[i] = load_any<uint4v>(from + off(i));
     }
   }
-  __device__ __forceinline__ void store(char* tile) const {
+  // `from`: the tile's first row; `count`: rows from there on, at least one.
+  __device__ __forceinline__ void issue(const char* from, char* tile, int count, uint32_t row_bytes, int dim) {
+    if (count >= ROWS) take(from, tile, [&](int i) { return offset[i]; });
+    else take(from, tile, [&](int i) { return offset_of(i, row_bytes, count - 1, dim); });
+  }
+  // Before the barrier behind which the tile is read.
+  __device__ __forceinline__ void land(char* tile) const {
+    if constexpr (!DIRECT) {
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int at = (int)threadIdx.x + i * kThreads;
-      *reinterpret_cast<uint4v*>(tile + TL::place(at / TL::kPieces, at % TL::kPieces)) = piece[i];
+      for (int i = 0; i < kEach; ++i) *reinterpret_cast<uint4v*>(tile + position(i)) = piece[i];
     }
   }
-  // Whether some element is an infinity or NaN.
-  __device__ __forceinline__ bool odd() const {
+  // Whether this lane's part of a tile has an infinity or NaN.
+  static __device__ __forceinline__ bool odd(const char* tile) {
     uint32_t top = 0, high = 0;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i)
+    for (int i = 0; i < kEach; ++i) {
+      const uint4v v = *reinterpret_cast<const uint4v*>(tile + position(i));
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         if constexpr (sizeof(T) == 4) {
-          top = max(top, piece[i][w] & 0x7fffffffu);
+          top = max(top, v[w] & 0x7fffffffu);
         } else {
-          top = max(top, piece[i][w] & 0x7fffu);
-          high = max(high, piece[i][w] & 0x7fff0000u);
+          top = max(top, v[w] & 0x7fffu);
+          high = max(high, v[w] & 0x7fff0000u);
         }
       }
+    }
     if constexpr (sizeof(T) == 4) return top >= 0x7f800000u;
     constexpr uint32_t first = __is_same(T, __bf16) ? 0x7f80u : 0x7c00u;
     return top >= first || high >= first << 16;
   }
 };
+__device__ __forceinline__ void tiles_are_here() { __builtin_amdgcn_s_waitcnt(0x0F70); }  // vmcnt(0)
 
-// Operand rows r0 .. r0 + 15 of a tile, contraction elements 32 ks .. 32 ks + 31 of the row.
-template <class T, int DP> __device__ __forceinline__ typename MatrixOf<T>::type::frag row_operand(const char* tile, int r0, int ks) {
+// Where a lane reads operands, in bytes from a tile's beginning.  Pieces are exchanged within runs of 8 or 16, so what an
+// operand's place adds to a lane's is one exclusive or and an offset of the instruction.
+template <class T, int DP> struct Lanes {
   typedef TileOf<T, DP> TL;
+  static constexpr int kRun = TL::kRowBytes % 256 == 0 ? 15 : 7;
+  int row, turned;
+  __device__ __forceinline__ Lanes() {
+    const int lane = (int)threadIdx.x & 63, n = lane & 15, g = lane >> 4, r = 4 * g + (n >> 2);
+    row = n * TL::kRowBytes + (((sizeof(T) == 2 ? g : 2 * g) ^ TL::turn(n)) << 4);
+    turned = sizeof(T) == 2 ? r * TL::kRowBytes + ((((n & 3) >> 1) ^ TL::turn(r)) << 4) + (n & 1) * 8 : 0;
+  }
+  static __device__ __forceinline__ int piece(int at, int c) { return (at ^ ((c & kRun) << 4)) + ((c & ~kRun) << 4); }
+};
+
+// Operand rows r0 .. r0 + 15 of a tile, contraction elements 32 ks .. 32 ks + 31 of the row.  `at`: the lane's `row` and the tile.
+template <class T, int DP>
+__device__ __forceinline__ typename MatrixOf<T>::type::frag row_operand(const char* tiles, int at, int r0, int ks) {
+  typedef Lanes<T, DP> L;
   typedef typename MatrixOf<T>::type::frag frag;
-  const int lane = (int)threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int o = r0 * L::TL::kRowBytes;
   if constexpr (sizeof(T) == 2) {
-    return __builtin_bit_cast(frag, *reinterpret_cast<const uint4v*>(tile + TL::place(r0 + n, 4 * ks + g)));
+    return __builtin_bit_cast(frag, *reinterpret_cast<const uint4v*>(tiles + L::piece(at, 4 * ks) + o));
   } else {
-    const float4v a = *reinterpret_cast<const float4v*>(tile + TL::place(r0 + n, 8 * ks + 2 * g));
-    const float4v b = *reinterpret_cast<const float4v*>(tile + TL::place(r0 + n, 8 * ks + 2 * g + 1));
+    const float4v a = *reinterpret_cast<const float4v*>(tiles + L::piece(at, 8 * ks) + o);
+    const float4v b = *reinterpret_cast<const float4v*>(tiles + L::piece(at, 8 * ks + 1) + o);
     return frag{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
   }
 }
 
 // Operand rows = elements 16 f .. 16 f + 15 of a tile's rows, contraction over its rows r0 .. r0 + 31 in the order of two
-// results side by side.
-template <class T, int DP> __device__ __forceinline__ typename MatrixOf<T>::type::frag turned_operand(const char* tile, int r0, int f) {
-  typedef TileOf<T, DP> TL;
+// results side by side.  `at`: the lane's `turned` and the tile.
+template <class T, int DP>
+__device__ __forceinline__ typename MatrixOf<T>::type::frag turned_operand(const char* tiles, int at, int r0, int f) {
+  typedef Lanes<T, DP> L;
+  typedef typename L::TL TL;
   typedef typename MatrixOf<T>::type::frag frag;
-  const int lane = (int)threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   if constexpr (sizeof(T) == 2) {
     typedef short short4v __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) short4v* lds_t;
     // lanes 4 r .. 4 r + 3 of sixteen name the 16 elements of row r; lane n gets element n of the four rows
-    const int r = r0 + 4 * g + (n >> 2), c = 2 * f + ((n & 3) >> 1), in = (n & 1) * 8;
-    const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(tile + TL::place(r, c) + in));
-    const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(tile + TL::place(r + 16, c) + in));
+    const char* p = tiles + L::piece(at, 2 * f) + r0 * TL::kRowBytes;
+    const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)p);
+    const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(p + 16 * TL::kRowBytes));
     typedef short short8v __attribute__((ext_vector_type(8)));
     return __builtin_bit_cast(frag, short8v{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
   } else {
+    const int lane = (int)threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     frag o;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      o[j] = *reinterpret_cast<const float*>(tile + TL::place(r0 + 4 * g + (j & 3) + 16 * (j >> 2), 4 * f + (n >> 2)) + (n & 3) * 4);
+      o[j] = *reinterpret_cast<const float*>(tiles + at + TL::place(r0 + 4 * g + (j & 3) + 16 * (j >> 2), 4 * f + (n >> 2)) + (n & 3) * 4);
     return o;
   }
 }
@@ -158,20 +203,45 @@ __device__ __forceinline__ void store_column(const Strided& s, int64_t row, int 
   }
 }
 
-// Weights of binary16 calls are held times 2^14, so that small ones keep their bits.
-template <class T> constexpr float weight_unit() { return __is_same(T, _Float16) ? 14.0f : 0.0f; }
+// Weights of binary16 calls are held times 2^7, so that small ones keep their bits.
+template <class T> constexpr float weight_unit() { return __is_same(T, _Float16) ? 7.0f : 0.0f; }
+template <bool B> struct Constant { static constexpr bool value = B; };
 
-template <class T, int DP, int QT, int BK, int WAVES_EU>
-__global__ __launch_bounds__(kThreads, WAVES_EU) void prompt_forward(PromptArgs a) {
+// Asks the compiler to keep 8 reads from the LDS ahead of a step's matrix instructions: FIRST reads with EACH of them behind every
+// read, then SECOND with EACH behind every SECOND_STEP.  Left to itself it reads two operands and waits for them (dK and dV of
+// 10239 tokens, 32 heads of 128: 720 us, 612 with this).
+template <int FIRST, int SECOND, int EACH, int SECOND_STEP> __device__ __forceinline__ void interleave() {
+  constexpr int kAhead = 8 < FIRST ? 8 : FIRST, kRead = 0x100, kMatrix = 0x008;
+  __builtin_amdgcn_sched_group_barrier(kRead, kAhead, 0);
+#pragma unroll
+  for (int i = 0; i < FIRST - kAhead; ++i) {
+    __builtin_amdgcn_sched_group_barrier(kMatrix, EACH, 0);
+    __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
+  }
+#pragma unroll
+  for (int i = 0; i < SECOND / SECOND_STEP; ++i) {
+    __builtin_amdgcn_sched_group_barrier(kMatrix, EACH, 0);
+    __builtin_amdgcn_sched_group_barrier(kRead, SECOND_STEP, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(kMatrix, kAhead * EACH, 0);
+}
+
+// A row's running maximum (base 2) may be passed by this much before sums are scaled down to a new one: weights stay below 2^8
+// (binary16: 2^15).  Without it most steps of a long sequence have a row of the wave's 32 whose maximum moves.
+constexpr float kSlack = 8.0f;
+
+template <class T, int DP, int QT, int BK, int WAVES, int OCCUPANCY, bool DIRECT>
+__global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptArgs a) {
   typedef typename MatrixOf<T>::type M;
   typedef typename M::frag frag;
   typedef TileOf<T, DP> TL;
-  constexpr int KS = DP / 32, F = DP / 16, TT = BK / 16, kRows = 64 * QT, kTile = BK * TL::kRowBytes;
-  extern __shared__ __attribute__((aligned(128))) char tiles[];  // [2][keys, values], [2] flags
-  int* const odd_flags = reinterpret_cast<int*>(tiles + 4 * kTile);
+  typedef Loader<T, DP, BK, WAVES, DIRECT> Load;
+  constexpr int KS = DP / 32, F = DP / 16, TT = BK / 16, kRows = 16 * WAVES * QT, kTile = BK * TL::kRowBytes;
+  extern __shared__ __attribute__((aligned(1024))) char tiles[];  // [2][keys, values], a flag
+  int* const odd_flag = reinterpret_cast<int*>(tiles + 4 * kTile);
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const int turn = (int)(blockIdx.x % (uint32_t)a.heads), kv_head = turn % a.kv_heads, head = kv_head * a.group + turn / a.kv_heads;
-  Tile tile = find_tile(a.queries, blockIdx.x / (uint32_t)a.heads, 1, kRows);
+  const Tile tile = find_tile(a.queries, blockIdx.x / (uint32_t)a.heads, 1, kRows);
   if (tile.sequence < 0) return;
   // the longest tiles of a causal sequence first
   const int seq = tile.sequence, first = (tile.tiles - 1 - tile.index) * kRows;
@@ -189,10 +259,10 @@ __global__ __launch_bounds__(kThreads, WAVES_EU) void prompt_forward(PromptArgs 
     seen[t] = live ? sees(r) : 0;
     own_operand<T, KS>(q[t], a.q, q0 + (live ? r : 0), head, live, a.dim);
   }
-  const int wave_least = mine < rows ? sees(mine) : keys;  // keys that all rows of the wave see
   const int wave_most = mine < rows ? sees(min(mine + 16 * QT, rows) - 1) : 0;
-  const int most = sees(min(first + kRows, rows) - 1), least = sees(first);
+  const int most = sees(min(first + kRows, rows) - 1);
   const int steps = (most + BK - 1) / BK;
+  const int whole = first + kRows <= rows ? sees(first) / BK : 0;  // steps of which all rows see all keys
 
   float4v o[QT][F];
   float largest[QT], sum[QT];
@@ -202,116 +272,138 @@ __global__ __launch_bounds__(kThreads, WAVES_EU) void prompt_forward(PromptArgs 
 #pragma unroll
     for (int f = 0; f < F; ++f) o[t][f] = float4v{0, 0, 0, 0};
   }
-  Staged<T, DP, BK> sk, sv;
-  auto put = [&](int j) {
+  const uint32_t k_bytes = (uint32_t)a.k.row * sizeof(T), v_bytes = (uint32_t)a.v.row * sizeof(T);
+  const char* const k_from = (const char*)element<T>(a.k, k0, kv_head);
+  const char* const v_from = (const char*)element<T>(a.v, k0, kv_head);
+  Load lk, lv;
+  const Lanes<T, DP> at;
+  lk.begin(k_bytes, a.dim);
+  lv.begin(v_bytes, a.dim);
+  auto issue = [&](int j) {
     char* at = tiles + (j & 1) * 2 * kTile;
-    sk.store(at);
-    sv.store(at + kTile);
-    // a value that some row of the workgroup does not see
-    if ((j + 1) * BK > least && lanes_where(sv.odd()) && lane == 0) odd_flags[j & 1] = j + 1;
+    lk.issue(k_from + (int64_t)j * BK * k_bytes, at, keys - j * BK, k_bytes, a.dim);
+    lv.issue(v_from + (int64_t)j * BK * v_bytes, at + kTile, keys - j * BK, v_bytes, a.dim);
   };
-  if (threadIdx.x < 2) odd_flags[threadIdx.x] = 0;
+  auto land = [&](int j) {
+    char* at = tiles + (j & 1) * 2 * kTile;
+    lk.land(at);
+    lv.land(at + kTile);
+    if (DIRECT) tiles_are_here();
+  };
   if (steps > 0) {
-    sk.load(a.k, k0, kv_head, keys, a.dim);
-    sv.load(a.v, k0, kv_head, keys, a.dim);
+    issue(0);
+    land(0);
   }
   __syncthreads();
-  if (steps > 0) put(0);
-  __syncthreads();
-#pragma unroll 1
-  for (int j = 0; j < steps; ++j) {
-    if (j + 1 < steps) {
-      sk.load(a.k, k0 + (j + 1) * BK, kv_head, keys - (j + 1) * BK, a.dim);
-      sv.load(a.v, k0 + (j + 1) * BK, kv_head, keys - (j + 1) * BK, a.dim);
+
+  auto step = [&](int j, auto some_hidden) {
+    constexpr bool kHidden = decltype(some_hidden)::value;
+    const int kt = at.row + (j & 1) * 2 * kTile, vt = at.turned + (j & 1) * 2 * kTile + kTile;
+    bool odd = false;
+    if constexpr (kHidden) {
+      // a weight of 0 would not keep an infinity or NaN of a hidden value out
+      if (threadIdx.x == 0) *odd_flag = 0;
+      __syncthreads();
+      if (lanes_where(Load::odd(tiles + (j & 1) * 2 * kTile + kTile)) && lane == 0) *odd_flag = 1;
+      __syncthreads();
+      odd = __builtin_amdgcn_readfirstlane(*odd_flag) != 0;
+      if (j * BK >= wave_most) return;
     }
-    const char* kt = tiles + (j & 1) * 2 * kTile;
-    const char* vt = kt + kTile;
-    if (j * BK < wave_most) {
-      float4v s[TT][QT];
+    float4v s[TT][QT];
 #pragma unroll
-      for (int tt = 0; tt < TT; ++tt) {
+    for (int tt = 0; tt < TT; ++tt) {
 #pragma unroll
-        for (int t = 0; t < QT; ++t) s[tt][t] = float4v{0, 0, 0, 0};
+      for (int t = 0; t < QT; ++t) s[tt][t] = float4v{0, 0, 0, 0};
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const frag k = row_operand<T, DP>(kt, 16 * tt, ks);
+      for (int ks = 0; ks < KS; ++ks) {
+        const frag k = row_operand<T, DP>(tiles, kt, 16 * tt, ks);
 #pragma unroll
-          for (int t = 0; t < QT; ++t) s[tt][t] = M::mma(k, q[t][ks], s[tt][t]);
-        }
+        for (int t = 0; t < QT; ++t) s[tt][t] = M::mma(k, q[t][ks], s[tt][t]);
       }
-      const bool some_hidden = (j + 1) * BK > wave_least;
-      if (some_hidden) {
+    }
+    if constexpr (kHidden) {
 #pragma unroll
-        for (int tt = 0; tt < TT; ++tt)
+      for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
-          for (int t = 0; t < QT; ++t)
+        for (int t = 0; t < QT; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (j * BK + 16 * tt + 4 * g + i >= seen[t]) s[tt][t][i] = -kInfinity;
-      }
+          for (int i = 0; i < 4; ++i)
+            if (j * BK + 16 * tt + 4 * g + i >= seen[t]) s[tt][t][i] = -kInfinity;
+    }
 #pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        float m = s[0][t][0];
+    for (int t = 0; t < QT; ++t) {
+      float m = s[0][t][0];
 #pragma unroll
-        for (int tt = 0; tt < TT; ++tt)
+      for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) m = fmaxf(m, s[tt][t][i]);
-        m = over_groups_max(m) * a.scale2;
-        if (lanes_where(m > largest[t])) {
-          const float more = fmaxf(m, largest[t]);
-          const float shrink = more == -kInfinity ? 1.0f : exp2_fast(largest[t] - more);
-          sum[t] *= shrink;
-#pragma unroll
-          for (int f = 0; f < F; ++f)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[t][f][i] *= shrink;
-          largest[t] = more;
-        }
-        const float base = largest[t] == -kInfinity ? 0.0f : weight_unit<T>() - largest[t];
-#pragma unroll
-        for (int tt = 0; tt < TT; ++tt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            s[tt][t][i] = exp2_fast(__builtin_fmaf(s[tt][t][i], a.scale2, base));
-            sum[t] += s[tt][t][i];
-          }
-      }
-      frag p[QT][TT / 2];
-#pragma unroll
-      for (int t = 0; t < QT; ++t)
-#pragma unroll
-        for (int kk = 0; kk < TT / 2; ++kk) p[t][kk] = as_operand<T>(s[2 * kk][t], s[2 * kk + 1][t]);
-      const bool odd = some_hidden && __builtin_amdgcn_readfirstlane(odd_flags[j & 1]) == j + 1;
-      if (!odd) {
+        for (int i = 0; i < 4; ++i) m = fmaxf(m, s[tt][t][i]);
+      m = over_groups_max(m) * a.scale2;
+      if (lanes_where(m > largest[t] + kSlack)) {
+        const float more = fmaxf(m, largest[t]);
+        const float shrink = more == -kInfinity ? 1.0f : exp2_fast(largest[t] - more);
+        sum[t] *= shrink;
 #pragma unroll
         for (int f = 0; f < F; ++f)
 #pragma unroll
-          for (int kk = 0; kk < TT / 2; ++kk) {
-            const frag v = turned_operand<T, DP>(vt, 32 * kk, f);
-#pragma unroll
-            for (int t = 0; t < QT; ++t) o[t][f] = M::mma(v, p[t][kk], o[t][f]);
-          }
-      } else {
-        // a weight of 0 would not keep an infinity or NaN out: token by token, rows that do not see it left out
-#pragma unroll
-        for (int kk = 0; kk < TT / 2; ++kk)
-#pragma unroll 1
-          for (int token = 0; token < 32; ++token)
-#pragma unroll
-            for (int f = 0; f < F; ++f) {
-              frag v = turned_operand<T, DP>(vt, 32 * kk, f);
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (4 * g + (e & 3) + 16 * (e >> 2) != token) v[e] = (T)0.0f;
-#pragma unroll
-              for (int t = 0; t < QT; ++t) {
-                const float4v one = M::mma(v, p[t][kk], float4v{0, 0, 0, 0});
-                if (j * BK + 32 * kk + token < seen[t]) o[t][f] += one;
-              }
-            }
+          for (int i = 0; i < 4; ++i) o[t][f][i] *= shrink;
+        largest[t] = more;
       }
+      const float base = largest[t] == -kInfinity ? 0.0f : weight_unit<T>() - largest[t];
+#pragma unroll
+      for (int tt = 0; tt < TT; ++tt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[tt][t][i] = exp2_fast(__builtin_fmaf(s[tt][t][i], a.scale2, base));
+          sum[t] += s[tt][t][i];
+        }
     }
-    if (j + 1 < steps) put(j + 1);
+    frag p[QT][TT / 2];
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int kk = 0; kk < TT / 2; ++kk) p[t][kk] = as_operand<T>(s[2 * kk][t], s[2 * kk + 1][t]);
+    if (!odd) {
+#pragma unroll
+      for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int kk = 0; kk < TT / 2; ++kk) {
+          const frag v = turned_operand<T, DP>(tiles, vt, 32 * kk, f);
+#pragma unroll
+          for (int t = 0; t < QT; ++t) o[t][f] = M::mma(v, p[t][kk], o[t][f]);
+        }
+    } else {
+      // token by token, rows that do not see it left out
+#pragma unroll
+      for (int kk = 0; kk < TT / 2; ++kk)
+#pragma unroll 1
+        for (int token = 0; token < 32; ++token)
+#pragma unroll
+          for (int f = 0; f < F; ++f) {
+            frag v = turned_operand<T, DP>(tiles, vt, 32 * kk, f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (4 * g + (e & 3) + 16 * (e >> 2) != token) v[e] = (T)0.0f;
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+              const float4v one = M::mma(v, p[t][kk], float4v{0, 0, 0, 0});
+              if (j * BK + 32 * kk + token < seen[t]) o[t][f] += one;
+            }
+          }
+    }
+  };
+  int j = 0;
+#pragma unroll 1
+  for (; j < whole; ++j) {
+    if (j + 1 < steps) issue(j + 1);
+    step(j, Constant<false>{});
+    if (j + 1 < steps) land(j + 1);
+    __syncthreads();
+  }
+#pragma unroll 1
+  for (; j < steps; ++j) {
+    if (j + 1 < steps) issue(j + 1);
+    step(j, Constant<true>{});
+    if (j + 1 < steps) land(j + 1);
     __syncthreads();
   }
 #pragma unroll
@@ -352,13 +444,21 @@ __device__ __forceinline__ int gradient_exponent(uint32_t top) {
 
 // KEYS: the workgroup owns keys and values and walks over queries (dK, dV); otherwise it owns queries and walks over keys (dQ).
 // First operands: keys and queries; second: values and the output's gradient.
-template <class T, int DP, int OT, int BS, bool KEYS>
-__global__ __launch_bounds__(kThreads) void prompt_backward(PromptArgs a) {
+//
+// delta.  dS's rows add up to 0.  delta from the output as it was stored is off by its rounding (and the weights' in it), by
+// the same for all of a row's keys: with binary16 and bfloat16 as much as everything else together (dQ and dK of 1024
+// causal tokens of 128: 2.7e-3 off, 2.3e-3 without it, 1.7e-3 the rounding of the result).  So the dQ kernel adds up its dS in
+// binary32 and P K beside dS K: sum dS = delta's error, which it takes off both dQ and delta, before the other kernel reads it.  One
+// product more, of operands that are there.
+template <class T, int DP, int OT, int BS, int WAVES, int OCCUPANCY, bool KEYS, bool DIRECT>
+__global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_backward(PromptArgs a) {
   typedef typename MatrixOf<T>::type M;
   typedef typename M::frag frag;
   typedef TileOf<T, DP> TL;
-  constexpr int KS = DP / 32, F = DP / 16, TT = BS / 16, kRows = 64 * OT, kTile = BS * TL::kRowBytes;
-  extern __shared__ __attribute__((aligned(128))) char tiles[];  // [2][first, second], [2][2][BS] row statistics
+  typedef Loader<T, DP, BS, WAVES, DIRECT> Load;
+  constexpr bool kMend = !KEYS && sizeof(T) == 2, kSecond = KEYS || kMend;
+  constexpr int KS = DP / 32, F = DP / 16, TT = BS / 16, kRows = 16 * WAVES * OT, kTile = BS * TL::kRowBytes;
+  extern __shared__ __attribute__((aligned(1024))) char tiles[];  // [2][first, second], [2][2][BS] row statistics
   float* const stats = reinterpret_cast<float*>(tiles + 4 * kTile);
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const uint32_t heads = (uint32_t)(KEYS ? a.kv_heads : a.heads);
@@ -372,7 +472,7 @@ __global__ __launch_bounds__(kThreads) void prompt_backward(PromptArgs a) {
   const int rows = real || !KEYS ? a.queries.length(min(seq, a.queries.count)) : 0, q0 = a.queries.start(min(seq, a.queries.count));
   const int keys = real || KEYS ? a.keys.length(min(seq, a.keys.count)) : 0, k0 = a.keys.start(min(seq, a.keys.count));
   const int own_count = KEYS ? keys : rows, own0 = KEYS ? k0 : q0;
-  const int walk_count = KEYS ? (real ? rows : 0) : (real ? keys : 0), walk0 = KEYS ? q0 : k0;
+  const int walk_count = real ? (KEYS ? rows : keys) : 0, walk0 = KEYS ? q0 : k0;
   const int shift = keys - rows;  // query i sees key j if j <= i + shift
   const Strided& own1 = KEYS ? a.k : a.q;
   const Strided& own2 = KEYS ? a.v : a.d_o;
@@ -381,7 +481,7 @@ __global__ __launch_bounds__(kThreads) void prompt_backward(PromptArgs a) {
 
   const int mine = first + wave * 16 * OT;
   frag x1[OT][KS], x2[OT][KS];
-  float own_lse[OT], own_delta[OT];
+  float own_lse[OT], own_delta[OT], own_left[OT];
 #pragma unroll
   for (int t = 0; t < OT; ++t) {
     const int r = mine + 16 * t + n;
@@ -390,20 +490,20 @@ __global__ __launch_bounds__(kThreads) void prompt_backward(PromptArgs a) {
     const int head = KEYS ? kv_head : head0;
     own_operand<T, KS>(x1[t], own1, at, head, live, a.dim);
     own_operand<T, KS>(x2[t], own2, at, head, live, a.dim);
-    own_lse[t] = own_delta[t] = 0.0f;
+    own_lse[t] = own_delta[t] = own_left[t] = 0.0f;
     if (!KEYS && live) {
       const float l = a.lse[(int64_t)head0 * a.queries.rows + at];
       own_lse[t] = l == -kInfinity ? kInfinity : l * kLog2E;
       own_delta[t] = a.delta[(int64_t)head0 * a.queries.rows + at];
     }
   }
-  float4v acc1[OT][F], acc2[KEYS ? OT : 1][KEYS ? F : 1];
+  float4v acc1[OT][F], acc2[kSecond ? OT : 1][kSecond ? F : 1];
 #pragma unroll
   for (int t = 0; t < OT; ++t)
 #pragma unroll
     for (int f = 0; f < F; ++f) {
       acc1[t][f] = float4v{0, 0, 0, 0};
-      if constexpr (KEYS) acc2[t][f] = float4v{0, 0, 0, 0};
+      if constexpr (kSecond) acc2[t][f] = float4v{0, 0, 0, 0};
     }
   int ds_e = 126;
 
@@ -416,40 +516,41 @@ __global__ __launch_bounds__(kThreads) void prompt_backward(PromptArgs a) {
   const int per_head = to > from ? (to - from + BS - 1) / BS : 0;
   const int steps = KEYS ? per_head * a.group : per_head;
 
-  Staged<T, DP, BS> s1, s2;
+  const uint32_t bytes1 = (uint32_t)walk1.row * sizeof(T), bytes2 = (uint32_t)walk2.row * sizeof(T);
+  const char* const from1 = (const char*)element<T>(walk1, walk0, KEYS ? head0 : kv_head);
+  const char* const from2 = (const char*)element<T>(walk2, walk0, KEYS ? head0 : kv_head);
+  Load l1, l2;
+  const Lanes<T, DP> lanes;
+  l1.begin(bytes1, a.dim);
+  l2.begin(bytes2, a.dim);
   float row_stat = 0.0f;
-  auto load = [&](int j) {
-    const int member = KEYS ? j / per_head : 0, at = from + (j - member * per_head) * BS;
-    const int head = KEYS ? head0 + member : kv_head;
-    s1.load(walk1, walk0 + at, head, walk_count - at, a.dim);
-    s2.load(walk2, walk0 + at, head, walk_count - at, a.dim);
+  int next_at = from, next_member = 0;  // of the tile that is on its way
+  auto issue = [&](int j) {
+    char* to_tile = tiles + (j & 1) * 2 * kTile;
+    l1.issue(from1 + (int64_t)next_at * bytes1 + (KEYS ? (int64_t)next_member * walk1.head * (int64_t)sizeof(T) : 0), to_tile, walk_count - next_at, bytes1, a.dim);
+    l2.issue(from2 + (int64_t)next_at * bytes2 + (KEYS ? (int64_t)next_member * walk2.head * (int64_t)sizeof(T) : 0), to_tile + kTile, walk_count - next_at, bytes2, a.dim);
     if (KEYS && threadIdx.x < 2 * BS) {
-      const int r = at + (int)threadIdx.x % BS;
-      row_stat = 0.0f;
-      if (r < walk_count) {
-        const float* p = (int)threadIdx.x < BS ? a.lse : a.delta;
-        row_stat = p[(int64_t)head * a.queries.rows + walk0 + r];
-        if ((int)threadIdx.x < BS) row_stat = row_stat == -kInfinity ? kInfinity : row_stat * kLog2E;
-      }
+      const int r = min(next_at + (int)threadIdx.x % BS, walk_count - 1);
+      const float* p = (int)threadIdx.x < BS ? a.lse : a.delta;
+      row_stat = p[(int64_t)(head0 + next_member) * a.queries.rows + walk0 + r];
     }
   };
-  auto put = [&](int j) {
+  auto land = [&](int j) {
     char* at = tiles + (j & 1) * 2 * kTile;
-    s1.store(at);
-    s2.store(at + kTile);
-    if (KEYS && threadIdx.x < 2 * BS) stats[(j & 1) * 2 * BS + threadIdx.x] = row_stat;
+    l1.land(at);
+    l2.land(at + kTile);
+    if (KEYS && threadIdx.x < 2 * BS)
+      stats[(j & 1) * 2 * BS + threadIdx.x] = (int)threadIdx.x >= BS ? row_stat : row_stat == -kInfinity ? kInfinity : row_stat * kLog2E;
+    if (DIRECT) tiles_are_here();
   };
   if (steps > 0) {
-    load(0);
-    put(0);
+    issue(0);
+    land(0);
   }
   __syncthreads();
-#pragma unroll 1
-  for (int j = 0; j < steps; ++j) {
-    if (j + 1 < steps) load(j + 1);
-    const int member = KEYS ? j / per_head : 0, at = from + (j - member * per_head) * BS;
-    const char* t1 = tiles + (j & 1) * 2 * kTile;
-    const char* t2 = t1 + kTile;
+  auto step = [&](int j, int at, auto hidden) {
+    constexpr bool kHidden = decltype(hidden)::value;
+    const int t1 = (j & 1) * 2 * kTile, t2 = t1 + kTile, rows1 = lanes.row + t1, rows2 = lanes.row + t2;
     // scores (base 2) and dO V^T: rows are the tile's, columns ours
     float4v s[TT][OT], d[TT][OT];
 #pragma unroll
@@ -458,7 +559,7 @@ __global__ __launch_bounds__(kThreads) void prompt_backward(PromptArgs a) {
       for (int t = 0; t < OT; ++t) s[tt][t] = d[tt][t] = float4v{0, 0, 0, 0};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const frag y1 = row_operand<T, DP>(t1, 16 * tt, ks), y2 = row_operand<T, DP>(t2, 16 * tt, ks);
+        const frag y1 = row_operand<T, DP>(tiles, rows1, 16 * tt, ks), y2 = row_operand<T, DP>(tiles, rows2, 16 * tt, ks);
 #pragma unroll
         for (int t = 0; t < OT; ++t) {
           s[tt][t] = M::mma(y1, x1[t][ks], s[tt][t]);
@@ -466,8 +567,6 @@ __global__ __launch_bounds__(kThreads) void prompt_backward(PromptArgs a) {
         }
       }
     }
-    bool some_hidden = at + BS > walk_count || mine + 16 * OT > own_count;
-    if (a.causal) some_hidden = some_hidden || (KEYS ? mine + 16 * OT - 1 > at + shift : at + BS - 1 > mine + shift);
 #pragma unroll
     for (int tt = 0; tt < TT; ++tt) {
       float4v tile_lse, tile_delta;
@@ -482,7 +581,7 @@ __global__ __launch_bounds__(kThreads) void prompt_backward(PromptArgs a) {
           const float lse = KEYS ? tile_lse[i] : own_lse[t], delta = KEYS ? tile_delta[i] : own_delta[t];
           float p = exp2_fast(__builtin_fmaf(s[tt][t][i], a.scale2, weight_unit<T>() - lse));
           float ds = p * (d[tt][t][i] - delta);
-          if (some_hidden) {
+          if constexpr (kHidden) {
             const int theirs = at + 16 * tt + 4 * g + i, ours = mine + 16 * t + n;
             const int query = KEYS ? theirs : ours, key = KEYS ? ours : theirs;
             const bool visible = query < rows && key < keys && (!a.causal || key <= query + shift);
@@ -491,6 +590,7 @@ __global__ __launch_bounds__(kThreads) void prompt_backward(PromptArgs a) {
           }
           s[tt][t][i] = p;
           d[tt][t][i] = ds;
+          if constexpr (kMend) own_left[t] += ds;
         }
     }
     if constexpr (__is_same(T, _Float16)) {
@@ -529,98 +629,126 @@ __global__ __launch_bounds__(kThreads) void prompt_backward(PromptArgs a) {
 #pragma unroll
       for (int t = 0; t < OT; ++t) {
         ds[t] = as_operand<T>(d[2 * kk][t], d[2 * kk + 1][t]);
-        if constexpr (KEYS) p[t] = as_operand<T>(s[2 * kk][t], s[2 * kk + 1][t]);
+        if constexpr (kSecond) p[t] = as_operand<T>(s[2 * kk][t], s[2 * kk + 1][t]);
       }
 #pragma unroll
       for (int f = 0; f < F; ++f) {
-        const frag y1 = turned_operand<T, DP>(t1, 32 * kk, f);
+        const frag y1 = turned_operand<T, DP>(tiles, lanes.turned + t1, 32 * kk, f);
 #pragma unroll
         for (int t = 0; t < OT; ++t) acc1[t][f] = M::mma(y1, ds[t], acc1[t][f]);
-        if constexpr (KEYS) {
-          const frag y2 = turned_operand<T, DP>(t2, 32 * kk, f);
+        if constexpr (kSecond) {
+          const frag y2 = kMend ? y1 : turned_operand<T, DP>(tiles, lanes.turned + t2, 32 * kk, f);
 #pragma unroll
           for (int t = 0; t < OT; ++t) acc2[t][f] = M::mma(y2, p[t], acc2[t][f]);
         }
       }
     }
-    if (j + 1 < steps) put(j + 1);
+    if constexpr (!kHidden && sizeof(T) == 2) interleave<TT * KS * 2, F * (TT / 2) * (KEYS ? 4 : 2), OT, KEYS ? 2 : 1>();
+  };
+  // Loops of their own for steps with hidden pairs and for those without: together in one, sums move between registers at each step.
+  int at = from, member = 0, j = 0;
+  auto some_hidden = [&]() {
+    const bool end = at + BS > walk_count || mine + 16 * OT > own_count;
+    return end || (a.causal && (KEYS ? mine + 16 * OT - 1 > at + shift : at + BS - 1 > mine + shift));
+  };
+  auto one = [&](auto hidden) {
+    next_at = at + BS, next_member = member;
+    if (KEYS && next_at >= to) next_at = from, next_member = member + 1;
+    if (j + 1 < steps) issue(j + 1);
+    step(j, at, hidden);
+    if (j + 1 < steps) land(j + 1);
     __syncthreads();
+    at = next_at, member = next_member;
+    ++j;
+  };
+#pragma unroll 1
+  while (j < steps) {
+#pragma unroll 1
+    while (j < steps && !some_hidden()) one(Constant<false>{});
+#pragma unroll 1
+    while (j < steps && some_hidden()) one(Constant<true>{});
   }
+  constexpr float kUnit = __is_same(T, _Float16) ? 1.0f / 128.0f : 1.0f;
 #pragma unroll
   for (int t = 0; t < OT; ++t) {
     const int r = mine + 16 * t + n;
+    const float left = kMend ? over_groups_sum(own_left[t]) * kUnit : 0.0f;
     if (r >= own_count) continue;
-    float by = a.scale;
     if constexpr (__is_same(T, _Float16)) {
 #pragma unroll
       for (int f = 0; f < F; ++f)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc1[t][f][i] = ldexpf(acc1[t][f][i], -ds_e - (int)weight_unit<T>());
     }
-    store_column<T, F>(KEYS ? a.dk : a.dq, own0 + r, KEYS ? kv_head : head0, a.dim, acc1[t], by);
-    if constexpr (KEYS) store_column<T, F>(a.dv, own0 + r, kv_head, a.dim, acc2[t], __is_same(T, _Float16) ? 0.00006103515625f : 1.0f);
+    if constexpr (kMend) {
+#pragma unroll
+      for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc1[t][f][i] -= left * (acc2[t][f][i] * kUnit);
+      if (g == 0) a.delta[(int64_t)head0 * a.queries.rows + own0 + r] = own_delta[t] + left;
+    }
+    store_column<T, F>(KEYS ? a.dk : a.dq, own0 + r, KEYS ? kv_head : head0, a.dim, acc1[t], a.scale);
+    if constexpr (KEYS) store_column<T, F>(a.dv, own0 + r, kv_head, a.dim, acc2[t], kUnit);
   }
 }
 
-// Rows a wave owns and rows of a tile, by type and (padded) head size: what fits registers and LDS.
-struct PromptShape {
-  int rows;       // of a workgroup
-  int walked;     // of a tile
-  size_t lds;
-};
 typedef void (*prompt_t)(PromptArgs);
 struct PromptKernel {
   prompt_t run;
-  PromptShape shape;
+  int rows;     // of a workgroup
+  int threads;
+  size_t lds;
 };
 
-template <class T, int DP, int QT, int BK, int WAVES_EU> PromptKernel forward_of() {
-  return {prompt_forward<T, DP, QT, BK, WAVES_EU>, {64 * QT, BK, (size_t)4 * BK * TileOf<T, DP>::kRowBytes + 16}};
+template <class T, int DP, int QT, int BK, int WAVES, int OCCUPANCY> PromptKernel forward_of(bool direct) {
+  return {direct ? prompt_forward<T, DP, QT, BK, WAVES, OCCUPANCY, true> : prompt_forward<T, DP, QT, BK, WAVES, OCCUPANCY, false>, 16 * WAVES * QT,
+          64 * WAVES, (size_t)4 * BK * TileOf<T, DP>::kRowBytes + 16};
 }
-template <class T, int DP, int OT, int BS, bool KEYS> PromptKernel backward_of() {
-  return {prompt_backward<T, DP, OT, BS, KEYS>, {64 * OT, BS, (size_t)4 * BS * TileOf<T, DP>::kRowBytes + 16 * BS}};
+template <class T, int DP, int OT, int BS, int WAVES, int OCCUPANCY, bool KEYS> PromptKernel backward_of(bool direct) {
+  return {direct ? prompt_backward<T, DP, OT, BS, WAVES, OCCUPANCY, KEYS, true> : prompt_backward<T, DP, OT, BS, WAVES, OCCUPANCY, KEYS, false>,
+          16 * WAVES * OT, 64 * WAVES, (size_t)4 * BS * TileOf<T, DP>::kRowBytes + 16 * BS};
 }
 
-// By the head's size.
-PromptKernel prompt_forward_bf16(int dim);
-PromptKernel prompt_forward_f16(int dim);
-PromptKernel prompt_forward_f32(int dim);
-PromptKernel prompt_keys_bf16(int dim);
-PromptKernel prompt_keys_f16(int dim);
-PromptKernel prompt_keys_f32(int dim);
-PromptKernel prompt_queries_bf16(int dim);
-PromptKernel prompt_queries_f16(int dim);
-PromptKernel prompt_queries_f32(int dim);
+// By the head's size; `direct`: what is walked over lies at multiples of 16 bytes.
+PromptKernel prompt_forward_bf16(int dim, bool direct);
+PromptKernel prompt_forward_f16(int dim, bool direct);
+PromptKernel prompt_forward_f32(int dim, bool direct);
+PromptKernel prompt_keys_bf16(int dim, bool direct);
+PromptKernel prompt_keys_f16(int dim, bool direct);
+PromptKernel prompt_keys_f32(int dim, bool direct);
+PromptKernel prompt_queries_bf16(int dim, bool direct);
+PromptKernel prompt_queries_f16(int dim, bool direct);
+PromptKernel prompt_queries_f32(int dim, bool direct);
 prompt_t prompt_delta_kernel(int type);
 
-template <class T> PromptKernel forward_for(int dim) {
+template <class T> PromptKernel forward_for(int dim, bool direct) {
   if constexpr (sizeof(T) == 2) {
-    if (dim <= 64) return forward_of<T, 64, 2, 64, 2>();
-    if (dim <= 96) return forward_of<T, 96, 2, 64, 2>();
-    if (dim <= 128) return forward_of<T, 128, 2, 64, 2>();
-    if (dim <= 192) return forward_of<T, 192, 1, 32, 2>();
-    return forward_of<T, 256, 1, 32, 2>();
+    if (dim <= 64) return forward_of<T, 64, 2, 64, 4, 2>(direct);
+    if (dim <= 96) return forward_of<T, 96, 2, 64, 4, 2>(direct);
+    if (dim <= 128) return forward_of<T, 128, 2, 64, 4, 2>(direct);
+    if (dim <= 192) return forward_of<T, 192, 1, 32, 4, 2>(direct);
+    return forward_of<T, 256, 1, 32, 4, 2>(direct);
   } else {
-    if (dim <= 64) return forward_of<T, 64, 1, 32, 2>();
-    if (dim <= 96) return forward_of<T, 96, 1, 32, 2>();
-    if (dim <= 128) return forward_of<T, 128, 1, 32, 2>();
-    if (dim <= 192) return forward_of<T, 192, 1, 32, 1>();
-    return forward_of<T, 256, 1, 32, 1>();
+    if (dim <= 64) return forward_of<T, 64, 1, 32, 4, 2>(direct);
+    if (dim <= 96) return forward_of<T, 96, 1, 32, 4, 2>(direct);
+    if (dim <= 128) return forward_of<T, 128, 1, 32, 4, 2>(direct);
+    if (dim <= 192) return forward_of<T, 192, 1, 32, 4, 1>(direct);
+    return forward_of<T, 256, 1, 32, 4, 1>(direct);
   }
 }
-template <class T, bool KEYS> PromptKernel backward_for(int dim) {
+template <class T, bool KEYS> PromptKernel backward_for(int dim, bool direct) {
   if constexpr (sizeof(T) == 2) {
-    if (dim <= 64) return backward_of<T, 64, 2, 32, KEYS>();
-    if (dim <= 96) return backward_of<T, 96, 2, 64, KEYS>();
-    if (dim <= 128) return backward_of<T, 128, 2, 32, KEYS>();
-    if (dim <= 192) return backward_of<T, 192, 1, 32, KEYS>();
-    return backward_of<T, 256, 1, 32, KEYS>();
+    if (dim <= 64) return backward_of<T, 64, 1, 64, 4, 2, KEYS>(direct);
+    if (dim <= 96) return backward_of<T, 96, 1, 64, 4, 2, KEYS>(direct);
+    if (dim <= 128) return backward_of<T, 128, 1, 64, 4, 2, KEYS>(direct);
+    if (dim <= 192) return backward_of<T, 192, 1, 32, 4, 1, KEYS>(direct);
+    return backward_of<T, 256, 1, 32, 4, 1, KEYS>(direct);
   } else {
-    if (dim <= 64) return backward_of<T, 64, 1, 32, KEYS>();
-    if (dim <= 96) return backward_of<T, 96, 1, 32, KEYS>();
-    if (dim <= 128) return backward_of<T, 128, 1, 32, KEYS>();
-    if (dim <= 192) return backward_of<T, 192, 1, 32, KEYS>();
-    return backward_of<T, 256, 1, 32, KEYS>();
+    if (dim <= 64) return backward_of<T, 64, 1, 32, 4, 2, KEYS>(direct);
+    if (dim <= 96) return backward_of<T, 96, 1, 32, 4, 1, KEYS>(direct);
+    if (dim <= 128) return backward_of<T, 128, 1, 32, 4, 1, KEYS>(direct);
+    if (dim <= 192) return backward_of<T, 192, 1, 32, 4, 1, KEYS>(direct);
+    return backward_of<T, 256, 1, 32, 4, 1, KEYS>(direct);
   }
 }
 
