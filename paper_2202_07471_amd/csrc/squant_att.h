@@ -131,6 +131,8 @@ __device__ __forceinline__ float over_groups_sum(float v) {
   return v + __shfl_xor(v, 32);
 }
 
+template <bool B> struct Constant { static constexpr bool value = B; };
+
 constexpr float kInfinity = __builtin_inff();
 
 }  // namespace att

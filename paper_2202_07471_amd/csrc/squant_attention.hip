@@ -119,7 +119,7 @@ constexpr int64_t kGroups = 2048, kLeastChunk = 256, kMostChunk = 8192;
 bool split_cache(int64_t rows, int32_t heads, const squant_cache_t& c, const squant_paged_t& w, CacheSplit& s) {
   const int group = heads / c.heads;
   const int64_t each = w.sequences ? (rows + w.sequences - 1) / w.sequences : 0;
-  s.rt = each * group > 16 && c.head_dim <= 128 ? 2 : 1;
+  s.rt = each * group > 16 && c.head_dim <= 128 && c.page_size % 16 == 0 ? 2 : 1;
   const int tile = 16 * s.rt;
   s.tiles = w.starts ? tiles_bound(rows, group, tile, w.sequences) : (int64_t)w.sequences * ((group + tile - 1) / tile);
   const int64_t capacity = std::min<int64_t>((int64_t)w.table_width * c.page_size, kMost);
@@ -210,8 +210,9 @@ int squant_cache_attention(const squant_heads_t* h_q, squant_wtype_t type, int64
   if (s.splits > 1) a.stats = (float2*)d_workspace, a.partial = (float*)((char*)d_workspace + s.stats_bytes);
   const int ng = c.head_dim / kGroup;
   const bool wide = type == SQUANT_W_F32;
-  const cache_attention_t k = c.format == SQUANT_OUT_INT4 ? (wide ? cache_attention_int4_2 : cache_attention_int4_1)(ng, s.rt)
-                                                          : (wide ? cache_attention_int8_2 : cache_attention_int8_1)(ng, s.rt);
+  const auto of = c.format == SQUANT_OUT_INT4 ? (wide ? cache_attention_int4_f32 : cache_attention_int4)
+                  : wide ? cache_attention_int8_f32 : type == SQUANT_W_F16 ? cache_attention_int8_f16 : cache_attention_int8_bf16;
+  const cache_attention_t k = of(ng, s.rt, c.page_size % 16 == 0);
   hipStream_t st = (hipStream_t)stream;
   if (int rc = launch(k, s.tiles * c.heads, s.splits, cache_attention_lds(ng, s.rt), st, a)) return rc;
   return s.splits > 1 ? launch(join_splits_kernel(), (rows * heads + kWaves - 1) / kWaves, 1, 0, st, a) : SQUANT_OK;

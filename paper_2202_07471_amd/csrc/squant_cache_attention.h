@@ -6,7 +6,8 @@
 // waves 32 tokens each in turn; a wave reads codes and scales from memory straight into the lanes that multiply them, a block of
 // tokens ahead.  Codes become binary16 numbers code * scale * 2^e with an exponent for the wave (running: a block with a
 // larger scale lowers it, and the output's sums with it), which for 4 bits is exact: 3 bits of a code and 8 of a scale are 11.
-// For 8 bits it rounds to 11 bits (2^-12 of an element); binary32 calls take the remainder as a second plane.  Queries are
+// For 8 bits it would round to 11 bits (2^-12 of an element): binary16 and binary32 calls take the remainder as a second plane
+// (11 drafted tokens' binary16 outputs 5.5e-4 off without it, 2.1e-4 with), bfloat16 ones do without.  Queries are
 // binary16 with an exponent for each row: exact for 16-bit types, two planes for binary32.  Softmax weights
 // are rounded to 11 bits times 2^14 (binary32: two planes).  Sums are binary32.
 //
@@ -54,13 +55,14 @@ template <int FMT, int NG> struct Layout {
   static constexpr int kValueScales = NG == 3 || NG == 6 ? 2 : 1;
 };
 
+// A block of tokens on its way or at work.  `bad`: those whose page is none.
 template <int FMT, int NG> struct Block {
   typedef Layout<FMT, NG> L;
   uint32_t key[2][L::kKeyWords];
   uint32_t value[8][L::kValueWords];
   uint16_t key_scale[2][L::kKeyScales];
   uint16_t value_scale[8][L::kValueScales];
-  int32_t row;  // of token lane % 32, for what is known of it
+  uint32_t bad;
 };
 
 // 8 codes as binary16 integers (times 16 where `sixteen` says so); element order as `slot_element` has it.
@@ -118,8 +120,13 @@ __device__ __forceinline__ uint32_t finite_bits(float v) {
   return m < 0x7f800000u ? m : 0u;
 }
 
-template <int FMT, int NG, int PL, int RT>
-__global__ __launch_bounds__(kThreads) void cache_attention(CacheAttentionArgs a) {
+// Waves a SIMD that the registers are kept for.  The wave waits for memory: three hide it better than two with more loads on their way.
+constexpr int cache_occupancy(int ng, int rt) { return ng <= 2 ? 4 : ng <= 4 && rt == 1 ? 3 : 2; }
+
+// PL: planes of queries and weights; LOW: the remainder of an 8-bit element as well.  HALVES: pages of a multiple of 16 tokens, of
+// which each half of a block has consecutive rows: their addresses are a number for the wave plus one of the lane that stays.
+template <int FMT, int NG, int PL, bool LOW, int RT, bool HALVES>
+__global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_attention(CacheAttentionArgs a) {
   typedef Layout<FMT, NG> L;
   typedef Block<FMT, NG> B;
   constexpr int D = NG * kGroup, F = D / 16, TR = 16 * RT;
@@ -196,70 +203,82 @@ __global__ __launch_bounds__(kThreads) void cache_attention(CacheAttentionArgs a
       }
   }
 
-  // where tokens lie
+  // where tokens lie: pages of the block's halves, or of token t0 + lane % 32
   const uint32_t head_row = (uint32_t)head * (uint32_t)c.page_size;
-  const bool whole_blocks = c.page_size % kTokens == 0;  // a block lies in one page: its rows follow each other
-  auto page_id = [&](int t0) {
-    const int t = min(t0 + (lane & 31), max(length - 1, 0));
-    return length > 0 ? c.table_at(seq, c.page_of(t)) : -1;
-  };
-  auto load_block = [&](B& b, int t0, int32_t id) {
-    const int last = max(length - 1, 0);
-    {
-      const int t = min(t0 + (lane & 31), last);
-      const int32_t r = c.row_of(t, c.page_of(t), id);
-      b.row = r < 0 ? -1 : (int32_t)(r + head_row);
-    }
-    int32_t key_row[2], value_row[8];
-    if (whole_blocks) {
-      const int32_t first = __builtin_amdgcn_readfirstlane(max(b.row, 0));
+  const int last = max(length - 1, 0);
+  auto page_ids = [&](int t0, int32_t (&id)[2]) {
+    if constexpr (HALVES) {
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) key_row[tt] = first + min(16 * tt + n, max(last - t0, 0));
-#pragma unroll
-      for (int j = 0; j < 8; ++j) value_row[j] = first + min(4 * g + (j & 3) + 16 * (j >> 2), max(last - t0, 0));
+      for (int h = 0; h < 2; ++h) id[h] = __builtin_amdgcn_readfirstlane(c.table_at(seq, c.page_of(min(t0 + 16 * h, last))));
     } else {
-      const int32_t r = max(b.row, 0);
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt) key_row[tt] = __shfl(r, 16 * tt + n);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) value_row[j] = __shfl(r, 4 * g + (j & 3) + 16 * (j >> 2));
+      id[0] = id[1] = c.table_at(seq, c.page_of(min(t0 + (lane & 31), last)));
     }
+  };
+  auto load_value = [&](uint32_t (&o)[L::kValueWords], const uint8_t* p) {
+    __builtin_memset(o, 0, sizeof(o));
+    if constexpr (L::kValueBytes % 4 == 0) {
+      struct Words { uint32_t w[L::kValueWords]; };
+      const Words w = *reinterpret_cast<const Words*>(p);
+#pragma unroll
+      for (int i = 0; i < L::kValueWords; ++i) o[i] = w.w[i];
+    } else if constexpr (L::kValueBytes == 6) {
+      struct Halves { uint16_t w[3]; };
+      const Halves w = *reinterpret_cast<const Halves*>(p);
+      o[0] = w.w[0] | (uint32_t)w.w[1] << 16;
+      o[1] = w.w[2];
+    } else if constexpr (L::kValueBytes == 2) {
+      o[0] = *reinterpret_cast<const uint16_t*>(p);
+    } else if constexpr (L::kValueBytes == 3) {
+      o[0] = p[0] | (uint32_t)p[1] << 8 | (uint32_t)p[2] << 16;
+    } else {
+      static_assert(L::kValueBytes == 1, "");
+      o[0] = p[0];
+    }
+  };
+  // codes and scales of key token 16 tt + n and of value token 4 g + j (j < 4), 16 + 4 g + j - 4, by their rows
+  auto load_rows = [&](B& b, auto row_of) {
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
       struct Words { uint32_t w[L::kKeyWords]; };
-      const Words w = load_any<Words>(c.codes[0] + (int64_t)key_row[tt] * L::kRow + g * (L::kRow / 4));
+      const auto at = row_of(tt, n, g * (L::kRow / 4));
+      const Words w = load_any<Words>(c.codes[0] + at.bytes);
 #pragma unroll
       for (int i = 0; i < L::kKeyWords; ++i) b.key[tt][i] = w.w[i];
-      const uint16_t* s = c.scales[0] + (int64_t)key_row[tt] * NG;
 #pragma unroll
-      for (int k = 0; k < L::kKeyScales; ++k) b.key_scale[tt][k] = s[min(((g * NG) >> 2) + k, NG - 1)];
+      for (int k = 0; k < L::kKeyScales; ++k) b.key_scale[tt][k] = c.scales[0][at.scales + min(((g * NG) >> 2) + k, NG - 1)];
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      struct Bytes { uint8_t w[L::kValueBytes]; };
-      const uint8_t* p = c.codes[1] + (int64_t)value_row[j] * L::kRow + n * L::kValueBytes;
-      __builtin_memset(b.value[j], 0, sizeof(b.value[j]));
-      if constexpr (L::kValueBytes % 4 == 0) {
-        struct Words { uint32_t w[L::kValueWords]; };
-        const Words w = *reinterpret_cast<const Words*>(p);
+      const auto at = row_of(j >> 2, 4 * g + (j & 3), n * L::kValueBytes);
+      load_value(b.value[j], c.codes[1] + at.bytes);
 #pragma unroll
-        for (int i = 0; i < L::kValueWords; ++i) b.value[j][i] = w.w[i];
-      } else if constexpr (L::kValueBytes == 6) {
-        struct Halves { uint16_t w[3]; };
-        const Halves w = *reinterpret_cast<const Halves*>(p);
-        b.value[j][0] = w.w[0] | (uint32_t)w.w[1] << 16;
-        b.value[j][1] = w.w[2];
-      } else if constexpr (L::kValueBytes == 2) {
-        b.value[j][0] = *reinterpret_cast<const uint16_t*>(p);
-      } else if constexpr (L::kValueBytes == 3) {
-        b.value[j][0] = p[0] | (uint32_t)p[1] << 8 | (uint32_t)p[2] << 16;
-      } else {
-        static_assert(L::kValueBytes == 1, "");
-        b.value[j][0] = p[0];
+      for (int k = 0; k < L::kValueScales; ++k) b.value_scale[j][k] = c.scales[1][at.scales + min(((2 * NG * n) >> 5) + k, NG - 1)];
+    }
+  };
+  struct Place { int64_t bytes, scales; };
+  auto load_block = [&](B& b, int t0, const int32_t (&id)[2]) {
+    if constexpr (HALVES) {
+      int64_t first[2];
+      b.bad = 0;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int t = min(t0 + 16 * h, last);
+        const int32_t r = c.row_of(t / 16 * 16, c.page_of(t), id[h]);
+        if (r < 0) b.bad |= 0xffffu << (16 * h);
+        first[h] = r < 0 ? 0 : (int64_t)(r + head_row);  // rows 0 to 15 are there
       }
-      const uint16_t* s = c.scales[1] + (int64_t)value_row[j] * NG;
-#pragma unroll
-      for (int k = 0; k < L::kValueScales; ++k) b.value_scale[j][k] = s[min(((2 * NG * n) >> 5) + k, NG - 1)];
+      load_rows(b, [&](int h, int token, int byte) {
+        return Place{first[h] * L::kRow + (uint32_t)(token * L::kRow + byte), first[h] * NG + (uint32_t)(token * NG)};
+      });
+    } else {
+      const int t = min(t0 + (lane & 31), last);
+      const int32_t r = c.row_of(t, c.page_of(t), id[0]);
+      b.bad = (uint32_t)lanes_where(r < 0);
+      const int32_t mine = r < 0 ? 0 : (int32_t)(r + head_row);
+      load_rows(b, [&](int h, int token, int byte) {
+        const int64_t row = __shfl(mine, 16 * h + token);
+        return Place{row * L::kRow + byte, row * NG};
+      });
     }
   };
 
@@ -280,23 +299,9 @@ __global__ __launch_bounds__(kThreads) void cache_attention(CacheAttentionArgs a
   least_seen = __builtin_amdgcn_readfirstlane(least_seen);
 
   constexpr int kStep = kWaves * kTokens;
-  B cur;
-  int t0 = begin + wave * kTokens;
-  int32_t id_next = 0;
-  if (t0 < end) {
-    load_block(cur, t0, page_id(t0));
-    id_next = page_id(t0 + kStep);
-  }
-  for (; t0 < end; t0 += kStep) {
-    B next = cur;
-    if (t0 + kStep < end) {
-      load_block(next, t0 + kStep, id_next);
-      id_next = page_id(t0 + 2 * kStep);
-    }
-    const bool some_hidden = t0 + kTokens > least_seen;  // of the block's tokens, for some row
-
+  auto work = [&](B& cur, int t0, auto hidden) {
+    constexpr bool kHidden = decltype(hidden)::value;
     // a token whose page is none makes its rows NaN; tokens past the end count nothing, whatever is there
-    const uint64_t bad = lanes_where(cur.row < 0);
     float key_scale[2][L::kKeyScales], value_scale[8][L::kValueScales];
     float top = 0.0f;
 #pragma unroll
@@ -304,8 +309,7 @@ __global__ __launch_bounds__(kThreads) void cache_attention(CacheAttentionArgs a
 #pragma unroll
       for (int k = 0; k < L::kKeyScales; ++k) {
         float s = from_bfloat16(cur.key_scale[tt][k]);
-        if (some_hidden && t0 + 16 * tt + n >= end) s = 0.0f;
-        if (bad && (bad >> (16 * tt + n) & 1)) s = __builtin_nanf("");
+        if constexpr (kHidden) s = t0 + 16 * tt + n >= end ? 0.0f : cur.bad >> (16 * tt + n) & 1 ? __builtin_nanf("") : s;
         key_scale[tt][k] = s;
         top = fmaxf(top, fabsf(s));
       }
@@ -338,7 +342,7 @@ __global__ __launch_bounds__(kThreads) void cache_attention(CacheAttentionArgs a
         for (int d = 0; d < 4; ++d) {
           const half2v v = codes[d] * pair(w, w);
           hi[2 * d] = v[0], hi[2 * d + 1] = v[1];
-          if constexpr (PL == 2 && FMT == SQUANT_OUT_INT8) {
+          if constexpr (LOW) {
             const half2v rest = __builtin_elementwise_fma(codes[d], pair(w, w), -v);
             lo[2 * d] = rest[0], lo[2 * d + 1] = rest[1];
           }
@@ -347,7 +351,7 @@ __global__ __launch_bounds__(kThreads) void cache_attention(CacheAttentionArgs a
         for (int rt = 0; rt < RT; ++rt) {
           s[tt][rt] = Half::mma(hi, q[rt][0][i], s[tt][rt]);
           if constexpr (PL == 2) s[tt][rt] = Half::mma(hi, q[rt][1][i], s[tt][rt]);
-          if constexpr (PL == 2 && FMT == SQUANT_OUT_INT8) s[tt][rt] = Half::mma(lo, q[rt][0][i], s[tt][rt]);
+          if constexpr (LOW) s[tt][rt] = Half::mma(lo, q[rt][0][i], s[tt][rt]);
         }
       }
     }
@@ -362,7 +366,7 @@ __global__ __launch_bounds__(kThreads) void cache_attention(CacheAttentionArgs a
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         x[j] = s[j >> 2][rt][j & 3] * f;
-        if (some_hidden) x[j] = t0 + 16 * (j >> 2) + 4 * g + (j & 3) < min(seen[rt], end) ? x[j] : -kInfinity;
+        if constexpr (kHidden) x[j] = t0 + 16 * (j >> 2) + 4 * g + (j & 3) < min(seen[rt], end) ? x[j] : -kInfinity;
         m = fmaxf(m, x[j]);
       }
       m = over_groups_max(m);
@@ -394,8 +398,7 @@ __global__ __launch_bounds__(kThreads) void cache_attention(CacheAttentionArgs a
 #pragma unroll
       for (int k = 0; k < L::kValueScales; ++k) {
         float v = from_bfloat16(cur.value_scale[j][k]);
-        if (some_hidden && t0 + at >= end) v = 0.0f;
-        if (bad && (bad >> at & 1)) v = t0 + at < end ? __builtin_nanf("") : 0.0f;
+        if constexpr (kHidden) v = t0 + at >= end ? 0.0f : cur.bad >> at & 1 ? __builtin_nanf("") : v;
         value_scale[j][k] = v;
         top = fmaxf(top, fabsf(v));
       }
@@ -424,24 +427,20 @@ __global__ __launch_bounds__(kThreads) void cache_attention(CacheAttentionArgs a
                             (_Float16)(value_scale[2 * m + 1][k] * power_of_two(value_e)));
     // a scale of NaN or infinity at a token that some row does not see: that row's weight of 0 would not keep it out
     bool odd = false;
-    if (some_hidden) odd = lanes_where(!(top < kInfinity)) != 0;
-    if (some_hidden) {
-      // fmaxf passes over a NaN
+    if constexpr (kHidden) {
       bool any = false;
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
         for (int k = 0; k < L::kValueScales; ++k) any |= !(fabsf(value_scale[j][k]) < kInfinity);
-      odd = odd || lanes_where(any) != 0;
+      odd = lanes_where(any) != 0;
     }
     // codes plus 8 or 128
 #pragma unroll
     for (int j = 0; j < 8; ++j)
 #pragma unroll
       for (int i = 0; i < L::kValueWords; ++i) cur.value[j][i] ^= FMT == SQUANT_OUT_INT4 ? 0x88888888u : 0x80808080u;
-#pragma unroll
-    for (int f = 0; f < F; ++f) {
-      half8 hi, lo = {};
+    auto element_operand = [&](int f, half8& hi, half8& lo) {
       const int byte = FMT == SQUANT_OUT_INT4 ? f / 2 : f;
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
@@ -450,36 +449,74 @@ __global__ __launch_bounds__(kThreads) void cache_attention(CacheAttentionArgs a
         const half2v codes = value_codes<FMT>(cur.value[2 * m][byte / 4], cur.value[2 * m + 1][byte / 4], byte % 4, f & 1);
         const half2v v = codes * w;
         hi[2 * m] = v[0], hi[2 * m + 1] = v[1];
-        if constexpr (PL == 2 && FMT == SQUANT_OUT_INT8) {
+        if constexpr (LOW) {
           const half2v rest = __builtin_elementwise_fma(codes, w, -v);
           lo[2 * m] = rest[0], lo[2 * m + 1] = rest[1];
         }
       }
-      auto add = [&](const half8& h, const half8& l, float4v acc, int rt) {
-        acc = Half::mma(h, p[rt][0], acc);
-        if constexpr (PL == 2) acc = Half::mma(h, p[rt][1], acc);
-        if constexpr (PL == 2 && FMT == SQUANT_OUT_INT8) acc = Half::mma(l, p[rt][0], acc);
-        return acc;
-      };
-      if (!odd) {
+    };
+    auto add = [&](const half8& h, const half8& l, float4v acc, int rt) {
+      acc = Half::mma(h, p[rt][0], acc);
+      if constexpr (PL == 2) acc = Half::mma(h, p[rt][1], acc);
+      if constexpr (LOW) acc = Half::mma(l, p[rt][0], acc);
+      return acc;
+    };
+    if (!odd) {
+#pragma unroll
+      for (int f = 0; f < F; ++f) {
+        half8 hi, lo = {};
+        element_operand(f, hi, lo);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) o[f][rt] = add(hi, lo, o[f][rt], rt);
-      } else {
+      }
+    } else {
+      // token by token, rows that do not see it left out
 #pragma unroll 1
-        for (int t = 0; t < kTokens; ++t) {
-          half8 h = hi, l = lo;
+      for (int t = 0; t < kTokens; ++t)
+#pragma unroll
+        for (int f = 0; f < F; ++f) {
+          half8 hi, lo = {};
+          element_operand(f, hi, lo);
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (4 * g + (j & 3) + 16 * (j >> 2) != t) h[j] = l[j] = (_Float16)0.0f;
+            if (4 * g + (j & 3) + 16 * (j >> 2) != t) hi[j] = lo[j] = (_Float16)0.0f;
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) {
-            const float4v one = add(h, l, float4v{0, 0, 0, 0}, rt);
-            if (t0 + t < min(seen[rt], end)) o[f][rt] += one;
+            const float4v alone = add(hi, lo, float4v{0, 0, 0, 0}, rt);
+            if (t0 + t < min(seen[rt], end)) o[f][rt] += alone;
           }
         }
-      }
     }
-    cur = next;
+  };
+  // Blocks of which all rows see all tokens, the next one on its way; then the others, one by one.
+  B cur;
+  int t0 = begin + wave * kTokens;
+  const int seen_by_all = min(end, least_seen);
+  if (t0 + kTokens <= seen_by_all) {
+    int32_t ids[2];
+    page_ids(t0, ids);
+    load_block(cur, t0, ids);
+    page_ids(t0 + kStep, ids);
+#pragma unroll 1
+    while (!cur.bad) {
+      B next;
+      const bool more = t0 + kStep + kTokens <= seen_by_all;
+      if (more) {
+        load_block(next, t0 + kStep, ids);
+        page_ids(t0 + 2 * kStep, ids);
+      }
+      work(cur, t0, Constant<false>{});
+      t0 += kStep;
+      if (!more) break;
+      cur = next;
+    }
+  }
+#pragma unroll 1
+  for (; t0 < end; t0 += kStep) {
+    int32_t ids[2];
+    page_ids(t0, ids);
+    load_block(cur, t0, ids);
+    work(cur, t0, Constant<true>{});
   }
 
   // the waves' sums become one
@@ -605,27 +642,34 @@ template <int FORMATS> __global__ __launch_bounds__(kThreads) void join_splits(C
 inline size_t cache_attention_lds(int ng, int rt) { return (size_t)kWaves * 2 * 16 * rt * 4 + (size_t)2 * (ng * 2) * rt * 64 * 16; }
 
 typedef void (*cache_attention_t)(CacheAttentionArgs);
-template <int FMT, int PL> cache_attention_t cache_attention_of(int ng, int rt) {
-  switch (ng * 4 + rt) {
-    case 1 * 4 + 1: return cache_attention<FMT, 1, PL, 1>;
-    case 1 * 4 + 2: return cache_attention<FMT, 1, PL, 2>;
-    case 2 * 4 + 1: return cache_attention<FMT, 2, PL, 1>;
-    case 2 * 4 + 2: return cache_attention<FMT, 2, PL, 2>;
-    case 3 * 4 + 1: return cache_attention<FMT, 3, PL, 1>;
-    case 3 * 4 + 2: return cache_attention<FMT, 3, PL, 2>;
-    case 4 * 4 + 1: return cache_attention<FMT, 4, PL, 1>;
-    case 4 * 4 + 2: return cache_attention<FMT, 4, PL, 2>;
-    case 6 * 4 + 1: return cache_attention<FMT, 6, PL, 1>;
-    case 6 * 4 + 2: return cache_attention<FMT, 6, PL, 2>;
-    case 8 * 4 + 1: return cache_attention<FMT, 8, PL, 1>;
-    case 8 * 4 + 2: return cache_attention<FMT, 8, PL, 2>;
+template <int FMT, int PL, bool LOW, bool HALVES> cache_attention_t cache_attention_of(int ng, int rt) {
+  if constexpr (HALVES) {
+    if (rt == 2) switch (ng) {
+      case 1: return cache_attention<FMT, 1, PL, LOW, 2, HALVES>;
+      case 2: return cache_attention<FMT, 2, PL, LOW, 2, HALVES>;
+      case 3: return cache_attention<FMT, 3, PL, LOW, 2, HALVES>;
+      case 4: return cache_attention<FMT, 4, PL, LOW, 2, HALVES>;
+    }
+  }
+  switch (ng) {
+    case 1: return cache_attention<FMT, 1, PL, LOW, 1, HALVES>;
+    case 2: return cache_attention<FMT, 2, PL, LOW, 1, HALVES>;
+    case 3: return cache_attention<FMT, 3, PL, LOW, 1, HALVES>;
+    case 4: return cache_attention<FMT, 4, PL, LOW, 1, HALVES>;
+    case 6: return cache_attention<FMT, 6, PL, LOW, 1, HALVES>;
+    case 8: return cache_attention<FMT, 8, PL, LOW, 1, HALVES>;
     default: return nullptr;
   }
 }
-cache_attention_t cache_attention_int4_1(int ng, int rt);
-cache_attention_t cache_attention_int4_2(int ng, int rt);
-cache_attention_t cache_attention_int8_1(int ng, int rt);
-cache_attention_t cache_attention_int8_2(int ng, int rt);
+template <int FMT, int PL, bool LOW> cache_attention_t cache_attention_of(int ng, int rt, bool halves) {
+  return halves ? cache_attention_of<FMT, PL, LOW, true>(ng, rt) : cache_attention_of<FMT, PL, LOW, false>(ng, rt);
+}
+// By format, and by type: bfloat16 (8 bits only), 16 bits, binary32.
+cache_attention_t cache_attention_int4(int ng, int rt, bool halves);
+cache_attention_t cache_attention_int4_f32(int ng, int rt, bool halves);
+cache_attention_t cache_attention_int8_bf16(int ng, int rt, bool halves);
+cache_attention_t cache_attention_int8_f16(int ng, int rt, bool halves);
+cache_attention_t cache_attention_int8_f32(int ng, int rt, bool halves);
 cache_attention_t join_splits_kernel();
 
 }  // namespace att

@@ -4,7 +4,7 @@
 namespace squant {
 namespace att {
 
-cache_attention_t cache_attention_int4_1(int ng, int rt) { return cache_attention_of<SQUANT_OUT_INT4, 1>(ng, rt); }
+cache_attention_t cache_attention_int4(int ng, int rt, bool halves) { return cache_attention_of<SQUANT_OUT_INT4, 1, false>(ng, rt, halves); }
 cache_attention_t join_splits_kernel() { return join_splits<0>; }
 
 }  // namespace att

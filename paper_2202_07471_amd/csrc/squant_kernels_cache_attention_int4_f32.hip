@@ -4,7 +4,7 @@
 namespace squant {
 namespace att {
 
-cache_attention_t cache_attention_int4_2(int ng, int rt) { return cache_attention_of<SQUANT_OUT_INT4, 2>(ng, rt); }
+cache_attention_t cache_attention_int4_f32(int ng, int rt, bool halves) { return cache_attention_of<SQUANT_OUT_INT4, 2, false>(ng, rt, halves); }
 
 }  // namespace att
 }  // namespace squant

@@ -205,7 +205,6 @@ __device__ __forceinline__ void store_column(const Strided& s, int64_t row, int 
 
 // Weights of binary16 calls are held times 2^7, so that small ones keep their bits.
 template <class T> constexpr float weight_unit() { return __is_same(T, _Float16) ? 7.0f : 0.0f; }
-template <bool B> struct Constant { static constexpr bool value = B; };
 
 // Asks the compiler to keep 8 reads from the LDS ahead of a step's matrix instructions: FIRST reads with EACH of them behind every
 // read, then SECOND with EACH behind every SECOND_STEP.  Left to itself it reads two operands and waits for them (dK and dV of
