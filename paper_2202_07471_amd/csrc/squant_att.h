@@ -121,14 +121,20 @@ __device__ __forceinline__ Tile find_tile(const Packed& p, int64_t id, int per_r
   return t;
 }
 
-// A value over the four lanes that hold a column of a result (16 apart).
+// A value over the four lanes that hold a column of a result (16 apart).  Swapping a register's rows of lanes with its own copy's puts
+// a lane's value and its neighbour's side by side.
+template <class OP> __device__ __forceinline__ float over_groups(float v, OP op) {
+  const uint32_t u = __float_as_uint(v);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t w = __float_as_uint(op(__uint_as_float(a[0]), __uint_as_float(a[1])));
+  const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+  return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
 __device__ __forceinline__ float over_groups_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
+  return over_groups(v, [](float x, float y) { return fmaxf(x, y); });
 }
 __device__ __forceinline__ float over_groups_sum(float v) {
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+  return over_groups(v, [](float x, float y) { return x + y; });
 }
 
 template <bool B> struct Constant { static constexpr bool value = B; };

@@ -114,7 +114,11 @@ struct CacheSplit {
   int64_t splits, chunk;
   size_t stats_bytes, bytes;
 };
-constexpr int64_t kGroups = 2048, kLeastChunk = 256, kMostChunk = 8192;
+#ifndef CG
+#define CG 2048
+#define CL 512
+#endif
+constexpr int64_t kGroups = CG, kLeastChunk = CL, kMostChunk = 8192;
 
 bool split_cache(int64_t rows, int32_t heads, const squant_cache_t& c, const squant_paged_t& w, CacheSplit& s) {
   const int group = heads / c.heads;
@@ -209,9 +213,9 @@ int squant_cache_attention(const squant_heads_t* h_q, squant_wtype_t type, int64
   a.scale = std::max(scale * kLog2E, 1.4e-45f);
   if (s.splits > 1) a.stats = (float2*)d_workspace, a.partial = (float*)((char*)d_workspace + s.stats_bytes);
   const int ng = c.head_dim / kGroup;
-  const bool wide = type == SQUANT_W_F32;
-  const auto of = c.format == SQUANT_OUT_INT4 ? (wide ? cache_attention_int4_f32 : cache_attention_int4)
-                  : wide ? cache_attention_int8_f32 : type == SQUANT_W_F16 ? cache_attention_int8_f16 : cache_attention_int8_bf16;
+  const auto of = c.format == SQUANT_OUT_INT4
+                      ? (type == SQUANT_W_F32 ? cache_attention_int4_f32 : type == SQUANT_W_F16 ? cache_attention_int4_f16 : cache_attention_int4_bf16)
+                      : (type == SQUANT_W_F32 ? cache_attention_int8_f32 : type == SQUANT_W_F16 ? cache_attention_int8_f16 : cache_attention_int8_bf16);
   const cache_attention_t k = of(ng, s.rt, c.page_size % 16 == 0);
   hipStream_t st = (hipStream_t)stream;
   if (int rc = launch(k, s.tiles * c.heads, s.splits, cache_attention_lds(ng, s.rt), st, a)) return rc;

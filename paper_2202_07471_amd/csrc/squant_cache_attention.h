@@ -55,25 +55,25 @@ template <int FMT, int NG> struct Layout {
   static constexpr int kValueScales = NG == 3 || NG == 6 ? 2 : 1;
 };
 
-// A block of tokens on its way or at work.  `bad`: those whose page is none.
-template <int FMT, int NG> struct Block {
-  typedef Layout<FMT, NG> L;
-  uint32_t key[2][L::kKeyWords];
-  uint32_t value[8][L::kValueWords];
-  uint16_t key_scale[2][L::kKeyScales];
-  uint16_t value_scale[8][L::kValueScales];
-  uint32_t bad;
+// Bits that make a 4-bit two's complement code in the low, or the high, half of a byte the binary16 number 1024 + code + 8, or
+// 1024 + 16 (code + 8): (u & mask) ^ magic.  One instruction, which takes one constant from a scalar register; these are in vector registers.
+struct Magic {
+  uint32_t low, high;
+  __device__ __forceinline__ Magic() {
+    asm("v_mov_b32 %0, 0x64086408" : "=v"(low));
+    asm("v_mov_b32 %0, 0x64806480" : "=v"(high));
+  }
 };
 
-// 8 codes as binary16 integers (times 16 where `sixteen` says so); element order as `slot_element` has it.
-template <int FMT> __device__ __forceinline__ void key_codes(const uint32_t* w, half2v (&o)[4]) {
+// 8 codes as binary16 integers (times 16 where `slot_unit` says so); element order as `slot_element` has it.
+template <int FMT> __device__ __forceinline__ void key_codes(const uint32_t* w, const Magic& magic, half2v (&o)[4]) {
   if constexpr (FMT == SQUANT_OUT_INT4) {
-    const uint32_t u = w[0] ^ 0x88888888u, v = u >> 8;
+    const uint32_t u = w[0], v = u >> 8;
     const half2v low = pair((_Float16)1032.0f, (_Float16)1032.0f), high = pair((_Float16)1152.0f, (_Float16)1152.0f);
-    o[0] = lin::as_half2((u & 0x000f000fu) | 0x64006400u) - low;
-    o[1] = lin::as_half2((u & 0x00f000f0u) | 0x64006400u) - high;
-    o[2] = lin::as_half2((v & 0x000f000fu) | 0x64006400u) - low;
-    o[3] = lin::as_half2((v & 0x00f000f0u) | 0x64006400u) - high;
+    o[0] = lin::as_half2((u & 0x000f000fu) ^ magic.low) - low;
+    o[1] = lin::as_half2((u & 0x00f000f0u) ^ magic.high) - high;
+    o[2] = lin::as_half2((v & 0x000f000fu) ^ magic.low) - low;
+    o[3] = lin::as_half2((v & 0x00f000f0u) ^ magic.high) - high;
   } else {
     const half2v bias = pair((_Float16)1152.0f, (_Float16)1152.0f);
 #pragma unroll
@@ -92,15 +92,13 @@ template <int FMT> __device__ __forceinline__ constexpr float slot_unit(int s) {
   return FMT == SQUANT_OUT_INT4 && (s & 2) ? 0.0625f : 1.0f;
 }
 
-// Codes of tokens 2 m and 2 m + 1 for one element: byte `p` (low or high half of it) of a and b, which hold codes plus 8 or
-// 128.  Codes of high halves are times 16.
-template <int FMT> __device__ __forceinline__ half2v value_codes(uint32_t a, uint32_t b, int p, int high) {
+// Codes of tokens 2 m and 2 m + 1 for one element: byte `p` (low or high half of it) of a and b.  Codes of high halves are times 16.
+template <int FMT> __device__ __forceinline__ half2v value_codes(uint32_t a, uint32_t b, const Magic& magic, int p, int high) {
   const uint32_t u = lin::pick(b, a, 0x0c040c00u + 0x00010001u * (uint32_t)p);
-  if constexpr (FMT == SQUANT_OUT_INT4) {
-    const half2v bias = high ? pair((_Float16)1152.0f, (_Float16)1152.0f) : pair((_Float16)1032.0f, (_Float16)1032.0f);
-    return lin::as_half2((u & (high ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u) - bias;
-  }
-  return lin::as_half2(u | 0x64006400u) - pair((_Float16)1152.0f, (_Float16)1152.0f);
+  if constexpr (FMT == SQUANT_OUT_INT4)
+    return high ? lin::as_half2((u & 0x00f000f0u) ^ magic.high) - pair((_Float16)1152.0f, (_Float16)1152.0f)
+                : lin::as_half2((u & 0x000f000fu) ^ magic.low) - pair((_Float16)1032.0f, (_Float16)1032.0f);
+  return lin::as_half2(u ^ magic.high) - pair((_Float16)1152.0f, (_Float16)1152.0f);
 }
 
 __device__ __forceinline__ uint32_t over_lanes_max(uint32_t v) {
@@ -119,17 +117,29 @@ __device__ __forceinline__ uint32_t finite_bits(float v) {
   const uint32_t m = magnitude(v);
   return m < 0x7f800000u ? m : 0u;
 }
+// bfloat16 bits of 512 / 2^e: scales from there on are too large for e, or no numbers.
+__device__ __forceinline__ uint32_t too_large(int e) { return min((uint32_t)(9 - e + 127) << 7, 0x7f80u); }
 
-// Waves a SIMD that the registers are kept for.  The wave waits for memory: three hide it better than two with more loads on their way.
-constexpr int cache_occupancy(int ng, int rt) { return ng <= 2 ? 4 : ng <= 4 && rt == 1 ? 3 : 2; }
+#ifndef CO
+#define CO 2
+#define CP 3
+#endif
+// Waves a SIMD that registers are kept for.
+constexpr int cache_occupancy(int ng, int rt) { return ng <= 2 && rt == 1 ? CP : CO; }
 
-// PL: planes of queries and weights; LOW: the remainder of an 8-bit element as well.  HALVES: pages of a multiple of 16 tokens, of
-// which each half of a block has consecutive rows: their addresses are a number for the wave plus one of the lane that stays.
-template <int FMT, int NG, int PL, bool LOW, int RT, bool HALVES>
+// HALVES: pages of a multiple of 16 tokens, of which each half of a block has consecutive rows: their addresses are a number for the
+// wave plus one of the lane that stays.
+//
+// One body for all blocks, with branches of the wave around what only some need: a call of a short sequence spends its time
+// on fetching instructions for the first time (with a body of its own for blocks that hide tokens and two blocks a turn
+// one token of 8192 took 12 us in this kernel, whether it multiplied or only read).  For the same reason the next block's keys are
+// read behind this one's scores, and its values behind this one's products, into the registers that have become free.
+template <class T, int FMT, int NG, int RT, bool HALVES>
 __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_attention(CacheAttentionArgs a) {
   typedef Layout<FMT, NG> L;
-  typedef Block<FMT, NG> B;
-  constexpr int D = NG * kGroup, F = D / 16, TR = 16 * RT;
+  constexpr int PL = sizeof(T) == 4 ? 2 : 1;                                 // planes of queries and weights
+  constexpr bool LOW = FMT == SQUANT_OUT_INT8 && !__is_same(T, __bf16);      // the remainder of an element as well
+  constexpr int D = NG * kGroup, F = D / 16, TR = 16 * RT, kStep = kWaves * kTokens;
   extern __shared__ float lds[];
   const Cache& c = a.cache;
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -139,37 +149,39 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
 
   // whose rows these are
   Tile tile;
-  const int64_t tile_id = blockIdx.x / (uint32_t)c.heads;
+  const int tile_id = (int)(blockIdx.x / (uint32_t)c.heads);
   if (a.rows.one_each) {
     const int each = (a.group + TR - 1) / TR;
-    tile.sequence = (int)(tile_id / each);
-    tile.first = (int)(tile_id - (int64_t)tile.sequence * each) * TR;
+    tile.sequence = tile_id / each;
+    tile.first = (tile_id - tile.sequence * each) * TR;
     if (tile.sequence >= a.rows.count) return;
   } else {
     tile = find_tile(a.rows, tile_id, a.group, TR);
   }
   if (tile.sequence < 0) return;
   const int seq = tile.sequence, row0 = a.rows.start(seq), count = a.rows.length(seq);
-  int64_t capacity = (int64_t)c.table_width * c.page_size;
+  const int64_t capacity = (int64_t)c.table_width * c.page_size;
   const int said = seq < a.rows.count ? max(c.lengths[seq], 0) : 0;
-  const int length = (int)min((int64_t)said, capacity);
+  const int length = (int)min((int64_t)said, capacity), last = max(length - 1, 0);
   const int begin = split * a.chunk, end = min(length, begin + a.chunk);
-  if (a.splits > 1 && begin >= max(length, 1)) return;  // the join knows
-  if (a.splits > 1 && seq == a.rows.count) return;
+  if (a.splits > 1 && (begin >= max(length, 1) || seq == a.rows.count)) return;  // the join knows
 
   // this lane's columns of the scores: rows of the queries
   int row[RT], qhead[RT], seen[RT];
   bool live[RT];
+  int least_seen = 0x7fffffff;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int r = tile.first + 16 * rt + n;
     const int token = r / a.group;
     live[rt] = r < count * a.group;
     row[rt] = row0 + (live[rt] ? token : 0);
-    qhead[rt] = head * a.group + (r - token * a.group);
-    seen[rt] = live[rt] ? min(max(said - count + token + 1, 0), length) : 0;
-    if (!live[rt]) qhead[rt] = head * a.group;
+    qhead[rt] = head * a.group + (live[rt] ? r - token * a.group : 0);
+    seen[rt] = live[rt] ? min(max(said - count + token + 1, 0), end) : 0;
+    if (live[rt]) least_seen = min(least_seen, seen[rt]);
   }
+  // rows of a tile see no less than its first
+  least_seen = min(__builtin_amdgcn_readfirstlane(least_seen), end);
   const float poison = said > length ? __builtin_nanf("") : 1.0f;
 
   half8 q[RT][PL][NG];
@@ -180,10 +192,7 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < NG; ++i) {
-      const int d = (g * NG + i) * 8;
-      if (a.type == SQUANT_W_F32) load8(element<float>(a.q, row[rt], qhead[rt]) + d, x[i]);
-      else if (a.type == SQUANT_W_F16) load8(element<_Float16>(a.q, row[rt], qhead[rt]) + d, x[i]);
-      else load8(element<__bf16>(a.q, row[rt], qhead[rt]) + d, x[i]);
+      load8(element<T>(a.q, row[rt], qhead[rt]) + (g * NG + i) * 8, x[i]);
 #pragma unroll
       for (int s = 0; s < 8; ++s) top = max(top, finite_bits(x[i][s]));
     }
@@ -203,9 +212,13 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
       }
   }
 
-  // where tokens lie: pages of the block's halves, or of token t0 + lane % 32
+  // Where a block's tokens lie.  `bad`: tokens whose page is none.
+  struct Where {
+    int64_t first[2];  // HALVES: rows of the halves' first tokens
+    int32_t row;       // else: the row of token t0 + lane % 32
+    uint32_t bad;
+  };
   const uint32_t head_row = (uint32_t)head * (uint32_t)c.page_size;
-  const int last = max(length - 1, 0);
   auto page_ids = [&](int t0, int32_t (&id)[2]) {
     if constexpr (HALVES) {
 #pragma unroll
@@ -214,71 +227,77 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
       id[0] = id[1] = c.table_at(seq, c.page_of(min(t0 + (lane & 31), last)));
     }
   };
-  auto load_value = [&](uint32_t (&o)[L::kValueWords], const uint8_t* p) {
-    __builtin_memset(o, 0, sizeof(o));
-    if constexpr (L::kValueBytes % 4 == 0) {
-      struct Words { uint32_t w[L::kValueWords]; };
-      const Words w = *reinterpret_cast<const Words*>(p);
-#pragma unroll
-      for (int i = 0; i < L::kValueWords; ++i) o[i] = w.w[i];
-    } else if constexpr (L::kValueBytes == 6) {
-      struct Halves { uint16_t w[3]; };
-      const Halves w = *reinterpret_cast<const Halves*>(p);
-      o[0] = w.w[0] | (uint32_t)w.w[1] << 16;
-      o[1] = w.w[2];
-    } else if constexpr (L::kValueBytes == 2) {
-      o[0] = *reinterpret_cast<const uint16_t*>(p);
-    } else if constexpr (L::kValueBytes == 3) {
-      o[0] = p[0] | (uint32_t)p[1] << 8 | (uint32_t)p[2] << 16;
-    } else {
-      static_assert(L::kValueBytes == 1, "");
-      o[0] = p[0];
-    }
-  };
-  // codes and scales of key token 16 tt + n and of value token 4 g + j (j < 4), 16 + 4 g + j - 4, by their rows
-  auto load_rows = [&](B& b, auto row_of) {
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      struct Words { uint32_t w[L::kKeyWords]; };
-      const auto at = row_of(tt, n, g * (L::kRow / 4));
-      const Words w = load_any<Words>(c.codes[0] + at.bytes);
-#pragma unroll
-      for (int i = 0; i < L::kKeyWords; ++i) b.key[tt][i] = w.w[i];
-#pragma unroll
-      for (int k = 0; k < L::kKeyScales; ++k) b.key_scale[tt][k] = c.scales[0][at.scales + min(((g * NG) >> 2) + k, NG - 1)];
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const auto at = row_of(j >> 2, 4 * g + (j & 3), n * L::kValueBytes);
-      load_value(b.value[j], c.codes[1] + at.bytes);
-#pragma unroll
-      for (int k = 0; k < L::kValueScales; ++k) b.value_scale[j][k] = c.scales[1][at.scales + min(((2 * NG * n) >> 5) + k, NG - 1)];
-    }
-  };
-  struct Place { int64_t bytes, scales; };
-  auto load_block = [&](B& b, int t0, const int32_t (&id)[2]) {
+  auto find = [&](Where& w, int t0, const int32_t (&id)[2]) {
+    w.bad = 0;
     if constexpr (HALVES) {
-      int64_t first[2];
-      b.bad = 0;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int t = min(t0 + 16 * h, last);
         const int32_t r = c.row_of(t / 16 * 16, c.page_of(t), id[h]);
-        if (r < 0) b.bad |= 0xffffu << (16 * h);
-        first[h] = r < 0 ? 0 : (int64_t)(r + head_row);  // rows 0 to 15 are there
+        if (r < 0) w.bad |= 0xffffu << (16 * h);
+        w.first[h] = r < 0 ? 0 : (int64_t)(r + head_row);  // rows 0 to 15 are there
       }
-      load_rows(b, [&](int h, int token, int byte) {
-        return Place{first[h] * L::kRow + (uint32_t)(token * L::kRow + byte), first[h] * NG + (uint32_t)(token * NG)};
-      });
     } else {
       const int t = min(t0 + (lane & 31), last);
       const int32_t r = c.row_of(t, c.page_of(t), id[0]);
-      b.bad = (uint32_t)lanes_where(r < 0);
-      const int32_t mine = r < 0 ? 0 : (int32_t)(r + head_row);
-      load_rows(b, [&](int h, int token, int byte) {
-        const int64_t row = __shfl(mine, 16 * h + token);
-        return Place{row * L::kRow + byte, row * NG};
-      });
+      w.bad = (uint32_t)lanes_where(r < 0);
+      w.row = r < 0 ? 0 : (int32_t)(r + head_row);
+    }
+  };
+  // bases for the wave and offsets of the lane
+  struct Place {
+    const uint8_t* codes;
+    const uint16_t* scales;
+    uint32_t byte, scale;
+  };
+  auto place = [&](const Where& w, int tensor, int h, int token) {
+    if constexpr (HALVES) {
+      return Place{c.codes[tensor] + w.first[h] * L::kRow, c.scales[tensor] + w.first[h] * NG, (uint32_t)(token * L::kRow), (uint32_t)(token * NG)};
+    } else {
+      const int64_t r = __shfl(w.row, 16 * h + token);
+      return Place{c.codes[tensor] + r * L::kRow, c.scales[tensor] + r * NG, 0, 0};
+    }
+  };
+  uint32_t key[2][L::kKeyWords], value[8][L::kValueWords];
+  uint16_t key_scale[2][L::kKeyScales], value_scale[8][L::kValueScales];
+  // key token 16 tt + n, value token 4 g + j (j < 4), 16 + 4 g + j - 4
+  auto load_keys = [&](const Where& w) {
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      struct Words { uint32_t w[L::kKeyWords]; };
+      const Place at = place(w, 0, tt, n);
+      const Words v = load_any<Words>(at.codes + (uint32_t)(at.byte + (uint32_t)(g * (L::kRow / 4))));
+#pragma unroll
+      for (int i = 0; i < L::kKeyWords; ++i) key[tt][i] = v.w[i];
+#pragma unroll
+      for (int k = 0; k < L::kKeyScales; ++k) key_scale[tt][k] = at.scales[(uint32_t)(at.scale + (uint32_t)min(((g * NG) >> 2) + k, NG - 1))];
+    }
+  };
+  auto load_values = [&](const Where& w) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const Place at = place(w, 1, j >> 2, 4 * g + (j & 3));
+      const uint8_t* p = at.codes + (uint32_t)(at.byte + (uint32_t)(n * L::kValueBytes));
+      if constexpr (L::kValueBytes % 4 == 0) {
+        struct Words { uint32_t w[L::kValueWords]; };
+        const Words v = *reinterpret_cast<const Words*>(p);
+#pragma unroll
+        for (int i = 0; i < L::kValueWords; ++i) value[j][i] = v.w[i];
+      } else if constexpr (L::kValueBytes == 6) {
+        struct Halves { uint16_t w[3]; };
+        const Halves v = *reinterpret_cast<const Halves*>(p);
+        value[j][0] = v.w[0] | (uint32_t)v.w[1] << 16;
+        value[j][1] = v.w[2];
+      } else if constexpr (L::kValueBytes == 2) {
+        value[j][0] = *reinterpret_cast<const uint16_t*>(p);
+      } else if constexpr (L::kValueBytes == 3) {
+        value[j][0] = p[0] | (uint32_t)p[1] << 8 | (uint32_t)p[2] << 16;
+      } else {
+        static_assert(L::kValueBytes == 1, "");
+        value[j][0] = p[0];
+      }
+#pragma unroll
+      for (int k = 0; k < L::kValueScales; ++k) value_scale[j][k] = at.scales[(uint32_t)(at.scale + (uint32_t)min(((2 * NG * n) >> 5) + k, NG - 1))];
     }
   };
 
@@ -291,37 +310,39 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) largest[rt] = -kInfinity, sum[rt] = 0.0f;
   int key_e = 126, value_e = 126;
-  int least_seen = 0x7fffffff;
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) least_seen = min(least_seen, live[rt] ? seen[rt] : 0x7fffffff);
-#pragma unroll
-  for (int w = 1; w < 16; w <<= 1) least_seen = min(least_seen, __shfl_xor(least_seen, w));
-  least_seen = __builtin_amdgcn_readfirstlane(least_seen);
+  const Magic magic;
 
-  constexpr int kStep = kWaves * kTokens;
-  auto work = [&](B& cur, int t0, auto hidden) {
-    constexpr bool kHidden = decltype(hidden)::value;
-    // a token whose page is none makes its rows NaN; tokens past the end count nothing, whatever is there
-    float key_scale[2][L::kKeyScales], value_scale[8][L::kValueScales];
-    float top = 0.0f;
+  int t0 = begin + wave * kTokens;
+  Where at, next;
+  int32_t ids[2];
+  if (t0 < end) {
+    page_ids(t0, ids);
+    find(at, t0, ids);
+    load_keys(at);
+    load_values(at);
+    page_ids(t0 + kStep, ids);
+  }
+#pragma unroll 1
+  for (; t0 < end; t0 += kStep) {
+    const bool some_hidden = t0 + kTokens > least_seen;  // of the block's tokens, for some row
+    uint32_t nan_tokens = at.bad;                         // rows that see one of them are NaN
+
+    uint32_t top = 0;
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
       for (int k = 0; k < L::kKeyScales; ++k) {
-        float s = from_bfloat16(cur.key_scale[tt][k]);
-        if constexpr (kHidden) s = t0 + 16 * tt + n >= end ? 0.0f : cur.bad >> (16 * tt + n) & 1 ? __builtin_nanf("") : s;
-        key_scale[tt][k] = s;
-        top = fmaxf(top, fabsf(s));
+        if (some_hidden && t0 + 16 * tt + n >= end) key_scale[tt][k] = 0;
+        top = max(top, (uint32_t)key_scale[tt][k] & 0x7fffu);
       }
-    if (lanes_where(top * power_of_two(key_e) >= 512.0f)) {
+    if (lanes_where(top >= too_large(key_e))) {
       uint32_t m = 0;
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int k = 0; k < L::kKeyScales; ++k) m = max(m, finite_bits(key_scale[tt][k]));
+        for (int k = 0; k < L::kKeyScales; ++k) m = max(m, finite_bits(from_bfloat16(key_scale[tt][k])));
       key_e = min(key_e, __builtin_amdgcn_readfirstlane(scale_exponent(over_lanes_max(m))));
     }
-
     float4v s[2][RT];
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
@@ -329,14 +350,14 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
       for (int rt = 0; rt < RT; ++rt) s[tt][rt] = float4v{0, 0, 0, 0};
       _Float16 scale[L::kKeyScales];
 #pragma unroll
-      for (int k = 0; k < L::kKeyScales; ++k) scale[k] = (_Float16)(key_scale[tt][k] * power_of_two(key_e));
+      for (int k = 0; k < L::kKeyScales; ++k) scale[k] = (_Float16)(from_bfloat16(key_scale[tt][k]) * power_of_two(key_e));
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
         _Float16 w = scale[0];
         if constexpr (NG % 4 == 0) w = scale[i >> 2];
         else if constexpr (L::kKeyScales == 2) w = ((g * NG + i) >> 2) > ((g * NG) >> 2) ? scale[1] : scale[0];
         half2v codes[4];
-        key_codes<FMT>(cur.key[tt] + i * (L::kBits / 4), codes);
+        key_codes<FMT>(key[tt] + i * (L::kBits / 4), magic, codes);
         half8 hi, lo = {};
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
@@ -355,60 +376,43 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
         }
       }
     }
-
-    // softmax weights of the block, times 2^14; what they add up to stays with the lane until the end
-    half8 p[RT][PL];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const float f = factor[rt] * power_of_two(-key_e);
-      float x[8];
-      float m = -kInfinity;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        x[j] = s[j >> 2][rt][j & 3] * f;
-        if constexpr (kHidden) x[j] = t0 + 16 * (j >> 2) + 4 * g + (j & 3) < min(seen[rt], end) ? x[j] : -kInfinity;
-        m = fmaxf(m, x[j]);
-      }
-      m = over_groups_max(m);
-      if (lanes_where(m > largest[rt])) {
-        const float more = fmaxf(m, largest[rt]);
-        const float shrink = more == -kInfinity ? 1.0f : exp2_fast(largest[rt] - more);
-        sum[rt] *= shrink;
-#pragma unroll
-        for (int f2 = 0; f2 < F; ++f2)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[f2][rt][i] *= shrink;
-        largest[rt] = more;
-      }
-      const float base = largest[rt] == -kInfinity ? 0.0f : largest[rt] - kWeightUnit;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float w = exp2_fast(x[j] - base);
-        sum[rt] += w;
-        const _Float16 hi = (_Float16)w;
-        p[rt][0][j] = hi;
-        if constexpr (PL == 2) p[rt][1][j] = (_Float16)(w - (float)hi);
-      }
+    const bool more = t0 + kStep < end;
+    if (more) {
+      find(next, t0 + kStep, ids);
+      load_keys(next);
+      page_ids(t0 + 2 * kStep, ids);
     }
 
-    top = 0.0f;
+    // the values' scales: 0 for tokens past the end, whatever is there, and for those that make rows NaN
+    top = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int at = 4 * g + (j & 3) + 16 * (j >> 2);
+    for (int j = 0; j < 8; ++j)
 #pragma unroll
       for (int k = 0; k < L::kValueScales; ++k) {
-        float v = from_bfloat16(cur.value_scale[j][k]);
-        if constexpr (kHidden) v = t0 + at >= end ? 0.0f : cur.bad >> at & 1 ? __builtin_nanf("") : v;
-        value_scale[j][k] = v;
-        top = fmaxf(top, fabsf(v));
+        const int token = 4 * g + (j & 3) + 16 * (j >> 2);
+        if (some_hidden && t0 + token >= end) value_scale[j][k] = 0;
+        top = max(top, (uint32_t)value_scale[j][k] & 0x7fffu);
       }
-    }
-    if (lanes_where(top * power_of_two(value_e) >= 512.0f)) {
+    if (nan_tokens || lanes_where(top >= too_large(value_e))) {
       uint32_t m = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int token = 4 * g + (j & 3) + 16 * (j >> 2);
+        bool none = nan_tokens >> token & 1;
+#pragma unroll
+        for (int k = 0; k < L::kValueScales; ++k) none |= (value_scale[j][k] & 0x7fffu) >= 0x7f80u;
+        const uint64_t odd = lanes_where(none);  // sixteen lanes of a group share a token
+#pragma unroll
+        for (int g2 = 0; g2 < 4; ++g2)
+          if (odd >> (16 * g2) & 0xffffu) nan_tokens |= 1u << (4 * g2 + (j & 3) + 16 * (j >> 2));
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int k = 0; k < L::kValueScales; ++k) m = max(m, finite_bits(value_scale[j][k]));
+        for (int k = 0; k < L::kValueScales; ++k) {
+          if (nan_tokens >> (4 * g + (j & 3) + 16 * (j >> 2)) & 1) value_scale[j][k] = 0;
+          m = max(m, finite_bits(from_bfloat16(value_scale[j][k])));
+        }
       const int e = min(value_e, __builtin_amdgcn_readfirstlane(scale_exponent(over_lanes_max(m))));
 #pragma unroll
       for (int f = 0; f < F; ++f)
@@ -418,35 +422,63 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
           for (int i = 0; i < 4; ++i) o[f][rt][i] = ldexpf(o[f][rt][i], e - value_e);
       value_e = e;
     }
+    if (some_hidden || nan_tokens) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int token = 4 * g + (j & 3) + 16 * (j >> 2);
+          if (nan_tokens >> token & 1) s[j >> 2][rt][j & 3] = __builtin_nanf("");
+          if (t0 + token >= seen[rt]) s[j >> 2][rt][j & 3] = -kInfinity;
+        }
+    }
+
+    // softmax weights of the block, times 2^14; what they add up to stays with the lane until the end
+    half8 p[RT][PL];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const float f = factor[rt] * power_of_two(-key_e);
+      float m = -kInfinity;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m = fmaxf(m, s[j >> 2][rt][j & 3]);
+      m = over_groups_max(m) * f;
+      if (lanes_where(m > largest[rt])) {
+        const float most = fmaxf(m, largest[rt]);
+        const float shrink = most == -kInfinity ? 1.0f : exp2_fast(largest[rt] - most);
+        sum[rt] *= shrink;
+#pragma unroll
+        for (int f2 = 0; f2 < F; ++f2)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[f2][rt][i] *= shrink;
+        largest[rt] = most;
+      }
+      const float base = largest[rt] == -kInfinity ? 0.0f : kWeightUnit - largest[rt];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float w = exp2_fast(__builtin_fmaf(s[j >> 2][rt][j & 3], f, base));
+        sum[rt] += w;
+        const _Float16 hi = (_Float16)w;
+        p[rt][0][j] = hi;
+        if constexpr (PL == 2) p[rt][1][j] = (_Float16)(w - (float)hi);
+      }
+    }
+
     half2v scale2[4][L::kValueScales];
 #pragma unroll
     for (int m = 0; m < 4; ++m)
 #pragma unroll
       for (int k = 0; k < L::kValueScales; ++k)
-        scale2[m][k] = pair((_Float16)(value_scale[2 * m][k] * power_of_two(value_e)),
-                            (_Float16)(value_scale[2 * m + 1][k] * power_of_two(value_e)));
-    // a scale of NaN or infinity at a token that some row does not see: that row's weight of 0 would not keep it out
-    bool odd = false;
-    if constexpr (kHidden) {
-      bool any = false;
+        scale2[m][k] = pair((_Float16)(from_bfloat16(value_scale[2 * m][k]) * power_of_two(value_e)),
+                            (_Float16)(from_bfloat16(value_scale[2 * m + 1][k]) * power_of_two(value_e)));
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int k = 0; k < L::kValueScales; ++k) any |= !(fabsf(value_scale[j][k]) < kInfinity);
-      odd = lanes_where(any) != 0;
-    }
-    // codes plus 8 or 128
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-#pragma unroll
-      for (int i = 0; i < L::kValueWords; ++i) cur.value[j][i] ^= FMT == SQUANT_OUT_INT4 ? 0x88888888u : 0x80808080u;
-    auto element_operand = [&](int f, half8& hi, half8& lo) {
+    for (int f = 0; f < F; ++f) {
       const int byte = FMT == SQUANT_OUT_INT4 ? f / 2 : f;
+      half8 hi, lo = {};
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
         half2v w = scale2[m][0];
         if constexpr (L::kValueScales == 2) w = ((2 * NG * n + f) >> 5) > ((2 * NG * n) >> 5) ? scale2[m][1] : scale2[m][0];
-        const half2v codes = value_codes<FMT>(cur.value[2 * m][byte / 4], cur.value[2 * m + 1][byte / 4], byte % 4, f & 1);
+        const half2v codes = value_codes<FMT>(value[2 * m][byte / 4], value[2 * m + 1][byte / 4], magic, byte % 4, f & 1);
         const half2v v = codes * w;
         hi[2 * m] = v[0], hi[2 * m + 1] = v[1];
         if constexpr (LOW) {
@@ -454,69 +486,17 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
           lo[2 * m] = rest[0], lo[2 * m + 1] = rest[1];
         }
       }
-    };
-    auto add = [&](const half8& h, const half8& l, float4v acc, int rt) {
-      acc = Half::mma(h, p[rt][0], acc);
-      if constexpr (PL == 2) acc = Half::mma(h, p[rt][1], acc);
-      if constexpr (LOW) acc = Half::mma(l, p[rt][0], acc);
-      return acc;
-    };
-    if (!odd) {
 #pragma unroll
-      for (int f = 0; f < F; ++f) {
-        half8 hi, lo = {};
-        element_operand(f, hi, lo);
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) o[f][rt] = add(hi, lo, o[f][rt], rt);
+      for (int rt = 0; rt < RT; ++rt) {
+        o[f][rt] = Half::mma(hi, p[rt][0], o[f][rt]);
+        if constexpr (PL == 2) o[f][rt] = Half::mma(hi, p[rt][1], o[f][rt]);
+        if constexpr (LOW) o[f][rt] = Half::mma(lo, p[rt][0], o[f][rt]);
       }
-    } else {
-      // token by token, rows that do not see it left out
-#pragma unroll 1
-      for (int t = 0; t < kTokens; ++t)
-#pragma unroll
-        for (int f = 0; f < F; ++f) {
-          half8 hi, lo = {};
-          element_operand(f, hi, lo);
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (4 * g + (j & 3) + 16 * (j >> 2) != t) hi[j] = lo[j] = (_Float16)0.0f;
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
-            const float4v alone = add(hi, lo, float4v{0, 0, 0, 0}, rt);
-            if (t0 + t < min(seen[rt], end)) o[f][rt] += alone;
-          }
-        }
     }
-  };
-  // Blocks of which all rows see all tokens, the next one on its way; then the others, one by one.
-  B cur;
-  int t0 = begin + wave * kTokens;
-  const int seen_by_all = min(end, least_seen);
-  if (t0 + kTokens <= seen_by_all) {
-    int32_t ids[2];
-    page_ids(t0, ids);
-    load_block(cur, t0, ids);
-    page_ids(t0 + kStep, ids);
-#pragma unroll 1
-    while (!cur.bad) {
-      B next;
-      const bool more = t0 + kStep + kTokens <= seen_by_all;
-      if (more) {
-        load_block(next, t0 + kStep, ids);
-        page_ids(t0 + 2 * kStep, ids);
-      }
-      work(cur, t0, Constant<false>{});
-      t0 += kStep;
-      if (!more) break;
-      cur = next;
+    if (more) {
+      load_values(next);
+      at = next;
     }
-  }
-#pragma unroll 1
-  for (; t0 < end; t0 += kStep) {
-    int32_t ids[2];
-    page_ids(t0, ids);
-    load_block(cur, t0, ids);
-    work(cur, t0, Constant<true>{});
   }
 
   // the waves' sums become one
@@ -583,22 +563,17 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
         const float v0 = o[f][rt][i] * inverse, v1 = o[f + 1][rt][i] * inverse;
         if (a.splits > 1) {
           *reinterpret_cast<float2*>(a.partial + at * D + d + f) = make_float2(v0, v1);
-        } else if (a.type == SQUANT_W_F32) {
-          struct Two { float v[2]; };
-          store_any(element<float>(a.out, row[rt], qhead[rt]) + d + f, Two{{v0, v1}});
-        } else if (a.type == SQUANT_W_F16) {
-          struct Two { _Float16 v[2]; };
-          store_any(element<_Float16>(a.out, row[rt], qhead[rt]) + d + f, Two{{(_Float16)v0, (_Float16)v1}});
         } else {
-          struct Two { __bf16 v[2]; };
-          store_any(element<__bf16>(a.out, row[rt], qhead[rt]) + d + f, Two{{(__bf16)v0, (__bf16)v1}});
+          struct Two { T v[2]; };
+          store_any(element<T>(a.out, row[rt], qhead[rt]) + d + f, Two{{(T)v0, (T)v1}});
         }
       }
     }
   }
 }
 
-// The splits of each row and head become its output: a wave for each.
+// The splits of each row and head become its output: a wave for each, lanes in groups of dim / 4 that take a split each, four
+// splits of a group on their way at once.
 template <int FORMATS> __global__ __launch_bounds__(kThreads) void join_splits(CacheAttentionArgs a) {
   const int lane = (int)threadIdx.x & 63;
   const int64_t at = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -611,30 +586,54 @@ template <int FORMATS> __global__ __launch_bounds__(kThreads) void join_splits(C
     const int64_t length = min((int64_t)max(a.cache.lengths[s], 0), (int64_t)a.cache.table_width * a.cache.page_size);
     parts = (int)((length + a.chunk - 1) / a.chunk);
   }
+  // 64, 32 (dim 96: 24), 16 or 8 lanes hold a row of four elements each
+  const int lanes = dim / 4, groups = dim == 192 ? 1 : 64 / lanes, group = lane / lanes, d = (lane - group * lanes) * 4;
+  const bool mine = group < groups;
   float m = -kInfinity;
   for (int i = lane; i < parts; i += 64) m = fmaxf(m, a.stats[i * all + at].x);
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
   const float base = m == -kInfinity ? 0.0f : m;
-  float total = 0.0f, v[4] = {0, 0, 0, 0};
-  for (int i = 0; i < parts; ++i) {
-    const float2 st = a.stats[i * all + at];
-    const float w = exp2_fast(st.x - base);
-    total += st.y * w;
-    const float* p = a.partial + (i * all + at) * dim;
+  float total = 0.0f;
+  float4v v = {0, 0, 0, 0};
+  for (int i = group; i < parts; i += 4 * groups) {
+    float2 st[4];
+    float4v p[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (k * 64 + lane < dim) v[k] = __builtin_fmaf(p[k * 64 + lane], w, v[k]);
+    for (int k = 0; k < 4; ++k) {
+      const int64_t j = min(i + k * groups, parts - 1);
+      st[k] = a.stats[j * all + at];
+      p[k] = *reinterpret_cast<const float4v*>(a.partial + (j * all + at) * dim + d);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float w = mine && i + k * groups < parts ? exp2_fast(st[k].x - base) : 0.0f;
+      if (w == 0.0f && i + k * groups >= parts) continue;
+      total += st[k].y * w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(p[k][e], w, v[e]);
+    }
   }
-  const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+  // the groups' sums, in their order
+  float sum = 0.0f;
+  float4v out = {0, 0, 0, 0};
+  for (int g = 0; g < groups; ++g) {
+    const int from = g * lanes + d / 4;
+    sum += __shfl(total, from);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int d = k * 64 + lane;
-    if (d >= dim) continue;
-    const float x = v[k] * inverse;
-    if (a.type == SQUANT_W_F32) element<float>(a.out, row, head)[d] = x;
-    else if (a.type == SQUANT_W_F16) element<_Float16>(a.out, row, head)[d] = (_Float16)x;
-    else element<__bf16>(a.out, row, head)[d] = (__bf16)x;
+    for (int e = 0; e < 4; ++e) out[e] += __shfl(v[e], from);
+  }
+  if (group != 0) return;
+  const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
+  if (a.type == SQUANT_W_F32) {
+    struct Four { float v[4]; };
+    store_any(element<float>(a.out, row, head) + d, Four{{out[0] * inverse, out[1] * inverse, out[2] * inverse, out[3] * inverse}});
+  } else if (a.type == SQUANT_W_F16) {
+    struct Four { _Float16 v[4]; };
+    store_any(element<_Float16>(a.out, row, head) + d, Four{{(_Float16)(out[0] * inverse), (_Float16)(out[1] * inverse), (_Float16)(out[2] * inverse), (_Float16)(out[3] * inverse)}});
+  } else {
+    struct Four { __bf16 v[4]; };
+    store_any(element<__bf16>(a.out, row, head) + d, Four{{(__bf16)(out[0] * inverse), (__bf16)(out[1] * inverse), (__bf16)(out[2] * inverse), (__bf16)(out[3] * inverse)}});
   }
 }
 
@@ -642,30 +641,30 @@ template <int FORMATS> __global__ __launch_bounds__(kThreads) void join_splits(C
 inline size_t cache_attention_lds(int ng, int rt) { return (size_t)kWaves * 2 * 16 * rt * 4 + (size_t)2 * (ng * 2) * rt * 64 * 16; }
 
 typedef void (*cache_attention_t)(CacheAttentionArgs);
-template <int FMT, int PL, bool LOW, bool HALVES> cache_attention_t cache_attention_of(int ng, int rt) {
+template <class T, int FMT, bool HALVES> cache_attention_t cache_attention_of(int ng, int rt) {
   if constexpr (HALVES) {
     if (rt == 2) switch (ng) {
-      case 1: return cache_attention<FMT, 1, PL, LOW, 2, HALVES>;
-      case 2: return cache_attention<FMT, 2, PL, LOW, 2, HALVES>;
-      case 3: return cache_attention<FMT, 3, PL, LOW, 2, HALVES>;
-      case 4: return cache_attention<FMT, 4, PL, LOW, 2, HALVES>;
+      case 1: return cache_attention<T, FMT, 1, 2, HALVES>;
+      case 2: return cache_attention<T, FMT, 2, 2, HALVES>;
+      case 3: return cache_attention<T, FMT, 3, 2, HALVES>;
+      case 4: return cache_attention<T, FMT, 4, 2, HALVES>;
     }
   }
   switch (ng) {
-    case 1: return cache_attention<FMT, 1, PL, LOW, 1, HALVES>;
-    case 2: return cache_attention<FMT, 2, PL, LOW, 1, HALVES>;
-    case 3: return cache_attention<FMT, 3, PL, LOW, 1, HALVES>;
-    case 4: return cache_attention<FMT, 4, PL, LOW, 1, HALVES>;
-    case 6: return cache_attention<FMT, 6, PL, LOW, 1, HALVES>;
-    case 8: return cache_attention<FMT, 8, PL, LOW, 1, HALVES>;
+    case 1: return cache_attention<T, FMT, 1, 1, HALVES>;
+    case 2: return cache_attention<T, FMT, 2, 1, HALVES>;
+    case 3: return cache_attention<T, FMT, 3, 1, HALVES>;
+    case 4: return cache_attention<T, FMT, 4, 1, HALVES>;
+    case 6: return cache_attention<T, FMT, 6, 1, HALVES>;
+    case 8: return cache_attention<T, FMT, 8, 1, HALVES>;
     default: return nullptr;
   }
 }
-template <int FMT, int PL, bool LOW> cache_attention_t cache_attention_of(int ng, int rt, bool halves) {
-  return halves ? cache_attention_of<FMT, PL, LOW, true>(ng, rt) : cache_attention_of<FMT, PL, LOW, false>(ng, rt);
+template <class T, int FMT> cache_attention_t cache_attention_of(int ng, int rt, bool halves) {
+  return halves ? cache_attention_of<T, FMT, true>(ng, rt) : cache_attention_of<T, FMT, false>(ng, rt);
 }
-// By format, and by type: bfloat16 (8 bits only), 16 bits, binary32.
-cache_attention_t cache_attention_int4(int ng, int rt, bool halves);
+cache_attention_t cache_attention_int4_bf16(int ng, int rt, bool halves);
+cache_attention_t cache_attention_int4_f16(int ng, int rt, bool halves);
 cache_attention_t cache_attention_int4_f32(int ng, int rt, bool halves);
 cache_attention_t cache_attention_int8_bf16(int ng, int rt, bool halves);
 cache_attention_t cache_attention_int8_f16(int ng, int rt, bool halves);

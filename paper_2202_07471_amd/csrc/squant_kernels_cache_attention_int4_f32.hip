@@ -1,10 +1,10 @@
-// Attention over a cache of 4-bit codes, binary32 queries.
+// Attention over a cache of 4-bit codes, binary32.
 #include "squant_cache_attention.h"
 
 namespace squant {
 namespace att {
 
-cache_attention_t cache_attention_int4_f32(int ng, int rt, bool halves) { return cache_attention_of<SQUANT_OUT_INT4, 2, false>(ng, rt, halves); }
+cache_attention_t cache_attention_int4_f32(int ng, int rt, bool halves) { return cache_attention_of<float, SQUANT_OUT_INT4>(ng, rt, halves); }
 
 }  // namespace att
 }  // namespace squant

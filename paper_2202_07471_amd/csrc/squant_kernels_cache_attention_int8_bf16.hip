@@ -1,10 +1,10 @@
-// Attention over a cache of 8-bit codes, bfloat16 queries.
+// Attention over a cache of 8-bit codes, bfloat16.
 #include "squant_cache_attention.h"
 
 namespace squant {
 namespace att {
 
-cache_attention_t cache_attention_int8_bf16(int ng, int rt, bool halves) { return cache_attention_of<SQUANT_OUT_INT8, 1, false>(ng, rt, halves); }
+cache_attention_t cache_attention_int8_bf16(int ng, int rt, bool halves) { return cache_attention_of<__bf16, SQUANT_OUT_INT8>(ng, rt, halves); }
 
 }  // namespace att
 }  // namespace squant
