@@ -347,7 +347,8 @@ typedef struct {
 /* Where sequences lie in a cache, and which of their tokens a call is about.  Token t of sequence b is in slot
  * t % page_size of page table[b][t / page_size].  lengths[b] tokens of it count, the call's own among them: row r of
  * sequence b is token lengths[b] - (starts[b + 1] - r), the rows being its last ones.  starts NULL: one row for each
- * sequence.  A table's entry that is no page, or lengths beyond the table: nothing is written there, and NaN is read. */
+ * sequence.  A table's entry that is no page, or lengths beyond the table: nothing is written there, and NaN is read.  A row
+ * that sees a token whose scale is NaN or infinite is NaN.  For attention a table holds at most 2^30 tokens. */
 typedef struct {
   const int32_t* table;   /* device, [sequences][table_width] */
   const int32_t* lengths; /* device, [sequences] */

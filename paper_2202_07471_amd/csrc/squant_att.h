@@ -105,19 +105,32 @@ __host__ __device__ __forceinline__ int64_t tiles_bound(int64_t rows, int per_ro
 }
 struct Tile {
   int sequence;  // -1: this tile is no one's
+  int start, length;  // its sequence's rows
   int first;     // its first unit within the sequence
   int index, tiles;
 };
 __device__ __forceinline__ Tile find_tile(const Packed& p, int64_t id, int per_row, int tile) {
   Tile t;
-  auto v = [&](int i) { return (int64_t)p.start(i) * per_row / tile + i; };
-  t.sequence = last_not_above(v, p.count + 1, id);
-  if (t.sequence < 0) return t;
-  const int64_t units = (int64_t)p.length(t.sequence) * per_row, at = id - v(t.sequence);
+  auto place = [&](int start, int i) { return (int64_t)start * per_row / tile + i; };
+  if (p.starts && p.count < 63) {
+    // a lane for each sequence: what is found of it is in another lane's registers already
+    const int lane = (int)(threadIdx.x & 63u), mine = p.start(min(lane, p.count));
+    const int found = __popcll(lanes_where(lane <= p.count && place(mine, lane) <= id)) - 1;
+    t.sequence = __builtin_amdgcn_readfirstlane(found);
+    if (t.sequence < 0) return t;
+    t.start = __builtin_amdgcn_readlane(mine, t.sequence);
+    t.length = max((t.sequence < p.count ? __builtin_amdgcn_readlane(mine, t.sequence + 1) : p.rows) - t.start, 0);
+  } else {
+    t.sequence = last_not_above([&](int i) { return place(p.start(i), i); }, p.count + 1, id);
+    if (t.sequence < 0) return t;
+    t.start = p.start(t.sequence);
+    t.length = p.length(t.sequence);
+  }
+  const int64_t units = (int64_t)t.length * per_row, at = id - place(t.start, t.sequence);
   t.tiles = (int)((units + tile - 1) / tile);
   t.index = (int)at;
   t.first = (int)(at * tile);
-  if (at * tile >= units) t.sequence = -1;
+  if (at < 0 || at * tile >= units) t.sequence = -1;  // below 0: starts that fall
   return t;
 }
 

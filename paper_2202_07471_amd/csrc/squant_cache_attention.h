@@ -147,22 +147,26 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
   const int head = (int)blockIdx.x % c.heads;
   const int split = (int)blockIdx.y;
 
-  // whose rows these are
+  // whose rows these are; of few sequences, lengths are on their way meanwhile
   Tile tile;
   const int tile_id = (int)(blockIdx.x / (uint32_t)c.heads);
+  const bool few = a.rows.count <= 64;
+  const int lane_length = few && a.rows.count ? c.lengths[min(lane, a.rows.count - 1)] : 0;
   if (a.rows.one_each) {
     const int each = (a.group + TR - 1) / TR;
     tile.sequence = tile_id / each;
     tile.first = (tile_id - tile.sequence * each) * TR;
+    tile.start = tile.sequence, tile.length = 1;
     if (tile.sequence >= a.rows.count) return;
   } else {
     tile = find_tile(a.rows, tile_id, a.group, TR);
   }
   if (tile.sequence < 0) return;
-  const int seq = tile.sequence, row0 = a.rows.start(seq), count = a.rows.length(seq);
+  const int seq = tile.sequence, row0 = tile.start, count = tile.length;
   const int64_t capacity = (int64_t)c.table_width * c.page_size;
-  const int said = seq < a.rows.count ? max(c.lengths[seq], 0) : 0;
-  const int length = (int)min((int64_t)said, capacity), last = max(length - 1, 0);
+  int said = 0;
+  if (seq < a.rows.count) said = max(few ? __builtin_amdgcn_readlane(lane_length, seq) : c.lengths[seq], 0);
+  const int length = (int)min((int64_t)said, capacity);
   const int begin = split * a.chunk, end = min(length, begin + a.chunk);
   if (a.splits > 1 && (begin >= max(length, 1) || seq == a.rows.count)) return;  // the join knows
 
@@ -183,6 +187,22 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
   // rows of a tile see no less than its first
   least_seen = min(__builtin_amdgcn_readfirstlane(least_seen), end);
   const float poison = said > length ? __builtin_nanf("") : 1.0f;
+
+  // where a block's tokens are: on its way before the queries
+  const uint32_t head_row = (uint32_t)head * (uint32_t)c.page_size;
+  auto page_ids = [&](int t0, int32_t (&id)[2]) {
+    id[0] = id[1] = -1;
+    if (seq >= a.rows.count) return;  // rows behind the last sequence have no row of the table
+    if constexpr (HALVES) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) id[h] = __builtin_amdgcn_readfirstlane(c.table_at(seq, c.page_of(t0 + 16 * h)));
+    } else {
+      id[0] = id[1] = c.table_at(seq, c.page_of(t0 + (lane & 31)));
+    }
+  };
+  int t0 = begin + wave * kTokens;
+  int32_t ids[2];
+  page_ids(t0, ids);
 
   half8 q[RT][PL][NG];
   float factor[RT];
@@ -212,33 +232,24 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
       }
   }
 
-  // Where a block's tokens lie.  `bad`: tokens whose page is none.
+  // Where a block's tokens lie, those past the sequence's end wherever the table says.  `bad`: tokens whose page is none.
   struct Where {
     int64_t first[2];  // HALVES: rows of the halves' first tokens
     int32_t row;       // else: the row of token t0 + lane % 32
     uint32_t bad;
-  };
-  const uint32_t head_row = (uint32_t)head * (uint32_t)c.page_size;
-  auto page_ids = [&](int t0, int32_t (&id)[2]) {
-    if constexpr (HALVES) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) id[h] = __builtin_amdgcn_readfirstlane(c.table_at(seq, c.page_of(min(t0 + 16 * h, last))));
-    } else {
-      id[0] = id[1] = c.table_at(seq, c.page_of(min(t0 + (lane & 31), last)));
-    }
   };
   auto find = [&](Where& w, int t0, const int32_t (&id)[2]) {
     w.bad = 0;
     if constexpr (HALVES) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int t = min(t0 + 16 * h, last);
-        const int32_t r = c.row_of(t / 16 * 16, c.page_of(t), id[h]);
+        const int t = t0 + 16 * h;
+        const int32_t r = c.row_of(t, c.page_of(t), id[h]);
         if (r < 0) w.bad |= 0xffffu << (16 * h);
         w.first[h] = r < 0 ? 0 : (int64_t)(r + head_row);  // rows 0 to 15 are there
       }
     } else {
-      const int t = min(t0 + (lane & 31), last);
+      const int t = t0 + (lane & 31);
       const int32_t r = c.row_of(t, c.page_of(t), id[0]);
       w.bad = (uint32_t)lanes_where(r < 0);
       w.row = r < 0 ? 0 : (int32_t)(r + head_row);
@@ -312,11 +323,8 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
   int key_e = 126, value_e = 126;
   const Magic magic;
 
-  int t0 = begin + wave * kTokens;
   Where at, next;
-  int32_t ids[2];
   if (t0 < end) {
-    page_ids(t0, ids);
     find(at, t0, ids);
     load_keys(at);
     load_values(at);

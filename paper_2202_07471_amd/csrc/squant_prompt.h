@@ -244,7 +244,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
   if (tile.sequence < 0) return;
   // the longest tiles of a causal sequence first
   const int seq = tile.sequence, first = (tile.tiles - 1 - tile.index) * kRows;
-  const int rows = a.queries.length(seq), q0 = a.queries.start(seq);
+  const int rows = tile.length, q0 = tile.start;
   const int keys = seq < a.queries.count ? a.keys.length(seq) : 0, k0 = a.keys.start(min(seq, a.keys.count));
   const int shift = keys - rows;
   auto sees = [&](int r) { return a.causal ? min(max(r + shift + 1, 0), keys) : keys; };
