@@ -92,6 +92,9 @@ class QuantizedCache(NamedTuple):
         return cls(*one(), *one())
 
 
+_HEAD_DIMS = frozenset((32, 64, 96, 128, 192, 256))
+
+
 def _cache(cache: QuantizedCache, device: int) -> squant_cache_t:
     kc, ks, vc, vs = cache
     shape = kc.shape
@@ -101,16 +104,17 @@ def _cache(cache: QuantizedCache, device: int) -> squant_cache_t:
         fmt, dim = OUT_INT8, shape[-1] if len(shape) == 4 else 0
     else:
         raise ValueError("a cache's codes must be int8, or uint8 with two 4-bit codes a byte")
-    if dim not in (32, 64, 96, 128, 192, 256):
+    if dim not in _HEAD_DIMS:
         raise ValueError("a cache's codes must be [pages, heads, page_size, bytes] of heads of 32, 64, 96, 128, 192 or 256 elements")
-    scales = shape[:3] + (dim // _SCALE_GROUP,)
+    pages, heads, page_size, _ = shape
+    scales = (pages, heads, page_size, dim // _SCALE_GROUP)
     if (vc.dtype is not kc.dtype or vc.shape != shape or ks.shape != scales or vs.shape != scales
             or ks.dtype is not torch.bfloat16 or vs.dtype is not torch.bfloat16):
         raise ValueError("a cache's values must be like its keys, its scales bfloat16 with one for each 32 elements")
-    for t in cache:
-        if not t.is_contiguous() or t.get_device() != device:
-            raise ValueError("a cache's tensors must be contiguous and on the activations' device")
-    return squant_cache_t(kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr(), shape[0], shape[2], shape[1], dim, fmt)
+    if not (kc.is_contiguous() and ks.is_contiguous() and vc.is_contiguous() and vs.is_contiguous()
+            and kc.get_device() == ks.get_device() == vc.get_device() == vs.get_device() == device):
+        raise ValueError("a cache's tensors must be contiguous and on the activations' device")
+    return squant_cache_t(kc.data_ptr(), ks.data_ptr(), vc.data_ptr(), vs.data_ptr(), pages, page_size, heads, dim, fmt)
 
 
 def _ints(t: torch.Tensor, count: Optional[int], what: str, device: int) -> int:
@@ -125,36 +129,45 @@ def _paged(table: torch.Tensor, lengths: torch.Tensor, starts: Optional[torch.Te
     if table.dtype is not torch.int32 or table.dim() != 2 or not table.is_contiguous() or table.get_device() != device:
         raise ValueError("table must be a contiguous int32 tensor [sequences, pages of each] on the activations' device")
     sequences, width = table.shape
-    _ints(lengths, sequences, "lengths", device)
+    at = _ints(lengths, sequences, "lengths", device)
     if starts is not None:
-        _ints(starts, sequences + 1, "starts", device)
-    elif rows != sequences:
+        return squant_paged_t(table.data_ptr(), at, _ints(starts, sequences + 1, "starts", device), sequences, width)
+    if rows != sequences:
         raise ValueError("without starts there must be one row for each sequence")
-    return squant_paged_t(table.data_ptr(), lengths.data_ptr(), None if starts is None else starts.data_ptr(), sequences, width)
+    return squant_paged_t(table.data_ptr(), at, None, sequences, width)
 
 
-def _heads(t: torch.Tensor, heads: Optional[int], dim: Optional[int], what: str, device: int, like: Optional[torch.Tensor] = None,
-           rows: Optional[int] = None) -> squant_heads_t:
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or (heads is not None and shape[1] != heads) or (dim is not None and shape[2] != dim) or (
-            rows is not None and shape[0] != rows):
-        raise ValueError(f"{what} must be [{'rows' if rows is None else rows}, {'heads' if heads is None else heads}, "
-                         f"{'head_dim' if dim is None else dim}]")
-    if t.get_device() != device or (like is not None and t.dtype is not like.dtype):
+def _heads(t: torch.Tensor, shape, what: str, device: int, dtype) -> squant_heads_t:
+    """t as [rows, heads, head_dim] of this shape."""
+    if t.shape != shape:
+        raise ValueError(f"{what} must be [{shape[0]}, {shape[1]}, {shape[2]}]")
+    if t.dtype is not dtype or t.get_device() != device:
         raise ValueError(f"{what} must have the type and the device of the other activations")
-    if (shape[2] > 1 and stride[2] != 1) or (shape[1] > 1 and stride[1] < shape[2]) or (shape[0] > 1 and stride[0] < shape[2]):
-        raise ValueError(f"{what} must have contiguous heads that do not overlap")
-    return squant_heads_t(t.data_ptr(), stride[0], stride[1])
+    row, head, element = t.stride()
+    rows, heads, dim = shape
+    if element != 1 or head < dim or row < dim:
+        if (dim > 1 and element != 1) or (heads > 1 and head < dim) or (rows > 1 and row < dim):
+            raise ValueError(f"{what} must have contiguous heads that do not overlap")
+    return squant_heads_t(t.data_ptr(), row, head)
 
 
-def _result(t: torch.Tensor, like: torch.Tensor, heads: int, dim: int, what: str, device: int, rows: int) -> squant_heads_t:
-    h = _heads(t, heads, dim, what, device, like, rows)
-    if rows > 1 and heads > 1 and abs(t.stride(0)) < (heads - 1) * t.stride(1) + dim and t.stride(1) < (rows - 1) * t.stride(0) + dim:
+def _result(t: Optional[torch.Tensor], shape, what: str, device: int, dtype, like: torch.Tensor):
+    """(t, or a new tensor like `like`, as [rows, heads, head_dim] that may be written)."""
+    rows, heads, dim = shape
+    if t is None:
+        t = torch.empty(shape, dtype=dtype, device=like.device)
+        return t, squant_heads_t(t.data_ptr(), heads * dim, dim)
+    h = _heads(t, shape, what, device, dtype)
+    if rows > 1 and heads > 1 and h.row < (heads - 1) * h.head + dim and h.head < (rows - 1) * h.row + dim:
         raise ValueError(f"rows and heads of {what} overlap")
-    return h
+    return t, h
 
 
-_ref = ctypes.byref
+def _shape3(t: torch.Tensor, what: str):
+    shape = t.shape
+    if len(shape) != 3:
+        raise ValueError(f"{what} must be [rows, heads, head_dim]")
+    return shape
 
 
 def squant_cache_write(k: torch.Tensor, v: torch.Tensor, cache: QuantizedCache, table: torch.Tensor, lengths: torch.Tensor,
@@ -169,11 +182,12 @@ def squant_cache_write(k: torch.Tensor, v: torch.Tensor, cache: QuantizedCache, 
             return squant_cache_write(k, v, cache, table, lengths, starts)
     device = _device(k, "k")
     c = _cache(cache, device)
-    rows = k.shape[0] if k.dim() else 0
-    hk = _heads(k, c.heads, c.head_dim, "k", device)
-    hv = _heads(v, c.heads, c.head_dim, "v", device, k, rows)
+    rows = _shape3(k, "k")[0]
+    shape, dtype = (rows, c.heads, c.head_dim), k.dtype
+    hk = _heads(k, shape, "k", device, dtype)
+    hv = _heads(v, shape, "v", device, dtype)
     w = _paged(table, lengths, starts, rows, device)
-    _check(_lib().squant_cache_write(_ref(hk), _ref(hv), _WTYPES[k.dtype], rows, _ref(c), _ref(w), _current_stream(device)))
+    _check(_lib().squant_cache_write(hk, hv, _WTYPES[dtype], rows, c, w, _current_stream(device)))
 
 
 def squant_cache_read(cache: QuantizedCache, table: torch.Tensor, lengths: torch.Tensor, starts: Optional[torch.Tensor], rows: int,
@@ -191,16 +205,10 @@ def squant_cache_read(cache: QuantizedCache, table: torch.Tensor, lengths: torch
     if rows < 0:
         raise ValueError("rows must not be negative")
     shape = (rows, c.heads, c.head_dim)
-    if k is None:
-        k = torch.empty(shape, dtype=dtype, device=cache.key_scales.device)
-    if v is None:
-        v = torch.empty(shape, dtype=dtype, device=cache.key_scales.device)
-    if k.dtype is not dtype:
-        raise ValueError("k must have the type asked for")
-    hk = _result(k, k, c.heads, c.head_dim, "k", device, rows)
-    hv = _result(v, k, c.heads, c.head_dim, "v", device, rows)
+    k, hk = _result(k, shape, "k", device, dtype, cache.key_scales)
+    v, hv = _result(v, shape, "v", device, dtype, cache.key_scales)
     w = _paged(table, lengths, starts, rows, device)
-    _check(_lib().squant_cache_read(_ref(c), _ref(w), _WTYPES[dtype], rows, _ref(hk), _ref(hv), _current_stream(device)))
+    _check(_lib().squant_cache_read(c, w, _WTYPES[dtype], rows, hk, hv, _current_stream(device)))
     return k, v
 
 
@@ -211,32 +219,31 @@ def squant_cache_attention(q: torch.Tensor, cache: QuantizedCache, table: torch.
     rows are placed as in squant_cache_write, and each sees the tokens up to its own.
 
     heads is a multiple of the cache's; scale defaults to head_dim ** -0.5.  For one or a few new tokens of each sequence; a whole
-    prompt is squant_attention's.  Rows that see nothing are 0, rows behind the last sequence too."""
+    prompt is squant_attention's.  Rows that see nothing are 0, rows behind the last sequence too.  `out` may be q."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return squant_cache_attention(q, cache, table, lengths, starts, scale, out)
     device = _device(q, "q")
     c = _cache(cache, device)
-    hq = _heads(q, None, c.head_dim, "q", device)
-    rows, heads = q.shape[0], q.shape[1]
+    dim = c.head_dim
+    rows, heads, _ = _shape3(q, "q")
     if heads % c.heads or heads == 0:
         raise ValueError("q must have a multiple of the cache's heads")
+    shape, dtype = (rows, heads, dim), q.dtype
+    hq = _heads(q, shape, "q", device, dtype)
     w = _paged(table, lengths, starts, rows, device)
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    ho = _result(out, q, heads, c.head_dim, "out", device, rows)
-    nbytes = _lib().squant_cache_attention_workspace_bytes(rows, heads, _ref(c), _ref(w))
+    out, ho = _result(out, shape, "out", device, dtype, q)
+    L = _lib()
+    nbytes = L.squant_cache_attention_workspace_bytes(rows, heads, c, w)
     ws = _workspace(q, nbytes)
-    _check(_lib().squant_cache_attention(_ref(hq), _WTYPES[q.dtype], rows, heads, _ref(c), _ref(w),
-                                         c.head_dim ** -0.5 if scale is None else scale, _ref(ho),
-                                         None if ws is None else ws.data_ptr(), nbytes, _current_stream(device)))
+    _check(L.squant_cache_attention(hq, _WTYPES[dtype], rows, heads, c, w, dim ** -0.5 if scale is None else scale, ho,
+                                    None if ws is None else ws.data_ptr(), nbytes, _current_stream(device)))
     return out
 
 
 def _packed(q: torch.Tensor, k: torch.Tensor, starts, k_starts, scale, causal, device: int) -> squant_packed_t:
-    if q.dim() != 3 or k.dim() != 3:
-        raise ValueError("q, k and v must be [rows, heads, head_dim]")
-    heads, dim, kv_heads = q.shape[1], q.shape[2], k.shape[1]
+    rows, heads, dim = _shape3(q, "q")
+    keys, kv_heads, _ = _shape3(k, "k")
     if dim == 0 or dim % 8 or dim > 256:
         raise ValueError("head_dim must be a multiple of 8 up to 256")
     if kv_heads == 0 or heads == 0 or heads % kv_heads:
@@ -249,13 +256,13 @@ def _packed(q: torch.Tensor, k: torch.Tensor, starts, k_starts, scale, causal, d
     else:
         qs = _ints(starts, None, "starts", device)
         sequences = starts.shape[0] - 1
-        if k_starts is None and k.shape[0] != q.shape[0]:
+        if k_starts is None and keys != rows:
             raise ValueError("without k_starts there must be as many keys as queries")
         ks = qs if k_starts is None else _ints(k_starts, sequences + 1, "k_starts", device)
     scale = dim ** -0.5 if scale is None else float(scale)
     if not (0 <= scale < math.inf):
         raise ValueError("scale must be finite and not negative")
-    return squant_packed_t(qs, ks, sequences, q.shape[0], k.shape[0], heads, kv_heads, dim, bool(causal), scale)
+    return squant_packed_t(qs, ks, sequences, rows, keys, heads, kv_heads, dim, bool(causal), scale)
 
 
 def squant_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None,
@@ -265,21 +272,21 @@ def squant_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: 
 
     Query head h goes with key head h // (heads / kv_heads).  starts are the sequences' first rows of q (and of k, unless
     k_starts says otherwise), None: one sequence.  causal: a sequence's last row sees all of its keys, the row before it one
-    less, and so on.  lse [heads, q_rows] is the float32 log-sum-exp of each row's scores.  Rows that see no key are 0."""
+    less, and so on.  lse [heads, q_rows] is the float32 log-sum-exp of each row's scores.  Rows that see no key are 0.
+    `out` may be q."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return squant_attention(q, k, v, starts, k_starts, scale, causal, out)
     device = _device(q, "q")
     p = _packed(q, k, starts, k_starts, scale, causal, device)
-    hq = _heads(q, None, None, "q", device)
-    hk = _heads(k, p.kv_heads, p.head_dim, "k", device, q)
-    hv = _heads(v, p.kv_heads, p.head_dim, "v", device, q, p.k_rows)
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    ho = _result(out, q, p.heads, p.head_dim, "out", device, p.q_rows)
+    dtype = q.dtype
+    q_shape, k_shape = (p.q_rows, p.heads, p.head_dim), (p.k_rows, p.kv_heads, p.head_dim)
+    hq = _heads(q, q_shape, "q", device, dtype)
+    hk = _heads(k, k_shape, "k", device, dtype)
+    hv = _heads(v, k_shape, "v", device, dtype)
+    out, ho = _result(out, q_shape, "out", device, dtype, q)
     lse = torch.empty((p.heads, p.q_rows), dtype=torch.float32, device=q.device)
-    _check(_lib().squant_attention(_ref(hq), _ref(hk), _ref(hv), _WTYPES[q.dtype], _ref(p), _ref(ho), lse.data_ptr(),
-                                   _current_stream(device)))
+    _check(_lib().squant_attention(hq, hk, hv, _WTYPES[dtype], p, ho, lse.data_ptr(), _current_stream(device)))
     return out, lse
 
 
@@ -294,25 +301,23 @@ def squant_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tens
             return squant_attention_backward(dout, q, k, v, out, lse, starts, k_starts, scale, causal, dq, dk, dv)
     device = _device(q, "q")
     p = _packed(q, k, starts, k_starts, scale, causal, device)
-    h, kv, dim = p.heads, p.kv_heads, p.head_dim
-    hq = _heads(q, None, None, "q", device)
-    hk = _heads(k, kv, dim, "k", device, q)
-    hv = _heads(v, kv, dim, "v", device, q, p.k_rows)
-    ho = _heads(out, h, dim, "out", device, q, p.q_rows)
-    hd = _heads(dout, h, dim, "dout", device, q, p.q_rows)
-    if lse.dtype is not torch.float32 or lse.shape != (h, p.q_rows) or not lse.is_contiguous() or lse.get_device() != device:
+    dtype = q.dtype
+    q_shape, k_shape = (p.q_rows, p.heads, p.head_dim), (p.k_rows, p.kv_heads, p.head_dim)
+    hq = _heads(q, q_shape, "q", device, dtype)
+    hk = _heads(k, k_shape, "k", device, dtype)
+    hv = _heads(v, k_shape, "v", device, dtype)
+    ho = _heads(out, q_shape, "out", device, dtype)
+    hd = _heads(dout, q_shape, "dout", device, dtype)
+    if lse.dtype is not torch.float32 or lse.shape != (p.heads, p.q_rows) or not lse.is_contiguous() or lse.get_device() != device:
         raise ValueError("lse must be what squant_attention returned for these rows")
-    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
-    dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dk is None else dk
-    dv = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dv is None else dv
-    gq = _result(dq, q, h, dim, "dq", device, p.q_rows)
-    gk = _result(dk, q, kv, dim, "dk", device, p.k_rows)
-    gv = _result(dv, q, kv, dim, "dv", device, p.k_rows)
-    nbytes = _lib().squant_attention_backward_workspace_bytes(_ref(p))
+    dq, gq = _result(dq, q_shape, "dq", device, dtype, q)
+    dk, gk = _result(dk, k_shape, "dk", device, dtype, q)
+    dv, gv = _result(dv, k_shape, "dv", device, dtype, q)
+    L = _lib()
+    nbytes = L.squant_attention_backward_workspace_bytes(p)
     ws = _workspace(q, nbytes)
-    _check(_lib().squant_attention_backward(_ref(hd), _ref(hq), _ref(hk), _ref(hv), _ref(ho), lse.data_ptr(), _WTYPES[q.dtype],
-                                            _ref(p), _ref(gq), _ref(gk), _ref(gv), None if ws is None else ws.data_ptr(), nbytes,
-                                            _current_stream(device)))
+    _check(L.squant_attention_backward(hd, hq, hk, hv, ho, lse.data_ptr(), _WTYPES[dtype], p, gq, gk, gv,
+                                       None if ws is None else ws.data_ptr(), nbytes, _current_stream(device)))
     return dq, dk, dv
 
 
