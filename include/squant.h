@@ -395,7 +395,7 @@ int squant_attention(const squant_heads_t* h_q, const squant_heads_t* h_k, const
  * dv = sum p dout,  ds = p (dout . v - dout . out),  dq = scale * sum ds k,  dk = scale * sum ds q, the latter two sums
  * over the query heads of a group as well.  Rows of no sequence get 0.  A NaN or an infinity in a position that a row
  * does not see may make gradients of up to 128 rows beside it NaN.  rows = 0: keys without queries get 0. */
-size_t squant_attention_backward_workspace_bytes(const squant_packed_t* h_packed);
+size_t squant_attention_backward_workspace_bytes(const squant_packed_t* h_packed, squant_wtype_t type);
 int squant_attention_backward(const squant_heads_t* h_dout, const squant_heads_t* h_q, const squant_heads_t* h_k,
                               const squant_heads_t* h_v, const squant_heads_t* h_out, const float* d_lse,
                               squant_wtype_t type, const squant_packed_t* h_packed, const squant_heads_t* h_dq,

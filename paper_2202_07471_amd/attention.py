@@ -56,7 +56,7 @@ def _lib():
         L.squant_cache_attention_workspace_bytes.argtypes = [i64, i32, cp, wp]
         L.squant_cache_attention.argtypes = [hp, en, i64, i32, cp, wp, fl, hp, vp, sz, vp]
         L.squant_attention.argtypes = [hp, hp, hp, en, pp, hp, vp, vp]
-        L.squant_attention_backward_workspace_bytes.argtypes = [pp]
+        L.squant_attention_backward_workspace_bytes.argtypes = [pp, en]
         L.squant_attention_backward.argtypes = [hp, hp, hp, hp, hp, vp, en, pp, hp, hp, hp, vp, sz, vp]
         for f in ("cache_write", "cache_read", "cache_attention", "attention", "attention_backward"):
             getattr(L, f"squant_{f}").restype = en
@@ -314,7 +314,7 @@ def squant_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tens
     dk, gk = _result(dk, k_shape, "dk", device, dtype, q)
     dv, gv = _result(dv, k_shape, "dv", device, dtype, q)
     L = _lib()
-    nbytes = L.squant_attention_backward_workspace_bytes(p)
+    nbytes = L.squant_attention_backward_workspace_bytes(p, _WTYPES[dtype])
     ws = _workspace(q, nbytes)
     _check(L.squant_attention_backward(hd, hq, hk, hv, ho, lse.data_ptr(), _WTYPES[dtype], p, gq, gk, gv,
                                        None if ws is None else ws.data_ptr(), nbytes, _current_stream(device)))

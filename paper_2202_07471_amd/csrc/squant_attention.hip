@@ -173,7 +173,37 @@ int64_t prompt_groups(const Packed& p, const PromptKernel& k, int32_t heads) {
   return tiles_bound(p.rows, 1, k.rows, p.count) * heads;
 }
 
-size_t delta_bytes(const squant_packed_t& p) { return ((size_t)p.q_rows * p.heads * 4 + 255) / 256 * 256; }
+// A backward pass's workspace and launches.  Where there are fewer workgroups than run at once, walks are cut into pieces whose sums
+// a launch more adds up: about 512 workgroups, at least 2 tiles a piece on average, at most 8 pieces.  Queries are walked over by
+// dK and dV of all types, keys by dQ of binary32 (16-bit types have more to add up there, and are a tenth of the time).
+// Six packed sequences of up to 515 tokens, six heads of 96, binary32: SPLIT_FIGURES.
+struct BackwardPlan {
+  PromptKernel queries, keys;
+  int64_t q_groups, k_groups, delta_groups;
+  int q_splits, k_splits;
+  size_t delta, q_partial, k_partial;  // bytes; the partial sums follow delta, one after the other's use
+  bool fit;
+  size_t bytes() const { return delta + std::max(q_partial, k_partial); }
+};
+int walk_splits(int64_t groups, int64_t walked, int64_t sequences, int heads, int tile) {
+  const int64_t tiles = heads * (walked / std::max<int64_t>(1, sequences)) / tile;
+  return (int)std::max<int64_t>(1, std::min({(int64_t)8, 512 / std::max<int64_t>(1, groups), tiles / 2}));
+}
+BackwardPlan plan_backward(const squant_packed_t& p, int type, bool queries_direct, bool keys_direct) {
+  BackwardPlan b{};
+  b.queries = (type == SQUANT_W_F32 ? prompt_queries_f32 : type == SQUANT_W_F16 ? prompt_queries_f16 : prompt_queries_bf16)(p.head_dim, keys_direct);
+  b.keys = (type == SQUANT_W_F32 ? prompt_keys_f32 : type == SQUANT_W_F16 ? prompt_keys_f16 : prompt_keys_bf16)(p.head_dim, queries_direct);
+  const PromptArgs a = prompt_args(p);
+  b.delta_groups = (p.q_rows * p.heads * 16 + kThreads - 1) / kThreads;
+  b.q_groups = prompt_groups(a.queries, b.queries, p.heads), b.k_groups = prompt_groups(a.keys, b.keys, p.kv_heads);
+  b.q_splits = type == SQUANT_W_F32 ? walk_splits(b.q_groups, p.k_rows, p.sequences, 1, b.queries.walked) : 1;
+  b.k_splits = walk_splits(b.k_groups, p.q_rows, p.sequences, a.group, b.keys.walked);
+  b.delta = ((size_t)p.q_rows * p.heads * 4 + 255) / 256 * 256;
+  b.q_partial = b.q_splits > 1 ? (size_t)b.q_splits * p.q_rows * p.heads * p.head_dim * 4 : 0;
+  b.k_partial = b.k_splits > 1 ? (size_t)b.k_splits * p.k_rows * p.kv_heads * 2 * p.head_dim * 4 : 0;
+  b.fit = (!p.q_rows || (fits(b.delta_groups) && fits(b.q_groups, b.q_splits, b.queries.threads))) && (!p.k_rows || fits(b.k_groups, b.k_splits, b.keys.threads));
+  return b;
+}
 
 }  // namespace
 
@@ -248,8 +278,10 @@ int squant_attention(const squant_heads_t* h_q, const squant_heads_t* h_k, const
   return launch(k.run, prompt_groups(a.queries, k, p.heads), 1, k.lds, (hipStream_t)stream, a, k.threads);
 }
 
-size_t squant_attention_backward_workspace_bytes(const squant_packed_t* h_packed) {
-  return check_packed(h_packed) || !h_packed->q_rows ? 0 : delta_bytes(*h_packed);
+size_t squant_attention_backward_workspace_bytes(const squant_packed_t* h_packed, squant_wtype_t type) {
+  if (check_type((int)type) || check_packed(h_packed) || !h_packed->q_rows) return 0;
+  const BackwardPlan b = plan_backward(*h_packed, (int)type, true, true);
+  return b.fit ? b.bytes() : 0;
 }
 
 int squant_attention_backward(const squant_heads_t* h_dout, const squant_heads_t* h_q, const squant_heads_t* h_k, const squant_heads_t* h_v,
@@ -269,7 +301,11 @@ int squant_attention_backward(const squant_heads_t* h_dout, const squant_heads_t
   if (p.k_rows)
     for (const squant_heads_t* h : {h_k, h_v, h_dk, h_dv})
       if (int rc = check_heads(h, p.k_rows, p.kv_heads, p.head_dim, t)) return rc;
-  const size_t need = p.q_rows ? delta_bytes(p) : 0;
+  const bool keys_direct = !p.k_rows || (whole_pieces(h_k, t) && whole_pieces(h_v, t));
+  const bool queries_direct = !p.q_rows || (whole_pieces(h_q, t) && whole_pieces(h_dout, t));
+  const BackwardPlan b = plan_backward(p, t, queries_direct, keys_direct);
+  if (!b.fit) return SQUANT_ERR_SHAPE;
+  const size_t need = p.q_rows ? b.bytes() : 0;
   if (workspace_bytes < need || (need && (!d_workspace || misaligned(d_workspace, 256)))) return SQUANT_ERR_WORKSPACE;
   PromptArgs a = prompt_args(p);
   const int64_t qr = p.q_rows, kr = p.k_rows;
@@ -277,19 +313,20 @@ int squant_attention_backward(const squant_heads_t* h_dout, const squant_heads_t
   if (kr) a.k = strided(h_k, kr), a.v = strided(h_v, kr), a.dk = strided(h_dk, kr), a.dv = strided(h_dv, kr);
   a.lse = const_cast<float*>(d_lse);
   a.delta = (float*)d_workspace;
-  const bool keys_direct = !p.k_rows || (whole_pieces(h_k, t) && whole_pieces(h_v, t));
-  const bool queries_direct = !p.q_rows || (whole_pieces(h_q, t) && whole_pieces(h_dout, t));
-  const PromptKernel kq = (t == SQUANT_W_F32 ? prompt_queries_f32 : t == SQUANT_W_F16 ? prompt_queries_f16 : prompt_queries_bf16)(p.head_dim, keys_direct);
-  const PromptKernel kk = (t == SQUANT_W_F32 ? prompt_keys_f32 : t == SQUANT_W_F16 ? prompt_keys_f16 : prompt_keys_bf16)(p.head_dim, queries_direct);
-  const int64_t delta_groups = (p.q_rows * p.heads * 16 + kThreads - 1) / kThreads;
-  const int64_t q_groups = prompt_groups(a.queries, kq, p.heads), k_groups = prompt_groups(a.keys, kk, p.kv_heads);
-  if ((p.q_rows && (!fits(delta_groups) || !fits(q_groups, 1, kq.threads))) || (p.k_rows && !fits(k_groups, 1, kk.threads))) return SQUANT_ERR_SHAPE;
+  a.partial = (float*)((char*)d_workspace + b.delta);
   hipStream_t st = (hipStream_t)stream;
-  if (p.q_rows) {
-    if (int rc = launch(prompt_delta_kernel(t), delta_groups, 1, 0, st, a)) return rc;
-    if (int rc = launch(kq.run, q_groups, 1, kq.lds, st, a, kq.threads)) return rc;
+  const auto join_groups = [&](int64_t elements) { return (elements / 4 + kThreads - 1) / kThreads; };
+  if (qr) {
+    if (int rc = launch(prompt_delta_kernel(t), b.delta_groups, 1, 0, st, a)) return rc;
+    a.splits = b.q_splits;
+    if (int rc = launch(b.queries.run, b.q_groups, b.q_splits, b.queries.lds, st, a, b.queries.threads)) return rc;
+    if (b.q_splits > 1)
+      if (int rc = launch(prompt_join_kernel(t, false), join_groups(qr * p.heads * p.head_dim), 1, 0, st, a)) return rc;
   }
-  return p.k_rows ? launch(kk.run, k_groups, 1, kk.lds, st, a, kk.threads) : SQUANT_OK;
+  if (!kr) return SQUANT_OK;
+  a.splits = qr ? b.k_splits : 1;
+  if (int rc = launch(b.keys.run, b.k_groups, a.splits, b.keys.lds, st, a, b.keys.threads)) return rc;
+  return a.splits > 1 ? launch(prompt_join_kernel(t, true), join_groups(kr * p.kv_heads * 2 * p.head_dim), 1, 0, st, a) : SQUANT_OK;
 }
 
 }  // extern "C"

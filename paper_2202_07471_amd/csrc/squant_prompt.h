@@ -29,6 +29,9 @@ struct PromptArgs {
   int32_t heads, kv_heads, group, dim;
   int32_t causal;
   float scale, scale2;    // scale2: times log2(e), never 0 (a hidden score's minus infinity stays one)
+  // a backward pass whose walks are cut into `splits` (the grid's y): their sums, [splits][rows][heads][1 or 2][dim]
+  int32_t splits;
+  float* partial;
 };
 
 template <class T, int DP> struct TileOf {
@@ -513,7 +516,9 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_backward(PromptA
     else to = min(max(min(first + kRows, rows) + shift, 0), walk_count);
   }
   const int per_head = to > from ? (to - from + BS - 1) / BS : 0;
-  const int steps = KEYS ? per_head * a.group : per_head;
+  const int all_steps = KEYS ? per_head * a.group : per_head;
+  const int begin = (int)((int64_t)all_steps * blockIdx.y / gridDim.y), steps = (int)((int64_t)all_steps * (blockIdx.y + 1) / gridDim.y);
+  int member = KEYS && begin ? begin / per_head : 0, at = from + (begin - member * per_head) * BS;
 
   const uint32_t bytes1 = (uint32_t)walk1.row * sizeof(T), bytes2 = (uint32_t)walk2.row * sizeof(T);
   const char* const from1 = (const char*)element<T>(walk1, walk0, KEYS ? head0 : kv_head);
@@ -523,7 +528,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_backward(PromptA
   l1.begin(bytes1, a.dim);
   l2.begin(bytes2, a.dim);
   float row_stat = 0.0f;
-  int next_at = from, next_member = 0;  // of the tile that is on its way
+  int next_at = at, next_member = member;  // of the tile that is on its way
   auto issue = [&](int j) {
     char* to_tile = tiles + (j & 1) * 2 * kTile;
     l1.issue(from1 + (int64_t)next_at * bytes1 + (KEYS ? (int64_t)next_member * walk1.head * (int64_t)sizeof(T) : 0), to_tile, walk_count - next_at, bytes1, a.dim);
@@ -542,9 +547,9 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_backward(PromptA
       stats[(j & 1) * 2 * BS + threadIdx.x] = (int)threadIdx.x >= BS ? row_stat : row_stat == -kInfinity ? kInfinity : row_stat * kLog2E;
     if (DIRECT) tiles_are_here();
   };
-  if (steps > 0) {
-    issue(0);
-    land(0);
+  if (steps > begin) {
+    issue(begin);
+    land(begin);
   }
   __syncthreads();
   auto step = [&](int j, int at, auto hidden) {
@@ -645,7 +650,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_backward(PromptA
     if constexpr (!kHidden && sizeof(T) == 2) interleave<TT * KS * 2, F * (TT / 2) * (KEYS ? 4 : 2), OT, KEYS ? 2 : 1>();
   };
   // Loops of their own for steps with hidden pairs and for those without: together in one, sums move between registers at each step.
-  int at = from, member = 0, j = 0;
+  int j = begin;
   auto some_hidden = [&]() {
     const bool end = at + BS > walk_count || mine + 16 * OT > own_count;
     return end || (a.causal && (KEYS ? mine + 16 * OT - 1 > at + shift : at + BS - 1 > mine + shift));
@@ -686,26 +691,58 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_backward(PromptA
         for (int i = 0; i < 4; ++i) acc1[t][f][i] -= left * (acc2[t][f][i] * kUnit);
       if (g == 0) a.delta[(int64_t)head0 * a.queries.rows + own0 + r] = own_delta[t] + left;
     }
+    if constexpr (!kMend) {
+      if (gridDim.y > 1) {
+        constexpr int kSums = KEYS ? 2 : 1;
+        float* p = a.partial + (((int64_t)blockIdx.y * own.rows + own0 + r) * heads + (KEYS ? kv_head : head0)) * kSums * a.dim + 4 * g;
+#pragma unroll
+        for (int f = 0; f < F; ++f) {
+          if (16 * f + 4 * g >= a.dim) continue;
+          *reinterpret_cast<float4v*>(p + 16 * f) = acc1[t][f];
+          if constexpr (KEYS) *reinterpret_cast<float4v*>(p + a.dim + 16 * f) = acc2[t][f] * kUnit;
+        }
+        continue;
+      }
+    }
     store_column<T, F>(KEYS ? a.dk : a.dq, own0 + r, KEYS ? kv_head : head0, a.dim, acc1[t], a.scale);
     if constexpr (KEYS) store_column<T, F>(a.dv, own0 + r, kv_head, a.dim, acc2[t], kUnit);
   }
+}
+
+// Sums of cut walks, in their order: four elements a thread.
+template <class T, bool KEYS> __global__ __launch_bounds__(kThreads) void prompt_join(PromptArgs a) {
+  constexpr int kSums = KEYS ? 2 : 1;
+  const int heads = KEYS ? a.kv_heads : a.heads, quads = a.dim / 4;
+  const int64_t all = (int64_t)(KEYS ? a.keys.rows : a.queries.rows) * heads * kSums * quads;
+  const int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (at >= all) return;
+  float4v sum = {0, 0, 0, 0};
+  for (int i = 0; i < a.splits; ++i) sum += *reinterpret_cast<const float4v*>(a.partial + (i * all + at) * 4);
+  const int64_t line = at / quads, row_head = line / kSums;
+  const int d = (int)(at - line * quads) * 4, which = (int)(line - row_head * kSums);
+  const int64_t row = row_head / heads;
+  struct Four { T v[4]; } o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o.v[i] = (T)(which ? sum[i] : sum[i] * a.scale);
+  store_any(element<T>(which ? a.dv : KEYS ? a.dk : a.dq, row, (int)(row_head - row * heads)) + d, o);
 }
 
 typedef void (*prompt_t)(PromptArgs);
 struct PromptKernel {
   prompt_t run;
   int rows;     // of a workgroup
+  int walked;   // rows of a tile
   int threads;
   size_t lds;
 };
 
 template <class T, int DP, int QT, int BK, int WAVES, int OCCUPANCY> PromptKernel forward_of(bool direct) {
   return {direct ? prompt_forward<T, DP, QT, BK, WAVES, OCCUPANCY, true> : prompt_forward<T, DP, QT, BK, WAVES, OCCUPANCY, false>, 16 * WAVES * QT,
-          64 * WAVES, (size_t)4 * BK * TileOf<T, DP>::kRowBytes + 16};
+          BK, 64 * WAVES, (size_t)4 * BK * TileOf<T, DP>::kRowBytes + 16};
 }
 template <class T, int DP, int OT, int BS, int WAVES, int OCCUPANCY, bool KEYS> PromptKernel backward_of(bool direct) {
   return {direct ? prompt_backward<T, DP, OT, BS, WAVES, OCCUPANCY, KEYS, true> : prompt_backward<T, DP, OT, BS, WAVES, OCCUPANCY, KEYS, false>,
-          16 * WAVES * OT, 64 * WAVES, (size_t)4 * BS * TileOf<T, DP>::kRowBytes + 16 * BS};
+          16 * WAVES * OT, BS, 64 * WAVES, (size_t)4 * BS * TileOf<T, DP>::kRowBytes + 16 * BS};
 }
 
 // By the head's size; `direct`: what is walked over lies at multiples of 16 bytes.
@@ -719,6 +756,7 @@ PromptKernel prompt_queries_bf16(int dim, bool direct);
 PromptKernel prompt_queries_f16(int dim, bool direct);
 PromptKernel prompt_queries_f32(int dim, bool direct);
 prompt_t prompt_delta_kernel(int type);
+prompt_t prompt_join_kernel(int type, bool keys);
 
 template <class T> PromptKernel forward_for(int dim, bool direct) {
   if constexpr (sizeof(T) == 2) {

@@ -116,7 +116,7 @@ def test_attention_over_prompts(A):
                       (FORMAT, dict(qs=P + 2)), (FORMAT, dict(ks=P + 1)), (MODE, dict(scale=-0.5)), (MODE, dict(scale=math.nan)),
                       (MODE, dict(scale=math.inf)), (MODE, dict(causal=2)), (SHAPE, dict(q_rows=1 << 30))]:
         assert f(p=packed(A, **bad)) == want and g(p=packed(A, **bad)) == want, bad
-        assert L.squant_attention_backward_workspace_bytes(ref(packed(A, **bad))) == 0
+        assert L.squant_attention_backward_workspace_bytes(ref(packed(A, **bad)), 2) == 0
     for want, bad in BAD_ROWS:
         h = heads(A, **bad)
         assert all(f(**{x: h}) == want for x in ("q", "k", "v", "out")), bad
@@ -124,8 +124,10 @@ def test_attention_over_prompts(A):
     assert f(type_=3) == FORMAT and g(type_=-1) == FORMAT and f(lse=P + 2) == FORMAT and g(lse=P + 2) == FORMAT and g(lse=None) == NULL
     assert g(ws=None) == WORKSPACE and g(nbytes=8) == WORKSPACE and g(ws=WS + 16) == WORKSPACE
     assert f(p=packed(A, q_rows=0)) == 0 and g(p=packed(A, q_rows=0, k_rows=0), ws=None, nbytes=0) == 0
-    need = L.squant_attention_backward_workspace_bytes(ref(packed(A)))
-    assert need >= 50 * 4 * 4
+    need = L.squant_attention_backward_workspace_bytes(ref(packed(A)), 2)
+    assert need >= 50 * 4 * 4 and L.squant_attention_backward_workspace_bytes(ref(packed(A)), 3) == 0
+    few, many = (L.squant_attention_backward_workspace_bytes(ref(packed(A, sequences=1, q_rows=n, k_rows=n)), 0) for n in (500, 50000))
+    assert few > 500 * 4 * 4 * 64 and many == 50000 * 4 * 4  # a short sequence's walks are cut, a long one's are not
 
 
 def test_the_binding_refuses(A):
