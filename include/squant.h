@@ -388,8 +388,10 @@ typedef struct {
 } squant_packed_t;
 
 /* out[r][h] = sum_t p[t] v[t],  lse[h][r] = log sum_t exp(scale * q[r][h] . k[t])  (binary32 [heads][q_rows]; may be NULL). */
+size_t squant_attention_workspace_bytes(const squant_packed_t* h_packed, squant_wtype_t type);
 int squant_attention(const squant_heads_t* h_q, const squant_heads_t* h_k, const squant_heads_t* h_v, squant_wtype_t type,
-                     const squant_packed_t* h_packed, const squant_heads_t* h_out, float* d_lse, void* stream);
+                     const squant_packed_t* h_packed, const squant_heads_t* h_out, float* d_lse, void* d_workspace,
+                     size_t workspace_bytes, void* stream);
 
 /* Gradients of squant_attention for the output's gradient (lse's own is not taken): with p = exp(scale * q . k - lse),
  * dv = sum p dout,  ds = p (dout . v - dout . out),  dq = scale * sum ds k,  dk = scale * sum ds q, the latter two sums

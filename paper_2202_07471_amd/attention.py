@@ -55,12 +55,14 @@ def _lib():
         L.squant_cache_read.argtypes = [cp, wp, en, i64, hp, hp, vp]
         L.squant_cache_attention_workspace_bytes.argtypes = [i64, i32, cp, wp]
         L.squant_cache_attention.argtypes = [hp, en, i64, i32, cp, wp, fl, hp, vp, sz, vp]
-        L.squant_attention.argtypes = [hp, hp, hp, en, pp, hp, vp, vp]
+        L.squant_attention_workspace_bytes.argtypes = [pp, en]
+        L.squant_attention.argtypes = [hp, hp, hp, en, pp, hp, vp, vp, sz, vp]
         L.squant_attention_backward_workspace_bytes.argtypes = [pp, en]
         L.squant_attention_backward.argtypes = [hp, hp, hp, hp, hp, vp, en, pp, hp, hp, hp, vp, sz, vp]
         for f in ("cache_write", "cache_read", "cache_attention", "attention", "attention_backward"):
             getattr(L, f"squant_{f}").restype = en
         L.squant_cache_attention_workspace_bytes.restype = sz
+        L.squant_attention_workspace_bytes.restype = sz
         L.squant_attention_backward_workspace_bytes.restype = sz
         _ready = L
     return _ready
@@ -286,7 +288,11 @@ def squant_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: 
     hv = _heads(v, k_shape, "v", device, dtype)
     out, ho = _result(out, q_shape, "out", device, dtype, q)
     lse = torch.empty((p.heads, p.q_rows), dtype=torch.float32, device=q.device)
-    _check(_lib().squant_attention(hq, hk, hv, _WTYPES[dtype], p, ho, lse.data_ptr(), _current_stream(device)))
+    L, type_ = _lib(), _WTYPES[dtype]
+    nbytes = L.squant_attention_workspace_bytes(p, type_)
+    ws = _workspace(q, nbytes)
+    _check(L.squant_attention(hq, hk, hv, type_, p, ho, lse.data_ptr(), None if ws is None else ws.data_ptr(), nbytes,
+                              _current_stream(device)))
     return out, lse
 
 

@@ -173,10 +173,36 @@ int64_t prompt_groups(const Packed& p, const PromptKernel& k, int32_t heads) {
   return tiles_bound(p.rows, 1, k.rows, p.count) * heads;
 }
 
-// A backward pass's workspace and launches.  Where there are fewer workgroups than run at once, walks are cut into pieces whose sums
-// a launch more adds up: about 512 workgroups, at least 2 tiles a piece on average, at most 8 pieces.  Queries are walked over by
-// dK and dV of all types, keys by dQ of binary32 (16-bit types have more to add up there, and are a tenth of the time).
-// Six packed sequences of up to 515 tokens, six heads of 96, binary32: SPLIT_FIGURES.
+// Where there are fewer workgroups than run at once, walks are cut into pieces whose sums a launch more adds up: about 512 workgroups, at
+// least 2 tiles a piece on average, at most 8 pieces.  Six packed sequences of up to 515 tokens, six heads of 96 on two, binary32: dK and dV
+// 199 us, 47 and a join of 5 with eight pieces; dQ 58, 29 and 4 with three.
+int walk_splits(int64_t groups, int64_t walked, int64_t sequences, int heads, int tile) {
+  const int64_t tiles = heads * (walked / std::max<int64_t>(1, sequences)) / tile;
+  return (int)std::max<int64_t>(1, std::min({(int64_t)8, 512 / std::max<int64_t>(1, groups), tiles / 2}));
+}
+
+struct ForwardPlan {
+  PromptKernel run;
+  int64_t groups;
+  int splits;
+  size_t stats, partial;
+  bool fit;
+  size_t bytes() const { return stats + partial; }
+};
+ForwardPlan plan_forward(const squant_packed_t& p, int type, bool direct) {
+  ForwardPlan f{};
+  f.run = (type == SQUANT_W_F32 ? prompt_forward_f32 : type == SQUANT_W_F16 ? prompt_forward_f16 : prompt_forward_bf16)(p.head_dim, direct);
+  f.groups = prompt_groups(prompt_args(p).queries, f.run, p.heads);
+  f.splits = walk_splits(f.groups, p.k_rows, p.sequences, 1, f.run.walked);
+  if (f.splits > 1) {
+    f.stats = ((size_t)f.splits * p.q_rows * p.heads * 8 + 255) / 256 * 256;
+    f.partial = (size_t)f.splits * p.q_rows * p.heads * p.head_dim * 4;
+  }
+  f.fit = fits(f.groups, f.splits, f.run.threads);
+  return f;
+}
+
+// Queries are walked over by dK and dV of all types, keys by dQ of binary32 (16-bit types have three sums to add up there).
 struct BackwardPlan {
   PromptKernel queries, keys;
   int64_t q_groups, k_groups, delta_groups;
@@ -185,10 +211,6 @@ struct BackwardPlan {
   bool fit;
   size_t bytes() const { return delta + std::max(q_partial, k_partial); }
 };
-int walk_splits(int64_t groups, int64_t walked, int64_t sequences, int heads, int tile) {
-  const int64_t tiles = heads * (walked / std::max<int64_t>(1, sequences)) / tile;
-  return (int)std::max<int64_t>(1, std::min({(int64_t)8, 512 / std::max<int64_t>(1, groups), tiles / 2}));
-}
 BackwardPlan plan_backward(const squant_packed_t& p, int type, bool queries_direct, bool keys_direct) {
   BackwardPlan b{};
   b.queries = (type == SQUANT_W_F32 ? prompt_queries_f32 : type == SQUANT_W_F16 ? prompt_queries_f16 : prompt_queries_bf16)(p.head_dim, keys_direct);
@@ -256,8 +278,15 @@ int squant_cache_attention(const squant_heads_t* h_q, squant_wtype_t type, int64
   return s.splits > 1 ? launch(join_splits_kernel(), (rows * heads + kWaves - 1) / kWaves, 1, 0, st, a) : SQUANT_OK;
 }
 
+size_t squant_attention_workspace_bytes(const squant_packed_t* h_packed, squant_wtype_t type) {
+  if (check_type((int)type) || check_packed(h_packed) || !h_packed->q_rows) return 0;
+  const ForwardPlan f = plan_forward(*h_packed, (int)type, true);
+  return f.fit ? f.bytes() : 0;
+}
+
 int squant_attention(const squant_heads_t* h_q, const squant_heads_t* h_k, const squant_heads_t* h_v, squant_wtype_t type,
-                     const squant_packed_t* h_packed, const squant_heads_t* h_out, float* d_lse, void* stream) {
+                     const squant_packed_t* h_packed, const squant_heads_t* h_out, float* d_lse, void* d_workspace, size_t workspace_bytes,
+                     void* stream) {
   if (int rc = check_type((int)type)) return rc;
   if (int rc = check_packed(h_packed)) return rc;
   const squant_packed_t& p = *h_packed;
@@ -269,13 +298,19 @@ int squant_attention(const squant_heads_t* h_q, const squant_heads_t* h_k, const
     if (int rc = check_heads(h_v, p.k_rows, p.kv_heads, p.head_dim, (int)type)) return rc;
   }
   if (misaligned(d_lse, 4)) return SQUANT_ERR_FORMAT;
+  const bool direct = !p.k_rows || (whole_pieces(h_k, (int)type) && whole_pieces(h_v, (int)type));
+  const ForwardPlan f = plan_forward(p, (int)type, direct);
+  if (!f.fit) return SQUANT_ERR_SHAPE;
+  if (workspace_bytes < f.bytes() || (f.bytes() && (!d_workspace || misaligned(d_workspace, 256)))) return SQUANT_ERR_WORKSPACE;
   PromptArgs a = prompt_args(p);
   a.q = strided(h_q, p.q_rows), a.o = strided(h_out, p.q_rows);
   if (p.k_rows) a.k = strided(h_k, p.k_rows), a.v = strided(h_v, p.k_rows);
   a.lse = d_lse;
-  const bool direct = !p.k_rows || (whole_pieces(h_k, (int)type) && whole_pieces(h_v, (int)type));
-  const PromptKernel k = (type == SQUANT_W_F32 ? prompt_forward_f32 : type == SQUANT_W_F16 ? prompt_forward_f16 : prompt_forward_bf16)(p.head_dim, direct);
-  return launch(k.run, prompt_groups(a.queries, k, p.heads), 1, k.lds, (hipStream_t)stream, a, k.threads);
+  a.splits = f.splits, a.stats = (float2*)d_workspace, a.partial = (float*)((char*)d_workspace + f.stats);
+  hipStream_t st = (hipStream_t)stream;
+  if (int rc = launch(f.run.run, f.groups, f.splits, f.run.lds, st, a, f.run.threads)) return rc;
+  if (f.splits == 1) return SQUANT_OK;
+  return launch(prompt_join_forward_kernel((int)type), (p.q_rows * p.heads * (p.head_dim / 4) + kThreads - 1) / kThreads, 1, 0, st, a);
 }
 
 size_t squant_attention_backward_workspace_bytes(const squant_packed_t* h_packed, squant_wtype_t type) {

@@ -29,9 +29,11 @@ struct PromptArgs {
   int32_t heads, kv_heads, group, dim;
   int32_t causal;
   float scale, scale2;    // scale2: times log2(e), never 0 (a hidden score's minus infinity stays one)
-  // a backward pass whose walks are cut into `splits` (the grid's y): their sums, [splits][rows][heads][1 or 2][dim]
+  // walks that are cut into `splits` (the grid's y): their sums, [splits][rows][heads][1 or 2][dim], and, forward, the rows' largest
+  // scores (base 2) and sums of weights, [splits][rows][heads]
   int32_t splits;
   float* partial;
+  float2* stats;
 };
 
 template <class T, int DP> struct TileOf {
@@ -263,8 +265,9 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
   }
   const int wave_most = mine < rows ? sees(min(mine + 16 * QT, rows) - 1) : 0;
   const int most = sees(min(first + kRows, rows) - 1);
-  const int steps = (most + BK - 1) / BK;
-  const int whole = first + kRows <= rows ? sees(first) / BK : 0;  // steps of which all rows see all keys
+  const int all_steps = (most + BK - 1) / BK;
+  const int begin = (int)((int64_t)all_steps * blockIdx.y / gridDim.y), steps = (int)((int64_t)all_steps * (blockIdx.y + 1) / gridDim.y);
+  const int whole = min(first + kRows <= rows ? sees(first) / BK : 0, steps);  // steps of which all rows see all keys
 
   float4v o[QT][F];
   float largest[QT], sum[QT];
@@ -292,9 +295,9 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
     lv.land(at + kTile);
     if (DIRECT) tiles_are_here();
   };
-  if (steps > 0) {
-    issue(0);
-    land(0);
+  if (steps > begin) {
+    issue(begin);
+    land(begin);
   }
   __syncthreads();
 
@@ -393,7 +396,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
           }
     }
   };
-  int j = 0;
+  int j = begin;
 #pragma unroll 1
   for (; j < whole; ++j) {
     if (j + 1 < steps) issue(j + 1);
@@ -413,6 +416,15 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
     const int r = mine + 16 * t + n;
     const float total = over_groups_sum(sum[t]);
     if (r >= rows) continue;
+    if (gridDim.y > 1) {
+      const int64_t at = ((int64_t)blockIdx.y * a.queries.rows + q0 + r) * a.heads + head;
+      if (g == 0) a.stats[at] = make_float2(largest[t], total);
+      float* p = a.partial + at * a.dim + 4 * g;
+#pragma unroll
+      for (int f = 0; f < F; ++f)
+        if (16 * f + 4 * g < a.dim) *reinterpret_cast<float4v*>(p + 16 * f) = o[t][f];
+      continue;
+    }
     store_column<T, F>(a.o, q0 + r, head, a.dim, o[t], total == 0.0f ? 0.0f : 1.0f / total);
     if (a.lse && g == 0)
       a.lse[(int64_t)head * a.queries.rows + q0 + r] =
@@ -709,6 +721,34 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_backward(PromptA
   }
 }
 
+// Outputs of cut walks, in their order: four elements a thread.
+template <class T> __global__ __launch_bounds__(kThreads) void prompt_join_forward(PromptArgs a) {
+  const int quads = a.dim / 4;
+  const int64_t rows = (int64_t)a.queries.rows * a.heads, at = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (at >= rows * quads) return;
+  const int64_t line = at / quads, row = line / a.heads;
+  const int d = (int)(at - line * quads) * 4, head = (int)(line - row * a.heads);
+  float most = -kInfinity;
+  for (int i = 0; i < a.splits; ++i) most = fmaxf(most, a.stats[i * rows + line].x);
+  const float base = most == -kInfinity ? 0.0f : most;
+  float total = 0.0f;
+  float4v sum = {0, 0, 0, 0};
+  for (int i = 0; i < a.splits; ++i) {
+    const float2 st = a.stats[i * rows + line];
+    const float w = exp2_fast(st.x - base);
+    total += st.y * w;
+    sum += *reinterpret_cast<const float4v*>(a.partial + (i * rows + line) * a.dim + d) * w;
+  }
+  const float by = total == 0.0f ? 0.0f : 1.0f / total;
+  struct Four { T v[4]; } o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o.v[i] = (T)(sum[i] * by);
+  store_any(element<T>(a.o, row, head) + d, o);
+  if (a.lse && d == 0)
+    a.lse[(int64_t)head * a.queries.rows + row] =
+        total == 0.0f ? -kInfinity : (most - weight_unit<T>() + __builtin_amdgcn_logf(total)) * kLn2;
+}
+
 // Sums of cut walks, in their order: four elements a thread.
 template <class T, bool KEYS> __global__ __launch_bounds__(kThreads) void prompt_join(PromptArgs a) {
   constexpr int kSums = KEYS ? 2 : 1;
@@ -757,6 +797,7 @@ PromptKernel prompt_queries_f16(int dim, bool direct);
 PromptKernel prompt_queries_f32(int dim, bool direct);
 prompt_t prompt_delta_kernel(int type);
 prompt_t prompt_join_kernel(int type, bool keys);
+prompt_t prompt_join_forward_kernel(int type);
 
 template <class T> PromptKernel forward_for(int dim, bool direct) {
   if constexpr (sizeof(T) == 2) {

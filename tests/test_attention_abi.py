@@ -103,9 +103,9 @@ def test_attention_over_a_cache(A):
 def test_attention_over_prompts(A):
     L = A._lib()
 
-    def f(q=None, k=None, v=None, type_=2, p=None, out=None, lse=P):
+    def f(q=None, k=None, v=None, type_=2, p=None, out=None, lse=P, ws=WS, nbytes=BIG):
         return L.squant_attention(ref(q or heads(A)), ref(k or heads(A)), ref(v or heads(A)), type_, ref(p or packed(A)), ref(out or heads(A)),
-                                  lse, None)
+                                  lse, ws, nbytes, None)
 
     def g(d=None, q=None, k=None, v=None, out=None, lse=P, type_=2, p=None, dq=None, dk=None, dv=None, ws=WS, nbytes=BIG):
         return L.squant_attention_backward(*(ref(t or heads(A)) for t in (d, q, k, v, out)), lse, type_, ref(p or packed(A)),
@@ -124,6 +124,9 @@ def test_attention_over_prompts(A):
     assert f(type_=3) == FORMAT and g(type_=-1) == FORMAT and f(lse=P + 2) == FORMAT and g(lse=P + 2) == FORMAT and g(lse=None) == NULL
     assert g(ws=None) == WORKSPACE and g(nbytes=8) == WORKSPACE and g(ws=WS + 16) == WORKSPACE
     assert f(p=packed(A, q_rows=0)) == 0 and g(p=packed(A, q_rows=0, k_rows=0), ws=None, nbytes=0) == 0
+    alone = packed(A, sequences=1, q_rows=50, k_rows=2000)  # few rows and many keys are cut
+    assert f(p=alone, ws=None) == WORKSPACE and f(p=alone, nbytes=100) == WORKSPACE and f(p=alone, ws=WS + 8) == WORKSPACE
+    assert L.squant_attention_workspace_bytes(ref(alone), 2) > 2 * 50 * 4 * 64 * 4 and L.squant_attention_workspace_bytes(ref(alone), 7) == 0
     need = L.squant_attention_backward_workspace_bytes(ref(packed(A)), 2)
     assert need >= 50 * 4 * 4 and L.squant_attention_backward_workspace_bytes(ref(packed(A)), 3) == 0
     few, many = (L.squant_attention_backward_workspace_bytes(ref(packed(A, sequences=1, q_rows=n, k_rows=n)), 0) for n in (500, 50000))

@@ -72,6 +72,15 @@ def test_long(sq, dtype):
 
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
 @pytest.mark.parametrize("causal", [True, False])
+def test_few_rows_and_many_keys(sq, dtype, causal):
+    """Walks that are cut: pieces that no row of a tile sees, rows that see nothing in some pieces."""
+    check(sq, 18, [40], [2000], 2, 1, 64, dtype, causal)
+    check(sq, 19, [5, 0, 130], [900, 1300, 60], 3, 1, 72, dtype, causal, q_pad=2, k_pad=1)
+    check(sq, 20, [900], [20], 2, 2, 64, dtype, causal)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("causal", [True, False])
 def test_rows_that_see_nothing(sq, dtype, causal):
     """More queries than keys (causal: the first rows see none), a sequence without keys, one without queries, padding rows."""
     check(sq, 4, [40, 9, 0, 5], [17, 0, 12, 5], 4, 2, 64, dtype, causal, q_pad=7, k_pad=70)
