@@ -120,20 +120,21 @@ __device__ __forceinline__ uint32_t finite_bits(float v) {
 // bfloat16 bits of 512 / 2^e: scales from there on are too large for e, or no numbers.
 __device__ __forceinline__ uint32_t too_large(int e) { return min((uint32_t)(9 - e + 127) << 7, 0x7f80u); }
 
-#ifndef CO
-#define CO 2
-#define CP 3
-#endif
-// Waves a SIMD that registers are kept for.
-constexpr int cache_occupancy(int ng, int rt) { return ng <= 2 && rt == 1 ? CP : CO; }
+// Waves a SIMD that registers are kept for.  Three are what most take; asked for more, heads of 128 spill (96 sequences 171 us, 211), and so do
+// 32 rows at three (eleven sequences' drafts 36 us, 61).
+constexpr int cache_occupancy(int ng, int rt) { return ng <= 2 && rt == 1 ? 3 : 2; }
 
 // HALVES: pages of a multiple of 16 tokens, of which each half of a block has consecutive rows: their addresses are a number for the
 // wave plus one of the lane that stays.
 //
 // One body for all blocks, with branches of the wave around what only some need: a call of a short sequence spends its time
 // on fetching instructions for the first time (with a body of its own for blocks that hide tokens and two blocks a turn
-// one token of 8192 took 12 us in this kernel, whether it multiplied or only read).  For the same reason the next block's keys are
-// read behind this one's scores, and its values behind this one's products, into the registers that have become free.
+// one token of 8192 took 12 us in this kernel, whether it multiplied or only read).  The next block's keys are on their way from
+// a block's beginning on, its values from the end of the products, into the registers that have become free there.
+//
+// What bounds it: 96 sequences of 1024 to 16384 tokens, 32 heads of 128 on 8, 4 bits: 165 us, 3.4 TB/s of codes and scales; reading them
+// without the products takes 125, and vector instructions (1.7 a code: place, centre, scale) issue for about half of the time.
+// One token of 8192: 12 us, of which reading alone takes nearly all: a chain of lengths, table, codes, and two joins.
 template <class T, int FMT, int NG, int RT, bool HALVES>
 __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_attention(CacheAttentionArgs a) {
   typedef Layout<FMT, NG> L;
@@ -272,7 +273,9 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
   uint32_t key[2][L::kKeyWords], value[8][L::kValueWords];
   uint16_t key_scale[2][L::kKeyScales], value_scale[8][L::kValueScales];
   // key token 16 tt + n, value token 4 g + j (j < 4), 16 + 4 g + j - 4
-  auto load_keys = [&](const Where& w) {
+  uint32_t next_key[2][L::kKeyWords];
+  uint16_t next_key_scale[2][L::kKeyScales];
+  auto load_keys = [&](const Where& w, uint32_t (&key)[2][L::kKeyWords], uint16_t (&key_scale)[2][L::kKeyScales]) {
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
       struct Words { uint32_t w[L::kKeyWords]; };
@@ -326,12 +329,19 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
   Where at, next;
   if (t0 < end) {
     find(at, t0, ids);
-    load_keys(at);
+    load_keys(at, key, key_scale);
     load_values(at);
     page_ids(t0 + kStep, ids);
   }
 #pragma unroll 1
   for (; t0 < end; t0 += kStep) {
+    const bool more = t0 + kStep < end;
+    if (more) {
+      find(next, t0 + kStep, ids);
+      load_keys(next, next_key, next_key_scale);
+      page_ids(t0 + 2 * kStep, ids);
+    }
+
     const bool some_hidden = t0 + kTokens > least_seen;  // of the block's tokens, for some row
     uint32_t nan_tokens = at.bad;                         // rows that see one of them are NaN
 
@@ -384,13 +394,6 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
         }
       }
     }
-    const bool more = t0 + kStep < end;
-    if (more) {
-      find(next, t0 + kStep, ids);
-      load_keys(next);
-      page_ids(t0 + 2 * kStep, ids);
-    }
-
     // the values' scales: 0 for tokens past the end, whatever is there, and for those that make rows NaN
     top = 0;
 #pragma unroll
@@ -504,6 +507,13 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
     if (more) {
       load_values(next);
       at = next;
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+#pragma unroll
+        for (int i = 0; i < L::kKeyWords; ++i) key[tt][i] = next_key[tt][i];
+#pragma unroll
+        for (int k = 0; k < L::kKeyScales; ++k) key_scale[tt][k] = next_key_scale[tt][k];
+      }
     }
   }
 
