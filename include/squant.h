@@ -319,7 +319,8 @@ int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t t
  *
  * Query heads share key heads in groups: heads is a multiple of the key heads, query head h goes with key head
  * h / (heads / key heads).  No atomics: results are the same from run to run.  The calls launch kernels only and may be
- * captured into a HIP graph.  rows = 0 is a no-op unless said otherwise.  Workspaces as for the calls above. */
+ * captured into a HIP graph.  rows = 0 is a no-op unless said otherwise.  Workspaces as for the calls above.  Results overlap
+ * neither each other nor what is read, but attention's output may be its queries' own buffer (the same steps). */
 
 /* [rows][heads][head_dim] elements; a head's elements lie beside each other. */
 typedef struct {

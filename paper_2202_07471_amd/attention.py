@@ -165,6 +165,44 @@ def _result(t: Optional[torch.Tensor], shape, what: str, device: int, dtype, lik
     return t, h
 
 
+def _extent(h: squant_heads_t, shape, size: int):
+    rows, heads, dim = shape
+    return h.data or 0, (h.data or 0) + ((rows - 1) * h.row + (heads - 1) * h.head + dim) * size if rows and heads else 0
+
+
+def _disjoint(a: squant_heads_t, a_shape, b: squant_heads_t, b_shape, size: int) -> bool:
+    """Whether no byte belongs to both: one ends before the other begins, or both repeat with one step (of rows, or of heads) and
+    lie side by side within it, as slices of a buffer do."""
+    (a0, a1), (b0, b1) = _extent(a, a_shape, size), _extent(b, b_shape, size)
+    if a1 <= b0 or b1 <= a0:
+        return True
+    for step_a, step_b, inner_a, inner_b, dim in ((a.row, b.row, a.head, b.head, 1), (a.head, b.head, a.row, b.row, 0)):
+        if step_a == step_b and step_a > 0:
+            shift = (b0 - a0) % (step_a * size)
+            if (((a_shape[dim] - 1) * inner_a + a_shape[2]) * size <= shift
+                    and shift + ((b_shape[dim] - 1) * inner_b + b_shape[2]) * size <= step_a * size):
+                return True
+    return False
+
+
+def _apart(result: squant_heads_t, shape, what: str, size: int, others) -> None:
+    """Refuses a result over what is read, or over another result: (name, tensor's heads, shape) each."""
+    for name, h, other in others:
+        if not _disjoint(result, shape, h, other, size):
+            raise ValueError(f"{what} overlaps {name}")
+
+
+def _same(a: squant_heads_t, b: squant_heads_t) -> bool:
+    return (a.data, a.row, a.head) == (b.data, b.row, b.head)
+
+
+def _apart_from_cache(result: squant_heads_t, shape, what: str, size: int, cache: QuantizedCache) -> None:
+    first, last = _extent(result, shape, size)
+    for t in cache:
+        if first < t.data_ptr() + t.numel() * t.element_size() and t.data_ptr() < last:
+            raise ValueError(f"{what} overlaps the cache")
+
+
 def _shape3(t: torch.Tensor, what: str):
     shape = t.shape
     if len(shape) != 3:
@@ -207,8 +245,14 @@ def squant_cache_read(cache: QuantizedCache, table: torch.Tensor, lengths: torch
     if rows < 0:
         raise ValueError("rows must not be negative")
     shape = (rows, c.heads, c.head_dim)
+    given = (k is not None, v is not None)
     k, hk = _result(k, shape, "k", device, dtype, cache.key_scales)
     v, hv = _result(v, shape, "v", device, dtype, cache.key_scales)
+    if all(given):
+        _apart(hk, shape, "k", dtype.itemsize, (("v", hv, shape),))
+    for there, h, what in zip(given, (hk, hv), "kv"):
+        if there:
+            _apart_from_cache(h, shape, what, dtype.itemsize, cache)
     w = _paged(table, lengths, starts, rows, device)
     _check(_lib().squant_cache_read(c, w, _WTYPES[dtype], rows, hk, hv, _current_stream(device)))
     return k, v
@@ -221,7 +265,8 @@ def squant_cache_attention(q: torch.Tensor, cache: QuantizedCache, table: torch.
     rows are placed as in squant_cache_write, and each sees the tokens up to its own.
 
     heads is a multiple of the cache's; scale defaults to head_dim ** -0.5.  For one or a few new tokens of each sequence; a whole
-    prompt is squant_attention's.  Rows that see nothing are 0, rows behind the last sequence too.  `out` may be q."""
+    prompt is squant_attention's.  Rows that see nothing are 0, rows behind the last sequence too.  `out` may be q, but
+    overlaps it in no other way."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return squant_cache_attention(q, cache, table, lengths, starts, scale, out)
@@ -234,7 +279,12 @@ def squant_cache_attention(q: torch.Tensor, cache: QuantizedCache, table: torch.
     shape, dtype = (rows, heads, dim), q.dtype
     hq = _heads(q, shape, "q", device, dtype)
     w = _paged(table, lengths, starts, rows, device)
+    given = out is not None
     out, ho = _result(out, shape, "out", device, dtype, q)
+    if given:
+        if not _same(ho, hq):
+            _apart(ho, shape, "out", dtype.itemsize, (("q", hq, shape),))
+        _apart_from_cache(ho, shape, "out", dtype.itemsize, cache)
     L = _lib()
     nbytes = L.squant_cache_attention_workspace_bytes(rows, heads, c, w)
     ws = _workspace(q, nbytes)
@@ -275,7 +325,7 @@ def squant_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: 
     Query head h goes with key head h // (heads / kv_heads).  starts are the sequences' first rows of q (and of k, unless
     k_starts says otherwise), None: one sequence.  causal: a sequence's last row sees all of its keys, the row before it one
     less, and so on.  lse [heads, q_rows] is the float32 log-sum-exp of each row's scores.  Rows that see no key are 0.
-    `out` may be q."""
+    `out` may be q, but overlaps no input otherwise."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return squant_attention(q, k, v, starts, k_starts, scale, causal, out)
@@ -286,7 +336,10 @@ def squant_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: 
     hq = _heads(q, q_shape, "q", device, dtype)
     hk = _heads(k, k_shape, "k", device, dtype)
     hv = _heads(v, k_shape, "v", device, dtype)
+    given = out is not None
     out, ho = _result(out, q_shape, "out", device, dtype, q)
+    if given:
+        _apart(ho, q_shape, "out", dtype.itemsize, (() if _same(ho, hq) else (("q", hq, q_shape),)) + (("k", hk, k_shape), ("v", hv, k_shape)))
     lse = torch.empty((p.heads, p.q_rows), dtype=torch.float32, device=q.device)
     L, type_ = _lib(), _WTYPES[dtype]
     nbytes = L.squant_attention_workspace_bytes(p, type_)
@@ -301,7 +354,8 @@ def squant_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tens
                               scale: Optional[float] = None, causal: bool = True, dq: Optional[torch.Tensor] = None,
                               dk: Optional[torch.Tensor] = None, dv: Optional[torch.Tensor] = None,
                               stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
-    """(dq, dk, dv) of squant_attention for the gradient dout of its output; out and lse are what it returned."""
+    """(dq, dk, dv) of squant_attention for the gradient dout of its output; out and lse are what it returned.  dq, dk and dv
+    overlap neither each other nor what is read; slices of one buffer are fine."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return squant_attention_backward(dout, q, k, v, out, lse, starts, k_starts, scale, causal, dq, dk, dv)
@@ -316,9 +370,20 @@ def squant_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tens
     hd = _heads(dout, q_shape, "dout", device, dtype)
     if lse.dtype is not torch.float32 or lse.shape != (p.heads, p.q_rows) or not lse.is_contiguous() or lse.get_device() != device:
         raise ValueError("lse must be what squant_attention returned for these rows")
+    given = [(what, q_shape if what == "dq" else k_shape) for what, t in (("dq", dq), ("dk", dk), ("dv", dv)) if t is not None]
     dq, gq = _result(dq, q_shape, "dq", device, dtype, q)
     dk, gk = _result(dk, k_shape, "dk", device, dtype, q)
     dv, gv = _result(dv, k_shape, "dv", device, dtype, q)
+    if given:
+        results = {"dq": gq, "dk": gk, "dv": gv}
+        read = [("dout", hd, q_shape), ("q", hq, q_shape), ("k", hk, k_shape), ("v", hv, k_shape), ("out", ho, q_shape)]
+        first, last = lse.data_ptr(), lse.data_ptr() + 4 * lse.numel()
+        for what, shape in given:
+            _apart(results[what], shape, what, dtype.itemsize, read)
+            begin, end = _extent(results[what], shape, dtype.itemsize)
+            if begin < last and first < end:
+                raise ValueError(f"{what} overlaps lse")
+            read.append((what, results[what], shape))
     L = _lib()
     nbytes = L.squant_attention_backward_workspace_bytes(p, _WTYPES[dtype])
     ws = _workspace(q, nbytes)
@@ -353,6 +418,24 @@ class _Attention(torch.autograd.Function):
         return dq if need[0] else None, dk if need[1] else None, dv if need[2] else None, None, None, None, None
 
 
+def _leaves(*tensors):
+    """The nodes that add to the gradients of those which are leaves.  Autograd keeps one for a leaf while any graph uses it, on the
+    stream of its first use: a backward pass that is captured while an eager graph holds that node waits on a stream outside
+    the capture, which ends the process.  Nodes that an eager call here uses are marked; a captured call refuses them."""
+    nodes = [torch.autograd.graph.get_gradient_edge(t).node for t in tensors if t.requires_grad and t.is_leaf]
+    if nodes and torch.cuda.is_current_stream_capturing():
+        if any("squant_eager" in node.metadata for node in nodes):
+            raise RuntimeError("a graph of these leaves that was built outside the capture is still alive: release its outputs first")
+    else:
+        for node in nodes:
+            node.metadata["squant_eager"] = True
+    return nodes
+
+
 def packed_attention(q, k, v, starts=None, k_starts=None, scale: Optional[float] = None, causal: bool = True) -> torch.Tensor:
-    """squant_attention's output with gradients for q, k and v."""
+    """squant_attention's output with gradients for q, k and v.
+
+    For a captured step, forward and backward are captured together, and no graph of the same leaves from outside the capture
+    may be alive then: where q, k or v themselves are such leaves of an earlier call, this is refused."""
+    nodes = _leaves(q, k, v) if torch.is_grad_enabled() else None  # alive until the graph holds them
     return _Attention.apply(q, k, v, starts, k_starts, scale, causal)

@@ -149,3 +149,28 @@ def test_the_binding_refuses(A):
         sq.squant_cache_read(c, ints, ints[:, 0], None, 4, torch.float32)
     with pytest.raises(ValueError):
         sq.squant_cache_attention(q, c, ints, ints[:, 0])
+
+
+def test_disjoint(A):
+    """Never calls two places apart that share an element; knows slices of rows and of heads to be."""
+    import random
+    rng = random.Random(1)
+
+    def place(h, shape):
+        return {h.data // 2 + r * h.row + i * h.head + e for r in range(shape[0]) for i in range(shape[1]) for e in range(shape[2])}
+    apart = 0
+    for _ in range(4000):
+        shapes = [(rng.randint(0, 4), rng.randint(0, 4), 4) for _ in range(2)]
+        steps = [(rng.choice((4, 8, 12, 16, 20)), rng.choice((4, 8, 12, 16, 20))) for _ in range(2)]
+        if rng.random() < 0.5:
+            steps[1] = steps[0]
+        hs = [A.squant_heads_t(64 + 2 * rng.randint(0, 40), *s) for s in steps]
+        if A._disjoint(hs[0], shapes[0], hs[1], shapes[1], 2):
+            assert not place(hs[0], shapes[0]) & place(hs[1], shapes[1])
+            apart += 1
+    assert apart > 1000
+    fused = [A.squant_heads_t(64 + 2 * 4 * i, 32, 4) for i in (0, 4, 6)]
+    shapes = [(9, 4, 4), (9, 2, 4), (9, 2, 4)]
+    for i in range(3):
+        for j in range(3):
+            assert A._disjoint(fused[i], shapes[i], fused[j], shapes[j], 2) == (i != j)

@@ -280,3 +280,119 @@ def test_refusals(sq):
     for f in bad:
         with pytest.raises(ValueError):
             f()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("sequences", [63, 64, 200])
+def test_many_sequences(sq, sequences, dtype):
+    counts = [(7 * i) % 23 for i in range(sequences)]
+    keys = [(5 * i) % 19 + (90 if i % 50 == 49 else 0) for i in range(sequences)]
+    check(sq, 30, counts, keys, 2, 1, 32, dtype, True, q_pad=3, k_pad=2)
+
+
+def test_output_over_the_queries(sq):
+    for rows, keys in ((150, 150), (20, 2000)):  # the second is cut
+        q, k, v, _ = (t.cuda() for t in inputs(31, rows, keys, 4, 2, 64, BF16))
+        want, lse = sq.squant_attention(q, k, v)
+        got, lse2 = sq.squant_attention(q, k, v, out=q)
+        assert got is q and torch.equal(q, want) and torch.equal(lse, lse2)
+
+
+def test_overlaps(sq):
+    """Results beside what is read, in one buffer, are taken; over it they are refused."""
+    rows, dim = 40, 32
+    gen = torch.Generator().manual_seed(32)
+    fused = torch.randn(rows, 4 + 2 + 2, dim, generator=gen).to(BF16).cuda()
+    both_ = torch.cat((fused, torch.zeros(rows, 12, dim, dtype=BF16, device="cuda")), 1)
+    q, k, v = both_[:, :4], both_[:, 4:6], both_[:, 6:8]
+    out, lse = sq.squant_attention(q, k, v, out=both_[:, 8:12])
+    want, _ = sq.squant_attention(q.clone(), k.clone(), v.clone())
+    assert torch.equal(out, want)
+    dout = torch.randn(rows, 4, dim, generator=gen).to(BF16).cuda()
+    grads = torch.empty(rows, 8, dim, dtype=BF16, device="cuda")
+    dq, dk, dv = grads[:, :4], grads[:, 4:6], grads[:, 6:]
+    got = sq.squant_attention_backward(dout, q, k, v, out, lse, dq=dq, dk=dk, dv=dv)
+    fresh = sq.squant_attention_backward(dout, q, k, v, out, lse)
+    assert all(torch.equal(a, b) for a, b in zip(got, fresh))
+    heads_first = torch.empty(8, rows, dim, dtype=BF16, device="cuda").transpose(0, 1)
+    got = sq.squant_attention_backward(dout, q, k, v, out, lse, dq=heads_first[:, :4], dk=heads_first[:, 4:6], dv=heads_first[:, 6:])
+    assert all(torch.equal(a, b) for a, b in zip(got, fresh))
+    before = both_.clone()
+    over_lse = lse.view(torch.uint8).flatten().view(BF16)[:rows * 2 * dim].unflatten(0, (-1, 2, dim))
+    bad = [lambda: sq.squant_attention(q, k, v, out=both_[:, 1:5]), lambda: sq.squant_attention(q, k, v, out=both_[:, 5:9]),
+           lambda: sq.squant_attention(q[:20], k, v, k_starts=None, out=both_[10:30, :4]),
+           lambda: sq.squant_attention(q, k, v, out=both_.flatten()[16:16 + rows * 4 * dim].unflatten(0, (rows, 4, dim))),
+           lambda: sq.squant_attention_backward(dout, q, k, v, out, lse, dq=q), lambda: sq.squant_attention_backward(dout, q, k, v, out, lse, dq=dout),
+           lambda: sq.squant_attention_backward(dout, q, k, v, out, lse, dq=out), lambda: sq.squant_attention_backward(dout, q, k, v, out, lse, dk=v),
+           lambda: sq.squant_attention_backward(dout, q, k, v, out, lse, dk=dk, dv=dk),
+           lambda: sq.squant_attention_backward(dout, q, k, v, out, lse, dq=dq, dv=grads[:, 3:5]),
+           lambda: sq.squant_attention_backward(dout, q[:, :, :], k[:5], v[:5], out, lse, k_starts=None, starts=None, dk=over_lse[:5])]
+    for f in bad:
+        with pytest.raises(ValueError):
+            f()
+    assert torch.equal(both_, before)
+
+
+def test_two_streams_at_once(sq):
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    work = [tuple(t.cuda() for t in inputs(33 + i, 600, 600, 6, 2, 96, F32)) for i in range(2)]
+    want = [both(sq, *w, None, None, None, True) for w in work]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(4):
+        for i, (q, k, v, dout) in enumerate(work):
+            out, lse = sq.squant_attention(q, k, v, stream=sides[i])
+            got[i].append((out, lse) + sq.squant_attention_backward(dout, q, k, v, out, lse, stream=sides[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for g in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(g, want[i]))
+
+
+def test_broken_starts(sq):
+    """Starts that fall, are negative or beyond the rows: what is computed is anything, in the buffers given."""
+    rows, dim = 300, 64
+    q, k, v, dout = (t.cuda() for t in inputs(35, rows, rows, 2, 1, dim, BF16))
+    for broken in ([0, 200, 100, 300], [5, 5, -7, 90], [0, 10 ** 9, 20, 2 ** 31 - 1], [300, 200, 100, 0]):
+        starts = torch.tensor(broken, dtype=torch.int32).cuda()
+        bufs = [torch.full((rows + 2, h, dim), 7.0, dtype=BF16, device="cuda") for h in (2, 2, 1, 1)]
+        out, dq, dk, dv = (b[1:-1] for b in bufs)
+        lse = sq.squant_attention(q, k, v, starts, out=out)[1]
+        sq.squant_attention_backward(dout, q, k, v, out, lse, starts, dq=dq, dk=dk, dv=dv)
+        assert all((b[0] == 7).all() and (b[-1] == 7).all() for b in bufs)
+
+
+def test_autograd_in_a_graph(sq):
+    """A captured training step; while an eager graph of the same leaves lives, the capture's call is refused."""
+    q, k, v, dout = (t.cuda() for t in inputs(36, 130, 130, 4, 2, 64, BF16))
+    starts = starts_of([100, 30]).cuda()
+    leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+    eager = sq.packed_attention(*leaves, starts)
+    graph = torch.cuda.CUDAGraph()
+    scratch = torch.ones(4, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        scratch.mul_(2.0)
+        with pytest.raises(RuntimeError):
+            sq.packed_attention(*leaves, starts)
+    del eager
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.autograd.grad(sq.packed_attention(*leaves, starts), leaves, dout)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = sq.packed_attention(*leaves, starts)
+        grads = torch.autograd.grad(out, leaves, dout)
+    held = out.detach()
+    del out
+    for counts in ([100, 30], [1, 129], [60, 20]):
+        starts.copy_(starts_of(counts))
+        torch.cuda.synchronize()
+        graph.replay()
+        want, lse = sq.squant_attention(q, k, v, starts)
+        want = (want,) + sq.squant_attention_backward(dout, q, k, v, want, lse, starts)
+        for a, b in zip((held,) + grads, want):
+            assert torch.equal(a, b)

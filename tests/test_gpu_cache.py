@@ -393,3 +393,82 @@ def test_refusals(sq):
             f()
     with pytest.raises(sq.SQuantError):
         sq.squant_cache_attention(q, cache, table, lens, scale=-1.0)
+
+
+@pytest.mark.parametrize("one_each", [True, False])
+def test_many_sequences(sq, one_each):
+    for sequences in (63, 64, 65, 300):
+        lengths = [(11 * i) % 40 + 1 for i in range(sequences)]
+        new = [1 if one_each else min((3 * i) % 4, lengths[i]) for i in range(sequences)]
+        attend(sq, sequences, lengths, new, 4, 2, 32, 16, BF16, 4, one_each=one_each, pad=0 if one_each else 2)
+
+
+@pytest.mark.parametrize("sequences", [255, 256, 700])
+def test_rows_of_many_sequences(sq, sequences):
+    gen = torch.Generator().manual_seed(sequences)
+    lengths = [(5 * i) % 17 for i in range(sequences)]
+    new = [min((3 * i) % 5, lengths[i]) for i in range(sequences)]
+    pages, table = layout(gen, lengths, 8)
+    cache = sq.QuantizedCache.empty(pages, 2, 8, 64, sq.OUT_INT8)
+    k, v = (torch.randn(sum(new) + 4, 2, 64, generator=gen).to(F16) for _ in range(2))
+    args = (table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), starts_of(new).cuda())
+    sq.squant_cache_write(k.cuda(), v.cuda(), cache, *args)
+    for got, x in zip(sq.squant_cache_read(cache, *args, sum(new) + 4, F32), (k, v)):
+        want = values(*quantise(x, 8)).float()
+        want[sum(new):] = 0
+        assert torch.equal(got.cpu(), want)
+    r = 0
+    for b, (n, m) in enumerate(zip(new, lengths)):  # and in the slots that they belong to
+        p, s = slots_of(table, 8, b, m - n, m)
+        codes, scales = quantise(v[r:r + n], 8)
+        assert torch.equal(cache.value_codes.cpu()[p, :, s], codes)
+        r += n
+
+
+def test_broken_starts(sq):
+    """Starts that fall, are negative or beyond the rows: what is computed is anything, in the buffers given."""
+    q, cache, host, table, lens, out = attend(sq, 61, [600, 90, 40], [9, 2, 1], 4, 2, 64, 16, BF16, 4)
+    rows = q.shape[0]
+    for broken in ([0, 9, 3, 12], [4, -7, 90, 2], [0, 10 ** 9, 20, 2 ** 31 - 1], [12, 8, 4, 0]):
+        starts = torch.tensor(broken, dtype=torch.int32).cuda()
+        bufs = [torch.full((rows + 2, h, 64), 7.0, dtype=BF16, device="cuda") for h in (4, 2, 2)]
+        sq.squant_cache_attention(q.cuda(), cache, table.cuda(), lens.cuda(), starts, out=bufs[0][1:-1])
+        sq.squant_cache_read(cache, table.cuda(), lens.cuda(), starts, rows, BF16, k=bufs[1][1:-1], v=bufs[2][1:-1])
+        assert all((b[0] == 7).all() and (b[-1] == 7).all() for b in bufs)
+
+
+def test_overlaps(sq):
+    q, cache, host, table, lens, out = attend(sq, 62, [40, 700], [1, 1], 4, 2, 64, 16, BF16, 8, one_each=True)
+    qg, args = q.cuda(), (table.cuda(), lens.cuda())
+    got = sq.squant_cache_attention(qg, cache, *args, out=qg)
+    assert got is qg and torch.equal(qg, out)
+    pair = torch.empty(2, 4, 64, dtype=BF16, device="cuda")
+    k, v = sq.squant_cache_read(cache, *args, None, 2, BF16, k=pair[:, :2], v=pair[:, 2:])
+    for a, b in zip((k, v), sq.squant_cache_read(cache, *args, None, 2, BF16)):
+        assert torch.equal(a, b)
+    inside = cache.key_codes.view(torch.uint8).flatten()[:2 * 4 * 64 * 2].view(BF16).view(2, 4, 64)
+    wide = torch.zeros(3, 4, 64, dtype=BF16, device="cuda")
+    before = [t.clone() for t in cache]
+    bad = [lambda: sq.squant_cache_attention(wide[:2], cache, *args, out=wide[1:]), lambda: sq.squant_cache_attention(qg, cache, *args, out=inside),
+           lambda: sq.squant_cache_read(cache, *args, None, 2, BF16, k=pair[:, :2], v=pair[:, 1:3]),
+           lambda: sq.squant_cache_read(cache, *args, None, 2, BF16, v=inside[:, :2])]
+    for f in bad:
+        with pytest.raises(ValueError):
+            f()
+    assert all(torch.equal(a.view(torch.int8), b.view(torch.int8)) for a, b in zip(cache, before))
+
+
+def test_two_streams_at_once(sq):
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    work = []
+    for i in range(2):
+        q, cache, host, table, lens, out = attend(sq, 63 + i, [3000, 1700], [1, 1], 8, 2, 64, 16, BF16, 4, one_each=True)
+        work.append((q.cuda(), cache, table.cuda(), lens.cuda(), out))
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(6):
+        for i, (q, cache, table, lens, out) in enumerate(work):
+            got[i].append(sq.squant_cache_attention(q, cache, table, lens, stream=sides[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(g, work[i][4]) for g in got[i])
