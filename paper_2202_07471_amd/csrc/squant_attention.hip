@@ -306,6 +306,7 @@ int squant_attention(const squant_heads_t* h_q, const squant_heads_t* h_k, const
   a.q = strided(h_q, p.q_rows), a.o = strided(h_out, p.q_rows);
   if (p.k_rows) a.k = strided(h_k, p.k_rows), a.v = strided(h_v, p.k_rows);
   a.lse = d_lse;
+  a.by_length = f.groups > kRunAtOnce && p.sequences > 1;
   a.splits = f.splits, a.stats = (float2*)d_workspace, a.partial = (float*)((char*)d_workspace + f.stats);
   hipStream_t st = (hipStream_t)stream;
   if (int rc = launch(f.run.run, f.groups, f.splits, f.run.lds, st, a, f.run.threads)) return rc;
@@ -353,13 +354,13 @@ int squant_attention_backward(const squant_heads_t* h_dout, const squant_heads_t
   const auto join_groups = [&](int64_t elements) { return (elements / 4 + kThreads - 1) / kThreads; };
   if (qr) {
     if (int rc = launch(prompt_delta_kernel(t), b.delta_groups, 1, 0, st, a)) return rc;
-    a.splits = b.q_splits;
+    a.splits = b.q_splits, a.by_length = b.q_groups > kRunAtOnce && p.sequences > 1;
     if (int rc = launch(b.queries.run, b.q_groups, b.q_splits, b.queries.lds, st, a, b.queries.threads)) return rc;
     if (b.q_splits > 1)
       if (int rc = launch(prompt_join_kernel(t, false), join_groups(qr * p.heads * p.head_dim), 1, 0, st, a)) return rc;
   }
   if (!kr) return SQUANT_OK;
-  a.splits = qr ? b.k_splits : 1;
+  a.splits = qr ? b.k_splits : 1, a.by_length = b.k_groups > kRunAtOnce && p.sequences > 1;
   if (int rc = launch(b.keys.run, b.k_groups, a.splits, b.keys.lds, st, a, b.keys.threads)) return rc;
   return a.splits > 1 ? launch(prompt_join_kernel(t, true), join_groups(kr * p.kv_heads * 2 * p.head_dim), 1, 0, st, a) : SQUANT_OK;
 }

@@ -28,6 +28,7 @@ struct PromptArgs {
   Packed queries, keys;
   int32_t heads, kv_heads, group, dim;
   int32_t causal;
+  int32_t by_length;      // the order of tiles
   float scale, scale2;    // scale2: times log2(e), never 0 (a hidden score's minus infinity stays one)
   // walks that are cut into `splits` (the grid's y): their sums, [splits][rows][heads][1 or 2][dim], and, forward, the rows' largest
   // scores (base 2) and sums of weights, [splits][rows][heads]
@@ -81,10 +82,12 @@ template <class T, int DP, int ROWS, int WAVES, bool DIRECT> struct Loader {
         piece[i] = load_any<uint4v>(from + off(i));
     }
   }
-  // `from`: the tile's first row; `count`: rows from there on, at least one.
-  __device__ __forceinline__ void issue(const char* from, char* tile, int count, uint32_t row_bytes, int dim) {
-    if (count >= ROWS) take(from, tile, [&](int i) { return offset[i]; });
-    else take(from, tile, [&](int i) { return offset_of(i, row_bytes, count - 1, dim); });
+  // `from`: the tile's first row; `count`: rows from there on, at least one.  KEPT: full tiles by the offsets kept.  The loops of
+  // hidden steps make them anew: they have no registers for them, and reading them back from memory waits for what is on its way,
+  // each time (forward of 34 sequences of 300 tokens, 32 heads of 128: 131 us, 103).
+  template <bool KEPT> __device__ __forceinline__ void issue(const char* from, char* tile, int count, uint32_t row_bytes, int dim, Constant<KEPT>) {
+    if (KEPT && count >= ROWS) take(from, tile, [&](int i) { return offset[i]; });
+    else take(from, tile, [&](int i) { return offset_of(i, row_bytes, min(count, ROWS) - 1, dim); });
   }
   // Before the barrier behind which the tile is read.
   __device__ __forceinline__ void land(char* tile) const {
@@ -234,6 +237,89 @@ template <int FIRST, int SECOND, int EACH, int SECOND_STEP> __device__ __forcein
 // (binary16: 2^15).  Without it most steps of a long sequence have a row of the wave's 32 whose maximum moves.
 constexpr float kSlack = 8.0f;
 
+// The tile of a workgroup, and the rows that its sequence walks over.
+//
+// Where there are more workgroups than run at once, sequences with longer walks come first (and, `by_tile`, tiles with longer ones over all sequences):
+// what is left for the end is short, and the compute units end together.  10239 tokens in seven causal sequences of 261
+// to 4096, the second longest in the fifth place, 32 heads of 128 on 8: forward 322 us in their own order, 301; dK and dV 632, 569
+// (its walks are 64 tiles times four heads, and few).  Forward takes whole sequences: tile by tile, ten of 1024 tokens, which
+// all begin and end together then, took 158 us, 148 otherwise.
+// With T a tile's rows, tile i of a sequence (the first being its longest walk) is on level
+//   by_tile: max(0, min(ceil(walked / T), its tiles - i)),  else ceil(walked / T),
+// its walk's length in tiles.  A lane for each sequence knows how many of its tiles lie above a level; the level at which they
+// are more than `id` is searched by halves.
+constexpr int kRunAtOnce = 512;  // two a compute unit
+// Where piece i of a walk's steps (less than 2^27) begins.
+__device__ __forceinline__ int piece_of(int steps, uint32_t i, int splits) { return (int)((uint32_t)steps * i / (uint32_t)splits); }
+
+struct PromptTile {
+  int sequence;  // -1: this tile is no one's
+  int index, tiles;
+  int start, length;  // its sequence's rows
+  int walk_start, walk_length;
+};
+// Sums over the lanes up to each, by moves within the vector registers: within 16 lanes, then of those before.
+__device__ __forceinline__ int up_to_lane(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+__device__ __forceinline__ int over_lanes_sum(int v) { return __builtin_amdgcn_readlane(up_to_lane(v), 63); }
+
+__device__ __forceinline__ PromptTile find_walk(const Packed& own, const Packed& walk, bool by_length, bool by_tile, int id, int tile) {
+  PromptTile t;
+  if (!own.starts || own.count >= 63) {
+    const Tile f = find_tile(own, id, 1, tile);
+    t.sequence = f.sequence;
+    if (t.sequence < 0) return t;
+    auto one = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    t.index = one(f.index), t.tiles = one(f.tiles), t.start = one(f.start), t.length = one(f.length);
+    t.walk_start = one(walk.start(min(t.sequence, walk.count))), t.walk_length = one(t.sequence < own.count ? walk.length(t.sequence) : 0);
+    return t;
+  }
+  const int lane = (int)(threadIdx.x & 63u), here = min(lane, own.count);
+  const int own_at = own.starts[here], walk_at = walk.starts[here];
+  auto inside = [](const Packed& p, int at) { return min(max(at, 0), p.rows); };
+  const int start = inside(own, own_at), walk_start = inside(walk, walk_at);
+  // the next lane's
+  const int end = __builtin_amdgcn_update_dpp(0, start, 0x130, 0xf, 0xf, false), walk_end = __builtin_amdgcn_update_dpp(0, walk_start, 0x130, 0xf, 0xf, false);
+  const bool real = lane < own.count;
+  const int length = lane > own.count ? 0 : max((real ? end : own.rows) - start, 0), walk_length = real ? max(walk_end - walk_start, 0) : 0;
+  auto in_tiles = [&](int n) { return (int)(((uint32_t)n + (uint32_t)tile - 1) / (uint32_t)tile); };
+  const int cap = in_tiles(walk_length);
+  t.sequence = -1;
+  if (by_length && (by_tile || lanes_where(real && cap != __builtin_amdgcn_readfirstlane(cap)))) {
+    const int tiles = in_tiles(length), top = by_tile && real ? tiles : 0x40000000;
+    auto above = [&](int level) { return level < 0 ? tiles : cap > level ? min(max(top - level, 0), tiles) : 0; };
+    if (id >= over_lanes_sum(tiles)) return t;
+    // tiles above `high` are no more than id, those above `low` more
+    int low = -1, high = in_tiles(walk.rows);
+    while (high - low > 1) {
+      const int middle = (high + low) / 2;
+      if (over_lanes_sum(above(middle)) <= id) high = middle;
+      else low = middle;
+    }
+    const int before = above(high), at = id - over_lanes_sum(before), upto = up_to_lane(above(high - 1) - before);
+    t.sequence = (int)__builtin_ctzll(lanes_where(upto > at));
+    t.index = __builtin_amdgcn_readlane(before, t.sequence) + at - (t.sequence ? __builtin_amdgcn_readlane(upto, t.sequence - 1) : 0);
+  } else {
+    // as find_tile does
+    const int place = start / tile + lane;
+    t.sequence = __popcll(lanes_where(lane <= own.count && place <= id)) - 1;
+    if (t.sequence < 0) return t;
+    t.index = id - __builtin_amdgcn_readlane(place, t.sequence);
+  }
+  t.start = __builtin_amdgcn_readlane(start, t.sequence), t.length = __builtin_amdgcn_readlane(length, t.sequence);
+  t.walk_start = __builtin_amdgcn_readlane(walk_start, t.sequence), t.walk_length = __builtin_amdgcn_readlane(walk_length, t.sequence);
+  t.index = __builtin_amdgcn_readfirstlane(t.index), t.tiles = __builtin_amdgcn_readfirstlane(in_tiles(t.length));
+  if (t.index < 0 || t.index >= t.tiles) t.sequence = -1;
+  return t;
+}
+
 template <class T, int DP, int QT, int BK, int WAVES, int OCCUPANCY, bool DIRECT>
 __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptArgs a) {
   typedef typename MatrixOf<T>::type M;
@@ -245,28 +331,26 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
   int* const odd_flag = reinterpret_cast<int*>(tiles + 4 * kTile);
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const int turn = (int)(blockIdx.x % (uint32_t)a.heads), kv_head = turn % a.kv_heads, head = kv_head * a.group + turn / a.kv_heads;
-  const Tile tile = find_tile(a.queries, blockIdx.x / (uint32_t)a.heads, 1, kRows);
+  const PromptTile tile = find_walk(a.queries, a.keys, a.by_length, false, (int)(blockIdx.x / (uint32_t)a.heads), kRows);
   if (tile.sequence < 0) return;
   // the longest tiles of a causal sequence first
-  const int seq = tile.sequence, first = (tile.tiles - 1 - tile.index) * kRows;
-  const int rows = tile.length, q0 = tile.start;
-  const int keys = seq < a.queries.count ? a.keys.length(seq) : 0, k0 = a.keys.start(min(seq, a.keys.count));
+  const int first = (tile.tiles - 1 - tile.index) * kRows;
+  const int rows = tile.length, q0 = tile.start, keys = tile.walk_length, k0 = tile.walk_start;
   const int shift = keys - rows;
   auto sees = [&](int r) { return a.causal ? min(max(r + shift + 1, 0), keys) : keys; };
   const int mine = first + wave * 16 * QT;
-  int seen[QT];
   frag q[QT][KS];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     const int r = mine + 16 * t + n;
     const bool live = r < rows;
-    seen[t] = live ? sees(r) : 0;
     own_operand<T, KS>(q[t], a.q, q0 + (live ? r : 0), head, live, a.dim);
   }
   const int wave_most = mine < rows ? sees(min(mine + 16 * QT, rows) - 1) : 0;
   const int most = sees(min(first + kRows, rows) - 1);
   const int all_steps = (most + BK - 1) / BK;
-  const int begin = (int)((int64_t)all_steps * blockIdx.y / gridDim.y), steps = (int)((int64_t)all_steps * (blockIdx.y + 1) / gridDim.y);
+  int begin = 0, steps = all_steps;
+  if (a.splits > 1) begin = piece_of(all_steps, blockIdx.y, a.splits), steps = piece_of(all_steps, blockIdx.y + 1, a.splits);
   const int whole = min(first + kRows <= rows ? sees(first) / BK : 0, steps);  // steps of which all rows see all keys
 
   float4v o[QT][F];
@@ -284,10 +368,10 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
   const Lanes<T, DP> at;
   lk.begin(k_bytes, a.dim);
   lv.begin(v_bytes, a.dim);
-  auto issue = [&](int j) {
+  auto issue = [&](int j, auto kept) {
     char* at = tiles + (j & 1) * 2 * kTile;
-    lk.issue(k_from + (int64_t)j * BK * k_bytes, at, keys - j * BK, k_bytes, a.dim);
-    lv.issue(v_from + (int64_t)j * BK * v_bytes, at + kTile, keys - j * BK, v_bytes, a.dim);
+    lk.issue(k_from + (int64_t)j * BK * k_bytes, at, keys - j * BK, k_bytes, a.dim, kept);
+    lv.issue(v_from + (int64_t)j * BK * v_bytes, at + kTile, keys - j * BK, v_bytes, a.dim, kept);
   };
   auto land = [&](int j) {
     char* at = tiles + (j & 1) * 2 * kTile;
@@ -296,11 +380,16 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
     if (DIRECT) tiles_are_here();
   };
   if (steps > begin) {
-    issue(begin);
+    issue(begin, Constant<true>{});
     land(begin);
   }
   __syncthreads();
 
+  // Keys from step j on that the lane's row t sees, made anew: kept, they would be put into memory.  Rows past the last hold zeros.
+  auto seen_from = [&](int j, int t) {
+    const int left = keys - j * BK;
+    return a.causal ? min(max(mine + 16 * t + shift + 1 - j * BK + n, -j * BK), left) : left;
+  };
   auto step = [&](int j, auto some_hidden) {
     constexpr bool kHidden = decltype(some_hidden)::value;
     const int kt = at.row + (j & 1) * 2 * kTile, vt = at.turned + (j & 1) * 2 * kTile + kTile;
@@ -328,12 +417,14 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
     }
     if constexpr (kHidden) {
 #pragma unroll
-      for (int tt = 0; tt < TT; ++tt)
+      for (int t = 0; t < QT; ++t) {
+        const int here = seen_from(j, t) - 4 * g;
 #pragma unroll
-        for (int t = 0; t < QT; ++t)
+        for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (j * BK + 16 * tt + 4 * g + i >= seen[t]) s[tt][t][i] = -kInfinity;
+            if (16 * tt + i >= here) s[tt][t][i] = -kInfinity;
+      }
     }
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
@@ -391,7 +482,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
 #pragma unroll
             for (int t = 0; t < QT; ++t) {
               const float4v one = M::mma(v, p[t][kk], float4v{0, 0, 0, 0});
-              if (j * BK + 32 * kk + token < seen[t]) o[t][f] += one;
+              if (32 * kk + token < seen_from(j, t)) o[t][f] += one;
             }
           }
     }
@@ -399,14 +490,14 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
   int j = begin;
 #pragma unroll 1
   for (; j < whole; ++j) {
-    if (j + 1 < steps) issue(j + 1);
+    if (j + 1 < steps) issue(j + 1, Constant<true>{});
     step(j, Constant<false>{});
     if (j + 1 < steps) land(j + 1);
     __syncthreads();
   }
 #pragma unroll 1
   for (; j < steps; ++j) {
-    if (j + 1 < steps) issue(j + 1);
+    if (j + 1 < steps) issue(j + 1, Constant<false>{});
     step(j, Constant<true>{});
     if (j + 1 < steps) land(j + 1);
     __syncthreads();
@@ -416,7 +507,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
     const int r = mine + 16 * t + n;
     const float total = over_groups_sum(sum[t]);
     if (r >= rows) continue;
-    if (gridDim.y > 1) {
+    if (a.splits > 1) {
       const int64_t at = ((int64_t)blockIdx.y * a.queries.rows + q0 + r) * a.heads + head;
       if (g == 0) a.stats[at] = make_float2(largest[t], total);
       float* p = a.partial + at * a.dim + 4 * g;
@@ -479,14 +570,11 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_backward(PromptA
   const int turn = (int)(blockIdx.x % heads);
   const int kv_head = KEYS ? turn : turn % a.kv_heads, head0 = kv_head * a.group + (KEYS ? 0 : turn / a.kv_heads);
   const Packed& own = KEYS ? a.keys : a.queries;
-  const Tile tile = find_tile(own, blockIdx.x / heads, 1, kRows);
+  const PromptTile tile = find_walk(own, KEYS ? a.queries : a.keys, a.by_length, KEYS && a.causal, (int)(blockIdx.x / heads), kRows);
   if (tile.sequence < 0) return;
-  const int seq = tile.sequence, first = (KEYS ? tile.index : tile.tiles - 1 - tile.index) * kRows;
-  const bool real = seq < own.count;
-  const int rows = real || !KEYS ? a.queries.length(min(seq, a.queries.count)) : 0, q0 = a.queries.start(min(seq, a.queries.count));
-  const int keys = real || KEYS ? a.keys.length(min(seq, a.keys.count)) : 0, k0 = a.keys.start(min(seq, a.keys.count));
-  const int own_count = KEYS ? keys : rows, own0 = KEYS ? k0 : q0;
-  const int walk_count = real ? (KEYS ? rows : keys) : 0, walk0 = KEYS ? q0 : k0;
+  const int first = (KEYS ? tile.index : tile.tiles - 1 - tile.index) * kRows;
+  const int own_count = tile.length, own0 = tile.start, walk_count = tile.walk_length, walk0 = tile.walk_start;
+  const int rows = KEYS ? walk_count : own_count, keys = KEYS ? own_count : walk_count;
   const int shift = keys - rows;  // query i sees key j if j <= i + shift
   const Strided& own1 = KEYS ? a.k : a.q;
   const Strided& own2 = KEYS ? a.v : a.d_o;
@@ -529,7 +617,8 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_backward(PromptA
   }
   const int per_head = to > from ? (to - from + BS - 1) / BS : 0;
   const int all_steps = KEYS ? per_head * a.group : per_head;
-  const int begin = (int)((int64_t)all_steps * blockIdx.y / gridDim.y), steps = (int)((int64_t)all_steps * (blockIdx.y + 1) / gridDim.y);
+  int begin = 0, steps = all_steps;
+  if (a.splits > 1) begin = piece_of(all_steps, blockIdx.y, a.splits), steps = piece_of(all_steps, blockIdx.y + 1, a.splits);
   int member = KEYS && begin ? begin / per_head : 0, at = from + (begin - member * per_head) * BS;
 
   const uint32_t bytes1 = (uint32_t)walk1.row * sizeof(T), bytes2 = (uint32_t)walk2.row * sizeof(T);
@@ -541,10 +630,10 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_backward(PromptA
   l2.begin(bytes2, a.dim);
   float row_stat = 0.0f;
   int next_at = at, next_member = member;  // of the tile that is on its way
-  auto issue = [&](int j) {
+  auto issue = [&](int j, auto kept) {
     char* to_tile = tiles + (j & 1) * 2 * kTile;
-    l1.issue(from1 + (int64_t)next_at * bytes1 + (KEYS ? (int64_t)next_member * walk1.head * (int64_t)sizeof(T) : 0), to_tile, walk_count - next_at, bytes1, a.dim);
-    l2.issue(from2 + (int64_t)next_at * bytes2 + (KEYS ? (int64_t)next_member * walk2.head * (int64_t)sizeof(T) : 0), to_tile + kTile, walk_count - next_at, bytes2, a.dim);
+    l1.issue(from1 + (int64_t)next_at * bytes1 + (KEYS ? (int64_t)next_member * walk1.head * (int64_t)sizeof(T) : 0), to_tile, walk_count - next_at, bytes1, a.dim, kept);
+    l2.issue(from2 + (int64_t)next_at * bytes2 + (KEYS ? (int64_t)next_member * walk2.head * (int64_t)sizeof(T) : 0), to_tile + kTile, walk_count - next_at, bytes2, a.dim, kept);
     if (KEYS && threadIdx.x < 2 * BS) {
       const int r = min(next_at + (int)threadIdx.x % BS, walk_count - 1);
       const float* p = (int)threadIdx.x < BS ? a.lse : a.delta;
@@ -560,7 +649,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_backward(PromptA
     if (DIRECT) tiles_are_here();
   };
   if (steps > begin) {
-    issue(begin);
+    issue(begin, Constant<true>{});
     land(begin);
   }
   __syncthreads();
@@ -670,7 +759,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_backward(PromptA
   auto one = [&](auto hidden) {
     next_at = at + BS, next_member = member;
     if (KEYS && next_at >= to) next_at = from, next_member = member + 1;
-    if (j + 1 < steps) issue(j + 1);
+    if (j + 1 < steps) issue(j + 1, Constant<!decltype(hidden)::value>{});
     step(j, at, hidden);
     if (j + 1 < steps) land(j + 1);
     __syncthreads();
@@ -704,7 +793,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_backward(PromptA
       if (g == 0) a.delta[(int64_t)head0 * a.queries.rows + own0 + r] = own_delta[t] + left;
     }
     if constexpr (!kMend) {
-      if (gridDim.y > 1) {
+      if (a.splits > 1) {
         constexpr int kSums = KEYS ? 2 : 1;
         float* p = a.partial + (((int64_t)blockIdx.y * own.rows + own0 + r) * heads + (KEYS ? kv_head : head0)) * kSums * a.dim + 4 * g;
 #pragma unroll
