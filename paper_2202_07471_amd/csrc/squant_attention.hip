@@ -118,10 +118,11 @@ struct CacheSplit {
   int64_t splits, chunk;
   size_t stats_bytes, bytes;
 };
-// A workgroup costs as much as a few hundred tokens before its first and behind its last: as many as run at once, and no more
+// A workgroup costs as much as a few hundred tokens before its first and behind its last: about as many as run at once, and no more
 // than kMostChunk tokens each, so that sequences of different lengths balance.  96 sequences of 1024 to 16384 tokens: 179 us with stretches
-// of 6144, 171 with 1536; 11 of up to 6007 with five rows each: 48 us with 512, 37 with 768.
-constexpr int64_t kGroups = 768, kLeastChunk = 512, kMostChunk = 1536, kMostSplits = 1024;
+// of 6144, 171 with 1536.  Of 32 rows two run on a compute unit, 11 sequences of up to 6007 tokens with five rows each: 48 us with 512
+// workgroups, 37 with 768, 38 with 1024; of 16 rows three or more, 13 sequences of up to 3001 tokens with a row each: 23 us with 768, 21 with 1024.
+constexpr int64_t kGroups16 = 1024, kGroups32 = 768, kLeastChunk = 512, kMostChunk = 1536, kMostSplits = 1024;
 
 bool split_cache(int64_t rows, int32_t heads, const squant_cache_t& c, const squant_paged_t& w, CacheSplit& s) {
   const int group = heads / c.heads;
@@ -131,7 +132,7 @@ bool split_cache(int64_t rows, int32_t heads, const squant_cache_t& c, const squ
   s.tiles = w.starts ? tiles_bound(rows, group, tile, w.sequences) : (int64_t)w.sequences * ((group + tile - 1) / tile);
   const int64_t capacity = (int64_t)w.table_width * c.page_size;
   const int64_t groups = s.tiles * c.heads;
-  int64_t chunk = capacity * groups / kGroups;
+  int64_t chunk = capacity * groups / (s.rt == 2 ? kGroups32 : kGroups16);
   chunk = std::max({kLeastChunk, std::min(kMostChunk, (chunk + 127) / 128 * 128), (capacity / kMostSplits + 127) / 128 * 128});
   s.splits = std::max<int64_t>(1, (capacity + chunk - 1) / chunk);
   s.chunk = s.splits == 1 ? std::max<int64_t>(128, (capacity + 127) / 128 * 128) : chunk;
