@@ -396,3 +396,31 @@ def test_autograd_in_a_graph(sq):
         want = (want,) + sq.squant_attention_backward(dout, q, k, v, want, lse, starts)
         for a, b in zip((held,) + grads, want):
             assert torch.equal(a, b)
+
+
+def test_autograd_of_views(sq):
+    """One sequence without starts; keys of one head for several, broadcast; queries whose elements are not beside each other."""
+    q, k, v, w = (t.cuda() for t in inputs(37, 50, 50, 4, 1, 32, F32, peak=1.0))
+    base = q.transpose(1, 2).contiguous().requires_grad_()
+    k2, v2 = k.clone().requires_grad_(), v.clone().requires_grad_()
+    out = sq.packed_attention(base.transpose(1, 2), k2.expand(50, 2, 32), v2.expand(50, 2, 32))
+    out.backward(w)
+    r = packed64(*(t.double().cpu() for t in (q, k, v)), [50], [50], 32 ** -0.5, True, F32, w.double().cpu())
+    close(out, r, "out")
+    close(base.grad.transpose(1, 2), r, "dq")
+    for t, name in ((k2, "dk"), (v2, "dv")):
+        close(t.grad, {name: r[name], name + "_tol": 2 * r[name + "_tol"]}, name)
+
+
+def test_two_steps_of_one_graph(sq):
+    """The same keys twice in a graph: their gradients add up; a second backward pass over a kept graph gives the same again."""
+    q, k, v, w = (t.cuda() for t in inputs(38, 40, 40, 2, 1, 64, BF16))
+    leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+    out = sq.packed_attention(*leaves)
+    once = torch.autograd.grad(out, leaves, w, retain_graph=True)
+    again = torch.autograd.grad(out, leaves, w)
+    assert all(torch.equal(a, b) for a, b in zip(once, again))
+    both_ = sq.packed_attention(leaves[0], leaves[1], leaves[1])
+    both_.backward(w)
+    _, dk, dv = both(sq, q, k, k, w, None, None, None, True)[2:]
+    assert torch.equal(leaves[1].grad, dk + dv)
