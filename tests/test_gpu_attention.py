@@ -424,3 +424,15 @@ def test_two_steps_of_one_graph(sq):
     both_.backward(w)
     _, dk, dv = both(sq, q, k, k, w, None, None, None, True)[2:]
     assert torch.equal(leaves[1].grad, dk + dv)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("causal", [True, False])
+def test_more_tiles_than_run_at_once(sq, causal, dtype):
+    """Tiles in the order of their walks: sequences without queries or keys, more queries than keys, padding, all alike, 61 to 63 of them."""
+    for q_counts, k_counts, heads, kv in (([0, 300, 17, 130, 260, 1, 129, 3], [5, 300, 90, 130, 400, 64, 0, 1], 64, 32), ([128] * 6, [128] * 6, 64, 64),
+                                          ([260] * 4, [200, 260, 200, 264], 64, 32), ([5, 200], [700, 30], 128, 64)):
+        check(sq, 39, q_counts, k_counts, heads, kv, 32, dtype, causal, q_pad=140, k_pad=70)
+    for sequences in (61, 62, 63):
+        counts = [(7 * i) % 23 + (200 if i % 20 == 19 else 0) for i in range(sequences)]
+        check(sq, 40, counts, counts[::-1], 16, 16, 32, dtype, causal, q_pad=1)
