@@ -206,7 +206,7 @@ ForwardPlan plan_forward(const squant_packed_t& p, int type, bool direct) {
 // Queries are walked over by dK and dV of all types, keys by dQ of binary32 (16-bit types have three sums to add up there).
 struct BackwardPlan {
   PromptKernel queries, keys;
-  int64_t q_groups, k_groups, delta_groups;
+  int64_t q_groups, k_groups;
   int q_splits, k_splits;
   size_t delta, q_partial, k_partial;  // bytes; the partial sums follow delta, one after the other's use
   bool fit;
@@ -217,14 +217,13 @@ BackwardPlan plan_backward(const squant_packed_t& p, int type, bool queries_dire
   b.queries = (type == SQUANT_W_F32 ? prompt_queries_f32 : type == SQUANT_W_F16 ? prompt_queries_f16 : prompt_queries_bf16)(p.head_dim, keys_direct);
   b.keys = (type == SQUANT_W_F32 ? prompt_keys_f32 : type == SQUANT_W_F16 ? prompt_keys_f16 : prompt_keys_bf16)(p.head_dim, queries_direct);
   const PromptArgs a = prompt_args(p);
-  b.delta_groups = (p.q_rows * p.heads * 16 + kThreads - 1) / kThreads;
   b.q_groups = prompt_groups(a.queries, b.queries, p.heads), b.k_groups = prompt_groups(a.keys, b.keys, p.kv_heads);
   b.q_splits = type == SQUANT_W_F32 ? walk_splits(b.q_groups, p.k_rows, p.sequences, 1, b.queries.walked) : 1;
   b.k_splits = walk_splits(b.k_groups, p.q_rows, p.sequences, a.group, b.keys.walked);
   b.delta = ((size_t)p.q_rows * p.heads * 4 + 255) / 256 * 256;
   b.q_partial = b.q_splits > 1 ? (size_t)b.q_splits * p.q_rows * p.heads * p.head_dim * 4 : 0;
   b.k_partial = b.k_splits > 1 ? (size_t)b.k_splits * p.k_rows * p.kv_heads * 2 * p.head_dim * 4 : 0;
-  b.fit = (!p.q_rows || (fits(b.delta_groups) && fits(b.q_groups, b.q_splits, b.queries.threads))) && (!p.k_rows || fits(b.k_groups, b.k_splits, b.keys.threads));
+  b.fit = (!p.q_rows || fits(b.q_groups, b.q_splits, b.queries.threads)) && (!p.k_rows || fits(b.k_groups, b.k_splits, b.keys.threads));
   return b;
 }
 
@@ -354,7 +353,6 @@ int squant_attention_backward(const squant_heads_t* h_dout, const squant_heads_t
   hipStream_t st = (hipStream_t)stream;
   const auto join_groups = [&](int64_t elements) { return (elements / 4 + kThreads - 1) / kThreads; };
   if (qr) {
-    if (int rc = launch(prompt_delta_kernel(t), b.delta_groups, 1, 0, st, a)) return rc;
     a.splits = b.q_splits, a.by_length = b.q_groups > kRunAtOnce && p.sequences > 1;
     if (int rc = launch(b.queries.run, b.q_groups, b.q_splits, b.queries.lds, st, a, b.queries.threads)) return rc;
     if (b.q_splits > 1)

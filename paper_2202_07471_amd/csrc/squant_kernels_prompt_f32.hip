@@ -6,10 +6,6 @@ namespace att {
 
 PromptKernel prompt_forward_f32(int dim, bool direct) { return forward_for<float>(dim, direct); }
 
-prompt_t prompt_delta_kernel(int type) {
-  return type == SQUANT_W_F32 ? prompt_delta<float> : type == SQUANT_W_F16 ? prompt_delta<_Float16> : prompt_delta<__bf16>;
-}
-
 prompt_t prompt_join_forward_kernel(int type) {
   return type == SQUANT_W_F32 ? prompt_join_forward<float> : type == SQUANT_W_F16 ? prompt_join_forward<_Float16> : prompt_join_forward<__bf16>;
 }

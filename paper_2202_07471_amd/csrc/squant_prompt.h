@@ -523,24 +523,6 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
   }
 }
 
-// delta[h][r] = dO . O: 16 lanes a row and head.
-template <class T> __global__ __launch_bounds__(kThreads) void prompt_delta(PromptArgs a) {
-  const int64_t at = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / 16;
-  if (at >= (int64_t)a.queries.rows * a.heads) return;
-  const int64_t row = at / a.heads;
-  const int head = (int)(at - row * a.heads), lane = (int)threadIdx.x & 15;
-  float sum = 0.0f;
-  for (int d = lane * 8; d < a.dim; d += 128) {
-    struct Eight { T v[8]; };
-    const Eight x = load_any<Eight>(element<T>(a.o, row, head) + d), y = load_any<Eight>(element<T>(a.d_o, row, head) + d);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sum = __builtin_fmaf((float)x.v[i], (float)y.v[i], sum);
-  }
-#pragma unroll
-  for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor(sum, o);
-  if (lane == 0) a.delta[(int64_t)head * a.queries.rows + row] = sum;
-}
-
 // Binary16 gradients: dS is held times 2^e, e running for the wave (a tile with a larger one lowers it, and the sums with it): its
 // largest magnitude stays below 2^15, and 2^-39 of the largest so far is still told from 0.
 __device__ __forceinline__ int gradient_exponent(uint32_t top) {
@@ -550,7 +532,8 @@ __device__ __forceinline__ int gradient_exponent(uint32_t top) {
 // KEYS: the workgroup owns keys and values and walks over queries (dK, dV); otherwise it owns queries and walks over keys (dQ).
 // First operands: keys and queries; second: values and the output's gradient.
 //
-// delta.  dS's rows add up to 0.  delta from the output as it was stored is off by its rounding (and the weights' in it), by
+// delta.  The dQ kernel has dO in registers and reads O beside it; the other kernel reads what it leaves (a launch of its own for
+// delta took 28 us for 10239 rows of 32 heads of 128).  dS's rows add up to 0.  delta from the output as it was stored is off by its rounding (and the weights' in it), by
 // the same for all of a row's keys: with binary16 and bfloat16 as much as everything else together (dQ and dK of 1024
 // causal tokens of 128: 2.7e-3 off, 2.3e-3 without it, 1.7e-3 the rounding of the result).  So the dQ kernel adds up its dS in
 // binary32 and P K beside dS K: sum dS = delta's error, which it takes off both dQ and delta, before the other kernel reads it.  One
@@ -593,10 +576,20 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_backward(PromptA
     own_operand<T, KS>(x1[t], own1, at, head, live, a.dim);
     own_operand<T, KS>(x2[t], own2, at, head, live, a.dim);
     own_lse[t] = own_delta[t] = own_left[t] = 0.0f;
-    if (!KEYS && live) {
-      const float l = a.lse[(int64_t)head0 * a.queries.rows + at];
-      own_lse[t] = l == -kInfinity ? kInfinity : l * kLog2E;
-      own_delta[t] = a.delta[(int64_t)head0 * a.queries.rows + at];
+    if constexpr (!KEYS) {
+      frag o[KS];
+      own_operand<T, KS>(o, a.o, at, head, live, a.dim);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) own_delta[t] = __builtin_fmaf((float)o[ks][i], (float)x2[t][ks][i], own_delta[t]);
+      own_delta[t] = over_groups_sum(own_delta[t]);
+      if (live) {
+        const int64_t line = (int64_t)head0 * a.queries.rows + at;
+        const float l = a.lse[line];
+        own_lse[t] = l == -kInfinity ? kInfinity : l * kLog2E;
+        if (!kMend && blockIdx.y == 0 && g == 0) a.delta[line] = own_delta[t];
+      }
     }
   }
   float4v acc1[OT][F], acc2[kSecond ? OT : 1][kSecond ? F : 1];
@@ -884,7 +877,6 @@ PromptKernel prompt_keys_f32(int dim, bool direct);
 PromptKernel prompt_queries_bf16(int dim, bool direct);
 PromptKernel prompt_queries_f16(int dim, bool direct);
 PromptKernel prompt_queries_f32(int dim, bool direct);
-prompt_t prompt_delta_kernel(int type);
 prompt_t prompt_join_kernel(int type, bool keys);
 prompt_t prompt_join_forward_kernel(int type);
 
