@@ -436,3 +436,37 @@ def test_more_tiles_than_run_at_once(sq, causal, dtype):
     for sequences in (61, 62, 63):
         counts = [(7 * i) % 23 + (200 if i % 20 == 19 else 0) for i in range(sequences)]
         check(sq, 40, counts, counts[::-1], 16, 16, 32, dtype, causal, q_pad=1)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_far_rows(sq, dtype):
+    """Rows as far apart as they may be, the last ones beyond 2^32 bytes; further is refused."""
+    rows, heads, kv, dim, step = 600 if dtype == BF16 else 300, 4, 2, 64, 1 << 22
+    q, k, v, dout = (t.cuda() for t in inputs(41, rows, rows, heads, kv, dim, dtype))
+    wide = torch.empty(rows, step, dtype=dtype, device="cuda")
+    x = wide[:, :(2 * heads + 2 * kv + 2 * heads + 2 * kv) * dim].unflatten(1, (-1, dim))
+    parts = x.split([heads, kv, kv, heads, heads, heads, kv, kv], 1)
+    for a, b in zip(parts, (q, k, v, dout)):
+        a.copy_(b)
+    starts = starts_of([rows - 50, 50]).cuda()
+    want, lse = sq.squant_attention(q, k, v, starts)
+    want_grads = sq.squant_attention_backward(dout, q, k, v, want, lse, starts)
+    out, lse2 = sq.squant_attention(*parts[:3], starts, out=parts[4])
+    grads = sq.squant_attention_backward(parts[3], *parts[:3], out, lse2, starts, dq=parts[5], dk=parts[6], dv=parts[7])
+    for a, b in zip((out, lse2) + grads, (want, lse) + want_grads):
+        assert torch.equal(a, b)
+    cache = sq.QuantizedCache.empty(2, kv, rows, dim)
+    args = (torch.tensor([[1]], dtype=torch.int32).cuda(), torch.tensor([rows], dtype=torch.int32).cuda(), starts_of([rows]).cuda())
+    near = sq.QuantizedCache.empty(2, kv, rows, dim)
+    sq.squant_cache_write(parts[1], parts[2], cache, *args)
+    sq.squant_cache_write(k, v, near, *args)
+    assert all(torch.equal(a[1].view(torch.int8), b[1].view(torch.int8)) for a, b in zip(cache, near))
+    sq.squant_cache_read(cache, *args, rows, dtype, k=parts[6], v=parts[7])
+    for a, b in zip(parts[6:], sq.squant_cache_read(cache, *args, rows, dtype)):
+        assert torch.equal(a, b)
+    sq.squant_cache_attention(parts[0], cache, *args, out=parts[5])
+    assert torch.equal(parts[5], sq.squant_cache_attention(q, cache, *args))
+    del wide, x, parts, out, grads
+    far = torch.empty(3 * (step + 8), dtype=dtype, device="cuda").view(3, -1)[:, :heads * dim].unflatten(1, (heads, dim))
+    with pytest.raises(sq.SQuantError):
+        sq.squant_attention(far, k[:3], v[:3])
