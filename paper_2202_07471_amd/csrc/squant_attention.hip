@@ -174,13 +174,20 @@ int64_t prompt_groups(const Packed& p, const PromptKernel& k, int32_t heads) {
   return tiles_bound(p.rows, 1, k.rows, p.count) * heads;
 }
 
-// Where there are fewer workgroups than run at once, walks are cut into pieces whose sums a launch more adds up: about 512 workgroups, at
-// least 2 tiles a piece on average, at most 8 pieces.  Six packed sequences of up to 515 tokens, six heads of 96 on two, binary32: dK and dV
-// 199 us, 47 and a join of 5 with eight pieces; dQ 58, 29 and 4 with three.
-int walk_splits(int64_t groups, int64_t walked, int64_t sequences, int heads, int tile) {
-  const int64_t tiles = heads * (walked / std::max<int64_t>(1, sequences)) / tile;
-  return (int)std::max<int64_t>(1, std::min({(int64_t)8, 512 / std::max<int64_t>(1, groups), tiles / 2}));
+// Where there are few workgroups, walks are cut into at most 8 pieces whose sums a launch more adds up.
+// Fewer than run at once: to about 512, at least 2 tiles a piece on average.  Six packed sequences of up to 515 tokens, six heads of 96 on two,
+// binary32: dK and dV 199 us, 47 and a join of 5 with eight pieces; dQ 58, 29 and 4 with three.
+// Hardly more than that: the longest walk of a causal sequence, twice the average, ends last, so long walks are cut on, to `most`
+// workgroups and 12 tiles a piece.  2048 tokens, 32 heads of 128 on 8, bfloat16: all gradients 269 us, 209 with five pieces for dK and dV; 4096
+// tokens 675, 570 with two; binary32 1748, 1244.  Pieces of 8 tiles (1024 tokens of 32 heads on 32): 63 us, 77.
+int walk_splits(int64_t groups, int64_t walked, const squant_packed_t& p, int heads, int tile, int64_t most) {
+  const int64_t tiles = heads * (walked / std::max<int64_t>(1, p.sequences)) / tile, any = std::max<int64_t>(1, groups);
+  const int64_t few = std::min<int64_t>(kRunAtOnce / any, tiles / 2), uneven = p.causal ? std::min(most / any, tiles / 12) : 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(8, std::max(few, uneven)));
 }
+// Forward walks of 16-bit types and of large heads are short against what a piece costs: 2048 tokens, 32 heads of 128: 64 us, 78 with two
+// pieces; 4096 of 8 heads 93, 68 with three; binary32, 16 heads of 128: 238, 196 with two, of 256: 440, 472.
+constexpr int64_t kMostForward = 1024, kMostPieces = 1536;
 
 struct ForwardPlan {
   PromptKernel run;
@@ -194,7 +201,7 @@ ForwardPlan plan_forward(const squant_packed_t& p, int type, bool direct) {
   ForwardPlan f{};
   f.run = (type == SQUANT_W_F32 ? prompt_forward_f32 : type == SQUANT_W_F16 ? prompt_forward_f16 : prompt_forward_bf16)(p.head_dim, direct);
   f.groups = prompt_groups(prompt_args(p).queries, f.run, p.heads);
-  f.splits = walk_splits(f.groups, p.k_rows, p.sequences, 1, f.run.walked);
+  f.splits = walk_splits(f.groups, p.k_rows, p, 1, f.run.walked, type == SQUANT_W_F32 && p.head_dim <= 128 ? kMostPieces : kMostForward);
   if (f.splits > 1) {
     f.stats = ((size_t)f.splits * p.q_rows * p.heads * 8 + 255) / 256 * 256;
     f.partial = (size_t)f.splits * p.q_rows * p.heads * p.head_dim * 4;
@@ -218,8 +225,8 @@ BackwardPlan plan_backward(const squant_packed_t& p, int type, bool queries_dire
   b.keys = (type == SQUANT_W_F32 ? prompt_keys_f32 : type == SQUANT_W_F16 ? prompt_keys_f16 : prompt_keys_bf16)(p.head_dim, queries_direct);
   const PromptArgs a = prompt_args(p);
   b.q_groups = prompt_groups(a.queries, b.queries, p.heads), b.k_groups = prompt_groups(a.keys, b.keys, p.kv_heads);
-  b.q_splits = type == SQUANT_W_F32 ? walk_splits(b.q_groups, p.k_rows, p.sequences, 1, b.queries.walked) : 1;
-  b.k_splits = walk_splits(b.k_groups, p.q_rows, p.sequences, a.group, b.keys.walked);
+  b.q_splits = type == SQUANT_W_F32 ? walk_splits(b.q_groups, p.k_rows, p, 1, b.queries.walked, kMostPieces) : 1;
+  b.k_splits = walk_splits(b.k_groups, p.q_rows, p, a.group, b.keys.walked, kMostPieces);
   b.delta = ((size_t)p.q_rows * p.heads * 4 + 255) / 256 * 256;
   b.q_partial = b.q_splits > 1 ? (size_t)b.q_splits * p.q_rows * p.heads * p.head_dim * 4 : 0;
   b.k_partial = b.k_splits > 1 ? (size_t)b.k_splits * p.k_rows * p.kv_heads * 2 * p.head_dim * 4 : 0;
