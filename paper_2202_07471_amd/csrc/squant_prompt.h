@@ -49,6 +49,8 @@ template <class T, int DP> struct TileOf {
   static __device__ __forceinline__ int place(int r, int c) { return r * kRowBytes + ((c ^ turn(r)) << 4); }
 };
 
+constexpr bool keeps_offsets(int dim) { return dim < 256; }
+
 // Tiles of ROWS rows on their way from memory to the LDS.  DIRECT: without passing through registers, which takes rows at
 // multiples of 16 bytes; otherwise by registers.  A row past the last is the last one again, a piece past the head's elements the
 // first one: both meet zeros or are hidden.  Bytes of the tile are dealt to lanes in their order, 16 each.
@@ -83,8 +85,9 @@ template <class T, int DP, int ROWS, int WAVES, bool DIRECT> struct Loader {
     }
   }
   // `from`: the tile's first row; `count`: rows from there on, at least one.  KEPT: full tiles by the offsets kept.  The loops of
-  // hidden steps make them anew: they have no registers for them, and reading them back from memory waits for what is on its way,
-  // each time (forward of 34 sequences of 300 tokens, 32 heads of 128: 131 us, 103).
+  // hidden steps, and all of the largest heads, make them anew: they have no registers for them, and reading them back from memory waits
+  // for what is on its way, each time (forward of 34 sequences of 300 tokens, 32 heads of 128: 131 us, 103; of 8192 tokens, 16
+  // heads of 256: 697, 580).  Heads of 192 keep them (488, 512 without).
   template <bool KEPT> __device__ __forceinline__ void issue(const char* from, char* tile, int count, uint32_t row_bytes, int dim, Constant<KEPT>) {
     if (KEPT && count >= ROWS) take(from, tile, [&](int i) { return offset[i]; });
     else take(from, tile, [&](int i) { return offset_of(i, row_bytes, min(count, ROWS) - 1, dim); });
@@ -327,6 +330,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
   typedef TileOf<T, DP> TL;
   typedef Loader<T, DP, BK, WAVES, DIRECT> Load;
   constexpr int KS = DP / 32, F = DP / 16, TT = BK / 16, kRows = 16 * WAVES * QT, kTile = BK * TL::kRowBytes;
+  constexpr bool kKept = keeps_offsets(DP);
   extern __shared__ __attribute__((aligned(1024))) char tiles[];  // [2][keys, values], a flag
   int* const odd_flag = reinterpret_cast<int*>(tiles + 4 * kTile);
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
@@ -380,7 +384,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
     if (DIRECT) tiles_are_here();
   };
   if (steps > begin) {
-    issue(begin, Constant<true>{});
+    issue(begin, Constant<kKept>{});
     land(begin);
   }
   __syncthreads();
@@ -490,7 +494,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
   int j = begin;
 #pragma unroll 1
   for (; j < whole; ++j) {
-    if (j + 1 < steps) issue(j + 1, Constant<true>{});
+    if (j + 1 < steps) issue(j + 1, Constant<kKept>{});
     step(j, Constant<false>{});
     if (j + 1 < steps) land(j + 1);
     __syncthreads();
@@ -546,6 +550,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_backward(PromptA
   typedef Loader<T, DP, BS, WAVES, DIRECT> Load;
   constexpr bool kMend = !KEYS && sizeof(T) == 2, kSecond = KEYS || kMend;
   constexpr int KS = DP / 32, F = DP / 16, TT = BS / 16, kRows = 16 * WAVES * OT, kTile = BS * TL::kRowBytes;
+  constexpr bool kKept = keeps_offsets(DP);
   extern __shared__ __attribute__((aligned(1024))) char tiles[];  // [2][first, second], [2][2][BS] row statistics
   float* const stats = reinterpret_cast<float*>(tiles + 4 * kTile);
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
@@ -642,7 +647,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_backward(PromptA
     if (DIRECT) tiles_are_here();
   };
   if (steps > begin) {
-    issue(begin, Constant<true>{});
+    issue(begin, Constant<kKept>{});
     land(begin);
   }
   __syncthreads();
@@ -752,7 +757,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_backward(PromptA
   auto one = [&](auto hidden) {
     next_at = at + BS, next_member = member;
     if (KEYS && next_at >= to) next_at = from, next_member = member + 1;
-    if (j + 1 < steps) issue(j + 1, Constant<!decltype(hidden)::value>{});
+    if (j + 1 < steps) issue(j + 1, Constant<!decltype(hidden)::value && kKept>{});
     step(j, at, hidden);
     if (j + 1 < steps) land(j + 1);
     __syncthreads();
@@ -885,8 +890,9 @@ template <class T> PromptKernel forward_for(int dim, bool direct) {
     if (dim <= 64) return forward_of<T, 64, 2, 64, 4, 2>(direct);
     if (dim <= 96) return forward_of<T, 96, 2, 64, 4, 2>(direct);
     if (dim <= 128) return forward_of<T, 128, 2, 64, 4, 2>(direct);
-    if (dim <= 192) return forward_of<T, 192, 1, 32, 4, 2>(direct);
-    return forward_of<T, 256, 1, 32, 4, 2>(direct);
+    // 16 rows a wave: 8192 tokens, 16 heads of 192 on 4: 545 us, 488; of 256: 750, 580
+    if (dim <= 192) return forward_of<T, 192, 2, 32, 4, 2>(direct);
+    return forward_of<T, 256, 2, 32, 4, 2>(direct);
   } else {
     if (dim <= 64) return forward_of<T, 64, 1, 32, 4, 2>(direct);
     if (dim <= 96) return forward_of<T, 96, 1, 32, 4, 2>(direct);
@@ -900,8 +906,9 @@ template <class T, bool KEYS> PromptKernel backward_for(int dim, bool direct) {
     if (dim <= 64) return backward_of<T, 64, 1, 64, 4, 2, KEYS>(direct);
     if (dim <= 96) return backward_of<T, 96, 1, 64, 4, 2, KEYS>(direct);
     if (dim <= 128) return backward_of<T, 128, 1, 64, 4, 2, KEYS>(direct);
-    if (dim <= 192) return backward_of<T, 192, 1, 64, 4, 1, KEYS>(direct);  // steps of 32: 8192 tokens, 16 heads of 256 on 4: 2770 us, 2400
-    return backward_of<T, 256, 1, 64, 4, 1, KEYS>(direct);
+    // one wave a SIMD: the gradients of 8192 tokens, 16 heads of 192 on 4: 2665 us, 1660; of 256: 2770 (binary16 4055), 2417 (2556)
+    if (dim <= 192) return backward_of<T, 192, 1, 32, 4, 2, KEYS>(direct);
+    return backward_of<T, 256, 1, 32, 4, 2, KEYS>(direct);
   } else {
     if (dim <= 64) return backward_of<T, 64, 1, 32, 4, 2, KEYS>(direct);
     if (dim <= 96) return backward_of<T, 96, 1, 32, 4, 1, KEYS>(direct);
