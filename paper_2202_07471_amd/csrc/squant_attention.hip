@@ -221,9 +221,10 @@ struct BackwardPlan {
 };
 BackwardPlan plan_backward(const squant_packed_t& p, int type, bool queries_direct, bool keys_direct) {
   BackwardPlan b{};
-  b.queries = (type == SQUANT_W_F32 ? prompt_queries_f32 : type == SQUANT_W_F16 ? prompt_queries_f16 : prompt_queries_bf16)(p.head_dim, keys_direct);
-  b.keys = (type == SQUANT_W_F32 ? prompt_keys_f32 : type == SQUANT_W_F16 ? prompt_keys_f16 : prompt_keys_bf16)(p.head_dim, queries_direct);
   const PromptArgs a = prompt_args(p);
+  const auto many = [](const Packed& own, int32_t heads, int most) { return tiles_bound(own.rows, 1, 128, own.count) * heads > most; };
+  b.queries = (type == SQUANT_W_F32 ? prompt_queries_f32 : type == SQUANT_W_F16 ? prompt_queries_f16 : prompt_queries_bf16)(p.head_dim, keys_direct, many(a.queries, p.heads, 2 * kRunAtOnce));
+  b.keys = (type == SQUANT_W_F32 ? prompt_keys_f32 : type == SQUANT_W_F16 ? prompt_keys_f16 : prompt_keys_bf16)(p.head_dim, queries_direct, many(a.keys, p.kv_heads, kRunAtOnce));
   b.q_groups = prompt_groups(a.queries, b.queries, p.heads), b.k_groups = prompt_groups(a.keys, b.keys, p.kv_heads);
   b.q_splits = type == SQUANT_W_F32 ? walk_splits(b.q_groups, p.k_rows, p, 1, b.queries.walked, kMostPieces) : 1;
   b.k_splits = walk_splits(b.k_groups, p.q_rows, p, a.group, b.keys.walked, kMostPieces);

@@ -4,7 +4,7 @@
 namespace squant {
 namespace att {
 
-PromptKernel prompt_keys_f32(int dim, bool direct) { return backward_for<float, true>(dim, direct); }
+PromptKernel prompt_keys_f32(int dim, bool direct, bool many) { return backward_for<float, true>(dim, direct, many); }
 
 }  // namespace att
 }  // namespace squant

@@ -872,22 +872,23 @@ template <class T, int DP, int OT, int BS, int WAVES, int OCCUPANCY, bool KEYS> 
           16 * WAVES * OT, BS, 64 * WAVES, (size_t)4 * BS * TileOf<T, DP>::kRowBytes + 16 * BS};
 }
 
-// By the head's size; `direct`: what is walked over lies at multiples of 16 bytes.
+// By the head's size; `direct`: what is walked over lies at multiples of 16 bytes; `many`: tiles of 128 rows are
+// more than run at once (of queries, whose walks are short, twice that).
 PromptKernel prompt_forward_bf16(int dim, bool direct);
 PromptKernel prompt_forward_f16(int dim, bool direct);
 PromptKernel prompt_forward_f32(int dim, bool direct);
-PromptKernel prompt_keys_bf16(int dim, bool direct);
-PromptKernel prompt_keys_f16(int dim, bool direct);
-PromptKernel prompt_keys_f32(int dim, bool direct);
-PromptKernel prompt_queries_bf16(int dim, bool direct);
-PromptKernel prompt_queries_f16(int dim, bool direct);
-PromptKernel prompt_queries_f32(int dim, bool direct);
+PromptKernel prompt_keys_bf16(int dim, bool direct, bool many);
+PromptKernel prompt_keys_f16(int dim, bool direct, bool many);
+PromptKernel prompt_keys_f32(int dim, bool direct, bool many);
+PromptKernel prompt_queries_bf16(int dim, bool direct, bool many);
+PromptKernel prompt_queries_f16(int dim, bool direct, bool many);
+PromptKernel prompt_queries_f32(int dim, bool direct, bool many);
 prompt_t prompt_join_kernel(int type, bool keys);
 prompt_t prompt_join_forward_kernel(int type);
 
 template <class T> PromptKernel forward_for(int dim, bool direct) {
   if constexpr (sizeof(T) == 2) {
-    if (dim <= 64) return forward_of<T, 64, 2, 64, 4, 2>(direct);
+    if (dim <= 64) return forward_of<T, 64, 2, 64, 4, 3>(direct);  // two waves a SIMD: 8192 tokens, 32 heads: 419 us, 397
     if (dim <= 96) return forward_of<T, 96, 2, 64, 4, 2>(direct);
     if (dim <= 128) return forward_of<T, 128, 2, 64, 4, 2>(direct);
     // 16 rows a wave: 8192 tokens, 16 heads of 192 on 4: 545 us, 488; of 256: 750, 580
@@ -901,9 +902,13 @@ template <class T> PromptKernel forward_for(int dim, bool direct) {
     return forward_of<T, 256, 1, 32, 4, 1>(direct);
   }
 }
-template <class T, bool KEYS> PromptKernel backward_for(int dim, bool direct) {
+template <class T, bool KEYS> PromptKernel backward_for(int dim, bool direct, bool many) {
   if constexpr (sizeof(T) == 2) {
+    // 32 rows a wave where that leaves enough workgroups: gradients of 8192 tokens, 32 heads of 64 on 8: 1236 us, 1134 (binary16 1385,
+    // 1234); of 96: 1815, 1498 (2049, 1677); of 2048 tokens 127, 145 and 186, 201
+    if (dim <= 64 && many) return backward_of<T, 64, 2, 64, 4, 2, KEYS>(direct);
     if (dim <= 64) return backward_of<T, 64, 1, 64, 4, 2, KEYS>(direct);
+    if (dim <= 96 && many) return backward_of<T, 96, 2, 32, 4, 2, KEYS>(direct);
     if (dim <= 96) return backward_of<T, 96, 1, 64, 4, 2, KEYS>(direct);
     if (dim <= 128) return backward_of<T, 128, 1, 64, 4, 2, KEYS>(direct);
     // one wave a SIMD: the gradients of 8192 tokens, 16 heads of 192 on 4: 2665 us, 1660; of 256: 2770 (binary16 4055), 2417 (2556)

@@ -470,3 +470,11 @@ def test_far_rows(sq, dtype):
     far = torch.empty(3 * (step + 8), dtype=dtype, device="cuda").view(3, -1)[:, :heads * dim].unflatten(1, (heads, dim))
     with pytest.raises(sq.SQuantError):
         sq.squant_attention(far, k[:3], v[:3])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("dim", [40, 64, 72, 96])
+def test_many_heads(sq, dim, dtype):
+    """Gradients by 32 rows a wave."""
+    check(sq, 42, [300, 200, 65], [280, 200, 90], 160, 80, dim, dtype, True, q_pad=3)
+    check(sq, 43, [130, 257], [257, 140], 288, 144, dim, dtype, False, k_pad=5)
