@@ -274,7 +274,7 @@ int squant_cache_attention(const squant_heads_t* h_q, squant_wtype_t type, int64
   a.q = strided(h_q, rows), a.out = strided(h_out, rows);
   a.type = (int)type, a.heads = heads, a.group = heads / c.heads;
   a.splits = (int32_t)s.splits, a.chunk = (int32_t)s.chunk;
-  a.scale = std::max(scale * kLog2E, 1.4e-45f);
+  a.scale = scale * kLog2E;
   if (s.splits > 1) a.stats = (float2*)d_workspace, a.partial = (float*)((char*)d_workspace + s.stats_bytes);
   const int ng = c.head_dim / kGroup;
   const auto of = c.format == SQUANT_OUT_INT4

@@ -206,7 +206,7 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
   page_ids(t0, ids);
 
   half8 q[RT][PL][NG];
-  float factor[RT];
+  int q_e[RT];  // queries are held times 2^q_e
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     float x[NG][8];
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
     top = max(top, (uint32_t)__shfl_xor((int)top, 32));
     const int e = lin::row_exponent(top);
     const float up = power_of_two(e);
-    factor[rt] = a.scale * power_of_two(-e) * poison;
+    q_e[rt] = e;
 #pragma unroll
     for (int i = 0; i < NG; ++i)
 #pragma unroll
@@ -448,7 +448,10 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
     half8 p[RT][PL];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      const float f = factor[rt] * power_of_two(-key_e);
+      // Both powers at once: where keys are zeros so far and queries small, or scale is 0, they leave binary32.  Never 0 itself: a
+      // hidden score's minus infinity stays one, and scores times 2^-149 are nothing.
+      float f = ldexpf(a.scale * poison, -(q_e[rt] + key_e));
+      f = f == 0.0f ? 0x1p-149f : f;
       float m = -kInfinity;
 #pragma unroll
       for (int j = 0; j < 8; ++j) m = fmaxf(m, s[j >> 2][rt][j & 3]);

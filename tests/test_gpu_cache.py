@@ -472,3 +472,31 @@ def test_two_streams_at_once(sq):
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(g, work[i][4]) for g in got[i])
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("scale", [0.0, 1e-45, 1e-38, 1e-3, 1.0])
+def test_scales_of_scores(sq, scale, dtype, bits):
+    """0, subnormal and ordinary ones; lengths that end inside a block, and a sequence that is split."""
+    attend(sq, 71, [1, 33, 70, 1100], [1, 1, 1, 1], 8, 2, 64, 16, dtype, bits, one_each=True, scale=scale)
+    attend(sq, 72, [45, 3, 130], [4, 3, 0], 4, 4, 96, 24, dtype, bits, pad=2, scale=scale)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("power", [-7, -14, -100])
+def test_zero_keys_and_small_queries(sq, power, dtype, bits):
+    """Keys of zero scales, all of a sequence's or its first ones, and queries whose products with them leave binary32: the mean of
+    the values, or the later keys' softmax."""
+    gen = torch.Generator().manual_seed(73)
+    lengths, page = [1, 40, 75, 700], 16
+    pages, table = layout(gen, lengths, page)
+    cache, host = filled(sq, gen, pages, 2, page, 128, bits)
+    for b, zeros in enumerate((1, 40, 64, 640)):
+        p, s = slots_of(table, page, b, 0, zeros)
+        host[1][p, :, s] = 0.0
+    cache = sq.QuantizedCache(*(t.cuda() for t in host))
+    q = (torch.randn(4, 8, 128, generator=gen) * 2.0 ** power).to(dtype)
+    out = sq.squant_cache_attention(q.cuda(), cache, table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda())
+    check(out, q, host, table, lengths, [1] * 4, page, dtype, bits, 128 ** -0.5)
