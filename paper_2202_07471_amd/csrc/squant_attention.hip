@@ -1,4 +1,5 @@
 // Host side of attention and of the quantised cache: argument checks, how far a sequence is split, launches.
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -18,6 +19,9 @@ using namespace squant::att;
 constexpr int64_t kMost = 0x7fffffffLL, kMostTokens = 1 << 30;  // of a table
 // Elements between rows and between heads: a tile's rows are within 32 bits of bytes of each other, a buffer's within 64.
 constexpr int64_t kFarRow = (int64_t)1 << 22, kFarHead = (int64_t)1 << 31;
+
+// A scale times log2(e) stays a number: a score of 0 times infinity would be none.
+float base2(float scale) { return std::min(scale * kLog2E, FLT_MAX); }
 
 int element_bytes(int type) { return type == SQUANT_W_F32 ? 4 : 2; }
 bool misaligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
@@ -167,7 +171,7 @@ PromptArgs prompt_args(const squant_packed_t& p) {
   a.keys = Packed{p.k_starts, p.sequences, (int32_t)p.k_rows, false};
   a.heads = p.heads, a.kv_heads = p.kv_heads, a.group = p.heads / p.kv_heads, a.dim = p.head_dim;
   a.causal = p.causal, a.scale = p.scale;
-  a.scale2 = std::max(p.scale * kLog2E, 1.4e-45f);
+  a.scale2 = std::max(base2(p.scale), 1.4e-45f);
   return a;
 }
 int64_t prompt_groups(const Packed& p, const PromptKernel& k, int32_t heads) {
@@ -274,7 +278,7 @@ int squant_cache_attention(const squant_heads_t* h_q, squant_wtype_t type, int64
   a.q = strided(h_q, rows), a.out = strided(h_out, rows);
   a.type = (int)type, a.heads = heads, a.group = heads / c.heads;
   a.splits = (int32_t)s.splits, a.chunk = (int32_t)s.chunk;
-  a.scale = scale * kLog2E;
+  a.scale = base2(scale);
   if (s.splits > 1) a.stats = (float2*)d_workspace, a.partial = (float*)((char*)d_workspace + s.stats_bytes);
   const int ng = c.head_dim / kGroup;
   const auto of = c.format == SQUANT_OUT_INT4

@@ -500,3 +500,24 @@ def test_zero_keys_and_small_queries(sq, power, dtype, bits):
     q = (torch.randn(4, 8, 128, generator=gen) * 2.0 ** power).to(dtype)
     out = sq.squant_cache_attention(q.cuda(), cache, table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda())
     check(out, q, host, table, lengths, [1] * 4, page, dtype, bits, 128 ** -0.5)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_largest_scale_of_scores(sq, dtype):
+    """A scale whose product with log2(e) leaves binary32: scores of 0 stay 0, over a cache and over prompts."""
+    scale = torch.finfo(F32).max
+    gen = torch.Generator().manual_seed(74)
+    pages, table = layout(gen, [37], 16)
+    cache, host = filled(sq, gen, pages, 2, 16, 64, 4)
+    q = torch.zeros(1, 4, 64, dtype=dtype)
+    out = sq.squant_cache_attention(q.cuda(), cache, table.cuda(), torch.tensor([37], dtype=torch.int32).cuda(), scale=scale)
+    check(out, q, host, table, [37], [1], 16, dtype, 4, scale)
+    v = torch.randn(37, 2, 64, generator=gen).to(dtype)
+    out, lse = sq.squant_attention(q.cuda(), v.cuda(), v.cuda(), torch.tensor([0, 1], dtype=torch.int32).cuda(),
+                                   torch.tensor([0, 37], dtype=torch.int32).cuda(), scale=scale)
+    ref = attention64(q.double(), v.double(), v.double(), scale, True, dtype)
+    close(out, ref, "out")
+    close(lse, ref, "lse")
+    for got in sq.squant_attention_backward(torch.zeros_like(out), q.cuda(), v.cuda(), v.cuda(), out, lse, torch.tensor([0, 1], dtype=torch.int32).cuda(),
+                                            torch.tensor([0, 37], dtype=torch.int32).cuda(), scale=scale):
+        assert (got == 0).all()
