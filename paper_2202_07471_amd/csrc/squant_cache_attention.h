@@ -356,9 +356,17 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
     if (lanes_where(top >= too_large(key_e))) {
       uint32_t m = 0;
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
+      for (int tt = 0; tt < 2; ++tt) {
+        bool none = false;
 #pragma unroll
-        for (int k = 0; k < L::kKeyScales; ++k) m = max(m, finite_bits(from_bfloat16(key_scale[tt][k])));
+        for (int k = 0; k < L::kKeyScales; ++k) {
+          none |= (key_scale[tt][k] & 0x7fffu) >= 0x7f80u;
+          m = max(m, finite_bits(from_bfloat16(key_scale[tt][k])));
+        }
+        // four lanes, 16 apart, share a token.  An infinite scale's products may all be minus infinity: a weight of 0, unless marked
+        const uint64_t odd = lanes_where(none), pairs = odd | odd >> 32;
+        nan_tokens |= (uint32_t)((pairs | pairs >> 16) & 0xffffu) << (16 * tt);
+      }
       key_e = min(key_e, __builtin_amdgcn_readfirstlane(scale_exponent(over_lanes_max(m))));
     }
     float4v s[2][RT];

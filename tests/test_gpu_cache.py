@@ -521,3 +521,36 @@ def test_largest_scale_of_scores(sq, dtype):
     for got in sq.squant_attention_backward(torch.zeros_like(out), q.cuda(), v.cuda(), v.cuda(), out, lse, torch.tensor([0, 1], dtype=torch.int32).cuda(),
                                             torch.tensor([0, 37], dtype=torch.int32).cuda(), scale=scale):
         assert (got == 0).all()
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("which", ["key", "value"])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_one_broken_scale(sq, value, which, dtype, bits):
+    """A token with one scale of its keys, or of its values, that is no number: rows that see it are NaN throughout, also where all products
+    with an infinite key are minus infinity; others are as they are."""
+    lengths, new, page = [45, 300], [4, 2], 16
+    gen = torch.Generator().manual_seed(75)
+    pages, table = layout(gen, lengths, page)
+    cache, host = filled(sq, gen, pages, 2, page, 64, bits)
+    p, s = slots_of(table, page, 0, 43, 44)
+    if bits == 4:
+        host[0][p, :, s] = 0xdd  # -3, -3
+    else:
+        host[0][p, :, s] = -3
+    cache = sq.QuantizedCache(*(t.cuda() for t in host))
+    q = (torch.randn(6, 8, 64, generator=gen).abs() + 0.5).to(dtype)
+    args = (table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), starts_of(new).cuda())
+    out = sq.squant_cache_attention(q.cuda(), cache, *args)
+    check(out, q, host, table, lengths, new, page, dtype, bits, 0.125)
+    scales = cache.key_scales if which == "key" else cache.value_scales
+    for heads, group in ((slice(0, 1), 1), (slice(0, 2), 0)):
+        scales[p.cuda(), heads, s.cuda(), group] = value
+        again = sq.squant_cache_attention(q.cuda(), cache, *args)
+        seen = slice(0, 4 * heads.stop)  # query heads of those key heads
+        assert again[2:4, seen].isnan().all()
+        assert torch.equal(again[2:4, 4 * heads.stop:], out[2:4, 4 * heads.stop:])
+        close_rows = again.clone()
+        close_rows[2:4] = out[2:4]
+        check(close_rows, q, host, table, lengths, new, page, dtype, bits, 0.125)
