@@ -173,7 +173,7 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
 
   // this lane's columns of the scores: rows of the queries
   int row[RT], qhead[RT], seen[RT];
-  bool live[RT];
+  bool live[RT], beyond[RT];  // beyond: it sees tokens past the table, and is NaN
   int least_seen = 0x7fffffff;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
@@ -182,12 +182,13 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
     live[rt] = r < count * a.group;
     row[rt] = row0 + (live[rt] ? token : 0);
     qhead[rt] = head * a.group + (live[rt] ? r - token * a.group : 0);
-    seen[rt] = live[rt] ? min(max(said - count + token + 1, 0), end) : 0;
+    const int upto = live[rt] ? said - count + token + 1 : 0;
+    beyond[rt] = upto > capacity;
+    seen[rt] = min(max(upto, 0), end);
     if (live[rt]) least_seen = min(least_seen, seen[rt]);
   }
   // rows of a tile see no less than its first
   least_seen = min(__builtin_amdgcn_readfirstlane(least_seen), end);
-  const float poison = said > length ? __builtin_nanf("") : 1.0f;
 
   // where a block's tokens are: on its way before the queries
   const uint32_t head_row = (uint32_t)head * (uint32_t)c.page_size;
@@ -322,7 +323,7 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
     for (int rt = 0; rt < RT; ++rt) o[f][rt] = float4v{0, 0, 0, 0};
   float largest[RT], sum[RT];
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) largest[rt] = -kInfinity, sum[rt] = 0.0f;
+  for (int rt = 0; rt < RT; ++rt) largest[rt] = -kInfinity, sum[rt] = beyond[rt] ? __builtin_nanf("") : 0.0f;
   int key_e = 126, value_e = 126;
   const Magic magic;
 
@@ -458,7 +459,7 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
     for (int rt = 0; rt < RT; ++rt) {
       // Both powers at once: where keys are zeros so far and queries small, or scale is 0, they leave binary32.  Never 0 itself: a
       // hidden score's minus infinity stays one, and scores times 2^-149 are nothing.
-      float f = ldexpf(a.scale * poison, -(q_e[rt] + key_e));
+      float f = ldexpf(a.scale, -(q_e[rt] + key_e));
       f = f == 0.0f ? 0x1p-149f : f;
       float m = -kInfinity;
 #pragma unroll

@@ -554,3 +554,23 @@ def test_one_broken_scale(sq, value, which, dtype, bits):
         close_rows = again.clone()
         close_rows[2:4] = out[2:4]
         check(close_rows, q, host, table, lengths, new, page, dtype, bits, 0.125)
+
+
+@pytest.mark.parametrize("page,width", [(16, 3), (7, 5), (16, 0), (16, 200)])
+def test_rows_that_see_beyond_the_table(sq, page, width):
+    """Rows of a sequence that is longer than its table are NaN where they see a token beyond it, and only there; rows that see nothing are 0."""
+    gen = torch.Generator().manual_seed(76)
+    capacity = page * width
+    pages, table = layout(gen, [max(capacity, 1)], page)
+    table = table[:, :width].contiguous()
+    cache, host = filled(sq, gen, pages, 2, page, 64, 4)
+    for new, beyond in ((1, 1), (5, 2), (5, 5), (5, 9), (40, 3)):
+        length = capacity + beyond
+        q = torch.randn(new, 4, 64, generator=gen).to(BF16)
+        out = sq.squant_cache_attention(q.cuda(), cache, table.cuda(), torch.tensor([length], dtype=torch.int32).cuda(), starts_of([new]).cuda())
+        whole = max(new - beyond, 0)  # rows that end within the table
+        assert out[whole:].isnan().all()
+        nothing = min(max(new - length, 0), whole)
+        assert (out[:nothing] == 0).all()
+        if whole > nothing:
+            check(out[nothing:whole], q[nothing:whole], host, table, [capacity], [whole - nothing], page, BF16, 4, 0.125)
