@@ -150,6 +150,21 @@ __device__ __forceinline__ float over_groups_sum(float v) {
   return over_groups(v, [](float x, float y) { return x + y; });
 }
 
+template <class T> struct Eight { T t[8]; };
+template <class T> __device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
+  const Eight<T> e = load_any<Eight<T>>(p);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (float)e.t[i];
+}
+
+// Weights are 2^(score * factor - largest) in one operation, whose product keeps all of its bits; the largest's were rounded.  From
+// scores of 2^20 on that difference is no longer small against 1 (at 2^25 a weight leaves binary16, at 2^31 binary32): such a
+// wave takes the largest off first, so that its own weight is exact.
+__device__ __forceinline__ bool far_scores(float largest) {
+  const float m = fabsf(largest);
+  return lanes_where(m > 0x1p20f && m < __builtin_inff()) != 0;
+}
+
 template <bool B> struct Constant { static constexpr bool value = B; };
 
 constexpr float kInfinity = __builtin_inff();

@@ -98,12 +98,6 @@ struct Piece {
 };
 constexpr int kAtOnce = 4;  // pieces of a thread on their way
 
-template <class T> struct Eight { T t[8]; };
-template <class T> __device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
-  const Eight<T> e = load_any<Eight<T>>(p);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = (float)e.t[i];
-}
 // Past the caches: what is read back is more than they hold, and kept there it goes to memory in pieces (66815 tokens of 8 heads of 128 in 4 bits
 // to bfloat16 106 us, 66 like this).
 typedef uint32_t stream4v __attribute__((ext_vector_type(4), aligned(2)));

@@ -475,7 +475,13 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
           for (int i = 0; i < 4; ++i) o[f2][rt][i] *= shrink;
         largest[rt] = most;
       }
-      const float base = largest[rt] == -kInfinity ? 0.0f : kWeightUnit - largest[rt];
+      float base = largest[rt] == -kInfinity ? 0.0f : kWeightUnit - largest[rt];
+      if (far_scores(largest[rt])) {
+        const float from = largest[rt] == -kInfinity ? 0.0f : largest[rt];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j >> 2][rt][j & 3] = s[j >> 2][rt][j & 3] * f - from;
+        f = 1.0f, base = kWeightUnit;
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float w = exp2_fast(__builtin_fmaf(s[j >> 2][rt][j & 3], f, base));

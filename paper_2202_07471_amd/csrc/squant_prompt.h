@@ -323,6 +323,86 @@ __device__ __forceinline__ PromptTile find_walk(const Packed& own, const Packed&
   return t;
 }
 
+// One row against keys `from` to `to` - 1 by a wave, the largest score taken off before it is multiplied: for rows with far scores, which are
+// seldom.  A lane for each key, then for each element.
+template <class T, int DP>
+__device__ __forceinline__ void far_row(const PromptArgs& a, int64_t q_row, int head, int kv_head, int64_t k0, int from, int to) {
+  constexpr int E = (DP + 63) / 64;
+  const int lane = (int)threadIdx.x & 63;
+  const T* q = element<T>(a.q, q_row, head);
+  auto score = [&](int t) {
+    const T* k = element<T>(a.k, k0 + t, kv_head);
+    float s = 0.0f;
+#pragma unroll 4
+    for (int d = 0; d < a.dim; d += 8) {
+      float x[8], y[8];
+      load8(q + d, x);
+      load8(k + d, y);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s = __builtin_fmaf(x[i], y[i], s);
+    }
+    return s;
+  };
+  float top = -kInfinity;
+#pragma unroll 1
+  for (int t = from + lane; t < to; t += 64) top = fmaxf(top, score(t));
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+  float total = 0.0f, sum[E] = {};
+#pragma unroll 1
+  for (int t0 = from; t0 < to; t0 += 64) {
+    const float w = t0 + lane < to ? exp2_fast((score(t0 + lane) - top) * a.scale2) : 0.0f;
+    total += w;
+    const int count = min(64, to - t0);
+#pragma unroll 8
+    for (int i = 0; i < count; ++i) {
+      const T* v = element<T>(a.v, k0 + t0 + i, kv_head);
+      const float one = __shfl(w, i);
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (lane + 64 * e < a.dim) sum[e] = __builtin_fmaf(one, (float)v[lane + 64 * e], sum[e]);
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o);
+  const float largest = top * a.scale2;
+  if (a.splits > 1) {
+    const float unit = weight_unit<T>() != 0.0f ? 128.0f : 1.0f;
+    const int64_t at = ((int64_t)blockIdx.y * a.queries.rows + q_row) * a.heads + head;
+    if (lane == 0) a.stats[at] = make_float2(largest, total * unit);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (lane + 64 * e < a.dim) a.partial[at * a.dim + lane + 64 * e] = sum[e] * unit;
+    return;
+  }
+  T* o = element<T>(a.o, q_row, head);
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (lane + 64 * e < a.dim) o[lane + 64 * e] = (T)(total == 0.0f ? 0.0f : sum[e] / total);
+  if (a.lse && lane == 0) a.lse[(int64_t)head * a.queries.rows + q_row] = total == 0.0f ? -kInfinity : (largest + __builtin_amdgcn_logf(total)) * kLn2;
+}
+
+// All rows of a wave.  The arguments and the tile are found anew, from a pointer that the compiler does not know: kept through the loops before,
+// they would put others' registers into memory.
+template <class T, int DP, int QT, int BK, int WAVES> __device__ __forceinline__ void far_rows() {
+  typedef const __attribute__((address_space(4))) PromptArgs* args_t;
+  args_t p = (args_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  const PromptArgs& a = *(const PromptArgs*)p;
+  constexpr int kRows = 16 * WAVES * QT;
+  const int turn = (int)(blockIdx.x % (uint32_t)a.heads), kv_head = turn % a.kv_heads, head = kv_head * a.group + turn / a.kv_heads;
+  const PromptTile tile = find_walk(a.queries, a.keys, a.by_length, false, (int)(blockIdx.x / (uint32_t)a.heads), kRows);
+  const int first = (tile.tiles - 1 - tile.index) * kRows, rows = tile.length, keys = tile.walk_length;
+  auto sees = [&](int r) { return a.causal ? min(max(r + keys - rows + 1, 0), keys) : keys; };
+  const int all_steps = (sees(min(first + kRows, rows) - 1) + BK - 1) / BK;
+  int begin = 0, steps = all_steps;
+  if (a.splits > 1) begin = piece_of(all_steps, blockIdx.y, a.splits), steps = piece_of(all_steps, blockIdx.y + 1, a.splits);
+  const int mine = first + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 16 * QT;
+#pragma unroll 1
+  for (int r = mine; r < min(mine + 16 * QT, rows); ++r)
+    far_row<T, DP>(a, tile.start + r, head, kv_head, tile.walk_start, begin * BK, min(sees(r), steps * BK));
+}
+
 template <class T, int DP, int QT, int BK, int WAVES, int OCCUPANCY, bool DIRECT>
 __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptArgs a) {
   typedef typename MatrixOf<T>::type M;
@@ -389,6 +469,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
   }
   __syncthreads();
 
+  bool far = false;  // whether a row of the wave met far scores
   // Keys from step j on that the lane's row t sees, made anew: kept, they would be put into memory.  Rows past the last hold zeros.
   auto seen_from = [&](int j, int t) {
     const int left = keys - j * BK;
@@ -447,6 +528,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[t][f][i] *= shrink;
         largest[t] = more;
+        far |= far_scores(more);
       }
       const float base = largest[t] == -kInfinity ? 0.0f : weight_unit<T>() - largest[t];
 #pragma unroll
@@ -505,6 +587,11 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
     step(j, Constant<true>{});
     if (j + 1 < steps) land(j + 1);
     __syncthreads();
+  }
+  if (__builtin_expect(far, false)) {
+    // whatever that takes: a branch in the loops costs all others 1 to 5 %
+    far_rows<T, DP, QT, BK, WAVES>();
+    return;
   }
 #pragma unroll
   for (int t = 0; t < QT; ++t) {

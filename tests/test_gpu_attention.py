@@ -478,3 +478,27 @@ def test_many_heads(sq, dim, dtype):
     """Gradients by 32 rows a wave."""
     check(sq, 42, [300, 200, 65], [280, 200, 90], 160, 80, dim, dtype, True, q_pad=3)
     check(sq, 43, [130, 257], [257, 140], 288, 144, dim, dtype, False, k_pad=5)
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("dtype,power", [(BF16, 24), (BF16, 60), (F16, 24), (F32, 24), (F32, 60)])
+@pytest.mark.parametrize("rows,keys", [(100, 100), (3, 900)])
+def test_scores_of_any_size(sq, rows, keys, dtype, power, sign):
+    """Scores so far apart that a row's output is the value of its largest one, where a product's rounding is more than a weight's exponent."""
+    gen = torch.Generator().manual_seed(81)
+    count = torch.randperm(keys, generator=gen) % 97 + 1  # scores are multiples of 2^power / 8; equal ones have equal values
+    half = power // 2
+    q = torch.zeros(rows, 2, 64)
+    k, v = torch.zeros(keys, 1, 64), torch.randn(100, 1, 64, generator=gen)[count]
+    q[..., 0], k[..., 0] = 2.0 ** (power - half + 2), sign * count[:, None].float() * 2.0 ** (half - 3)
+    q, k, v = (t.to(dtype) for t in (q, k, v))
+    ints = dict(dtype=torch.int32, device="cuda")
+    out, lse = sq.squant_attention(q.cuda(), k.cuda(), v.cuda(), torch.tensor([0, rows], **ints), torch.tensor([0, keys], **ints))
+    score = sign * count.double() * 2.0 ** (power - 4)
+    for i in range(rows):
+        best = score[:keys - rows + i + 1].argmax()
+        # equal scores' weights and their sum: rounded once each, to the element type and in binary32
+        tol = (2.0 ** -20 + (2 if dtype != F32 else 0) * torch.finfo(dtype).eps / 2 + torch.finfo(dtype).eps / 2) * v[best].double().abs()
+        assert ((out[i].cpu().double() - v[best].double()).abs() <= tol).all(), i
+        want = score[best] + (score[:keys - rows + i + 1] == score[best]).double().sum().log()
+        assert ((lse[:, i].cpu().double() - want).abs() <= 2.0 ** -21 * want.abs()).all()

@@ -574,3 +574,34 @@ def test_rows_that_see_beyond_the_table(sq, page, width):
         assert (out[:nothing] == 0).all()
         if whole > nothing:
             check(out[nothing:whole], q[nothing:whole], host, table, [capacity], [whole - nothing], page, BF16, 4, 0.125)
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype,power", [(BF16, 24), (BF16, 60), (F16, 24), (F32, 24), (F32, 60)])
+def test_scores_of_any_size(sq, dtype, power, bits, sign):
+    """Scores so far apart that a row's output is the value of its largest one, where a product's rounding is more than a weight's exponent."""
+    gen = torch.Generator().manual_seed(78)
+    lengths, new, page, half = [70, 1100], [3, 1], 16, power // 2
+    pages, table = layout(gen, lengths, page)
+    cache, host = filled(sq, gen, pages, 1, page, 64, bits)
+    host[0].zero_()
+    host[0][..., 0] = 1
+    counts = []
+    for b, m in enumerate(lengths):
+        p, s = slots_of(table, page, b, 0, m)
+        counts.append(torch.randperm(m, generator=gen) % 97 + 1)
+        host[1][p, :, s, 0] = (sign * counts[-1].float() * 2.0 ** (half - 3)).to(BF16)[:, None]
+        for t in host[2:]:
+            t[p, :, s] = torch.stack([t[p[counts[-1] == c][0], :, s[counts[-1] == c][0]] for c in counts[-1]])  # equal ones have equal values
+    cache = sq.QuantizedCache(*(t.cuda() for t in host))
+    q = torch.zeros(4, 2, 64, dtype=dtype)
+    q[..., 0] = 2.0 ** (power - half + 2)
+    out = sq.squant_cache_attention(q.cuda(), cache, table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), starts_of(new).cuda())
+    for r, (b, sees) in enumerate(((0, 68), (0, 69), (0, 70), (1, 1100))):
+        p, s = slots_of(table, page, b, 0, sees)
+        best = (sign * counts[b][:sees]).argmax()
+        v = values(host[2][p, :, s], host[3][p, :, s])[best]
+        # elements of 11 bits (a remainder in the other types); weights and their sum; the output
+        tol = (2.0 ** -20 + 2.0 ** -11 * 2 + torch.finfo(dtype).eps / 2) * v.abs()
+        assert ((out[r].cpu().double() - v).abs() <= tol).all(), r
