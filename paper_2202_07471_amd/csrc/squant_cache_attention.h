@@ -557,14 +557,15 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
     const float base = m == -kInfinity ? 0.0f : m;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) l += stats[(w * 2 + 1) * TR + 16 * rt + n] * exp2_fast(stats[w * 2 * TR + 16 * rt + n] - base);
-    total[rt] = l, most[rt] = m;
+    // without the weights' unit from here on: with it, values from 2^113 on left binary32
+    total[rt] = l * 0x1p-14f, most[rt] = m;
     const float mine = exp2_fast(largest[rt] - base);
 #pragma unroll
     for (int f = 0; f < F; ++f)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         // odd elements of 4-bit codes are held times 16
-        o[f][rt][i] = ldexpf(o[f][rt][i] * mine, -value_e - (FMT == SQUANT_OUT_INT4 && (f & 1) ? 4 : 0));
+        o[f][rt][i] = ldexpf(o[f][rt][i] * mine, -value_e - (int)kWeightUnit - (FMT == SQUANT_OUT_INT4 && (f & 1) ? 4 : 0));
   }
   float4v* piles = reinterpret_cast<float4v*>(pile);
 #pragma unroll

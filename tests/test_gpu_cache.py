@@ -605,3 +605,24 @@ def test_scores_of_any_size(sq, dtype, power, bits, sign):
         # elements of 11 bits (a remainder in the other types); weights and their sum; the output
         tol = (2.0 ** -20 + 2.0 ** -11 * 2 + torch.finfo(dtype).eps / 2) * v.abs()
         assert ((out[r].cpu().double() - v).abs() <= tol).all(), r
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("power", [108, 118, 121])
+def test_large_values(sq, power, dtype, bits):
+    """Values whose products with the weights' unit leave binary32, and their means do not."""
+    gen = torch.Generator().manual_seed(79)
+    lengths, new, page = [7, 600], [2, 1], 16
+    pages, table = layout(gen, lengths, page)
+    cache, host = filled(sq, gen, pages, 2, page, 64, bits)
+    host[1].mul_(2.0 ** -12)  # scores next to each other
+    host[3].fill_(2.0 ** (power - (0 if bits == 4 else 4)))  # 8 bits: codes to 127
+    if power > 118:  # the sum of a sequence's values would leave binary32 too
+        lengths = [7, 12]
+        table = table[:, :1].contiguous()
+    cache = sq.QuantizedCache(*(t.cuda() for t in host))
+    q = torch.randn(3, 4, 64, generator=gen).to(dtype)
+    out = sq.squant_cache_attention(q.cuda(), cache, table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), starts_of(new).cuda())
+    check(out, q, host, table, lengths, new, page, dtype, bits, 0.125)
+    assert out.isfinite().all()
