@@ -124,6 +124,96 @@ __device__ __forceinline__ uint32_t too_large(int e) { return min((uint32_t)(9 -
 // 32 rows at three (eleven sequences' drafts 36 us, 61).
 constexpr int cache_occupancy(int ng, int rt) { return ng <= 2 && rt == 1 ? 3 : 2; }
 
+// One row by a wave, in binary32 and token by token: for tiles whose rows cannot share exponents, which are seldom.  A lane for each token, then
+// for each element.
+template <class T, int FMT, int NG>
+__device__ __forceinline__ void row_alone(const CacheAttentionArgs& a, int seq, int row, int qhead, int head, int split, int begin, int upto, bool beyond) {
+  constexpr int W = FMT == SQUANT_OUT_INT4 ? 1 : 2, D = NG * kGroup, E = (D + 63) / 64;
+  const Cache& c = a.cache;
+  const int lane = (int)threadIdx.x & 63;
+  const T* q = element<T>(a.q, row, qhead);
+  // the token's row of the cache, -1: its page is none
+  auto where = [&](int t) -> int64_t {
+    const int page = c.page_of(t);
+    const int32_t r = c.row_of(t, page, c.table_at(seq, page));
+    return r < 0 ? -1 : (int64_t)r + (int64_t)head * c.page_size;
+  };
+  auto scale_of = [&](int tensor, int64_t r, int group) {
+    const uint16_t bits = r < 0 ? (uint16_t)0x7fc0 : c.scales[tensor][r * NG + group];
+    return (bits & 0x7fffu) < 0x7f80u ? from_bfloat16(bits) : __builtin_nanf("");
+  };
+  auto score = [&](int t) {
+    const int64_t r = where(t);
+    float s = 0.0f;
+#pragma unroll 1
+    for (int i = 0; i < 4 * NG; ++i) {
+      uint32_t words[W];
+#pragma unroll
+      for (int w = 0; w < W; ++w) words[w] = *reinterpret_cast<const uint32_t*>(c.codes[0] + max(r, (int64_t)0) * (D / 8 * 4 * W) + (i * W + w) * 4);
+      float x[8], y[8];
+      load8(q + 8 * i, x);
+      decode<FMT>(words, scale_of(0, r, i >> 2), y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = __builtin_fmaf(x[e], y[e], s);
+    }
+    return s;
+  };
+  float top = -kInfinity;
+#pragma unroll 1
+  for (int t = begin + lane; t < upto; t += 64) top = fmaxf(top, score(t));
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+  float total = beyond ? __builtin_nanf("") : 0.0f, sum[E] = {};
+#pragma unroll 1
+  for (int t0 = begin; t0 < upto; t0 += 64) {
+    const float w = t0 + lane < upto ? exp2_fast((score(t0 + lane) - top) * a.scale) : 0.0f;
+    total += w;
+    const int count = min(64, upto - t0);
+#pragma unroll 1
+    for (int i = 0; i < count; ++i) {
+      const int64_t r = where(t0 + i);
+      const float one = __shfl(w, i);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int d = lane + 64 * e;
+        if (d >= D) continue;
+        const uint8_t byte = c.codes[1][max(r, (int64_t)0) * (D / 2 * W) + (FMT == SQUANT_OUT_INT4 ? d / 2 : d)];
+        const int code = FMT == SQUANT_OUT_INT4 ? (int)((uint32_t)byte << (28 - 4 * (d & 1))) >> 28 : (int)(int8_t)byte;
+        sum[e] = __builtin_fmaf(one, (float)code * scale_of(1, r, d / kGroup), sum[e]);
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o);
+  const int64_t at = ((int64_t)split * a.rows.rows + row) * a.heads + qhead;
+  if (a.splits > 1 && lane == 0) a.stats[at] = make_float2(top * a.scale, total);
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int d = lane + 64 * e;
+    if (d >= D) continue;
+    if (a.splits > 1) a.partial[at * D + d] = sum[e];
+    else element<T>(a.out, row, qhead)[d] = (T)(total == 0.0f ? 0.0f : sum[e] / total);
+  }
+}
+
+// All rows of a tile, dealt to the workgroup's waves.  Arguments are read anew, from a pointer that the compiler does not know: kept until here
+// they would take registers from the loop before.
+template <class T, int FMT, int NG>
+__device__ __forceinline__ void rows_alone(int seq, int row0, int first, int count, int said, int rows_each) {
+  typedef const __attribute__((address_space(4))) CacheAttentionArgs* args_t;
+  args_t p = (args_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  const CacheAttentionArgs& a = *(const CacheAttentionArgs*)p;
+  const int head = (int)blockIdx.x % a.cache.heads, split = (int)blockIdx.y;
+  const int64_t capacity = (int64_t)a.cache.table_width * a.cache.page_size;
+  const int begin = split * a.chunk, end = min((int)min((int64_t)said, capacity), begin + a.chunk);
+#pragma unroll 1
+  for (int r = first + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); r < min(first + rows_each, count * a.group); r += kWaves) {
+    const int token = r / a.group, upto = said - count + token + 1;
+    row_alone<T, FMT, NG>(a, seq, row0 + token, head * a.group + r - token * a.group, head, split, begin, min(max(upto, 0), end), upto > capacity);
+  }
+}
+
 // HALVES: pages of a multiple of 16 tokens, of which each half of a block has consecutive rows: their addresses are a number for the
 // wave plus one of the lane that stays.
 //
@@ -326,6 +416,11 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
   for (int rt = 0; rt < RT; ++rt) largest[rt] = -kInfinity, sum[rt] = beyond[rt] ? __builtin_nanf("") : 0.0f;
   int key_e = 126, value_e = 126;
   const Magic magic;
+  // Tokens share exponents, and large scales cost small ones their bits.  What a row gets must not depend on tokens that it does not see:
+  // `wide` where some row sees a token that another does not, with a scale more than 2^7 times all of those before (of this
+  // block, or met by the wave).  An element is otherwise off by at most 8 * 2^-25 (a code's product and its scale, both rounded next to 0)
+  // where the largest that the row sees is at least 7 * 2^0: 2^-24 of it.
+  bool wide = false;
 
   Where at, next;
   if (t0 < end) {
@@ -345,6 +440,15 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
 
     const bool some_hidden = t0 + kTokens > least_seen;  // of the block's tokens, for some row
     uint32_t nan_tokens = at.bad;                         // rows that see one of them are NaN
+    // Whether the block's largest scale, `most`, is too large for e and for the tokens that are before those which only some rows see.  e stands for
+    // scales below 2^(8 - e): an exponent of 134 - e; 126 before there are any.
+    auto spread = [&](int e, uint32_t most, auto each) {
+      const int cut = max(least_seen, t0 + (e == 126 ? 1 : 0)), top = (int)(most >> 23) - 7;
+      if (cut >= min(end, t0 + kTokens) || top <= 134 - e) return false;
+      uint32_t before = 0;
+      each([&](int t, uint32_t scale) { before = max(before, t < cut ? scale & 0x7fffu : 0u); });
+      return lanes_where((int)(before >> 7) >= top) == 0;
+    };
 
     uint32_t top = 0;
 #pragma unroll
@@ -368,7 +472,15 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
         const uint64_t odd = lanes_where(none), pairs = odd | odd >> 32;
         nan_tokens |= (uint32_t)((pairs | pairs >> 16) & 0xffffu) << (16 * tt);
       }
-      key_e = min(key_e, __builtin_amdgcn_readfirstlane(scale_exponent(over_lanes_max(m))));
+      const uint32_t most = (uint32_t)__builtin_amdgcn_readfirstlane((int)over_lanes_max(m));
+      if (__builtin_expect(some_hidden, false))
+        wide |= spread(key_e, most, [&](auto take) {
+#pragma unroll
+          for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int k = 0; k < L::kKeyScales; ++k) take(t0 + 16 * tt + n, key_scale[tt][k]);
+        });
+      key_e = min(key_e, scale_exponent(most));
     }
     float4v s[2][RT];
 #pragma unroll
@@ -433,7 +545,15 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
           if (nan_tokens >> (4 * g + (j & 3) + 16 * (j >> 2)) & 1) value_scale[j][k] = 0;
           m = max(m, finite_bits(from_bfloat16(value_scale[j][k])));
         }
-      const int e = min(value_e, __builtin_amdgcn_readfirstlane(scale_exponent(over_lanes_max(m))));
+      const uint32_t most = (uint32_t)__builtin_amdgcn_readfirstlane((int)over_lanes_max(m));
+      if (__builtin_expect(some_hidden, false))
+        wide |= spread(value_e, most, [&](auto take) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int k = 0; k < L::kValueScales; ++k) take(t0 + 4 * g + (j & 3) + 16 * (j >> 2), value_scale[j][k]);
+        });
+      const int e = min(value_e, scale_exponent(most));
 #pragma unroll
       for (int f = 0; f < F; ++f)
 #pragma unroll
@@ -476,7 +596,7 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
         largest[rt] = most;
       }
       float base = largest[rt] == -kInfinity ? 0.0f : kWeightUnit - largest[rt];
-      if (far_scores(largest[rt])) {
+      if (__builtin_expect(far_scores(largest[rt]), false)) {
         const float from = largest[rt] == -kInfinity ? 0.0f : largest[rt];
 #pragma unroll
         for (int j = 0; j < 8; ++j) s[j >> 2][rt][j & 3] = s[j >> 2][rt][j & 3] * f - from;
@@ -539,7 +659,9 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) sum[rt] = over_groups_sum(sum[rt]);
   float* stats = lds;                      // [wave][2][TR]
-  float* pile = lds + kWaves * 2 * TR;     // [2][F][RT][64] of four
+  float* wides = lds + kWaves * 2 * TR;    // [wave]
+  float* pile = wides + kWaves;            // [2][F][RT][64] of four
+  if (lane == 0) wides[wave] = wide ? 1.0f : 0.0f;
   if (g == 0) {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -548,6 +670,11 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
     }
   }
   __syncthreads();
+  const float4v any = *reinterpret_cast<const float4v*>(wides);
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(any[0] + any[1] + any[2] + any[3] != 0.0f), false)) {
+    rows_alone<T, FMT, NG>(seq, row0, tile.first, count, said, TR);
+    return;
+  }
   float total[RT], most[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
@@ -675,7 +802,7 @@ template <int FORMATS> __global__ __launch_bounds__(kThreads) void join_splits(C
 }
 
 // LDS of a workgroup: the waves' statistics, and half of their sums.
-inline size_t cache_attention_lds(int ng, int rt) { return (size_t)kWaves * 2 * 16 * rt * 4 + (size_t)2 * (ng * 2) * rt * 64 * 16; }
+inline size_t cache_attention_lds(int ng, int rt) { return (size_t)kWaves * 2 * 16 * rt * 4 + kWaves * 4 + (size_t)2 * (ng * 2) * rt * 64 * 16; }
 
 typedef void (*cache_attention_t)(CacheAttentionArgs);
 template <class T, int FMT, bool HALVES> cache_attention_t cache_attention_of(int ng, int rt) {

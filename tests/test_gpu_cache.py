@@ -626,3 +626,48 @@ def test_large_values(sq, power, dtype, bits):
     out = sq.squant_cache_attention(q.cuda(), cache, table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), starts_of(new).cuda())
     check(out, q, host, table, lengths, new, page, dtype, bits, 0.125)
     assert out.isfinite().all()
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("which", ["keys", "values", "both"])
+@pytest.mark.parametrize("power", [3, 12, 30, 60, -12, -30])
+def test_later_tokens_of_other_sizes(sq, power, which, dtype, bits):
+    """New tokens whose scales are each 2^power times those of the one before: a row is as good as it is without the tokens behind it.
+    (60 times four is beyond bfloat16: the scale is infinite, the rows that see it NaN.)
+
+    Bound beside check's: an element is off by at most 2^-24 of the largest that the row sees, and a score by that for its key."""
+    gen = torch.Generator().manual_seed(77)
+    lengths, new, page, dim, heads = [45, 34, 3, 300], [4, 5, 3, 2], 16, 64, 8
+    pages, table = layout(gen, lengths, page)
+    cache, host = filled(sq, gen, pages, 2, page, dim, bits)
+    for b, (m, n) in enumerate(zip(lengths, new)):
+        for i in range(1, n):
+            p, s = slots_of(table, page, b, m - n + i, m - n + i + 1)
+            for j, name in ((1, "keys"), (3, "values")):
+                if which in (name, "both"):
+                    host[j][p, :, s] = 2.0 ** (power * i - 4)
+    cache = sq.QuantizedCache(*(t.cuda() for t in host))
+    q = (torch.randn(sum(new), heads, dim, generator=gen) * 0.25).to(dtype)
+    out = sq.squant_cache_attention(q.cuda(), cache, table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), starts_of(new).cuda())
+    rounded = 2.0 ** -11 if bits == 8 and dtype != F32 else 0.0 if dtype != F32 else 2.0 ** -22
+    r = 0
+    for b, (m, n) in enumerate(zip(lengths, new)):
+        for i in range(n):
+            sees = m - n + i + 1
+            p, s = slots_of(table, page, b, 0, sees)
+            if any(not host[x][p, :, s].isfinite().all() for x in (1, 3)):
+                assert out[r].isnan().all()
+                r += 1
+                continue
+            k, v = (values(host[2 * x][p, :, s], host[2 * x + 1][p, :, s]) for x in range(2))
+            row = q[r:r + 1].double()
+            ref = attention64(row, k, v, 0.125, True, F16 if dtype != F32 else F32, key_error=rounded, value_error=rounded, floor=FLOOR)
+            worst = 0.125 * 2.0 ** -24 * k.abs().amax((0, 2)).repeat_interleave(heads // 2) * row.abs().sum(-1)[0]  # of a score
+            most = v.abs().amax((0, 2)).repeat_interleave(heads // 2)
+            ref["out_tol"] += ((2.0 ** -24 + 4 * worst) * most)[None, :, None]
+            if dtype == BF16:
+                ref["out_tol"] += 2.0 ** -8 * ref["out"].abs()
+            if dtype != F16 or most.max() < 6e4:  # binary16's range
+                close(out[r:r + 1], ref, "out", f"row {i} of {n}, {sees} tokens")
+            r += 1
