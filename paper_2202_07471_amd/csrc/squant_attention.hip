@@ -126,7 +126,10 @@ struct CacheSplit {
 // than kMostChunk tokens each, so that sequences of different lengths balance.  96 sequences of 1024 to 16384 tokens: 179 us with stretches
 // of 6144, 171 with 1536.  Of 32 rows two run on a compute unit, 11 sequences of up to 6007 tokens with five rows each: 48 us with 512
 // workgroups, 37 with 768, 38 with 1024; of 16 rows three or more, 13 sequences of up to 3001 tokens with a row each: 23 us with 768, 21 with 1024.
-constexpr int64_t kGroups16 = 1024, kGroups32 = 768, kLeastChunk = 512, kMostChunk = 1536, kMostSplits = 1024;
+// Pieces' sums take kMostSums bytes at most, whatever a table could hold; those of 8000 workgroups or more, so where it binds there are enough.
+// 1024 sequences of up to 1500 tokens, 32 heads of 128 on 8, tables of 131072 tokens: 765 us and 1.5 GB with stretches of 1536, 246 us and
+// 119 MB with seven of 18816.
+constexpr int64_t kGroups16 = 1024, kGroups32 = 768, kLeastChunk = 512, kMostChunk = 1536, kMostSplits = 1024, kMostSums = 1 << 27;
 
 bool split_cache(int64_t rows, int32_t heads, const squant_cache_t& c, const squant_paged_t& w, CacheSplit& s) {
   const int group = heads / c.heads;
@@ -138,6 +141,8 @@ bool split_cache(int64_t rows, int32_t heads, const squant_cache_t& c, const squ
   const int64_t groups = s.tiles * c.heads;
   int64_t chunk = capacity * groups / (s.rt == 2 ? kGroups32 : kGroups16);
   chunk = std::max({kLeastChunk, std::min(kMostChunk, (chunk + 127) / 128 * 128), (capacity / kMostSplits + 127) / 128 * 128});
+  const int64_t sums = rows * heads * (4 * (int64_t)c.head_dim + 8), pieces = std::max<int64_t>(1, kMostSums / std::max<int64_t>(1, sums));
+  chunk = std::max(chunk, ((capacity + pieces - 1) / pieces + 127) / 128 * 128);
   s.splits = std::max<int64_t>(1, (capacity + chunk - 1) / chunk);
   s.chunk = s.splits == 1 ? std::max<int64_t>(128, (capacity + 127) / 128 * 128) : chunk;
   s.stats_bytes = s.splits > 1 ? (size_t)(s.splits * rows * heads * 8 + 255) / 256 * 256 : 0;

@@ -100,6 +100,19 @@ def test_attention_over_a_cache(A):
     assert 0 < one and many <= 1000 * one
 
 
+def test_workspace_of_wide_tables(A):
+    """What a table could hold does not decide how much memory a call takes."""
+    size = A._lib().squant_cache_attention_workspace_bytes
+    for rows in (1, 7, 96, 128, 1024, 20000):
+        for h, kv, dim in ((1, 1, 32), (32, 8, 128), (64, 8, 128), (28, 4, 96), (16, 16, 256)):
+            for tokens in (600, 16384, 131072, 1 << 20, 1 << 30):
+                for starts, sequences in ((None, rows), (P, max(1, rows // 5))):
+                    got = size(rows, h, ref(cache(A, h=kv, dim=dim)), ref(paged(A, starts=starts, sequences=sequences, width=tokens // 16)))
+                    assert got <= (1 << 27) + 256, (rows, h, kv, dim, tokens)
+                    if tokens >= 16384 and rows * h * dim <= 1 << 16:
+                        assert got > 0  # few rows' long sequences are cut
+
+
 def test_attention_over_prompts(A):
     L = A._lib()
 

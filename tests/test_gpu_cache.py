@@ -671,3 +671,15 @@ def test_later_tokens_of_other_sizes(sq, power, which, dtype, bits):
             if dtype != F16 or most.max() < 6e4:  # binary16's range
                 close(out[r:r + 1], ref, "out", f"row {i} of {n}, {sees} tokens")
             r += 1
+
+
+def test_many_sequences_of_a_wide_table(sq):
+    """More pieces than the workspace's ceiling allows: stretches grow, and sequences lie in several of them all the same."""
+    lengths = [(37 * i) % 200 + 1 for i in range(300)]
+    lengths[7], lengths[251] = 9000, 4001
+    attend(sq, 80, lengths, [1] * 300, 32, 2, 64, 16, BF16, 4, wider=9600, one_each=True)
+    import ctypes
+    A = sq.attention
+    place = A.squant_paged_t(256, 256, None, 300, 563 + 9600)
+    codes = A.squant_cache_t(256, 256, 256, 256, 10, 16, 2, 64, sq.OUT_INT4)
+    assert A._lib().squant_cache_attention_workspace_bytes(300, 32, ctypes.byref(codes), ctypes.byref(place)) > 2 * 300 * 32 * 264
