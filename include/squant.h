@@ -335,7 +335,8 @@ typedef struct {
  *   scale = max|x| / qmax in binary32, rounded to bfloat16 (qmax = 7 or 127),
  *   code  = round-half-even(x / scale), at most qmax in magnitude; 0 where the scale is 0.
  * A NaN or an infinity among the 32 makes the scale NaN and the codes 0.  The value held is code * scale.
- * head_dim is 32, 64, 96, 128, 192 or 256; codes are aligned to 16 bytes; pages * heads * page_size < 2^31. */
+ * head_dim is 32, 64, 96, 128, 192 or 256; codes are aligned to 16 bytes; pages * heads * page_size < 2^31 and
+ * heads * head_dim <= 2^17. */
 typedef struct {
   void* key_codes;    /* all: device */
   void* key_scales;

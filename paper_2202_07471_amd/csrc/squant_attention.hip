@@ -17,6 +17,8 @@ using namespace squant;
 using namespace squant::att;
 
 constexpr int64_t kMost = 0x7fffffffLL, kMostTokens = 1 << 30;  // of a table
+// Of a token's keys (512 heads of 256): 2^15 pieces of 8 with its values', whose divisions by multiplication are exact to 2^16.
+constexpr int64_t kMostElements = 1 << 17;
 // Elements between rows and between heads: a tile's rows are within 32 bits of bytes of each other, a buffer's within 64.
 constexpr int64_t kFarRow = (int64_t)1 << 22, kFarHead = (int64_t)1 << 31;
 
@@ -50,6 +52,7 @@ int check_cache(const squant_cache_t* c) {
   if (c->pages <= 0 || c->page_size <= 0 || c->heads <= 0) return SQUANT_ERR_SHAPE;
   if ((double)c->pages * c->page_size * c->heads > (double)kMost) return SQUANT_ERR_SHAPE;
   const int32_t d = c->head_dim;
+  if ((int64_t)c->heads * d > kMostElements) return SQUANT_ERR_SHAPE;
   return d == 32 || d == 64 || d == 96 || d == 128 || d == 192 || d == 256 ? SQUANT_OK : SQUANT_ERR_SHAPE;
 }
 
@@ -102,7 +105,6 @@ int cache_rows(bool write, const squant_heads_t* k, const squant_heads_t* v, int
   a.rows = packed_of(*w, rows);
   a.x[0] = strided(k, rows), a.x[1] = strided(v, rows);
   const int64_t pieces = (int64_t)2 * c->heads * (c->head_dim / 8);
-  if (pieces > 1 << 15) return SQUANT_ERR_SHAPE;  // 1024 heads of 256: what the divisions by multiplication are exact for
   a.pieces = (int32_t)pieces, a.dim_pieces = c->head_dim / 8;
   a.piece_magic = (uint32_t)((((uint64_t)1 << 32) / (uint64_t)pieces) + 1);
   a.dim_magic = (uint32_t)((((uint64_t)1 << 32) / (uint64_t)a.dim_pieces) + 1);

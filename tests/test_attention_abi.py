@@ -100,6 +100,19 @@ def test_attention_over_a_cache(A):
     assert 0 < one and many <= 1000 * one
 
 
+def test_heads_of_a_cache(A):
+    """What one call takes, all of them take."""
+    L = A._lib()
+    for h, dim, want in ((512, 256, 0), (513, 256, SHAPE), (4096, 32, 0), (4097, 32, SHAPE), (1 << 20, 64, SHAPE)):
+        c, w, x = cache(A, h=h, dim=dim), paged(A, width=400), heads(A, row=1 << 18, head=dim)
+        x.row = max(x.row, h * dim)
+        none = paged(A, starts=P, width=400)
+        assert L.squant_cache_write(ref(x), ref(x), 2, 0, ref(c), ref(none), None) == want
+        assert L.squant_cache_read(ref(c), ref(none), 2, 0, ref(x), ref(x), None) == want
+        assert L.squant_cache_attention(ref(x), 2, 0, h, ref(c), ref(w), 1.0, ref(x), WS, BIG, None) == want
+        assert (L.squant_cache_attention_workspace_bytes(5, h, ref(c), ref(w)) > 0) == (want == 0)
+
+
 def test_workspace_of_wide_tables(A):
     """What a table could hold does not decide how much memory a call takes."""
     size = A._lib().squant_cache_attention_workspace_bytes

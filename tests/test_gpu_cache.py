@@ -683,3 +683,23 @@ def test_many_sequences_of_a_wide_table(sq):
     place = A.squant_paged_t(256, 256, None, 300, 563 + 9600)
     codes = A.squant_cache_t(256, 256, 256, 256, 10, 16, 2, 64, sq.OUT_INT4)
     assert A._lib().squant_cache_attention_workspace_bytes(300, 32, ctypes.byref(codes), ctypes.byref(place)) > 2 * 300 * 32 * 264
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("heads,dim", [(512, 256), (1365, 96), (4096, 32)])
+def test_most_heads(sq, heads, dim, bits):
+    gen = torch.Generator().manual_seed(heads)
+    cache = sq.QuantizedCache.empty(3, heads, 2, dim, formats(sq, bits))
+    args = (torch.tensor([[1, 2]], dtype=torch.int32).cuda(), torch.tensor([3], dtype=torch.int32).cuda(), starts_of([3]).cuda())
+    k, v = (torch.randn(3, heads, dim, generator=gen).to(BF16) for _ in range(2))
+    sq.squant_cache_write(k.cuda(), v.cuda(), cache, *args)
+    for got, x in zip(sq.squant_cache_read(cache, *args, 3, F32), (k, v)):
+        assert torch.equal(got.cpu(), values(*quantise(x, bits)).float())
+    q = torch.randn(3, heads, dim, generator=gen).to(BF16)
+    out = sq.squant_cache_attention(q.cuda(), cache, *args)
+    some = torch.tensor([0, 1, heads // 2, heads - 1])
+    rounded = 2.0 ** -11 if bits == 8 else 0.0
+    ref = attention64(q[:, some].double(), values(*quantise(k[:, some], bits)), values(*quantise(v[:, some], bits)), dim ** -0.5, True, F16,
+                      key_error=rounded, value_error=rounded, floor=FLOOR)
+    ref["out_tol"] += 2.0 ** -8 * ref["out"].abs()
+    close(out[:, some.cuda()], ref, "out")
