@@ -283,7 +283,7 @@ int squant_cache_attention(const squant_heads_t* h_q, squant_wtype_t type, int64
   a.cache = cache_of(c, *h_where);
   a.rows = packed_of(*h_where, rows);
   a.q = strided(h_q, rows), a.out = strided(h_out, rows);
-  a.type = (int)type, a.heads = heads, a.group = heads / c.heads;
+  a.heads = heads, a.group = heads / c.heads;
   a.splits = (int32_t)s.splits, a.chunk = (int32_t)s.chunk;
   a.scale = base2(scale);
   if (s.splits > 1) a.stats = (float2*)d_workspace, a.partial = (float*)((char*)d_workspace + s.stats_bytes);
@@ -294,7 +294,7 @@ int squant_cache_attention(const squant_heads_t* h_q, squant_wtype_t type, int64
   const cache_attention_t k = of(ng, s.rt, c.page_size % 16 == 0);
   hipStream_t st = (hipStream_t)stream;
   if (int rc = launch(k, s.tiles * c.heads, s.splits, cache_attention_lds(ng, s.rt), st, a)) return rc;
-  return s.splits > 1 ? launch(join_splits_kernel(), (rows * heads + kWaves - 1) / kWaves, 1, 0, st, a) : SQUANT_OK;
+  return s.splits > 1 ? launch(join_splits_kernel((int)type), (rows * heads + kWaves - 1) / kWaves, 1, 0, st, a) : SQUANT_OK;
 }
 
 size_t squant_attention_workspace_bytes(const squant_packed_t* h_packed, squant_wtype_t type) {

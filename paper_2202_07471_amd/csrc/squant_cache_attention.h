@@ -27,9 +27,7 @@ struct CacheAttentionArgs {
   Cache cache;
   Packed rows;
   Strided q, out;
-  int type;
   int32_t heads, group;  // query heads, and of a key head
-  int32_t tiles;         // of rows
   int32_t splits;
   int32_t chunk;         // tokens of a split, a multiple of 128
   float scale;           // times log2(e)
@@ -738,7 +736,7 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
 
 // The splits of each row and head become its output: a wave for each, lanes in groups of dim / 4 that take a split each, four
 // splits of a group on their way at once.
-template <int FORMATS> __global__ __launch_bounds__(kThreads) void join_splits(CacheAttentionArgs a) {
+template <class T> __global__ __launch_bounds__(kThreads) void join_splits(CacheAttentionArgs a) {
   const int lane = (int)threadIdx.x & 63;
   const int64_t at = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int64_t all = (int64_t)a.rows.rows * a.heads;
@@ -789,16 +787,10 @@ template <int FORMATS> __global__ __launch_bounds__(kThreads) void join_splits(C
   }
   if (group != 0) return;
   const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
-  if (a.type == SQUANT_W_F32) {
-    struct Four { float v[4]; };
-    store_any(element<float>(a.out, row, head) + d, Four{{out[0] * inverse, out[1] * inverse, out[2] * inverse, out[3] * inverse}});
-  } else if (a.type == SQUANT_W_F16) {
-    struct Four { _Float16 v[4]; };
-    store_any(element<_Float16>(a.out, row, head) + d, Four{{(_Float16)(out[0] * inverse), (_Float16)(out[1] * inverse), (_Float16)(out[2] * inverse), (_Float16)(out[3] * inverse)}});
-  } else {
-    struct Four { __bf16 v[4]; };
-    store_any(element<__bf16>(a.out, row, head) + d, Four{{(__bf16)(out[0] * inverse), (__bf16)(out[1] * inverse), (__bf16)(out[2] * inverse), (__bf16)(out[3] * inverse)}});
-  }
+  struct Four { T v[4]; } o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o.v[e] = (T)(out[e] * inverse);
+  store_any(element<T>(a.out, row, head) + d, o);
 }
 
 // LDS of a workgroup: the waves' statistics, and half of their sums.
@@ -833,7 +825,7 @@ cache_attention_t cache_attention_int4_f32(int ng, int rt, bool halves);
 cache_attention_t cache_attention_int8_bf16(int ng, int rt, bool halves);
 cache_attention_t cache_attention_int8_f16(int ng, int rt, bool halves);
 cache_attention_t cache_attention_int8_f32(int ng, int rt, bool halves);
-cache_attention_t join_splits_kernel();
+cache_attention_t join_splits_kernel(int type);
 
 }  // namespace att
 }  // namespace squant
