@@ -703,3 +703,56 @@ def test_most_heads(sq, heads, dim, bits):
                       key_error=rounded, value_error=rounded, floor=FLOOR)
     ref["out_tol"] += 2.0 ** -8 * ref["out"].abs()
     close(out[:, some.cuda()], ref, "out")
+
+
+def eleven_bits(x):
+    """x (64 bits) rounded to 11 significant bits."""
+    m, e = torch.frexp(x)
+    return torch.ldexp(torch.round(m * 2.0 ** 11), e - 11)
+
+
+def whole_elements(gen, dtype, which):
+    """48 sequences of two tokens, 8 bits, whose output shows the last bits of their elements: (q, host cache, exact output [48, 1, 64], bound,
+    output with elements of 11 bits)."""
+    n, dim = 48, 64
+    codes = [torch.zeros(n, 1, 2, dim, dtype=torch.int8) for _ in range(2)]
+    scales = [(torch.randint(129, 255, (n, 1, 2, 2), generator=gen) * 2.0 ** -7).to(BF16) for _ in range(2)]
+    q = torch.zeros(n, 1, dim, dtype=dtype)
+    if which == "values":
+        # equal weights, 2^14 each: the sum of the two values, which nearly cancel, is exact
+        scales[1][:, :, 1] = scales[1][:, :, 0]
+        first = torch.randint(100, 127, (n, 1, dim), generator=gen)
+        codes[1][:, :, 0], codes[1][:, :, 1] = first.to(torch.int8), (torch.randint(-4, 5, (n, 1, dim), generator=gen) - first).to(torch.int8)
+    else:
+        # scores of about 2^9 next to each other, of different elements of the query; values 1 and -1
+        codes[0][:, :, 0, 0], codes[0][:, :, 1, 40] = 127, 101
+        k = values(codes[0], scales[0])
+        a = 2.0 ** 12 / k[:, 0, 0, 0] * (1 + torch.rand(n, generator=gen).double() / 4)
+        q[:, 0, 0] = a.to(dtype)
+        q[:, 0, 40] = (q[:, 0, 0].double() * k[:, 0, 0, 0] / k[:, 0, 1, 40]).to(dtype)
+        codes[1][:, :, 0], codes[1][:, :, 1], scales[1][:] = 1, -1, 1.0
+
+    def run(of):
+        k, v = of(values(codes[0], scales[0]))[:, 0], of(values(codes[1], scales[1]))[:, 0]
+        s = 0.125 * (k @ q.double().transpose(1, 2))[..., 0]
+        return (torch.softmax(s, 1)[..., None] * v).sum(1, keepdim=True)
+    exact = run(lambda x: x)
+    half = torch.finfo(dtype).eps / 2
+    if which == "values":
+        tol = half * exact.abs()  # one rounding
+    else:
+        # binary32 sums of products of 2^9 or less each, 24 steps; a weight is rounded (11 or 22 bits), the output once
+        tol = torch.full_like(exact, 2 * 24 * 2.0 ** -23 * 2 * 640 + 2.0 ** -11 + 2.0 ** -20) + half * exact.abs()
+    return q, [codes[0], scales[0], codes[1], scales[1]], exact, tol, run(eleven_bits)
+
+
+@pytest.mark.parametrize("which", ["keys", "values"])
+@pytest.mark.parametrize("dtype", [F16, F32])
+def test_whole_elements_of_8_bits(sq, dtype, which):
+    """Binary16 and binary32 calls multiply by all 15 bits of an element."""
+    q, host, exact, tol, short = whole_elements(torch.Generator().manual_seed(82), dtype, which)
+    assert ((short - exact).abs() > tol).double().mean() > 0.5  # elements of 11 bits would be seen
+    cache = sq.QuantizedCache(*(t.cuda() for t in host))
+    table, lens = torch.arange(48, dtype=torch.int32).view(48, 1).cuda(), torch.full((48,), 2, dtype=torch.int32).cuda()
+    out = sq.squant_cache_attention(q.cuda(), cache, table, lens).cpu().double()
+    assert ((out - exact).abs() <= tol).all()
