@@ -575,10 +575,9 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
     half8 p[RT][PL];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      // Both powers at once: where keys are zeros so far and queries small, or scale is 0, they leave binary32.  Never 0 itself: a
-      // hidden score's minus infinity stays one, and scores times 2^-149 are nothing.
-      float f = ldexpf(a.scale, -(q_e[rt] + key_e));
-      f = f == 0.0f ? 0x1p-149f : f;
+      // Both powers at once: where keys are zeros so far and queries small, or scale is 0, they leave binary32.  Never 0 itself, nor
+      // infinite: a hidden score's minus infinity stays one, and a score of 0 too; others times 2^-149 are nothing.
+      float f = __builtin_amdgcn_fmed3f(ldexpf(a.scale, -(q_e[rt] + key_e)), 0x1p-149f, 0x1.fffffep127f);
       float m = -kInfinity;
 #pragma unroll
       for (int j = 0; j < 8; ++j) m = fmaxf(m, s[j >> 2][rt][j & 3]);

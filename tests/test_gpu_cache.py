@@ -756,3 +756,22 @@ def test_whole_elements_of_8_bits(sq, dtype, which):
     table, lens = torch.arange(48, dtype=torch.int32).view(48, 1).cuda(), torch.full((48,), 2, dtype=torch.int32).cuda()
     out = sq.squant_cache_attention(q.cuda(), cache, table, lens).cpu().double()
     assert ((out - exact).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_scores_beyond_binary32(sq, dtype, bits):
+    """A zero key among those whose scores are minus infinity in binary32: its value."""
+    gen = torch.Generator().manual_seed(83)
+    pages, table = layout(gen, [50], 16)
+    cache, host = filled(sq, gen, pages, 1, 16, 64, bits)
+    host[0].fill_(0x11 if bits == 4 else 1)
+    host[1].fill_(-2.0 ** 100)
+    p, s = slots_of(table, 16, 0, 20, 21)
+    host[1][p, :, s] = 0.0
+    cache = sq.QuantizedCache(*(t.cuda() for t in host))
+    q = torch.full((1, 2, 64), 2.0 ** 100, dtype=dtype)
+    out = sq.squant_cache_attention(q.cuda(), cache, table.cuda(), torch.tensor([50], dtype=torch.int32).cuda())
+    want = values(host[2][p, :, s], host[3][p, :, s])[0]
+    tol = (2.0 ** -11 + torch.finfo(dtype).eps / 2) * want.abs()
+    assert ((out[0].cpu().double() - want).abs() <= tol).all()
