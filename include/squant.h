@@ -304,11 +304,18 @@ int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t t
  * Attention, and a cache of keys and values in 4 or 8 bits: what a language model of quantised layers has between
  * its projections.
  *
- * Element type (squant_wtype_t): that of queries, keys, values, outputs and gradients of a call.  Products are taken
- * of the elements as they are (binary32: in binary32) and added in binary32, softmax statistics are binary32.  What is
- * multiplied by the values (and, in a backward pass, by queries, keys and output gradients) is rounded to the
- * element type first (binary32: not; attention over a cache: to 11 bits, binary32 to 22, or to 2^-39 of the row's
- * largest weight where that is more).  Every output is rounded once.
+ * Element type (squant_wtype_t): that of queries, keys, values, outputs and gradients of a call.  Over prompts products
+ * are taken of the elements as they are and added in binary32, softmax statistics are binary32; what is multiplied by the
+ * values (and, in a backward pass, by queries, keys and output gradients) is rounded to the element type first (binary32:
+ * not).  Gradients take weights as exp(score - log-sum-exp), which makes them off by 2^-22 |log-sum-exp| (relative), however
+ * large scores are.  Every output is rounded once.
+ *
+ * Over a cache matrix products are of binary16 numbers, with shared powers of two:
+ *   elements code * scale: all bits (4-bit codes 11, 8-bit ones 15), but 11 of 8-bit ones in bfloat16 calls;
+ *   queries: all bits, binary32 22 (the last of these do not meet the last 4 of an 8-bit element);
+ *   weights: 11 bits, binary32 22.
+ * What is small against others keeps less: an element is off by up to 2^-24 of the largest scale times qmax, of the head's
+ * keys or values, that the row sees; a query's by 2^-35 of its row's largest; a weight by 2^-39 of its row's largest.
  *
  * Rows are tokens.  Sequences lie one after the other: sequence b has the rows starts[b] to starts[b + 1] - 1, starts
  * holding sequences + 1 numbers that begin with 0 and do not fall; sequences may be empty.  Rows from
@@ -350,7 +357,8 @@ typedef struct {
  * t % page_size of page table[b][t / page_size].  lengths[b] tokens of it count, the call's own among them: row r of
  * sequence b is token lengths[b] - (starts[b + 1] - r), the rows being its last ones.  starts NULL: one row for each
  * sequence.  A table's entry that is no page, or lengths beyond the table: nothing is written there, and NaN is read.  A row
- * that sees a token whose scale is NaN or infinite is NaN.  For attention a table holds at most 2^30 tokens. */
+ * that sees such a token, or one with a scale that is NaN or infinite, is NaN.  For attention a table holds at most 2^30
+ * tokens. */
 typedef struct {
   const int32_t* table;   /* device, [sequences][table_width] */
   const int32_t* lengths; /* device, [sequences] */

@@ -5,11 +5,12 @@
 // A workgroup takes 16 or 32 rows (new tokens times the query heads of a key head) and a stretch of the sequence, its four
 // waves 32 tokens each in turn; a wave reads codes and scales from memory straight into the lanes that multiply them, a block of
 // tokens ahead.  Codes become binary16 numbers code * scale * 2^e with an exponent for the wave (running: a block with a
-// larger scale lowers it, and the output's sums with it), which for 4 bits is exact: 3 bits of a code and 8 of a scale are 11.
+// larger scale lowers it, and the output's sums with it).  For 4 bits that is exact, 3 bits of a code and 8 of a scale being 11, for scales
+// down to about 2^-24 of the largest that the wave has met; below, an element loses bits (`wide` says what of them).
 // For 8 bits it would round to 11 bits (2^-12 of an element): binary16 and binary32 calls take the remainder as a second plane
 // (11 drafted tokens' binary16 outputs 5.5e-4 off without it, 2.1e-4 with), bfloat16 ones do without.  Queries are
-// binary16 with an exponent for each row: exact for 16-bit types, two planes for binary32.  Softmax weights
-// are rounded to 11 bits times 2^14 (binary32: two planes).  Sums are binary32.
+// binary16 with an exponent for each row: two planes for binary32, whose lower one does not meet the remainders (2^-24 of a product).  Softmax
+// weights are rounded to 11 bits times 2^14 (binary32: two planes).  Sums are binary32.
 //
 // Layout of a block: lane 16 g + n.
 //   keys    lane holds token n (and 16 + n), the g-th quarter of its codes: NG fragments of 8 codes.
@@ -119,7 +120,8 @@ __device__ __forceinline__ uint32_t finite_bits(float v) {
 __device__ __forceinline__ uint32_t too_large(int e) { return min((uint32_t)(9 - e + 127) << 7, 0x7f80u); }
 
 // Waves a SIMD that registers are kept for.  Three are what most take; asked for more, heads of 128 spill (96 sequences 171 us, 211), and so do
-// 32 rows at three (eleven sequences' drafts 36 us, 61).
+// 32 rows at three (eleven sequences' drafts 36 us, 61).  At two, heads of 256 over 8 bits keep 22 to 43 registers in memory, binary32 calls
+// 101 to 126 (9 to 33 of others with 32 rows or heads of 192).
 constexpr int cache_occupancy(int ng, int rt) { return ng <= 2 && rt == 1 ? 3 : 2; }
 
 // One row by a wave, in binary32 and token by token: for tiles whose rows cannot share exponents, which are seldom.  A lane for each token, then

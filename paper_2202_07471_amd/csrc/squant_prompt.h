@@ -5,8 +5,8 @@
 //             delta = dO . O for each row.
 //
 // The backward pass is two kernels: one whose workgroups own queries (dQ) and one whose workgroups own keys (dK, dV, over all
-// query heads of a group).  They compute S and dO V^T twice, seven products instead of five, and need no sums between workgroups: no
-// atomics, the same bits from run to run.
+// query heads of a group).  They compute S and dO V^T twice, seven products instead of five (16-bit types eight: P K beside dS K, for
+// delta), and need no sums between workgroups: no atomics, the same bits from run to run.
 //
 // A workgroup is four waves.  What it owns (16 or 32 rows a wave) stays in registers as matrix operands; what it walks over
 // goes through the LDS in tiles, the next one on its way while one is multiplied.  A tile is kept once, as rows; its
@@ -251,7 +251,10 @@ constexpr float kSlack = 8.0f;
 //   by_tile: max(0, min(ceil(walked / T), its tiles - i)),  else ceil(walked / T),
 // its walk's length in tiles.  A lane for each sequence knows how many of its tiles lie above a level; the level at which they
 // are more than `id` is searched by halves.
-constexpr int kRunAtOnce = 512;  // two a compute unit
+
+// Workgroups that count as run at once: two a compute unit, as heads of 128 have them.  Heads of 64 run three or four, 192 and 256 in
+// binary32 one; plans that knew that have not been measured.
+constexpr int kRunAtOnce = 512;
 // Where piece i of a walk's steps (less than 2^27) begins.
 __device__ __forceinline__ int piece_of(int steps, uint32_t i, int splits) { return (int)((uint32_t)steps * i / (uint32_t)splits); }
 
@@ -973,6 +976,8 @@ PromptKernel prompt_queries_f32(int dim, bool direct, bool many);
 prompt_t prompt_join_kernel(int type, bool keys);
 prompt_t prompt_join_forward_kernel(int type);
 
+// The loop of hidden steps, with its token-by-token path inlined, keeps registers in memory: 42 to 142 of heads of 192 and 256 (16 bits), 45 and
+// 103 of 128 and 256 (binary32), up to 11 of 64 and 128; the other loop none.
 template <class T> PromptKernel forward_for(int dim, bool direct) {
   if constexpr (sizeof(T) == 2) {
     if (dim <= 64) return forward_of<T, 64, 2, 64, 4, 3>(direct);  // two waves a SIMD: 8192 tokens, 32 heads: 419 us, 397
