@@ -222,7 +222,7 @@ __device__ __forceinline__ void rows_alone(int seq, int row0, int first, int cou
 // one token of 8192 took 12 us in this kernel, whether it multiplied or only read).  The next block's keys are on their way from
 // a block's beginning on, its values from the end of the products, into the registers that have become free there.
 //
-// What bounds it: 96 sequences of 1024 to 16384 tokens, 32 heads of 128 on 8, 4 bits: 165 us, 3.4 TB/s of codes and scales; reading them
+// What bounds it: 96 sequences of 1024 to 16384 tokens, 32 heads of 128 on 8, 4 bits: 167 us, 3.4 TB/s of codes and scales; reading them
 // without the products takes 125, and vector instructions (1.7 a code: place, centre, scale) issue for about half of the time.
 // One token of 8192: 12 us, of which reading alone takes nearly all: a chain of lengths, table, codes, and two joins.
 template <class T, int FMT, int NG, int RT, bool HALVES>
