@@ -163,10 +163,11 @@ __device__ __forceinline__ void row_alone(const CacheAttentionArgs& a, int seq, 
   for (int t = begin + lane; t < upto; t += 64) top = fmaxf(top, score(t));
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+  const float none = top == -kInfinity ? 0.0f : top, scale = fmaxf(a.scale, 0x1p-149f);
   float total = beyond ? __builtin_nanf("") : 0.0f, sum[E] = {};
 #pragma unroll 1
   for (int t0 = begin; t0 < upto; t0 += 64) {
-    const float w = t0 + lane < upto ? exp2_fast((score(t0 + lane) - top) * a.scale) : 0.0f;
+    const float w = t0 + lane < upto ? exp2_fast((score(t0 + lane) - none) * scale) : 0.0f;
     total += w;
     const int count = min(64, upto - t0);
 #pragma unroll 1
@@ -186,7 +187,7 @@ __device__ __forceinline__ void row_alone(const CacheAttentionArgs& a, int seq, 
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o);
   const int64_t at = ((int64_t)split * a.rows.rows + row) * a.heads + qhead;
-  if (a.splits > 1 && lane == 0) a.stats[at] = make_float2(top * a.scale, total);
+  if (a.splits > 1 && lane == 0) a.stats[at] = make_float2(top * scale, total);
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const int d = lane + 64 * e;

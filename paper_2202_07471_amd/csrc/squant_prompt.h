@@ -351,13 +351,14 @@ __device__ __forceinline__ void far_row(const PromptArgs& a, int64_t q_row, int 
   for (int t = from + lane; t < to; t += 64) top = fmaxf(top, score(t));
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+  const float none = top == -kInfinity ? 0.0f : top;
   float total = 0.0f, sum[E] = {};
 #pragma unroll 1
   for (int t0 = from; t0 < to; t0 += 64) {
-    const float w = t0 + lane < to ? exp2_fast((score(t0 + lane) - top) * a.scale2) : 0.0f;
+    const float w = t0 + lane < to ? exp2_fast((score(t0 + lane) - none) * a.scale2) : 0.0f;
     total += w;
     const int count = min(64, to - t0);
-#pragma unroll 8
+#pragma unroll 1
     for (int i = 0; i < count; ++i) {
       const T* v = element<T>(a.v, k0 + t0 + i, kv_head);
       const float one = __shfl(w, i);
