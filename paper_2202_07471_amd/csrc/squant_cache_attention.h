@@ -124,8 +124,8 @@ __device__ __forceinline__ uint32_t too_large(int e) { return min((uint32_t)(9 -
 // 101 to 126 (9 to 33 of others with 32 rows or heads of 192).
 constexpr int cache_occupancy(int ng, int rt) { return ng <= 2 && rt == 1 ? 3 : 2; }
 
-// One row by a wave, in binary32 and token by token: for tiles whose rows cannot share exponents, which are seldom.  A lane for each token, then
-// for each element.
+// One row by a wave, token by token: for tiles whose rows cannot share exponents, which are seldom.  Scores and sums are binary64: with powers of two
+// of their own, the other rows' do not leave binary32 either.  A lane for each token, then for each element.
 template <class T, int FMT, int NG>
 __device__ __forceinline__ void row_alone(const CacheAttentionArgs& a, int seq, int row, int qhead, int head, int split, int begin, int upto, bool beyond) {
   constexpr int W = FMT == SQUANT_OUT_INT4 ? 1 : 2, D = NG * kGroup, E = (D + 63) / 64;
@@ -144,7 +144,7 @@ __device__ __forceinline__ void row_alone(const CacheAttentionArgs& a, int seq, 
   };
   auto score = [&](int t) {
     const int64_t r = where(t);
-    float s = 0.0f;
+    double s = 0.0;
 #pragma unroll 1
     for (int i = 0; i < 4 * NG; ++i) {
       uint32_t words[W];
@@ -154,20 +154,20 @@ __device__ __forceinline__ void row_alone(const CacheAttentionArgs& a, int seq, 
       load8(q + 8 * i, x);
       decode<FMT>(words, scale_of(0, r, i >> 2), y);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s = __builtin_fmaf(x[e], y[e], s);
+      for (int e = 0; e < 8; ++e) s = __builtin_fma((double)x[e], (double)y[e], s);
     }
     return s;
   };
-  float top = -kInfinity;
+  double top = -(double)kInfinity;
 #pragma unroll 1
-  for (int t = begin + lane; t < upto; t += 64) top = fmaxf(top, score(t));
+  for (int t = begin + lane; t < upto; t += 64) top = fmax(top, score(t));
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-  const float none = top == -kInfinity ? 0.0f : top, scale = fmaxf(a.scale, 0x1p-149f);
-  float total = beyond ? __builtin_nanf("") : 0.0f, sum[E] = {};
+  for (int o = 1; o < 64; o <<= 1) top = fmax(top, __shfl_xor(top, o));
+  const double none = top == -(double)kInfinity ? 0.0 : top, scale = fmaxf(a.scale, 0x1p-149f);
+  double total = beyond ? (double)__builtin_nanf("") : 0.0, sum[E] = {};
 #pragma unroll 1
   for (int t0 = begin; t0 < upto; t0 += 64) {
-    const float w = t0 + lane < upto ? exp2_fast((score(t0 + lane) - none) * scale) : 0.0f;
+    const float w = t0 + lane < upto ? exp2_fast((float)((score(t0 + lane) - none) * scale)) : 0.0f;
     total += w;
     const int count = min(64, upto - t0);
 #pragma unroll 1
@@ -180,20 +180,20 @@ __device__ __forceinline__ void row_alone(const CacheAttentionArgs& a, int seq, 
         if (d >= D) continue;
         const uint8_t byte = c.codes[1][max(r, (int64_t)0) * (D / 2 * W) + (FMT == SQUANT_OUT_INT4 ? d / 2 : d)];
         const int code = FMT == SQUANT_OUT_INT4 ? (int)((uint32_t)byte << (28 - 4 * (d & 1))) >> 28 : (int)(int8_t)byte;
-        sum[e] = __builtin_fmaf(one, (float)code * scale_of(1, r, d / kGroup), sum[e]);
+        sum[e] = __builtin_fma((double)one, (double)code * (double)scale_of(1, r, d / kGroup), sum[e]);
       }
     }
   }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o);
   const int64_t at = ((int64_t)split * a.rows.rows + row) * a.heads + qhead;
-  if (a.splits > 1 && lane == 0) a.stats[at] = make_float2(top * scale, total);
+  if (a.splits > 1 && lane == 0) a.stats[at] = make_float2((float)(top * scale), (float)total);
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const int d = lane + 64 * e;
     if (d >= D) continue;
-    if (a.splits > 1) a.partial[at * D + d] = sum[e];
-    else element<T>(a.out, row, qhead)[d] = (T)(total == 0.0f ? 0.0f : sum[e] / total);
+    if (a.splits > 1) a.partial[at * D + d] = (float)sum[e];
+    else element<T>(a.out, row, qhead)[d] = (T)(float)(total == 0.0 ? 0.0 : sum[e] / total);
   }
 }
 

@@ -628,19 +628,13 @@ def test_large_values(sq, power, dtype, bits):
     assert out.isfinite().all()
 
 
-@pytest.mark.parametrize("bits", [4, 8])
-@pytest.mark.parametrize("dtype", [BF16, F16, F32])
-@pytest.mark.parametrize("which", ["keys", "values", "both"])
-@pytest.mark.parametrize("power", [3, 12, 30, 60, -12, -30])
-def test_later_tokens_of_other_sizes(sq, power, which, dtype, bits):
+def later_tokens(sq, lengths, new, page, dim, heads, kv, wider, power, which, dtype, bits):
     """New tokens whose scales are each 2^power times those of the one before: a row is as good as it is without the tokens behind it.
-    (60 times four is beyond bfloat16: the scale is infinite, the rows that see it NaN.)
 
     Bound beside check's: an element is off by at most 2^-24 of the largest that the row sees, and a score by that for its key."""
     gen = torch.Generator().manual_seed(77)
-    lengths, new, page, dim, heads = [45, 34, 3, 300], [4, 5, 3, 2], 16, 64, 8
-    pages, table = layout(gen, lengths, page)
-    cache, host = filled(sq, gen, pages, 2, page, dim, bits)
+    pages, table = layout(gen, lengths, page, wider=wider)
+    cache, host = filled(sq, gen, pages, kv, page, dim, bits)
     for b, (m, n) in enumerate(zip(lengths, new)):
         for i in range(1, n):
             p, s = slots_of(table, page, b, m - n + i, m - n + i + 1)
@@ -650,6 +644,7 @@ def test_later_tokens_of_other_sizes(sq, power, which, dtype, bits):
     cache = sq.QuantizedCache(*(t.cuda() for t in host))
     q = (torch.randn(sum(new), heads, dim, generator=gen) * 0.25).to(dtype)
     out = sq.squant_cache_attention(q.cuda(), cache, table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(), starts_of(new).cuda())
+    scale, group = dim ** -0.5, heads // kv
     rounded = 2.0 ** -11 if bits == 8 and dtype != F32 else 0.0 if dtype != F32 else 2.0 ** -22
     r = 0
     for b, (m, n) in enumerate(zip(lengths, new)):
@@ -662,15 +657,36 @@ def test_later_tokens_of_other_sizes(sq, power, which, dtype, bits):
                 continue
             k, v = (values(host[2 * x][p, :, s], host[2 * x + 1][p, :, s]) for x in range(2))
             row = q[r:r + 1].double()
-            ref = attention64(row, k, v, 0.125, True, F16 if dtype != F32 else F32, key_error=rounded, value_error=rounded, floor=FLOOR)
-            worst = 0.125 * 2.0 ** -24 * k.abs().amax((0, 2)).repeat_interleave(heads // 2) * row.abs().sum(-1)[0]  # of a score
-            most = v.abs().amax((0, 2)).repeat_interleave(heads // 2)
+            ref = attention64(row, k, v, scale, True, F16 if dtype != F32 else F32, key_error=rounded, value_error=rounded, floor=FLOOR)
+            worst = scale * 2.0 ** -24 * k.abs().amax((0, 2)).repeat_interleave(group) * row.abs().sum(-1)[0]  # of a score
+            most = v.abs().amax((0, 2)).repeat_interleave(group)
             ref["out_tol"] += ((2.0 ** -24 + 4 * worst) * most)[None, :, None]
             if dtype == BF16:
                 ref["out_tol"] += 2.0 ** -8 * ref["out"].abs()
-            if dtype != F16 or most.max() < 6e4:  # binary16's range
+            held = max(k.abs().max(), v.abs().max()) < 2.0 ** 128  # 127 * 2^121 is beyond binary32, and no token written holds it
+            if held and (dtype != F16 or most.max() < 6e4):  # binary16's range
                 close(out[r:r + 1], ref, "out", f"row {i} of {n}, {sees} tokens")
             r += 1
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("which", ["keys", "values", "both"])
+@pytest.mark.parametrize("power", [3, 12, 30, 60, -12, -30])  # 60 times four is beyond bfloat16: the scale is infinite, the rows that see it NaN
+def test_later_tokens_of_other_sizes(sq, power, which, dtype, bits):
+    later_tokens(sq, [45, 34, 3, 300], [4, 5, 3, 2], 16, 64, 8, 2, 0, power, which, dtype, bits)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("power", [4, 12, 25])
+@pytest.mark.parametrize("lengths,new,page,dim,heads,kv,wider",
+                         [([45, 700, 1030], [4, 5, 3], 16, 64, 8, 2, 90), ([45, 70], [4, 5], 7, 96, 3, 3, 0), ([514, 1200], [5, 6], 24, 32, 4, 1, 40),
+                          ([70, 40], [6, 6], 32, 128, 8, 2, 0), ([520, 33], [6, 6], 64, 128, 8, 1, 40), ([90], [9], 16, 256, 4, 2, 0),
+                          ([80, 66], [9, 10], 50, 192, 2, 1, 0), ([100, 64], [28, 3], 16, 64, 4, 1, 60)])
+def test_later_tokens_in_other_layouts(sq, lengths, new, page, dim, heads, kv, wider, power, dtype, bits):
+    """Pieces of sequences, odd pages, two halves of 16 rows, sizes of head, more rows than a tile."""
+    later_tokens(sq, lengths, new, page, dim, heads, kv, wider, power, "both", dtype, bits)
 
 
 def test_many_sequences_of_a_wide_table(sq):
