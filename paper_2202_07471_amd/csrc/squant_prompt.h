@@ -236,9 +236,11 @@ template <int FIRST, int SECOND, int EACH, int SECOND_STEP> __device__ __forcein
   __builtin_amdgcn_sched_group_barrier(kMatrix, kAhead * EACH, 0);
 }
 
-// A row's running maximum (base 2) may be passed by this much before sums are scaled down to a new one: weights stay below 2^8
-// (binary16: 2^15).  Without it most steps of a long sequence have a row of the wave's 32 whose maximum moves.
+// A row's running maximum (base 2) may be passed by this much before sums are scaled down to a new one: weights, held times
+// 2^forward_unit, stay below 1 (binary16: 2^15), so that sums of values leave binary32 no sooner than with weights of at most 1.  Without it most steps of a long sequence have a row of the wave's 32 whose maximum moves.
 constexpr float kSlack = 8.0f;
+template <class T> constexpr float forward_unit() { return __is_same(T, _Float16) ? weight_unit<T>() : -kSlack; }
+template <class T> constexpr float without_unit() { return __is_same(T, _Float16) ? 0x1p-7f : 0x1p8f; }
 
 // The tile of a workgroup, and the rows that its sequence walks over.
 //
@@ -371,7 +373,7 @@ __device__ __forceinline__ void far_row(const PromptArgs& a, int64_t q_row, int 
   for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o);
   const float largest = top * a.scale2;
   if (a.splits > 1) {
-    const float unit = weight_unit<T>() != 0.0f ? 128.0f : 1.0f;
+    const float unit = 1.0f / without_unit<T>();
     const int64_t at = ((int64_t)blockIdx.y * a.queries.rows + q_row) * a.heads + head;
     if (lane == 0) a.stats[at] = make_float2(largest, total * unit);
 #pragma unroll
@@ -534,7 +536,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
         largest[t] = more;
         far |= far_scores(more);
       }
-      const float base = largest[t] == -kInfinity ? 0.0f : weight_unit<T>() - largest[t];
+      const float base = largest[t] == -kInfinity ? 0.0f : forward_unit<T>() - largest[t];
 #pragma unroll
       for (int tt = 0; tt < TT; ++tt)
 #pragma unroll
@@ -614,7 +616,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void prompt_forward(PromptAr
     store_column<T, F>(a.o, q0 + r, head, a.dim, o[t], total == 0.0f ? 0.0f : 1.0f / total);
     if (a.lse && g == 0)
       a.lse[(int64_t)head * a.queries.rows + q0 + r] =
-          total == 0.0f ? -kInfinity : (largest[t] - weight_unit<T>() + __builtin_amdgcn_logf(total)) * kLn2;
+          total == 0.0f ? -kInfinity : (largest[t] + __builtin_amdgcn_logf(total * without_unit<T>())) * kLn2;
   }
 }
 
@@ -924,7 +926,7 @@ template <class T> __global__ __launch_bounds__(kThreads) void prompt_join_forwa
   store_any(element<T>(a.o, row, head) + d, o);
   if (a.lse && d == 0)
     a.lse[(int64_t)head * a.queries.rows + row] =
-        total == 0.0f ? -kInfinity : (most - weight_unit<T>() + __builtin_amdgcn_logf(total)) * kLn2;
+        total == 0.0f ? -kInfinity : (most + __builtin_amdgcn_logf(total * without_unit<T>())) * kLn2;
 }
 
 // Sums of cut walks, in their order: four elements a thread.

@@ -502,3 +502,20 @@ def test_scores_of_any_size(sq, rows, keys, dtype, power, sign):
         assert ((out[i].cpu().double() - v[best].double()).abs() <= tol).all(), i
         want = score[best] + (score[:keys - rows + i + 1] == score[best]).double().sum().log()
         assert ((lse[:, i].cpu().double() - want).abs() <= 2.0 ** -21 * want.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,keys", [(40, 160), (3, 900), (300, 300)])
+def test_large_values(sq, rows, keys, dtype):
+    """Values whose sums leave binary32 where weights are more than 1, and stay within it where they are not."""
+    gen = torch.Generator().manual_seed(84)
+    q, k = torch.zeros(rows, 2, 64), torch.zeros(keys, 1, 64)
+    q[..., 0] = 8.0
+    k[..., 0] = torch.arange(keys)[:, None] // 32 * 0.75  # largest scores that rise by little with each tile
+    v = (1 + torch.rand(keys, 1, 64, generator=gen)) * 2.0 ** 120
+    q, k, v = (t.to(dtype) for t in (q, k, v))
+    ints = dict(dtype=torch.int32, device="cuda")
+    out, lse = sq.squant_attention(q.cuda(), k.cuda(), v.cuda(), torch.tensor([0, rows], **ints), torch.tensor([0, keys], **ints))
+    ref = attention64(q.double(), k.double(), v.double(), 0.125, True, dtype)
+    close(out, ref, "out")
+    close(lse, ref, "lse")
