@@ -378,7 +378,7 @@ int squant_cache_read(const squant_cache_t* h_cache, const squant_paged_t* h_whe
 
 /* out[r][h] = sum_t p[t] value[t],  p = softmax over t of scale * q[r][h] . key[t],  t the tokens up to the row's own
  * (which are in the cache already).  scale is finite and not negative.  For one or a few rows a sequence: 16 or 32 rows
- * times grouped heads share a pass over the cache.  The workspace is 128 MiB at most. */
+ * times grouped heads share a pass over the cache.  The workspace is about 128 MiB at most. */
 size_t squant_cache_attention_workspace_bytes(int64_t rows, int32_t heads, const squant_cache_t* h_cache,
                                               const squant_paged_t* h_where);
 int squant_cache_attention(const squant_heads_t* h_q, squant_wtype_t type, int64_t rows, int32_t heads,
