@@ -307,7 +307,7 @@ int squant_cross_entropy_backward(const void* d_h, int64_t ldh, squant_wtype_t t
  * Element type (squant_wtype_t): that of queries, keys, values, outputs and gradients of a call.  Over prompts products
  * are taken of the elements as they are and added in binary32, softmax statistics are binary32; what is multiplied by the
  * values (and, in a backward pass, by queries, keys and output gradients) is rounded to the element type first (binary32:
- * not).  Gradients take weights as exp(score - log-sum-exp), which makes them off by 2^-22 |log-sum-exp| (relative), however
+ * not).  Gradients take weights as exp(score - log-sum-exp), which makes them off by 2^-21 |log-sum-exp| (relative), however
  * large scores are.  Every output is rounded once.
  *
  * Over a cache matrix products are of binary16 numbers, with shared powers of two:
