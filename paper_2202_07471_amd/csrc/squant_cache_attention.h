@@ -419,7 +419,7 @@ __global__ __launch_bounds__(kThreads, cache_occupancy(NG, RT)) void cache_atten
   const Magic magic;
   // Tokens share exponents, and large scales cost small ones their bits.  What a row gets must not depend on tokens that it does not see:
   // `wide` where some row sees a token that another does not, with a scale more than 2^7 times all of those before (of this
-  // block, or met by the wave).  An element is otherwise off by at most 8 * 2^-25 (a code's product and its scale, both rounded next to 0)
+  // block, or met by the wave).  An element is otherwise off by at most 9 * 2^-25 (a code's product and its scale, both rounded next to 0)
   // where the largest that the row sees is at least 7 * 2^0: 2^-24 of it.
   bool wide = false;
 
